@@ -14,7 +14,8 @@
  * input inside the GEMM rather than written out.  A dispatcher picks one by measured input sparsity.
  *
  * Conventions shared by every entry point
- *   - All tensors are fp32 (indices int32/uint32), dense and row-major:
+ *   - All tensors are fp32 (indices int32/uint32), dense and row-major (the
+ *     feed-forward operators at the end have conventions of their own):
  *     input  x  N x C x H x W   (NCHW)
  *     filter w  K x C x R x S   (KCRS)
  *     output y  N x K x Ho x Wo (NCHW),
@@ -427,6 +428,171 @@ int isc_im2col(const isc_conv_desc *d, const float *x, float *col, int64_t ldc,
  * DEVICE, HIP. */
 int isc_gemm_f32(int32_t M, int32_t Ncols, int32_t Kd, const float *a, int64_t lda,
                  const float *b, int64_t ldb, float *c, int64_t ldc, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Operators of a rectified feed-forward block: the norm in front of it, the
+ * router to its experts, and its products on 4-bit weights, the second of
+ * which skips the zeros that the rectifier left, as the convolutions do.
+ *
+ * Conventions of this section, beside those above
+ *   - Tensors are rows of consecutive values; a leading dimension (elements,
+ *     at least the row's length) says how far apart rows are.  Element types
+ *     are isc_type values; sums are fp32 whatever the type, and a value is
+ *     rounded once, to nearest, where it is stored.  Pointers are aligned to
+ *     their element; rows that all start on 16 bytes are read 16 bytes at a
+ *     time, others value by value.
+ *   - T, the number of tokens, may be 0: such a call checks its arguments and
+ *     writes what does not depend on a token.
+ *   - An output that has an input's rows may be that very tensor (the same
+ *     pointer and leading dimension) where the call says so.
+ *   - A group scale is one byte b, 2^(b - 127); 255 is NaN.
+ */
+typedef enum isc_type {
+    ISC_F32 = 0,
+    ISC_F16 = 1,
+    ISC_BF16 = 2,
+    ISC_MX8 = 3 /* inputs of isc_w4_linear: 8-bit floats (4 exponent and 3
+                   mantissa bits, bias 7, largest 448, no infinity), a group
+                   scale for every 32 values of a row */
+} isc_type;
+
+/* h = x + r, y = h * rstd * w with rstd = (mean(h^2) + eps)^(-1/2), row by row.
+ *   T, D: rows and their length, D <= 65536.  type: of x, r, h and y; w_type:
+ *     of w.  r: the residual, or NULL (then h = x).
+ *   h, y, q with scales, rstd: outputs, each NULL where it is not wanted, one
+ *     at least given.  h and y are stored in `type`; y is computed from the
+ *     sum before its rounding.  h or y may be x or r in place.
+ *   q, scales: y in 8 bits, T x D values and T x ceil(D/32) group scales (row
+ *     strides ldq and lds bytes): a group's scale is the smallest power of two
+ *     that brings its largest magnitude to 448 or below; a group with a value
+ *     that is not finite has scale 255 and NaN values.
+ *   rstd: T floats, as isc_rmsnorm_bwd takes them.
+ * One launch.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_rmsnorm(int32_t T, int32_t D, int32_t type, const void *x, int64_t ldx, const void *r, int64_t ldr,
+                const void *w, int32_t w_type, float eps, void *h, int64_t ldh, void *y, int64_t ldy, void *q,
+                int64_t ldq, void *scales, int64_t lds, float *rstd, void *stream);
+
+/* Bytes of workspace of isc_rmsnorm_bwd.  Host-only.  Errors: NULL, SHAPE, LIMIT. */
+int isc_rmsnorm_bwd_workspace_size(int32_t T, int32_t D, size_t *bytes);
+
+/* The gradient of isc_rmsnorm: with n = h * rstd and g = dy * w,
+ *   dx = rstd * (g - n * mean(g * n)) + dh     (of x and of r alike)
+ *   dw = sum over rows of dy * n               (fp32, D values)
+ *   dy, h, dh, dx: T x D of `type`, D <= 16384.  dh: the gradient that reaches
+ *     h past the norm (the residual stream's), or NULL.  dx may be dy, h or dh
+ *     in place.  ws: isc_rmsnorm_bwd_workspace_size bytes, 256-byte aligned.
+ * Two launches: workgroups walk rows and keep their columns' sums, which are
+ * then added in order.  Deterministic.
+ * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_rmsnorm_bwd(int32_t T, int32_t D, int32_t type, const void *dy, int64_t ldy, const void *h, int64_t ldh,
+                    const void *w, int32_t w_type, const float *rstd, const void *dh, int64_t ldd, void *dx,
+                    int64_t ldx, float *dw, void *ws, size_t ws_bytes, void *stream);
+
+typedef enum isc_score {
+    ISC_SCORE_SOFTMAX = 0, /* over all experts of a token */
+    ISC_SCORE_SIGMOID = 1
+} isc_score;
+
+/* Bytes of workspace of isc_route (0 up to 64 tokens).  Host-only.
+ * Errors: NULL, SHAPE, LIMIT. */
+int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes);
+
+/* Routes T tokens to k of E experts each (E <= 1024, k <= 64).
+ *   logits: T x E of `type`.  s = softmax or sigmoid of a token's logits;
+ *   bias: E floats added to s for the choice only (NULL: none).
+ *   groups: the experts fall into that many groups of E/groups consecutive
+ *     ones (at most 64), of which the keep_groups with the largest sums of
+ *     their two largest s + bias stay in the choice.
+ *   The k experts with the largest s + bias are chosen, in that order, ties to
+ *   the lowest index, among groups too.  An expert whose logit or s + bias is
+ *   -inf or NaN is never chosen; a token with fewer than k others has id -1
+ *   and weight 0 in its last slots.
+ *   ids, weights: T x k; weights = scale * s, divided by (the chosen s's sum +
+ *     1e-20) if renorm.
+ *   offsets, order: E + 1 and T x k, or both NULL: the pairs t*k + j by expert,
+ *     in order within one; expert e has order[offsets[e] .. offsets[e+1]).
+ *     Entries from offsets[E] on are -1.
+ *   ws: isc_route_workspace_size bytes, 256-byte aligned (unused without lists).
+ * One launch up to 64 tokens, else two.
+ * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_route(int32_t T, int32_t E, int32_t k, int32_t type, const void *logits, int64_t ld, const float *bias,
+              int32_t score, int32_t groups, int32_t keep_groups, int32_t renorm, float scale, int32_t *ids,
+              float *weights, int32_t *offsets, int32_t *order, void *ws, size_t ws_bytes, void *stream);
+
+/* The gradient of isc_route's weights to its logits (the choice itself has
+ * none): dweights T x k, ids as isc_route gave them (all different within a
+ * token; an id outside [0, E) is an empty slot), score, renorm and scale as
+ * there.  dlogits: T x E of `type`, fully written; may be logits in place.
+ * One launch.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_route_bwd(int32_t T, int32_t E, int32_t k, int32_t type, const float *dweights, const void *logits, int64_t ld,
+                  const int32_t *ids, int32_t score, int32_t renorm, float scale, void *dlogits, int64_t ldd,
+                  void *stream);
+
+/* E matrices of 4-bit weights, N outputs x K inputs each.  A weight is a code
+ * (a sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ * times its group's scale; a group is 32 inputs of an output.  Plain form:
+ * codes E x N x ceil(K/2) bytes, the even input's in the low half; scales
+ * E x N x ceil(K/32) bytes.  The products read one of two layouts of them. */
+typedef enum isc_w4_layout {
+    ISC_W4_TILES = 0, /* matrix operands, for isc_w4_linear */
+    ISC_W4_ROWS = 1   /* one input's weights contiguous, for isc_w4_skip */
+} isc_w4_layout;
+
+typedef struct isc_w4_desc {
+    int32_t E, N, K; /* E <= 1024, N and K <= 2^24, N * K about 2^36 at most */
+    int32_t layout;  /* isc_w4_layout */
+} isc_w4_desc;
+
+/* Bytes of the packed weights.  Host-only.  Errors: NULL, SHAPE, LIMIT, ARG. */
+int isc_w4_size(const isc_w4_desc *d, size_t *bytes);
+
+/* Plain codes and scales of E*N rows of K weights (leading dimension ld): a
+ * group's scale is the smallest power of two that brings its largest magnitude
+ * to 6 or below, codes to nearest, ties to even.  A group with a weight that
+ * is not finite has scale 255.
+ * Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_w4_quantize(const isc_w4_desc *d, const void *w, int32_t type, int64_t ld, uint8_t *codes, uint8_t *scales,
+                    void *stream);
+
+/* The packed weights (isc_w4_size bytes, 256-byte aligned) from their plain
+ * form.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_w4_pack_codes(const isc_w4_desc *d, const uint8_t *codes, const uint8_t *scales, void *packed, void *stream);
+
+/* y[t][n] = sum over k of w[n][k] * x[t][k], with max(0, .) if relu (a NaN
+ * stays), on the matrix cores; weights in the layout ISC_W4_TILES.
+ *   x: T x K (T <= 2^20) of any isc_type; x_scales: an ISC_MX8 x's group scales
+ *     (row stride ld_scales bytes), else NULL.  fp16 and fp32 inputs enter the
+ *     products in full, as sums of bfloat16 values.
+ *   slots: 0 for one matrix (E = 1; ids, offsets, order unused), else the
+ *     experts per token: pair p = t*slots + j gets row p of y from expert
+ *     ids[p], by isc_route's ids, offsets and order; rows of pairs with an id
+ *     outside [0, E) are 0.
+ *   y: T x N, or T*slots x N, of y_type (ISC_F32, ISC_F16, ISC_BF16).
+ * One launch, no workspace.  Deterministic.
+ * Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const void *x, int32_t x_type, int64_t ldx,
+                  const void *x_scales, int64_t ld_scales, int32_t slots, const int32_t *ids, const int32_t *offsets,
+                  const int32_t *order, void *y, int32_t y_type, int64_t ldy, int32_t relu, void *stream);
+
+/* Bytes of workspace of isc_w4_skip.  Host-only.
+ * Errors: NULL, SHAPE, LIMIT, ARG. */
+int isc_w4_skip_workspace_size(const isc_w4_desc *d, int32_t T, int32_t slots, size_t *bytes);
+
+/* The same product for a rectified x, whose zeros are skipped: an input of 0
+ * adds nothing, whatever its weights, and its weights are not read (layout
+ * ISC_W4_ROWS).
+ *   slots 0: x is T x K, y = w x, E = 1.
+ *   slots > 0: x is T*slots x K (isc_w4_linear's y), and y[t] = sum over j of
+ *     weights[t][j] * w_e x[t][j], e = ids[t][j]; a slot with an id outside
+ *     [0, E) adds nothing.
+ *   x_type, y_type: ISC_F32, ISC_F16 or ISC_BF16.  y: T x N.
+ *   ws: isc_w4_skip_workspace_size bytes, 256-byte aligned.
+ * One launch, and a second that adds ranges of the inputs up where there are
+ * several.  Deterministic.
+ * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_w4_skip(const isc_w4_desc *d, const void *packed, int32_t T, const void *x, int32_t x_type, int64_t ldx,
+                int32_t slots, const int32_t *ids, const float *weights, void *y, int32_t y_type, int64_t ldy, void *ws,
+                size_t ws_bytes, void *stream);
 
 /* Short text for a status code (static storage). */
 const char *isc_status_str(int status);

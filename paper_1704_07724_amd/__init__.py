@@ -14,6 +14,9 @@ The functions carry the C names:
     isc_sparse_conv, isc_sparse_conv_fused, isc_sparse_kernel, isc_sparse_plan,
     isc_crossover_sparsity,
     isc_im2col, isc_gemm_f32, isc_status_str, isc_version
+and, for a rectified feed-forward block (ffn.py, imported here):
+    isc_rmsnorm, isc_rmsnorm_bwd, isc_route, isc_route_bwd,
+    isc_w4_quantize, isc_w4_pack_codes, isc_w4_linear, isc_w4_skip
 
 Defaults a user may set in the environment (read here, by the binding, at
 each call; the C library reads no environment): ISC_PATH = auto | sparse |
@@ -49,6 +52,10 @@ EXPORTS = ("isc_out_shape", "isc_workspace_size", "isc_conv2d", "isc_conv2d_tune
            "isc_im2col", "isc_gemm_f32", "isc_sparse_conv_fused", "isc_sparse_kernel",
            "isc_census_size", "isc_conv2d_relu", "isc_census_read",
            "isc_conv2d_dw_workspace_size", "isc_conv2d_dw",
+           "isc_rmsnorm", "isc_rmsnorm_bwd_workspace_size", "isc_rmsnorm_bwd",
+           "isc_route_workspace_size", "isc_route", "isc_route_bwd",
+           "isc_w4_size", "isc_w4_quantize", "isc_w4_pack_codes", "isc_w4_linear",
+           "isc_w4_skip_workspace_size", "isc_w4_skip",
            "isc_status_str", "isc_version")
 
 
@@ -142,6 +149,7 @@ def lib():
     L.isc_census_read.argtypes = [vp, sz, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64), vp]
     L.isc_conv2d_dw_workspace_size.argtypes = [dp, ctypes.POINTER(sz)]
     L.isc_conv2d_dw.argtypes = [dp, vp, vp, vp, vp, sz, tp, vp]
+    ffn.declare(L)
     for name in EXPORTS[:-2]:
         getattr(L, name).restype = ctypes.c_int
     L.isc_status_str.argtypes = [ctypes.c_int]
@@ -604,3 +612,8 @@ def _gemm(torch, a, b, out, stream):
     _check(lib().isc_gemm_f32(M, N, Kd, a.data_ptr(), Kd, b.data_ptr(), N, out.data_ptr(), N,
                               _stream(stream)), "isc_gemm_f32")
     return out
+
+
+from . import ffn  # noqa: E402  (its functions use the helpers above)
+from .ffn import (Mx8, Norm, Route, W4, W4Desc, isc_rmsnorm, isc_rmsnorm_bwd, isc_route,  # noqa: E402,F401
+                  isc_route_bwd, isc_w4_linear, isc_w4_pack_codes, isc_w4_quantize, isc_w4_skip)

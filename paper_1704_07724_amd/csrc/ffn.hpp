@@ -1,0 +1,257 @@
+// Shared by the feed-forward operators (norm, routing, products on 4-bit
+// weights): element types, wavefront reductions, the 8-bit and 4-bit group
+// formats, and the launchers behind the C entry points in ffn_api.hip.
+#pragma once
+
+#include "isc_internal.hpp"
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+
+namespace isc {
+
+// --- element types ----------------------------------------------------------
+
+struct F32 {
+    using type = float;
+    static __device__ __forceinline__ float load(const float *p) { return *p; }
+    static __device__ __forceinline__ float round(float v) { return v; }
+};
+struct F16 {
+    using type = uint16_t;
+    static __device__ __forceinline__ float widen(uint32_t b) {
+        return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(b)));
+    }
+    static __device__ __forceinline__ uint32_t narrow(float v) {
+        return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
+    }
+    static __device__ __forceinline__ float load(const uint16_t *p) { return widen(*p); }
+};
+struct BF16 {
+    using type = uint16_t;
+    static __device__ __forceinline__ float widen(uint32_t b) { return __uint_as_float(b << 16); }
+    // to nearest, ties to even; a NaN stays one (the compiler's conversion)
+    static __device__ __forceinline__ uint32_t narrow(float v) {
+        return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+    }
+    static __device__ __forceinline__ float load(const uint16_t *p) { return widen(*p); }
+};
+
+template <class T>
+__device__ __forceinline__ void store(typename T::type *p, float v) {
+    if constexpr (sizeof(typename T::type) == 4)
+        *p = v;
+    else
+        *p = static_cast<uint16_t>(T::narrow(v));
+}
+
+// One value of a type known at run time.
+__device__ __forceinline__ float load_as(const void *p, int64_t i, int type) {
+    if (type == ISC_F32) return static_cast<const float *>(p)[i];
+    const uint32_t b = static_cast<const uint16_t *>(p)[i];
+    return type == ISC_BF16 ? BF16::widen(b) : F16::widen(b);
+}
+__device__ __forceinline__ void store_as(void *p, int64_t i, float v, int type) {
+    if (type == ISC_F32)
+        static_cast<float *>(p)[i] = v;
+    else
+        static_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(type == ISC_BF16 ? BF16::narrow(v) : F16::narrow(v));
+}
+
+// Eight consecutive values: one or two 16-byte accesses where the caller
+// knows the address to be 16-byte aligned and all eight to be there
+// (`whole`), else one access each for the first `n`.
+template <class T>
+__device__ __forceinline__ void load8(float (&v)[8], const typename T::type *p, int n, bool whole) {
+    if (whole) {
+        if constexpr (sizeof(typename T::type) == 4) {
+            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = *reinterpret_cast<const uint4 *>(p);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = T::widen(w[i] & 0xffffu);
+                v[2 * i + 1] = T::widen(w[i] >> 16);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? T::load(p + i) : 0.0f;
+}
+template <class T>
+__device__ __forceinline__ void store8(typename T::type *p, const float (&v)[8], int n, bool whole) {
+    if (whole) {
+        if constexpr (sizeof(typename T::type) == 4) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = T::narrow(v[2 * i]) | T::narrow(v[2 * i + 1]) << 16;
+            *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) store<T>(p + i, v[i]);
+}
+
+// --- wavefront reductions by data-parallel moves ----------------------------
+// Each step takes the other operand from a lane of the same row of 16, then
+// from the row before, so no LDS round trip is paid; every lane gets lane
+// 63's total.
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t v) {
+    return static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(static_cast<int>(old), static_cast<int>(v), CTRL, ROWS, 0xf, false));
+}
+#define ISC_WAVE_REDUCE(v, ident, op)                              \
+    v = op(v, dpp<0x111, 0xf>(ident, v)); /* row_shr:1 */          \
+    v = op(v, dpp<0x112, 0xf>(ident, v)); /* row_shr:2 */          \
+    v = op(v, dpp<0x114, 0xf>(ident, v)); /* row_shr:4 */          \
+    v = op(v, dpp<0x118, 0xf>(ident, v)); /* row_shr:8 */          \
+    v = op(v, dpp<0x142, 0xa>(ident, v)); /* row_bcast:15 */       \
+    v = op(v, dpp<0x143, 0xc>(ident, v)); /* row_bcast:31 */       \
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63))
+
+__device__ __forceinline__ uint32_t op_max(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t op_min(uint32_t a, uint32_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint32_t op_sum(uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) { ISC_WAVE_REDUCE(v, 0u, op_max); }
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) { ISC_WAVE_REDUCE(v, 0xffffffffu, op_min); }
+__device__ __forceinline__ uint32_t wave_sum_bits(uint32_t v) { ISC_WAVE_REDUCE(v, 0u, op_sum); }
+#undef ISC_WAVE_REDUCE
+__device__ __forceinline__ float wave_sum(float v) { return __uint_as_float(wave_sum_bits(__float_as_uint(v))); }
+
+// An unsigned order of floats: a > b as numbers exactly when order(a) > order(b)
+// (NaN aside; -0 orders below +0, so a caller ranks v + 0.0f).
+__device__ __forceinline__ uint32_t order(float v) {
+    const uint32_t b = __float_as_uint(v);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unorder(uint32_t o) {
+    return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+
+// --- group formats ----------------------------------------------------------
+// A scale is one byte b and stands for 2^(b - 127); 255 stands for NaN.
+
+__device__ __forceinline__ float scale_value(uint32_t b) {
+    return __uint_as_float(b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
+}
+// The scale byte of a group whose largest magnitude has the bits `abits`:
+// the smallest power of two that brings it to `top` or below, where
+// top = (1 + TOPM / 2^23) 2^TOPE.  255 where the magnitude is not finite.
+template <int TOPE, uint32_t TOPM>
+__device__ __forceinline__ uint32_t group_scale(uint32_t abits) {
+    if (abits >= 0x7f800000u) return 255u;
+    const int e = static_cast<int>(abits >> 23) - TOPE + ((abits & 0x7fffffu) > TOPM ? 1 : 0);
+    return static_cast<uint32_t>(e > 0 ? e : 0);
+}
+
+// --- launchers --------------------------------------------------------------
+
+struct NormArgs {
+    const void *x, *r, *w;      // r: nullptr without a residual
+    void *h, *y, *q, *scales;   // each nullptr where it is not asked for
+    float *rstd;
+    int64_t ldx, ldr, ldh, ldy, ldq, lds;
+    int T, D, type, wtype;
+    float eps;
+    bool whole;  // every row 16-byte aligned and D a multiple of 8
+};
+hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t s);
+
+struct NormBwdArgs {
+    const void *dy, *h, *w, *dh;  // dh: nullptr without a second gradient
+    const float *rstd;
+    void *dx;
+    float *dw, *part;  // part: norm_bwd_blocks() rows of D sums
+    int64_t ldy, ldh, ldd, ldx;
+    int T, D, type, wtype;
+    bool whole;
+};
+int norm_bwd_blocks(int T, int D);
+hipError_t launch_rmsnorm_bwd(const NormBwdArgs &a, hipStream_t s);
+
+struct RouteArgs {
+    const void *logits;
+    const float *bias;  // nullptr: none
+    int64_t ld;
+    int T, E, k, type, sigmoid, groups, keep, renorm;
+    float scale;
+    int32_t *ids;
+    float *weights;
+    int32_t *offsets, *order;  // both nullptr where the lists are not asked for
+    uint16_t *counts;          // route_blocks() rows of E counts
+};
+int route_blocks(int T);
+hipError_t launch_route(const RouteArgs &a, hipStream_t s);
+
+struct RouteBwdArgs {
+    const float *dweights;
+    const void *logits;
+    const int32_t *ids;
+    void *dlogits;
+    int64_t ld, ldd;
+    int T, E, k, type, sigmoid, renorm;
+    float scale;
+};
+hipError_t launch_route_bwd(const RouteBwdArgs &a, hipStream_t s);
+
+// 4-bit weights of E matrices N x K in one of two layouts.
+//   tiles: for every 16 outputs and 128 inputs one KiB, lane l of a wavefront
+//     owning 16 bytes: output l % 16, inputs 32 (l / 16) .. + 32, in order; so
+//     a lane's load is a matrix operand.  The scales of four such steps follow
+//     each other in a word per lane, after all codes of the matrix.
+//   rows: for every 32 inputs the outputs' scales (Np bytes), then 32 rows of
+//     Np / 2 bytes, one per input, outputs in order (Np: N up to 128s); so the
+//     weights of one input are contiguous, as the convolution's filters are.
+struct W4Shape {
+    int E, N, K;
+    __host__ __device__ int64_t tiles() const { return (N + 15) / 16; }
+    __host__ __device__ int64_t steps() const { return (K + 127) / 128; }
+    __host__ __device__ int64_t units() const { return (K + 511) / 512; }
+    __host__ __device__ int64_t tile_codes() const { return tiles() * steps() * 1024; }
+    __host__ __device__ int64_t tile_bytes() const { return tile_codes() + tiles() * units() * 256; }
+    __host__ __device__ int64_t np() const { return (N + 127) / 128 * 128; }
+    __host__ __device__ int64_t groups() const { return (K + 31) / 32; }
+    __host__ __device__ int64_t row_bytes() const { return groups() * 17 * np(); }
+    int64_t bytes(int layout) const { return E * (layout == ISC_W4_TILES ? tile_bytes() : row_bytes()); }
+};
+hipError_t launch_w4_quantize(const W4Shape &w, const void *src, int type, int64_t ld, uint8_t *codes,
+                              uint8_t *scales, hipStream_t s);
+hipError_t launch_w4_pack(const W4Shape &w, int layout, const uint8_t *codes, const uint8_t *scales, uint8_t *packed,
+                          hipStream_t s);
+
+struct W4Args {
+    W4Shape w;
+    const uint8_t *packed;
+    const void *x;
+    const uint8_t *xs;  // the scales of an 8-bit x
+    int64_t ldx, ldxs, ldy;
+    int T, slots, xtype, ytype, relu;  // slots 0: one matrix, no experts
+    const int32_t *ids, *offsets, *order;
+    const float *weights;
+    void *y;
+    float *part;
+    bool whole;  // every row of x 16-byte aligned
+};
+hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);
+// Ranges that the skipping product's inputs are cut into (each a row of sums
+// in `part` where there are several).
+int w4_skip_ranges(const W4Shape &w, int T, int slots);
+hipError_t launch_w4_skip(const W4Args &a, hipStream_t s);
+
+// The current device's check of the C entry points (isc_api.hip).
+int require_gfx950();
+
+}  // namespace isc

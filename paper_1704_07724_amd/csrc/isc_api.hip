@@ -1,4 +1,4 @@
-// C ABI of the library (include/isc.h): argument validation on the host,
+// C ABI of the convolutions (include/isc.h): argument validation on the host,
 // workspace layout, and the launch sequences of the sparse path (ISC steps
 // 1-3), the dense path (Fig. 3) and the dispatcher between them.
 #include "isc.h"
@@ -13,6 +13,7 @@
 
 namespace isc {
 bool sparse_conv_feasible(const SparseShape &sh);
+int require_gfx950();
 }
 
 namespace {
@@ -366,6 +367,10 @@ int conv_impl(const isc_conv_desc *d, const float *x, const float *w, float *y, 
 }
 
 }  // namespace
+
+namespace isc {
+int require_gfx950() { return check_device(); }
+}  // namespace isc
 
 extern "C" {
 

@@ -1,0 +1,369 @@
+// Routing of tokens to experts, and its gradient.
+//
+//   s = softmax(l) or 1 / (1 + exp(-l)),  key = s + bias
+//   a group's key: the sum of its two largest keys; the best groups stay
+//   the k largest keys of those, ties to the lowest index
+//   w_j = scale s_j / (sum of the chosen s + 1e-20), or scale s_j
+//
+// An expert whose logit (or key) is -inf or NaN is never chosen; a token with
+// fewer than k experts left gets id -1 and weight 0 in its last slots.
+//
+// One wavefront per token, E / 64 experts a lane: the keys stay in registers
+// as unsigned integers in the floats' order, a slot is one wavefront maximum
+// by data-parallel moves, a ballot finds its lane.
+//
+// The experts' lists.  A token meets an expert at most once, so 64 tokens and
+// an expert make one 64-bit word: a pair's place among its expert's pairs is
+// the number of bits below its token's, whatever order the bits were set in.
+// Workgroups of 64 tokens leave their counts; a second launch adds up the
+// counts of the workgroups before, and the experts' totals, and places pairs.
+#include "ffn.hpp"
+
+#include <atomic>
+
+namespace isc {
+namespace {
+
+constexpr int kTokens = 64;   // tokens per workgroup: the bits of a word
+constexpr int kWaves = 16;    // wavefronts per workgroup
+constexpr int kMaxE = 1024;   // experts, and threads of a workgroup
+
+__device__ __forceinline__ float token_logit(const RouteArgs &a, int64_t t, int e) {
+    return load_as(a.logits, t * a.ld + e, a.type);
+}
+
+// A token's scores from its logits (64 experts a step of i, lane the lowest
+// part of the index); logits that are not above -inf score 0.  A logit of
+// +inf stands for all others' limit: it shares the softmax with its equals.
+template <int C>
+__device__ __forceinline__ void scores(const float (&l)[C], float (&s)[C], int sigmoid) {
+    if (sigmoid) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) s[i] = l[i] > -__builtin_inff() ? 1.0f / (1.0f + expf(-l[i])) : 0.0f;
+        return;
+    }
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+        if (l[i] > -__builtin_inff()) mx = op_max(mx, order(l[i]));
+    mx = wave_max(mx);
+    const float m = mx ? unorder(mx) : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        s[i] = l[i] > -__builtin_inff() ? (l[i] == m ? 1.0f : expf(l[i] - m)) : 0.0f;
+        sum += s[i];
+    }
+    sum = wave_sum(sum);
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) s[i] *= inv;
+}
+
+// One token by the calling wavefront; `row` is LDS of E words of its own
+// (used with groups only).  Lane j < k returns slot j's expert, or -1.
+template <int C>
+__device__ __forceinline__ int route_token(const RouteArgs &a, int64_t t, uint32_t *row) {
+    const int lane = threadIdx.x & 63;
+    float l[C], s[C];
+    uint32_t key[C];  // 0: not to be chosen
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int e = i * 64 + lane;
+        l[i] = e < a.E ? token_logit(a, t, e) : -__builtin_inff();
+    }
+    scores<C>(l, s, a.sigmoid);
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int e = i * 64 + lane;
+        const float v = e < a.E && a.bias ? s[i] + a.bias[e] : s[i];
+        key[i] = l[i] > -__builtin_inff() && v > -__builtin_inff() ? order(v + 0.0f) : 0u;
+    }
+    if (a.groups > 1) {
+        const int size = a.E / a.groups;
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (i * 64 + lane < a.E) row[i * 64 + lane] = key[i];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        uint32_t g = 0;  // lane g's group; 0: none of its experts can be chosen
+        if (lane < a.groups) {
+            uint32_t best = 0, second = 0;
+            for (int e = lane * size; e < (lane + 1) * size; ++e) {
+                const uint32_t v = row[e];
+                second = op_max(second, op_min(best, v));
+                best = op_max(best, v);
+            }
+            if (best) g = order(unorder(best) + (second ? unorder(second) : 0.0f) + 0.0f);
+        }
+        int before = 0;  // groups ranked before the lane's
+        for (int j = 0; j < a.groups; ++j) {
+            const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(g), j));
+            before += v > g || (v == g && j < lane);
+        }
+        const unsigned long long kept = __ballot(lane < a.groups && g && before < a.keep);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int e = i * 64 + lane;
+            if (e < a.E && !(kept >> (e / size) & 1)) key[i] = 0u;
+        }
+    }
+    int id = -1;
+    float w = 0.0f;
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t best = key[0];
+        int at = 0;
+#pragma unroll
+        for (int i = 1; i < C; ++i)
+            if (key[i] > best) best = key[i], at = i;
+        const uint32_t top = wave_max(best);
+        if (top == 0u) break;
+        const unsigned long long tied = __ballot(best == top);
+        int e = at * 64 + lane;
+        if (tied & (tied - 1))  // equal keys in several lanes: the lowest index
+            e = static_cast<int>(wave_min(best == top ? static_cast<uint32_t>(e) : 0xffffffffu));
+        else
+            e = __builtin_amdgcn_readlane(e, __builtin_ctzll(tied));
+        float score = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (i == e >> 6) {
+                score = s[i];
+                if (lane == (e & 63)) key[i] = 0u;
+            }
+        score = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(score), e & 63));
+        if (lane == j) id = e, w = score;
+    }
+    if (a.renorm) w = w / (wave_sum(w) + 1e-20f);
+    if (lane < a.k) {
+        a.ids[t * a.k + lane] = id;
+        a.weights[t * a.k + lane] = w * a.scale;
+    }
+    return id;
+}
+
+// Exclusive sum of one value per thread over the workgroup of kMaxE threads.
+__device__ __forceinline__ int block_scan(int v, int *sums) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int in = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(in, d);
+        if (lane >= d) in += u;
+    }
+    if (lane == 63) sums[wave] = in;
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < wave; ++i) before += sums[i];
+    return before + in - v;
+}
+
+// Routes 64 tokens a workgroup.  ONE: there is one workgroup, which also
+// writes the lists; else it leaves its counts for place_kernel.
+template <int C, bool ONE>
+__global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
+    extern __shared__ uint32_t rows[];  // kWaves rows of E words, with groups
+    __shared__ unsigned long long bits[kMaxE];
+    __shared__ int base[kMaxE], sums[kWaves], total;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool lists = a.order != nullptr;
+    if (lists) {
+        bits[threadIdx.x] = 0ull;
+        __syncthreads();
+    }
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens;
+    int id[kTokens / kWaves];
+#pragma unroll
+    for (int i = 0; i < kTokens / kWaves; ++i) {
+        const int64_t t = t0 + i * kWaves + wave;
+        id[i] = -1;
+        if (t >= a.T) continue;
+        id[i] = route_token<C>(a, t, rows + wave * a.E);
+        if (lists && id[i] >= 0) atomicOr(&bits[id[i]], 1ull << (i * kWaves + wave));
+    }
+    if (!lists) return;
+    __syncthreads();
+    const int e = threadIdx.x;
+    const int count = e < a.E ? __popcll(bits[e]) : 0;
+    if constexpr (!ONE) {
+        if (e < a.E) a.counts[static_cast<int64_t>(blockIdx.x) * a.E + e] = static_cast<uint16_t>(count);
+        return;
+    }
+    base[e] = block_scan(count, sums);
+    if (e < a.E) a.offsets[e] = base[e];
+    if (e == kMaxE - 1) {
+        total = base[e] + count;
+        a.offsets[a.E] = total;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTokens / kWaves; ++i) {
+        const int t = i * kWaves + wave;
+        if (id[i] >= 0)
+            a.order[base[id[i]] + __popcll(bits[id[i]] & ((1ull << t) - 1))] = t * a.k + lane;
+    }
+    for (int p = total + static_cast<int>(threadIdx.x); p < a.T * a.k; p += kMaxE) a.order[p] = -1;
+}
+
+// The lists of several workgroups' tokens.
+__global__ void __launch_bounds__(kMaxE) place_kernel(RouteArgs a) {
+    __shared__ unsigned long long bits[kMaxE];
+    __shared__ int base[kMaxE], all[kMaxE], sums[kWaves], total;
+    const int nb = (a.T + kTokens - 1) / kTokens;
+    const int b = blockIdx.x;
+    bits[threadIdx.x] = 0ull;
+    base[threadIdx.x] = all[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t p0 = static_cast<int64_t>(b) * kTokens * a.k;
+    const int64_t left = static_cast<int64_t>(a.T) * a.k - p0;
+    const int pairs = static_cast<int>(left < kTokens * a.k ? left : kTokens * a.k);
+    for (int p = threadIdx.x; p < pairs; p += kMaxE) {
+        const int id = a.ids[p0 + p];
+        if (id >= 0) atomicOr(&bits[id], 1ull << (p / a.k));
+    }
+    // threads share the counts: each an expert and every `step`-th workgroup
+    // (integer sums: any order gives the same)
+    const int step = kMaxE / a.E;
+    if (static_cast<int>(threadIdx.x) < step * a.E) {
+        const int e = threadIdx.x % a.E;
+        int before = 0, n = 0;
+        for (int i = threadIdx.x / a.E; i < nb; i += step) {
+            const int c = a.counts[static_cast<int64_t>(i) * a.E + e];
+            n += c;
+            if (i < b) before += c;
+        }
+        atomicAdd(&all[e], n);
+        atomicAdd(&base[e], before);
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    const int n = all[e];
+    const int start = block_scan(n, sums);
+    base[e] += start;
+    if (b == 0 && e < a.E) a.offsets[e] = start;
+    if (e == kMaxE - 1) {
+        total = start + n;
+        if (b == 0) a.offsets[a.E] = total;
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < pairs; p += kMaxE) {
+        const int id = a.ids[p0 + p];
+        if (id >= 0)
+            a.order[base[id] + __popcll(bits[id] & ((1ull << (p / a.k)) - 1))] = static_cast<int>(p0) + p;
+    }
+    // the unused tail, spread over the workgroups
+    for (int64_t p = total + static_cast<int64_t>(b) * kMaxE + threadIdx.x; p < static_cast<int64_t>(a.T) * a.k;
+         p += static_cast<int64_t>(nb) * kMaxE)
+        a.order[p] = -1;
+}
+
+// dlogits of four tokens a workgroup, one wavefront each.
+template <int C>
+__global__ void __launch_bounds__(256) route_bwd_kernel(RouteBwdArgs a) {
+    extern __shared__ float grad[];  // four rows of E: the chosen scores' gradients
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    if (t >= a.T) return;
+    float *row = grad + wave * a.E;
+    float l[C], s[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int e = i * 64 + lane;
+        l[i] = e < a.E ? load_as(a.logits, t * a.ld + e, a.type) : -__builtin_inff();
+        if (e < a.E) row[e] = 0.0f;
+    }
+    int id = lane < a.k ? a.ids[t * a.k + lane] : -1;
+    if (id >= a.E) id = -1;
+    float dw = id >= 0 ? a.dweights[t * a.k + lane] * a.scale : 0.0f;
+    scores<C>(l, s, a.sigmoid);
+    float chosen = 0.0f;  // slot `lane`'s score, from the lane that holds it
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const float v = __shfl(s[i], id & 63);
+        if (id >= 0 && id >> 6 == i) chosen = v;
+    }
+    float ds = dw;
+    if (a.renorm) {
+        const float total = wave_sum(chosen) + 1e-20f;
+        ds = (dw - wave_sum(dw * chosen) / total) / total;
+    }
+    if (id < 0) ds = 0.0f;
+    const float dot = a.sigmoid ? 0.0f : wave_sum(ds * chosen);
+    __builtin_amdgcn_wave_barrier();
+    if (id >= 0) row[id] = ds;  // an expert of its own for every lane
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int e = i * 64 + lane;
+        if (e >= a.E) continue;
+        const float d = row[e];
+        const float v = a.sigmoid ? d * s[i] * (1.0f - s[i]) : s[i] * (d - dot);
+        store_as(a.dlogits, t * a.ldd + e, v, a.type);
+    }
+}
+
+// Grants a kernel the most dynamic LDS a call can ask for, once.
+template <typename Kern>
+hipError_t grant_lds(Kern kern, std::atomic<bool> &granted, size_t asked) {
+    if (asked <= 32 * 1024 || granted.load(std::memory_order_acquire)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(sizeof(uint32_t)) * kWaves * kMaxE);
+    if (e == hipSuccess) granted.store(true, std::memory_order_release);
+    return e;
+}
+
+template <int C>
+hipError_t route_of(const RouteArgs &a, hipStream_t s) {
+    const int nb = route_blocks(a.T);
+    const size_t lds = a.groups > 1 ? sizeof(uint32_t) * kWaves * static_cast<size_t>(a.E) : 0;
+    const dim3 grid(static_cast<unsigned>(nb)), block(kMaxE);
+    if (nb == 1) {
+        static std::atomic<bool> granted{false};
+        if (const hipError_t e = grant_lds(route_kernel<C, true>, granted, lds); e != hipSuccess) return e;
+        route_kernel<C, true><<<grid, block, lds, s>>>(a);
+        return hipGetLastError();
+    }
+    static std::atomic<bool> granted{false};
+    hipError_t e = grant_lds(route_kernel<C, false>, granted, lds);
+    if (e != hipSuccess) return e;
+    route_kernel<C, false><<<grid, block, lds, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess || !a.order) return e;
+    place_kernel<<<grid, block, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int C>
+hipError_t route_bwd_of(const RouteBwdArgs &a, hipStream_t s) {
+    const size_t lds = sizeof(float) * 4 * static_cast<size_t>(a.E);
+    route_bwd_kernel<C><<<dim3(static_cast<unsigned>((static_cast<int64_t>(a.T) + 3) / 4)), dim3(256), lds, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int route_blocks(int T) { return T > kTokens ? (T + kTokens - 1) / kTokens : 1; }
+
+hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
+    const int c = (a.E + 63) / 64;
+    return c <= 1 ? route_of<1>(a, s)
+           : c <= 2 ? route_of<2>(a, s)
+           : c <= 4 ? route_of<4>(a, s)
+           : c <= 8 ? route_of<8>(a, s)
+                    : route_of<16>(a, s);
+}
+
+hipError_t launch_route_bwd(const RouteBwdArgs &a, hipStream_t s) {
+    const int c = (a.E + 63) / 64;
+    return c <= 1 ? route_bwd_of<1>(a, s)
+           : c <= 2 ? route_bwd_of<2>(a, s)
+           : c <= 4 ? route_bwd_of<4>(a, s)
+           : c <= 8 ? route_bwd_of<8>(a, s)
+                    : route_bwd_of<16>(a, s);
+}
+
+}  // namespace isc

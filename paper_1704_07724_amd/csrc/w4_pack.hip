@@ -1,0 +1,137 @@
+// 4-bit weights: quantisation of fp32, fp16 or bf16 weights, and the two
+// layouts that the products read (W4Shape).
+//
+// A code is a sign, two exponent bits and one mantissa bit (0, 0.5, 1, 1.5, 2,
+// 3, 4, 6); 32 codes along an output's inputs share a power-of-two scale.
+// Plain form: two codes a byte, the even input's in the low half, each output's
+// row of ceil(K / 2) bytes after the other; scales ceil(K / 32) bytes a row.
+#include "ffn.hpp"
+
+namespace isc {
+namespace {
+
+// One thread per group of 32 weights.
+__global__ void __launch_bounds__(256) w4_quantize_kernel(const void *src, int type, int64_t ld, int64_t rows, int K,
+                                                          uint8_t *codes, uint8_t *scales) {
+    const int groups = (K + 31) / 32;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (item >= rows * groups) return;
+    const int64_t row = item / groups;
+    const int g = static_cast<int>(item % groups);
+    const int n = K - g * 32 < 32 ? K - g * 32 : 32;
+    uint32_t m = 0;
+    for (int i = 0; i < n; ++i)
+        m = op_max(m, __float_as_uint(load_as(src, row * ld + g * 32 + i, type)) & 0x7fffffffu);
+    const uint32_t b = group_scale<2, 0x400000u>(m);  // 6 = 1.5 * 2^2
+    scales[row * groups + g] = static_cast<uint8_t>(b);
+    const float inv = __uint_as_float((254u - (b > 253u ? 253u : b)) << 23);
+    uint8_t *out = codes + row * ((K + 1) / 2) + g * 16;
+    for (int i = 0; i < n; i += 2) {
+        // a group with a weight that is not finite is NaN by its scale: codes 0
+        const float lo = b == 255u ? 0.0f : load_as(src, row * ld + g * 32 + i, type) * inv;
+        const float hi = b == 255u || i + 1 >= n ? 0.0f : load_as(src, row * ld + g * 32 + i + 1, type) * inv;
+        out[i / 2] = static_cast<uint8_t>(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, lo, hi, 1.0f, 0));
+    }
+}
+
+__device__ __forceinline__ uint32_t code_of(const uint8_t *codes, int64_t row_bytes, int n, int k, int N, int K) {
+    if (n >= N || k >= K) return 0u;
+    const uint32_t b = codes[n * row_bytes + (k >> 1)];
+    return k & 1 ? b >> 4 : b & 15u;
+}
+
+// tiles: one thread per 16 bytes of codes (32 inputs of an output) and their scale.
+__global__ void __launch_bounds__(256) w4_tiles_kernel(W4Shape w, const uint8_t *codes, const uint8_t *scales,
+                                                       uint8_t *packed) {
+    const int64_t per = w.tiles() * w.units() * 4 * 64;  // steps up to a whole unit: their scales are there too
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (item >= per) return;
+    const int e = blockIdx.y;
+    const int lane = static_cast<int>(item & 63);
+    const int64_t step = (item >> 6) % (w.units() * 4), tile = (item >> 6) / (w.units() * 4);
+    const int n = static_cast<int>(tile * 16 + (lane & 15));
+    const int k = static_cast<int>(step * 128 + (lane >> 4) * 32);
+    const int64_t rb = (w.K + 1) / 2, groups = w.groups();
+    const uint8_t *src = codes + static_cast<int64_t>(e) * w.N * rb;
+    uint8_t *dst = packed + static_cast<int64_t>(e) * w.tile_bytes();
+    if (step < w.steps()) {
+        uint32_t v[4];
+        const uint8_t *at = src + n * rb + (k >> 1);
+        if (n < w.N && k + 32 <= w.K && (reinterpret_cast<uintptr_t>(at) & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const uint32_t *>(at)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = 0u;
+                for (int j = 0; j < 8; ++j) v[i] |= code_of(src, rb, n, k + 8 * i + j, w.N, w.K) << (4 * j);
+            }
+        }
+        reinterpret_cast<uint4 *>(dst)[(tile * w.steps() + step) * 64 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    const uint8_t s = n < w.N && k < w.K ? scales[(static_cast<int64_t>(e) * w.N + n) * groups + k / 32] : 127;
+    dst[w.tile_codes() + ((tile * w.units() + step / 4) * 64 + lane) * 4 + step % 4] = s;
+}
+
+// rows: one thread per 8 outputs x 8 inputs.
+__global__ void __launch_bounds__(256) w4_rows_kernel(W4Shape w, const uint8_t *codes, const uint8_t *scales,
+                                                      uint8_t *packed) {
+    const int64_t np = w.np(), groups = w.groups(), oct = np / 8;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (item >= oct * groups * 4) return;
+    const int e = blockIdx.y;
+    const int n0 = static_cast<int>(item % oct) * 8;
+    const int64_t part = item / oct;
+    const int64_t g = part / 4;
+    const int q = static_cast<int>(part % 4);
+    const int64_t rb = (w.K + 1) / 2;
+    const uint8_t *src = codes + static_cast<int64_t>(e) * w.N * rb;
+    uint8_t *dst = packed + static_cast<int64_t>(e) * w.row_bytes() + g * 17 * np;
+    const int k0 = static_cast<int>(g * 32) + q * 8;
+    uint32_t in[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint8_t *at = src + (n0 + i) * rb + (k0 >> 1);
+        in[i] = 0u;
+        if (n0 + i < w.N && k0 + 8 <= w.K && (reinterpret_cast<uintptr_t>(at) & 3) == 0)
+            in[i] = *reinterpret_cast<const uint32_t *>(at);
+        else
+            for (int j = 0; j < 8; ++j) in[i] |= code_of(src, rb, n0 + i, k0 + j, w.N, w.K) << (4 * j);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t v = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v |= (in[i] >> (4 * j) & 15u) << (4 * i);
+        reinterpret_cast<uint32_t *>(dst + np + (q * 8 + j) * (np / 2))[n0 / 8] = v;
+    }
+    if (q == 0)
+        for (int i = 0; i < 8; ++i)
+            dst[n0 + i] = n0 + i < w.N ? scales[(static_cast<int64_t>(e) * w.N + n0 + i) * groups + g] : 127;
+}
+
+unsigned blocks_for(int64_t items) { return static_cast<unsigned>((items + 255) / 256); }
+
+}  // namespace
+
+hipError_t launch_w4_quantize(const W4Shape &w, const void *src, int type, int64_t ld, uint8_t *codes, uint8_t *scales,
+                              hipStream_t s) {
+    const int64_t rows = static_cast<int64_t>(w.E) * w.N;
+    w4_quantize_kernel<<<dim3(blocks_for(rows * w.groups())), dim3(256), 0, s>>>(src, type, ld, rows, w.K, codes,
+                                                                                scales);
+    return hipGetLastError();
+}
+
+hipError_t launch_w4_pack(const W4Shape &w, int layout, const uint8_t *codes, const uint8_t *scales, uint8_t *packed,
+                          hipStream_t s) {
+    if (layout == ISC_W4_TILES) {
+        const dim3 grid(blocks_for(w.tiles() * w.units() * 256), static_cast<unsigned>(w.E));
+        w4_tiles_kernel<<<grid, dim3(256), 0, s>>>(w, codes, scales, packed);
+    } else {
+        const dim3 grid(blocks_for(w.np() / 8 * w.groups() * 4), static_cast<unsigned>(w.E));
+        w4_rows_kernel<<<grid, dim3(256), 0, s>>>(w, codes, scales, packed);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace isc
