@@ -209,9 +209,10 @@ hipError_t launch_route_bwd(const RouteBwdArgs &a, hipStream_t s);
 
 // 4-bit weights of E matrices N x K in one of two layouts.
 //   tiles: for every 16 outputs and 128 inputs one KiB, lane l of a wavefront
-//     owning 16 bytes: output l % 16, inputs 32 (l / 16) .. + 32, in order; so
-//     a lane's load is a matrix operand.  The scales of four such steps follow
-//     each other in a word per lane, after all codes of the matrix.
+//     owning 16 bytes: output l % 16, and in word j the inputs 32 j + 8 (l / 16)
+//     .. + 8, in order; so a lane's word is a matrix operand of 32 inputs, one
+//     group.  The scales of such a step, a word for each of the 16 outputs,
+//     follow after all codes of the matrix.
 //   rows: for every 32 inputs the outputs' scales (Np bytes), then 32 rows of
 //     Np / 2 bytes, one per input, outputs in order (Np: N up to 128s); so the
 //     weights of one input are contiguous, as the convolution's filters are.
@@ -219,9 +220,8 @@ struct W4Shape {
     int E, N, K;
     __host__ __device__ int64_t tiles() const { return (N + 15) / 16; }
     __host__ __device__ int64_t steps() const { return (K + 127) / 128; }
-    __host__ __device__ int64_t units() const { return (K + 511) / 512; }
     __host__ __device__ int64_t tile_codes() const { return tiles() * steps() * 1024; }
-    __host__ __device__ int64_t tile_bytes() const { return tile_codes() + tiles() * units() * 256; }
+    __host__ __device__ int64_t tile_bytes() const { return tile_codes() + tiles() * steps() * 64; }
     __host__ __device__ int64_t np() const { return (N + 127) / 128 * 128; }
     __host__ __device__ int64_t groups() const { return (K + 31) / 32; }
     __host__ __device__ int64_t row_bytes() const { return groups() * 17 * np(); }
@@ -243,7 +243,7 @@ struct W4Args {
     const float *weights;
     void *y;
     float *part;
-    bool whole;  // every row of x 16-byte aligned
+    bool whole;  // every row of x 16-byte aligned, and of an 8-bit x's scales 4-byte
 };
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);
 // Ranges that the skipping product's inputs are cut into (each a row of sums

@@ -264,7 +264,7 @@ int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const voi
     if (const int st = isc::require_gfx950()) return st;
     const isc::W4Args a{w, static_cast<const uint8_t *>(packed), x, static_cast<const uint8_t *>(x_scales), ldx,
                         ld_scales, ldy, T, slots, x_type, y_type, relu != 0, ids, offsets, order, nullptr, y, nullptr,
-                        in[0].whole()};
+                        in[0].whole() && (x_type != ISC_MX8 || (aligned(x_scales, 4) && ld_scales % 4 == 0))};
     return hip_status(isc::launch_w4_linear(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -40,37 +40,39 @@ __device__ __forceinline__ uint32_t code_of(const uint8_t *codes, int64_t row_by
     return k & 1 ? b >> 4 : b & 15u;
 }
 
-// tiles: one thread per 16 bytes of codes (32 inputs of an output) and their scale.
+// tiles: one thread per 16 bytes of codes (four words of 8 inputs each) and, for
+// 16 of 64 threads, the word of four scales.
 __global__ void __launch_bounds__(256) w4_tiles_kernel(W4Shape w, const uint8_t *codes, const uint8_t *scales,
                                                        uint8_t *packed) {
-    const int64_t per = w.tiles() * w.units() * 4 * 64;  // steps up to a whole unit: their scales are there too
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (item >= per) return;
+    if (item >= w.tiles() * w.steps() * 64) return;
     const int e = blockIdx.y;
     const int lane = static_cast<int>(item & 63);
-    const int64_t step = (item >> 6) % (w.units() * 4), tile = (item >> 6) / (w.units() * 4);
-    const int n = static_cast<int>(tile * 16 + (lane & 15));
-    const int k = static_cast<int>(step * 128 + (lane >> 4) * 32);
+    const int64_t block = item >> 6, step = block % w.steps(), tile = block / w.steps();
+    const int n = static_cast<int>(tile * 16 + (lane & 15)), g = lane >> 4;
+    const int k = static_cast<int>(step * 128 + g * 8);
     const int64_t rb = (w.K + 1) / 2, groups = w.groups();
     const uint8_t *src = codes + static_cast<int64_t>(e) * w.N * rb;
     uint8_t *dst = packed + static_cast<int64_t>(e) * w.tile_bytes();
-    if (step < w.steps()) {
-        uint32_t v[4];
-        const uint8_t *at = src + n * rb + (k >> 1);
-        if (n < w.N && k + 32 <= w.K && (reinterpret_cast<uintptr_t>(at) & 3) == 0) {
+    uint32_t v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const uint32_t *>(at)[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = 0u;
-                for (int j = 0; j < 8; ++j) v[i] |= code_of(src, rb, n, k + 8 * i + j, w.N, w.K) << (4 * j);
-            }
-        }
-        reinterpret_cast<uint4 *>(dst)[(tile * w.steps() + step) * 64 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+    for (int j = 0; j < 4; ++j) {
+        const uint8_t *at = src + n * rb + ((k + 32 * j) >> 1);
+        v[j] = 0u;
+        if (n < w.N && k + 32 * j + 8 <= w.K && (reinterpret_cast<uintptr_t>(at) & 3) == 0)
+            v[j] = *reinterpret_cast<const uint32_t *>(at);
+        else
+            for (int i = 0; i < 8; ++i) v[j] |= code_of(src, rb, n, k + 32 * j + i, w.N, w.K) << (4 * i);
     }
-    const uint8_t s = n < w.N && k < w.K ? scales[(static_cast<int64_t>(e) * w.N + n) * groups + k / 32] : 127;
-    dst[w.tile_codes() + ((tile * w.units() + step / 4) * 64 + lane) * 4 + step % 4] = s;
+    reinterpret_cast<uint4 *>(dst)[block * 64 + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+    if (g != 0) return;
+    uint32_t s = 0u;
+    for (int j = 0; j < 4; ++j) {
+        const int64_t group = step * 4 + j;
+        const uint32_t b = n < w.N && group < groups ? scales[(static_cast<int64_t>(e) * w.N + n) * groups + group] : 127u;
+        s |= b << (8 * j);
+    }
+    reinterpret_cast<uint32_t *>(dst + w.tile_codes())[block * 16 + lane] = s;
 }
 
 // rows: one thread per 8 outputs x 8 inputs.
@@ -125,7 +127,7 @@ hipError_t launch_w4_quantize(const W4Shape &w, const void *src, int type, int64
 hipError_t launch_w4_pack(const W4Shape &w, int layout, const uint8_t *codes, const uint8_t *scales, uint8_t *packed,
                           hipStream_t s) {
     if (layout == ISC_W4_TILES) {
-        const dim3 grid(blocks_for(w.tiles() * w.units() * 256), static_cast<unsigned>(w.E));
+        const dim3 grid(blocks_for(w.tiles() * w.steps() * 64), static_cast<unsigned>(w.E));
         w4_tiles_kernel<<<grid, dim3(256), 0, s>>>(w, codes, scales, packed);
     } else {
         const dim3 grid(blocks_for(w.np() / 8 * w.groups() * 4), static_cast<unsigned>(w.E));

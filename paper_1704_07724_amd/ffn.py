@@ -77,42 +77,67 @@ def declare(L):
     L.isc_w4_skip.argtypes = [dp, vp, i32, vp, i32, i64, i32, vp, vp, vp, i32, i64, vp, sz, vp]
 
 
-_types = {}
+_state = None
 
 
-def _type(t, name):
-    """The isc_type of a floating tensor's dtype."""
-    if not _types:
+class _State:
+    """What every call needs, looked up once: the library, torch's types and
+    its query for the current stream of a device."""
+
+    def __init__(self):
         torch = _isc._torch()
-        _types.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
-    code = _types.get(getattr(t, "dtype", t))
+        self.torch, self.lib = torch, _isc.lib()
+        self.types = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+        self.f8, self.e8, self.f32, self.i32, self.u8 = (torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32,
+                                                         torch.int32, torch.uint8)
+        # the stream's handle itself where torch hands it out: a Stream object costs
+        # 2.8 us, a fifth of a one-token call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.stream_of = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self.device = torch.cuda.current_device
+
+
+def _ready():
+    global _state
+    if _state is None:
+        _state = _State()
+    return _state
+
+
+def _type(st, dtype, name):
+    """The isc_type of a dtype."""
+    code = st.types.get(dtype)
     if code is None:
-        raise TypeError("%s must be float32, float16 or bfloat16" % name)
+        raise TypeError("%s must be float32, float16 or bfloat16, not %s" % (name, dtype))
     return code
 
 
-def _on_device(torch, device, **tensors):
-    """Every tensor given is on `device`, which is the current one."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current CUDA/HIP device, not %s" % device)
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+def _stream(st, stream, device):
+    return st.stream_of(device) if stream is None else _isc._stream(stream)
+
+
+def _device(st, first, *others):
+    """The index of the device that holds every tensor given; it is the current one."""
+    index = first.get_device()
+    if index < 0 or index != st.device():
+        raise ValueError("tensors must be on the current CUDA/HIP device, not on %s" % first.device)
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError("tensors are on %s and %s" % (first.device, t.device))
+    return index
 
 
 def _rows(t, cols, name):
     """(tensor, leading dimension) of t as rows of `cols` values: t itself where its
     rows are evenly spaced and do not overlap, else a contiguous copy."""
-    if t.dim() < 1 or t.shape[-1] != cols:
-        raise ValueError("%s must have %d values in its last dimension, not %r" % (name, cols, tuple(t.shape)))
+    sizes = t.shape
+    if not sizes or sizes[-1] != cols:
+        raise ValueError("%s must have %d values in its last dimension, not %r" % (name, cols, tuple(sizes)))
     if t.is_contiguous():
         return t, cols
-    if t.dim() == 1:
-        return t.contiguous(), cols
-    sizes, strides = t.shape, t.stride()
-    ld = None
-    span = 1
-    if strides[-1] == 1 or cols == 1:
+    strides = t.stride()
+    if len(sizes) > 1 and (strides[-1] == 1 or cols == 1):
+        ld, span = None, 1
         for n, s in zip(reversed(sizes[:-1]), reversed(strides[:-1])):
             if n == 1:
                 continue
@@ -130,27 +155,25 @@ def _rows(t, cols, name):
 
 
 def _vector(t, n, name):
-    if tuple(t.shape) != (n,):
+    if t.dim() != 1 or t.shape[0] != n:
         raise ValueError("%s must be [%d], not %r" % (name, n, tuple(t.shape)))
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _float32(t, shape, name):
-    torch = _isc._torch()
-    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be float32 %r, not %s %r" % (name, tuple(shape), t.dtype, tuple(t.shape)))
-    return t.contiguous()
+def _exact(t, dtype, shape, name):
+    """A contiguous tensor of that type and shape."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError("%s must be %s %r, not %s %r" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    return t if t.is_contiguous() else t.contiguous()
 
 
-def _int32(t, shape, name):
-    torch = _isc._torch()
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be int32 %r, not %s %r" % (name, tuple(shape), t.dtype, tuple(t.shape)))
-    return t.contiguous()
+def _bytes(st, n, like):
+    """A workspace of n bytes."""
+    return st.torch.empty(n, dtype=st.u8, device=like.device)
 
 
 def isc_rmsnorm(x, weight, eps=1e-6, residual=None, y=True, mx8=False, rstd=False, stream=None):
@@ -160,34 +183,44 @@ def isc_rmsnorm(x, weight, eps=1e-6, residual=None, y=True, mx8=False, rstd=Fals
     of any of those types.  Returns Norm(y, h, mx8, rstd): y in x's type (if y),
     h (with a residual), the norm in 8 bits with scales (if mx8), the reciprocal
     root mean squares for isc_rmsnorm_bwd (if rstd)."""
-    torch = _isc._torch()
+    st = _state or _ready()
     if not (y or mx8 or rstd or residual is not None):
         raise ValueError("nothing is asked for")
-    with _isc._on(stream):
-        D = x.shape[-1]
-        code = _type(x, "x")
-        _on_device(torch, x.device, weight=weight, residual=residual)
-        T = x.numel() // D if D else 0
-        xr, ldx = _rows(x, D, "x")
-        rr, ldr = None, D
-        if residual is not None:
-            if residual.dtype != x.dtype or residual.shape != x.shape:
-                raise ValueError("residual must have x's shape and type")
-            rr, ldr = _rows(residual, D, "residual")
-        wr = _vector(weight, D, "weight")
-        lead = x.shape[:-1]
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None else None
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y else None
-        groups = (D + 31) // 32
-        form = None
-        if mx8:
-            form = Mx8(torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device),
-                       torch.empty((*lead, groups), dtype=torch.float8_e8m0fnu, device=x.device))
-        rs = torch.empty(lead, dtype=torch.float32, device=x.device) if rstd else None
-        _isc._check(_isc.lib().isc_rmsnorm(
-            T, D, code, xr.data_ptr(), ldx, _ptr(rr), ldr, wr.data_ptr(), _type(wr, "weight"), eps, _ptr(h), D,
-            _ptr(out), D, form[0].data_ptr() if mx8 else None, D, form[1].data_ptr() if mx8 else None, groups,
-            _ptr(rs), _isc._stream(stream)), "isc_rmsnorm")
+    if stream is not None:
+        with _isc._on(stream):
+            return _rmsnorm(st, x, weight, eps, residual, y, mx8, rstd, stream)
+    return _rmsnorm(st, x, weight, eps, residual, y, mx8, rstd, None)
+
+
+def _rmsnorm(st, x, weight, eps, residual, y, mx8, rstd, stream):
+    shape = x.shape
+    D = shape[-1]
+    code = _type(st, x.dtype, "x")
+    device = _device(st, x, weight, residual)
+    xr, ldx = _rows(x, D, "x")
+    new = st.torch.empty_like if xr.is_contiguous() else lambda t, **kw: st.torch.empty(shape, device=x.device, **kw)
+    rp, ldr, h, hp = None, D, None, None
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != shape:
+            raise ValueError("residual must have x's shape and type")
+        rr, ldr = _rows(residual, D, "residual")
+        rp = rr.data_ptr()
+        h = new(xr, dtype=x.dtype)
+        hp = h.data_ptr()
+    wr = _vector(weight, D, "weight")
+    out = new(xr, dtype=x.dtype) if y else None
+    groups = (D + 31) // 32
+    form, qp, sp = None, None, None
+    if mx8:
+        form = Mx8(new(xr, dtype=st.f8), st.torch.empty((*shape[:-1], groups), dtype=st.e8, device=x.device))
+        qp, sp = form[0].data_ptr(), form[1].data_ptr()
+    rs = st.torch.empty(shape[:-1], dtype=st.f32, device=x.device) if rstd else None
+    status = st.lib.isc_rmsnorm(
+        x.numel() // D if D else 0, D, code, xr.data_ptr(), ldx, rp, ldr, wr.data_ptr(),
+        _type(st, wr.dtype, "weight"), eps, hp, D, _ptr(out), D, qp, D, sp, groups, _ptr(rs),
+        _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_rmsnorm")
     return Norm(out, h, form, rs)
 
 
@@ -198,30 +231,30 @@ def isc_rmsnorm_bwd(dy, h, weight, rstd, dh=None, ws=None, stream=None):
     residual); rstd: [...] float32 from there; dh: the gradient that reaches h
     past the norm, or None.  dx (in h's type) is the gradient of x and of the
     residual alike; dweight is float32 [D]."""
-    torch = _isc._torch()
+    st = _state or _ready()
     with _isc._on(stream):
-        D = h.shape[-1]
-        code = _type(h, "h")
-        _on_device(torch, h.device, dy=dy, weight=weight, rstd=rstd, dh=dh, ws=ws)
+        torch, D = st.torch, h.shape[-1]
+        code = _type(st, h.dtype, "h")
+        device = _device(st, h, dy, weight, rstd, dh, ws)
         for t, name in ((dy, "dy"), (dh, "dh")):
             if t is not None and (t.dtype != h.dtype or t.shape != h.shape):
                 raise ValueError("%s must have h's shape and type" % name)
         T = h.numel() // D if D else 0
-        rs = _float32(rstd, h.shape[:-1], "rstd")
+        rs = _exact(rstd, st.f32, h.shape[:-1], "rstd")
         hr, ldh = _rows(h, D, "h")
         yr, ldy = _rows(dy, D, "dy")
         gr, ldd = (None, D) if dh is None else _rows(dh, D, "dh")
         wr = _vector(weight, D, "weight")
         dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        dw = torch.empty(D, dtype=torch.float32, device=h.device)
-        n = ctypes.c_size_t()
-        _isc._check(_isc.lib().isc_rmsnorm_bwd_workspace_size(T, D, n), "isc_rmsnorm_bwd_workspace_size")
+        dw = torch.empty(D, dtype=st.f32, device=h.device)
         if ws is None:
-            ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=h.device)
-        _isc._check(_isc.lib().isc_rmsnorm_bwd(
-            T, D, code, yr.data_ptr(), ldy, hr.data_ptr(), ldh, wr.data_ptr(), _type(wr, "weight"), rs.data_ptr(),
-            _ptr(gr), ldd, dx.data_ptr(), D, dw.data_ptr(), ws.data_ptr(), _isc._nbytes(ws), _isc._stream(stream)),
-            "isc_rmsnorm_bwd")
+            n = ctypes.c_size_t()
+            _isc._check(st.lib.isc_rmsnorm_bwd_workspace_size(T, D, n), "isc_rmsnorm_bwd_workspace_size")
+            ws = _bytes(st, n.value, h)
+        _isc._check(st.lib.isc_rmsnorm_bwd(
+            T, D, code, yr.data_ptr(), ldy, hr.data_ptr(), ldh, wr.data_ptr(), _type(st, wr.dtype, "weight"),
+            rs.data_ptr(), _ptr(gr), ldd, dx.data_ptr(), D, dw.data_ptr(), ws.data_ptr(), _isc._nbytes(ws),
+            _stream(st, stream, device)), "isc_rmsnorm_bwd")
     return dx, dw
 
 
@@ -239,32 +272,33 @@ def isc_route(logits, k, bias=None, score="softmax", groups=1, keep_groups=None,
     scores for the choice only; groups, keep_groups: the choice is among the
     experts of the best keep_groups (default: all) of that many groups; renorm:
     weights divided by their sum; lists=False: no offsets and order."""
-    torch = _isc._torch()
+    st = _state or _ready()
     which = _score(score)
     with _isc._on(stream):
         if logits.dim() != 2:
             raise ValueError("logits must be [T, E], not %r" % (tuple(logits.shape),))
         T, E = logits.shape
-        code = _type(logits, "logits")
-        dev = logits.device
-        _on_device(torch, dev, bias=bias, ws=ws)
+        code = _type(st, logits.dtype, "logits")
+        device, dev, empty = _device(st, logits, bias, ws), logits.device, st.torch.empty
         lr, ld = _rows(logits, E, "logits")
-        br = None if bias is None else _float32(bias, (E,), "bias")
+        br = None if bias is None else _exact(bias, st.f32, (E,), "bias")
         k = int(k)
-        ids = torch.empty((T, max(k, 0)), dtype=torch.int32, device=dev)
-        weights = torch.empty((T, max(k, 0)), dtype=torch.float32, device=dev)
-        offsets = torch.empty(E + 1, dtype=torch.int32, device=dev) if lists else None
-        order = torch.empty(max(T * k, 0), dtype=torch.int32, device=dev) if lists else None
+        if k < 1:
+            raise ValueError("k must be at least 1, not %d" % k)
+        ids = empty((T, k), dtype=st.i32, device=dev)
+        weights = empty((T, k), dtype=st.f32, device=dev)
+        offsets = empty(E + 1, dtype=st.i32, device=dev) if lists else None
+        order = empty(T * k, dtype=st.i32, device=dev) if lists else None
         if ws is None and lists and T > 64:
             n = ctypes.c_size_t()
-            _isc._check(_isc.lib().isc_route_workspace_size(T, E, n), "isc_route_workspace_size")
-            ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=dev)
+            _isc._check(st.lib.isc_route_workspace_size(T, E, n), "isc_route_workspace_size")
+            ws = _bytes(st, n.value, logits)
         # an empty tensor has no address, and without tokens there is no order to write
         at = order.data_ptr() or offsets.data_ptr() if lists and not T else _ptr(order)
-        _isc._check(_isc.lib().isc_route(
+        _isc._check(st.lib.isc_route(
             T, E, k, code, lr.data_ptr(), ld, _ptr(br), which, groups, groups if keep_groups is None else keep_groups,
             bool(renorm), scale, ids.data_ptr(), weights.data_ptr(), _ptr(offsets), at, _ptr(ws),
-            0 if ws is None else _isc._nbytes(ws), _isc._stream(stream)), "isc_route")
+            0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device)), "isc_route")
     return Route(ids, weights, offsets, order)
 
 
@@ -273,21 +307,21 @@ def isc_route_bwd(dweights, logits, ids, score="softmax", renorm=True, scale=1.0
 
     dweights: [T, k] float32; ids: [T, k] int32 as isc_route gave them; score,
     renorm, scale: as there."""
-    torch = _isc._torch()
+    st = _state or _ready()
     which = _score(score)
     with _isc._on(stream):
         if logits.dim() != 2 or ids.dim() != 2:
             raise ValueError("logits must be [T, E] and ids [T, k]")
         T, E = logits.shape
         k = ids.shape[1]
-        code = _type(logits, "logits")
-        _on_device(torch, logits.device, dweights=dweights, ids=ids)
+        code = _type(st, logits.dtype, "logits")
+        device = _device(st, logits, dweights, ids)
         lr, ld = _rows(logits, E, "logits")
-        dr = _float32(dweights, (T, k), "dweights")
-        ir = _int32(ids, (T, k), "ids")
-        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
-        _isc._check(_isc.lib().isc_route_bwd(T, E, k, code, dr.data_ptr(), lr.data_ptr(), ld, ir.data_ptr(), which,
-                                             bool(renorm), scale, out.data_ptr(), E, _isc._stream(stream)),
+        dr = _exact(dweights, st.f32, (T, k), "dweights")
+        ir = _exact(ids, st.i32, (T, k), "ids")
+        out = st.torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        _isc._check(st.lib.isc_route_bwd(T, E, k, code, dr.data_ptr(), lr.data_ptr(), ld, ir.data_ptr(), which,
+                                         bool(renorm), scale, out.data_ptr(), E, _stream(st, stream, device)),
                     "isc_route_bwd")
     return out
 
@@ -295,18 +329,20 @@ def isc_route_bwd(dweights, logits, ids, score="softmax", renorm=True, scale=1.0
 def isc_w4_quantize(w, stream=None):
     """(codes, scales) of 4-bit weights: w [N, K] or [E, N, K] float32, float16 or
     bfloat16; codes [..., N, ceil(K / 2)] uint8, scales [..., N, ceil(K / 32)] float8_e8m0fnu."""
-    torch = _isc._torch()
+    st = _state or _ready()
     with _isc._on(stream):
+        torch = st.torch
         if w.dim() not in (2, 3):
             raise ValueError("w must be [N, K] or [E, N, K], not %r" % (tuple(w.shape),))
         E = w.shape[0] if w.dim() == 3 else 1
         N, K = w.shape[-2:]
-        _on_device(torch, w.device)
+        device = _device(st, w)
         wr, ld = _rows(w, K, "w")
         codes = torch.empty((*w.shape[:-1], (K + 1) // 2), dtype=torch.uint8, device=w.device)
         scales = torch.empty((*w.shape[:-1], (K + 31) // 32), dtype=torch.float8_e8m0fnu, device=w.device)
-        _isc._check(_isc.lib().isc_w4_quantize(W4Desc(E, N, K, 0), wr.data_ptr(), _type(w, "w"), ld, codes.data_ptr(),
-                                               scales.data_ptr(), _isc._stream(stream)), "isc_w4_quantize")
+        _isc._check(st.lib.isc_w4_quantize(W4Desc(E, N, K, 0), wr.data_ptr(), _type(st, w.dtype, "w"), ld,
+                                           codes.data_ptr(), scales.data_ptr(), _stream(st, stream, device)),
+                    "isc_w4_quantize")
     return codes, scales
 
 
@@ -315,7 +351,8 @@ def isc_w4_pack_codes(codes, scales, layout, K=None, stream=None):
 
     layout: "tiles" for isc_w4_linear, "rows" for isc_w4_skip; K: the number of
     inputs where it is odd (the last byte's high half is then ignored)."""
-    torch = _isc._torch()
+    st = _state or _ready()
+    torch = st.torch
     if layout not in LAYOUTS:
         raise ValueError("layout must be one of %s, not %r" % (", ".join(LAYOUTS), layout))
     with _isc._on(stream):
@@ -327,19 +364,19 @@ def isc_w4_pack_codes(codes, scales, layout, K=None, stream=None):
         if scales.dtype not in (torch.float8_e8m0fnu, torch.uint8) or \
                 tuple(scales.shape) != (*codes.shape[:-1], (K + 31) // 32):
             raise ValueError("scales must be float8_e8m0fnu or uint8 %r" % ((*codes.shape[:-1], (K + 31) // 32),))
-        _on_device(torch, codes.device, scales=scales)
+        device = _device(st, codes, scales)
         E = codes.shape[0] if codes.dim() == 3 else 1
         desc = W4Desc(E, codes.shape[-2], K, LAYOUTS[layout])
         n = ctypes.c_size_t()
-        _isc._check(_isc.lib().isc_w4_size(desc, n), "isc_w4_size")
-        data = torch.empty(n.value, dtype=torch.uint8, device=codes.device)
+        _isc._check(st.lib.isc_w4_size(desc, n), "isc_w4_size")
+        data = _bytes(st, n.value, codes)
         cr, sr = codes.contiguous(), scales.contiguous()
-        _isc._check(_isc.lib().isc_w4_pack_codes(desc, cr.data_ptr(), sr.data_ptr(), data.data_ptr(),
-                                                 _isc._stream(stream)), "isc_w4_pack_codes")
+        _isc._check(st.lib.isc_w4_pack_codes(desc, cr.data_ptr(), sr.data_ptr(), data.data_ptr(),
+                                             _stream(st, stream, device)), "isc_w4_pack_codes")
     return W4(desc, data, codes.dim() == 3)
 
 
-def _routed(route, w4, T):
+def _routed(st, route, w4, T):
     """The slots per token and the route's tensors, checked."""
     if route is None:
         if w4.stacked:
@@ -350,7 +387,8 @@ def _routed(route, w4, T):
     ids, weights, offsets, order = route
     if ids.dim() != 2 or ids.shape[0] != T:
         raise ValueError("the route has %r slots, x %d tokens" % (tuple(ids.shape), T))
-    return ids.shape[1], ids, weights, offsets, order
+    slots = ids.shape[1]
+    return slots, _exact(ids, st.i32, (T, slots), "ids"), weights, offsets, order
 
 
 def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, stream=None):
@@ -360,36 +398,41 @@ def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, stream=None):
     Without a route: y is [..., N].  With one: x is [T, K], w4 holds the experts'
     matrices, and y is [T, k, N], slot j by the token's j-th expert (0 where it
     has none).  dtype: y's (default: x's, bfloat16 for an Mx8)."""
-    torch = _isc._torch()
+    st = _state or _ready()
     with _isc._on(stream):
-        scales, lds = None, 0
+        K, N = w4.K, w4.N
+        sp, lds, scales = None, 0, None
         if isinstance(x, tuple):
             x, scales = x
-            if x.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu:
+            if x.dtype != st.f8 or scales.dtype != st.e8:
                 raise TypeError("an Mx8 is float8_e4m3fn values and float8_e8m0fnu scales")
-            code = MX8
             if scales.shape[:-1] != x.shape[:-1]:
                 raise ValueError("scales are %r, for values %r" % (tuple(scales.shape), tuple(x.shape)))
-            scales, lds = _rows(scales, (w4.K + 31) // 32, "scales")
+            code = MX8
+            scales, lds = _rows(scales, (K + 31) // 32, "scales")
+            sp = scales.data_ptr()
         else:
-            code = _type(x, "x")
-        xr, ldx = _rows(x, w4.K, "x")
-        T = x.numel() // w4.K
-        if route is not None and x.dim() != 2:
+            code = _type(st, x.dtype, "x")
+        shape = x.shape
+        xr, ldx = _rows(x, K, "x")
+        T = x.numel() // K
+        if route is not None and len(shape) != 2:
             raise ValueError("x must be [T, K] with a route")
-        slots, ids, _, offsets, order = _routed(route, w4, T)
-        _on_device(torch, x.device, scales=scales, weights=w4.data, ids=ids, offsets=offsets, order=order)
+        slots, ids, _, offsets, order = _routed(st, route, w4, T)
+        device = _device(st, x, scales, w4.data, ids, offsets, order)
         if slots:
-            ids = _int32(ids, (T, slots), "ids")
             if offsets is None or order is None:
                 raise ValueError("the route has no lists")
-            offsets, order = _int32(offsets, (w4.E + 1,), "offsets"), _int32(order, (T * slots,), "order")
+            offsets = _exact(offsets, st.i32, (w4.E + 1,), "offsets")
+            order = _exact(order, st.i32, (T * slots,), "order")
         if dtype is None:
-            dtype = torch.bfloat16 if code == MX8 else x.dtype
-        y = torch.empty((T, slots, w4.N) if slots else (*x.shape[:-1], w4.N), dtype=dtype, device=x.device)
-        _isc._check(_isc.lib().isc_w4_linear(
-            w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, _ptr(scales), lds, slots, _ptr(ids), _ptr(offsets),
-            _ptr(order), y.data_ptr(), _type(dtype, "dtype"), w4.N, bool(relu), _isc._stream(stream)), "isc_w4_linear")
+            dtype = st.torch.bfloat16 if code == MX8 else x.dtype
+        y = st.torch.empty((T, slots, N) if slots else (*shape[:-1], N), dtype=dtype, device=x.device)
+        status = st.lib.isc_w4_linear(
+            w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, sp, lds, slots, _ptr(ids), _ptr(offsets),
+            _ptr(order), y.data_ptr(), _type(st, dtype, "dtype"), N, bool(relu), _stream(st, stream, device))
+        if status:
+            _isc._check(status, "isc_w4_linear")
     return y
 
 
@@ -400,27 +443,32 @@ def isc_w4_skip(x, w4, route=None, dtype=None, ws=None, stream=None):
     Without a route: x is [..., K], y [..., N].  With one: x is [T, k, K]
     (isc_w4_linear's output), and y [T, N] the sum over a token's experts under
     the route's weights.  dtype: y's (default: x's)."""
-    torch = _isc._torch()
+    st = _state or _ready()
     with _isc._on(stream):
-        code = _type(x, "x")
-        xr, ldx = _rows(x, w4.K, "x")
-        if route is not None and x.dim() != 3:
+        K, N = w4.K, w4.N
+        shape = x.shape
+        code = _type(st, x.dtype, "x")
+        xr, ldx = _rows(x, K, "x")
+        if route is not None and len(shape) != 3:
             raise ValueError("x must be [T, k, K] with a route")
-        T = x.shape[0] if route is not None else x.numel() // w4.K
-        slots, ids, weights, _, _ = _routed(route, w4, T)
-        _on_device(torch, x.device, w4=w4.data, ids=ids, weights=weights, ws=ws)
+        T = shape[0] if route is not None else x.numel() // K
+        slots, ids, weights, _, _ = _routed(st, route, w4, T)
+        device = _device(st, x, w4.data, ids, weights, ws)
         if slots:
-            if x.shape[1] != slots:
-                raise ValueError("x has %d slots, the route %d" % (x.shape[1], slots))
-            ids, weights = _int32(ids, (T, slots), "ids"), _float32(weights, (T, slots), "weights")
-        n = ctypes.c_size_t()
-        _isc._check(_isc.lib().isc_w4_skip_workspace_size(w4.desc, T, slots, n), "isc_w4_skip_workspace_size")
-        if ws is None and n.value:
-            ws = torch.empty(n.value, dtype=torch.uint8, device=x.device)
+            if shape[1] != slots:
+                raise ValueError("x has %d slots, the route %d" % (shape[1], slots))
+            weights = _exact(weights, st.f32, (T, slots), "weights")
+        if ws is None:
+            n = ctypes.c_size_t()
+            _isc._check(st.lib.isc_w4_skip_workspace_size(w4.desc, T, slots, n), "isc_w4_skip_workspace_size")
+            if n.value:
+                ws = _bytes(st, n.value, x)
         dtype = x.dtype if dtype is None else dtype
-        y = torch.empty((T, w4.N) if slots else (*x.shape[:-1], w4.N), dtype=dtype, device=x.device)
-        _isc._check(_isc.lib().isc_w4_skip(
+        y = st.torch.empty((T, N) if slots else (*shape[:-1], N), dtype=dtype, device=x.device)
+        status = st.lib.isc_w4_skip(
             w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, slots, _ptr(ids), _ptr(weights), y.data_ptr(),
-            _type(dtype, "dtype"), w4.N, _ptr(ws), 0 if ws is None else _isc._nbytes(ws), _isc._stream(stream)),
-            "isc_w4_skip")
+            _type(st, dtype, "dtype"), N, _ptr(ws), 0 if ws is None else _isc._nbytes(ws),
+            _stream(st, stream, device))
+        if status:
+            _isc._check(status, "isc_w4_skip")
     return y

@@ -1,0 +1,174 @@
+"""The feed-forward operators' refusals, on the host: the C entry points turn bad
+arguments into a status before they touch a device, the binding into exceptions."""
+import ctypes
+
+import pytest
+
+import paper_1704_07724_amd as isc
+
+NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, DEVICE, ALIGN, ARG = 1, 2, 3, 4, 5, 7, 9, 10
+OK = (0, DEVICE)  # valid arguments: with no GPU in the process the device check ends the call
+A, B, C, D, E, F = (0x10000000 * i for i in range(1, 7))  # addresses that are only compared
+
+
+@pytest.fixture(scope="module", autouse=True)
+def no_gpu():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("made-up addresses: only where no call can reach a GPU")
+
+
+def norm(T=2, N=64, t=2, x=A, ldx=64, r=B, ldr=64, w=C, wt=2, eps=1e-6, h=D, ldh=64, y=E, ldy=64, q=F, ldq=64,
+         s=F + 4096, lds=2, rstd=F + 8192):
+    return isc.lib().isc_rmsnorm(T, N, t, x, ldx, r, ldr, w, wt, eps, h, ldh, y, ldy, q, ldq, s, lds, rstd, None)
+
+
+def test_norm_refusals():
+    assert norm() in OK and norm(T=0, x=None) == 0
+    assert norm(x=None) == NULL and norm(w=None) == NULL and norm(s=None) == NULL and norm(q=None) == NULL
+    assert norm(h=None, y=None, q=None, s=None, rstd=None) == NULL
+    assert norm(T=-1) == SHAPE and norm(N=0) == SHAPE
+    assert norm(ldx=63) == SHAPE and norm(ldy=63) == SHAPE and norm(lds=1) == SHAPE and norm(ldr=0) == SHAPE
+    assert norm(t=3) == ARG and norm(t=7) == ARG and norm(wt=3) == ARG
+    assert norm(eps=-1.0) == ARG and norm(eps=float("nan")) == ARG and norm(eps=float("inf")) == ARG
+    assert norm(N=65537, ldx=70000, ldr=70000, ldh=70000, ldy=70000, ldq=70000, lds=4000) == LIMIT
+    assert norm(x=A + 1) == ALIGN and norm(y=E + 1) == ALIGN and norm(rstd=F + 8193) == ALIGN
+    assert norm(h=B) in OK and norm(h=A) in OK and norm(y=A) in OK       # in place
+    assert norm(h=B, ldh=72) == ALIAS and norm(h=B + 16) == ALIAS        # across
+    assert norm(y=D) == ALIAS and norm(q=A) == ALIAS and norm(h=C) == ALIAS and norm(rstd=E) == ALIAS
+
+
+def norm_bwd(T=2, N=64, t=0, dy=A, ldy=64, h=B, ldh=64, w=C, wt=0, rstd=C + 4096, dh=D, ldd=64, dx=E, ldx=64,
+             dw=E + 4096, ws=F, n=1 << 20):
+    return isc.lib().isc_rmsnorm_bwd(T, N, t, dy, ldy, h, ldh, w, wt, rstd, dh, ldd, dx, ldx, dw, ws, n, None)
+
+
+def test_norm_bwd_refusals():
+    assert norm_bwd() in OK and norm_bwd(dh=None) in OK and norm_bwd(dx=A) in OK and norm_bwd(dx=D) in OK
+    assert norm_bwd(dy=None) == NULL and norm_bwd(dw=None) == NULL and norm_bwd(ws=None) == NULL
+    assert norm_bwd(T=0, dy=None, h=None, w=None, rstd=None, dx=None) in OK  # dw = 0 is still written
+    assert norm_bwd(N=0) == SHAPE and norm_bwd(ldh=63) == SHAPE and norm_bwd(ldx=1) == SHAPE
+    assert norm_bwd(N=16385, ldy=20000, ldh=20000, ldd=20000, ldx=20000) == LIMIT
+    assert norm_bwd(n=511) == WORKSPACE and norm_bwd(ws=F + 16) == ALIGN and norm_bwd(t=3) == ARG
+    assert norm_bwd(dw=C) == ALIAS and norm_bwd(dx=A + 4) == ALIAS and norm_bwd(ws=A) == ALIAS
+    n = ctypes.c_size_t()
+    assert isc.lib().isc_rmsnorm_bwd_workspace_size(2, 64, None) == NULL
+    assert isc.lib().isc_rmsnorm_bwd_workspace_size(-1, 64, n) == SHAPE
+    assert isc.lib().isc_rmsnorm_bwd_workspace_size(2, 64, n) == 0 and n.value >= 2 * 64 * 4
+
+
+def route(T=100, N=16, k=2, t=0, l=A, ld=16, bias=B, score=0, groups=4, keep=2, renorm=1, scale=1.0, ids=C, w=D, off=E,
+          order=E + 4096, ws=F, n=1 << 20):
+    return isc.lib().isc_route(T, N, k, t, l, ld, bias, score, groups, keep, renorm, scale, ids, w, off, order, ws, n,
+                               None)
+
+
+def test_route_refusals():
+    assert route() in OK and route(bias=None) in OK and route(off=None, order=None, ws=None, n=0) in OK
+    assert route(T=64, ws=None, n=0) in OK  # one workgroup needs no workspace
+    assert route(l=None) == NULL and route(ids=None) == NULL and route(order=None) == NULL and route(ws=None) == NULL
+    for bad in (dict(T=-1), dict(N=0), dict(k=0), dict(k=17), dict(groups=3), dict(groups=0), dict(keep=0), dict(keep=5),
+                dict(ld=15)):
+        assert route(**bad) == SHAPE, bad
+    assert route(score=2) == ARG and route(t=3) == ARG and route(scale=float("nan")) == ARG
+    assert route(N=1025, ld=1025, groups=1, keep=1) == LIMIT
+    assert route(N=130, ld=130, k=65, groups=1, keep=1) == LIMIT and route(N=130, ld=130, groups=65) == LIMIT
+    assert route(T=1 << 30, k=4) == LIMIT
+    assert route(n=8) == WORKSPACE and route(ws=F + 8) == ALIGN and route(l=A + 2) == ALIGN
+    assert route(ids=A) == ALIAS and route(w=C) == ALIAS and route(ws=D) == ALIAS and route(off=B) == ALIAS
+
+
+def route_bwd(T=3, N=16, k=2, t=0, dw=A, l=B, ld=16, ids=C, score=1, renorm=1, scale=1.0, dl=D, ldd=16):
+    return isc.lib().isc_route_bwd(T, N, k, t, dw, l, ld, ids, score, renorm, scale, dl, ldd, None)
+
+
+def test_route_bwd_refusals():
+    assert route_bwd() in OK and route_bwd(dl=B) in OK and route_bwd(T=0, l=None) == 0
+    assert route_bwd(dw=None) == NULL and route_bwd(ids=None) == NULL and route_bwd(dl=None) == NULL
+    assert route_bwd(k=0) == SHAPE and route_bwd(k=17) == SHAPE and route_bwd(ldd=15) == SHAPE
+    assert route_bwd(N=1025, ld=1025, ldd=1025) == LIMIT and route_bwd(score=5) == ARG and route_bwd(t=3) == ARG
+    assert route_bwd(dl=B, ldd=20) == ALIAS and route_bwd(dl=C) == ALIAS and route_bwd(ids=C + 2) == ALIGN
+
+
+def desc(E=1, N=32, K=64, layout=0):
+    return isc.W4Desc(E, N, K, layout)
+
+
+def test_w4_sizes_and_packing():
+    L, n = isc.lib(), ctypes.c_size_t()
+    for layout in (0, 1):
+        assert L.isc_w4_size(desc(layout=layout), n) == 0 and n.value >= 32 * 64 // 2 + 32 * 2
+        # 17/32 of a byte a weight where nothing is padded
+        assert L.isc_w4_size(desc(3, 1024, 2048, layout), n) == 0 and n.value == 3 * 1024 * 2048 * 17 // 32
+    assert L.isc_w4_size(None, n) == NULL and L.isc_w4_size(desc(), None) == NULL
+    assert L.isc_w4_size(desc(E=0), n) == SHAPE and L.isc_w4_size(desc(N=0), n) == SHAPE
+    assert L.isc_w4_size(desc(layout=2), n) == ARG and L.isc_w4_size(desc(E=1025), n) == LIMIT
+    assert L.isc_w4_size(desc(N=1 << 20, K=1 << 20), n) == LIMIT
+    pack = lambda d=desc(), c=A, s=B, p=C: L.isc_w4_pack_codes(d, c, s, p, None)  # noqa: E731
+    assert pack() in OK
+    assert pack(c=None) == NULL and pack(p=C + 16) == ALIGN and pack(p=A) == ALIAS and pack(d=desc(K=0)) == SHAPE
+    quant = lambda w=A, t=0, ld=64, c=B, s=C: L.isc_w4_quantize(desc(), w, t, ld, c, s, None)  # noqa: E731
+    assert quant() in OK and quant(w=None) == NULL and quant(t=3) == ARG and quant(ld=63) == SHAPE
+    assert quant(w=A + 2) == ALIGN and quant(c=A) == ALIAS and quant(s=B) == ALIAS
+
+
+def linear(d=desc(), p=A, T=3, x=B, xt=3, ldx=64, xs=C, lds=2, slots=0, ids=None, off=None, order=None, y=D, yt=2, ldy=32):
+    return isc.lib().isc_w4_linear(d, p, T, x, xt, ldx, xs, lds, slots, ids, off, order, y, yt, ldy, 0, None)
+
+
+def test_linear_refusals():
+    routed = dict(d=desc(E=4), slots=2, ids=E, off=E + 256, order=E + 512)
+    assert linear() in OK and linear(xt=0, xs=None) in OK and linear(**routed) in OK and linear(T=0, x=None) == 0
+    assert linear(p=None) == NULL and linear(xs=None) == NULL and linear(xt=0) == NULL and linear(y=None) == NULL
+    assert linear(**{**routed, "order": None}) == NULL
+    assert linear(T=-1) == SHAPE and linear(ldx=63) == SHAPE and linear(lds=1) == SHAPE and linear(ldy=31) == SHAPE
+    assert linear(slots=-1) == SHAPE
+    assert linear(d=desc(layout=1)) == ARG and linear(yt=3) == ARG and linear(xt=4) == ARG and linear(d=desc(E=2)) == ARG
+    assert linear(T=(1 << 20) + 1) == LIMIT and linear(**{**routed, "slots": 65}) == LIMIT
+    assert linear(p=A + 16) == ALIGN and linear(xt=0, xs=None, x=B + 2) == ALIGN and linear(y=D + 1) == ALIGN
+    assert linear(y=B) == ALIAS and linear(y=A) == ALIAS and linear(**{**routed, "y": E}) == ALIAS
+
+
+def skip(d=desc(layout=1), p=A, T=3, x=B, xt=2, ldx=64, slots=0, ids=None, w=None, y=D, yt=2, ldy=32, ws=F, n=1 << 24):
+    return isc.lib().isc_w4_skip(d, p, T, x, xt, ldx, slots, ids, w, y, yt, ldy, ws, n, None)
+
+
+def test_skip_refusals():
+    wide = desc(N=32, K=65536, layout=1)
+    routed = dict(d=desc(E=4, layout=1), slots=2, ids=E, w=E + 256)
+    assert skip() in OK and skip(**routed) in OK and skip(T=0, x=None) == 0
+    assert skip(x=None) == NULL and skip(**{**routed, "w": None}) == NULL and skip(d=wide, ldx=65536, ws=None) == NULL
+    assert skip(T=-1) == SHAPE and skip(ldx=63) == SHAPE and skip(ldy=31) == SHAPE
+    assert skip(d=desc(layout=0)) == ARG and skip(xt=3) == ARG and skip(yt=3) == ARG and skip(d=desc(E=2, layout=1)) == ARG
+    assert skip(T=(1 << 20) + 1) == LIMIT and skip(**{**routed, "slots": 65}) == LIMIT
+    assert skip(d=wide, ldx=65536, n=16) == WORKSPACE and skip(d=wide, ldx=65536, ws=F + 8) == ALIGN
+    assert skip(y=B) == ALIAS and skip(d=wide, ldx=65536, ws=B) == ALIAS
+
+
+def test_binding_refusals():
+    """What the binding itself refuses, before any address is taken."""
+    import torch
+    x, w = torch.zeros(2, 64), torch.ones(64)
+    with pytest.raises(ValueError, match="device"):
+        isc.isc_rmsnorm(x, w)
+    with pytest.raises(ValueError, match="nothing"):
+        isc.isc_rmsnorm(x, w, y=False)
+    with pytest.raises(TypeError):
+        isc.isc_rmsnorm(x.double(), w)
+    with pytest.raises(ValueError, match="score"):
+        isc.isc_route(x, 2, score="best")
+    with pytest.raises(ValueError):
+        isc.isc_route(x[0], 2)
+    with pytest.raises(ValueError, match="layout"):
+        isc.isc_w4_pack_codes(torch.zeros(2, 4, dtype=torch.uint8), torch.zeros(2, 1, dtype=torch.uint8), "columns")
+    with pytest.raises(ValueError, match="codes"):
+        isc.isc_w4_pack_codes(torch.zeros(2, 4), torch.zeros(2, 1, dtype=torch.uint8), "rows")
+    with pytest.raises(ValueError, match="scales"):
+        isc.isc_w4_pack_codes(torch.zeros(2, 4, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.uint8), "rows")
+    w4 = isc.W4(desc(), torch.zeros(4), False)
+    with pytest.raises(ValueError, match="last dimension"):
+        isc.isc_w4_linear(torch.zeros(2, 63), w4)
+    with pytest.raises(ValueError, match="route"):
+        isc.isc_w4_linear(x, isc.W4(desc(E=2), torch.zeros(4), True))
+    with pytest.raises(TypeError):
+        isc.isc_w4_linear((x, x), w4)
