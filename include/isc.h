@@ -558,6 +558,11 @@ int isc_w4_quantize(const isc_w4_desc *d, const void *w, int32_t type, int64_t l
  * form.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_w4_pack_codes(const isc_w4_desc *d, const uint8_t *codes, const uint8_t *scales, void *packed, void *stream);
 
+/* Bytes of workspace of isc_w4_linear (0 where x fills one matrix operand's 16
+ * columns: 16 tokens, 8 in fp16, 5 in fp32; and with experts).  Host-only.
+ * Errors: NULL, SHAPE, LIMIT, ARG. */
+int isc_w4_linear_workspace_size(const isc_w4_desc *d, int32_t T, int32_t x_type, int32_t slots, size_t *bytes);
+
 /* y[t][n] = sum over k of w[n][k] * x[t][k], with max(0, .) if relu (a NaN
  * stays), on the matrix cores; weights in the layout ISC_W4_TILES.
  *   x: T x K (T <= 2^20) of any isc_type; x_scales: an ISC_MX8 x's group scales
@@ -568,11 +573,14 @@ int isc_w4_pack_codes(const isc_w4_desc *d, const uint8_t *codes, const uint8_t 
  *     ids[p], by isc_route's ids, offsets and order; rows of pairs with an id
  *     outside [0, E) are 0.
  *   y: T x N, or T*slots x N, of y_type (ISC_F32, ISC_F16, ISC_BF16).
- * One launch, no workspace.  Deterministic.
- * Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+ *   ws: isc_w4_linear_workspace_size bytes, 256-byte aligned.
+ * One launch, and one before it that lays x out where there is a workspace.
+ * Deterministic.
+ * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const void *x, int32_t x_type, int64_t ldx,
                   const void *x_scales, int64_t ld_scales, int32_t slots, const int32_t *ids, const int32_t *offsets,
-                  const int32_t *order, void *y, int32_t y_type, int64_t ldy, int32_t relu, void *stream);
+                  const int32_t *order, void *y, int32_t y_type, int64_t ldy, int32_t relu, void *ws,
+                  size_t ws_bytes, void *stream);
 
 /* Bytes of workspace of isc_w4_skip.  Host-only.
  * Errors: NULL, SHAPE, LIMIT, ARG. */

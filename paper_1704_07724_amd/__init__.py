@@ -54,7 +54,8 @@ EXPORTS = ("isc_out_shape", "isc_workspace_size", "isc_conv2d", "isc_conv2d_tune
            "isc_conv2d_dw_workspace_size", "isc_conv2d_dw",
            "isc_rmsnorm", "isc_rmsnorm_bwd_workspace_size", "isc_rmsnorm_bwd",
            "isc_route_workspace_size", "isc_route", "isc_route_bwd",
-           "isc_w4_size", "isc_w4_quantize", "isc_w4_pack_codes", "isc_w4_linear",
+           "isc_w4_size", "isc_w4_quantize", "isc_w4_pack_codes",
+           "isc_w4_linear_workspace_size", "isc_w4_linear",
            "isc_w4_skip_workspace_size", "isc_w4_skip",
            "isc_status_str", "isc_version")
 

@@ -243,8 +243,11 @@ struct W4Args {
     const float *weights;
     void *y;
     float *part;
+    uint8_t *columns;  // w4_linear_column_bytes() of room for x as matrix operands
     bool whole;  // every row of x 16-byte aligned, and of an 8-bit x's scales 4-byte
+    bool whole_y;  // four consecutive outputs of a row can be stored at once
 };
+size_t w4_linear_column_bytes(const W4Shape &w, int T, int xtype, int slots);
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);
 // Ranges that the skipping product's inputs are cut into (each a row of sums
 // in `part` where there are several).

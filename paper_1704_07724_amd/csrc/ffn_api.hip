@@ -234,18 +234,29 @@ int isc_w4_pack_codes(const isc_w4_desc *d, const uint8_t *codes, const uint8_t 
                                           static_cast<hipStream_t>(stream)));
 }
 
-int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const void *x, int32_t x_type, int64_t ldx,
-                  const void *x_scales, int64_t ld_scales, int32_t slots, const int32_t *ids, const int32_t *offsets,
-                  const int32_t *order, void *y, int32_t y_type, int64_t ldy, int32_t relu, void *stream) {
+int isc_w4_linear_workspace_size(const isc_w4_desc *d, int32_t T, int32_t x_type, int32_t slots, size_t *bytes) {
+    if (!bytes) return ISC_ERR_NULL;
     isc::W4Shape w;
     if (const int st = check_w4(d, &w)) return st;
     if (T < 0 || slots < 0) return ISC_ERR_SHAPE;
-    if (d->layout != ISC_W4_TILES || (!element_type(x_type) && x_type != ISC_MX8) || !element_type(y_type) ||
-        (slots == 0 && w.E != 1))
-        return ISC_ERR_ARG;
+    if (!element_type(x_type) && x_type != ISC_MX8) return ISC_ERR_ARG;
     if (T > kMaxTokens || slots > kMaxSlots) return ISC_ERR_LIMIT;
+    *bytes = isc::w4_linear_column_bytes(w, T, x_type, slots);
+    return ISC_OK;
+}
+
+int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const void *x, int32_t x_type, int64_t ldx,
+                  const void *x_scales, int64_t ld_scales, int32_t slots, const int32_t *ids, const int32_t *offsets,
+                  const int32_t *order, void *y, int32_t y_type, int64_t ldy, int32_t relu, void *ws, size_t ws_bytes,
+                  void *stream) {
+    size_t need = 0;
+    if (const int st = isc_w4_linear_workspace_size(d, T, x_type, slots, &need)) return st;
+    isc::W4Shape w;
+    if (const int st = check_w4(d, &w)) return st;
+    if (d->layout != ISC_W4_TILES || !element_type(y_type) || (slots == 0 && w.E != 1)) return ISC_ERR_ARG;
     if (T == 0) return ISC_OK;
-    if (!packed || !x || !y || (x_type == ISC_MX8) != (x_scales != nullptr) || (slots && (!ids || !offsets || !order)))
+    if (!packed || !x || !y || (x_type == ISC_MX8) != (x_scales != nullptr) ||
+        (slots && (!ids || !offsets || !order)) || (need && !ws))
         return ISC_ERR_NULL;
     const int64_t rows = slots ? static_cast<int64_t>(T) * slots : T;
     const Span in[6] = {{x, T, w.K, ldx, type_bytes(x_type)},
@@ -254,17 +265,29 @@ int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const voi
                         flat(slots ? ids : nullptr, rows, 4),
                         flat(slots ? offsets : nullptr, w.E + 1, 4),
                         flat(slots ? order : nullptr, rows, 4)};
-    const Span out = {y, rows, w.N, ldy, type_bytes(y_type)};
-    if (!in[0].shape_ok() || !in[1].shape_ok() || !out.shape_ok()) return ISC_ERR_SHAPE;
+    const Span out[2] = {{y, rows, w.N, ldy, type_bytes(y_type)},
+                         flat(need ? ws : nullptr, static_cast<int64_t>(need), 1)};
+    if (!in[0].shape_ok() || !in[1].shape_ok() || !out[0].shape_ok()) return ISC_ERR_SHAPE;
     if (!aligned(x, type_bytes(x_type)) || !aligned(packed, kAlign) || !aligned(y, type_bytes(y_type)) ||
+        (need && !aligned(ws, kAlign)) ||
         (slots && (!aligned(ids, 4) || !aligned(offsets, 4) || !aligned(order, 4))))
         return ISC_ERR_ALIGN;
-    for (const Span &s : in)
-        if (overlap(out, s)) return ISC_ERR_ALIAS;
+    if (ws_bytes < need) return ISC_ERR_WORKSPACE;
+    for (const Span &o : out)
+        for (const Span &s : in)
+            if (overlap(o, s)) return ISC_ERR_ALIAS;
+    if (overlap(out[0], out[1])) return ISC_ERR_ALIAS;
     if (const int st = isc::require_gfx950()) return st;
-    const isc::W4Args a{w, static_cast<const uint8_t *>(packed), x, static_cast<const uint8_t *>(x_scales), ldx,
-                        ld_scales, ldy, T, slots, x_type, y_type, relu != 0, ids, offsets, order, nullptr, y, nullptr,
-                        in[0].whole() && (x_type != ISC_MX8 || (aligned(x_scales, 4) && ld_scales % 4 == 0))};
+    isc::W4Args a{};
+    a.w = w;
+    a.packed = static_cast<const uint8_t *>(packed);
+    a.x = x, a.ldx = ldx, a.xtype = x_type;
+    a.xs = static_cast<const uint8_t *>(x_scales), a.ldxs = ld_scales;
+    a.T = T, a.slots = slots, a.ids = ids, a.offsets = offsets, a.order = order;
+    a.y = y, a.ldy = ldy, a.ytype = y_type, a.relu = relu != 0;
+    a.columns = static_cast<uint8_t *>(ws);
+    a.whole = in[0].whole() && (x_type != ISC_MX8 || (aligned(x_scales, 4) && ld_scales % 4 == 0));
+    a.whole_y = aligned(y, 4 * type_bytes(y_type)) && ldy % 4 == 0;
     return hip_status(isc::launch_w4_linear(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -307,8 +330,14 @@ int isc_w4_skip(const isc_w4_desc *d, const void *packed, int32_t T, const void 
             if (overlap(o, s)) return ISC_ERR_ALIAS;
     if (overlap(out[0], out[1])) return ISC_ERR_ALIAS;
     if (const int st = isc::require_gfx950()) return st;
-    const isc::W4Args a{w, static_cast<const uint8_t *>(packed), x, nullptr, ldx, 0, ldy, T, slots, x_type, y_type, 0,
-                        ids, nullptr, nullptr, weights, y, static_cast<float *>(ws), in[0].whole()};
+    isc::W4Args a{};
+    a.w = w;
+    a.packed = static_cast<const uint8_t *>(packed);
+    a.x = x, a.ldx = ldx, a.xtype = x_type;
+    a.T = T, a.slots = slots, a.ids = ids, a.weights = weights;
+    a.y = y, a.ldy = ldy, a.ytype = y_type;
+    a.part = static_cast<float *>(ws);
+    a.whole = in[0].whole();
     return hip_status(isc::launch_w4_skip(a, static_cast<hipStream_t>(stream)));
 }
 

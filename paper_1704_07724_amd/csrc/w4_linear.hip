@@ -27,20 +27,23 @@ using f32x4 = float __attribute__((ext_vector_type(4)));
 using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 
-constexpr int kMx8 = 0, kBf16 = 1, kF16 = 2, kF32 = 3;  // how x is fed
+// How x is fed: from its rows as they stand, or (from kPacked on, one, two or
+// three parts a value) as pack_x_kernel has laid its columns out.
+constexpr int kMx8 = 0, kBf16 = 1, kF16 = 2, kF32 = 3, kPacked = 4;
 template <int MODE>
-constexpr int kParts = MODE == kF32 ? 3 : MODE == kF16 ? 2 : 1;
+constexpr int kParts = MODE >= kPacked ? MODE - kPacked + 1 : MODE == kF32 ? 3 : MODE == kF16 ? 2 : 1;
 template <int MODE>
 constexpr int kTokens = 16 / kParts<MODE>;
 // 16- and 32-bit floats other than bfloat16 go through LDS, cut into parts once.
 template <int MODE>
-constexpr bool kStaged = MODE >= kF16;
+constexpr bool kStaged = MODE == kF16 || MODE == kF32;
 // 32-bit words of a step's inputs that a lane loads: a column's 32 inputs as they
 // stand, or for a staged type two neighbouring inputs of every token.
 template <int MODE>
-constexpr int kWords = MODE == kMx8 ? 8 : MODE == kBf16 ? 16 : MODE == kF16 ? kTokens<kF16> : 2 * kTokens<kF32>;
+constexpr int kWords = MODE == kMx8 ? 8 : MODE == kF16 ? kTokens<kF16> : MODE == kF32 ? 2 * kTokens<kF32> : 16;
 constexpr int kStageRow = 272;  // bytes of a staged column's 128 inputs; 16 spare spread the columns over the banks
 constexpr int kStageTile = 16 * kStageRow;
+constexpr int kSumTile = 4 * 17;  // a tile's sums, four outputs each, with a spare one a row for the banks
 
 // One step's operands of a wavefront, as loaded.
 template <int MODE, int NT, int MT>
@@ -135,7 +138,7 @@ __device__ __forceinline__ void cut(uint32_t (&w)[P], float a, float b) {
 // The bfloat16 operand of eight inputs of a column.
 template <int MODE>
 __device__ __forceinline__ bf16x8 operand(const uint32_t *x, uint32_t sx, int j) {
-    if constexpr (MODE == kBf16) {
+    if constexpr (MODE != kMx8) {
         return __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
     } else {
         const float s = scale_word(sx, j);
@@ -155,11 +158,32 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t w, float s) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
+__device__ __forceinline__ uint32_t word_of(const uint4 &q, int j) {
+    return j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w;
+}
+
+// Four consecutive outputs, `n` of them there.
+__device__ __forceinline__ void store4_as(void *y, int64_t at, const f32x4 &v, int64_t n, int type, bool whole) {
+    if (!whole || n < 4) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (c < n) store_as(y, at + c, v[c], type);
+    } else if (type == ISC_F32) {
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(y) + at) = v;
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = type == ISC_BF16 ? BF16::narrow(v[c]) : F16::narrow(v[c]);
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(y) + at) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    }
+}
+
 template <int MODE, int NT, int MT, int DEPTH, int THREADS>
 __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
     constexpr int TOK = kTokens<MODE>, P = kParts<MODE>;
     constexpr int kSize = MODE == kF32 ? 4 : MODE == kMx8 ? 1 : 2;
-    extern __shared__ f32x4 sums[];  // [wavefronts][NT][64], a tile of columns at a time; then the staged columns
+    constexpr int ROUND = MT < 2 ? MT : 2;  // tiles of columns whose sums are in LDS together
+    extern __shared__ f32x4 sums[];         // [wavefronts][NT][ROUND][kSumTile]; then the staged columns
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, col = lane & 15;
@@ -212,13 +236,14 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
             s.sw[i] = *reinterpret_cast<const uint32_t *>(scales[i] + static_cast<uint32_t>(step * 64 + col * 4));
         }
     };
-    const int full = a.whole ? a.w.K / 128 : 0;  // steps whose inputs are all there, and aligned
+    // steps whose inputs are all there, and aligned
+    const int full = MODE >= kPacked ? steps : a.whole ? a.w.K / 128 : 0;
 
     for (int64_t r0 = first; r0 < last; r0 += TOK * MT) {
         S ring[DEPTH];
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
-            if (wave + d * waves < full) load_w(ring[d], wave + d * waves);
+        for (int d = 0; d < DEPTH; ++d)  // weights first: they wait for nothing
+            if (full > wave) load_w(ring[d], wave + d * waves < full ? wave + d * waves : wave);
         // a direct type's lane owns a column of each tile, a row of x; columns past
         // the last row read it again, and nothing reads their sums
         const uint8_t *xrow[kStaged<MODE> ? TOK * MT : MT], *srow[MODE == kMx8 ? MT : 1];
@@ -226,6 +251,13 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
 #pragma unroll
             for (int t = 0; t < TOK * MT; ++t)
                 xrow[t] = static_cast<const uint8_t *>(a.x) + (r0 + t < last ? row_of(r0 + t) : 0) * a.ldx * kSize;
+        } else if constexpr (MODE >= kPacked) {
+            const int64_t tiles = (a.T + TOK - 1) / TOK;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const int64_t tile = r0 / TOK + m;
+                xrow[m] = a.columns + (tile < tiles ? tile : tiles - 1) * steps * 4096;
+            }
         } else {
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -244,6 +276,16 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
                     for (int t = 0; t < TOK; ++t)
                         if (r0 + m * TOK + t < last)
                             load_pair<MODE, kWhole>(s.x[m] + t * per, xrow[m * TOK + t], step * 128 + 2 * lane, a.w.K);
+                } else if constexpr (MODE >= kPacked) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(
+                            xrow[m] + static_cast<uint32_t>(step * 4096 + j * 1024 + lane * 16));
+                        s.x[m][4 * j] = v.x;
+                        s.x[m][4 * j + 1] = v.y;
+                        s.x[m][4 * j + 2] = v.z;
+                        s.x[m][4 * j + 3] = v.w;
+                    }
                 } else {
                     load_column<MODE, kWhole>(s.x[m], xrow[m], step * 128 + 8 * g, a.w.K);
                 }
@@ -257,12 +299,13 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
             }
         };
         f32x4 acc[NT][MT] = {};
-        const auto multiply = [&](const S &s) {
+        bf16x8 w8[NT];  // the weights of a step's first word
+        const auto multiply = [&](const S &s, const S &after) {
             uint8_t *stage = nullptr;
             if constexpr (kStaged<MODE>) {
                 // the wavefront's own columns: no other reads or writes them
                 constexpr int per = kWords<MODE> / TOK;
-                stage = reinterpret_cast<uint8_t *>(sums + waves * NT * 64) + wave * (MT * kStageTile);
+                stage = reinterpret_cast<uint8_t *>(sums + waves * NT * ROUND * kSumTile) + wave * (MT * kStageTile);
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
@@ -286,11 +329,13 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                // the next word's weights are widened between this word's products
                 bf16x8 f[NT];
 #pragma unroll
-                for (int i = 0; i < NT; ++i)
-                    f[i] = widen8(j == 0 ? s.q[i].x : j == 1 ? s.q[i].y : j == 2 ? s.q[i].z : s.q[i].w,
-                                  scale_word(s.sw[i], j));
+                for (int i = 0; i < NT; ++i) f[i] = w8[i];
+                const S &from = j < 3 ? s : after;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) w8[i] = widen8(word_of(from.q[i], (j + 1) & 3), scale_word(from.sw[i], (j + 1) & 3));
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     bf16x8 b;
@@ -302,55 +347,125 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
                     for (int i = 0; i < NT; ++i)
                         acc[i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], b, acc[i][m], 0, 0, 0);
                 }
+                if constexpr (MT * NT >= 4) {
+#pragma unroll
+                    for (int i = 0; i < MT * NT; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // a matrix instruction,
+                        __builtin_amdgcn_sched_group_barrier(0x002, (24 + MT * NT - 1) / (MT * NT), 0);  // its share of the rest
+                    }
+                }
             }
         };
-        // steps wave, wave + waves, ...: DEPTH of them loaded ahead; a last step
-        // that is not full, and rows off 16-byte boundaries, value by value
+        const auto widen_first = [&](const S &s) {
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
-            if (wave + d * waves < full) load_x(ring[d], wave + d * waves, std::true_type{});
-        for (int step = wave; step < full; step += DEPTH * waves) {
+            for (int i = 0; i < NT; ++i) w8[i] = widen8(s.q[i].x, scale_word(s.sw[i], 0));
+        };
+        // steps wave, wave + waves, ...: DEPTH of them loaded ahead, without a branch
+        // around a load (past the last step it is loaded again), so that a wait
+        // counts the loads behind it and leaves them in flight; a last step that is
+        // not full, and rows off 16-byte boundaries, value by value
+        const int mine = full > wave ? (full - wave + waves - 1) / waves : 0;
+        if (mine > 0) {
+            const auto step_of = [&](int i) { return wave + (i < mine ? i : mine - 1) * waves; };
 #pragma unroll
-            for (int d = 0; d < DEPTH; ++d) {
-                const int now = step + d * waves, next = now + DEPTH * waves;
-                if (now < full) multiply(ring[d]);
-                if (next < full) {
+            for (int d = 0; d < DEPTH; ++d) load_x(ring[d], step_of(d), std::true_type{});
+            __builtin_amdgcn_sched_barrier(0);
+            widen_first(ring[0]);
+            int i = 0;
+            for (; i + DEPTH <= mine; i += DEPTH) {
+#pragma unroll
+                for (int d = 0; d < DEPTH; ++d) {
+                    multiply(ring[d], ring[(d + 1) % DEPTH]);
+                    const int next = step_of(i + d + DEPTH);
                     load_w(ring[d], next);
                     load_x(ring[d], next, std::true_type{});
+                    __builtin_amdgcn_sched_barrier(0);  // the loads stay here, a ring ahead of their use
                 }
             }
-        }
-        for (int rest = full + (wave + waves - full % waves) % waves; rest < steps; rest += waves) {
-            load_w(ring[0], rest);
-            load_x(ring[0], rest, std::false_type{});
-            multiply(ring[0]);
-        }
-        // add the wavefronts' sums up and the parts, and store
-        const float *flat = reinterpret_cast<const float *>(sums);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            __syncthreads();  // what was there is stored
+            for (int d = 0; d < DEPTH - 1; ++d)
+                if (i + d < mine) multiply(ring[d], ring[d + 1]);
+        }
+        if constexpr (MODE < kPacked)
+            for (int rest = full + (wave + waves - full % waves) % waves; rest < steps; rest += waves) {
+                load_w(ring[0], rest);
+                load_x(ring[0], rest, std::false_type{});
+                widen_first(ring[0]);
+                multiply(ring[0], ring[0]);
+            }
+        // add the wavefronts' sums up and the parts, and store: a thread four
+        // outputs of a token, neighbouring threads neighbouring outputs
 #pragma unroll
-            for (int i = 0; i < NT; ++i) sums[(wave * NT + i) * 64 + lane] = acc[i][m];
+        for (int m0 = 0; m0 < MT; m0 += ROUND) {
+            if (m0 > 0 || r0 > first) __syncthreads();  // what was there is stored
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int m = 0; m < ROUND; ++m)
+                    sums[((wave * NT + i) * ROUND + m) * kSumTile + g * 17 + col] = acc[i][m0 + m];
             __syncthreads();
-            for (int o = threadIdx.x; o < NT * TOK * 16; o += blockDim.x) {
-                const int n = o & 15, t = (o >> 4) % TOK, i = (o >> 4) / TOK;
-                const int64_t r = r0 + m * TOK + t, out = (tile0 + i) * 16 + n;
+            for (int o = threadIdx.x; o < ROUND * TOK * NT * 4; o += blockDim.x) {
+                const int quad = o % (NT * 4), t = o / (NT * 4) % TOK, m = o / (NT * 4) / TOK, i = quad >> 2;
+                const int64_t r = r0 + (m0 + m) * TOK + t, out = tile0 * 16 + quad * 4;
                 if (r >= last || out >= a.w.N) continue;
-                float v = 0.0f;
+                f32x4 v = {};
 #pragma unroll
                 for (int part = P - 1; part >= 0; --part) {
-                    float u = 0.0f;
+                    f32x4 u = {};
                     for (int z = 0; z < waves; ++z)
-                        u += flat[((z * NT + i) * 64 + (n >> 2) * 16 + t * P + part) * 4 + (n & 3)];
+                        u += sums[((z * NT + i) * ROUND + m) * kSumTile + (quad & 3) * 17 + t * P + part];
                     v += u;
                 }
-                if (a.relu && v <= 0.0f) v = 0.0f;
+                if (a.relu)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[c] = v[c] <= 0.0f ? 0.0f : v[c];
                 const int64_t p = a.slots ? a.order[r] : r;
-                if (p >= 0 && p < all) store_as(a.y, p * a.ldy + out, v, a.ytype);
+                if (p >= 0 && p < all) store4_as(a.y, p * a.ldy + out, v, a.w.N - out, a.ytype, a.whole_y);
             }
         }
     }
+}
+
+// x as matrix operands: for every tile of 16 columns, step of 128 inputs and
+// word j of the weights' layout, 16 bytes a lane.  One thread each; inputs past
+// K are 0, so the product needs no last step of its own.
+template <int XTYPE>
+__global__ void __launch_bounds__(256) pack_x_kernel(W4Args a) {
+    constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, TOK = 16 / P;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t steps = a.w.steps(), tiles = (a.T + TOK - 1) / TOK;
+    if (item >= tiles * steps * 256) return;
+    const int lane = static_cast<int>(item & 63), j = static_cast<int>(item >> 6 & 3);
+    const int64_t tile = (item >> 8) / steps;
+    const int step = static_cast<int>((item >> 8) % steps);
+    const int col = lane & 15, k = step * 128 + j * 32 + (lane >> 4) * 8;
+    const int64_t t = tile * TOK + col / P;
+    uint32_t out[4] = {0u, 0u, 0u, 0u};
+    const int n = t < a.T && col < TOK * P ? a.w.K - k : 0;
+    if (n > 0) {
+        if constexpr (XTYPE == ISC_MX8) {
+            const uint8_t *p = static_cast<const uint8_t *>(a.x) + t * a.ldx + k;
+            uint32_t v[2] = {0u, 0u};
+            for (int i = 0; i < 8; ++i)
+                if (i < n) v[i / 4] |= static_cast<uint32_t>(p[i]) << (8 * (i & 3));
+            const bf16x8 b = operand<kMx8>(v, a.xs[t * a.ldxs + k / 32], 0);
+            const uint4 u = __builtin_bit_cast(uint4, b);
+            out[0] = u.x, out[1] = u.y, out[2] = u.z, out[3] = u.w;
+        } else {
+            using T = std::conditional_t<XTYPE == ISC_F32, F32, std::conditional_t<XTYPE == ISC_F16, F16, BF16>>;
+            float v[8];
+            load8<T>(v, static_cast<const typename T::type *>(a.x) + t * a.ldx + k, n, a.whole && n >= 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t parts[P];
+                cut<P>(parts, v[2 * i], v[2 * i + 1]);
+                out[i] = parts[0];
+                if (P > 1 && col % P == 1) out[i] = parts[P > 1 ? 1 : 0];
+                if (P > 2 && col % P == 2) out[i] = parts[P > 2 ? 2 : 0];
+            }
+        }
+    }
+    reinterpret_cast<uint4 *>(a.columns)[item] = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
 template <int MODE, int NT, int MT, int DEPTH, int THREADS>
@@ -358,37 +473,70 @@ hipError_t run(const W4Args &a, int waves, hipStream_t s) {
     const int64_t tiles = (a.w.tiles() + NT - 1) / NT;
     const int64_t rows = kTokens<MODE> * MT;
     const unsigned y = static_cast<unsigned>(a.slots ? a.w.E + 1 : (a.T + rows - 1) / rows);
-    if (waves > THREADS / 64) waves = THREADS / 64;
-    const size_t lds = static_cast<size_t>(waves) * (sizeof(f32x4) * 64 * NT + (kStaged<MODE> ? MT * kStageTile : 0));
+    while (waves > 1 && waves / 2 >= a.w.steps()) waves /= 2;  // no more wavefronts than steps
+    const size_t lds = static_cast<size_t>(waves) * (sizeof(f32x4) * kSumTile * NT * (MT < 2 ? MT : 2) + (kStaged<MODE> ? MT * kStageTile : 0));
     w4_linear_kernel<MODE, NT, MT, DEPTH, THREADS>
         <<<dim3(static_cast<unsigned>(tiles), y), dim3(static_cast<unsigned>(64 * waves)), lds, s>>>(a);
     return hipGetLastError();
 }
 
+int parts_of(int xtype) { return xtype == ISC_F32 ? 3 : xtype == ISC_F16 ? 2 : 1; }
+
+// Whether x is laid out first: where its columns fill more than one tile.
+bool packs(int T, int xtype, int slots) { return slots == 0 && T > 16 / parts_of(xtype); }
+
+// Tiles of outputs a wavefront keeps (NT), wavefronts that share the inputs and
+// steps loaded ahead, by the workgroups there are to fill 256 compute units
+// with.  Few tiles: one each.  From 512 on two, so that x is read half as often
+// (8192 x 16384, one bfloat16 token: 13.1 us against 14.7), with 1024 and more
+// columns than a few four (16 tokens: 16.1 us against 21.9).  Four wavefronts a
+// workgroup rather than eight (4096 x 4096, one token: 4.2 us against 4.8), but
+// for long rows (9216 x 4096: 6.6 us against 7.4).  An expert has few rows and
+// many experts run: four tiles, or two where a token is alone (64 experts of
+// 2048 x 1408: 16 tokens 18.9 us against 20.8, one token 8.3 against 7.5).
 template <int MODE>
-hipError_t by_tokens(const W4Args &a, hipStream_t s) {
-    const int64_t rows = a.slots ? (static_cast<int64_t>(a.T) * a.slots + a.w.E - 1) / a.w.E : a.T;
-    int waves = 1;
-    while (waves < 8 && waves < a.w.steps()) waves *= 2;
+hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
+    const int64_t tiles = a.w.tiles(), steps = a.w.steps();
     if constexpr (kStaged<MODE>) {
-        if (rows <= kTokens<MODE>) return run<MODE, 1, 1, 4, 512>(a, waves, s);
-        return run<MODE, 4, 2, 2, 256>(a, waves, s);
+        // 8192 x 16384, one fp32 token: 15.1 us against 18.2 with one tile
+        if (tiles >= 512) return run<MODE, 2, 1, 2, 512>(a, 8, s);
+        return run<MODE, 1, 1, 4, 512>(a, 8, s);
     } else {
-        if (a.slots && rows <= kTokens<MODE>) return run<MODE, 1, 1, 2, 256>(a, waves, s);
-        if (rows <= kTokens<MODE>) return run<MODE, 1, 1, 4, 512>(a, waves, s);
-        if (rows <= 2 * kTokens<MODE>) return run<MODE, 2, 2, 2, 512>(a, waves, s);
-        return run<MODE, 4, 4, 2, 256>(a, waves, s);
+        if (a.slots) return a.T > 4 ? run<MODE, 4, 1, 1, 256>(a, 4, s) : run<MODE, 2, 1, 2, 256>(a, 4, s);
+        if (tiles >= 1024 && a.T > 4) return run<MODE, 4, 1, 2, 256>(a, 4, s);
+        if (tiles >= 512) return run<MODE, 2, 1, 2, 256>(a, 4, s);
+        if (steps > 48) return run<MODE, 1, 1, 2, 512>(a, 8, s);
+        return run<MODE, 1, 1, 2, 256>(a, 4, s);
     }
+}
+
+template <int XTYPE>
+hipError_t packed(const W4Args &a, hipStream_t s) {
+    constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, MODE = kPacked + P - 1;
+    const int64_t tiles = (a.T + kTokens<MODE> - 1) / kTokens<MODE>;
+    pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (tiles <= 2) return run<MODE, 2, 2, 2, 512>(a, 8, s);
+    return run<MODE, 4, 4, 2, 256>(a, 4, s);
 }
 
 }  // namespace
 
+size_t w4_linear_column_bytes(const W4Shape &w, int T, int xtype, int slots) {
+    if (!packs(T, xtype, slots)) return 0;
+    const int tokens = 16 / parts_of(xtype);
+    return static_cast<size_t>((T + tokens - 1) / tokens) * static_cast<size_t>(w.steps()) * 4096;
+}
+
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t s) {
+    // a workgroup never spans more tokens than its tiles of columns hold, so one
+    // tile is the limit of the rows as they stand
+    const bool pack = packs(a.T, a.xtype, a.slots);
     switch (a.xtype) {
-    case ISC_MX8: return by_tokens<kMx8>(a, s);
-    case ISC_BF16: return by_tokens<kBf16>(a, s);
-    case ISC_F16: return by_tokens<kF16>(a, s);
-    default: return by_tokens<kF32>(a, s);
+    case ISC_MX8: return pack ? packed<ISC_MX8>(a, s) : rows_as_they_stand<kMx8>(a, s);
+    case ISC_BF16: return pack ? packed<ISC_BF16>(a, s) : rows_as_they_stand<kBf16>(a, s);
+    case ISC_F16: return pack ? packed<ISC_F16>(a, s) : rows_as_they_stand<kF16>(a, s);
+    default: return pack ? packed<ISC_F32>(a, s) : rows_as_they_stand<kF32>(a, s);
     }
 }
 

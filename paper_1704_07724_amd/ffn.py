@@ -21,6 +21,8 @@ import paper_1704_07724_amd as _isc
 F32, F16, BF16, MX8 = 0, 1, 2, 3
 SCORES = {"softmax": 0, "sigmoid": 1}
 LAYOUTS = {"tiles": 0, "rows": 1}
+# Tokens up to which isc_w4_linear has no workspace, by type.
+COLUMNS = {F32: 5, F16: 8, BF16: 16, MX8: 16}
 
 
 class W4Desc(ctypes.Structure):
@@ -72,7 +74,8 @@ def declare(L):
     L.isc_w4_size.argtypes = [dp, szp]
     L.isc_w4_quantize.argtypes = [dp, vp, i32, i64, vp, vp, vp]
     L.isc_w4_pack_codes.argtypes = [dp, vp, vp, vp, vp]
-    L.isc_w4_linear.argtypes = [dp, vp, i32, vp, i32, i64, vp, i64, i32, vp, vp, vp, vp, i32, i64, i32, vp]
+    L.isc_w4_linear_workspace_size.argtypes = [dp, i32, i32, i32, szp]
+    L.isc_w4_linear.argtypes = [dp, vp, i32, vp, i32, i64, vp, i64, i32, vp, vp, vp, vp, i32, i64, i32, vp, sz, vp]
     L.isc_w4_skip_workspace_size.argtypes = [dp, i32, i32, szp]
     L.isc_w4_skip.argtypes = [dp, vp, i32, vp, i32, i64, i32, vp, vp, vp, i32, i64, vp, sz, vp]
 
@@ -391,7 +394,7 @@ def _routed(st, route, w4, T):
     return slots, _exact(ids, st.i32, (T, slots), "ids"), weights, offsets, order
 
 
-def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, stream=None):
+def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, ws=None, stream=None):
     """y = x w^T on 4-bit weights (layout "tiles"), with max(0, .) if relu.
 
     x: [..., K] float32, float16 or bfloat16, or an Mx8 (values, scales).
@@ -419,7 +422,7 @@ def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, stream=None):
         if route is not None and len(shape) != 2:
             raise ValueError("x must be [T, K] with a route")
         slots, ids, _, offsets, order = _routed(st, route, w4, T)
-        device = _device(st, x, scales, w4.data, ids, offsets, order)
+        device = _device(st, x, scales, w4.data, ids, offsets, order, ws)
         if slots:
             if offsets is None or order is None:
                 raise ValueError("the route has no lists")
@@ -427,10 +430,15 @@ def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, stream=None):
             order = _exact(order, st.i32, (T * slots,), "order")
         if dtype is None:
             dtype = st.torch.bfloat16 if code == MX8 else x.dtype
+        if ws is None and not slots and T > COLUMNS[code]:
+            n = ctypes.c_size_t()
+            _isc._check(st.lib.isc_w4_linear_workspace_size(w4.desc, T, code, slots, n), "isc_w4_linear_workspace_size")
+            ws = _bytes(st, n.value, x)
         y = st.torch.empty((T, slots, N) if slots else (*shape[:-1], N), dtype=dtype, device=x.device)
         status = st.lib.isc_w4_linear(
             w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, sp, lds, slots, _ptr(ids), _ptr(offsets),
-            _ptr(order), y.data_ptr(), _type(st, dtype, "dtype"), N, bool(relu), _stream(st, stream, device))
+            _ptr(order), y.data_ptr(), _type(st, dtype, "dtype"), N, bool(relu), _ptr(ws),
+            0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device))
         if status:
             _isc._check(status, "isc_w4_linear")
     return y

@@ -112,8 +112,9 @@ def test_w4_sizes_and_packing():
     assert quant(w=A + 2) == ALIGN and quant(c=A) == ALIAS and quant(s=B) == ALIAS
 
 
-def linear(d=desc(), p=A, T=3, x=B, xt=3, ldx=64, xs=C, lds=2, slots=0, ids=None, off=None, order=None, y=D, yt=2, ldy=32):
-    return isc.lib().isc_w4_linear(d, p, T, x, xt, ldx, xs, lds, slots, ids, off, order, y, yt, ldy, 0, None)
+def linear(d=desc(), p=A, T=3, x=B, xt=3, ldx=64, xs=C, lds=2, slots=0, ids=None, off=None, order=None, y=D, yt=2, ldy=32,
+           ws=None, n=0):
+    return isc.lib().isc_w4_linear(d, p, T, x, xt, ldx, xs, lds, slots, ids, off, order, y, yt, ldy, 0, ws, n, None)
 
 
 def test_linear_refusals():
@@ -126,6 +127,12 @@ def test_linear_refusals():
     assert linear(d=desc(layout=1)) == ARG and linear(yt=3) == ARG and linear(xt=4) == ARG and linear(d=desc(E=2)) == ARG
     assert linear(T=(1 << 20) + 1) == LIMIT and linear(**{**routed, "slots": 65}) == LIMIT
     assert linear(p=A + 16) == ALIGN and linear(xt=0, xs=None, x=B + 2) == ALIGN and linear(y=D + 1) == ALIGN
+    assert linear(T=17) == NULL and linear(T=17, ws=F, n=16) == WORKSPACE and linear(T=17, ws=F, n=1 << 20) in OK
+    assert linear(T=17, ws=F + 8, n=1 << 20) == ALIGN and linear(T=17, ws=B, n=1 << 20) == ALIAS
+    n = ctypes.c_size_t()
+    for xt, most in isc.ffn.COLUMNS.items():
+        assert isc.lib().isc_w4_linear_workspace_size(desc(), most, xt, 0, n) == 0 and n.value == 0
+        assert isc.lib().isc_w4_linear_workspace_size(desc(), most + 1, xt, 0, n) == 0 and n.value >= (most + 1) * 64 * 2
     assert linear(y=B) == ALIAS and linear(y=A) == ALIAS and linear(**{**routed, "y": E}) == ALIAS
 
 
