@@ -23,6 +23,9 @@ struct F16 {
         return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(b)));
     }
     static __device__ __forceinline__ uint32_t narrow(float v) {
+        // the fp32 value, rounded: not folded into the instruction that made it, whose
+        // one rounding would give another last bit from kernel to kernel
+        asm("" : "+v"(v));
         return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
     }
     static __device__ __forceinline__ float load(const uint16_t *p) { return widen(*p); }

@@ -2,10 +2,12 @@
 //
 //   h = x + r,  rstd = (mean(h^2) + eps)^(-1/2),  y = h rstd w
 //
-// One workgroup per row, the row in registers: eight consecutive values per
-// thread and chunk, so x and r are read once, and a group of 32 outputs (the
-// 8-bit form's unit) lies in four neighbouring lanes.  Sums are fp32; h is
-// normalised as it was added, before its rounding to x's type.
+// One workgroup per row, the row in registers, so x and r are read once: eight
+// consecutive values per thread and chunk, a group of 32 outputs (the 8-bit
+// form's unit) in four neighbouring lanes.  Rows that do not all start on 16
+// bytes are read value by value, neighbouring lanes neighbouring values, and
+// change places within a wavefront through LDS; the sums are the same.  Sums are
+// fp32; h is normalised as it was added, before its rounding to x's type.
 //
 // The gradient, with n = h rstd and g = dy w:
 //   dx = rstd (g - n mean(g n)) + dh,   dw = sum over rows of dy n
@@ -28,129 +30,186 @@ __device__ __forceinline__ float block_sum(float v, float *sums) {
     return t;
 }
 
-__device__ __forceinline__ void load_weight8(float (&w)[8], const void *p, int64_t i, int n, int type, bool whole) {
-    if (type == ISC_F32)
-        load8<F32>(w, static_cast<const float *>(p) + i, n, whole);
-    else if (type == ISC_BF16)
-        load8<BF16>(w, static_cast<const uint16_t *>(p) + i, n, whole);
-    else
-        load8<F16>(w, static_cast<const uint16_t *>(p) + i, n, whole);
+// First of the eight values of a row that a thread holds in chunk c.
+__device__ __forceinline__ int at(int c) {
+    return (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
 }
 
-template <class T, int C>
+// A wavefront's 512 values of a chunk, lane by lane or value by value: in LDS of
+// its own, so only the order within the wavefront matters.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+struct Swap {
+    float v[16][512];
+    __device__ __forceinline__ float *mine() { return v[threadIdx.x >> 6]; }
+};
+
+// Chunk c of a row of D values, 0 where there are none (D is a multiple of 8 if WHOLE).
+template <class T, bool WHOLE>
+__device__ __forceinline__ void load_chunk(float (&v)[8], const typename T::type *row, int c, int D, Swap *swap) {
+    if constexpr (WHOLE) {
+        if (at(c) < D) {
+            load8<T>(v, row + at(c), 8, true);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    } else {
+        const int lane = threadIdx.x & 63, i = at(c) - lane * 8 + lane;
+        float u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = i + j * 64 < D ? T::load(row + i + j * 64) : 0.0f;
+        float *buf = swap->mine();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) buf[j * 64 + lane] = u[j];
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = buf[lane * 8 + j];
+        wave_fence();
+    }
+}
+template <class T, bool WHOLE>
+__device__ __forceinline__ void store_chunk(typename T::type *row, const float (&v)[8], int c, int D, Swap *swap) {
+    if constexpr (WHOLE) {
+        if (at(c) < D) store8<T>(row + at(c), v, 8, true);
+    } else {
+        const int lane = threadIdx.x & 63, i = at(c) - lane * 8 + lane;
+        float *buf = swap->mine();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) buf[lane * 8 + j] = v[j];
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j * 64 < D) store<T>(row + i + j * 64, buf[j * 64 + lane]);
+        wave_fence();
+    }
+}
+template <bool WHOLE>
+__device__ __forceinline__ void load_weight(float (&w)[8], const void *p, int c, int D, int type, Swap *swap) {
+    if (type == ISC_F32)
+        load_chunk<F32, WHOLE>(w, static_cast<const float *>(p), c, D, swap);
+    else if (type == ISC_BF16)
+        load_chunk<BF16, WHOLE>(w, static_cast<const uint16_t *>(p), c, D, swap);
+    else
+        load_chunk<F16, WHOLE>(w, static_cast<const uint16_t *>(p), c, D, swap);
+}
+
+// The 8-bit form of a chunk of outputs.  A group's largest magnitude is taken
+// as bits, under which NaN comes out above everything.
+template <bool WHOLE>
+__device__ __forceinline__ void store_mx8(uint8_t *q, uint8_t *scales, const float (&v)[8], int c, int D, Swap *swap) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = op_max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+    m = op_max(m, dpp<0xb1, 0xf>(m, m));              // quad_perm 1,0,3,2
+    m = op_max(m, dpp<0x4e, 0xf>(m, m));              // quad_perm 2,3,0,1
+    const uint32_t b = group_scale<8, 0x600000u>(m);  // 448 = 1.75 * 2^8
+    const float inv = __uint_as_float((254u - (b > 253u ? 253u : b)) << 23);
+    uint32_t lo = 0x7f7f7f7fu, hi = 0x7f7f7f7fu;
+    if (b != 255u) {
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, lo, true);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inv, v[5] * inv, 0, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, hi, true);
+    }
+    if constexpr (WHOLE) {
+        if (at(c) < D) *reinterpret_cast<uint2 *>(q + at(c)) = make_uint2(lo, hi);
+    } else {
+        const int lane = threadIdx.x & 63, i = at(c) - lane * 8 + lane;
+        uint2 *buf = reinterpret_cast<uint2 *>(swap->mine());
+        buf[lane] = make_uint2(lo, hi);
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j * 64 < D) q[i + j * 64] = reinterpret_cast<const uint8_t *>(buf)[j * 64 + lane];
+        wave_fence();
+    }
+    if ((threadIdx.x & 3) == 0 && at(c) < D) scales[at(c) / 32] = static_cast<uint8_t>(b);
+}
+
+template <class T, int C, bool WHOLE>
 __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
     using E = typename T::type;
     __shared__ float sums[16];
+    Swap *swap = nullptr;
+    if constexpr (!WHOLE) {
+        __shared__ Swap room;
+        swap = &room;
+    }
     const int64_t t = blockIdx.x;
-    const E *x = static_cast<const E *>(a.x) + t * a.ldx;
-    const E *r = a.r ? static_cast<const E *>(a.r) + t * a.ldr : nullptr;
-    float v[C][8];
+    float v[C][8], w[C][8];
     float ss = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int i = (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
-        const int n = a.D - i;
-        if (n > 0) {
-            load8<T>(v[c], x + i, n, a.whole);
-            if (r) {
-                float u[8];
-                load8<T>(u, r + i, n, a.whole);
+    for (int c = 0; c < C; ++c) load_chunk<T, WHOLE>(v[c], static_cast<const E *>(a.x) + t * a.ldx, c, a.D, swap);
+    if (a.r) {
+        float u[C][8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] += u[j];
-            }
-        } else {
+        for (int c = 0; c < C; ++c) load_chunk<T, WHOLE>(u[c], static_cast<const E *>(a.r) + t * a.ldr, c, a.D, swap);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = 0.0f;
-        }
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[c][j] += u[c][j];
     }
+    // short rows: the weight on its way while the sum is taken
+    if (C <= 2)
+#pragma unroll
+        for (int c = 0; c < C; ++c) load_weight<WHOLE>(w[c], a.w, c, a.D, a.wtype, swap);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int j = 0; j < 8; ++j) ss = fmaf(v[c][j], v[c][j], ss);
-    if (a.h) {
-        E *h = static_cast<E *>(a.h) + t * a.ldh;
+    if (a.h)
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int i = (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
-            if (i < a.D) store8<T>(h + i, v[c], a.D - i, a.whole);
-        }
-    }
+        for (int c = 0; c < C; ++c) store_chunk<T, WHOLE>(static_cast<E *>(a.h) + t * a.ldh, v[c], c, a.D, swap);
     const float mean = block_sum(ss, sums) / static_cast<float>(a.D);
     const float rstd = 1.0f / sqrtf(mean + a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[t] = rstd;
     if (!a.y && !a.q) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int i = (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
-        const int n = a.D - i;
-        float w[8];
-        if (n > 0)
-            load_weight8(w, a.w, i, n, a.wtype, a.whole);
-        else
+        if (C > 2) load_weight<WHOLE>(w[c], a.w, c, a.D, a.wtype, swap);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[c][j] = n > j ? v[c][j] * rstd * w[j] : 0.0f;
-        if (a.y && n > 0) store8<T>(static_cast<E *>(a.y) + t * a.ldy + i, v[c], n, a.whole);
-        if (!a.q) continue;
-        // four lanes hold a group; its largest magnitude as bits, under which
-        // NaN comes out above everything
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = op_max(m, __float_as_uint(v[c][j]) & 0x7fffffffu);
-        m = op_max(m, dpp<0xb1, 0xf>(m, m));  // quad_perm 1,0,3,2
-        m = op_max(m, dpp<0x4e, 0xf>(m, m));  // quad_perm 2,3,0,1
-        const uint32_t b = group_scale<8, 0x600000u>(m);  // 448 = 1.75 * 2^8
-        const float inv = __uint_as_float((254u - (b > 253u ? 253u : b)) << 23);
-        uint32_t lo = 0x7f7f7f7fu, hi = 0x7f7f7f7fu;
-        if (b != 255u) {
-            lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[c][0] * inv, v[c][1] * inv, 0, false);
-            lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[c][2] * inv, v[c][3] * inv, lo, true);
-            hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[c][4] * inv, v[c][5] * inv, 0, false);
-            hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[c][6] * inv, v[c][7] * inv, hi, true);
-        }
-        if (n <= 0) continue;
-        uint8_t *q = static_cast<uint8_t *>(a.q) + t * a.ldq + i;
-        if (a.whole) {
-            *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < n) q[j] = static_cast<uint8_t>((j < 4 ? lo : hi) >> (8 * (j & 3)));
-        }
-        if ((threadIdx.x & 3) == 0) static_cast<uint8_t *>(a.scales)[t * a.lds + i / 32] = static_cast<uint8_t>(b);
+        for (int j = 0; j < 8; ++j) v[c][j] = at(c) + j < a.D ? v[c][j] * rstd * w[c][j] : 0.0f;
+        if (a.y) store_chunk<T, WHOLE>(static_cast<E *>(a.y) + t * a.ldy, v[c], c, a.D, swap);
+        if (a.q)
+            store_mx8<WHOLE>(static_cast<uint8_t *>(a.q) + t * a.ldq, static_cast<uint8_t *>(a.scales) + t * a.lds, v[c],
+                             c, a.D, swap);
     }
 }
 
-template <class T, int C>
+template <class T, int C, bool WHOLE>
 __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
     using E = typename T::type;
     __shared__ float sums[2][16];
+    Swap *swap = nullptr;
+    if constexpr (!WHOLE) {
+        __shared__ Swap room;
+        swap = &room;
+    }
     float w[C][8], acc[C][8];
-    const auto at = [](int c) { return (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8; };
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+        load_weight<WHOLE>(w[c], a.w, c, a.D, a.wtype, swap);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[c][j] = acc[c][j] = 0.0f;
-        if (at(c) < a.D) load_weight8(w[c], a.w, at(c), a.D - at(c), a.wtype, a.whole);
+        for (int j = 0; j < 8; ++j) acc[c][j] = 0.0f;
     }
     int turn = 0;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x, turn ^= 1) {
-        const E *h = static_cast<const E *>(a.h) + t * a.ldh;
-        const E *dy = static_cast<const E *>(a.dy) + t * a.ldy;
-        const E *dh = a.dh ? static_cast<const E *>(a.dh) + t * a.ldd : nullptr;
         const float rstd = a.rstd[t];
         float n[C][8], g[C][8], d[C][8];
         float dot = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            load_chunk<T, WHOLE>(n[c], static_cast<const E *>(a.h) + t * a.ldh, c, a.D, swap);
+            load_chunk<T, WHOLE>(g[c], static_cast<const E *>(a.dy) + t * a.ldy, c, a.D, swap);
+            if (a.dh)
+                load_chunk<T, WHOLE>(d[c], static_cast<const E *>(a.dh) + t * a.ldd, c, a.D, swap);
+            else
 #pragma unroll
-            for (int j = 0; j < 8; ++j) n[c][j] = g[c][j] = d[c][j] = 0.0f;
-            if (at(c) < a.D) {
-                load8<T>(n[c], h + at(c), a.D - at(c), a.whole);
-                load8<T>(g[c], dy + at(c), a.D - at(c), a.whole);
-                if (dh) load8<T>(d[c], dh + at(c), a.D - at(c), a.whole);
-            }
+                for (int j = 0; j < 8; ++j) d[c][j] = 0.0f;
         }
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -164,14 +223,12 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
         // two sets of sums in turn: a row's are read before the row after the
         // next overwrites them, with the barrier of the row between
         const float mean = block_sum(dot, sums[turn]) / static_cast<float>(a.D);
-        E *dx = static_cast<E *>(a.dx) + t * a.ldx;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (at(c) >= a.D) continue;
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = fmaf(rstd, fmaf(-n[c][j], mean, g[c][j]), d[c][j]);
-            store8<T>(dx + at(c), o, a.D - at(c), a.whole);
+            store_chunk<T, WHOLE>(static_cast<E *>(a.dx) + t * a.ldx, o, c, a.D, swap);
         }
     }
     float *part = a.part + static_cast<int64_t>(blockIdx.x) * a.D;
@@ -182,21 +239,27 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
             if (at(c) + j < a.D) part[at(c) + j] = acc[c][j];
 }
 
-// dw[i] = sum of part[b][i] over b: 64 columns a workgroup, 16 wavefronts
-// each a sixteenth of the rows, in order.
+// dw[i] = sum of part[b][i] over b: 32 columns a workgroup, each of its 32 half
+// wavefronts every 32nd row, eight loads in flight; then the halves in order.
 __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int rows, int D, float *dw) {
-    __shared__ float s[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i = blockIdx.x * 64 + lane;
+    __shared__ float s[32][33];
+    const int lane = threadIdx.x & 31, half = threadIdx.x >> 5;
+    const int i = blockIdx.x * 32 + lane;
+    const float *p = part + (i < D ? i : D - 1);
     float t = 0.0f;
-    if (i < D)
-        for (int b = wave; b < rows; b += 16) t += part[static_cast<int64_t>(b) * D + i];
-    s[wave][lane] = t;
+    for (int b = half; b < rows; b += 256) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = p[static_cast<int64_t>(b + 32 * j < rows ? b + 32 * j : b) * D];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t += b + 32 * j < rows ? v[j] : 0.0f;
+    }
+    s[half][lane] = t;
     __syncthreads();
-    if (wave == 0 && i < D) {
+    if (half == 0 && i < D) {
         float u = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) u += s[w][lane];
+        for (int h = 0; h < 32; ++h) u += s[h][lane];
         dw[i] = u;
     }
 }
@@ -214,50 +277,59 @@ RowPlan row_plan(int D, int most) {
     return {threads, chunks};
 }
 
-template <class T>
+template <class T, bool WHOLE>
 hipError_t norm_of(const NormArgs &a, hipStream_t s) {
     const RowPlan p = row_plan(a.D, 1024);
     const dim3 grid(static_cast<unsigned>(a.T)), block(static_cast<unsigned>(p.threads));
     switch (p.chunks) {
-    case 1: rmsnorm_kernel<T, 1><<<grid, block, 0, s>>>(a); break;
-    case 2: rmsnorm_kernel<T, 2><<<grid, block, 0, s>>>(a); break;
-    case 4: rmsnorm_kernel<T, 4><<<grid, block, 0, s>>>(a); break;
-    default: rmsnorm_kernel<T, 8><<<grid, block, 0, s>>>(a); break;
+    case 1: rmsnorm_kernel<T, 1, WHOLE><<<grid, block, 0, s>>>(a); break;
+    case 2: rmsnorm_kernel<T, 2, WHOLE><<<grid, block, 0, s>>>(a); break;
+    case 4: rmsnorm_kernel<T, 4, WHOLE><<<grid, block, 0, s>>>(a); break;
+    default: rmsnorm_kernel<T, 8, WHOLE><<<grid, block, 0, s>>>(a); break;
     }
     return hipGetLastError();
 }
 
-template <class T>
+template <class T, bool WHOLE>
 hipError_t norm_bwd_of(const NormBwdArgs &a, hipStream_t s) {
     const RowPlan p = row_plan(a.D, 1024);
     const int blocks = norm_bwd_blocks(a.T, a.D);
     const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(p.threads));
-    switch (p.chunks) {
-    case 1: rmsnorm_bwd_kernel<T, 1><<<grid, block, 0, s>>>(a); break;
-    default: rmsnorm_bwd_kernel<T, 2><<<grid, block, 0, s>>>(a); break;
-    }
+    if (p.chunks == 1)
+        rmsnorm_bwd_kernel<T, 1, WHOLE><<<grid, block, 0, s>>>(a);
+    else
+        rmsnorm_bwd_kernel<T, 2, WHOLE><<<grid, block, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    column_sum_kernel<<<dim3(static_cast<unsigned>((a.D + 63) / 64)), dim3(1024), 0, s>>>(a.part, blocks, a.D, a.dw);
+    column_sum_kernel<<<dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(1024), 0, s>>>(a.part, blocks, a.D, a.dw);
     return hipGetLastError();
+}
+
+template <class T>
+hipError_t norm_by(const NormArgs &a, hipStream_t s) {
+    return a.whole ? norm_of<T, true>(a, s) : norm_of<T, false>(a, s);
+}
+template <class T>
+hipError_t norm_bwd_by(const NormBwdArgs &a, hipStream_t s) {
+    return a.whole ? norm_bwd_of<T, true>(a, s) : norm_bwd_of<T, false>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t s) {
-    return a.type == ISC_F32 ? norm_of<F32>(a, s) : a.type == ISC_BF16 ? norm_of<BF16>(a, s) : norm_of<F16>(a, s);
+    return a.type == ISC_F32 ? norm_by<F32>(a, s) : a.type == ISC_BF16 ? norm_by<BF16>(a, s) : norm_by<F16>(a, s);
 }
 
 int norm_bwd_blocks(int T, int D) {
     const int threads = row_plan(D, 1024).threads;
-    const int most = 256 * (2048 / threads < 4 ? 2048 / threads : 4);
+    const int most = 256 * (threads > 512 ? 1 : 2);
     return T < most ? (T < 1 ? 1 : T) : most;
 }
 
 hipError_t launch_rmsnorm_bwd(const NormBwdArgs &a, hipStream_t s) {
-    return a.type == ISC_F32    ? norm_bwd_of<F32>(a, s)
-           : a.type == ISC_BF16 ? norm_bwd_of<BF16>(a, s)
-                                : norm_bwd_of<F16>(a, s);
+    return a.type == ISC_F32    ? norm_bwd_by<F32>(a, s)
+           : a.type == ISC_BF16 ? norm_bwd_by<BF16>(a, s)
+                                : norm_bwd_by<F16>(a, s);
 }
 
 }  // namespace isc

@@ -510,13 +510,22 @@ hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
     }
 }
 
+// The same choice for an x that was laid out, by the blocks of one tile of
+// outputs and two of columns: one block a workgroup while there are no more than
+// compute units, then two tiles of outputs, then four, then four of columns too
+// (bfloat16, us, in that order: 4096 x 4096 at 17 tokens 8.6 9.2 11.2 13.2, at 64
+// 12.0 9.6 11.7 14.8, 4096 x 8192 at 64 18.4 13.8 12.6 15.5, 8192 x 16384 at 64
+// 53.6 35.9 28.2 25.0).
 template <int XTYPE>
 hipError_t packed(const W4Args &a, hipStream_t s) {
     constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, MODE = kPacked + P - 1;
     const int64_t tiles = (a.T + kTokens<MODE> - 1) / kTokens<MODE>;
     pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (tiles <= 2) return run<MODE, 2, 2, 2, 512>(a, 8, s);
+    const int64_t blocks = a.w.tiles() * ((tiles + 1) / 2);
+    if (blocks <= 256) return run<MODE, 1, 2, 2, 256>(a, 4, s);
+    if (blocks <= 512) return run<MODE, 2, 2, 2, 256>(a, 4, s);
+    if (blocks <= 1024) return run<MODE, 4, 2, 2, 256>(a, 4, s);
     return run<MODE, 4, 4, 2, 256>(a, 4, s);
 }
 
