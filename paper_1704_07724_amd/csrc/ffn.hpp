@@ -134,6 +134,20 @@ __device__ __forceinline__ uint32_t wave_sum_bits(uint32_t v) { ISC_WAVE_REDUCE(
 #undef ISC_WAVE_REDUCE
 __device__ __forceinline__ float wave_sum(float v) { return __uint_as_float(wave_sum_bits(__float_as_uint(v))); }
 
+// The same within rows of 16 lanes: every lane gets its row's, the same in all
+// of them (each step adds or compares what the two sides hold alike).
+#define ISC_ROW_REDUCE(v, op)                           \
+    v = op(v, dpp<0xb1, 0xf>(v, v));  /* quad_perm 1,0,3,2 */ \
+    v = op(v, dpp<0x4e, 0xf>(v, v));  /* quad_perm 2,3,0,1 */ \
+    v = op(v, dpp<0x141, 0xf>(v, v)); /* row_half_mirror */   \
+    v = op(v, dpp<0x140, 0xf>(v, v)); /* row_mirror */        \
+    return v
+__device__ __forceinline__ uint32_t row_max(uint32_t v) { ISC_ROW_REDUCE(v, op_max); }
+__device__ __forceinline__ uint32_t row_min(uint32_t v) { ISC_ROW_REDUCE(v, op_min); }
+__device__ __forceinline__ uint32_t row_sum_bits(uint32_t v) { ISC_ROW_REDUCE(v, op_sum); }
+#undef ISC_ROW_REDUCE
+__device__ __forceinline__ float row_sum(float v) { return __uint_as_float(row_sum_bits(__float_as_uint(v))); }
+
 // An unsigned order of floats: a > b as numbers exactly when order(a) > order(b)
 // (NaN aside; -0 orders below +0, so a caller ranks v + 0.0f).
 __device__ __forceinline__ uint32_t order(float v) {

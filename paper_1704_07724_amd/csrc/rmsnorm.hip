@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
     float ss = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) load_chunk<T, WHOLE>(v[c], static_cast<const E *>(a.x) + t * a.ldx, c, a.D, swap);
-    if (a.r) {
+    if (a.r && C <= 4) {
         float u[C][8];
 #pragma unroll
         for (int c = 0; c < C; ++c) load_chunk<T, WHOLE>(u[c], static_cast<const E *>(a.r) + t * a.ldr, c, a.D, swap);
@@ -152,6 +152,15 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[c][j] += u[c][j];
+    } else if (a.r) {  // the longest rows: a chunk at a time, for want of registers
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float u[8];
+            load_chunk<T, WHOLE>(u, static_cast<const E *>(a.r) + t * a.ldr, c, a.D, swap);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[c][j] += u[j];
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     // short rows: the weight on its way while the sum is taken
     if (C <= 2)

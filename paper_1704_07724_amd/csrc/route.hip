@@ -8,9 +8,12 @@
 // An expert whose logit (or key) is -inf or NaN is never chosen; a token with
 // fewer than k experts left gets id -1 and weight 0 in its last slots.
 //
-// One wavefront per token, E / 64 experts a lane: the keys stay in registers
-// as unsigned integers in the floats' order, a slot is one wavefront maximum
-// by data-parallel moves, a ballot finds its lane.
+// LANES lanes share a token, 16 where it has at most 256 experts (and 16 slots
+// and groups), so that a wavefront routes four; else 64.  The keys stay in
+// registers as unsigned integers in the floats' order, the experts of a lane
+// LANES apart; a slot is a maximum and then a minimum of the indices that have
+// it, by data-parallel moves.  Four tokens a wavefront rather than one take
+// 8192 tokens of 128 experts from 16.4 to @@ us.
 //
 // The experts' lists.  A token meets an expert at most once, so 64 tokens and
 // an expert make one 64-bit word: a pair's place among its expert's pairs is
@@ -28,114 +31,171 @@ constexpr int kTokens = 64;   // tokens per workgroup: the bits of a word
 constexpr int kWaves = 16;    // wavefronts per workgroup
 constexpr int kMaxE = 1024;   // experts, and threads of a workgroup
 
-__device__ __forceinline__ float token_logit(const RouteArgs &a, int64_t t, int e) {
-    return load_as(a.logits, t * a.ld + e, a.type);
+// Reductions over a token's lanes.
+template <int LANES>
+__device__ __forceinline__ uint32_t max_of(uint32_t v) {
+    return LANES == 16 ? row_max(v) : wave_max(v);
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t min_of(uint32_t v) {
+    return LANES == 16 ? row_min(v) : wave_min(v);
+}
+template <int LANES>
+__device__ __forceinline__ float sum_of(float v) {
+    return LANES == 16 ? row_sum(v) : wave_sum(v);
 }
 
-// A token's scores from its logits (64 experts a step of i, lane the lowest
-// part of the index); logits that are not above -inf score 0.  A logit of
-// +inf stands for all others' limit: it shares the softmax with its equals.
-template <int C>
+// e^x for x <= 88, 0 below the smallest normal number: the exponent's product
+// with log2 e in two parts, so the error stays near one unit in the last place.
+// (A third of the instructions of the library's: a kernel that routes a few
+// tokens waits for its own code to arrive more than for anything else.)
+__device__ __forceinline__ float exponential(float x) {
+    const float t = x * 0x1.715476p+0f;
+    const float rest = fmaf(x, 0x1.4ae0cp-26f, fmaf(x, 0x1.715476p+0f, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return x < -87.0f ? 0.0f : fmaf(e, rest * 0x1.62e43p-1f, e);
+}
+
+// A token's scores from its logits, expert i * LANES + lane in place i; logits
+// that are not above -inf score 0.  A logit of +inf stands for all others'
+// limit: it shares the softmax with its equals.
+template <int C, int LANES>
 __device__ __forceinline__ void scores(const float (&l)[C], float (&s)[C], int sigmoid) {
     if (sigmoid) {
+        // below -88 the score itself is below the smallest normal number
 #pragma unroll
-        for (int i = 0; i < C; ++i) s[i] = l[i] > -__builtin_inff() ? 1.0f / (1.0f + expf(-l[i])) : 0.0f;
+        for (int i = 0; i < C; ++i) s[i] = l[i] > -88.0f ? __builtin_amdgcn_rcpf(1.0f + exponential(-l[i])) : 0.0f;
         return;
     }
     uint32_t mx = 0;
 #pragma unroll
     for (int i = 0; i < C; ++i)
         if (l[i] > -__builtin_inff()) mx = op_max(mx, order(l[i]));
-    mx = wave_max(mx);
+    mx = max_of<LANES>(mx);
     const float m = mx ? unorder(mx) : 0.0f;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        s[i] = l[i] > -__builtin_inff() ? (l[i] == m ? 1.0f : expf(l[i] - m)) : 0.0f;
+        s[i] = l[i] > -__builtin_inff() ? (l[i] == m ? 1.0f : exponential(l[i] - m)) : 0.0f;
         sum += s[i];
     }
-    sum = wave_sum(sum);
+    sum = sum_of<LANES>(sum);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) s[i] *= inv;
 }
 
-// One token by the calling wavefront; `row` is LDS of E words of its own
-// (used with groups only).  Lane j < k returns slot j's expert, or -1.
-template <int C>
+// A token's logits, -inf past the last expert.
+template <int C, int LANES>
+__device__ __forceinline__ void load_logits(float (&l)[C], const void *logits, int64_t at, int lane, int E, int type) {
+    uint32_t raw[C];
+    if (type == ISC_F32) {
+        const uint32_t *p = static_cast<const uint32_t *>(logits) + at;
+#pragma unroll
+        for (int i = 0; i < C; ++i) raw[i] = p[i * LANES + lane < E ? i * LANES + lane : 0];
+    } else {
+        const uint16_t *p = static_cast<const uint16_t *>(logits) + at;
+#pragma unroll
+        for (int i = 0; i < C; ++i) raw[i] = p[i * LANES + lane < E ? i * LANES + lane : 0];
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        l[i] = type == ISC_F16 ? F16::widen(raw[i]) : __uint_as_float(type == ISC_BF16 ? raw[i] << 16 : raw[i]);
+        if (i * LANES + lane >= E) l[i] = -__builtin_inff();
+    }
+}
+
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Token t by LANES lanes, all of the wavefront's tokens together (t past the
+// last one routes the last again and stores nothing); `row` is E words of LDS
+// of the token's own, used with groups only.  Lane j < k of the token returns
+// slot j's expert, or -1.
+template <int C, int LANES>
 __device__ __forceinline__ int route_token(const RouteArgs &a, int64_t t, uint32_t *row) {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & (LANES - 1), first = threadIdx.x & 63 & ~(LANES - 1);
+    const bool there = t < a.T;
+    const int64_t at = there ? t : a.T - 1;
     float l[C], s[C];
     uint32_t key[C];  // 0: not to be chosen
+    load_logits<C, LANES>(l, a.logits, at * a.ld, lane, a.E, a.type);
+    scores<C, LANES>(l, s, a.sigmoid);
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        const int e = i * 64 + lane;
-        l[i] = e < a.E ? token_logit(a, t, e) : -__builtin_inff();
-    }
-    scores<C>(l, s, a.sigmoid);
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int e = i * 64 + lane;
+        const int e = i * LANES + lane;
         const float v = e < a.E && a.bias ? s[i] + a.bias[e] : s[i];
         key[i] = l[i] > -__builtin_inff() && v > -__builtin_inff() ? order(v + 0.0f) : 0u;
     }
     if (a.groups > 1) {
         const int size = a.E / a.groups;
+        // e / size as a product: exact, as e times the factor's excess stays below 2^20 / size
+        const uint32_t factor = ((1u << 20) + static_cast<uint32_t>(size) - 1u) / static_cast<uint32_t>(size);
 #pragma unroll
         for (int i = 0; i < C; ++i)
-            if (i * 64 + lane < a.E) row[i * 64 + lane] = key[i];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            if (i * LANES + lane < a.E) row[i * LANES + lane] = key[i];
+        wave_fence();
         uint32_t g = 0;  // lane g's group; 0: none of its experts can be chosen
         if (lane < a.groups) {
             uint32_t best = 0, second = 0;
-            for (int e = lane * size; e < (lane + 1) * size; ++e) {
-                const uint32_t v = row[e];
+#pragma unroll 8
+            for (int i = 0; i < size; ++i) {
+                const uint32_t v = row[lane * size + i];
                 second = op_max(second, op_min(best, v));
                 best = op_max(best, v);
             }
             if (best) g = order(unorder(best) + (second ? unorder(second) : 0.0f) + 0.0f);
         }
+        wave_fence();
+        if (lane < a.groups) row[lane] = g;
+        wave_fence();
         int before = 0;  // groups ranked before the lane's
         for (int j = 0; j < a.groups; ++j) {
-            const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(g), j));
+            const uint32_t v = row[j];
             before += v > g || (v == g && j < lane);
         }
-        const unsigned long long kept = __ballot(lane < a.groups && g && before < a.keep);
+        const unsigned long long kept = __ballot(lane < a.groups && g && before < a.keep) >> first;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            const int e = i * 64 + lane;
-            if (e < a.E && !(kept >> (e / size) & 1)) key[i] = 0u;
+            const int e = i * LANES + lane;
+            if (e < a.E && !(kept >> (static_cast<uint32_t>(e) * factor >> 20) & 1)) key[i] = 0u;
         }
     }
     int id = -1;
-    float w = 0.0f;
     for (int j = 0; j < a.k; ++j) {
         uint32_t best = key[0];
-        int at = 0;
+        int e = lane;
 #pragma unroll
         for (int i = 1; i < C; ++i)
-            if (key[i] > best) best = key[i], at = i;
-        const uint32_t top = wave_max(best);
-        if (top == 0u) break;
-        const unsigned long long tied = __ballot(best == top);
-        int e = at * 64 + lane;
-        if (tied & (tied - 1))  // equal keys in several lanes: the lowest index
-            e = static_cast<int>(wave_min(best == top ? static_cast<uint32_t>(e) : 0xffffffffu));
-        else
-            e = __builtin_amdgcn_readlane(e, __builtin_ctzll(tied));
-        float score = 0.0f;
+            if (key[i] > best) best = key[i], e = i * LANES + lane;
+        const uint32_t top = max_of<LANES>(best);
+        // equal keys in several lanes: the lowest index
+        if constexpr (LANES == 64) {
+            const unsigned long long tied = __ballot(best == top);
+            if (tied & (tied - 1))
+                e = static_cast<int>(wave_min(best == top ? static_cast<uint32_t>(e) : 0xffffffffu));
+            else
+                e = __builtin_amdgcn_readlane(e, __builtin_ctzll(tied));
+        } else {
+            e = static_cast<int>(row_min(best == top ? static_cast<uint32_t>(e) : 0xffffffffu));
+        }
+        if (top == 0u) e = -1;  // none is left
 #pragma unroll
         for (int i = 0; i < C; ++i)
-            if (i == e >> 6) {
-                score = s[i];
-                if (lane == (e & 63)) key[i] = 0u;
-            }
-        score = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(score), e & 63));
-        if (lane == j) id = e, w = score;
+            if (e == i * LANES + lane) key[i] = 0u;
+        if (lane == j) id = e;
     }
-    if (a.renorm) w = w / (wave_sum(w) + 1e-20f);
+    float w = 0.0f;  // the slot's score, from the lane that holds it
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const float v = __shfl(s[i], first + (id & (LANES - 1)));
+        if (id >= 0 && id / LANES == i) w = v;
+    }
+    if (a.renorm) w = w / (sum_of<LANES>(w) + 1e-20f);
+    if (!there) return -1;
     if (lane < a.k) {
         a.ids[t * a.k + lane] = id;
         a.weights[t * a.k + lane] = w * a.scale;
@@ -161,26 +221,26 @@ __device__ __forceinline__ int block_scan(int v, int *sums) {
 
 // Routes 64 tokens a workgroup.  ONE: there is one workgroup, which also
 // writes the lists; else it leaves its counts for place_kernel.
-template <int C, bool ONE>
+template <int C, int LANES, bool ONE>
 __global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
-    extern __shared__ uint32_t rows[];  // kWaves rows of E words, with groups
+    constexpr int kAtOnce = 64 / LANES * kWaves, kTurns = kTokens / kAtOnce;  // tokens at once, and how often
+    extern __shared__ uint32_t rows[];  // kAtOnce rows of E words, with groups
     __shared__ unsigned long long bits[kMaxE];
     __shared__ int base[kMaxE], sums[kWaves], total;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & (LANES - 1), own = threadIdx.x / LANES;
     const bool lists = a.order != nullptr;
     if (lists) {
         bits[threadIdx.x] = 0ull;
         __syncthreads();
     }
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens;
-    int id[kTokens / kWaves];
-#pragma unroll
-    for (int i = 0; i < kTokens / kWaves; ++i) {
-        const int64_t t = t0 + i * kWaves + wave;
-        id[i] = -1;
-        if (t >= a.T) continue;
-        id[i] = route_token<C>(a, t, rows + wave * a.E);
-        if (lists && id[i] >= 0) atomicOr(&bits[id[i]], 1ull << (i * kWaves + wave));
+#pragma unroll 1
+    for (int i = 0; i < kTurns; ++i) {
+        const int t = i * kAtOnce + own;
+        // (a whole wavefront without tokens has nothing to do)
+        if (t0 + i * kAtOnce + static_cast<int>(threadIdx.x >> 6) * (64 / LANES) >= a.T) break;
+        const int id = route_token<C, LANES>(a, t0 + t, rows + own * a.E);
+        if (lists && lane < a.k && id >= 0) atomicOr(&bits[id], 1ull << t);
     }
     if (!lists) return;
     __syncthreads();
@@ -197,11 +257,10 @@ __global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
         a.offsets[a.E] = total;
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kTokens / kWaves; ++i) {
-        const int t = i * kWaves + wave;
-        if (id[i] >= 0)
-            a.order[base[id[i]] + __popcll(bits[id[i]] & ((1ull << t) - 1))] = t * a.k + lane;
+    const int pairs = a.T * a.k;
+    for (int p = threadIdx.x; p < pairs; p += kMaxE) {  // written by this workgroup, before the barriers
+        const int id = a.ids[p], t = p / a.k;
+        if (id >= 0) a.order[base[id] + __popcll(bits[id] & ((1ull << t) - 1))] = p;
     }
     for (int p = total + static_cast<int>(threadIdx.x); p < a.T * a.k; p += kMaxE) a.order[p] = -1;
 }
@@ -228,10 +287,17 @@ __global__ void __launch_bounds__(kMaxE) place_kernel(RouteArgs a) {
     if (static_cast<int>(threadIdx.x) < step * a.E) {
         const int e = threadIdx.x % a.E;
         int before = 0, n = 0;
-        for (int i = threadIdx.x / a.E; i < nb; i += step) {
-            const int c = a.counts[static_cast<int64_t>(i) * a.E + e];
-            n += c;
-            if (i < b) before += c;
+        for (int i = threadIdx.x / a.E; i < nb; i += 8 * step) {
+            int c[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                c[j] = a.counts[static_cast<int64_t>(i + j * step < nb ? i + j * step : i) * a.E + e];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int v = i + j * step < nb ? c[j] : 0;
+                n += v;
+                if (i + j * step < b) before += v;
+            }
         }
         atomicAdd(&all[e], n);
         atomicAdd(&base[e], before);
@@ -267,16 +333,14 @@ __global__ void __launch_bounds__(256) route_bwd_kernel(RouteBwdArgs a) {
     if (t >= a.T) return;
     float *row = grad + wave * a.E;
     float l[C], s[C];
+    load_logits<C, 64>(l, a.logits, t * a.ld, lane, a.E, a.type);
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int e = i * 64 + lane;
-        l[i] = e < a.E ? load_as(a.logits, t * a.ld + e, a.type) : -__builtin_inff();
-        if (e < a.E) row[e] = 0.0f;
-    }
+    for (int i = 0; i < C; ++i)
+        if (i * 64 + lane < a.E) row[i * 64 + lane] = 0.0f;
     int id = lane < a.k ? a.ids[t * a.k + lane] : -1;
     if (id >= a.E) id = -1;
     float dw = id >= 0 ? a.dweights[t * a.k + lane] * a.scale : 0.0f;
-    scores<C>(l, s, a.sigmoid);
+    scores<C, 64>(l, s, a.sigmoid);
     float chosen = 0.0f;  // slot `lane`'s score, from the lane that holds it
 #pragma unroll
     for (int i = 0; i < C; ++i) {
@@ -316,21 +380,21 @@ hipError_t grant_lds(Kern kern, std::atomic<bool> &granted, size_t asked) {
     return e;
 }
 
-template <int C>
+template <int C, int LANES>
 hipError_t route_of(const RouteArgs &a, hipStream_t s) {
     const int nb = route_blocks(a.T);
-    const size_t lds = a.groups > 1 ? sizeof(uint32_t) * kWaves * static_cast<size_t>(a.E) : 0;
+    const size_t lds = a.groups > 1 ? sizeof(uint32_t) * (64 / LANES) * kWaves * static_cast<size_t>(a.E) : 0;
     const dim3 grid(static_cast<unsigned>(nb)), block(kMaxE);
     if (nb == 1) {
         static std::atomic<bool> granted{false};
-        if (const hipError_t e = grant_lds(route_kernel<C, true>, granted, lds); e != hipSuccess) return e;
-        route_kernel<C, true><<<grid, block, lds, s>>>(a);
+        if (const hipError_t e = grant_lds(route_kernel<C, LANES, true>, granted, lds); e != hipSuccess) return e;
+        route_kernel<C, LANES, true><<<grid, block, lds, s>>>(a);
         return hipGetLastError();
     }
     static std::atomic<bool> granted{false};
-    hipError_t e = grant_lds(route_kernel<C, false>, granted, lds);
+    hipError_t e = grant_lds(route_kernel<C, LANES, false>, granted, lds);
     if (e != hipSuccess) return e;
-    route_kernel<C, false><<<grid, block, lds, s>>>(a);
+    route_kernel<C, LANES, false><<<grid, block, lds, s>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess || !a.order) return e;
     place_kernel<<<grid, block, 0, s>>>(a);
@@ -349,12 +413,10 @@ hipError_t route_bwd_of(const RouteBwdArgs &a, hipStream_t s) {
 int route_blocks(int T) { return T > kTokens ? (T + kTokens - 1) / kTokens : 1; }
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
-    const int c = (a.E + 63) / 64;
-    return c <= 1 ? route_of<1>(a, s)
-           : c <= 2 ? route_of<2>(a, s)
-           : c <= 4 ? route_of<4>(a, s)
-           : c <= 8 ? route_of<8>(a, s)
-                    : route_of<16>(a, s);
+    // up to 16 tokens a wavefront each: the fewer instructions count
+    if (a.T > kWaves && a.E <= 256 && a.k <= 16 && a.groups <= 16)
+        return a.E <= 64 ? route_of<4, 16>(a, s) : a.E <= 128 ? route_of<8, 16>(a, s) : route_of<16, 16>(a, s);
+    return a.E <= 256 ? route_of<4, 64>(a, s) : a.E <= 512 ? route_of<8, 64>(a, s) : route_of<16, 64>(a, s);
 }
 
 hipError_t launch_route_bwd(const RouteBwdArgs &a, hipStream_t s) {

@@ -14,6 +14,8 @@ device.  Outputs and workspaces are allocated on the stream of the call.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 from typing import NamedTuple
 
 import paper_1704_07724_amd as _isc
@@ -174,90 +176,117 @@ def _exact(t, dtype, shape, name):
     return t if t.is_contiguous() else t.contiguous()
 
 
+@functools.lru_cache(maxsize=4096)
+def _size(query, *shape):
+    """Bytes of workspace that a size query of the library gives for a shape."""
+    n = ctypes.c_size_t()
+    _isc._check(getattr(_isc.lib(), query)(*shape, n), query)
+    return n.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _w4_size(query, E, N, K, layout, *call):
+    """The same for a call with packed weights."""
+    return _size.__wrapped__(query, W4Desc(E, N, K, layout), *call)
+
+
+def _on_stream(call):
+    """call(st, ..., stream) with its temporaries allocated on the call's stream;
+    st, the package's state, is not the caller's to give."""
+    @functools.wraps(call)
+    def run(*args, stream=None, **kw):
+        st = _state or _ready()
+        if stream is None:
+            return call(st, *args, **kw)
+        with _isc._on(stream):
+            return call(st, *args, stream=stream, **kw)
+    own = inspect.signature(call)
+    run.__signature__ = own.replace(parameters=list(own.parameters.values())[1:])
+    return run
+
+
+def _new(st, like, dtype, *shape):
+    """A contiguous tensor on like's device; by torch's quickest way, as a one-token
+    call spends more time on its outputs than on the GPU."""
+    strides, n = [], 1
+    for size in reversed(shape):
+        strides.append(n)
+        n *= size
+    return st.torch.empty_strided(shape, strides[::-1], dtype=dtype, device=like.device)
+
+
 def _bytes(st, n, like):
     """A workspace of n bytes."""
-    return st.torch.empty(n, dtype=st.u8, device=like.device)
+    return st.torch.empty_strided((n,), (1,), dtype=st.u8, device=like.device)
 
 
-def isc_rmsnorm(x, weight, eps=1e-6, residual=None, y=True, mx8=False, rstd=False, stream=None):
+@_on_stream
+def isc_rmsnorm(st, x, weight, eps=1e-6, residual=None, y=True, mx8=False, rstd=False, stream=None):
     """h = x + residual, and its root-mean-square norm times `weight`, over the last dimension.
 
     x: [..., D] float32, float16 or bfloat16; residual: as x, or None; weight: [D]
     of any of those types.  Returns Norm(y, h, mx8, rstd): y in x's type (if y),
     h (with a residual), the norm in 8 bits with scales (if mx8), the reciprocal
     root mean squares for isc_rmsnorm_bwd (if rstd)."""
-    st = _state or _ready()
     if not (y or mx8 or rstd or residual is not None):
         raise ValueError("nothing is asked for")
-    if stream is not None:
-        with _isc._on(stream):
-            return _rmsnorm(st, x, weight, eps, residual, y, mx8, rstd, stream)
-    return _rmsnorm(st, x, weight, eps, residual, y, mx8, rstd, None)
-
-
-def _rmsnorm(st, x, weight, eps, residual, y, mx8, rstd, stream):
     shape = x.shape
     D = shape[-1]
     code = _type(st, x.dtype, "x")
     device = _device(st, x, weight, residual)
     xr, ldx = _rows(x, D, "x")
-    new = st.torch.empty_like if xr.is_contiguous() else lambda t, **kw: st.torch.empty(shape, device=x.device, **kw)
-    rp, ldr, h, hp = None, D, None, None
+    rp, ldr, h, hp, out, yp, form, qp, sp = None, D, None, None, None, None, None, None, None
     if residual is not None:
         if residual.dtype != x.dtype or residual.shape != shape:
             raise ValueError("residual must have x's shape and type")
         rr, ldr = _rows(residual, D, "residual")
         rp = rr.data_ptr()
-        h = new(xr, dtype=x.dtype)
+        h = _new(st, x, x.dtype, *shape)
         hp = h.data_ptr()
     wr = _vector(weight, D, "weight")
-    out = new(xr, dtype=x.dtype) if y else None
+    if y:
+        out = _new(st, x, x.dtype, *shape)
+        yp = out.data_ptr()
     groups = (D + 31) // 32
-    form, qp, sp = None, None, None
     if mx8:
-        form = Mx8(new(xr, dtype=st.f8), st.torch.empty((*shape[:-1], groups), dtype=st.e8, device=x.device))
-        qp, sp = form[0].data_ptr(), form[1].data_ptr()
-    rs = st.torch.empty(shape[:-1], dtype=st.f32, device=x.device) if rstd else None
+        q, scales = _new(st, x, st.f8, *shape), _new(st, x, st.e8, *shape[:-1], groups)
+        form, qp, sp = Mx8(q, scales), q.data_ptr(), scales.data_ptr()
+    rs = _new(st, x, st.f32, *shape[:-1]) if rstd else None
     status = st.lib.isc_rmsnorm(
         x.numel() // D if D else 0, D, code, xr.data_ptr(), ldx, rp, ldr, wr.data_ptr(),
-        _type(st, wr.dtype, "weight"), eps, hp, D, _ptr(out), D, qp, D, sp, groups, _ptr(rs),
-        _stream(st, stream, device))
+        _type(st, wr.dtype, "weight"), eps, hp, D, yp, D, qp, D, sp, groups, _ptr(rs), _stream(st, stream, device))
     if status:
         _isc._check(status, "isc_rmsnorm")
     return Norm(out, h, form, rs)
 
 
-def isc_rmsnorm_bwd(dy, h, weight, rstd, dh=None, ws=None, stream=None):
+@_on_stream
+def isc_rmsnorm_bwd(st, dy, h, weight, rstd, dh=None, ws=None, stream=None):
     """The gradient of isc_rmsnorm: (dx, dweight).
 
     dy, h: [..., D] of one type, h as the forward pass gave it (x without a
     residual); rstd: [...] float32 from there; dh: the gradient that reaches h
     past the norm, or None.  dx (in h's type) is the gradient of x and of the
     residual alike; dweight is float32 [D]."""
-    st = _state or _ready()
-    with _isc._on(stream):
-        torch, D = st.torch, h.shape[-1]
-        code = _type(st, h.dtype, "h")
-        device = _device(st, h, dy, weight, rstd, dh, ws)
-        for t, name in ((dy, "dy"), (dh, "dh")):
-            if t is not None and (t.dtype != h.dtype or t.shape != h.shape):
-                raise ValueError("%s must have h's shape and type" % name)
-        T = h.numel() // D if D else 0
-        rs = _exact(rstd, st.f32, h.shape[:-1], "rstd")
-        hr, ldh = _rows(h, D, "h")
-        yr, ldy = _rows(dy, D, "dy")
-        gr, ldd = (None, D) if dh is None else _rows(dh, D, "dh")
-        wr = _vector(weight, D, "weight")
-        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        dw = torch.empty(D, dtype=st.f32, device=h.device)
-        if ws is None:
-            n = ctypes.c_size_t()
-            _isc._check(st.lib.isc_rmsnorm_bwd_workspace_size(T, D, n), "isc_rmsnorm_bwd_workspace_size")
-            ws = _bytes(st, n.value, h)
-        _isc._check(st.lib.isc_rmsnorm_bwd(
-            T, D, code, yr.data_ptr(), ldy, hr.data_ptr(), ldh, wr.data_ptr(), _type(st, wr.dtype, "weight"),
-            rs.data_ptr(), _ptr(gr), ldd, dx.data_ptr(), D, dw.data_ptr(), ws.data_ptr(), _isc._nbytes(ws),
-            _stream(st, stream, device)), "isc_rmsnorm_bwd")
+    D = h.shape[-1]
+    code = _type(st, h.dtype, "h")
+    device = _device(st, h, dy, weight, rstd, dh, ws)
+    for t, name in ((dy, "dy"), (dh, "dh")):
+        if t is not None and (t.dtype != h.dtype or t.shape != h.shape):
+            raise ValueError("%s must have h's shape and type" % name)
+    T = h.numel() // D if D else 0
+    rs = _exact(rstd, st.f32, h.shape[:-1], "rstd")
+    hr, ldh = _rows(h, D, "h")
+    yr, ldy = _rows(dy, D, "dy")
+    gr, ldd = (None, D) if dh is None else _rows(dh, D, "dh")
+    wr = _vector(weight, D, "weight")
+    dx, dw = _new(st, h, h.dtype, *h.shape), _new(st, h, st.f32, D)
+    if ws is None:
+        ws = _bytes(st, _size("isc_rmsnorm_bwd_workspace_size", T, D), h)
+    _isc._check(st.lib.isc_rmsnorm_bwd(
+        T, D, code, yr.data_ptr(), ldy, hr.data_ptr(), ldh, wr.data_ptr(), _type(st, wr.dtype, "weight"),
+        rs.data_ptr(), _ptr(gr), ldd, dx.data_ptr(), D, dw.data_ptr(), ws.data_ptr(), _isc._nbytes(ws),
+        _stream(st, stream, device)), "isc_rmsnorm_bwd")
     return dx, dw
 
 
@@ -267,7 +296,8 @@ def _score(score):
     return SCORES[score]
 
 
-def isc_route(logits, k, bias=None, score="softmax", groups=1, keep_groups=None, renorm=True, scale=1.0, lists=True,
+@_on_stream
+def isc_route(st, logits, k, bias=None, score="softmax", groups=1, keep_groups=None, renorm=True, scale=1.0, lists=True,
               ws=None, stream=None):
     """Each token's k experts, their weights, and the pairs by expert: Route(ids, weights, offsets, order).
 
@@ -275,107 +305,98 @@ def isc_route(logits, k, bias=None, score="softmax", groups=1, keep_groups=None,
     scores for the choice only; groups, keep_groups: the choice is among the
     experts of the best keep_groups (default: all) of that many groups; renorm:
     weights divided by their sum; lists=False: no offsets and order."""
-    st = _state or _ready()
     which = _score(score)
-    with _isc._on(stream):
-        if logits.dim() != 2:
-            raise ValueError("logits must be [T, E], not %r" % (tuple(logits.shape),))
-        T, E = logits.shape
-        code = _type(st, logits.dtype, "logits")
-        device, dev, empty = _device(st, logits, bias, ws), logits.device, st.torch.empty
-        lr, ld = _rows(logits, E, "logits")
-        br = None if bias is None else _exact(bias, st.f32, (E,), "bias")
-        k = int(k)
-        if k < 1:
-            raise ValueError("k must be at least 1, not %d" % k)
-        ids = empty((T, k), dtype=st.i32, device=dev)
-        weights = empty((T, k), dtype=st.f32, device=dev)
-        offsets = empty(E + 1, dtype=st.i32, device=dev) if lists else None
-        order = empty(T * k, dtype=st.i32, device=dev) if lists else None
-        if ws is None and lists and T > 64:
-            n = ctypes.c_size_t()
-            _isc._check(st.lib.isc_route_workspace_size(T, E, n), "isc_route_workspace_size")
-            ws = _bytes(st, n.value, logits)
-        # an empty tensor has no address, and without tokens there is no order to write
-        at = order.data_ptr() or offsets.data_ptr() if lists and not T else _ptr(order)
-        _isc._check(st.lib.isc_route(
-            T, E, k, code, lr.data_ptr(), ld, _ptr(br), which, groups, groups if keep_groups is None else keep_groups,
-            bool(renorm), scale, ids.data_ptr(), weights.data_ptr(), _ptr(offsets), at, _ptr(ws),
-            0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device)), "isc_route")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, E], not %r" % (tuple(logits.shape),))
+    T, E = logits.shape
+    code = _type(st, logits.dtype, "logits")
+    device = _device(st, logits, bias, ws)
+    lr, ld = _rows(logits, E, "logits")
+    br = None if bias is None else _exact(bias, st.f32, (E,), "bias")
+    k = int(k)
+    if not 1 <= k <= E:
+        raise ValueError("k must be 1 to %d, not %d" % (E, k))
+    ids, weights = _new(st, logits, st.i32, T, k), _new(st, logits, st.f32, T, k)
+    offsets, order = (_new(st, logits, st.i32, E + 1), _new(st, logits, st.i32, T * k)) if lists else (None, None)
+    if ws is None and lists and T > 64:
+        ws = _bytes(st, _size("isc_route_workspace_size", T, E), logits)
+    # an empty tensor has no address, and without tokens there is no order to write
+    at = order.data_ptr() or offsets.data_ptr() if lists and not T else _ptr(order)
+    _isc._check(st.lib.isc_route(
+        T, E, k, code, lr.data_ptr(), ld, _ptr(br), which, groups, groups if keep_groups is None else keep_groups,
+        bool(renorm), scale, ids.data_ptr(), weights.data_ptr(), _ptr(offsets), at, _ptr(ws),
+        0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device)), "isc_route")
     return Route(ids, weights, offsets, order)
 
 
-def isc_route_bwd(dweights, logits, ids, score="softmax", renorm=True, scale=1.0, stream=None):
+@_on_stream
+def isc_route_bwd(st, dweights, logits, ids, score="softmax", renorm=True, scale=1.0, stream=None):
     """The gradient of isc_route's weights to its logits, in their type.
 
     dweights: [T, k] float32; ids: [T, k] int32 as isc_route gave them; score,
     renorm, scale: as there."""
-    st = _state or _ready()
     which = _score(score)
-    with _isc._on(stream):
-        if logits.dim() != 2 or ids.dim() != 2:
-            raise ValueError("logits must be [T, E] and ids [T, k]")
-        T, E = logits.shape
-        k = ids.shape[1]
-        code = _type(st, logits.dtype, "logits")
-        device = _device(st, logits, dweights, ids)
-        lr, ld = _rows(logits, E, "logits")
-        dr = _exact(dweights, st.f32, (T, k), "dweights")
-        ir = _exact(ids, st.i32, (T, k), "ids")
-        out = st.torch.empty((T, E), dtype=logits.dtype, device=logits.device)
-        _isc._check(st.lib.isc_route_bwd(T, E, k, code, dr.data_ptr(), lr.data_ptr(), ld, ir.data_ptr(), which,
-                                         bool(renorm), scale, out.data_ptr(), E, _stream(st, stream, device)),
-                    "isc_route_bwd")
+    if logits.dim() != 2 or ids.dim() != 2:
+        raise ValueError("logits must be [T, E] and ids [T, k]")
+    T, E = logits.shape
+    k = ids.shape[1]
+    code = _type(st, logits.dtype, "logits")
+    device = _device(st, logits, dweights, ids)
+    lr, ld = _rows(logits, E, "logits")
+    dr = _exact(dweights, st.f32, (T, k), "dweights")
+    ir = _exact(ids, st.i32, (T, k), "ids")
+    out = _new(st, logits, logits.dtype, T, E)
+    _isc._check(st.lib.isc_route_bwd(T, E, k, code, dr.data_ptr(), lr.data_ptr(), ld, ir.data_ptr(), which,
+                                     bool(renorm), scale, out.data_ptr(), E, _stream(st, stream, device)),
+                "isc_route_bwd")
     return out
 
 
-def isc_w4_quantize(w, stream=None):
+@_on_stream
+def isc_w4_quantize(st, w, stream=None):
     """(codes, scales) of 4-bit weights: w [N, K] or [E, N, K] float32, float16 or
     bfloat16; codes [..., N, ceil(K / 2)] uint8, scales [..., N, ceil(K / 32)] float8_e8m0fnu."""
-    st = _state or _ready()
-    with _isc._on(stream):
-        torch = st.torch
-        if w.dim() not in (2, 3):
-            raise ValueError("w must be [N, K] or [E, N, K], not %r" % (tuple(w.shape),))
-        E = w.shape[0] if w.dim() == 3 else 1
-        N, K = w.shape[-2:]
-        device = _device(st, w)
-        wr, ld = _rows(w, K, "w")
-        codes = torch.empty((*w.shape[:-1], (K + 1) // 2), dtype=torch.uint8, device=w.device)
-        scales = torch.empty((*w.shape[:-1], (K + 31) // 32), dtype=torch.float8_e8m0fnu, device=w.device)
-        _isc._check(st.lib.isc_w4_quantize(W4Desc(E, N, K, 0), wr.data_ptr(), _type(st, w.dtype, "w"), ld,
-                                           codes.data_ptr(), scales.data_ptr(), _stream(st, stream, device)),
-                    "isc_w4_quantize")
+    torch = st.torch
+    if w.dim() not in (2, 3):
+        raise ValueError("w must be [N, K] or [E, N, K], not %r" % (tuple(w.shape),))
+    E = w.shape[0] if w.dim() == 3 else 1
+    N, K = w.shape[-2:]
+    device = _device(st, w)
+    wr, ld = _rows(w, K, "w")
+    codes = torch.empty((*w.shape[:-1], (K + 1) // 2), dtype=torch.uint8, device=w.device)
+    scales = torch.empty((*w.shape[:-1], (K + 31) // 32), dtype=torch.float8_e8m0fnu, device=w.device)
+    _isc._check(st.lib.isc_w4_quantize(W4Desc(E, N, K, 0), wr.data_ptr(), _type(st, w.dtype, "w"), ld,
+                                       codes.data_ptr(), scales.data_ptr(), _stream(st, stream, device)),
+                "isc_w4_quantize")
     return codes, scales
 
 
-def isc_w4_pack_codes(codes, scales, layout, K=None, stream=None):
+@_on_stream
+def isc_w4_pack_codes(st, codes, scales, layout, K=None, stream=None):
     """The packed weights (a W4) of codes [N, K / 2] or [E, N, K / 2] and their scales.
 
     layout: "tiles" for isc_w4_linear, "rows" for isc_w4_skip; K: the number of
     inputs where it is odd (the last byte's high half is then ignored)."""
-    st = _state or _ready()
     torch = st.torch
     if layout not in LAYOUTS:
         raise ValueError("layout must be one of %s, not %r" % (", ".join(LAYOUTS), layout))
-    with _isc._on(stream):
-        if codes.dim() not in (2, 3) or codes.dtype != torch.uint8:
-            raise ValueError("codes must be uint8 [N, K / 2] or [E, N, K / 2]")
-        K = 2 * codes.shape[-1] if K is None else int(K)
-        if (K + 1) // 2 != codes.shape[-1]:
-            raise ValueError("codes have %d bytes a row, not those of %d inputs" % (codes.shape[-1], K))
-        if scales.dtype not in (torch.float8_e8m0fnu, torch.uint8) or \
-                tuple(scales.shape) != (*codes.shape[:-1], (K + 31) // 32):
-            raise ValueError("scales must be float8_e8m0fnu or uint8 %r" % ((*codes.shape[:-1], (K + 31) // 32),))
-        device = _device(st, codes, scales)
-        E = codes.shape[0] if codes.dim() == 3 else 1
-        desc = W4Desc(E, codes.shape[-2], K, LAYOUTS[layout])
-        n = ctypes.c_size_t()
-        _isc._check(st.lib.isc_w4_size(desc, n), "isc_w4_size")
-        data = _bytes(st, n.value, codes)
-        cr, sr = codes.contiguous(), scales.contiguous()
-        _isc._check(st.lib.isc_w4_pack_codes(desc, cr.data_ptr(), sr.data_ptr(), data.data_ptr(),
-                                             _stream(st, stream, device)), "isc_w4_pack_codes")
+    if codes.dim() not in (2, 3) or codes.dtype != torch.uint8:
+        raise ValueError("codes must be uint8 [N, K / 2] or [E, N, K / 2]")
+    K = 2 * codes.shape[-1] if K is None else int(K)
+    if (K + 1) // 2 != codes.shape[-1]:
+        raise ValueError("codes have %d bytes a row, not those of %d inputs" % (codes.shape[-1], K))
+    if scales.dtype not in (torch.float8_e8m0fnu, torch.uint8) or \
+            tuple(scales.shape) != (*codes.shape[:-1], (K + 31) // 32):
+        raise ValueError("scales must be float8_e8m0fnu or uint8 %r" % ((*codes.shape[:-1], (K + 31) // 32),))
+    device = _device(st, codes, scales)
+    E = codes.shape[0] if codes.dim() == 3 else 1
+    desc = W4Desc(E, codes.shape[-2], K, LAYOUTS[layout])
+    n = ctypes.c_size_t()
+    _isc._check(st.lib.isc_w4_size(desc, n), "isc_w4_size")
+    data = _bytes(st, n.value, codes)
+    cr, sr = codes.contiguous(), scales.contiguous()
+    _isc._check(st.lib.isc_w4_pack_codes(desc, cr.data_ptr(), sr.data_ptr(), data.data_ptr(),
+                                         _stream(st, stream, device)), "isc_w4_pack_codes")
     return W4(desc, data, codes.dim() == 3)
 
 
@@ -394,89 +415,84 @@ def _routed(st, route, w4, T):
     return slots, _exact(ids, st.i32, (T, slots), "ids"), weights, offsets, order
 
 
-def isc_w4_linear(x, w4, route=None, relu=False, dtype=None, ws=None, stream=None):
+@_on_stream
+def isc_w4_linear(st, x, w4, route=None, relu=False, dtype=None, ws=None, stream=None):
     """y = x w^T on 4-bit weights (layout "tiles"), with max(0, .) if relu.
 
     x: [..., K] float32, float16 or bfloat16, or an Mx8 (values, scales).
     Without a route: y is [..., N].  With one: x is [T, K], w4 holds the experts'
     matrices, and y is [T, k, N], slot j by the token's j-th expert (0 where it
     has none).  dtype: y's (default: x's, bfloat16 for an Mx8)."""
-    st = _state or _ready()
-    with _isc._on(stream):
-        K, N = w4.K, w4.N
-        sp, lds, scales = None, 0, None
-        if isinstance(x, tuple):
-            x, scales = x
-            if x.dtype != st.f8 or scales.dtype != st.e8:
-                raise TypeError("an Mx8 is float8_e4m3fn values and float8_e8m0fnu scales")
-            if scales.shape[:-1] != x.shape[:-1]:
-                raise ValueError("scales are %r, for values %r" % (tuple(scales.shape), tuple(x.shape)))
-            code = MX8
-            scales, lds = _rows(scales, (K + 31) // 32, "scales")
-            sp = scales.data_ptr()
-        else:
-            code = _type(st, x.dtype, "x")
-        shape = x.shape
-        xr, ldx = _rows(x, K, "x")
-        T = x.numel() // K
-        if route is not None and len(shape) != 2:
-            raise ValueError("x must be [T, K] with a route")
-        slots, ids, _, offsets, order = _routed(st, route, w4, T)
-        device = _device(st, x, scales, w4.data, ids, offsets, order, ws)
-        if slots:
-            if offsets is None or order is None:
-                raise ValueError("the route has no lists")
-            offsets = _exact(offsets, st.i32, (w4.E + 1,), "offsets")
-            order = _exact(order, st.i32, (T * slots,), "order")
-        if dtype is None:
-            dtype = st.torch.bfloat16 if code == MX8 else x.dtype
-        if ws is None and not slots and T > COLUMNS[code]:
-            n = ctypes.c_size_t()
-            _isc._check(st.lib.isc_w4_linear_workspace_size(w4.desc, T, code, slots, n), "isc_w4_linear_workspace_size")
-            ws = _bytes(st, n.value, x)
-        y = st.torch.empty((T, slots, N) if slots else (*shape[:-1], N), dtype=dtype, device=x.device)
-        status = st.lib.isc_w4_linear(
-            w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, sp, lds, slots, _ptr(ids), _ptr(offsets),
-            _ptr(order), y.data_ptr(), _type(st, dtype, "dtype"), N, bool(relu), _ptr(ws),
-            0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device))
-        if status:
-            _isc._check(status, "isc_w4_linear")
+    K, N = w4.K, w4.N
+    sp, lds, scales = None, 0, None
+    if isinstance(x, tuple):
+        x, scales = x
+        if x.dtype != st.f8 or scales.dtype != st.e8:
+            raise TypeError("an Mx8 is float8_e4m3fn values and float8_e8m0fnu scales")
+        if scales.shape[:-1] != x.shape[:-1]:
+            raise ValueError("scales are %r, for values %r" % (tuple(scales.shape), tuple(x.shape)))
+        code = MX8
+        scales, lds = _rows(scales, (K + 31) // 32, "scales")
+        sp = scales.data_ptr()
+    else:
+        code = _type(st, x.dtype, "x")
+    shape = x.shape
+    xr, ldx = _rows(x, K, "x")
+    T = x.numel() // K
+    if route is not None and len(shape) != 2:
+        raise ValueError("x must be [T, K] with a route")
+    slots, ids, _, offsets, order = _routed(st, route, w4, T)
+    device = _device(st, x, scales, w4.data, ids, offsets, order, ws)
+    if slots:
+        if offsets is None or order is None:
+            raise ValueError("the route has no lists")
+        offsets = _exact(offsets, st.i32, (w4.E + 1,), "offsets")
+        order = _exact(order, st.i32, (T * slots,), "order")
+    if dtype is None:
+        dtype = st.torch.bfloat16 if code == MX8 else x.dtype
+    if ws is None and not slots and T > COLUMNS[code]:
+        ws = _bytes(st, _w4_size("isc_w4_linear_workspace_size", w4.E, N, K, LAYOUTS["tiles"], T, code, 0), x)
+    y = _new(st, x, dtype, T, slots, N) if slots else _new(st, x, dtype, *shape[:-1], N)
+    status = st.lib.isc_w4_linear(
+        w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, sp, lds, slots, _ptr(ids), _ptr(offsets),
+        _ptr(order), y.data_ptr(), _type(st, dtype, "dtype"), N, bool(relu), _ptr(ws),
+        0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_w4_linear")
     return y
 
 
-def isc_w4_skip(x, w4, route=None, dtype=None, ws=None, stream=None):
+@_on_stream
+def isc_w4_skip(st, x, w4, route=None, dtype=None, ws=None, stream=None):
     """y = x w^T on 4-bit weights (layout "rows") for a rectified x: zeros are skipped and
     their weights not read.
 
     Without a route: x is [..., K], y [..., N].  With one: x is [T, k, K]
     (isc_w4_linear's output), and y [T, N] the sum over a token's experts under
     the route's weights.  dtype: y's (default: x's)."""
-    st = _state or _ready()
-    with _isc._on(stream):
-        K, N = w4.K, w4.N
-        shape = x.shape
-        code = _type(st, x.dtype, "x")
-        xr, ldx = _rows(x, K, "x")
-        if route is not None and len(shape) != 3:
-            raise ValueError("x must be [T, k, K] with a route")
-        T = shape[0] if route is not None else x.numel() // K
-        slots, ids, weights, _, _ = _routed(st, route, w4, T)
-        device = _device(st, x, w4.data, ids, weights, ws)
-        if slots:
-            if shape[1] != slots:
-                raise ValueError("x has %d slots, the route %d" % (shape[1], slots))
-            weights = _exact(weights, st.f32, (T, slots), "weights")
-        if ws is None:
-            n = ctypes.c_size_t()
-            _isc._check(st.lib.isc_w4_skip_workspace_size(w4.desc, T, slots, n), "isc_w4_skip_workspace_size")
-            if n.value:
-                ws = _bytes(st, n.value, x)
-        dtype = x.dtype if dtype is None else dtype
-        y = st.torch.empty((T, N) if slots else (*shape[:-1], N), dtype=dtype, device=x.device)
-        status = st.lib.isc_w4_skip(
-            w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, slots, _ptr(ids), _ptr(weights), y.data_ptr(),
-            _type(st, dtype, "dtype"), N, _ptr(ws), 0 if ws is None else _isc._nbytes(ws),
-            _stream(st, stream, device))
-        if status:
-            _isc._check(status, "isc_w4_skip")
+    K, N = w4.K, w4.N
+    shape = x.shape
+    code = _type(st, x.dtype, "x")
+    xr, ldx = _rows(x, K, "x")
+    if route is not None and len(shape) != 3:
+        raise ValueError("x must be [T, k, K] with a route")
+    T = shape[0] if route is not None else x.numel() // K
+    slots, ids, weights, _, _ = _routed(st, route, w4, T)
+    device = _device(st, x, w4.data, ids, weights, ws)
+    if slots:
+        if shape[1] != slots:
+            raise ValueError("x has %d slots, the route %d" % (shape[1], slots))
+        weights = _exact(weights, st.f32, (T, slots), "weights")
+    if ws is None:
+        n = _w4_size("isc_w4_skip_workspace_size", w4.E, N, K, LAYOUTS["rows"], T, slots)
+        if n:
+            ws = _bytes(st, n, x)
+    dtype = x.dtype if dtype is None else dtype
+    y = _new(st, x, dtype, T, N) if slots else _new(st, x, dtype, *shape[:-1], N)
+    status = st.lib.isc_w4_skip(
+        w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, slots, _ptr(ids), _ptr(weights), y.data_ptr(),
+        _type(st, dtype, "dtype"), N, _ptr(ws), 0 if ws is None else _isc._nbytes(ws),
+        _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_w4_skip")
     return y
