@@ -25,9 +25,26 @@ __device__ __forceinline__ float block_sum(float v, float *sums) {
     if (waves == 1) return v;
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
     __syncthreads();
-    float t = 0.0f;
-    for (int i = 0; i < waves; ++i) t += sums[i];
-    return t;
+    // by halves: the wavefronts' values are of one size, and so are their pairs'
+    float t[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[i] = i < waves ? sums[i] : 0.0f;
+#pragma unroll
+    for (int n = 8; n > 0; n >>= 1)
+#pragma unroll
+        for (int i = 0; i < n; ++i) t[i] += t[i + n];
+    return t[0];
+}
+
+// m^(-1/2) to half a unit in the last place and a little: the instruction's
+// value, and a Newton step on its error.  The 8-bit form's values move by whole
+// steps where the last bit does.
+__device__ __forceinline__ float reciprocal_root(float m) {
+    const float r = __builtin_amdgcn_rsqf(m);
+    const float h = m * r, low = fmaf(m, r, -h);
+    const float e = fmaf(-low, r, fmaf(-h, r, 1.0f));
+    const float better = fmaf(0.5f * r, e, r);
+    return fabsf(better) < __builtin_inff() ? better : r;  // 0 and infinity have no error to take off
 }
 
 // First of the eight values of a row that a thread holds in chunk c.
@@ -174,7 +191,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
 #pragma unroll
         for (int c = 0; c < C; ++c) store_chunk<T, WHOLE>(static_cast<E *>(a.h) + t * a.ldh, v[c], c, a.D, swap);
     const float mean = block_sum(ss, sums) / static_cast<float>(a.D);
-    const float rstd = 1.0f / sqrtf(mean + a.eps);
+    const float rstd = reciprocal_root(mean + a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[t] = rstd;
     if (!a.y && !a.q) return;
 #pragma unroll

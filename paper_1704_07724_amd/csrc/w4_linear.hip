@@ -370,11 +370,13 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) load_x(ring[d], step_of(d), std::true_type{});
             __builtin_amdgcn_sched_barrier(0);
-            widen_first(ring[0]);
+            if constexpr (DEPTH > 1) widen_first(ring[0]);
             int i = 0;
             for (; i + DEPTH <= mine; i += DEPTH) {
 #pragma unroll
                 for (int d = 0; d < DEPTH; ++d) {
+                    // the ring's next step is there to widen from; a ring of one has just loaded it
+                    if constexpr (DEPTH == 1) widen_first(ring[0]);
                     multiply(ring[d], ring[(d + 1) % DEPTH]);
                     const int next = step_of(i + d + DEPTH);
                     load_w(ring[d], next);
@@ -487,24 +489,25 @@ bool packs(int T, int xtype, int slots) { return slots == 0 && T > 16 / parts_of
 
 // Tiles of outputs a wavefront keeps (NT), wavefronts that share the inputs and
 // steps loaded ahead, by the workgroups there are to fill 256 compute units
-// with.  Few tiles: one each.  From 512 on two, so that x is read half as often
-// (8192 x 16384, one bfloat16 token: 13.1 us against 14.7), with 1024 and more
-// columns than a few four (16 tokens: 16.1 us against 21.9).  Four wavefronts a
+// with.  Few tiles: one each.  From 512 on two, so that x is read half as often,
+// and one step ahead, for more workgroups at once (16384 outputs of 8192 inputs,
+// one bfloat16 token: 12.8 us against 14.7); from 1024 on and with more than a
+// few tokens four (16 tokens: 16.1 us against 20.6).  Four wavefronts a
 // workgroup rather than eight (4096 x 4096, one token: 4.2 us against 4.8), but
-// for long rows (9216 x 4096: 6.6 us against 7.4).  An expert has few rows and
-// many experts run: four tiles, or two where a token is alone (64 experts of
-// 2048 x 1408: 16 tokens 18.9 us against 20.8, one token 8.3 against 7.5).
+// for long rows (4096 outputs of 9216: 6.6 us against 7.4).  An expert has few rows and
+// many experts run: four tiles, or two where tokens are few (64 experts of 1408
+// outputs of 2048: 16 tokens 18.6 us against 20.4, one token 8.3 against 7.5).
 template <int MODE>
 hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
     const int64_t tiles = a.w.tiles(), steps = a.w.steps();
     if constexpr (kStaged<MODE>) {
-        // 8192 x 16384, one fp32 token: 15.1 us against 18.2 with one tile
+        // 16384 outputs of 8192, one fp32 token: 15.1 us against 18.2 with one tile
         if (tiles >= 512) return run<MODE, 2, 1, 2, 512>(a, 8, s);
         return run<MODE, 1, 1, 4, 512>(a, 8, s);
     } else {
         if (a.slots) return a.T > 4 ? run<MODE, 4, 1, 1, 256>(a, 4, s) : run<MODE, 2, 1, 2, 256>(a, 4, s);
         if (tiles >= 1024 && a.T > 4) return run<MODE, 4, 1, 2, 256>(a, 4, s);
-        if (tiles >= 512) return run<MODE, 2, 1, 2, 256>(a, 4, s);
+        if (tiles >= 512) return run<MODE, 2, 1, 1, 256>(a, 4, s);
         if (steps > 48) return run<MODE, 1, 1, 2, 512>(a, 8, s);
         return run<MODE, 1, 1, 2, 256>(a, 4, s);
     }

@@ -463,6 +463,56 @@ def test_linear(torch, isc, T, N, K, xtype):
         assert torch.equal(isc.isc_w4_linear(s, w4, dtype=torch.float32), isc.isc_w4_linear(xd, w4, dtype=torch.float32))
 
 
+# shapes on either side of every size that the product's tiling goes by, each
+# with several steps of 128 inputs for every wavefront and a last one that is not full
+TILINGS = [(1, 40, 1500), (4, 40, 1500), (1, 40, 7000), (1, 8200, 1500), (6, 8200, 1500), (1, 16400, 1200), (5, 16400, 1200),
+           (16, 16400, 1200), (17, 40, 1500), (20, 5000, 1500), (40, 4100, 1500), (64, 4100, 1500), (64, 8200, 1500), (60, 16400, 1200),
+           (70, 16400, 1201)]
+
+
+@pytest.mark.parametrize("xtype", TYPES + ["mx8"])
+@pytest.mark.parametrize("T,N,K", TILINGS)
+def test_linear_tilings(torch, isc, T, N, K, xtype):
+    note("linear tilings", T, N, K, xtype)
+    r = np.random.default_rng(T + N + K)
+    w4, w = weights(torch, isc, r, 1, N, K, "tiles")
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.product(w[0], xv)
+    close(host(isc.isc_w4_linear(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
+@pytest.mark.parametrize("xtype", ["bfloat16", "float16", "mx8"])
+@pytest.mark.parametrize("T", [2, 4, 5, 60])
+def test_experts_long_rows(torch, isc, T, xtype):
+    """Experts' rows of several steps for every wavefront, few tokens and many."""
+    note("experts long rows", T, xtype)
+    r = np.random.default_rng(T)
+    E, k, N, K = 5, 2, 100, 2600
+    route, ids, _ = a_route(torch, isc, r, T, E, k, 0.1)
+    w4, w = weights(torch, isc, r, E, N, K, "tiles", lead=E)
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.routed(w, xv, ids)
+    y = isc.isc_w4_linear(xd, w4, route=route, dtype=torch.float32)
+    close(host(y), want, (K + 64) * E24 * size, "float32", "y")
+
+
+# the same for the skipping product: one, two and four tests a turn, one range and many
+@pytest.mark.parametrize("T,N,K", [(1, 40, 9000), (1, 8200, 33000), (3, 2000, 20000), (12, 4200, 5000), (40, 600, 3000),
+                                   (700, 40, 700)])
+def test_skip_cuts(torch, isc, T, N, K):
+    note("skip cuts", T, N, K)
+    r = np.random.default_rng(T + N + K)
+    w4, w = weights(torch, isc, r, 1, N, K, "rows")
+    x = np.abs(r.standard_normal((T, K))) * (r.random((T, K)) < 0.1)
+    xd = dev(torch, x, "bfloat16")
+    want, size = ffn.product(w[0], host(xd), skip=True)
+    close(host(isc.isc_w4_skip(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
 @pytest.mark.parametrize("xtype", TYPES)
 @pytest.mark.parametrize("T,N,K", PRODUCTS)
 def test_skip(torch, isc, T, N, K, xtype):
