@@ -439,8 +439,7 @@ int isc_gemm_f32(int32_t M, int32_t Ncols, int32_t Kd, const float *a, int64_t l
  *     at least the row's length) says how far apart rows are.  Element types
  *     are isc_type values; sums are fp32 whatever the type, and a value is
  *     rounded once, to nearest, where it is stored.  Pointers are aligned to
- *     their element; rows that all start on 16 bytes are read 16 bytes at a
- *     time, others value by value.
+ *     their element.
  *   - T, the number of tokens, may be 0: such a call checks its arguments and
  *     writes what does not depend on a token.
  *   - An output that has an input's rows may be that very tensor (the same

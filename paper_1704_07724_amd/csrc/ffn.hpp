@@ -61,18 +61,29 @@ __device__ __forceinline__ void store_as(void *p, int64_t i, float v, int type) 
         static_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(type == ISC_BF16 ? BF16::narrow(v) : F16::narrow(v));
 }
 
-// Eight consecutive values: one or two 16-byte accesses where the caller
-// knows the address to be 16-byte aligned and all eight to be there
-// (`whole`), else one access each for the first `n`.
+// Wide accesses at any address: the memory path takes a vector access at the
+// alignment of its elements and below, so rows need not start on 16 bytes.
+template <class V>
+__device__ __forceinline__ V load_any(const void *p) {
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+template <class V>
+__device__ __forceinline__ void store_any(void *p, const V &v) {
+    __builtin_memcpy(p, &v, sizeof(V));
+}
+
+// Eight consecutive values, or the first n of them and zeros.
 template <class T>
-__device__ __forceinline__ void load8(float (&v)[8], const typename T::type *p, int n, bool whole) {
-    if (whole) {
+__device__ __forceinline__ void load8(float (&v)[8], const typename T::type *p, int n) {
+    if (n >= 8) {
         if constexpr (sizeof(typename T::type) == 4) {
-            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+            const float4 a = load_any<float4>(p), b = load_any<float4>(p + 4);
             v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
             v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
-            const uint4 a = *reinterpret_cast<const uint4 *>(p);
+            const uint4 a = load_any<uint4>(p);
             const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -86,16 +97,16 @@ __device__ __forceinline__ void load8(float (&v)[8], const typename T::type *p, 
     for (int i = 0; i < 8; ++i) v[i] = i < n ? T::load(p + i) : 0.0f;
 }
 template <class T>
-__device__ __forceinline__ void store8(typename T::type *p, const float (&v)[8], int n, bool whole) {
-    if (whole) {
+__device__ __forceinline__ void store8(typename T::type *p, const float (&v)[8], int n) {
+    if (n >= 8) {
         if constexpr (sizeof(typename T::type) == 4) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            store_any(p, make_float4(v[0], v[1], v[2], v[3]));
+            store_any(p + 4, make_float4(v[4], v[5], v[6], v[7]));
         } else {
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = T::narrow(v[2 * i]) | T::narrow(v[2 * i + 1]) << 16;
-            *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+            store_any(p, make_uint4(w[0], w[1], w[2], w[3]));
         }
         return;
     }
@@ -183,7 +194,6 @@ struct NormArgs {
     int64_t ldx, ldr, ldh, ldy, ldq, lds;
     int T, D, type, wtype;
     float eps;
-    bool whole;  // every row 16-byte aligned and D a multiple of 8
 };
 hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t s);
 
@@ -194,7 +204,6 @@ struct NormBwdArgs {
     float *dw, *part;  // part: norm_bwd_blocks() rows of D sums
     int64_t ldy, ldh, ldd, ldx;
     int T, D, type, wtype;
-    bool whole;
 };
 int norm_bwd_blocks(int T, int D);
 hipError_t launch_rmsnorm_bwd(const NormBwdArgs &a, hipStream_t s);
@@ -261,8 +270,6 @@ struct W4Args {
     void *y;
     float *part;
     uint8_t *columns;  // w4_linear_column_bytes() of room for x as matrix operands
-    bool whole;  // every row of x 16-byte aligned, and of an 8-bit x's scales 4-byte
-    bool whole_y;  // four consecutive outputs of a row can be stored at once
 };
 size_t w4_linear_column_bytes(const W4Shape &w, int T, int xtype, int slots);
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);

@@ -23,8 +23,6 @@ struct Span {
     int64_t rows, cols, ld;
     size_t size;  // of an element
     size_t bytes() const { return rows < 1 ? 0 : size * static_cast<size_t>((rows - 1) * ld + cols); }
-    // every row starts on 16 bytes
-    bool whole() const { return !p || (aligned(p, 16) && (rows < 2 || ld * static_cast<int64_t>(size) % 16 == 0)); }
     bool shape_ok() const { return !p || (ld >= cols && (rows < 1 || ld <= kI64Room / rows)); }
 };
 
@@ -85,9 +83,7 @@ int isc_rmsnorm(int32_t T, int32_t D, int32_t type, const void *x, int64_t ldx, 
             if (overlap(out[i], out[j])) return ISC_ERR_ALIAS;
     }
     if (const int st = isc::require_gfx950()) return st;
-    const bool whole = D % 8 == 0 && in[0].whole() && in[1].whole() && in[2].whole() && out[0].whole() &&
-                       out[1].whole() && (!q || (aligned(q, 8) && (T < 2 || ldq % 8 == 0)));
-    const isc::NormArgs a{x, r, w, h, y, q, scales, rstd, ldx, ldr, ldh, ldy, ldq, lds, T, D, type, w_type, eps, whole};
+    const isc::NormArgs a{x, r, w, h, y, q, scales, rstd, ldx, ldr, ldh, ldy, ldq, lds, T, D, type, w_type, eps};
     return hip_status(isc::launch_rmsnorm(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -124,9 +120,8 @@ int isc_rmsnorm_bwd(int32_t T, int32_t D, int32_t type, const void *dy, int64_t 
             if (overlap(out[i], out[j])) return ISC_ERR_ALIAS;
     }
     if (const int st = isc::require_gfx950()) return st;
-    const bool whole = D % 8 == 0 && in[0].whole() && in[1].whole() && in[2].whole() && in[3].whole() && out[0].whole();
     const isc::NormBwdArgs a{dy, h, w, dh, rstd, dx, dw, static_cast<float *>(ws), ldy, ldh, ldd, ldx, T, D, type,
-                             w_type, whole};
+                             w_type};
     return hip_status(isc::launch_rmsnorm_bwd(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -286,8 +281,6 @@ int isc_w4_linear(const isc_w4_desc *d, const void *packed, int32_t T, const voi
     a.T = T, a.slots = slots, a.ids = ids, a.offsets = offsets, a.order = order;
     a.y = y, a.ldy = ldy, a.ytype = y_type, a.relu = relu != 0;
     a.columns = static_cast<uint8_t *>(ws);
-    a.whole = in[0].whole() && (x_type != ISC_MX8 || (aligned(x_scales, 4) && ld_scales % 4 == 0));
-    a.whole_y = aligned(y, 4 * type_bytes(y_type)) && ldy % 4 == 0;
     return hip_status(isc::launch_w4_linear(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -337,7 +330,6 @@ int isc_w4_skip(const isc_w4_desc *d, const void *packed, int32_t T, const void 
     a.T = T, a.slots = slots, a.ids = ids, a.weights = weights;
     a.y = y, a.ldy = ldy, a.ytype = y_type;
     a.part = static_cast<float *>(ws);
-    a.whole = in[0].whole();
     return hip_status(isc::launch_w4_skip(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -4,11 +4,8 @@
 //
 // One workgroup per row, the row in registers (up to 32768 values), so x and r
 // are read once: eight consecutive values per thread and chunk, a group of 32
-// outputs (the 8-bit form's unit) in four neighbouring lanes.  Rows that do not
-// all start on 16 bytes are read value by value, neighbouring lanes neighbouring
-// values, and change places within a wavefront through LDS; the sums are the
-// same.  Sums are fp32; h is normalised as it was added, before its rounding to
-// x's type.  Memory bounds it: 8192 rows of 8192 in bfloat16 with residual and
+// outputs (the 8-bit form's unit) in four neighbouring lanes.  Sums are fp32; h
+// is normalised as it was added, before its rounding to x's type.  Memory bounds it: 8192 rows of 8192 in bfloat16 with residual and
 // 8-bit output move 469 MB in 85 us, 5.5 TB/s.
 //
 // The gradient, with n = h rstd and g = dy w:
@@ -52,77 +49,38 @@ __device__ __forceinline__ float reciprocal_root(float m) {
     return fabsf(better) < __builtin_inff() ? better : r;  // 0 and infinity have no error to take off
 }
 
-// First of the eight values of a row that a thread holds in chunk c.
+constexpr int kShortRows = 8;  // rows of one wavefront that a workgroup of the gradient takes at once
+
+// First of the eight values of a row that a thread holds in chunk c.  SHORT: a
+// wavefront holds the row.
+template <bool SHORT = false>
 __device__ __forceinline__ int at(int c) {
-    return (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
+    return SHORT ? static_cast<int>(threadIdx.x & 63) * 8
+                 : (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
 }
 
-// A wavefront's 512 values of a chunk, lane by lane or value by value: in LDS of
-// its own, so only the order within the wavefront matters.
-__device__ __forceinline__ void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+// Chunk c of a row of D values, 0 where there are none.
+template <class T, bool SHORT = false>
+__device__ __forceinline__ void load_chunk(float (&v)[8], const typename T::type *row, int c, int D) {
+    load8<T>(v, row + at<SHORT>(c), D - at<SHORT>(c));
 }
-struct Swap {
-    float v[16][512];
-    __device__ __forceinline__ float *mine() { return v[threadIdx.x >> 6]; }
-};
-
-// Chunk c of a row of D values, 0 where there are none (D is a multiple of 8 if WHOLE).
-template <class T, bool WHOLE>
-__device__ __forceinline__ void load_chunk(float (&v)[8], const typename T::type *row, int c, int D, Swap *swap) {
-    if constexpr (WHOLE) {
-        if (at(c) < D) {
-            load8<T>(v, row + at(c), 8, true);
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    } else {
-        const int lane = threadIdx.x & 63, i = at(c) - lane * 8 + lane;
-        float u[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = i + j * 64 < D ? T::load(row + i + j * 64) : 0.0f;
-        float *buf = swap->mine();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) buf[j * 64 + lane] = u[j];
-        wave_fence();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = buf[lane * 8 + j];
-        wave_fence();
-    }
+template <class T, bool SHORT = false>
+__device__ __forceinline__ void store_chunk(typename T::type *row, const float (&v)[8], int c, int D) {
+    store8<T>(row + at<SHORT>(c), v, D - at<SHORT>(c));
 }
-template <class T, bool WHOLE>
-__device__ __forceinline__ void store_chunk(typename T::type *row, const float (&v)[8], int c, int D, Swap *swap) {
-    if constexpr (WHOLE) {
-        if (at(c) < D) store8<T>(row + at(c), v, 8, true);
-    } else {
-        const int lane = threadIdx.x & 63, i = at(c) - lane * 8 + lane;
-        float *buf = swap->mine();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) buf[lane * 8 + j] = v[j];
-        wave_fence();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i + j * 64 < D) store<T>(row + i + j * 64, buf[j * 64 + lane]);
-        wave_fence();
-    }
-}
-template <bool WHOLE>
-__device__ __forceinline__ void load_weight(float (&w)[8], const void *p, int c, int D, int type, Swap *swap) {
+template <bool SHORT = false>
+__device__ __forceinline__ void load_weight(float (&w)[8], const void *p, int c, int D, int type) {
     if (type == ISC_F32)
-        load_chunk<F32, WHOLE>(w, static_cast<const float *>(p), c, D, swap);
+        load_chunk<F32, SHORT>(w, static_cast<const float *>(p), c, D);
     else if (type == ISC_BF16)
-        load_chunk<BF16, WHOLE>(w, static_cast<const uint16_t *>(p), c, D, swap);
+        load_chunk<BF16, SHORT>(w, static_cast<const uint16_t *>(p), c, D);
     else
-        load_chunk<F16, WHOLE>(w, static_cast<const uint16_t *>(p), c, D, swap);
+        load_chunk<F16, SHORT>(w, static_cast<const uint16_t *>(p), c, D);
 }
 
 // The 8-bit form of a chunk of outputs.  A group's largest magnitude is taken
 // as bits, under which NaN comes out above everything.
-template <bool WHOLE>
-__device__ __forceinline__ void store_mx8(uint8_t *q, uint8_t *scales, const float (&v)[8], int c, int D, Swap *swap) {
+__device__ __forceinline__ void store_mx8(uint8_t *q, uint8_t *scales, const float (&v)[8], int c, int D) {
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = op_max(m, __float_as_uint(v[j]) & 0x7fffffffu);
@@ -137,39 +95,30 @@ __device__ __forceinline__ void store_mx8(uint8_t *q, uint8_t *scales, const flo
         hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inv, v[5] * inv, 0, false);
         hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, hi, true);
     }
-    if constexpr (WHOLE) {
-        if (at(c) < D) *reinterpret_cast<uint2 *>(q + at(c)) = make_uint2(lo, hi);
+    const int n = D - at(c);
+    if (n >= 8) {
+        store_any(q + at(c), make_uint2(lo, hi));
     } else {
-        const int lane = threadIdx.x & 63, i = at(c) - lane * 8 + lane;
-        uint2 *buf = reinterpret_cast<uint2 *>(swap->mine());
-        buf[lane] = make_uint2(lo, hi);
-        wave_fence();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (i + j * 64 < D) q[i + j * 64] = reinterpret_cast<const uint8_t *>(buf)[j * 64 + lane];
-        wave_fence();
+            if (j < n) q[at(c) + j] = static_cast<uint8_t>((j < 4 ? lo : hi) >> (8 * (j & 3)));
     }
     if ((threadIdx.x & 3) == 0 && at(c) < D) scales[at(c) / 32] = static_cast<uint8_t>(b);
 }
 
-template <class T, int C, bool WHOLE>
+template <class T, int C>
 __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
     using E = typename T::type;
     __shared__ float sums[16];
-    Swap *swap = nullptr;
-    if constexpr (!WHOLE) {
-        __shared__ Swap room;
-        swap = &room;
-    }
     const int64_t t = blockIdx.x;
     float v[C][8], w[C][8];
     float ss = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) load_chunk<T, WHOLE>(v[c], static_cast<const E *>(a.x) + t * a.ldx, c, a.D, swap);
+    for (int c = 0; c < C; ++c) load_chunk<T>(v[c], static_cast<const E *>(a.x) + t * a.ldx, c, a.D);
     if (a.r) {
         float u[C][8];
 #pragma unroll
-        for (int c = 0; c < C; ++c) load_chunk<T, WHOLE>(u[c], static_cast<const E *>(a.r) + t * a.ldr, c, a.D, swap);
+        for (int c = 0; c < C; ++c) load_chunk<T>(u[c], static_cast<const E *>(a.r) + t * a.ldr, c, a.D);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -178,48 +127,43 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
     // short rows: the weight on its way while the sum is taken
     if (C <= 2)
 #pragma unroll
-        for (int c = 0; c < C; ++c) load_weight<WHOLE>(w[c], a.w, c, a.D, a.wtype, swap);
+        for (int c = 0; c < C; ++c) load_weight(w[c], a.w, c, a.D, a.wtype);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int j = 0; j < 8; ++j) ss = fmaf(v[c][j], v[c][j], ss);
     if (a.h)
 #pragma unroll
-        for (int c = 0; c < C; ++c) store_chunk<T, WHOLE>(static_cast<E *>(a.h) + t * a.ldh, v[c], c, a.D, swap);
+        for (int c = 0; c < C; ++c) store_chunk<T>(static_cast<E *>(a.h) + t * a.ldh, v[c], c, a.D);
     const float mean = block_sum(ss, sums) / static_cast<float>(a.D);
     const float rstd = reciprocal_root(mean + a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[t] = rstd;
     if (!a.y && !a.q) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        if (C > 2) load_weight<WHOLE>(w[c], a.w, c, a.D, a.wtype, swap);
+        if (C > 2) load_weight(w[c], a.w, c, a.D, a.wtype);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[c][j] = at(c) + j < a.D ? v[c][j] * rstd * w[c][j] : 0.0f;
-        if (a.y) store_chunk<T, WHOLE>(static_cast<E *>(a.y) + t * a.ldy, v[c], c, a.D, swap);
+        if (a.y) store_chunk<T>(static_cast<E *>(a.y) + t * a.ldy, v[c], c, a.D);
         if (a.q)
-            store_mx8<WHOLE>(static_cast<uint8_t *>(a.q) + t * a.ldq, static_cast<uint8_t *>(a.scales) + t * a.lds, v[c],
-                             c, a.D, swap);
+            store_mx8(static_cast<uint8_t *>(a.q) + t * a.ldq, static_cast<uint8_t *>(a.scales) + t * a.lds, v[c],
+                             c, a.D);
     }
 }
 
 // Rows that the registers do not hold: read once for the sum and, from the
 // cache, once more for the outputs.  Nothing is written before the second
 // reading, so h may still stand in for x or r.
-template <class T, bool WHOLE>
+template <class T>
 __global__ void __launch_bounds__(1024) rmsnorm_long_kernel(NormArgs a, int chunks) {
     using E = typename T::type;
     __shared__ float sums[16];
-    Swap *swap = nullptr;
-    if constexpr (!WHOLE) {
-        __shared__ Swap room;
-        swap = &room;
-    }
     const int64_t t = blockIdx.x;
     const auto load = [&](float(&v)[8], int c) {
-        load_chunk<T, WHOLE>(v, static_cast<const E *>(a.x) + t * a.ldx, c, a.D, swap);
+        load_chunk<T>(v, static_cast<const E *>(a.x) + t * a.ldx, c, a.D);
         if (!a.r) return;
         float u[8];
-        load_chunk<T, WHOLE>(u, static_cast<const E *>(a.r) + t * a.ldr, c, a.D, swap);
+        load_chunk<T>(u, static_cast<const E *>(a.r) + t * a.ldr, c, a.D);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += u[j];
     };
@@ -236,48 +180,61 @@ __global__ void __launch_bounds__(1024) rmsnorm_long_kernel(NormArgs a, int chun
     for (int c = 0; c < chunks; ++c) {
         float v[8], w[8];
         load(v, c);
-        load_weight<WHOLE>(w, a.w, c, a.D, a.wtype, swap);
-        if (a.h) store_chunk<T, WHOLE>(static_cast<E *>(a.h) + t * a.ldh, v, c, a.D, swap);
+        load_weight(w, a.w, c, a.D, a.wtype);
+        if (a.h) store_chunk<T>(static_cast<E *>(a.h) + t * a.ldh, v, c, a.D);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = at(c) + j < a.D ? v[j] * rstd * w[j] : 0.0f;
-        if (a.y) store_chunk<T, WHOLE>(static_cast<E *>(a.y) + t * a.ldy, v, c, a.D, swap);
+        if (a.y) store_chunk<T>(static_cast<E *>(a.y) + t * a.ldy, v, c, a.D);
         if (a.q)
-            store_mx8<WHOLE>(static_cast<uint8_t *>(a.q) + t * a.ldq, static_cast<uint8_t *>(a.scales) + t * a.lds, v, c,
-                             a.D, swap);
+            store_mx8(static_cast<uint8_t *>(a.q) + t * a.ldq, static_cast<uint8_t *>(a.scales) + t * a.lds, v, c, a.D);
     }
 }
 
-template <class T, int C, bool WHOLE>
+// SHORT: rows of one wavefront, as many at once as the workgroup has wavefronts;
+// else one row at a time.  A row is on its way while the one before is worked on,
+// where the registers hold both (C of 1).
+template <class T, int C, bool SHORT>
 __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
     using E = typename T::type;
     __shared__ float sums[2][16];
-    Swap *swap = nullptr;
-    if constexpr (!WHOLE) {
-        __shared__ Swap room;
-        swap = &room;
-    }
+    __shared__ float joined[SHORT ? kShortRows : 1][SHORT ? 512 : 1];
+    const int wave = threadIdx.x >> 6;
+    const int64_t step = SHORT ? static_cast<int64_t>(gridDim.x) * kShortRows : gridDim.x;
     float w[C][8], acc[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        load_weight<WHOLE>(w[c], a.w, c, a.D, a.wtype, swap);
+        load_weight<SHORT>(w[c], a.w, c, a.D, a.wtype);
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[c][j] = 0.0f;
     }
-    int turn = 0;
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x, turn ^= 1) {
-        const float rstd = a.rstd[t];
-        float n[C][8], g[C][8], d[C][8];
-        float dot = 0.0f;
+    // a row of h, dy and dh, as loaded
+    const auto load = [&](int64_t t, float(&n)[C][8], float(&g)[C][8], float(&d)[C][8], float &rstd) {
+        if (t >= a.T) return;
+        rstd = a.rstd[t];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            load_chunk<T, WHOLE>(n[c], static_cast<const E *>(a.h) + t * a.ldh, c, a.D, swap);
-            load_chunk<T, WHOLE>(g[c], static_cast<const E *>(a.dy) + t * a.ldy, c, a.D, swap);
+            load_chunk<T, SHORT>(n[c], static_cast<const E *>(a.h) + t * a.ldh, c, a.D);
+            load_chunk<T, SHORT>(g[c], static_cast<const E *>(a.dy) + t * a.ldy, c, a.D);
             if (a.dh)
-                load_chunk<T, WHOLE>(d[c], static_cast<const E *>(a.dh) + t * a.ldd, c, a.D, swap);
+                load_chunk<T, SHORT>(d[c], static_cast<const E *>(a.dh) + t * a.ldd, c, a.D);
             else
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[c][j] = 0.0f;
         }
+    };
+    const int64_t t0 = SHORT ? static_cast<int64_t>(blockIdx.x) * kShortRows + wave : blockIdx.x;
+    float nn[C][8], ng[C][8], nd[C][8], nr = 0.0f;  // the next row
+    if constexpr (C == 1) load(t0, nn, ng, nd, nr);
+    int turn = 0;
+    for (int64_t t = t0; t < a.T; t += step, turn ^= 1) {
+        float n[C][8], g[C][8], d[C][8], rstd = nr;
+        if constexpr (C == 1) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) n[0][j] = nn[0][j], g[0][j] = ng[0][j], d[0][j] = nd[0][j];
+        } else {
+            load(t, n, g, d, rstd);
+        }
+        float dot = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -287,23 +244,35 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
                 g[c][j] *= w[c][j];
                 dot = fmaf(g[c][j], n[c][j], dot);
             }
+        // (dx may be one of the tensors that are read: row t is in registers now, and
+        // row t + step is no other row's output)
+        if constexpr (C == 1) load(t + step, nn, ng, nd, nr);
         // two sets of sums in turn: a row's are read before the row after the
         // next overwrites them, with the barrier of the row between
-        const float mean = block_sum(dot, sums[turn]) / static_cast<float>(a.D);
+        const float mean = (SHORT ? wave_sum(dot) : block_sum(dot, sums[turn])) / static_cast<float>(a.D);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = fmaf(rstd, fmaf(-n[c][j], mean, g[c][j]), d[c][j]);
-            store_chunk<T, WHOLE>(static_cast<E *>(a.dx) + t * a.ldx, o, c, a.D, swap);
+            store_chunk<T, SHORT>(static_cast<E *>(a.dx) + t * a.ldx, o, c, a.D);
         }
     }
     float *part = a.part + static_cast<int64_t>(blockIdx.x) * a.D;
+    if constexpr (SHORT) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+        for (int j = 0; j < 8; ++j) joined[wave][at<SHORT>(0) + j] = acc[0][j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.D; i += blockDim.x) {
+            float u = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (at(c) + j < a.D) part[at(c) + j] = acc[c][j];
+            for (int r = 0; r < kShortRows; ++r) u += joined[r][i];
+            part[i] = u;
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) store_chunk<F32>(part, acc[c], c, a.D);
+    }
 }
 
 // dw[i] = sum of part[b][i] over b: 32 columns a workgroup, each of its 32 half
@@ -344,59 +313,56 @@ RowPlan row_plan(int D, int most) {
     return {threads, chunks};
 }
 
-template <class T, bool WHOLE>
+template <class T>
 hipError_t norm_of(const NormArgs &a, hipStream_t s) {
     const RowPlan p = row_plan(a.D, 1024);
     const dim3 grid(static_cast<unsigned>(a.T)), block(static_cast<unsigned>(p.threads));
     switch (p.chunks) {
-    case 1: rmsnorm_kernel<T, 1, WHOLE><<<grid, block, 0, s>>>(a); break;
-    case 2: rmsnorm_kernel<T, 2, WHOLE><<<grid, block, 0, s>>>(a); break;
-    case 4: rmsnorm_kernel<T, 4, WHOLE><<<grid, block, 0, s>>>(a); break;
-    default: rmsnorm_long_kernel<T, WHOLE><<<grid, block, 0, s>>>(a, p.chunks); break;
+    case 1: rmsnorm_kernel<T, 1><<<grid, block, 0, s>>>(a); break;
+    case 2: rmsnorm_kernel<T, 2><<<grid, block, 0, s>>>(a); break;
+    case 4: rmsnorm_kernel<T, 4><<<grid, block, 0, s>>>(a); break;
+    default: rmsnorm_long_kernel<T><<<grid, block, 0, s>>>(a, p.chunks); break;
     }
     return hipGetLastError();
 }
 
-template <class T, bool WHOLE>
+template <class T>
 hipError_t norm_bwd_of(const NormBwdArgs &a, hipStream_t s) {
     const RowPlan p = row_plan(a.D, 1024);
+    const bool brief = p.threads == 64;
     const int blocks = norm_bwd_blocks(a.T, a.D);
-    const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(p.threads));
-    if (p.chunks == 1)
-        rmsnorm_bwd_kernel<T, 1, WHOLE><<<grid, block, 0, s>>>(a);
+    const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(brief ? 64 * kShortRows : p.threads));
+    if (brief)
+        rmsnorm_bwd_kernel<T, 1, true><<<grid, block, 0, s>>>(a);
+    else if (p.chunks == 1)
+        rmsnorm_bwd_kernel<T, 1, false><<<grid, block, 0, s>>>(a);
     else
-        rmsnorm_bwd_kernel<T, 2, WHOLE><<<grid, block, 0, s>>>(a);
+        rmsnorm_bwd_kernel<T, 2, false><<<grid, block, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     column_sum_kernel<<<dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(1024), 0, s>>>(a.part, blocks, a.D, a.dw);
     return hipGetLastError();
 }
 
-template <class T>
-hipError_t norm_by(const NormArgs &a, hipStream_t s) {
-    return a.whole ? norm_of<T, true>(a, s) : norm_of<T, false>(a, s);
-}
-template <class T>
-hipError_t norm_bwd_by(const NormBwdArgs &a, hipStream_t s) {
-    return a.whole ? norm_bwd_of<T, true>(a, s) : norm_bwd_of<T, false>(a, s);
-}
-
 }  // namespace
 
 hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t s) {
-    return a.type == ISC_F32 ? norm_by<F32>(a, s) : a.type == ISC_BF16 ? norm_by<BF16>(a, s) : norm_by<F16>(a, s);
+    return a.type == ISC_F32 ? norm_of<F32>(a, s) : a.type == ISC_BF16 ? norm_of<BF16>(a, s) : norm_of<F16>(a, s);
 }
 
 int norm_bwd_blocks(int T, int D) {
     const int threads = row_plan(D, 1024).threads;
-    const int most = 256 * (threads > 512 ? 1 : 2);
-    return T < most ? (T < 1 ? 1 : T) : most;
+    const int turns = threads == 64 ? (T + kShortRows - 1) / kShortRows : T;
+    // short turns want more workgroups at once, a second turn each its loads ahead
+    const int most = 256 * (threads > 512 ? 1 : threads > 256 || threads == 64 ? 2 : threads > 128 ? 4 : 8);
+    const int some = turns < 512 ? turns : (turns + 1) / 2;
+    return some < 1 ? 1 : some < most ? some : most;
 }
 
 hipError_t launch_rmsnorm_bwd(const NormBwdArgs &a, hipStream_t s) {
-    return a.type == ISC_F32    ? norm_bwd_by<F32>(a, s)
-           : a.type == ISC_BF16 ? norm_bwd_by<BF16>(a, s)
-                                : norm_bwd_by<F16>(a, s);
+    return a.type == ISC_F32    ? norm_bwd_of<F32>(a, s)
+           : a.type == ISC_BF16 ? norm_bwd_of<BF16>(a, s)
+                                : norm_bwd_of<F16>(a, s);
 }
 
 }  // namespace isc

@@ -55,19 +55,19 @@ struct Step {
 };
 
 // A column's inputs of one step: eight from 32 j + 8 g on for each j, k the
-// first.  WHOLE: all of them are there, and aligned.
-template <int MODE, bool WHOLE>
+// first.  FULL: all of them are there.
+template <int MODE, bool FULL>
 __device__ __forceinline__ void load_column(uint32_t (&x)[kWords<MODE>], const uint8_t *row, int k, int K) {
     constexpr int per = kWords<MODE> / 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int at = k + 32 * j;
-        if constexpr (WHOLE && MODE == kMx8) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(row + at);
+        if constexpr (FULL && MODE == kMx8) {
+            const uint2 v = load_any<uint2>(row + at);
             x[j * per] = v.x;
             x[j * per + 1] = v.y;
-        } else if constexpr (WHOLE) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(row + 2 * at);
+        } else if constexpr (FULL) {
+            const uint4 v = load_any<uint4>(row + 2 * at);
             x[j * per] = v.x;
             x[j * per + 1] = v.y;
             x[j * per + 2] = v.z;
@@ -89,12 +89,12 @@ __device__ __forceinline__ void load_column(uint32_t (&x)[kWords<MODE>], const u
 }
 
 // A token's inputs of one step, a staged type's: k and k + 1.
-template <int MODE, bool WHOLE>
+template <int MODE, bool FULL>
 __device__ __forceinline__ void load_pair(uint32_t *x, const uint8_t *row, int k, int K) {
     if constexpr (MODE == kF32) {
         const uint32_t *p = reinterpret_cast<const uint32_t *>(row) + k;
-        if constexpr (WHOLE) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        if constexpr (FULL) {
+            const uint2 v = load_any<uint2>(p);
             x[0] = v.x;
             x[1] = v.y;
         } else {
@@ -103,8 +103,8 @@ __device__ __forceinline__ void load_pair(uint32_t *x, const uint8_t *row, int k
         }
     } else {
         const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + k;
-        if constexpr (WHOLE)
-            x[0] = *reinterpret_cast<const uint32_t *>(p);
+        if constexpr (FULL)
+            x[0] = load_any<uint32_t>(p);
         else
             x[0] = (k < K ? p[0] : 0u) | (k + 1 < K ? static_cast<uint32_t>(p[1]) : 0u) << 16;
     }
@@ -163,18 +163,18 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &q, int j) {
 }
 
 // Four consecutive outputs, `n` of them there.
-__device__ __forceinline__ void store4_as(void *y, int64_t at, const f32x4 &v, int64_t n, int type, bool whole) {
-    if (!whole || n < 4) {
+__device__ __forceinline__ void store4_as(void *y, int64_t at, const f32x4 &v, int64_t n, int type) {
+    if (n < 4) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             if (c < n) store_as(y, at + c, v[c], type);
     } else if (type == ISC_F32) {
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(y) + at) = v;
+        store_any(static_cast<float *>(y) + at, v);
     } else {
         uint32_t w[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) w[c] = type == ISC_BF16 ? BF16::narrow(v[c]) : F16::narrow(v[c]);
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(y) + at) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+        store_any(static_cast<uint16_t *>(y) + at, make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16));
     }
 }
 
@@ -236,8 +236,7 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
             s.sw[i] = *reinterpret_cast<const uint32_t *>(scales[i] + static_cast<uint32_t>(step * 64 + col * 4));
         }
     };
-    // steps whose inputs are all there, and aligned
-    const int full = MODE >= kPacked ? steps : a.whole ? a.w.K / 128 : 0;
+    const int full = MODE >= kPacked ? steps : a.w.K / 128;  // steps whose inputs are all there
 
     for (int64_t r0 = first; r0 < last; r0 += TOK * MT) {
         S ring[DEPTH];
@@ -266,8 +265,8 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
                 if constexpr (MODE == kMx8) srow[m] = a.xs + r * a.ldxs;
             }
         }
-        const auto load_x = [&](S &s, int step, auto whole) {
-            constexpr bool kWhole = decltype(whole)::value;
+        const auto load_x = [&](S &s, int step, auto is_full) {
+            constexpr bool kFull = decltype(is_full)::value;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 if constexpr (kStaged<MODE>) {
@@ -275,7 +274,7 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
 #pragma unroll
                     for (int t = 0; t < TOK; ++t)
                         if (r0 + m * TOK + t < last)
-                            load_pair<MODE, kWhole>(s.x[m] + t * per, xrow[m * TOK + t], step * 128 + 2 * lane, a.w.K);
+                            load_pair<MODE, kFull>(s.x[m] + t * per, xrow[m * TOK + t], step * 128 + 2 * lane, a.w.K);
                 } else if constexpr (MODE >= kPacked) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -287,10 +286,10 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
                         s.x[m][4 * j + 3] = v.w;
                     }
                 } else {
-                    load_column<MODE, kWhole>(s.x[m], xrow[m], step * 128 + 8 * g, a.w.K);
+                    load_column<MODE, kFull>(s.x[m], xrow[m], step * 128 + 8 * g, a.w.K);
                 }
-                if constexpr (MODE == kMx8 && kWhole) {
-                    s.sx[m] = *reinterpret_cast<const uint32_t *>(srow[m] + step * 4);
+                if constexpr (MODE == kMx8 && kFull) {
+                    s.sx[m] = load_any<uint32_t>(srow[m] + step * 4);
                 } else if constexpr (MODE == kMx8) {
                     s.sx[m] = 0u;
                     for (int j = 0; j < 4; ++j)
@@ -363,7 +362,7 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
         // steps wave, wave + waves, ...: DEPTH of them loaded ahead, without a branch
         // around a load (past the last step it is loaded again), so that a wait
         // counts the loads behind it and leaves them in flight; a last step that is
-        // not full, and rows off 16-byte boundaries, value by value
+        // not full, value by value
         const int mine = full > wave ? (full - wave + waves - 1) / waves : 0;
         if (mine > 0) {
             const auto step_of = [&](int i) { return wave + (i < mine ? i : mine - 1) * waves; };
@@ -422,7 +421,7 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) v[c] = v[c] <= 0.0f ? 0.0f : v[c];
                 const int64_t p = a.slots ? a.order[r] : r;
-                if (p >= 0 && p < all) store4_as(a.y, p * a.ldy + out, v, a.w.N - out, a.ytype, a.whole_y);
+                if (p >= 0 && p < all) store4_as(a.y, p * a.ldy + out, v, a.w.N - out, a.ytype);
             }
         }
     }
@@ -456,7 +455,7 @@ __global__ void __launch_bounds__(256) pack_x_kernel(W4Args a) {
         } else {
             using T = std::conditional_t<XTYPE == ISC_F32, F32, std::conditional_t<XTYPE == ISC_F16, F16, BF16>>;
             float v[8];
-            load8<T>(v, static_cast<const typename T::type *>(a.x) + t * a.ldx + k, n, a.whole && n >= 8);
+            load8<T>(v, static_cast<const typename T::type *>(a.x) + t * a.ldx + k, n);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t parts[P];
