@@ -100,6 +100,7 @@ class _State:
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.stream_of = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         self.device = torch.cuda.current_device
+        self.like = torch.empty_like
 
 
 def _ready():
@@ -206,13 +207,17 @@ def _on_stream(call):
 
 
 def _new(st, like, dtype, *shape):
-    """A contiguous tensor on like's device; by torch's quickest way, as a one-token
-    call spends more time on its outputs than on the GPU."""
-    strides, n = [], 1
-    for size in reversed(shape):
-        strides.append(n)
-        n *= size
-    return st.torch.empty_strided(shape, strides[::-1], dtype=dtype, device=like.device)
+    """A contiguous tensor on like's device, by torch's quickest way: a one-token call
+    spends more time on its outputs than on the GPU."""
+    if len(shape) == 2:
+        strides = (shape[1], 1)
+    else:
+        strides, n = [], 1
+        for size in reversed(shape):
+            strides.append(n)
+            n *= size
+        strides.reverse()
+    return st.torch.empty_strided(shape, strides, dtype=dtype, device=like.device)
 
 
 def _bytes(st, n, like):
@@ -241,15 +246,16 @@ def isc_rmsnorm(st, x, weight, eps=1e-6, residual=None, y=True, mx8=False, rstd=
             raise ValueError("residual must have x's shape and type")
         rr, ldr = _rows(residual, D, "residual")
         rp = rr.data_ptr()
-        h = _new(st, x, x.dtype, *shape)
+        h = st.like(xr) if ldx == D else _new(st, x, x.dtype, *shape)
         hp = h.data_ptr()
     wr = _vector(weight, D, "weight")
     if y:
-        out = _new(st, x, x.dtype, *shape)
+        out = st.like(xr) if ldx == D else _new(st, x, x.dtype, *shape)
         yp = out.data_ptr()
     groups = (D + 31) // 32
     if mx8:
-        q, scales = _new(st, x, st.f8, *shape), _new(st, x, st.e8, *shape[:-1], groups)
+        q = st.like(xr, dtype=st.f8) if ldx == D else _new(st, x, st.f8, *shape)
+        scales = _new(st, x, st.e8, *shape[:-1], groups)
         form, qp, sp = Mx8(q, scales), q.data_ptr(), scales.data_ptr()
     rs = _new(st, x, st.f32, *shape[:-1]) if rstd else None
     status = st.lib.isc_rmsnorm(
@@ -280,13 +286,16 @@ def isc_rmsnorm_bwd(st, dy, h, weight, rstd, dh=None, ws=None, stream=None):
     yr, ldy = _rows(dy, D, "dy")
     gr, ldd = (None, D) if dh is None else _rows(dh, D, "dh")
     wr = _vector(weight, D, "weight")
-    dx, dw = _new(st, h, h.dtype, *h.shape), _new(st, h, st.f32, D)
+    dx = st.like(hr) if ldh == D else _new(st, h, h.dtype, *h.shape)
+    dw = _new(st, h, st.f32, D)
     if ws is None:
         ws = _bytes(st, _size("isc_rmsnorm_bwd_workspace_size", T, D), h)
-    _isc._check(st.lib.isc_rmsnorm_bwd(
+    status = st.lib.isc_rmsnorm_bwd(
         T, D, code, yr.data_ptr(), ldy, hr.data_ptr(), ldh, wr.data_ptr(), _type(st, wr.dtype, "weight"),
         rs.data_ptr(), _ptr(gr), ldd, dx.data_ptr(), D, dw.data_ptr(), ws.data_ptr(), _isc._nbytes(ws),
-        _stream(st, stream, device)), "isc_rmsnorm_bwd")
+        _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_rmsnorm_bwd")
     return dx, dw
 
 
@@ -316,16 +325,19 @@ def isc_route(st, logits, k, bias=None, score="softmax", groups=1, keep_groups=N
     k = int(k)
     if not 1 <= k <= E:
         raise ValueError("k must be 1 to %d, not %d" % (E, k))
-    ids, weights = _new(st, logits, st.i32, T, k), _new(st, logits, st.f32, T, k)
+    ids = _new(st, logits, st.i32, T, k)
+    weights = st.like(ids, dtype=st.f32)
     offsets, order = (_new(st, logits, st.i32, E + 1), _new(st, logits, st.i32, T * k)) if lists else (None, None)
     if ws is None and lists and T > 64:
         ws = _bytes(st, _size("isc_route_workspace_size", T, E), logits)
     # an empty tensor has no address, and without tokens there is no order to write
     at = order.data_ptr() or offsets.data_ptr() if lists and not T else _ptr(order)
-    _isc._check(st.lib.isc_route(
+    status = st.lib.isc_route(
         T, E, k, code, lr.data_ptr(), ld, _ptr(br), which, groups, groups if keep_groups is None else keep_groups,
         bool(renorm), scale, ids.data_ptr(), weights.data_ptr(), _ptr(offsets), at, _ptr(ws),
-        0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device)), "isc_route")
+        0 if ws is None else _isc._nbytes(ws), _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_route")
     return Route(ids, weights, offsets, order)
 
 
@@ -345,10 +357,11 @@ def isc_route_bwd(st, dweights, logits, ids, score="softmax", renorm=True, scale
     lr, ld = _rows(logits, E, "logits")
     dr = _exact(dweights, st.f32, (T, k), "dweights")
     ir = _exact(ids, st.i32, (T, k), "ids")
-    out = _new(st, logits, logits.dtype, T, E)
-    _isc._check(st.lib.isc_route_bwd(T, E, k, code, dr.data_ptr(), lr.data_ptr(), ld, ir.data_ptr(), which,
-                                     bool(renorm), scale, out.data_ptr(), E, _stream(st, stream, device)),
-                "isc_route_bwd")
+    out = st.like(lr) if ld == E else _new(st, logits, logits.dtype, T, E)
+    status = st.lib.isc_route_bwd(T, E, k, code, dr.data_ptr(), lr.data_ptr(), ld, ir.data_ptr(), which, bool(renorm),
+                                  scale, out.data_ptr(), E, _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_route_bwd")
     return out
 
 
