@@ -716,3 +716,16 @@ def test_offsets_past_32_bits(torch, isc):
         got = call(x, many, route=route) if layout == "tiles" else call(x[:, None], many, route=route)
         assert torch.equal(got.view(1, N), want), layout
         del data, many
+
+
+def test_example(torch, isc):
+    """The block as the example runs it, small: within bfloat16's rounding of the output and of the hidden layer."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "rectified_ffn.py")
+    spec = importlib.util.spec_from_file_location("rectified_ffn", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    note("example")
+    err = example.main(["--tokens", "3", "--width", "160", "--hidden", "96", "--experts", "6", "--slots", "2", "--steps", "3"])
+    assert err <= 2.0 ** -8
