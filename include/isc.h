@@ -492,7 +492,8 @@ typedef enum isc_score {
     ISC_SCORE_SIGMOID = 1
 } isc_score;
 
-/* Bytes of workspace of isc_route (0 up to 64 tokens).  Host-only.
+/* Bytes of workspace of isc_route (0 up to 16 tokens, and up to 64 of at most
+ * 256 experts).  Host-only.
  * Errors: NULL, SHAPE, LIMIT. */
 int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes);
 
@@ -512,7 +513,7 @@ int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes);
  *     in order within one; expert e has order[offsets[e] .. offsets[e+1]).
  *     Entries from offsets[E] on are -1.
  *   ws: isc_route_workspace_size bytes, 256-byte aligned (unused without lists).
- * One launch up to 64 tokens, else two.
+ * One launch where there is no workspace, else two.
  * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_route(int32_t T, int32_t E, int32_t k, int32_t type, const void *logits, int64_t ld, const float *bias,
               int32_t score, int32_t groups, int32_t keep_groups, int32_t renorm, float scale, int32_t *ids,

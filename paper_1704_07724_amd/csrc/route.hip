@@ -20,7 +20,8 @@
 // The experts' lists.  A token meets an expert at most once, so 64 tokens and
 // an expert make one 64-bit word: a pair's place among its expert's pairs is
 // the number of bits below its token's, whatever order the bits were set in.
-// Workgroups of 64 tokens leave their counts; a second launch adds up the
+// Workgroups of 64 tokens (16 where a wavefront routes one at a time and there
+// are few) leave their counts; a second launch adds up the
 // counts of the workgroups before, and the experts' totals, and places pairs.
 #include "ffn.hpp"
 
@@ -29,7 +30,6 @@
 namespace isc {
 namespace {
 
-constexpr int kTokens = 64;   // tokens per workgroup: the bits of a word
 constexpr int kWaves = 16;    // wavefronts per workgroup
 constexpr int kMaxE = 1024;   // experts, and threads of a workgroup
 
@@ -142,20 +142,28 @@ __device__ __forceinline__ int route_token(const RouteArgs &a, int64_t t, uint32
         for (int i = 0; i < C; ++i)
             if (i * LANES + lane < a.E) row[i * LANES + lane] = key[i];
         wave_fence();
-        uint32_t g = 0;  // lane g's group; 0: none of its experts can be chosen
-        if (lane < a.groups) {
-            uint32_t best = 0, second = 0;
-#pragma unroll 8
-            for (int i = 0; i < size; ++i) {
-                const uint32_t v = row[lane * size + i];
+        // a group's two largest keys, by the lanes that share it: a power of two
+        const int share = LANES >> (32 - __builtin_clz(a.groups - 1));
+        const int of = lane / share;  // the lane's group
+        uint32_t best = 0, second = 0;
+        if (of < a.groups)
+#pragma unroll 4
+            for (int i = lane % share; i < size; i += share) {
+                const uint32_t v = row[of * size + i];
                 second = op_max(second, op_min(best, v));
                 best = op_max(best, v);
             }
-            if (best) g = order(unorder(best) + (second ? unorder(second) : 0.0f) + 0.0f);
+        for (int d = 1; d < share; d <<= 1) {
+            const uint32_t b = __shfl_xor(best, d), c = __shfl_xor(second, d);
+            second = op_max(op_min(best, b), op_max(second, c));
+            best = op_max(best, b);
         }
         wave_fence();
-        if (lane < a.groups) row[lane] = g;
+        // 0: none of its experts can be chosen
+        if (lane % share == 0 && of < a.groups)
+            row[of] = best ? order(unorder(best) + (second ? unorder(second) : 0.0f) + 0.0f) : 0u;
         wave_fence();
+        const uint32_t g = lane < a.groups ? row[lane] : 0u;  // lane g's group
         int before = 0;  // groups ranked before the lane's
         for (int j = 0; j < a.groups; ++j) {
             const uint32_t v = row[j];
@@ -223,11 +231,11 @@ __device__ __forceinline__ int block_scan(int v, int *sums) {
     return before + in - v;
 }
 
-// Routes 64 tokens a workgroup.  ONE: there is one workgroup, which also
+// Routes TOKENS tokens a workgroup.  ONE: there is one workgroup, which also
 // writes the lists; else it leaves its counts for place_kernel.
-template <int C, int LANES, bool ONE>
+template <int C, int LANES, int TOKENS, bool ONE>
 __global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
-    constexpr int kAtOnce = 64 / LANES * kWaves, kTurns = kTokens / kAtOnce;  // tokens at once, and how often
+    constexpr int kAtOnce = 64 / LANES * kWaves, kTurns = TOKENS / kAtOnce;  // tokens at once, and how often
     extern __shared__ uint32_t rows[];  // kAtOnce rows of E words, with groups
     __shared__ unsigned long long bits[kMaxE];
     __shared__ int base[kMaxE], sums[kWaves], total;
@@ -238,7 +246,7 @@ __global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
         bits[threadIdx.x] = 0ull;
         __syncthreads();
     }
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * TOKENS;
 #pragma unroll 1
     for (int i = 0; i < kTurns; ++i) {
         const int t = i * kAtOnce + own;
@@ -270,18 +278,18 @@ __global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
     for (int p = total + static_cast<int>(threadIdx.x); p < a.T * a.k; p += kMaxE) a.order[p] = -1;
 }
 
-// The lists of several workgroups' tokens.
-__global__ void __launch_bounds__(kMaxE) place_kernel(RouteArgs a) {
+// The lists of several workgroups' tokens, `tokens` each.
+__global__ void __launch_bounds__(kMaxE) place_kernel(RouteArgs a, int tokens) {
     __shared__ unsigned long long bits[kMaxE];
     __shared__ int base[kMaxE], all[kMaxE], sums[kWaves], total;
-    const int nb = (a.T + kTokens - 1) / kTokens;
+    const int nb = static_cast<int>(gridDim.x);
     const int b = blockIdx.x;
     bits[threadIdx.x] = 0ull;
     base[threadIdx.x] = all[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t p0 = static_cast<int64_t>(b) * kTokens * a.k;
+    const int64_t p0 = static_cast<int64_t>(b) * tokens * a.k;
     const int64_t left = static_cast<int64_t>(a.T) * a.k - p0;
-    const int pairs = static_cast<int>(left < kTokens * a.k ? left : kTokens * a.k);
+    const int pairs = static_cast<int>(left < tokens * a.k ? left : tokens * a.k);
     for (int p = threadIdx.x; p < pairs; p += kMaxE) {
         const int id = a.ids[p0 + p];
         if (id >= 0) atomicOr(&bits[id], 1ull << (p / a.k));
@@ -387,25 +395,36 @@ hipError_t grant_lds(Kern kern, std::atomic<bool> &granted, size_t asked) {
     return e;
 }
 
-template <int C, int LANES>
+// Tokens of a workgroup.  Over 256 experts a wavefront routes one token at a
+// time: 16 of them, all at once, unless that makes many workgroups, whose counts
+// each placing workgroup adds up (41 tokens of 424 experts in groups: 14.6 us
+// against 26.4 with 64).
+int tokens_of(int T, int E) { return E > 256 && T <= 2048 ? 16 : 64; }
+
+template <int C, int LANES, int TOKENS>
 hipError_t route_of(const RouteArgs &a, hipStream_t s) {
-    const int nb = route_blocks(a.T);
+    const int nb = route_blocks(a.T, a.E);
     const size_t lds = a.groups > 1 ? sizeof(uint32_t) * (64 / LANES) * kWaves * static_cast<size_t>(a.E) : 0;
     const dim3 grid(static_cast<unsigned>(nb)), block(kMaxE);
     if (nb == 1) {
         static std::atomic<bool> granted{false};
-        if (const hipError_t e = grant_lds(route_kernel<C, LANES, true>, granted, lds); e != hipSuccess) return e;
-        route_kernel<C, LANES, true><<<grid, block, lds, s>>>(a);
+        if (const hipError_t e = grant_lds(route_kernel<C, LANES, TOKENS, true>, granted, lds); e != hipSuccess) return e;
+        route_kernel<C, LANES, TOKENS, true><<<grid, block, lds, s>>>(a);
         return hipGetLastError();
     }
     static std::atomic<bool> granted{false};
-    hipError_t e = grant_lds(route_kernel<C, LANES, false>, granted, lds);
+    hipError_t e = grant_lds(route_kernel<C, LANES, TOKENS, false>, granted, lds);
     if (e != hipSuccess) return e;
-    route_kernel<C, LANES, false><<<grid, block, lds, s>>>(a);
+    route_kernel<C, LANES, TOKENS, false><<<grid, block, lds, s>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess || !a.order) return e;
-    place_kernel<<<grid, block, 0, s>>>(a);
+    place_kernel<<<grid, block, 0, s>>>(a, TOKENS);
     return hipGetLastError();
+}
+
+template <int C>
+hipError_t one_at_a_time(const RouteArgs &a, hipStream_t s) {
+    return tokens_of(a.T, a.E) == 16 ? route_of<C, 64, 16>(a, s) : route_of<C, 64, 64>(a, s);
 }
 
 template <int C>
@@ -417,13 +436,16 @@ hipError_t route_bwd_of(const RouteBwdArgs &a, hipStream_t s) {
 
 }  // namespace
 
-int route_blocks(int T) { return T > kTokens ? (T + kTokens - 1) / kTokens : 1; }
+int route_blocks(int T, int E) {
+    const int tokens = tokens_of(T, E);
+    return T > tokens ? (T + tokens - 1) / tokens : 1;
+}
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
     // up to 16 tokens a wavefront each: the fewer instructions count
     if (a.T > kWaves && a.E <= 256 && a.k <= 16 && a.groups <= 16)
-        return a.E <= 64 ? route_of<4, 16>(a, s) : a.E <= 128 ? route_of<8, 16>(a, s) : route_of<16, 16>(a, s);
-    return a.E <= 256 ? route_of<4, 64>(a, s) : a.E <= 512 ? route_of<8, 64>(a, s) : route_of<16, 64>(a, s);
+        return a.E <= 64 ? route_of<4, 16, 64>(a, s) : a.E <= 128 ? route_of<8, 16, 64>(a, s) : route_of<16, 16, 64>(a, s);
+    return a.E <= 256 ? route_of<4, 64, 64>(a, s) : a.E <= 512 ? one_at_a_time<8>(a, s) : one_at_a_time<16>(a, s);
 }
 
 hipError_t launch_route_bwd(const RouteBwdArgs &a, hipStream_t s) {

@@ -493,7 +493,8 @@ bool packs(int T, int xtype, int slots) { return slots == 0 && T > 16 / parts_of
 // one bfloat16 token: 12.8 us against 14.7); from 1024 on and with more than a
 // few tokens four (16 tokens: 16.1 us against 20.6).  Four wavefronts a
 // workgroup rather than eight (4096 x 4096, one token: 4.2 us against 4.8), but
-// for long rows (4096 outputs of 9216: 6.6 us against 7.4).  An expert has few rows and
+// for long rows of many outputs and few tokens (4096 outputs of 9216, one token:
+// 6.6 us against 7.4; 512 of 16384 8.1 against 7.5).  An expert has few rows and
 // many experts run: four tiles, or two where tokens are few (64 experts of 1408
 // outputs of 2048: 16 tokens 18.6 us against 20.4, one token 8.3 against 7.5).
 template <int MODE>
@@ -507,17 +508,19 @@ hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
         if (a.slots) return a.T > 4 ? run<MODE, 4, 1, 1, 256>(a, 4, s) : run<MODE, 2, 1, 2, 256>(a, 4, s);
         if (tiles >= 1024 && a.T > 4) return run<MODE, 4, 1, 2, 256>(a, 4, s);
         if (tiles >= 512) return run<MODE, 2, 1, 1, 256>(a, 4, s);
-        if (steps > 48) return run<MODE, 1, 1, 2, 512>(a, 8, s);
+        if (steps > 48 && tiles >= 128 && a.T <= 4) return run<MODE, 1, 1, 2, 512>(a, 8, s);
         return run<MODE, 1, 1, 2, 256>(a, 4, s);
     }
 }
 
-// The same choice for an x that was laid out, by the blocks of one tile of
-// outputs and two of columns: one block a workgroup while there are no more than
-// compute units, then two tiles of outputs, then four, then four of columns too
-// (bfloat16, us, in that order: 4096 x 4096 at 17 tokens 8.6 9.2 11.2 13.2, at 64
-// 12.0 9.6 11.7 14.8, 4096 x 8192 at 64 18.4 13.8 12.6 15.5, 8192 x 16384 at 64
-// 53.6 35.9 28.2 25.0).
+// The same choice for an x that was laid out: a workgroup for every tile of
+// outputs and of columns while there are no more than compute units (1024
+// outputs of 8192, 47 bfloat16 tokens: 9.2 us against 11.1 with two tiles of
+// columns), then by the blocks of one tile of outputs and two of columns: one
+// block a workgroup up to 256, two tiles of outputs up to 512, four up to 1024,
+// then four of columns too (us, in that order: 4096 x 4096 at 64 tokens 12.0 9.6
+// 11.7 14.8, 8192 outputs of 4096 18.4 13.8 12.6 15.5, 16384 of 8192 53.6 35.9
+// 28.2 25.0).
 template <int XTYPE>
 hipError_t packed(const W4Args &a, hipStream_t s) {
     constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, MODE = kPacked + P - 1;
@@ -525,6 +528,7 @@ hipError_t packed(const W4Args &a, hipStream_t s) {
     pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const int64_t blocks = a.w.tiles() * ((tiles + 1) / 2);
+    if (a.w.tiles() * tiles <= 256) return run<MODE, 1, 1, 2, 256>(a, 4, s);
     if (blocks <= 256) return run<MODE, 1, 2, 2, 256>(a, 4, s);
     if (blocks <= 512) return run<MODE, 2, 2, 2, 256>(a, 4, s);
     if (blocks <= 1024) return run<MODE, 4, 2, 2, 256>(a, 4, s);

@@ -328,8 +328,9 @@ def isc_route(st, logits, k, bias=None, score="softmax", groups=1, keep_groups=N
     ids = _new(st, logits, st.i32, T, k)
     weights = st.like(ids, dtype=st.f32)
     offsets, order = (_new(st, logits, st.i32, E + 1), _new(st, logits, st.i32, T * k)) if lists else (None, None)
-    if ws is None and lists and T > 64:
-        ws = _bytes(st, _size("isc_route_workspace_size", T, E), logits)
+    if ws is None and lists and T > 16:
+        n = _size("isc_route_workspace_size", T, E)
+        ws = _bytes(st, n, logits) if n else None
     # an empty tensor has no address, and without tokens there is no order to write
     at = order.data_ptr() or offsets.data_ptr() if lists and not T else _ptr(order)
     status = st.lib.isc_route(

@@ -49,12 +49,14 @@ def test_norm_bwd_refusals():
     assert norm_bwd(T=0, dy=None, h=None, w=None, rstd=None, dx=None) in OK  # dw = 0 is still written
     assert norm_bwd(N=0) == SHAPE and norm_bwd(ldh=63) == SHAPE and norm_bwd(ldx=1) == SHAPE
     assert norm_bwd(N=16385, ldy=20000, ldh=20000, ldd=20000, ldx=20000) == LIMIT
-    assert norm_bwd(n=511) == WORKSPACE and norm_bwd(ws=F + 16) == ALIGN and norm_bwd(t=3) == ARG
+    assert norm_bwd(ws=F + 16) == ALIGN and norm_bwd(t=3) == ARG
     assert norm_bwd(dw=C) == ALIAS and norm_bwd(dx=A + 4) == ALIAS and norm_bwd(ws=A) == ALIAS
     n = ctypes.c_size_t()
     assert isc.lib().isc_rmsnorm_bwd_workspace_size(2, 64, None) == NULL
     assert isc.lib().isc_rmsnorm_bwd_workspace_size(-1, 64, n) == SHAPE
-    assert isc.lib().isc_rmsnorm_bwd_workspace_size(2, 64, n) == 0 and n.value >= 2 * 64 * 4
+    # a row of sums a workgroup at least, and nothing less than the size it names
+    assert isc.lib().isc_rmsnorm_bwd_workspace_size(2, 64, n) == 0 and n.value >= 64 * 4
+    assert norm_bwd(n=n.value - 1) == WORKSPACE and norm_bwd(n=n.value) in OK
 
 
 def route(T=100, N=16, k=2, t=0, l=A, ld=16, bias=B, score=0, groups=4, keep=2, renorm=1, scale=1.0, ids=C, w=D, off=E,
