@@ -18,6 +18,7 @@
 // DEPTH steps' operands in registers, loads in flight behind the matrix work.
 #include "ffn.hpp"
 
+#include <cstdint>
 #include <type_traits>
 
 namespace isc {
@@ -182,7 +183,7 @@ template <int MODE, int NT, int MT, int DEPTH, int THREADS>
 __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
     constexpr int TOK = kTokens<MODE>, P = kParts<MODE>;
     constexpr int kSize = MODE == kF32 ? 4 : MODE == kMx8 ? 1 : 2;
-    constexpr int ROUND = MT < 2 ? MT : 2;  // tiles of columns whose sums are in LDS together
+    constexpr int ROUND = MT % 2 ? 1 : 2;  // tiles of columns whose sums are in LDS together
     extern __shared__ f32x4 sums[];         // [wavefronts][NT][ROUND][kSumTile]; then the staged columns
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -475,7 +476,7 @@ hipError_t run(const W4Args &a, int waves, hipStream_t s) {
     const int64_t rows = kTokens<MODE> * MT;
     const unsigned y = static_cast<unsigned>(a.slots ? a.w.E + 1 : (a.T + rows - 1) / rows);
     while (waves > 1 && waves / 2 >= a.w.steps()) waves /= 2;  // no more wavefronts than steps
-    const size_t lds = static_cast<size_t>(waves) * (sizeof(f32x4) * kSumTile * NT * (MT < 2 ? MT : 2) + (kStaged<MODE> ? MT * kStageTile : 0));
+    const size_t lds = static_cast<size_t>(waves) * (sizeof(f32x4) * kSumTile * NT * (MT % 2 ? 1 : 2) + (kStaged<MODE> ? MT * kStageTile : 0));
     w4_linear_kernel<MODE, NT, MT, DEPTH, THREADS>
         <<<dim3(static_cast<unsigned>(tiles), y), dim3(static_cast<unsigned>(64 * waves)), lds, s>>>(a);
     return hipGetLastError();
@@ -513,26 +514,41 @@ hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
     }
 }
 
-// The same choice for an x that was laid out: a workgroup for every tile of
-// outputs and of columns while there are no more than compute units (1024
-// outputs of 8192, 47 bfloat16 tokens: 9.2 us against 11.1 with two tiles of
-// columns), then by the blocks of one tile of outputs and two of columns: one
-// block a workgroup up to 256, two tiles of outputs up to 512, four up to 1024,
-// then four of columns too (us, in that order: 4096 x 4096 at 64 tokens 12.0 9.6
-// 11.7 14.8, 8192 outputs of 4096 18.4 13.8 12.6 15.5, 16384 of 8192 53.6 35.9
-// 28.2 25.0).
+// The same choice for an x that was laid out: of the shapes below, the one whose
+// rounds of 256 workgroups take the least time together, a round's being what it
+// measured (8192 inputs, 64 bfloat16 tokens).  Small shapes fill the chip, large
+// ones read less for each product.  Measured against the next best shape: 1024
+// outputs of 8192, 47 tokens 9.2 us against 11.1; 4096 of 4096 at 64 tokens 9.6
+// (11.5) and at 130 14.0 (16.0); 5000 of 16384 at 64 24.4 (28.8) and at 256 65.9
+// (72.9); 16384 of 8192 at 64 25.0 (27.4), at 130 53.5 (60.0) and at 2048 635
+// (693), where 866 TFLOP/s are done.
+struct Shape {
+    int nt, mt, round;  // tiles of outputs and of columns a workgroup; 0.1 us a round
+};
+constexpr Shape kShapes[] = {{1, 1, 95}, {1, 2, 123}, {2, 2, 140}, {3, 2, 160}, {4, 2, 186}, {3, 3, 190}, {4, 3, 207}, {4, 4, 235}};
+
+template <int MODE, int I = 0>
+hipError_t run_shape(int i, const W4Args &a, hipStream_t s) {
+    if constexpr (I + 1 < static_cast<int>(sizeof(kShapes) / sizeof(kShapes[0])))
+        if (i != I) return run_shape<MODE, I + 1>(i, a, s);
+    return run<MODE, kShapes[I].nt, kShapes[I].mt, 2, 256>(a, 4, s);
+}
+
 template <int XTYPE>
 hipError_t packed(const W4Args &a, hipStream_t s) {
     constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, MODE = kPacked + P - 1;
     const int64_t tiles = (a.T + kTokens<MODE> - 1) / kTokens<MODE>;
     pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const int64_t blocks = a.w.tiles() * ((tiles + 1) / 2);
-    if (a.w.tiles() * tiles <= 256) return run<MODE, 1, 1, 2, 256>(a, 4, s);
-    if (blocks <= 256) return run<MODE, 1, 2, 2, 256>(a, 4, s);
-    if (blocks <= 512) return run<MODE, 2, 2, 2, 256>(a, 4, s);
-    if (blocks <= 1024) return run<MODE, 4, 2, 2, 256>(a, 4, s);
-    return run<MODE, 4, 4, 2, 256>(a, 4, s);
+    int best = 0, i = 0;
+    int64_t least = INT64_MAX;
+    for (const Shape &h : kShapes) {
+        const int64_t workgroups = ((a.w.tiles() + h.nt - 1) / h.nt) * ((tiles + h.mt - 1) / h.mt);
+        const int64_t time = (workgroups + 255) / 256 * h.round;
+        if (time < least) least = time, best = i;
+        ++i;
+    }
+    return run_shape<MODE>(best, a, s);
 }
 
 }  // namespace

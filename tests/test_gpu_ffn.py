@@ -483,6 +483,20 @@ def test_linear_tilings(torch, isc, T, N, K, xtype):
     close(host(isc.isc_w4_linear(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
 
 
+@pytest.mark.parametrize("xtype", TYPES + ["mx8"])
+@pytest.mark.parametrize("T,N", [(20, 8900), (20, 13000), (40, 11000), (40, 14001), (11, 11000), (11, 14000), (90, 4100), (130, 4100)])
+def test_linear_workgroup_shapes(torch, isc, T, N, xtype):
+    """Three and four tiles of outputs by two and three of columns."""
+    note("linear workgroup shapes", T, N, xtype)
+    r, K = np.random.default_rng(T + N), 700
+    w4, w = weights(torch, isc, r, 1, N, K, "tiles")
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.product(w[0], xv)
+    close(host(isc.isc_w4_linear(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
 @pytest.mark.parametrize("xtype", ["bfloat16", "float16", "mx8"])
 @pytest.mark.parametrize("T", [2, 4, 5, 60])
 def test_experts_long_rows(torch, isc, T, xtype):
