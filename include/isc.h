@@ -493,7 +493,7 @@ typedef enum isc_score {
 } isc_score;
 
 /* Bytes of workspace of isc_route (0 up to 16 tokens, and up to 64 of at most
- * 256 experts).  Host-only.
+ * 128 experts).  Host-only.
  * Errors: NULL, SHAPE, LIMIT. */
 int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes);
 

@@ -217,9 +217,9 @@ struct RouteArgs {
     int32_t *ids;
     float *weights;
     int32_t *offsets, *order;  // both nullptr where the lists are not asked for
-    uint16_t *counts;          // route_blocks() rows of E counts, where there are several
+    uint16_t *counts;          // a row of counts for every workgroup, where there are several
 };
-int route_blocks(int T, int E);
+size_t route_count_bytes(int T, int E);
 hipError_t launch_route(const RouteArgs &a, hipStream_t s);
 
 struct RouteBwdArgs {

@@ -129,8 +129,7 @@ int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes) {
     if (!bytes) return ISC_ERR_NULL;
     if (T < 0 || E < 1) return ISC_ERR_SHAPE;
     if (E > kMaxExperts) return ISC_ERR_LIMIT;
-    const int blocks = isc::route_blocks(T, E);
-    *bytes = blocks > 1 ? sizeof(uint16_t) * static_cast<size_t>(blocks) * static_cast<size_t>(E) : 0;
+    *bytes = isc::route_count_bytes(T, E);
     return ISC_OK;
 }
 

@@ -8,21 +8,21 @@
 // An expert whose logit (or key) is -inf or NaN is never chosen; a token with
 // fewer than k experts left gets id -1 and weight 0 in its last slots.
 //
-// LANES lanes share a token, 16 where it has at most 256 experts (and 16 slots
-// and groups), so that a wavefront routes four; else 64.  The keys stay in
-// registers as unsigned integers in the floats' order, the experts of a lane
-// LANES apart; a slot is a maximum and then a minimum of the indices that have
-// it, by data-parallel moves.  Four tokens a wavefront rather than one take
-// 8192 tokens of 128 experts from 16.4 to 9.2 us.  Latency bounds both ends: 16
-// tokens of 256 experts in groups take 8.8 us, 8192 of 128 with their lists
-// 14.5 us, where moving the 3 MB would take one.
+// LANES lanes share a token, 64 or (many tokens, at most 256 experts, 16 slots
+// and groups) 16, so that a wavefront routes four.  The keys stay in registers
+// as unsigned integers in the floats' order, the experts of a lane LANES apart;
+// a slot is a maximum and then a minimum of the indices that have it, by
+// data-parallel moves.  A token's slots wait for each other, and that bounds all
+// but the largest calls: 16 tokens of 256 experts in groups take 9.2 us, 4096
+// tokens 14.1, 8192 of 128 experts with their lists 11.9, where moving the 3 MB
+// would take one; 16384 of 256 in groups, where the instructions count, 24.2.
 //
 // The experts' lists.  A token meets an expert at most once, so 64 tokens and
 // an expert make one 64-bit word: a pair's place among its expert's pairs is
 // the number of bits below its token's, whatever order the bits were set in.
-// Workgroups of 64 tokens (16 where a wavefront routes one at a time and there
-// are few) leave their counts; a second launch adds up the
-// counts of the workgroups before, and the experts' totals, and places pairs.
+// Workgroups of 16 to 64 tokens leave their counts; a second launch, of 64 tokens
+// a workgroup, adds up the counts of the workgroups before, and the experts'
+// totals, and places pairs.
 #include "ffn.hpp"
 
 #include <atomic>
@@ -231,19 +231,35 @@ __device__ __forceinline__ int block_scan(int v, int *sums) {
     return before + in - v;
 }
 
+// Tokens of a workgroup.  One launch does for 16 tokens, and for 64 of at most
+// 128 experts (40 of 128: 8.1 us against 8.5 with two).  Else 16 tokens, then 32,
+// while that makes no more workgroups than compute units, or 64 (8 of 400 experts
+// at 4096 tokens 16.8, 21.5, 31.7 us, in that order; at 8192 26.6, 23.8, 33.2; at
+// 16384 46.7, 41.6, 36.9).
+int tokens_of(int T, int E) {
+    return T > 8192 || (T <= 64 && E <= 128) ? 64 : T > 4096 ? 32 : 16;
+}
+
+int blocks_of(int T, int E) {
+    const int tokens = tokens_of(T, E);
+    return T > tokens ? (T + tokens - 1) / tokens : 1;
+}
+
+// A workgroup's counts: whole words of four.
+__host__ __device__ constexpr int count_stride(int E) { return (E + 3) & ~3; }
+
 // Routes TOKENS tokens a workgroup.  ONE: there is one workgroup, which also
 // writes the lists; else it leaves its counts for place_kernel.
-template <int C, int LANES, int TOKENS, bool ONE>
-__global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
-    constexpr int kAtOnce = 64 / LANES * kWaves, kTurns = TOKENS / kAtOnce;  // tokens at once, and how often
+template <int C, int LANES, int THREADS, int TOKENS, bool ONE>
+__global__ void __launch_bounds__(THREADS) route_kernel(RouteArgs a) {
+    constexpr int kAtOnce = THREADS / LANES, kTurns = TOKENS / kAtOnce;  // tokens at once, and how often
     extern __shared__ uint32_t rows[];  // kAtOnce rows of E words, with groups
     __shared__ unsigned long long bits[kMaxE];
-    __shared__ int base[kMaxE], sums[kWaves], total;
     const int lane = threadIdx.x & (LANES - 1);
     const int own = LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / LANES;
     const bool lists = a.order != nullptr;
     if (lists) {
-        bits[threadIdx.x] = 0ull;
+        for (int e = threadIdx.x; e < a.E; e += THREADS) bits[e] = 0ull;
         __syncthreads();
     }
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * TOKENS;
@@ -257,63 +273,72 @@ __global__ void __launch_bounds__(kMaxE) route_kernel(RouteArgs a) {
     }
     if (!lists) return;
     __syncthreads();
-    const int e = threadIdx.x;
-    const int count = e < a.E ? __popcll(bits[e]) : 0;
     if constexpr (!ONE) {
-        if (e < a.E) a.counts[static_cast<int64_t>(blockIdx.x) * a.E + e] = static_cast<uint16_t>(count);
-        return;
+        const int stride = count_stride(a.E);
+        for (int e = threadIdx.x; e < stride; e += THREADS)
+            a.counts[static_cast<int64_t>(blockIdx.x) * stride + e] = static_cast<uint16_t>(e < a.E ? __popcll(bits[e]) : 0);
+    } else {
+        static_assert(THREADS == kMaxE);
+        __shared__ int base[kMaxE], sums[kWaves], total;
+        const int e = threadIdx.x;
+        const int count = e < a.E ? __popcll(bits[e]) : 0;
+        base[e] = block_scan(count, sums);
+        if (e < a.E) a.offsets[e] = base[e];
+        if (e == kMaxE - 1) {
+            total = base[e] + count;
+            a.offsets[a.E] = total;
+        }
+        __syncthreads();
+        const int pairs = a.T * a.k;
+        for (int p = threadIdx.x; p < pairs; p += kMaxE) {  // written by this workgroup, before the barriers
+            const int id = a.ids[p], t = p / a.k;
+            if (id >= 0) a.order[base[id] + __popcll(bits[id] & ((1ull << t) - 1))] = p;
+        }
+        for (int p = total + static_cast<int>(threadIdx.x); p < a.T * a.k; p += kMaxE) a.order[p] = -1;
     }
-    base[e] = block_scan(count, sums);
-    if (e < a.E) a.offsets[e] = base[e];
-    if (e == kMaxE - 1) {
-        total = base[e] + count;
-        a.offsets[a.E] = total;
-    }
-    __syncthreads();
-    const int pairs = a.T * a.k;
-    for (int p = threadIdx.x; p < pairs; p += kMaxE) {  // written by this workgroup, before the barriers
-        const int id = a.ids[p], t = p / a.k;
-        if (id >= 0) a.order[base[id] + __popcll(bits[id] & ((1ull << t) - 1))] = p;
-    }
-    for (int p = total + static_cast<int>(threadIdx.x); p < a.T * a.k; p += kMaxE) a.order[p] = -1;
 }
 
 // The lists of several workgroups' tokens, `tokens` each.
 __global__ void __launch_bounds__(kMaxE) place_kernel(RouteArgs a, int tokens) {
     __shared__ unsigned long long bits[kMaxE];
     __shared__ int base[kMaxE], all[kMaxE], sums[kWaves], total;
-    const int nb = static_cast<int>(gridDim.x);
+    const int nb = (a.T + tokens - 1) / tokens, own = 64 / tokens;  // workgroups that routed, and those of this one's tokens
     const int b = blockIdx.x;
     bits[threadIdx.x] = 0ull;
     base[threadIdx.x] = all[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t p0 = static_cast<int64_t>(b) * tokens * a.k;
+    const int64_t p0 = static_cast<int64_t>(b) * 64 * a.k;
     const int64_t left = static_cast<int64_t>(a.T) * a.k - p0;
-    const int pairs = static_cast<int>(left < tokens * a.k ? left : tokens * a.k);
+    const int pairs = static_cast<int>(left < 64 * a.k ? left : 64 * a.k);
     for (int p = threadIdx.x; p < pairs; p += kMaxE) {
         const int id = a.ids[p0 + p];
         if (id >= 0) atomicOr(&bits[id], 1ull << (p / a.k));
     }
-    // threads share the counts: each an expert and every `step`-th workgroup
+    // threads share the counts: each four experts of every `step`-th workgroup
     // (integer sums: any order gives the same)
-    const int step = kMaxE / a.E;
-    if (static_cast<int>(threadIdx.x) < step * a.E) {
-        const int e = threadIdx.x % a.E;
-        int before = 0, n = 0;
-        for (int i = threadIdx.x / a.E; i < nb; i += 8 * step) {
-            int c[8];
+    const int quads = count_stride(a.E) / 4, step = kMaxE / quads;
+    if (static_cast<int>(threadIdx.x) < step * quads) {
+        const int q = threadIdx.x % quads;
+        const uint2 *counts = reinterpret_cast<const uint2 *>(a.counts) + q;
+        int before[4] = {}, n[4] = {};
+        for (int i = threadIdx.x / quads; i < nb; i += 8 * step) {
+            uint2 c[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                c[j] = a.counts[static_cast<int64_t>(i + j * step < nb ? i + j * step : i) * a.E + e];
+            for (int j = 0; j < 8; ++j) c[j] = counts[static_cast<int64_t>(i + j * step < nb ? i + j * step : i) * quads];
+            uint2 u = {}, v = {};  // two counts a word: eight of at most 64 stay below 2^16
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int v = i + j * step < nb ? c[j] : 0;
-                n += v;
-                if (i + j * step < b) before += v;
+                if (i + j * step < nb) u.x += c[j].x, u.y += c[j].y;
+                if (i + j * step < b * own) v.x += c[j].x, v.y += c[j].y;
             }
+            n[0] += u.x & 0xffff, n[1] += u.x >> 16, n[2] += u.y & 0xffff, n[3] += u.y >> 16;
+            before[0] += v.x & 0xffff, before[1] += v.x >> 16, before[2] += v.y & 0xffff, before[3] += v.y >> 16;
         }
-        atomicAdd(&all[e], n);
-        atomicAdd(&base[e], before);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            atomicAdd(&all[4 * q + j], n[j]);
+            atomicAdd(&base[4 * q + j], before[j]);
+        }
     }
     __syncthreads();
     const int e = threadIdx.x;
@@ -333,7 +358,7 @@ __global__ void __launch_bounds__(kMaxE) place_kernel(RouteArgs a, int tokens) {
     }
     // the unused tail, spread over the workgroups
     for (int64_t p = total + static_cast<int64_t>(b) * kMaxE + threadIdx.x; p < static_cast<int64_t>(a.T) * a.k;
-         p += static_cast<int64_t>(nb) * kMaxE)
+         p += static_cast<int64_t>(gridDim.x) * kMaxE)
         a.order[p] = -1;
 }
 
@@ -395,36 +420,35 @@ hipError_t grant_lds(Kern kern, std::atomic<bool> &granted, size_t asked) {
     return e;
 }
 
-// Tokens of a workgroup.  Over 256 experts a wavefront routes one token at a
-// time: 16 of them, all at once, unless that makes many workgroups, whose counts
-// each placing workgroup adds up (41 tokens of 424 experts in groups: 14.6 us
-// against 26.4 with 64).
-int tokens_of(int T, int E) { return E > 256 && T <= 2048 ? 16 : 64; }
-
-template <int C, int LANES, int TOKENS>
-hipError_t route_of(const RouteArgs &a, hipStream_t s) {
-    const int nb = route_blocks(a.T, a.E);
-    const size_t lds = a.groups > 1 ? sizeof(uint32_t) * (64 / LANES) * kWaves * static_cast<size_t>(a.E) : 0;
-    const dim3 grid(static_cast<unsigned>(nb)), block(kMaxE);
-    if (nb == 1) {
-        static std::atomic<bool> granted{false};
-        if (const hipError_t e = grant_lds(route_kernel<C, LANES, TOKENS, true>, granted, lds); e != hipSuccess) return e;
-        route_kernel<C, LANES, TOKENS, true><<<grid, block, lds, s>>>(a);
-        return hipGetLastError();
-    }
+template <int C, int LANES, int THREADS, int TOKENS, bool ONE>
+hipError_t route_with(const RouteArgs &a, int blocks, hipStream_t s) {
     static std::atomic<bool> granted{false};
-    hipError_t e = grant_lds(route_kernel<C, LANES, TOKENS, false>, granted, lds);
-    if (e != hipSuccess) return e;
-    route_kernel<C, LANES, TOKENS, false><<<grid, block, lds, s>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess || !a.order) return e;
-    place_kernel<<<grid, block, 0, s>>>(a, TOKENS);
+    const size_t lds = a.groups > 1 ? sizeof(uint32_t) * (THREADS / LANES) * static_cast<size_t>(a.E) : 0;
+    if (const hipError_t e = grant_lds(route_kernel<C, LANES, THREADS, TOKENS, ONE>, granted, lds); e != hipSuccess) return e;
+    route_kernel<C, LANES, THREADS, TOKENS, ONE><<<dim3(static_cast<unsigned>(blocks)), dim3(THREADS), lds, s>>>(a);
     return hipGetLastError();
 }
 
+template <int C, int LANES, int THREADS, int TOKENS>
+hipError_t route_of(const RouteArgs &a, hipStream_t s) {
+    const int nb = blocks_of(a.T, a.E);
+    if (nb == 1) return route_with<C, LANES, kMaxE, 64, true>(a, 1, s);
+    const hipError_t e = route_with<C, LANES, THREADS, TOKENS, false>(a, nb, s);
+    if (e != hipSuccess || !a.order) return e;
+    place_kernel<<<dim3(static_cast<unsigned>((a.T + 63) / 64)), dim3(kMaxE), 0, s>>>(a, TOKENS);
+    return hipGetLastError();
+}
 template <int C>
 hipError_t one_at_a_time(const RouteArgs &a, hipStream_t s) {
-    return tokens_of(a.T, a.E) == 16 ? route_of<C, 64, 16>(a, s) : route_of<C, 64, 64>(a, s);
+    const int tokens = tokens_of(a.T, a.E);
+    return tokens == 16   ? route_of<C, 64, kMaxE, 16>(a, s)
+           : tokens == 32 ? route_of<C, 64, kMaxE, 32>(a, s)
+                          : route_of<C, 64, kMaxE, 64>(a, s);
+}
+
+template <int C>
+hipError_t four_at_a_time(const RouteArgs &a, hipStream_t s) {
+    return tokens_of(a.T, a.E) == 32 ? route_of<C, 16, 512, 32>(a, s) : route_of<C, 16, kMaxE, 64>(a, s);
 }
 
 template <int C>
@@ -436,16 +460,24 @@ hipError_t route_bwd_of(const RouteBwdArgs &a, hipStream_t s) {
 
 }  // namespace
 
-int route_blocks(int T, int E) {
-    const int tokens = tokens_of(T, E);
-    return T > tokens ? (T + tokens - 1) / tokens : 1;
+size_t route_count_bytes(int T, int E) {
+    const int blocks = blocks_of(T, E);
+    return blocks > 1 ? sizeof(uint16_t) * static_cast<size_t>(blocks) * static_cast<size_t>(count_stride(E)) : 0;
 }
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
-    // up to 16 tokens a wavefront each: the fewer instructions count
-    if (a.T > kWaves && a.E <= 256 && a.k <= 16 && a.groups <= 16)
-        return a.E <= 64 ? route_of<4, 16, 64>(a, s) : a.E <= 128 ? route_of<8, 16, 64>(a, s) : route_of<16, 16, 64>(a, s);
-    return a.E <= 256 ? route_of<4, 64, 64>(a, s) : a.E <= 512 ? one_at_a_time<8>(a, s) : one_at_a_time<16>(a, s);
+    // Four tokens a wavefront take fewer instructions a token, one a wavefront
+    // fewer in a row: the one where there are tokens enough for every wavefront,
+    // the other below (8 of 256 experts in groups at 4096 tokens 18.1 and 14.2 us,
+    // at 8192 19.5 and 20.1), but for a single workgroup (40 tokens of 128
+    // experts: 8.1 and 9.4 us; up to 16 tokens there is a wavefront for each).
+    if (tokens_of(a.T, a.E) > 16 && a.T > kWaves && a.E <= 256 && a.k <= 16 && a.groups <= 16)
+        return a.E <= 64 ? four_at_a_time<4>(a, s) : a.E <= 128 ? four_at_a_time<8>(a, s) : four_at_a_time<16>(a, s);
+    return a.E <= 64    ? one_at_a_time<1>(a, s)
+           : a.E <= 128 ? one_at_a_time<2>(a, s)
+           : a.E <= 256 ? one_at_a_time<4>(a, s)
+           : a.E <= 512 ? one_at_a_time<8>(a, s)
+                        : one_at_a_time<16>(a, s);
 }
 
 hipError_t launch_route_bwd(const RouteBwdArgs &a, hipStream_t s) {

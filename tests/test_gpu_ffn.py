@@ -318,6 +318,30 @@ def test_route(torch, isc, case):
     assert torch.equal(again.ids, got.ids) and torch.equal(again.weights, got.weights) and again.order is None
 
 
+@pytest.mark.parametrize("E,k,groups", [(64, 6, 1), (64, 20, 1), (100, 8, 20), (128, 8, 1), (256, 8, 8), (400, 8, 1), (603, 5, 9)])
+@pytest.mark.parametrize("T", [17, 64, 65, 700, 4097, 8192, 8205])
+def test_route_workgroups(torch, isc, T, E, k, groups):
+    """Many tokens: each as in a small call, and the lists of all of them."""
+    note("route workgroups", T, E, k, groups)
+    r = np.random.default_rng(T + E)
+    x = dev(torch, r.standard_normal((T, E)), "bfloat16")
+    x[T // 3] = float("-inf")
+    x[T // 2, 3:] = float("-inf")
+    keep = max(1, groups // 2)
+    got = isc.isc_route(x, k, score="sigmoid", groups=groups, keep_groups=keep)
+    ids, weights_ = host(got.ids), host(got.weights)
+    for t in sorted({0, 16 * (T // 32), max(0, T - 16)}):
+        small = isc.isc_route(x[t:t + 16], k, score="sigmoid", groups=groups, keep_groups=keep)
+        assert np.array_equal(ids[t:t + 16], host(small.ids))
+        # k weights of fp32, in another order of summing
+        assert np.abs(weights_[t:t + 16] - host(small.weights)).max() <= (k + 4) * E24
+    flat = ids.reshape(-1)
+    order = np.argsort(np.where(flat < 0, E, flat), kind="stable")
+    n = int((flat >= 0).sum())
+    assert host(got.offsets).tolist() == np.concatenate([[0], np.cumsum(np.bincount(flat[flat >= 0], minlength=E))]).tolist()
+    assert np.array_equal(host(got.order)[:n], order[:n]) and (host(got.order)[n:] == -1).all()
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 def test_route_types_and_ties(torch, isc, dtype):
     """Coarse logits: many exact ties, each to the lowest index."""
