@@ -515,23 +515,36 @@ hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
 }
 
 // The same choice for an x that was laid out: of the shapes below, the one whose
-// rounds of 256 workgroups take the least time together, a round's being what it
-// measured (8192 inputs, 64 bfloat16 tokens).  Small shapes fill the chip, large
-// ones read less for each product.  Measured against the next best shape: 1024
-// outputs of 8192, 47 tokens 9.2 us against 11.1; 4096 of 4096 at 64 tokens 9.6
-// (11.5) and at 130 14.0 (16.0); 5000 of 16384 at 64 24.4 (28.8) and at 256 65.9
-// (72.9); 16384 of 8192 at 64 25.0 (27.4), at 130 53.5 (60.0) and at 2048 635
-// (693), where 866 TFLOP/s are done.
+// workgroups take the least time together.  With two steps ahead a compute unit
+// holds one workgroup, with one step (fewer registers) two, which is better where
+// there are more than 256; a round's time is what it measured (8192 inputs, 64
+// bfloat16 tokens and more).  Small shapes fill the chip, large ones read less for
+// each product.  Measured against the next best shape: 1024 outputs of 8192, 47
+// tokens 9.2 us against 11.1; 4096 of 4096 at 64 tokens 9.6 (11.5) and at 130 14.0
+// (16.0); 5000 of 16384 at 64 24.4 (28.8); 16384 of 8192 at 64 25.0 (27.4), at 130
+// 50.2 (54.5), at 200 67.9 (73.2, and 78.7 with two steps ahead) and at 2048 549
+// (599, 633), where 1000 TFLOP/s are done.
 struct Shape {
-    int nt, mt, round;  // tiles of outputs and of columns a workgroup; 0.1 us a round
+    int nt, mt, depth;  // tiles of outputs and of columns a workgroup, steps ahead
+    int round, rest;    // 0.1 us a round of 256 workgroups, of 512 with one step ahead; a last round of 256 of those
 };
-constexpr Shape kShapes[] = {{1, 1, 95}, {1, 2, 123}, {2, 2, 140}, {3, 2, 160}, {4, 2, 186}, {3, 3, 190}, {4, 3, 207}, {4, 4, 235}};
+constexpr Shape kShapes[] = {{1, 1, 2, 95, 0},  {1, 2, 2, 123, 0}, {2, 2, 2, 140, 0},   {3, 2, 2, 160, 0},
+                             {4, 2, 2, 186, 0}, {3, 3, 2, 190, 0}, {4, 3, 2, 207, 0},   {4, 4, 2, 235, 0},
+                             {3, 3, 1, 245, 150}, {4, 3, 1, 285, 180}, {4, 4, 1, 360, 200}};
+constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
+
+int64_t time_of(const Shape &h, int64_t workgroups) {
+    if (h.depth == 2) return (workgroups + 255) / 256 * h.round;
+    if (workgroups <= 256) return INT64_MAX;
+    const int64_t left = workgroups % 512;
+    return workgroups / 512 * h.round + (left > 256 ? h.round : left > 0 ? h.rest : 0);
+}
 
 template <int MODE, int I = 0>
 hipError_t run_shape(int i, const W4Args &a, hipStream_t s) {
-    if constexpr (I + 1 < static_cast<int>(sizeof(kShapes) / sizeof(kShapes[0])))
+    if constexpr (I + 1 < kShapeCount)
         if (i != I) return run_shape<MODE, I + 1>(i, a, s);
-    return run<MODE, kShapes[I].nt, kShapes[I].mt, 2, 256>(a, 4, s);
+    return run<MODE, kShapes[I].nt, kShapes[I].mt, kShapes[I].depth, 256>(a, 4, s);
 }
 
 template <int XTYPE>
@@ -540,13 +553,12 @@ hipError_t packed(const W4Args &a, hipStream_t s) {
     const int64_t tiles = (a.T + kTokens<MODE> - 1) / kTokens<MODE>;
     pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    int best = 0, i = 0;
+    int best = 0;
     int64_t least = INT64_MAX;
-    for (const Shape &h : kShapes) {
-        const int64_t workgroups = ((a.w.tiles() + h.nt - 1) / h.nt) * ((tiles + h.mt - 1) / h.mt);
-        const int64_t time = (workgroups + 255) / 256 * h.round;
+    for (int i = 0; i < kShapeCount; ++i) {
+        const Shape &h = kShapes[i];
+        const int64_t time = time_of(h, ((a.w.tiles() + h.nt - 1) / h.nt) * ((tiles + h.mt - 1) / h.mt));
         if (time < least) least = time, best = i;
-        ++i;
     }
     return run_shape<MODE>(best, a, s);
 }

@@ -508,7 +508,8 @@ def test_linear_tilings(torch, isc, T, N, K, xtype):
 
 
 @pytest.mark.parametrize("xtype", TYPES + ["mx8"])
-@pytest.mark.parametrize("T,N", [(20, 8900), (20, 13000), (40, 11000), (40, 14001), (11, 11000), (11, 14000), (90, 4100), (130, 4100)])
+@pytest.mark.parametrize("T,N", [(20, 8900), (20, 13000), (40, 11000), (40, 14001), (11, 11000), (11, 14000), (90, 4100), (130, 4100),
+                                 (100, 16400), (130, 7000), (130, 16400)])
 def test_linear_workgroup_shapes(torch, isc, T, N, xtype):
     """Three and four tiles of outputs by two and three of columns."""
     note("linear workgroup shapes", T, N, xtype)
