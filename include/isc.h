@@ -558,8 +558,9 @@ int isc_w4_quantize(const isc_w4_desc *d, const void *w, int32_t type, int64_t l
  * form.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_w4_pack_codes(const isc_w4_desc *d, const uint8_t *codes, const uint8_t *scales, void *packed, void *stream);
 
-/* Bytes of workspace of isc_w4_linear (0 where x fills one matrix operand's 16
- * columns: 16 tokens, 8 in fp16, 5 in fp32; and with experts).  Host-only.
+/* Bytes of workspace of isc_w4_linear (0 with experts, and for no more tokens
+ * than fill one matrix operand's 16 columns, 8 in fp16 and 5 in fp32, unless rows
+ * are long).  Host-only.
  * Errors: NULL, SHAPE, LIMIT, ARG. */
 int isc_w4_linear_workspace_size(const isc_w4_desc *d, int32_t T, int32_t x_type, int32_t slots, size_t *bytes);
 

@@ -491,8 +491,19 @@ hipError_t run(const W4Args &a, int waves, hipStream_t s) {
 
 int parts_of(int xtype) { return xtype == ISC_F32 ? 3 : xtype == ISC_F16 ? 2 : 1; }
 
-// Whether x is laid out first: where its columns fill more than one tile.
-bool packs(int T, int xtype, int slots) { return slots == 0 && T > 16 / parts_of(xtype); }
+// Whether x is laid out first: where its columns fill more than one tile, and
+// where reading them as they stand, row by row and for every workgroup, takes
+// longer than the launch that lays them out: half a microsecond for a hundred
+// columns and steps together, less where a workgroup has several tiles of outputs
+// for them (us as they stand and laid out, bfloat16: 4096 outputs of 9216, 16
+// tokens 12.7 and 10.3, 8 tokens 9.5 and 10.3; 300 of 16384, 8 tokens 13.0 and 11.7,
+// 5 tokens 10.3 and 11.7; 5000 of 16384, 16 tokens 20.1 and 14.7, 8 tokens 14.8 and
+// 14.6; 8192 of 32768, 16 tokens 40.8 and 40.0, 8 tokens 34 and 40).
+bool packs(const W4Shape &w, int T, int xtype, int slots) {
+    if (slots) return false;
+    const int64_t columns = static_cast<int64_t>(T) * parts_of(xtype);
+    return T > 16 / parts_of(xtype) || (w.tiles() <= 512 && columns >= (w.tiles() > 256 ? 12 : 6) && columns * w.steps() >= 1024);
+}
 
 // Tiles of outputs a wavefront keeps (NT), wavefronts that share the inputs and
 // steps loaded ahead, by the workgroups there are to fill 256 compute units with;
@@ -577,6 +588,9 @@ hipError_t packed(const W4Args &a, hipStream_t s) {
     const int64_t tiles = (a.T + kTokens<MODE> - 1) / kTokens<MODE>;
     pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    // one tile of columns (long rows): two of outputs, as above (5000 outputs of
+    // 16384: 14.7 us against 18.1 with one)
+    if (tiles == 1 && a.w.tiles() > 256) return run<MODE, 2, 1, 1, 512>(a, 8, s);
     int best = 0;
     int64_t least = INT64_MAX;
     for (int i = 0; i < kShapeCount; ++i) {
@@ -590,7 +604,7 @@ hipError_t packed(const W4Args &a, hipStream_t s) {
 }  // namespace
 
 size_t w4_linear_column_bytes(const W4Shape &w, int T, int xtype, int slots) {
-    if (!packs(T, xtype, slots)) return 0;
+    if (!packs(w, T, xtype, slots)) return 0;
     const int tokens = 16 / parts_of(xtype);
     return static_cast<size_t>((T + tokens - 1) / tokens) * static_cast<size_t>(w.steps()) * 4096;
 }
@@ -598,7 +612,7 @@ size_t w4_linear_column_bytes(const W4Shape &w, int T, int xtype, int slots) {
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t s) {
     // a workgroup never spans more tokens than its tiles of columns hold, so one
     // tile is the limit of the rows as they stand
-    const bool pack = packs(a.T, a.xtype, a.slots);
+    const bool pack = packs(a.w, a.T, a.xtype, a.slots);
     switch (a.xtype) {
     case ISC_MX8: return pack ? packed<ISC_MX8>(a, s) : rows_as_they_stand<kMx8>(a, s);
     case ISC_BF16: return pack ? packed<ISC_BF16>(a, s) : rows_as_they_stand<kBf16>(a, s);

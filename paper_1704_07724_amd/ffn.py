@@ -23,7 +23,8 @@ import paper_1704_07724_amd as _isc
 F32, F16, BF16, MX8 = 0, 1, 2, 3
 SCORES = {"softmax": 0, "sigmoid": 1}
 LAYOUTS = {"tiles": 0, "rows": 1}
-# Tokens up to which isc_w4_linear has no workspace, by type.
+# Tokens that fill one matrix operand, by type: isc_w4_linear has a workspace for more, and
+# none for up to a third of them.
 COLUMNS = {F32: 5, F16: 8, BF16: 16, MX8: 16}
 
 
@@ -464,8 +465,9 @@ def isc_w4_linear(st, x, w4, route=None, relu=False, dtype=None, ws=None, stream
         order = _exact(order, st.i32, (T * slots,), "order")
     if dtype is None:
         dtype = st.torch.bfloat16 if code == MX8 else x.dtype
-    if ws is None and not slots and T > COLUMNS[code]:
-        ws = _bytes(st, _w4_size("isc_w4_linear_workspace_size", w4.E, N, K, LAYOUTS["tiles"], T, code, 0), x)
+    if ws is None and not slots and 3 * T > COLUMNS[code]:
+        n = _w4_size("isc_w4_linear_workspace_size", w4.E, N, K, LAYOUTS["tiles"], T, code, 0)
+        ws = _bytes(st, n, x) if n else None
     y = _new(st, x, dtype, T, slots, N) if slots else _new(st, x, dtype, *shape[:-1], N)
     status = st.lib.isc_w4_linear(
         w4.desc, w4.data.data_ptr(), T, xr.data_ptr(), code, ldx, sp, lds, slots, _ptr(ids), _ptr(offsets),

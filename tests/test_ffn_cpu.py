@@ -181,3 +181,14 @@ def test_binding_refusals():
         isc.isc_w4_linear(x, isc.W4(desc(E=2), torch.zeros(4), True))
     with pytest.raises(TypeError):
         isc.isc_w4_linear((x, x), w4)
+
+
+def test_linear_workspace_for_few_tokens():
+    """None for a third of an operand's tokens, whatever the matrix: the binding then asks for none."""
+    n = ctypes.c_size_t()
+    for xt, most in isc.ffn.COLUMNS.items():
+        for K in (1, 4096, 1 << 20):
+            for T in range(1, most // 3 + 1):
+                assert isc.lib().isc_w4_linear_workspace_size(desc(K=K), T, xt, 0, n) == 0 and n.value == 0
+        # and rows long enough have one before an operand is full
+        assert isc.lib().isc_w4_linear_workspace_size(desc(K=1 << 16), most, xt, 0, n) == 0 and n.value >= most << 17

@@ -524,7 +524,8 @@ def test_linear_workgroup_shapes(torch, isc, T, N, xtype):
 
 @pytest.mark.parametrize("xtype", TYPES + ["mx8"])
 @pytest.mark.parametrize("T,N,K", [(1, 5000, 4500), (5, 5000, 700), (3, 11000, 600), (5, 11000, 1500), (1, 15000, 600),
-                                   (5, 17000, 1500), (1, 33000, 600), (1, 2100, 6600), (16, 8200, 4300)])
+                                   (5, 17000, 1500), (1, 33000, 600), (1, 2100, 6600), (16, 8200, 4300),
+                                   (16, 100, 8100), (5, 300, 9001), (16, 4200, 8200), (8, 4200, 16400)])
 def test_linear_few_tokens(torch, isc, T, N, K, xtype):
     """One to four tiles of outputs a workgroup, four and eight wavefronts, rows shorter than those and longer."""
     note("linear few tokens", T, N, K, xtype)
