@@ -172,9 +172,6 @@ __device__ __forceinline__ float unorder(uint32_t o) {
 // --- group formats ----------------------------------------------------------
 // A scale is one byte b and stands for 2^(b - 127); 255 stands for NaN.
 
-__device__ __forceinline__ float scale_value(uint32_t b) {
-    return __uint_as_float(b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
-}
 // The scale byte of a group whose largest magnitude has the bits `abits`:
 // the smallest power of two that brings it to `top` or below, where
 // top = (1 + TOPM / 2^23) 2^TOPE.  255 where the magnitude is not finite.

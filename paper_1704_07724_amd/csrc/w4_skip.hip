@@ -3,51 +3,49 @@
 //
 // The convolution's step on a matrix: a wavefront tests 64 inputs or more by
 // ballots and lists the nonzeros in LDS, then reads one contiguous row of weights for
-// each, eight rows in flight, lanes running over outputs.  The bytes moved are
-// the nonzeros' rows and the scales of the groups of 32 inputs that hold one.
-// Products are summed per group in fp32 and then scaled, so a scale is applied
-// once a group and not once a weight.
+// each, five rows in flight, lanes running over outputs.  The bytes moved are the
+// nonzeros' rows and the scales of the groups of 32 inputs that hold one.  A weight
+// is widened under its own scale, so a row takes the same steps whether or not the
+// one before was of its group: 28 vector instructions for its eight outputs a lane
+// (57 where a group's sums were closed and scaled).  Sums are fp32, a slot's
+// weighted once.
 //
 // The inputs (of all a token's slots) are cut into ranges, a workgroup each;
 // its wavefronts take 64 TESTS inputs in turn.  Their sums meet in LDS in order, the
 // ranges' in a second launch, so a result does not depend on timing.
 //
-// A chain of waits bounds it (the inputs, the rows, the sums, the second launch):
-// 8192 outputs of 32768 inputs, a twentieth nonzero, one token, take 12.2 us for
-// 13.6 MB (10.3 us on the GPU alone, 8 of them this kernel's), and 8 tokens of 8
-// experts, 2048 outputs of 1408 with a tenth nonzero, 13.0 us for 13 MB.
+// With few tokens a chain of waits bounds it (the inputs, the rows, the sums, the
+// second launch): 8192 outputs of 32768 inputs, a twentieth nonzero, one token, take
+// 12.0 us for 13.6 MB (9.7 us on the GPU alone), and 8 tokens of 8 experts, 2048
+// outputs of 1408 with a tenth nonzero, 12.9 us for 13 MB.  With many the vector
+// instructions do: 16 tokens of the first 40.3 us.  Five rows in flight leave room
+// for eight wavefronts a unit; with eight rows it is 46.5 us, with three 40.0, and
+// with half of the inputs nonzero 222, 219 and 236 us for five, eight and three.
 #include "ffn.hpp"
 
 namespace isc {
 namespace {
 
-using f32x2 = float __attribute__((ext_vector_type(2)));
-
 constexpr int kWaves = 8;
 constexpr int kOutputs = 512;  // outputs of a workgroup: eight a lane
-constexpr int kFlight = 8;     // rows in flight
+constexpr int kFlight = 5;     // rows in flight
 
-__device__ __forceinline__ void add_row(float (&sum)[8], uint32_t w, float x) {
-    f32x2 v;
-    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
-    sum[0] = fmaf(v[0], x, sum[0]);
-    sum[1] = fmaf(v[1], x, sum[1]);
-    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-    sum[2] = fmaf(v[0], x, sum[2]);
-    sum[3] = fmaf(v[1], x, sum[3]);
-    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
-    sum[4] = fmaf(v[0], x, sum[4]);
-    sum[5] = fmaf(v[1], x, sum[5]);
-    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
-    sum[6] = fmaf(v[0], x, sum[6]);
-    sum[7] = fmaf(v[1], x, sum[7]);
+// Four outputs' products of one input: each weight widened under its own group's
+// scale, whose byte stands in the exponent of a word (the conversion reads nothing
+// else of it), then one multiply-add.  HALF: which four of the word of eight.
+template <int HALF>
+__device__ __forceinline__ void add_four(float *sum, uint32_t w, uint32_t scales, float x) {
+    sum[0] = fmaf(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, __uint_as_float(scales << 23), 2 * HALF)[0], x, sum[0]);
+    sum[1] = fmaf(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, __uint_as_float(scales << 15), 2 * HALF)[1], x, sum[1]);
+    sum[2] = fmaf(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, __uint_as_float(scales << 7), 2 * HALF + 1)[0], x, sum[2]);
+    sum[3] = fmaf(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, __uint_as_float(scales >> 1), 2 * HALF + 1)[1], x, sum[3]);
 }
 
-// A nonzero: its value and its place, the group's number times 32 and the
-// input within it.
+// A nonzero: its value and where its weights are, in half padded rows from the
+// turn's first group on: the codes in the low half, the group's scales in the high.
 struct Entry {
     float x;
-    int k;
+    uint32_t at;
 };
 
 template <int TESTS>
@@ -65,19 +63,29 @@ __global__ void __launch_bounds__(64 * kWaves) w4_skip_kernel(W4Args a, int rang
     const int per = (a.w.K + TESTS * 64 - 1) / (TESTS * 64);  // turns of a slot
     const int64_t turns = static_cast<int64_t>(per) * slots;
     // lanes past the matrix's last outputs read its last ones again, for nothing
-    const int64_t n0 = c0 + lane * 8 < np ? c0 + lane * 8 : np - 8;
+    const uint32_t n0 = static_cast<uint32_t>(c0 + lane * 8 < np ? c0 + lane * 8 : np - 8);
+    const uint32_t half = static_cast<uint32_t>(np / 2);
     Entry *list = lists[wave];
-    float acc[8] = {};
+    float acc[8] = {}, sum[8] = {};  // `sum`: of the slots under one weight
+    float factor = 1.0f;
+    int slot = -1;
+    const auto close = [&] {  // a slot's sums, weighted
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            acc[i] = fmaf(sum[i], factor, acc[i]);
+            sum[i] = 0.0f;
+        }
+    };
     for (int64_t turn = static_cast<int64_t>(range) * kWaves + wave; turn < turns;
          turn += static_cast<int64_t>(ranges) * kWaves) {
         const int j = static_cast<int>(turn / per), k0 = static_cast<int>(turn % per) * (TESTS * 64);
         const int64_t row = t * slots + j;
         const uint8_t *w = a.packed;
-        float factor = 1.0f;
+        float weight = 1.0f;
         if (a.slots) {
-            const int e = a.ids[row];
+            const int e = __builtin_amdgcn_readfirstlane(a.ids[row]);
             if (e < 0 || e >= a.w.E) continue;
-            factor = a.weights[row];
+            weight = a.weights[row];
             w += static_cast<int64_t>(e) * a.w.row_bytes();
         }
         float x[TESTS];
@@ -91,52 +99,48 @@ __global__ void __launch_bounds__(64 * kWaves) w4_skip_kernel(W4Args a, int rang
         for (int i = 0; i < TESTS; ++i) {
             const unsigned long long nz = __ballot(x[i] != 0.0f);
             const int before = __popcll(nz & ((1ull << lane) - 1));
-            if (x[i] != 0.0f) list[count + before] = Entry{x[i], k0 + i * 64 + lane};
+            const uint32_t group = static_cast<uint32_t>(i * 2 + (lane >> 5)) * 34u;  // 32 inputs and their scales
+            if (x[i] != 0.0f) list[count + before] = Entry{x[i], group << 16 | (group + 2u + (lane & 31))};
             count += __popcll(nz);
         }
         if (count == 0) continue;
-        // the last batch is filled up with its last row times 0
+        if (j != slot) {
+            if (slot >= 0) close();
+            slot = j;
+            factor = weight;
+        }
+        // the last batch is filled up with zeros, whose weights are set to 0 too
+        if (lane < kFlight) list[count + lane] = Entry{0.0f, 0u};
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        int group = -1;
-        float sum[8] = {};
-        uint2 scale = make_uint2(0u, 0u);
-        const auto close = [&] {  // a group's sums, scaled
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                acc[i] = fmaf(sum[i] * factor, scale_value(((i < 4 ? scale.x : scale.y) >> (8 * (i & 3))) & 255u), acc[i]);
-        };
+        const uint8_t *from = w + static_cast<int64_t>(k0 >> 5) * 17 * np;
         for (int base = 0; base < count; base += kFlight) {
             float xv[kFlight];
-            int kv[kFlight];
             uint32_t q[kFlight];
             uint2 sc[kFlight];
-            const Entry mine = list[base + lane < count ? base + lane : count - 1];
 #pragma unroll
             for (int i = 0; i < kFlight; ++i) {
-                kv[i] = __builtin_amdgcn_readlane(mine.k, i);
-                xv[i] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.x), i));
-                const uint8_t *g = w + static_cast<int64_t>(kv[i] >> 5) * 17 * np;
-                sc[i] = *reinterpret_cast<const uint2 *>(g + n0);
-                q[i] = *reinterpret_cast<const uint32_t *>(g + np + (kv[i] & 31) * (np / 2) + n0 / 2);
+                const Entry e = list[base + i];
+                xv[i] = e.x;
+                q[i] = *reinterpret_cast<const uint32_t *>(from + (__umul24(e.at & 0xffffu, half) + n0 / 2));
+                sc[i] = *reinterpret_cast<const uint2 *>(from + (__umul24(e.at >> 16, half) + n0));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (base + kFlight > count) {
+#pragma unroll
+                for (int i = 1; i < kFlight; ++i)
+                    if (base + i >= count) q[i] = 0u, sc[i] = make_uint2(0u, 0u);
             }
 #pragma unroll
             for (int i = 0; i < kFlight; ++i) {
-                if (base + i >= count) break;
-                if (kv[i] >> 5 != group) {
-                    if (group >= 0) close();
-                    group = kv[i] >> 5;
-                    scale = sc[i];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
-                }
-                add_row(sum, q[i], xv[i]);
+                add_four<0>(sum, q[i], sc[i].x, xv[i]);
+                add_four<1>(sum + 4, q[i], sc[i].y, xv[i]);
             }
         }
-        close();
         __builtin_amdgcn_wave_barrier();  // the list is read before the next turn writes it
     }
+    close();
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[wave][lane * 8 + i] = acc[i];
     __syncthreads();

@@ -555,6 +555,33 @@ def test_experts_long_rows(torch, isc, T, xtype):
     close(host(y), want, (K + 64) * E24 * size, "float32", "y")
 
 
+@pytest.mark.parametrize("T,K,N", [(1, 70, 40), (3, 900, 600), (16, 5000, 520)])
+def test_skip_scales(torch, isc, T, K, N):
+    """Scales from 2^-127 to 2^124 and NaN ones, counts of nonzeros that end a batch early: nothing leaks from
+    one group to the next, from a batch's last row to the entries behind it, or from what a 0 would meet."""
+    note("skip scales", T, K, N)
+    r = np.random.default_rng(K)
+    codes = r.integers(0, 256, (N, (K + 1) // 2), dtype=np.uint8)
+    scales = r.integers(0, 252, (N, (K + 31) // 32), dtype=np.uint8)
+    x = r.standard_normal((T, K)) * (r.random((T, K)) < 0.07)
+    w = ffn.fp4_values(codes, scales, K)
+    pack = lambda s: isc.isc_w4_pack_codes(torch.from_numpy(codes).cuda(), torch.from_numpy(s).cuda(), "rows", K=K)  # noqa: E731
+    xd = dev(torch, x)
+    x = host(xd)
+    # a term's own rounding is absolute below fp32's smallest normal number
+    with np.errstate(over="ignore"):
+        size = np.abs(x) @ np.abs(w).T
+        got, want = host(isc.isc_w4_skip(xd, pack(scales), dtype=torch.float32)), x @ w.T
+    fits = size < 1e38
+    assert fits.any()
+    assert (np.abs(got - want)[fits] <= ((K + 64) * E24 * size + K * 2.0 ** -149)[fits]).all()
+    # an output's NaN group is met by a token with a nonzero there, and by no other
+    scales[:, 0] = np.where(np.arange(N) % 3 == 0, 255, 127)
+    scales[:, 1:] = 127
+    meets = (x[:, :32] != 0).any(1)[:, None] & (np.arange(N) % 3 == 0)[None]
+    assert np.array_equal(np.isnan(host(isc.isc_w4_skip(xd, pack(scales), dtype=torch.float32))), meets)
+
+
 # the same for the skipping product: one, two and four tests a turn, one range and many
 @pytest.mark.parametrize("T,N,K", [(1, 40, 9000), (1, 8200, 33000), (3, 2000, 20000), (12, 4200, 5000), (40, 600, 3000),
                                    (700, 40, 700)])
