@@ -359,9 +359,11 @@ int norm_bwd_blocks(int T, int D) {
     // launch to read (8192 bfloat16 rows, us with 1, 2, 4, 8 workgroups a compute
     // unit: of 1024 52.6 31.0 22.4 21.9, of 2048 78.7 46.7 33.2 37.8, of 4096 89.1
     // 59.8 62.6 71.0, of 8192 116 118 126 142); two turns each at least, the second's
-    // loads ahead.
+    // loads ahead, from 256 turns on (rows of 4096: 330 of them 9.7 and 10.6 with one
+    // each, 200 of them 8.2 and 8.1), from 512 of short rows' (2400 rows of 500: 11.2
+    // and 10.2).
     const int most = 256 * (threads > 512 ? 1 : threads > 256 || threads == 64 ? 2 : threads > 128 ? 4 : 8);
-    const int some = turns < 512 ? turns : (turns + 1) / 2;
+    const int some = turns < (threads == 64 ? 512 : 256) ? turns : (turns + 1) / 2;
     return some < 1 ? 1 : some < most ? some : most;
 }
 
