@@ -202,6 +202,51 @@ def test_norm_in_place(torch, isc):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [9, 10, 11, 12, 13, 14, 15, 17, 257, 511, 513, 1001, 2046, 4099, 8191, 8195])
+def test_norm_uneven_widths(torch, isc, D, dtype):
+    """Rows that end inside eight values, between NaNs: nothing of the row before, the row after or the
+    values moved aside comes in, in both directions and in place."""
+    note("norm uneven widths", D, dtype)
+    r = np.random.default_rng(D)
+    T = 5
+
+    def held(scale):
+        t = torch.full((T, D + 11), float("nan"), dtype=getattr(torch, dtype), device="cuda")
+        t[:, 5:D + 5] = dev(torch, r.standard_normal((T, D)) * scale, dtype)
+        return t[:, 5:D + 5]
+    x, res, dy, dh = held(1), held(3), held(1), held(1)
+    w = dev(torch, 1 + 0.2 * r.standard_normal(D), dtype)
+    n = isc.isc_rmsnorm(x, w, eps=1e-5, residual=res, mx8=True, rstd=True)
+    h, rstd, y = ffn.rmsnorm(host(x), host(w), 1e-5, host(res))
+    close(host(n.h), h, E24 * np.abs(h), dtype, "h")
+    close(host(n.rstd), rstd, 128 * E24 * rstd, "float32", "rstd")
+    close(host(n.y), y, 128 * E24 * np.abs(y), dtype, "y")
+    check_mx8(host(n.mx8.q), host(n.mx8.scales), y, 128 * E24 * np.abs(y))
+    plain = [t.contiguous() for t in (x, res, dy, dh)]
+    same = isc.isc_rmsnorm(plain[0], w, eps=1e-5, residual=plain[1], rstd=True)
+    assert torch.equal(same.h, n.h) and torch.equal(same.y, n.y) and torch.equal(same.rstd, n.rstd)
+    dx, dw = isc.isc_rmsnorm_bwd(dy, n.h, w, n.rstd, dh=dh)
+    g, n1 = host(dy) * host(w), host(n.h) * host(n.rstd)[:, None]
+    want = host(n.rstd)[:, None] * (g - n1 * (g * n1).mean(1, keepdims=True)) + host(dh)
+    size = host(n.rstd)[:, None] * (np.abs(g) + np.abs(n1) * np.abs(g * n1).mean(1, keepdims=True)) + np.abs(host(dh))
+    close(host(dx), want, 128 * E24 * size, dtype, "dx")
+    close(host(dw), (host(dy) * n1).sum(0), 64 * E24 * np.abs(host(dy) * n1).sum(0), "float32", "dw")
+    # dx over dy, h over x
+    code = {"float32": 0, "float16": 1, "bfloat16": 2}[dtype]
+    n_ws = ctypes.c_size_t()
+    assert isc.lib().isc_rmsnorm_bwd_workspace_size(T, D, n_ws) == 0
+    ws, dw2 = torch.empty(n_ws.value, dtype=torch.uint8, device="cuda"), torch.empty(D, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    assert isc.lib().isc_rmsnorm_bwd(T, D, code, plain[2].data_ptr(), D, n.h.data_ptr(), D, w.data_ptr(), code,
+                                     n.rstd.data_ptr(), plain[3].data_ptr(), D, plain[2].data_ptr(), D, dw2.data_ptr(),
+                                     ws.data_ptr(), n_ws.value, stream) == 0
+    assert torch.equal(plain[2], dx) and torch.equal(dw2, dw)
+    assert isc.lib().isc_rmsnorm(T, D, code, plain[0].data_ptr(), D, plain[1].data_ptr(), D, w.data_ptr(), code, 1e-5,
+                                 plain[0].data_ptr(), D, None, D, None, D, None, (D + 31) // 32, None, stream) == 0
+    assert torch.equal(plain[0], n.h)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,D", [(1, 1), (2, 7), (3, 33), (65, 64), (700, 100), (5, 1000), (1, 4096), (9, 8200), (2, 16384),
                                  (2100, 520)])
 def test_norm_bwd(torch, isc, T, D, dtype):
