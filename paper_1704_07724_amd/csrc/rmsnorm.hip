@@ -7,7 +7,7 @@
 // outputs (the 8-bit form's unit) in four neighbouring lanes.  Sums are fp32; h
 // is normalised as it was added, before its rounding to x's type.  Memory bounds
 // it: 8192 rows of 8192 in bfloat16 with residual and 8-bit output move 472 MB in
-// 86 us, 5.5 TB/s; one row of 4096 takes 3.2 us on the GPU, all of it waits.  Rows
+// 85 us, 5.5 TB/s; one row of 4096 takes 3.0 us on the GPU, all of it waits.  Rows
 // of one wavefront have a workgroup each too: four or eight of them in one were no
 // faster (16384 rows of 512 12.2 us against 12.9 and 13.2).
 //
@@ -15,7 +15,7 @@
 //   dx = rstd (g - n mean(g n)) + dh,   dw = sum over rows of dy n
 // A workgroup walks rows and keeps its columns' sums of dy n in registers;
 // the workgroups' sums are added in order by a second launch.  8192 rows of 4096
-// in bfloat16 move 268 MB in 59 us, 4.6 TB/s; 777 rows of 1155 in fp32 take 9.7 us,
+// in bfloat16 move 268 MB in 50 us, 5.4 TB/s; 777 rows of 1155 in fp32 take 9.7 us,
 // two launches and a few rows one after another.
 #include "ffn.hpp"
 
@@ -61,48 +61,106 @@ __device__ __forceinline__ int at(int c) {
                  : (c * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8;
 }
 
-// Chunk c of a row of D values, 0 where there are none.  RAGGED, for 16-bit types
-// and a D over 8 that is no multiple of it: the row's last values come with one wide
-// load of the eight before its end and are moved to their places without a branch,
-// so that their wavefront has all tensors' loads in flight together like the others
-// (3000 bfloat16 rows of 3351: norm 16.8 us, value by value 24.9; gradient 24.1 and
-// 44.0).  Not where a thread holds several chunks (3000 rows of 8195: 56.7 and 55.2,
-// gradient 70.1 and 71.1), nor for fp32, whose values do not wait to be widened one
-// by one (3548 rows of 3351: 38.3 and 37.1, gradient 47.9 and 39.6).
-template <class T, bool SHORT = false, bool RAGGED = false>
-__device__ __forceinline__ void load_chunk(float (&v)[8], const typename T::type *row, int c, int D) {
-    if constexpr (!RAGGED || sizeof(typename T::type) == 4) {  // (a weight may be fp32)
-        load8<T>(v, row + at<SHORT>(c), D - at<SHORT>(c));
-    } else {
-        const int here = at<SHORT>(c), from = here < D - 8 ? here : D - 8, by = here - from;
-        const uint4 a = load_any<uint4>(row + from);
-        uint32_t w0 = a.x, w1 = a.y, w2 = a.z, w3 = a.w;
-        if (by & 4) w0 = w2, w1 = w3, w2 = 0u, w3 = 0u;
-        if (by & 2) w0 = w1, w1 = w2, w2 = w3, w3 = 0u;
-        const uint32_t half = by & 1 ? 16 : 0, all = by < 8 ? 0xffffffffu : 0u;
-        const uint32_t w[4] = {__builtin_amdgcn_alignbit(w1, w0, half) & all, __builtin_amdgcn_alignbit(w2, w1, half) & all,
-                               __builtin_amdgcn_alignbit(w3, w2, half) & all, __builtin_amdgcn_alignbit(0u, w3, half) & all};
+// How a thread's eight values of a row are read.  kEven, for widths that are a
+// multiple of 8, and kMoved, for other widths over 8 of 16-bit types: one wide load
+// without a branch, from the eight values before the row's end where the thread's own
+// would pass it, and what is the thread's taken out of it when the values are used.
+// So the loads of all tensors, and of the row after, are in flight together: behind a
+// branch each waits to be widened before the next is sent.  kAny: value by value at
+// the row's end.
+// (8192 bfloat16 rows of 4096, gradient: 50.4 us, each load behind its branch 59.4;
+// 3000 rows of 3351: norm 16.4, value by value 24.9, gradient 22.7 and 44.0.)  Not
+// for rows of several chunks that end inside eight (3000 rows of 8195: norm 56.7 and
+// 55.2), nor the gradient of fp32, whose values need no widening to wait for.
+enum Reading { kAny, kEven, kMoved };
+
+using Words = uint32_t[8];  // eight values as loaded; 16-bit ones take half of them
+
+template <class T, Reading READ, bool SHORT = false>
+struct Chunk {
+    static constexpr bool kWide = sizeof(typename T::type) == 4;
+    static constexpr Reading kRead = kWide && READ == kMoved ? kAny : READ;  // (a weight beside 16-bit values)
+
+    // Chunk c of a row of D values.
+    static __device__ __forceinline__ void load(Words &w, const typename T::type *row, int c, int D) {
+        if constexpr (kRead == kAny) {
+            float v[8];
+            load8<T>(v, row + at<SHORT>(c), D - at<SHORT>(c));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = T::widen(w[i] & 0xffffu);
-            v[2 * i + 1] = T::widen(w[i] >> 16);
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
+        } else {
+            const int here = at<SHORT>(c);
+            const typename T::type *p = row + (here < D - 8 ? here : D - 8);
+            const uint4 a = load_any<uint4>(p);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+            if constexpr (kWide) {
+                const uint4 b = load_any<uint4>(p + 4);
+                w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+            }
         }
     }
+
+    // Its values, 0 past the row's end.
+    static __device__ __forceinline__ void get(float (&v)[8], const Words &w, int c, int D) {
+        if constexpr (kRead == kAny) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        } else if constexpr (kWide) {
+            const bool there = at<SHORT>(c) < D;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = there ? __uint_as_float(w[i]) : 0.0f;
+        } else {
+            const int here = at<SHORT>(c), by = here < D - 8 ? 0 : here - (D - 8);
+            const uint32_t all = by < 8 ? 0xffffffffu : 0u;
+            uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
+            if constexpr (kRead == kMoved) {
+                if (by & 4) w0 = w2, w1 = w3, w2 = 0u, w3 = 0u;
+                if (by & 2) w0 = w1, w1 = w2, w2 = w3, w3 = 0u;
+                const uint32_t half = by & 1 ? 16 : 0;
+                w0 = __builtin_amdgcn_alignbit(w1, w0, half);
+                w1 = __builtin_amdgcn_alignbit(w2, w1, half);
+                w2 = __builtin_amdgcn_alignbit(w3, w2, half);
+                w3 = __builtin_amdgcn_alignbit(0u, w3, half);
+            }
+            const uint32_t u[4] = {w0 & all, w1 & all, w2 & all, w3 & all};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = T::widen(u[i] & 0xffffu);
+                v[2 * i + 1] = T::widen(u[i] >> 16);
+            }
+        }
+    }
+};
+
+// The same of the weight, whose type is known at run time.
+template <Reading READ, bool SHORT = false>
+struct WeightChunk {
+    static __device__ __forceinline__ void load(Words &w, const void *p, int c, int D, int type) {
+        if (type == ISC_F32)
+            Chunk<F32, READ, SHORT>::load(w, static_cast<const float *>(p), c, D);
+        else if (READ != kAny || type == ISC_BF16)  // (fp16 as well, unless it is widened at once)
+            Chunk<BF16, READ, SHORT>::load(w, static_cast<const uint16_t *>(p), c, D);
+        else
+            Chunk<F16, READ, SHORT>::load(w, static_cast<const uint16_t *>(p), c, D);
+    }
+    static __device__ __forceinline__ void get(float (&v)[8], const Words &w, int c, int D, int type) {
+        if (type == ISC_F32)
+            Chunk<F32, READ, SHORT>::get(v, w, c, D);
+        else if (type == ISC_BF16)
+            Chunk<BF16, READ, SHORT>::get(v, w, c, D);
+        else
+            Chunk<F16, READ, SHORT>::get(v, w, c, D);
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void load_chunk(float (&v)[8], const typename T::type *row, int c, int D) {
+    load8<T>(v, row + at(c), D - at(c));
 }
 template <class T, bool SHORT = false>
 __device__ __forceinline__ void store_chunk(typename T::type *row, const float (&v)[8], int c, int D) {
     store8<T>(row + at<SHORT>(c), v, D - at<SHORT>(c));
 }
-template <bool SHORT = false, bool RAGGED = false>
-__device__ __forceinline__ void load_weight(float (&w)[8], const void *p, int c, int D, int type) {
-    if (type == ISC_F32)
-        load_chunk<F32, SHORT, RAGGED>(w, static_cast<const float *>(p), c, D);
-    else if (type == ISC_BF16)
-        load_chunk<BF16, SHORT, RAGGED>(w, static_cast<const uint16_t *>(p), c, D);
-    else
-        load_chunk<F16, SHORT, RAGGED>(w, static_cast<const uint16_t *>(p), c, D);
-}
-
 // The 8-bit form of a chunk of outputs.  A group's largest magnitude is taken
 // as bits, under which NaN comes out above everything.
 __device__ __forceinline__ void store_mx8(uint8_t *q, uint8_t *scales, const float (&v)[8], int c, int D) {
@@ -131,28 +189,35 @@ __device__ __forceinline__ void store_mx8(uint8_t *q, uint8_t *scales, const flo
     if ((threadIdx.x & 3) == 0 && at(c) < D) scales[at(c) / 32] = static_cast<uint8_t>(b);
 }
 
-template <class T, int C, bool RAGGED>
+template <class T, int C, Reading READ>
 __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
     using E = typename T::type;
     __shared__ float sums[16];
     const int64_t t = blockIdx.x;
     float v[C][8], w[C][8];
     float ss = 0.0f;
+    using In = Chunk<T, READ>;
+    using Weight = WeightChunk<READ>;
+    Words x[C], r[C], weight[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) load_chunk<T, false, RAGGED>(v[c], static_cast<const E *>(a.x) + t * a.ldx, c, a.D);
-    if (a.r) {
-        float u[C][8];
+    for (int c = 0; c < C; ++c) In::load(x[c], static_cast<const E *>(a.x) + t * a.ldx, c, a.D);
+    if (a.r)
 #pragma unroll
-        for (int c = 0; c < C; ++c) load_chunk<T, false, RAGGED>(u[c], static_cast<const E *>(a.r) + t * a.ldr, c, a.D);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] += u[c][j];
-    }
+        for (int c = 0; c < C; ++c) In::load(r[c], static_cast<const E *>(a.r) + t * a.ldr, c, a.D);
     // short rows: the weight on its way while the sum is taken
     if (C <= 2)
 #pragma unroll
-        for (int c = 0; c < C; ++c) load_weight<false, RAGGED>(w[c], a.w, c, a.D, a.wtype);
+        for (int c = 0; c < C; ++c) Weight::load(weight[c], a.w, c, a.D, a.wtype);
+#pragma unroll
+    for (int c = 0; c < C; ++c) In::get(v[c], x[c], c, a.D);
+    if (a.r)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float u[8];
+            In::get(u, r[c], c, a.D);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[c][j] += u[j];
+        }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -166,7 +231,8 @@ __global__ void __launch_bounds__(1024) rmsnorm_kernel(NormArgs a) {
     if (!a.y && !a.q) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        if (C > 2) load_weight<false, RAGGED>(w[c], a.w, c, a.D, a.wtype);
+        if (C > 2) Weight::load(weight[c], a.w, c, a.D, a.wtype);
+        Weight::get(w[c], weight[c], c, a.D, a.wtype);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[c][j] = at(c) + j < a.D ? v[c][j] * rstd * w[c][j] : 0.0f;
         if (a.y) store_chunk<T>(static_cast<E *>(a.y) + t * a.ldy, v[c], c, a.D);
@@ -205,7 +271,9 @@ __global__ void __launch_bounds__(1024) rmsnorm_long_kernel(NormArgs a, int chun
     for (int c = 0; c < chunks; ++c) {
         float v[8], w[8];
         load(v, c);
-        load_weight(w, a.w, c, a.D, a.wtype);
+        Words weight;
+        WeightChunk<kAny>::load(weight, a.w, c, a.D, a.wtype);
+        WeightChunk<kAny>::get(w, weight, c, a.D, a.wtype);
         if (a.h) store_chunk<T>(static_cast<E *>(a.h) + t * a.ldh, v, c, a.D);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = at(c) + j < a.D ? v[j] * rstd * w[j] : 0.0f;
@@ -218,7 +286,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_long_kernel(NormArgs a, int chun
 // SHORT: rows of one wavefront, as many at once as the workgroup has wavefronts;
 // else one row at a time.  A row is on its way while the one before is worked on,
 // where the registers hold both (C of 1).
-template <class T, int C, bool SHORT, bool RAGGED>
+template <class T, int C, bool SHORT, Reading READ>
 __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
     using E = typename T::type;
     __shared__ float sums[2][16];
@@ -228,36 +296,53 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
     float w[C][8], acc[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        load_weight<SHORT, RAGGED>(w[c], a.w, c, a.D, a.wtype);
+        Words weight;
+        WeightChunk<READ, SHORT>::load(weight, a.w, c, a.D, a.wtype);
+        WeightChunk<READ, SHORT>::get(w[c], weight, c, a.D, a.wtype);
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[c][j] = 0.0f;
     }
-    // a row of h, dy and dh, as loaded
-    const auto load = [&](int64_t t, float(&n)[C][8], float(&g)[C][8], float(&d)[C][8], float &rstd) {
-        if (t >= a.T) return;
-        rstd = a.rstd[t];
+    // chunk c of a row of h, dy and dh: as loaded, and their values
+    using In = Chunk<T, READ, SHORT>;
+    const auto load = [&](int64_t t, int c, Words &h, Words &dy, Words &dh) {
+        In::load(h, static_cast<const E *>(a.h) + t * a.ldh, c, a.D);
+        In::load(dy, static_cast<const E *>(a.dy) + t * a.ldy, c, a.D);
+        if (a.dh)
+            In::load(dh, static_cast<const E *>(a.dh) + t * a.ldd, c, a.D);
+        else if (READ == kAny)
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            load_chunk<T, SHORT, RAGGED>(n[c], static_cast<const E *>(a.h) + t * a.ldh, c, a.D);
-            load_chunk<T, SHORT, RAGGED>(g[c], static_cast<const E *>(a.dy) + t * a.ldy, c, a.D);
-            if (a.dh)
-                load_chunk<T, SHORT, RAGGED>(d[c], static_cast<const E *>(a.dh) + t * a.ldd, c, a.D);
-            else
+            for (int i = 0; i < 8; ++i) dh[i] = 0u;
+    };
+    const auto get = [&](int c, const Words &h, const Words &dy, const Words &dh, float(&n)[8], float(&g)[8], float(&d)[8]) {
+        In::get(n, h, c, a.D);
+        In::get(g, dy, c, a.D);
+        if (READ == kAny || a.dh)  // (the one set 0 where there is none, the other not even loaded)
+            In::get(d, dh, c, a.D);
+        else
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[c][j] = 0.0f;
-        }
+            for (int j = 0; j < 8; ++j) d[j] = 0.0f;
     };
     const int64_t t0 = SHORT ? static_cast<int64_t>(blockIdx.x) * kShortRows + wave : blockIdx.x;
-    float nn[C][8], ng[C][8], nd[C][8], nr = 0.0f;  // the next row
-    if constexpr (C == 1) load(t0, nn, ng, nd, nr);
+    constexpr bool kAhead = C == 1;  // the next row is on its way
+    Words next_h, next_dy, next_dh;
+    float next_rstd = 0.0f;
+    if (kAhead && t0 < a.T) {
+        next_rstd = a.rstd[t0];
+        load(t0, 0, next_h, next_dy, next_dh);
+    }
     int turn = 0;
     for (int64_t t = t0; t < a.T; t += step, turn ^= 1) {
-        float n[C][8], g[C][8], d[C][8], rstd = nr;
-        if constexpr (C == 1) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) n[0][j] = nn[0][j], g[0][j] = ng[0][j], d[0][j] = nd[0][j];
+        float n[C][8], g[C][8], d[C][8];
+        const float rstd = kAhead ? next_rstd : a.rstd[t];
+        if constexpr (kAhead) {
+            get(0, next_h, next_dy, next_dh, n[0], g[0], d[0]);
         } else {
-            load(t, n, g, d, rstd);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                Words h, dy, dh;
+                load(t, c, h, dy, dh);
+                get(c, h, dy, dh, n[c], g[c], d[c]);
+            }
         }
         float dot = 0.0f;
 #pragma unroll
@@ -271,7 +356,10 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
             }
         // (dx may be one of the tensors that are read: row t is in registers now, and
         // row t + step is no other row's output)
-        if constexpr (C == 1) load(t + step, nn, ng, nd, nr);
+        if (kAhead && t + step < a.T) {
+            next_rstd = a.rstd[t + step];
+            load(t + step, 0, next_h, next_dy, next_dh);
+        }
         // two sets of sums in turn: a row's are read before the row after the
         // next overwrites them, with the barrier of the row between
         const float mean = (SHORT ? wave_sum(dot) : block_sum(dot, sums[turn])) / static_cast<float>(a.D);
@@ -338,10 +426,38 @@ RowPlan row_plan(int D, int most) {
     return {threads, chunks};
 }
 
-// Whether a row's last values are moved to their places (load_chunk).
 template <class T>
-bool ragged(int D) {
-    return sizeof(typename T::type) == 2 && D % 8 != 0 && D > 8;
+constexpr bool kHalf = sizeof(typename T::type) == 2;
+
+template <class T, int C>
+void norm_with(const NormArgs &a, dim3 grid, dim3 block, hipStream_t s) {
+    if (a.D % 8 == 0) {
+        rmsnorm_kernel<T, C, kEven><<<grid, block, 0, s>>>(a);
+        return;
+    }
+    if constexpr (kHalf<T> && C == 1)
+        if (a.D > 8) {
+            rmsnorm_kernel<T, C, kMoved><<<grid, block, 0, s>>>(a);
+            return;
+        }
+    rmsnorm_kernel<T, C, kAny><<<grid, block, 0, s>>>(a);
+}
+
+// (fp32 by kAny alone: 3000 rows of 2048 take 22.2 us, by kEven 23.9)
+template <class T, int C, bool SHORT>
+void norm_bwd_with(const NormBwdArgs &a, dim3 grid, dim3 block, hipStream_t s) {
+    if constexpr (kHalf<T>) {
+        if (a.D % 8 == 0) {
+            rmsnorm_bwd_kernel<T, C, SHORT, kEven><<<grid, block, 0, s>>>(a);
+            return;
+        }
+        if constexpr (C == 1)
+            if (a.D > 8) {
+                rmsnorm_bwd_kernel<T, C, SHORT, kMoved><<<grid, block, 0, s>>>(a);
+                return;
+            }
+    }
+    rmsnorm_bwd_kernel<T, C, SHORT, kAny><<<grid, block, 0, s>>>(a);
 }
 
 template <class T>
@@ -349,14 +465,9 @@ hipError_t norm_of(const NormArgs &a, hipStream_t s) {
     const RowPlan p = row_plan(a.D, 1024);
     const dim3 grid(static_cast<unsigned>(a.T)), block(static_cast<unsigned>(p.threads));
     switch (p.chunks) {
-    case 1:
-        if (ragged<T>(a.D))
-            rmsnorm_kernel<T, 1, true><<<grid, block, 0, s>>>(a);
-        else
-            rmsnorm_kernel<T, 1, false><<<grid, block, 0, s>>>(a);
-        break;
-    case 2: rmsnorm_kernel<T, 2, false><<<grid, block, 0, s>>>(a); break;
-    case 4: rmsnorm_kernel<T, 4, false><<<grid, block, 0, s>>>(a); break;
+    case 1: norm_with<T, 1>(a, grid, block, s); break;
+    case 2: norm_with<T, 2>(a, grid, block, s); break;
+    case 4: norm_with<T, 4>(a, grid, block, s); break;
     default: rmsnorm_long_kernel<T><<<grid, block, 0, s>>>(a, p.chunks); break;
     }
     return hipGetLastError();
@@ -368,17 +479,12 @@ hipError_t norm_bwd_of(const NormBwdArgs &a, hipStream_t s) {
     const bool brief = p.threads == 64;
     const int blocks = norm_bwd_blocks(a.T, a.D);
     const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(brief ? 64 * kShortRows : p.threads));
-    const bool uneven = ragged<T>(a.D);
-    if (brief && uneven)
-        rmsnorm_bwd_kernel<T, 1, true, true><<<grid, block, 0, s>>>(a);
-    else if (brief)
-        rmsnorm_bwd_kernel<T, 1, true, false><<<grid, block, 0, s>>>(a);
-    else if (p.chunks == 1 && uneven)
-        rmsnorm_bwd_kernel<T, 1, false, true><<<grid, block, 0, s>>>(a);
+    if (brief)
+        norm_bwd_with<T, 1, true>(a, grid, block, s);
     else if (p.chunks == 1)
-        rmsnorm_bwd_kernel<T, 1, false, false><<<grid, block, 0, s>>>(a);
+        norm_bwd_with<T, 1, false>(a, grid, block, s);
     else
-        rmsnorm_bwd_kernel<T, 2, false, false><<<grid, block, 0, s>>>(a);
+        norm_bwd_with<T, 2, false>(a, grid, block, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     column_sum_kernel<<<dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(1024), 0, s>>>(a.part, blocks, a.D, a.dw);
@@ -396,12 +502,13 @@ int norm_bwd_blocks(int T, int D) {
     const int turns = threads == 64 ? (T + kShortRows - 1) / kShortRows : T;
     // Short rows want more workgroups at once, long ones fewer sums for the second
     // launch to read (8192 bfloat16 rows, us with 1, 2, 4, 8 workgroups a compute
-    // unit: of 1024 52.6 31.0 22.4 21.9, of 2048 78.7 46.7 33.2 37.8, of 4096 89.1
-    // 59.8 62.6 71.0, of 8192 116 118 126 142); two turns each at least, the second's
-    // loads ahead, from 256 turns on (rows of 4096: 330 of them 9.7 and 10.6 with one
-    // each, 200 of them 8.2 and 8.1), from 512 of short rows' (2400 rows of 500: 11.2
-    // and 10.2).
-    const int most = 256 * (threads > 512 ? 1 : threads > 256 || threads == 64 ? 2 : threads > 128 ? 4 : 8);
+    // unit: of 1024 37.6 24.0 20.0 21.6, of 2048 50.1 33.9 31.8 35.6, of 4096 58.7
+    // 50.8 55.3 62.3, of 8192 103 107 116 132, and of 512, eight at once, 10.7 11.4
+    // 11.4 11.4; 1024 rows of 4096 13.6 15.4 15.5 15.5); two turns each at least, the
+    // second's loads ahead, from 256 turns on (rows of 4096: 330 of them 9.7 and 10.6
+    // with one each, 200 of them 8.2 and 8.1), from 512 of short rows' (2400 rows of
+    // 500: 11.2 and 10.2).
+    const int most = 256 * (threads == 64 || threads > 512 || (threads > 256 && turns < 2048) ? 1 : threads > 256 ? 2 : 4);
     const int some = turns < (threads == 64 ? 512 : 256) ? turns : (turns + 1) / 2;
     return some < 1 ? 1 : some < most ? some : most;
 }
