@@ -80,6 +80,17 @@ __global__ void __launch_bounds__(64 * kWaves) w4_skip_kernel(W4Args a, int rang
          turn += static_cast<int64_t>(ranges) * kWaves) {
         const int j = static_cast<int>(turn / per), k0 = static_cast<int>(turn % per) * (TESTS * 64);
         const int64_t row = t * slots + j;
+        // all tests' inputs on their way before anything waits
+        uint32_t raw[TESTS];
+        if (a.xtype == ISC_F32) {
+            const uint32_t *p = static_cast<const uint32_t *>(a.x) + row * a.ldx;
+#pragma unroll
+            for (int i = 0; i < TESTS; ++i) raw[i] = p[k0 + i * 64 + lane < a.w.K ? k0 + i * 64 + lane : a.w.K - 1];
+        } else {
+            const uint16_t *p = static_cast<const uint16_t *>(a.x) + row * a.ldx;
+#pragma unroll
+            for (int i = 0; i < TESTS; ++i) raw[i] = p[k0 + i * 64 + lane < a.w.K ? k0 + i * 64 + lane : a.w.K - 1];
+        }
         const uint8_t *w = a.packed;
         float weight = 1.0f;
         if (a.slots) {
@@ -91,8 +102,8 @@ __global__ void __launch_bounds__(64 * kWaves) w4_skip_kernel(W4Args a, int rang
         float x[TESTS];
 #pragma unroll
         for (int i = 0; i < TESTS; ++i) {
-            const int k = k0 + i * 64 + lane;
-            x[i] = k < a.w.K ? load_as(a.x, row * a.ldx + k, a.xtype) : 0.0f;
+            x[i] = a.xtype == ISC_F16 ? F16::widen(raw[i]) : __uint_as_float(a.xtype == ISC_BF16 ? raw[i] << 16 : raw[i]);
+            if (k0 + i * 64 + lane >= a.w.K) x[i] = 0.0f;
         }
         int count = 0;
 #pragma unroll
