@@ -74,6 +74,18 @@ __device__ __forceinline__ void store_any(void *p, const V &v) {
     __builtin_memcpy(p, &v, sizeof(V));
 }
 
+// Eight 16-bit values moved down by `by` of them, 0 from above.
+__device__ __forceinline__ void move_down(uint32_t (&w)[4], int by) {
+    uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
+    if (by & 4) w0 = w2, w1 = w3, w2 = 0u, w3 = 0u;
+    if (by & 2) w0 = w1, w1 = w2, w2 = w3, w3 = 0u;
+    const uint32_t half = by & 1 ? 16 : 0, all = by < 8 ? 0xffffffffu : 0u;
+    w[0] = __builtin_amdgcn_alignbit(w1, w0, half) & all;
+    w[1] = __builtin_amdgcn_alignbit(w2, w1, half) & all;
+    w[2] = __builtin_amdgcn_alignbit(w3, w2, half) & all;
+    w[3] = __builtin_amdgcn_alignbit(0u, w3, half) & all;
+}
+
 // Eight consecutive values, or the first n of them and zeros.
 template <class T>
 __device__ __forceinline__ void load8(float (&v)[8], const typename T::type *p, int n) {

@@ -111,18 +111,13 @@ struct Chunk {
             for (int i = 0; i < 8; ++i) v[i] = there ? __uint_as_float(w[i]) : 0.0f;
         } else {
             const int here = at<SHORT>(c), by = here < D - 8 ? 0 : here - (D - 8);
-            const uint32_t all = by < 8 ? 0xffffffffu : 0u;
-            uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
+            uint32_t u[4] = {w[0], w[1], w[2], w[3]};
             if constexpr (kRead == kMoved) {
-                if (by & 4) w0 = w2, w1 = w3, w2 = 0u, w3 = 0u;
-                if (by & 2) w0 = w1, w1 = w2, w2 = w3, w3 = 0u;
-                const uint32_t half = by & 1 ? 16 : 0;
-                w0 = __builtin_amdgcn_alignbit(w1, w0, half);
-                w1 = __builtin_amdgcn_alignbit(w2, w1, half);
-                w2 = __builtin_amdgcn_alignbit(w3, w2, half);
-                w3 = __builtin_amdgcn_alignbit(0u, w3, half);
+                move_down(u, by);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = by < 8 ? u[i] : 0u;
             }
-            const uint32_t u[4] = {w0 & all, w1 & all, w2 & all, w3 & all};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 v[2 * i] = T::widen(u[i] & 0xffffu);
