@@ -575,16 +575,23 @@ bool packs(const W4Shape &w, int T, int xtype, int slots) {
 //
 // An expert has few rows and many experts run: four tiles, or two where tokens are
 // few (64 experts of 1408 outputs of 2048: 16 tokens 18.6 against 20.4, one token
-// 8.3 against 7.5).
+// 8.3 against 7.5), and three tiles of columns where an expert has 32 pairs on average
+// (4096 tokens 545 against 685, 256 tokens 50.4 and 54.2; 128, 16 pairs, 39.0 and
+// 34.3); of a staged type two, or four with many tokens and outputs (the
+// same in fp32 with one, two and four: one token 16.2 9.3 9.7, 64 tokens 130 54.2
+// 49.9; 8 experts of 1024 of 512, 100 tokens 16.0 14.3 15.8).
 template <int MODE>
 hipError_t rows_as_they_stand(const W4Args &a, hipStream_t s) {
     const int64_t tiles = a.w.tiles(), steps = a.w.steps();
     if constexpr (kStaged<MODE>) {
+        if (a.slots)
+            return a.T > 16 && tiles * a.w.E >= 1024 ? run<MODE, 4, 1, 1, 256>(a, 4, s) : run<MODE, 2, 1, 1, 256>(a, 4, s);
         if (tiles > 1024) return run<MODE, 4, 1, 1, 256>(a, 4, s);
         if (tiles > 256) return run<MODE, 2, 1, 2, 512>(a, 8, s);
         return run<MODE, 1, 1, 4, 512>(a, 8, s);
     } else {
         const bool few = a.T <= 4;
+        if (a.slots && static_cast<int64_t>(a.T) * a.slots >= int64_t{32} * a.w.E) return run<MODE, 4, 3, 1, 256>(a, 4, s);
         if (a.slots) return few ? run<MODE, 2, 1, 2, 256>(a, 4, s) : run<MODE, 4, 1, 1, 256>(a, 4, s);
         if (tiles > 1024 && (!few || tiles >= 2048)) return run<MODE, 4, 1, 1, 256>(a, 4, s);
         if (tiles > 512 && tiles <= (few ? 896 : 1024)) return run<MODE, 4, 1, 1, 512>(a, 8, s);

@@ -673,6 +673,21 @@ def a_route(torch, isc, r, T, E, k, empty):
 
 
 @pytest.mark.parametrize("xtype", TYPES + ["mx8"])
+@pytest.mark.parametrize("T,E,N", [(20, 64, 260), (100, 3, 70), (300, 8, 530), (97, 2, 530)])
+def test_experts_many_rows(torch, isc, T, E, N, xtype):
+    """More rows an expert than one matrix operand holds, few and many outputs."""
+    note("experts many rows", T, E, N, xtype)
+    r, K, k = np.random.default_rng(T + N), 300, 2
+    route, ids, _ = a_route(torch, isc, r, T, E, k, 0.1)
+    w4, w = weights(torch, isc, r, E, N, K, "tiles", lead=E)
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.routed(w, xv, ids)
+    close(host(isc.isc_w4_linear(xd, w4, route=route, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
+@pytest.mark.parametrize("xtype", TYPES + ["mx8"])
 @pytest.mark.parametrize("T,E,k,N,K,empty", [(1, 3, 2, 20, 70, 0.0), (5, 4, 4, 33, 128, 0.3), (40, 6, 2, 17, 600, 0.1),
                                              (100, 2, 1, 40, 64, 0.5), (3, 64, 8, 16, 520, 0.0), (4, 5, 3, 30, 96, 1.0)])
 def test_experts(torch, isc, T, E, k, N, K, empty, xtype):
