@@ -472,16 +472,19 @@ template <class T>
 hipError_t norm_bwd_of(const NormBwdArgs &a, hipStream_t s) {
     const RowPlan p = row_plan(a.D, 1024);
     const bool brief = p.threads == 64;
-    const int blocks = norm_bwd_blocks(a.T, a.D);
-    const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(brief ? 64 * kShortRows : p.threads));
-    if (brief)
-        norm_bwd_with<T, 1, true>(a, grid, block, s);
-    else if (p.chunks == 1)
-        norm_bwd_with<T, 1, false>(a, grid, block, s);
-    else
-        norm_bwd_with<T, 2, false>(a, grid, block, s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    // without rows there are no sums to add: dw is 0, and the weight, which such a call
+    // need not have, is not read
+    const int blocks = a.T > 0 ? norm_bwd_blocks(a.T, a.D) : 0;
+    if (blocks > 0) {
+        const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(brief ? 64 * kShortRows : p.threads));
+        if (brief)
+            norm_bwd_with<T, 1, true>(a, grid, block, s);
+        else if (p.chunks == 1)
+            norm_bwd_with<T, 1, false>(a, grid, block, s);
+        else
+            norm_bwd_with<T, 2, false>(a, grid, block, s);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     column_sum_kernel<<<dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(1024), 0, s>>>(a.part, blocks, a.D, a.dw);
     return hipGetLastError();
 }

@@ -1,0 +1,106 @@
+"""What the feed-forward operators launch, on the host: the library runs over a
+recorder in place of the HIP runtime, which notes every kernel with its grid and
+runs nothing.  So calls can be looked at that are too large to make here, and calls
+that have no addresses to read."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+A, B, C, D, E, F, G = (0x100000000000 * i for i in range(1, 8))  # addresses that are only compared
+
+RECORDER = r"""
+#include <hip/hip_runtime_api.h>
+#include <cstdio>
+#include <cstring>
+#include <map>
+#include <string>
+
+namespace {
+std::map<const void *, std::string> names;
+std::string log;
+struct Call { dim3 grid, block; size_t lds; hipStream_t stream; } call;
+}  // namespace
+
+extern "C" {
+void **__hipRegisterFatBinary(const void *) { static void *handle; return &handle; }
+void __hipUnregisterFatBinary(void **) {}
+void __hipRegisterVar(void **, void *, char *, char *, int, size_t, int, int) {}
+void __hipRegisterFunction(void **, const void *host, char *, const char *name, unsigned, void *, void *, dim3 *, dim3 *,
+                           int *) { names[host] = name; }
+hipError_t __hipPushCallConfiguration(dim3 g, dim3 b, size_t lds, hipStream_t s) { call = Call{g, b, lds, s}; return hipSuccess; }
+hipError_t __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *lds, hipStream_t *s) {
+    *g = call.grid; *b = call.block; *lds = call.lds; *s = call.stream;
+    return hipSuccess;
+}
+hipError_t hipLaunchKernel(const void *f, dim3 g, dim3 b, void **, size_t lds, hipStream_t) {
+    char dims[200];
+    std::snprintf(dims, sizeof dims, " %u %u %u %u %u %u %zu\n", g.x, g.y, g.z, b.x, b.y, b.z, lds);
+    log += names[f] + dims;
+    return hipSuccess;
+}
+hipError_t hipGetDevice(int *d) { *d = 0; return hipSuccess; }
+hipError_t hipGetDevicePropertiesR0600(hipDeviceProp_tR0600 *p, int) {
+    std::memset(p, 0, sizeof *p);
+    std::strcpy(p->gcnArchName, "gfx950");
+    return hipSuccess;
+}
+hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipFuncSetAttribute(const void *, hipFuncAttribute, int) { return hipSuccess; }
+const char *recorded() { static std::string s; s = log; log.clear(); return s.c_str(); }
+}
+"""
+
+RUN = r"""
+import ctypes, json, sys
+recorder = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)  # found before the runtime that the library names
+recorder.recorded.restype = ctypes.c_char_p
+import paper_1704_07724_amd as isc
+out = []
+for name, args in json.loads(sys.stdin.read()):
+    args = [isc.W4Desc(*a) if isinstance(a, list) else a for a in args]
+    n = ctypes.c_size_t()
+    status = getattr(isc.lib(), name)(*args, *([n] if name.endswith("_size") else []))
+    kernels = [line.split() for line in recorder.recorded().decode().splitlines()]
+    out.append((status, n.value, [(k[0], [int(v) for v in k[1:]]) for k in kernels]))
+print(json.dumps(out))
+"""
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    """launches([(entry point, arguments), ...]) -> [(status, size, [(kernel, [grid, block, bytes of LDS]), ...]), ...]"""
+    tmp = tmp_path_factory.mktemp("recorder")
+    src, so = tmp / "recorder.cpp", tmp / "recorder.so"
+    src.write_text(RECORDER)
+    subprocess.run(["g++", "-shared", "-fPIC", "-O1", "-w", "-D__HIP_PLATFORM_AMD__=1", "-I", os.path.join(ROCM, "include"),
+                    str(src), "-o", str(so)], check=True)
+
+    def run(calls):
+        r = subprocess.run([sys.executable, "-c", RUN, str(so)], input=json.dumps(calls), cwd=ROOT, capture_output=True,
+                           text=True, timeout=300)
+        assert r.returncode == 0, r.stderr
+        return json.loads(r.stdout.splitlines()[-1])
+    return run
+
+
+def norm_bwd(T, N, t=2, **kw):
+    a = dict(dy=A, h=B, w=C, rstd=D, dh=None, dx=E, dw=F, ws=G)
+    a.update(kw)
+    return "isc_rmsnorm_bwd", [T, N, t, a["dy"], N, a["h"], N, a["w"], t, a["rstd"], a["dh"], N, a["dx"], N, a["dw"],
+                               a["ws"], 1 << 40, None]
+
+
+def test_norm_bwd_without_rows(launches):
+    """No kernel that reads a row or the weight: the sums of nothing alone are written."""
+    none = dict(dy=None, h=None, w=None, rstd=None, dx=None)
+    shapes = [(N, t) for N in (1, 64, 512, 1000, 4096, 16384) for t in (0, 1, 2)]
+    for (N, t), (status, _, kernels) in zip(shapes, launches([norm_bwd(0, N, t, **none) for N, t in shapes])):
+        assert status == 0 and len(kernels) == 1 and "column_sum" in kernels[0][0], (N, t, kernels)
+        assert kernels[0][1][0] == (N + 31) // 32
+    (_, _, kernels), = launches([norm_bwd(1, 64)])
+    assert len(kernels) == 2 and "rmsnorm_bwd" in kernels[0][0]

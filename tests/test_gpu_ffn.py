@@ -179,6 +179,19 @@ def test_norm_no_rows(torch, isc):
     assert dx.shape == (0, 64) and (host(dw) == 0).all()
 
 
+@pytest.mark.parametrize("D", [64, 1000, 16384])
+def test_norm_bwd_no_rows_no_weight(torch, isc, D):
+    """A call without rows needs none of their tensors, the weight among them: dw is 0."""
+    note("norm bwd no rows, no weight", D)
+    n = ctypes.c_size_t()
+    assert isc.lib().isc_rmsnorm_bwd_workspace_size(0, D, n) == 0
+    ws = torch.full((n.value,), 255, dtype=torch.uint8, device="cuda")
+    dw = torch.full((D,), float("nan"), device="cuda")
+    assert isc.lib().isc_rmsnorm_bwd(0, D, 2, None, D, None, D, None, 2, None, None, D, None, D, dw.data_ptr(),
+                                     ws.data_ptr(), n.value, isc._stream(None)) == 0
+    assert (host(dw) == 0).all()
+
+
 def test_norm_in_place(torch, isc):
     """h written over the residual, and dx over dy, through the C entry points."""
     note("norm in place")
