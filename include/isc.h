@@ -466,7 +466,8 @@ typedef enum isc_type {
  *     that brings its largest magnitude to 448 or below; a group with a value
  *     that is not finite has scale 255 and NaN values.
  *   rstd: T floats, as isc_rmsnorm_bwd takes them.
- * One launch.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+ * One launch, more only where T rows have 2^32 threads or more (from 2^22 rows of
+ * over 7680 values, 2^26 of up to 512).  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_rmsnorm(int32_t T, int32_t D, int32_t type, const void *x, int64_t ldx, const void *r, int64_t ldr,
                 const void *w, int32_t w_type, float eps, void *h, int64_t ldh, void *y, int64_t ldy, void *q,
                 int64_t ldq, void *scales, int64_t lds, float *rstd, void *stream);

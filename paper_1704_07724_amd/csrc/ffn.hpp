@@ -196,6 +196,16 @@ __device__ __forceinline__ uint32_t group_scale(uint32_t abits) {
 
 // --- launchers --------------------------------------------------------------
 
+// Threads that a launch may have along a dimension of its grid: fewer than 2^32.
+// Calls of more rows than that take are launched in parts.
+constexpr int64_t kLaunchThreads = (int64_t{1} << 32) - 1;
+
+// `bytes` past p, which may be none.
+template <class P>
+P *past(P *p, int64_t bytes) {
+    return p ? reinterpret_cast<P *>(reinterpret_cast<uintptr_t>(p) + static_cast<uintptr_t>(bytes)) : nullptr;
+}
+
 struct NormArgs {
     const void *x, *r, *w;      // r: nullptr without a residual
     void *h, *y, *q, *scales;   // each nullptr where it is not asked for

@@ -455,17 +455,34 @@ void norm_bwd_with(const NormBwdArgs &a, dim3 grid, dim3 block, hipStream_t s) {
     rmsnorm_bwd_kernel<T, C, SHORT, kAny><<<grid, block, 0, s>>>(a);
 }
 
+// Rows t0 .. t0 + n of a call.
+NormArgs rows_of(NormArgs a, int64_t t0, int64_t n, int64_t size) {
+    a.x = past(a.x, t0 * a.ldx * size), a.r = past(a.r, t0 * a.ldr * size);
+    a.h = past(a.h, t0 * a.ldh * size), a.y = past(a.y, t0 * a.ldy * size);
+    a.q = past(a.q, t0 * a.ldq), a.scales = past(a.scales, t0 * a.lds);
+    a.rstd = past(a.rstd, t0 * 4);
+    a.T = static_cast<int>(n);
+    return a;
+}
+
 template <class T>
-hipError_t norm_of(const NormArgs &a, hipStream_t s) {
-    const RowPlan p = row_plan(a.D, 1024);
-    const dim3 grid(static_cast<unsigned>(a.T)), block(static_cast<unsigned>(p.threads));
-    switch (p.chunks) {
-    case 1: norm_with<T, 1>(a, grid, block, s); break;
-    case 2: norm_with<T, 2>(a, grid, block, s); break;
-    case 4: norm_with<T, 4>(a, grid, block, s); break;
-    default: rmsnorm_long_kernel<T><<<grid, block, 0, s>>>(a, p.chunks); break;
+hipError_t norm_of(const NormArgs &all, hipStream_t s) {
+    const RowPlan p = row_plan(all.D, 1024);
+    // 2^26 - 1 rows of up to 512 values a launch, 2^22 - 1 from 7681 on
+    const int64_t most = kLaunchThreads / p.threads;
+    for (int64_t t0 = 0; t0 < all.T; t0 += most) {
+        const int64_t n = all.T - t0 < most ? all.T - t0 : most;
+        const NormArgs a = rows_of(all, t0, n, sizeof(typename T::type));
+        const dim3 grid(static_cast<unsigned>(n)), block(static_cast<unsigned>(p.threads));
+        switch (p.chunks) {
+        case 1: norm_with<T, 1>(a, grid, block, s); break;
+        case 2: norm_with<T, 2>(a, grid, block, s); break;
+        case 4: norm_with<T, 4>(a, grid, block, s); break;
+        default: rmsnorm_long_kernel<T><<<grid, block, 0, s>>>(a, p.chunks); break;
+        }
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 template <class T>

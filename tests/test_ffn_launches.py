@@ -11,7 +11,7 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
-A, B, C, D, E, F, G = (0x100000000000 * i for i in range(1, 8))  # addresses that are only compared
+A, B, C, D, E, F, G = (0x4000000000000 * i for i in range(1, 8))  # addresses that are only compared
 
 RECORDER = r"""
 #include <hip/hip_runtime_api.h>
@@ -104,3 +104,22 @@ def test_norm_bwd_without_rows(launches):
         assert kernels[0][1][0] == (N + 31) // 32
     (_, _, kernels), = launches([norm_bwd(1, 64)])
     assert len(kernels) == 2 and "rmsnorm_bwd" in kernels[0][0]
+
+
+def norm(T, N, t=2):
+    return "isc_rmsnorm", [T, N, t, A, N, B, N, C, t, 1e-6, D, N, E, N, F, N, G, (N + 31) // 32, None, None]
+
+
+def launchable(kernels):
+    """Every grid is one that a launch takes, with a workgroup at least; returns the kernels' workgroups."""
+    for name, (x, y, z, bx, by, bz, lds) in kernels:
+        assert 0 < x * bx < 2 ** 32 and 0 < y <= 65535 and z == by == bz == 1 and 0 < bx <= 1024, (name, x, y, bx)
+    return [k[1][0] for k in kernels]
+
+
+def test_norm_of_many_rows(launches):
+    """A workgroup a row, in as many launches as it takes."""
+    shapes = [(T, N, t) for T in (1, 2 ** 22 - 1, 2 ** 22, 2 ** 22 + 1, 2 ** 26, 2 ** 26 + 5, 2 ** 31 - 1)
+              for N in (1, 64, 512, 513, 4096, 8192, 65536) for t in (0, 1, 2)]
+    for (T, N, t), (status, _, kernels) in zip(shapes, launches([norm(*s) for s in shapes])):
+        assert status == 0 and sum(launchable(kernels)) == T, (T, N, t)

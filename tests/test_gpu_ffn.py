@@ -179,6 +179,28 @@ def test_norm_no_rows(torch, isc):
     assert dx.shape == (0, 64) and (host(dw) == 0).all()
 
 
+@pytest.mark.parametrize("D,T", [(3, 2 ** 26 + 7), (24, 2 ** 26 + 1)])
+def test_norm_more_rows_than_a_launch_takes(torch, isc, D, T):
+    """The rows of the last launch and those on either side of its start, each output, as in a small call."""
+    note("norm many rows", D, T)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x = torch.randn((T, D), generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(D, generator=g, device="cuda").bfloat16()
+    got = isc.isc_rmsnorm(x, w, residual=x, mx8=True, rstd=True)
+    cut = (2 ** 32 - 1) // 64
+    for rows in (slice(0, 4), slice(cut - 4, cut + 4), slice(T - 4, T)):
+        small = isc.isc_rmsnorm(x[rows], w, residual=x[rows], mx8=True, rstd=True)
+        for a, b in ((got.y, small.y), (got.h, small.h), (got.mx8.q, small.mx8.q), (got.mx8.scales, small.mx8.scales),
+                     (got.rstd, small.rstd)):
+            assert np.array_equal(host(a[rows]), host(b)), rows
+    # and no row in between was left out: every mean is that of its row
+    step = 1 << 22
+    for t in range(0, T, step):
+        h = x[t:t + step].float() * 2
+        want = torch.rsqrt((h * h).mean(-1) + 1e-6)
+        assert ((got.rstd[t:t + step] - want).abs() <= 256 * E24 * want).all(), t
+
+
 @pytest.mark.parametrize("D", [64, 1000, 16384])
 def test_norm_bwd_no_rows_no_weight(torch, isc, D):
     """A call without rows needs none of their tensors, the weight among them: dw is 0."""
