@@ -514,7 +514,7 @@ hipError_t launch_rmsnorm(const NormArgs &a, hipStream_t s) {
 
 int norm_bwd_blocks(int T, int D) {
     const int threads = row_plan(D, 1024).threads;
-    const int turns = threads == 64 ? (T + kShortRows - 1) / kShortRows : T;
+    const int64_t turns = threads == 64 ? (int64_t{T} + kShortRows - 1) / kShortRows : T;  // (T may be 2^31 - 1)
     // Short rows want more workgroups at once, long ones fewer sums for the second
     // launch to read (8192 bfloat16 rows, us with 1, 2, 4, 8 workgroups a compute
     // unit: of 1024 37.6 24.0 20.0 21.6, of 2048 50.1 33.9 31.8 35.6, of 4096 58.7
@@ -523,9 +523,9 @@ int norm_bwd_blocks(int T, int D) {
     // second's loads ahead, from 256 turns on (rows of 4096: 330 of them 9.7 and 10.6
     // with one each, 200 of them 8.2 and 8.1), from 512 of short rows' (2400 rows of
     // 500: 11.2 and 10.2).
-    const int most = 256 * (threads == 64 || threads > 512 || (threads > 256 && turns < 2048) ? 1 : threads > 256 ? 2 : 4);
-    const int some = turns < (threads == 64 ? 512 : 256) ? turns : (turns + 1) / 2;
-    return some < 1 ? 1 : some < most ? some : most;
+    const int64_t most = 256 * (threads == 64 || threads > 512 || (threads > 256 && turns < 2048) ? 1 : threads > 256 ? 2 : 4);
+    const int64_t some = turns < (threads == 64 ? 512 : 256) ? turns : (turns + 1) / 2;
+    return static_cast<int>(some < 1 ? 1 : some < most ? some : most);
 }
 
 hipError_t launch_rmsnorm_bwd(const NormBwdArgs &a, hipStream_t s) {

@@ -123,3 +123,12 @@ def test_norm_of_many_rows(launches):
               for N in (1, 64, 512, 513, 4096, 8192, 65536) for t in (0, 1, 2)]
     for (T, N, t), (status, _, kernels) in zip(shapes, launches([norm(*s) for s in shapes])):
         assert status == 0 and sum(launchable(kernels)) == T, (T, N, t)
+
+
+def test_norm_bwd_of_many_rows(launches):
+    """The count of workgroups holds up to the largest count of rows, and the workspace with it."""
+    shapes = [(T, N) for T in (2 ** 22, 2 ** 31 - 8, 2 ** 31 - 1) for N in (1, 64, 512, 513, 4096, 16384)]
+    calls = [norm_bwd(*s) for s in shapes] + [("isc_rmsnorm_bwd_workspace_size", list(s)) for s in shapes]
+    out = launches(calls)
+    for (T, N), (status, _, kernels), (_, size, _) in zip(shapes, out, out[len(shapes):]):
+        assert status == 0 and launchable(kernels)[0] >= 256 and size == 4 * N * kernels[0][1][0], (T, N, kernels)
