@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[c][j] = 0.0f;
     }
-    // chunk c of a row of h, dy and dh: as loaded, and their values
+    // chunk c of a row of h, dy and dh as loaded, and dh's values
     using In = Chunk<T, READ, SHORT>;
     const auto load = [&](int64_t t, int c, Words &h, Words &dy, Words &dh) {
         In::load(h, static_cast<const E *>(a.h) + t * a.ldh, c, a.D);
@@ -308,9 +308,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) dh[i] = 0u;
     };
-    const auto get = [&](int c, const Words &h, const Words &dy, const Words &dh, float(&n)[8], float(&g)[8], float(&d)[8]) {
-        In::get(n, h, c, a.D);
-        In::get(g, dy, c, a.D);
+    const auto get_dh = [&](int c, const Words &dh, float(&d)[8]) {
         if (READ == kAny || a.dh)  // (the one set 0 where there is none, the other not even loaded)
             In::get(d, dh, c, a.D);
         else
@@ -328,15 +326,22 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
     int turn = 0;
     for (int64_t t = t0; t < a.T; t += step, turn ^= 1) {
         float n[C][8], g[C][8], d[C][8];
+        // dh of two chunks stays as loaded until it is added, half the registers of its
+        // values, which would spill (8192 bfloat16 rows of 8200 119 us, 125 with spills,
+        // 2000 fp16 rows of 12288 38 and 42); one chunk has room for them
+        Words dh[C];
         const float rstd = kAhead ? next_rstd : a.rstd[t];
         if constexpr (kAhead) {
-            get(0, next_h, next_dy, next_dh, n[0], g[0], d[0]);
+            In::get(n[0], next_h, 0, a.D);
+            In::get(g[0], next_dy, 0, a.D);
+            get_dh(0, next_dh, d[0]);
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                Words h, dy, dh;
-                load(t, c, h, dy, dh);
-                get(c, h, dy, dh, n[c], g[c], d[c]);
+                Words h, dy;
+                load(t, c, h, dy, dh[c]);
+                In::get(n[c], h, c, a.D);
+                In::get(g[c], dy, c, a.D);
             }
         }
         float dot = 0.0f;
@@ -361,6 +366,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_kernel(NormBwdArgs a) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float o[8];
+            if (!kAhead) get_dh(c, dh[c], d[c]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = fmaf(rstd, fmaf(-n[c][j], mean, g[c][j]), d[c][j]);
             store_chunk<T, SHORT>(static_cast<E *>(a.dx) + t * a.ldx, o, c, a.D);
