@@ -524,7 +524,7 @@ int isc_route(int32_t T, int32_t E, int32_t k, int32_t type, const void *logits,
  * none): dweights T x k, ids as isc_route gave them (all different within a
  * token; an id outside [0, E) is an empty slot), score, renorm and scale as
  * there.  dlogits: T x E of `type`, fully written; may be logits in place.
- * One launch.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+ * One launch, one more for every 2^26 - 4 tokens.  Errors: NULL, SHAPE, LIMIT, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_route_bwd(int32_t T, int32_t E, int32_t k, int32_t type, const float *dweights, const void *logits, int64_t ld,
                   const int32_t *ids, int32_t score, int32_t renorm, float scale, void *dlogits, int64_t ldd,
                   void *stream);

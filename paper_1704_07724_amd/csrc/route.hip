@@ -454,8 +454,17 @@ hipError_t four_at_a_time(const RouteArgs &a, hipStream_t s) {
 template <int C>
 hipError_t route_bwd_of(const RouteBwdArgs &a, hipStream_t s) {
     const size_t lds = sizeof(float) * 4 * static_cast<size_t>(a.E);
-    route_bwd_kernel<C><<<dim3(static_cast<unsigned>((static_cast<int64_t>(a.T) + 3) / 4)), dim3(256), lds, s>>>(a);
-    return hipGetLastError();
+    constexpr int64_t most = kLaunchThreads / 256 * 4;  // tokens of a launch: 2^26 - 4
+    const int64_t size = a.type == ISC_F32 ? 4 : 2;
+    for (int64_t t0 = 0; t0 < a.T; t0 += most) {
+        RouteBwdArgs part = a;
+        part.T = static_cast<int>(a.T - t0 < most ? a.T - t0 : most);
+        part.dweights = past(a.dweights, t0 * a.k * 4), part.ids = past(a.ids, t0 * a.k * 4);
+        part.logits = past(a.logits, t0 * a.ld * size), part.dlogits = past(a.dlogits, t0 * a.ldd * size);
+        route_bwd_kernel<C><<<dim3(static_cast<unsigned>((int64_t{part.T} + 3) / 4)), dim3(256), lds, s>>>(part);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

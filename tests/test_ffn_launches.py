@@ -132,3 +132,14 @@ def test_norm_bwd_of_many_rows(launches):
     out = launches(calls)
     for (T, N), (status, _, kernels), (_, size, _) in zip(shapes, out, out[len(shapes):]):
         assert status == 0 and launchable(kernels)[0] >= 256 and size == 4 * N * kernels[0][1][0], (T, N, kernels)
+
+
+def route_bwd(T, N, k):
+    return "isc_route_bwd", [T, N, k, 2, A, B, N, C, 0, 1, 1.0, D, N, None]
+
+
+def test_route_bwd_of_many_tokens(launches):
+    """Four tokens a workgroup, in as many launches as it takes."""
+    shapes = [(T, N) for T in (1, 2 ** 26 - 5, 2 ** 26 - 4, 2 ** 26 - 3, 2 ** 26, 2 ** 30 + 1, 2 ** 31 - 1) for N in (2, 64, 1024)]
+    for (T, N), (status, _, kernels) in zip(shapes, launches([route_bwd(*s, 2) for s in shapes])):
+        assert status == 0 and sum(launchable(kernels)) == (T + 3) // 4, (T, N, kernels)

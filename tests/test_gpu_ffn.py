@@ -480,6 +480,28 @@ def test_route_bwd(torch, isc, T, E, k, score, renorm, dtype):
     assert np.array_equal(host(s), host(got))
 
 
+def test_route_bwd_more_tokens_than_a_launch_takes(torch, isc):
+    """Tokens on either side of a launch's last one, and the last, as in a small call; none left out."""
+    T, E, k = 2 ** 26 + 3, 4, 2
+    note("route bwd many tokens", T)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((T, E), generator=g, device="cuda", dtype=torch.bfloat16)
+    ids = torch.arange(k, device="cuda", dtype=torch.int32).expand(T, k).contiguous()
+    dw = torch.randn((T, k), generator=g, device="cuda")
+    got = isc.isc_route_bwd(dw, x, ids)
+    cut = 2 ** 26 - 4
+    for rows in (slice(0, 4), slice(cut - 4, cut + 4), slice(T - 4, T)):
+        assert torch.equal(got[rows], isc.isc_route_bwd(dw[rows], x[rows], ids[rows])), rows
+    # and every token's, by w (1 - w) (dweights_0 - dweights_1) of its two experts
+    for t in range(0, T, 1 << 23):
+        l, d = x[t:t + (1 << 23)].double(), dw[t:t + (1 << 23)].double()
+        w = torch.sigmoid(l[:, 0] - l[:, 1])
+        want = w * (1 - w) * (d[:, 0] - d[:, 1])
+        size = 128 * E24 * 2 * d.abs().sum(-1) + U["bfloat16"] * want.abs()
+        mine = got[t:t + (1 << 23)].double()
+        assert ((mine[:, 0] - want).abs() <= size).all() and ((mine[:, 1] + want).abs() <= size).all(), t
+
+
 def test_route_bwd_against_differences(torch, isc):
     """Along a direction that does not change the choice (the step is small against the gaps)."""
     note("route bwd differences")
