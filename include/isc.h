@@ -498,7 +498,8 @@ typedef enum isc_score {
  * Errors: NULL, SHAPE, LIMIT. */
 int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes);
 
-/* Routes T tokens to k of E experts each (E <= 1024, k <= 64).
+/* Routes T tokens to k of E experts each (E <= 1024, k <= 64, T <= 2^28 - 64,
+ * T * k < 2^31).
  *   logits: T x E of `type`.  s = softmax or sigmoid of a token's logits;
  *   bias: E floats added to s for the choice only (NULL: none).
  *   groups: the experts fall into that many groups of E/groups consecutive

@@ -12,6 +12,7 @@ constexpr int64_t kI32Max = std::numeric_limits<int32_t>::max();
 constexpr int64_t kI64Room = int64_t{1} << 56;  // elements a strided tensor may span
 constexpr size_t kAlign = 256;
 constexpr int32_t kMaxNorm = 65536, kMaxNormBwd = 16384, kMaxExperts = 1024, kMaxSlots = 64, kMaxTokens = 1 << 20;
+constexpr int32_t kMaxRouted = (1 << 28) - 64;  // 64 tokens for every workgroup of 1024 threads of a launch
 
 bool element_type(int32_t t) { return t == ISC_F32 || t == ISC_F16 || t == ISC_BF16; }
 size_t type_bytes(int32_t t) { return t == ISC_F32 ? 4 : t == ISC_MX8 ? 1 : 2; }
@@ -128,7 +129,7 @@ int isc_rmsnorm_bwd(int32_t T, int32_t D, int32_t type, const void *dy, int64_t 
 int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes) {
     if (!bytes) return ISC_ERR_NULL;
     if (T < 0 || E < 1) return ISC_ERR_SHAPE;
-    if (E > kMaxExperts) return ISC_ERR_LIMIT;
+    if (E > kMaxExperts || T > kMaxRouted) return ISC_ERR_LIMIT;
     *bytes = isc::route_count_bytes(T, E);
     return ISC_OK;
 }

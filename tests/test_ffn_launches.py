@@ -143,3 +143,20 @@ def test_route_bwd_of_many_tokens(launches):
     shapes = [(T, N) for T in (1, 2 ** 26 - 5, 2 ** 26 - 4, 2 ** 26 - 3, 2 ** 26, 2 ** 30 + 1, 2 ** 31 - 1) for N in (2, 64, 1024)]
     for (T, N), (status, _, kernels) in zip(shapes, launches([route_bwd(*s, 2) for s in shapes])):
         assert status == 0 and sum(launchable(kernels)) == (T + 3) // 4, (T, N, kernels)
+
+
+def route(T, N, k, groups=1):
+    return "isc_route", [T, N, k, 2, A, N, None, 1, groups, groups, 1, 1.0, B, C, D, E, F, 1 << 50, None]
+
+
+def test_route_of_many_tokens(launches):
+    """Up to the limit on tokens every launch is one that the device takes; past it the call and the
+    workspace's size are refused, not the launch."""
+    most = 2 ** 28 - 64
+    for N, k, groups in ((2, 1, 1), (64, 7, 1), (100, 7, 2), (300, 5, 4), (600, 3, 1)):
+        sizes = [("isc_route_workspace_size", [T, N]) for T in (most, most + 1, 2 ** 31 - 1)]
+        out = launches([route(T, N, k, groups) for T in (2 ** 22, most, most + 1, 2 ** 31 // k - 1)] + sizes)
+        for status, _, kernels in out[:2]:
+            assert status == 0 and len(kernels) == 2 and launchable(kernels), (N, kernels)
+        assert [(o[0], o[2]) for o in out[2:4]] == [(3, []), (3, [])], out[2:4]
+        assert [o[0] for o in out[4:]] == [0, 3, 3]
