@@ -599,7 +599,7 @@ int isc_w4_skip_workspace_size(const isc_w4_desc *d, int32_t T, int32_t slots, s
  *   x_type, y_type: ISC_F32, ISC_F16 or ISC_BF16.  y: T x N.
  *   ws: isc_w4_skip_workspace_size bytes, 256-byte aligned.
  * One launch, and a second that adds ranges of the inputs up where there are
- * several.  Deterministic.
+ * several; more where the tokens' outputs, 512 at a time, come to 2^23.  Deterministic.
  * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_w4_skip(const isc_w4_desc *d, const void *packed, int32_t T, const void *x, int32_t x_type, int64_t ldx,
                 int32_t slots, const int32_t *ids, const float *weights, void *y, int32_t y_type, int64_t ldy, void *ws,

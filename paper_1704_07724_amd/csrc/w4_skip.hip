@@ -221,15 +221,24 @@ int w4_skip_ranges(const W4Shape &w, int T, int slots) { return cut_of(w, T, slo
 
 hipError_t launch_w4_skip(const W4Args &a, hipStream_t s) {
     const Cut cut = cut_of(a.w, a.T, a.slots);
-    const dim3 grid(static_cast<unsigned>((a.w.np() + kOutputs - 1) / kOutputs * a.T), static_cast<unsigned>(cut.ranges));
-    if (cut.tests == 1)
-        w4_skip_kernel<1><<<grid, dim3(64 * kWaves), 0, s>>>(a, cut.ranges);
-    else if (cut.tests == 2)
-        w4_skip_kernel<2><<<grid, dim3(64 * kWaves), 0, s>>>(a, cut.ranges);
-    else
-        w4_skip_kernel<4><<<grid, dim3(64 * kWaves), 0, s>>>(a, cut.ranges);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || cut.ranges == 1) return e;
+    const int64_t cols = (a.w.np() + kOutputs - 1) / kOutputs;
+    const int64_t most = kLaunchThreads / (64 * kWaves) / cols;  // tokens of a launch
+    const int64_t xb = a.xtype == ISC_F32 ? 4 : 2, yb = a.ytype == ISC_F32 ? 4 : 2, slots = a.slots ? a.slots : 1;
+    for (int64_t t0 = 0; t0 < a.T; t0 += most) {  // (once where there are ranges, of a thousand workgroups at most)
+        W4Args part = a;
+        part.T = static_cast<int>(a.T - t0 < most ? a.T - t0 : most);
+        part.x = past(a.x, t0 * slots * a.ldx * xb), part.y = past(a.y, t0 * a.ldy * yb);
+        part.ids = past(a.ids, t0 * slots * 4), part.weights = past(a.weights, t0 * slots * 4);
+        const dim3 grid(static_cast<unsigned>(cols * part.T), static_cast<unsigned>(cut.ranges));
+        if (cut.tests == 1)
+            w4_skip_kernel<1><<<grid, dim3(64 * kWaves), 0, s>>>(part, cut.ranges);
+        else if (cut.tests == 2)
+            w4_skip_kernel<2><<<grid, dim3(64 * kWaves), 0, s>>>(part, cut.ranges);
+        else
+            w4_skip_kernel<4><<<grid, dim3(64 * kWaves), 0, s>>>(part, cut.ranges);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (cut.ranges == 1) return hipSuccess;
     const int64_t all = static_cast<int64_t>(a.T) * a.w.N;
     w4_ranges_kernel<<<dim3(static_cast<unsigned>((all + 63) / 64)), dim3(256), 0, s>>>(a, cut.ranges);
     return hipGetLastError();

@@ -160,3 +160,18 @@ def test_route_of_many_tokens(launches):
             assert status == 0 and len(kernels) == 2 and launchable(kernels), (N, kernels)
         assert [(o[0], o[2]) for o in out[2:4]] == [(3, []), (3, [])], out[2:4]
         assert [o[0] for o in out[4:]] == [0, 3, 3]
+
+
+def skip(T, N, K, slots=0, E_=1):
+    return "isc_w4_skip", [[E_, N, K, 1], A, T, B, 2, K, slots, C if slots else None, D if slots else None, E, 2, N, F, 1 << 50,
+                           None]
+
+
+def test_skip_of_many_tokens(launches):
+    """512 outputs of a token a workgroup, in as many launches as it takes."""
+    shapes = [(T, N, slots) for T in (1, 2 ** 19 - 1, 2 ** 19, 2 ** 20) for N in (1, 4096, 4097, 8192, 2 ** 24) for slots in (0, 3)]
+    for (T, N, slots), (status, _, kernels) in zip(shapes, launches([skip(T, N, 256, slots, 2 if slots else 1)
+                                                                     for T, N, slots in shapes])):
+        assert status == 0 and launchable(kernels), (T, N)
+        across = -(-(-(-N // 128) * 128) // 512)
+        assert sum(k[1][0] for k in kernels if "w4_skip" in k[0]) == T * across, (T, N, slots)

@@ -718,6 +718,46 @@ def test_skip(torch, isc, T, N, K, xtype):
     assert torch.equal(s, isc.isc_w4_skip(xd, w4))
 
 
+@pytest.mark.parametrize("slots", [0, 2])
+def test_skip_more_tokens_than_a_launch_takes(torch, isc, slots):
+    """Tokens on either side of a launch's last one, and the last, as in a small call; none left out."""
+    T, N, K, E = 2 ** 20, 4224, 32, 2  # nine workgroups a token: 932067 tokens a launch
+    note("skip many tokens", slots)
+    r = np.random.default_rng(slots)
+    w4, w = weights(torch, isc, r, E if slots else 1, N, K, "rows", lead=E if slots else None)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    shape = (T, slots, K) if slots else (T, K)
+    x = torch.relu(torch.randn(shape, generator=g, device="cuda")).bfloat16()
+    route = None
+    if slots:
+        first = torch.randint(0, E, (T, 1), generator=g, device="cuda", dtype=torch.int32)
+        route = isc.Route(torch.cat((first, 1 - first), 1), torch.rand((T, slots), generator=g, device="cuda"), None, None)
+    y = isc.isc_w4_skip(x, w4, route=route)
+    cut = (2 ** 32 - 1) // 512 // 9
+    for rows in (slice(0, 4), slice(cut - 4, cut + 4), slice(T - 4, T)):
+        part = route and isc.Route(route.ids[rows], route.weights[rows], None, None)
+        small = isc.isc_w4_skip(x[rows], w4, route=part)
+        # one range of inputs here, one there: the same sums
+        assert torch.equal(y[rows], small), rows
+    # and every token's first outputs, by a product in 64 bits
+    n = 8
+    wd = torch.from_numpy(w[:, :n]).cuda()
+    for t in range(0, T, 1 << 18):
+        v = x[t:t + (1 << 18)].double()
+        v = v if slots else v[:, None]
+        e = route.ids[t:t + (1 << 18)].long() if slots else torch.zeros((v.shape[0], 1), dtype=torch.long, device="cuda")
+        f = route.weights[t:t + (1 << 18)].double() if slots else torch.ones((v.shape[0], 1), device="cuda").double()
+        want, size = 0.0, 0.0
+        for j in range(v.shape[1]):
+            both = torch.stack([v[:, j] @ wd[i].t() for i in range(wd.shape[0])], 1)
+            sizes = torch.stack([v[:, j].abs() @ wd[i].abs().t() for i in range(wd.shape[0])], 1)
+            at = e[:, j, None, None].expand(-1, 1, n)
+            want = want + f[:, j, None] * both.gather(1, at)[:, 0]
+            size = size + f[:, j, None] * sizes.gather(1, at)[:, 0]
+        got = y[t:t + (1 << 18), :n].double()
+        assert ((got - want).abs() <= (2 * K + 64) * E24 * size + U["bfloat16"] * want.abs()).all(), t
+
+
 def a_route(torch, isc, r, T, E, k, empty):
     """A route whose ids and weights are drawn: some slots empty, lists by expert."""
     ids = np.stack([r.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
