@@ -470,52 +470,55 @@ __global__ void __launch_bounds__(THREADS) w4_linear_kernel(W4Args a) {
 }
 
 // x as matrix operands: for every tile of 16 columns, step of 128 inputs and
-// word j of the weights' layout, 16 bytes a lane.  One thread each; inputs past
-// K are 0, so the product needs no last step of its own.
+// word j of the weights' layout, 16 bytes a lane.  One thread each, and the next
+// ones where there are more than a grid's; inputs past K are 0, so the product needs
+// no last step of its own.
+constexpr int64_t kPackBlocks = 1 << 16;  // workgroups of a grid, 4 KiB each at a time
 template <int XTYPE>
 __global__ void __launch_bounds__(256) pack_x_kernel(W4Args a) {
     constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, TOK = 16 / P;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int64_t steps = a.w.steps(), tiles = (a.T + TOK - 1) / TOK;
-    if (item >= tiles * steps * 256) return;
-    const int lane = static_cast<int>(item & 63), j = static_cast<int>(item >> 6 & 3);
-    const int64_t tile = (item >> 8) / steps;
-    const int step = static_cast<int>((item >> 8) % steps);
-    const int col = lane & 15, k = step * 128 + j * 32 + (lane >> 4) * 8;
-    const int64_t t = tile * TOK + col / P;
-    uint32_t out[4] = {0u, 0u, 0u, 0u};
-    const int n = t < a.T && col < TOK * P ? a.w.K - k : 0;
-    if (n > 0) {
-        if constexpr (XTYPE == ISC_MX8) {
-            const uint8_t *p = static_cast<const uint8_t *>(a.x) + t * a.ldx + k;
-            uint32_t v[2] = {0u, 0u};
-            if (a.w.K >= 8) {  // (as load_column does)
-                const int by = n < 8 ? 8 - n : 0;
-                const uint64_t u = load_any<uint64_t>(p - by) >> (8 * by);
-                v[0] = static_cast<uint32_t>(u);
-                v[1] = static_cast<uint32_t>(u >> 32);
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; item < tiles * steps * 256;
+         item += static_cast<int64_t>(gridDim.x) * 256) {
+        const int lane = static_cast<int>(item & 63), j = static_cast<int>(item >> 6 & 3);
+        const int64_t tile = (item >> 8) / steps;
+        const int step = static_cast<int>((item >> 8) % steps);
+        const int col = lane & 15, k = step * 128 + j * 32 + (lane >> 4) * 8;
+        const int64_t t = tile * TOK + col / P;
+        uint32_t out[4] = {0u, 0u, 0u, 0u};
+        const int n = t < a.T && col < TOK * P ? a.w.K - k : 0;
+        if (n > 0) {
+            if constexpr (XTYPE == ISC_MX8) {
+                const uint8_t *p = static_cast<const uint8_t *>(a.x) + t * a.ldx + k;
+                uint32_t v[2] = {0u, 0u};
+                if (a.w.K >= 8) {  // (as load_column does)
+                    const int by = n < 8 ? 8 - n : 0;
+                    const uint64_t u = load_any<uint64_t>(p - by) >> (8 * by);
+                    v[0] = static_cast<uint32_t>(u);
+                    v[1] = static_cast<uint32_t>(u >> 32);
+                } else {
+                    for (int i = 0; i < 8; ++i)
+                        if (i < n) v[i / 4] |= static_cast<uint32_t>(p[i]) << (8 * (i & 3));
+                }
+                const bf16x8 b = operand<kMx8>(v, a.xs[t * a.ldxs + k / 32], 0);
+                const uint4 u = __builtin_bit_cast(uint4, b);
+                out[0] = u.x, out[1] = u.y, out[2] = u.z, out[3] = u.w;
             } else {
-                for (int i = 0; i < 8; ++i)
-                    if (i < n) v[i / 4] |= static_cast<uint32_t>(p[i]) << (8 * (i & 3));
-            }
-            const bf16x8 b = operand<kMx8>(v, a.xs[t * a.ldxs + k / 32], 0);
-            const uint4 u = __builtin_bit_cast(uint4, b);
-            out[0] = u.x, out[1] = u.y, out[2] = u.z, out[3] = u.w;
-        } else {
-            using T = std::conditional_t<XTYPE == ISC_F32, F32, std::conditional_t<XTYPE == ISC_F16, F16, BF16>>;
-            float v[8];
-            load8<T>(v, static_cast<const typename T::type *>(a.x) + t * a.ldx + k, n);
+                using T = std::conditional_t<XTYPE == ISC_F32, F32, std::conditional_t<XTYPE == ISC_F16, F16, BF16>>;
+                float v[8];
+                load8<T>(v, static_cast<const typename T::type *>(a.x) + t * a.ldx + k, n);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t parts[P];
-                cut<P>(parts, v[2 * i], v[2 * i + 1]);
-                out[i] = parts[0];
-                if (P > 1 && col % P == 1) out[i] = parts[P > 1 ? 1 : 0];
-                if (P > 2 && col % P == 2) out[i] = parts[P > 2 ? 2 : 0];
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t parts[P];
+                    cut<P>(parts, v[2 * i], v[2 * i + 1]);
+                    out[i] = parts[0];
+                    if (P > 1 && col % P == 1) out[i] = parts[P > 1 ? 1 : 0];
+                    if (P > 2 && col % P == 2) out[i] = parts[P > 2 ? 2 : 0];
+                }
             }
         }
+        reinterpret_cast<uint4 *>(a.columns)[item] = make_uint4(out[0], out[1], out[2], out[3]);
     }
-    reinterpret_cast<uint4 *>(a.columns)[item] = make_uint4(out[0], out[1], out[2], out[3]);
 }
 
 template <int MODE, int NT, int MT, int DEPTH, int THREADS>
@@ -639,7 +642,8 @@ template <int XTYPE>
 hipError_t packed(const W4Args &a, hipStream_t s) {
     constexpr int P = XTYPE == ISC_F32 ? 3 : XTYPE == ISC_F16 ? 2 : 1, MODE = kPacked + P - 1;
     const int64_t tiles = (a.T + kTokens<MODE> - 1) / kTokens<MODE>;
-    pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(tiles * a.w.steps())), dim3(256), 0, s>>>(a);
+    const int64_t blocks = tiles * a.w.steps();
+    pack_x_kernel<XTYPE><<<dim3(static_cast<unsigned>(blocks < kPackBlocks ? blocks : kPackBlocks)), dim3(256), 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     // one tile of columns (long rows): two of outputs, as above (5000 outputs of
     // 16384: 14.7 us against 18.1 with one)

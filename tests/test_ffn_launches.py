@@ -175,3 +175,28 @@ def test_skip_of_many_tokens(launches):
         assert status == 0 and launchable(kernels), (T, N)
         across = -(-(-(-N // 128) * 128) // 512)
         assert sum(k[1][0] for k in kernels if "w4_skip" in k[0]) == T * across, (T, N, slots)
+
+
+def linear(T, N, K, xt, slots=0, E_=1):
+    per = (B, None) if xt != 3 else (B, C)
+    return "isc_w4_linear", [[E_, N, K, 0], A, T, per[0], xt, K, per[1], (K + 31) // 32, slots, C + (1 << 48) if slots else None,
+                             C + (1 << 49) if slots else None, D if slots else None, E, 2, N, 0, F, 1 << 55, None]
+
+
+def test_linear_of_many_tokens(launches):
+    """Up to the limits on tokens and inputs x is laid out and multiplied by launches that the device takes."""
+    shapes = [(T, N, K, xt) for T in (1, 17, 2 ** 17, 2 ** 20) for N, K in ((16, 8), (48, 8), (48, 16384), (16, 65536), (4096, 32768),
+                                                                         (16, 2 ** 24), (2 ** 24, 16)) for xt in (0, 1, 2, 3)]
+    shapes = [s for s in shapes if s[3] != 0 or s[1] > 48 or s[0] < 2 ** 20]
+    calls = [linear(*s) for s in shapes]
+    sizes = [("isc_w4_linear_workspace_size", [[1, N, K, 0], T, xt, 0]) for T, N, K, xt in shapes]
+    out = launches(calls + sizes)
+    for shape, (status, _, kernels), (st, size, _) in zip(shapes, out, out[len(shapes):]):
+        assert st == 0 and (size == 0 or size >= shape[0] * shape[2] * 2), shape
+        assert status == 0 and launchable(kernels) and "w4_linear" in kernels[-1][0], (shape, kernels)
+
+
+def test_linear_of_many_tokens_by_experts(launches):
+    shapes = [(T, N, K, xt) for T in (1, 2 ** 20) for N, K in ((16, 8), (4096, 4096), (2 ** 20, 32)) for xt in (0, 1, 2, 3)]
+    for shape, (status, _, kernels) in zip(shapes, launches([linear(*s, slots=4, E_=1024) for s in shapes])):
+        assert status == 0 and launchable(kernels), (shape, kernels)

@@ -684,6 +684,27 @@ def test_skip_scales(torch, isc, T, K, N):
     assert np.array_equal(np.isnan(host(isc.isc_w4_skip(xd, pack(scales), dtype=torch.float32))), meets)
 
 
+@pytest.mark.parametrize("xtype,T,K", [("float32", 20003, 2500), ("float16", 20003, 4090), ("bfloat16", 20003, 8190), ("mx8", 20003, 8190)])
+def test_linear_laid_out_in_turns(torch, isc, xtype, T, K):
+    """More of x than the workgroups that lay it out hold at a time: every token, against a product in 64 bits."""
+    note("linear laid out in turns", xtype, T, K)
+    r, N = np.random.default_rng(K), 40
+    w4, w = weights(torch, isc, r, 1, N, K, "tiles")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    if xtype == "mx8":
+        q = torch.randint(0, 127, (T, K), generator=g, device="cuda", dtype=torch.uint8)
+        q |= torch.randint(0, 2, (T, K), generator=g, device="cuda", dtype=torch.uint8) << 7
+        scales = torch.randint(119, 130, (T, (K + 31) // 32), generator=g, device="cuda", dtype=torch.uint8)
+        x = isc.Mx8(q.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu))
+        v = x.q.double() * torch.exp2(scales.double() - 127).repeat_interleave(32, 1)[:, :K]
+    else:
+        x = torch.randn((T, K), generator=g, device="cuda").to(getattr(torch, xtype))
+        v = x.double()
+    wd = torch.from_numpy(w[0].T.copy()).cuda()
+    got = isc.isc_w4_linear(x, w4, dtype=torch.float32).double()
+    assert ((got - v @ wd).abs() <= (K + 64) * E24 * (v.abs() @ wd.abs()) + E24 * got.abs()).all()
+
+
 # the same for the skipping product: one, two and four tests a turn, one range and many
 @pytest.mark.parametrize("T,N,K", [(1, 40, 9000), (1, 8200, 33000), (3, 2000, 20000), (12, 4200, 5000), (40, 600, 3000),
                                    (700, 40, 700)])
