@@ -622,6 +622,7 @@ struct Shape {
 constexpr Shape kShapes[] = {{1, 1, 2, 95, 0},  {1, 2, 2, 123, 0}, {2, 2, 2, 140, 0},   {3, 2, 2, 160, 0},
                              {4, 2, 2, 186, 0}, {3, 3, 2, 190, 0}, {4, 3, 2, 207, 0},   {4, 4, 2, 235, 0},
                              {3, 3, 1, 245, 150}, {4, 3, 1, 285, 180}, {4, 4, 1, 360, 200}};
+constexpr int64_t kGridRows = 65535;  // a launch's limit; four tiles of columns stay under it
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 int64_t time_of(const Shape &h, int64_t workgroups) {
@@ -652,6 +653,7 @@ hipError_t packed(const W4Args &a, hipStream_t s) {
     int64_t least = INT64_MAX;
     for (int i = 0; i < kShapeCount; ++i) {
         const Shape &h = kShapes[i];
+        if ((tiles + h.mt - 1) / h.mt > kGridRows) continue;  // (a million fp32 tokens by three tiles)
         const int64_t time = time_of(h, ((a.w.tiles() + h.nt - 1) / h.nt) * ((tiles + h.mt - 1) / h.mt));
         if (time < least) least = time, best = i;
     }

@@ -684,6 +684,18 @@ def test_skip_scales(torch, isc, T, K, N):
     assert np.array_equal(np.isnan(host(isc.isc_w4_skip(xd, pack(scales), dtype=torch.float32))), meets)
 
 
+@pytest.mark.parametrize("N", [16, 48])
+def test_linear_a_million_tokens(torch, isc, N):
+    """The largest count of tokens, in fp32 the most columns: every one, against a product in 64 bits."""
+    note("linear a million tokens", N)
+    T, K = 2 ** 20, 8
+    w4, w = weights(torch, isc, np.random.default_rng(N), 1, N, K, "tiles")
+    x = torch.randn((T, K), generator=torch.Generator(device="cuda").manual_seed(N), device="cuda")
+    v, wd = x.double(), torch.from_numpy(w[0].T.copy()).cuda()
+    got = isc.isc_w4_linear(x, w4).double()
+    assert ((got - v @ wd).abs() <= (K + 64) * E24 * (v.abs() @ wd.abs()) + E24 * got.abs()).all()
+
+
 @pytest.mark.parametrize("xtype,T,K", [("float32", 20003, 2500), ("float16", 20003, 4090), ("bfloat16", 20003, 8190), ("mx8", 20003, 8190)])
 def test_linear_laid_out_in_turns(torch, isc, xtype, T, K):
     """More of x than the workgroups that lay it out hold at a time: every token, against a product in 64 bits."""
