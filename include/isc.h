@@ -506,7 +506,8 @@ int isc_route_workspace_size(int32_t T, int32_t E, size_t *bytes);
  *     ones (at most 64), of which the keep_groups with the largest sums of
  *     their two largest s + bias stay in the choice.
  *   The k experts with the largest s + bias are chosen, in that order, ties to
- *   the lowest index, among groups too.  An expert whose logit or s + bias is
+ *   the lowest index, among groups too.  Scores and keys are fp32, down to
+ *   2^-149; without a bias the logits themselves say the order within groups.  An expert whose logit or s + bias is
  *   -inf or NaN is never chosen; a token with fewer than k others has id -1
  *   and weight 0 in its last slots.
  *   ids, weights: T x k; weights = scale * s, divided by (the chosen s's sum +

@@ -47,28 +47,33 @@ __device__ __forceinline__ float sum_of(float v) {
     return LANES == 16 ? row_sum(v) : wave_sum(v);
 }
 
-// e^x for x <= 88, 0 below the smallest normal number: the exponent's product
-// with log2 e in two parts, so the error stays near one unit in the last place.
+// e^x for x <= 0, down to the smallest fp32 number: e^x = 2^n 2^f with n the nearest
+// whole number to x log2 e and |f| <= 1/2, the product with log2 e in two parts, so the
+// error stays near one unit in the last place; 2^n goes on last, since the instruction
+// has no results below 2^-126.
 // (A third of the instructions of the library's: a kernel that routes a few
 // tokens waits for its own code to arrive more than for anything else.)
 __device__ __forceinline__ float exponential(float x) {
-    const float t = x * 0x1.715476p+0f;
-    const float rest = fmaf(x, 0x1.4ae0cp-26f, fmaf(x, 0x1.715476p+0f, -t));
-    const float e = __builtin_amdgcn_exp2f(t);
-    return x < -87.0f ? 0.0f : fmaf(e, rest * 0x1.62e43p-1f, e);
+    x = __builtin_amdgcn_fmed3f(x, -104.0f, 0.0f);  // (0 from there down)
+    const float n = __builtin_rintf(x * 0x1.715476p+0f);
+    const float f = fmaf(x, 0x1.4ae0cp-26f, fmaf(x, 0x1.715476p+0f, -n));
+    return __builtin_ldexpf(__builtin_amdgcn_exp2f(f), static_cast<int>(n));
 }
 
 // A token's scores from its logits, expert i * LANES + lane in place i, written
 // over them; -1 for a logit that is not above -inf.  A logit of +inf stands for
-// all others' limit: it shares the softmax with its equals.
+// all others' limit: it shares the softmax with its equals.  Returns the softmax's
+// largest logit.
 template <int C, int LANES>
-__device__ __forceinline__ void scores(float (&s)[C], int sigmoid) {
+__device__ __forceinline__ float scores(float (&s)[C], int sigmoid) {
     if (sigmoid) {
-        // below -88 the score itself is below the smallest normal number
+        // from e^-|l| <= 1, which has a value wherever the score has one
 #pragma unroll
-        for (int i = 0; i < C; ++i)
-            s[i] = s[i] > -88.0f ? __builtin_amdgcn_rcpf(1.0f + exponential(-s[i])) : s[i] > -__builtin_inff() ? 0.0f : -1.0f;
-        return;
+        for (int i = 0; i < C; ++i) {
+            const float e = exponential(-fabsf(s[i])), r = __builtin_amdgcn_rcpf(1.0f + e);
+            s[i] = s[i] > -__builtin_inff() ? (s[i] < 0.0f ? e * r : r) : -1.0f;
+        }
+        return 0.0f;
     }
     uint32_t mx = 0;
 #pragma unroll
@@ -87,6 +92,7 @@ __device__ __forceinline__ void scores(float (&s)[C], int sigmoid) {
     const float inv = sum > 0.0f ? 1.0f / sum : 1.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) s[i] = s[i] < 0.0f ? s[i] : s[i] * inv;
+    return m;
 }
 
 // A token's logits, -inf past the last expert.
@@ -127,12 +133,22 @@ __device__ __forceinline__ int route_token(const RouteArgs &a, int64_t t, uint32
     float s[C];
     uint32_t key[C];  // 0: not to be chosen
     load_logits<C, LANES>(s, a.logits, at * a.ld, lane, a.E, a.type);
-    scores<C, LANES>(s, a.sigmoid);
+    // without a bias the logits rank as their scores do, and also where fp32's scores
+    // are equal: near a sigmoid of 1, and below 2^-149
+    if (!a.bias)
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int e = i * LANES + lane;
-        const float v = e < a.E && a.bias ? s[i] + a.bias[e] : s[i];
-        key[i] = s[i] >= 0.0f && v > -__builtin_inff() ? order(v + 0.0f) : 0u;
+        for (int i = 0; i < C; ++i) key[i] = s[i] > -__builtin_inff() ? order(s[i] + 0.0f) : 0u;
+    const float m = scores<C, LANES>(s, a.sigmoid);
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int e = i * LANES + lane;
+            const float v = e < a.E ? s[i] + a.bias[e] : s[i];
+            key[i] = s[i] >= 0.0f && v > -__builtin_inff() ? order(v + 0.0f) : 0u;
+        }
+    } else if (m == __builtin_inff()) {  // beside a logit of +inf the others' scores are 0, all alike
+#pragma unroll
+        for (int i = 0; i < C; ++i) key[i] = s[i] >= 0.0f ? order(s[i]) : 0u;
     }
     if (a.groups > 1) {
         const int size = a.E / a.groups;
@@ -140,7 +156,7 @@ __device__ __forceinline__ int route_token(const RouteArgs &a, int64_t t, uint32
         const uint32_t factor = ((1u << 20) + static_cast<uint32_t>(size) - 1u) / static_cast<uint32_t>(size);
 #pragma unroll
         for (int i = 0; i < C; ++i)
-            if (i * LANES + lane < a.E) row[i * LANES + lane] = key[i];
+            if (i * LANES + lane < a.E) row[i * LANES + lane] = key[i] && !a.bias ? order(s[i]) : key[i];
         wave_fence();
         // a group's two largest keys, by the lanes that share it: a power of two
         const int share = LANES >> (32 - __builtin_clz(a.groups - 1));

@@ -433,6 +433,47 @@ def test_route_types_and_ties(torch, isc, dtype):
         check_route(got, ffn.route(host(logits), 7, None, score, groups, keep), 96)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [9, 40, 5000])
+@pytest.mark.parametrize("E,k,groups,keep,step,bias", [(64, 12, 1, 1, 16.0, False), (200, 30, 1, 1, 16.0, False),
+                                                       (700, 12, 1, 1, 16.0, False), (24, 24, 1, 1, 4.0, True),
+                                                       (24, 12, 4, 2, 4.0, True), (24, 12, 4, 2, 4.0, False)])
+def test_route_logits_far_apart(torch, isc, E, k, groups, keep, step, bias, T, dtype):
+    """Experts whose softmax scores are hundreds of powers of e apart, or below fp32's smallest normal number beside a
+    bias of 0: each still has its place.  Weights err by a few of the smallest fp32 numbers where they are that small."""
+    note("route far apart", E, k, groups, keep, step, bias, T, dtype)
+    r = np.random.default_rng(E + T)
+    l = np.stack([np.minimum(r.permutation(E), 255) * -step for _ in range(T)])  # (as bfloat16 holds them)
+    x = dev(torch, l, dtype)
+    assert np.array_equal(host(x), l)
+    got = isc.isc_route(x, k, bias=torch.zeros(E, device="cuda") if bias else None, groups=groups, keep_groups=keep)
+    if T <= 40:
+        want = ffn.route(l, k, np.zeros(E) if bias else None, groups=groups, keep=keep)
+        for a, b in zip((got.ids, got.offsets, got.order), (want[0], *want[2:])):
+            assert np.array_equal(host(a), b)
+        assert (np.abs(host(got.weights) - want[1]) <= 64 * E24 * want[1] + 2.0 ** -147).all()
+    elif groups == 1:
+        assert np.array_equal(host(got.ids), np.argsort(-l, axis=1, kind="stable")[:, :k])
+    small = isc.isc_route(x[:9], k, bias=torch.zeros(E, device="cuda") if bias else None, groups=groups, keep_groups=keep)
+    assert torch.equal(small.ids, got.ids[:9])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [9, 5000])
+def test_route_sigmoid_far_apart(torch, isc, T, dtype):
+    """Confident experts, whose sigmoids are 1 in fp32, and faint ones, below its smallest normal number."""
+    note("route sigmoid far apart", T, dtype)
+    r, E, k = np.random.default_rng(T), 120, 60
+    l = np.stack([r.permutation(E) - 90.0 for _ in range(T)])
+    got = isc.isc_route(dev(torch, l, dtype), k, score="sigmoid", renorm=False)
+    assert np.array_equal(host(got.ids), np.argsort(-l, axis=1, kind="stable")[:, :k])
+    faint = isc.isc_route(dev(torch, l - 29.0, dtype), k, score="sigmoid", renorm=False)
+    assert np.array_equal(host(faint.ids), host(got.ids))
+    for g, shift in ((got, 0.0), (faint, 29.0)):
+        want = 1 / (1 + np.exp(shift - np.take_along_axis(l, host(got.ids).astype(np.int64), 1)))
+        assert (np.abs(host(g.weights) - want) <= 64 * E24 * want + 2.0 ** -147).all()
+
+
 def test_route_values(torch, isc):
     """NaN and infinite logits, a bias that shuts an expert out, no tokens."""
     note("route values")
