@@ -132,7 +132,11 @@ __device__ __forceinline__ int route_token(const RouteArgs &a, int64_t t, uint32
     const int64_t at = there ? t : a.T - 1;
     float s[C];
     uint32_t key[C];  // 0: not to be chosen
-    load_logits<C, LANES>(s, a.logits, at * a.ld, lane, a.E, a.type);
+    // with sixteen experts a lane the logits' addresses are made again for each token:
+    // kept from one to the next they do not fit the registers
+    int from = lane;
+    if constexpr (LANES * C == kMaxE) asm volatile("" : "+v"(from));
+    load_logits<C, LANES>(s, a.logits, at * a.ld, from, a.E, a.type);
     // without a bias the logits rank as their scores do, and also where fp32's scores
     // are equal: near a sigmoid of 1, and below 2^-149
     if (!a.bias)

@@ -7,7 +7,7 @@ import pytest
 from paper_1704_07724_amd import build
 
 
-@pytest.mark.parametrize("name", ["rmsnorm"])
+@pytest.mark.parametrize("name", ["rmsnorm", "route"])
 def test_no_scratch(name):
     build.generate()
     r = subprocess.run([build.HIPCC, *build.DEVICE_FLAGS, "-Rpass-analysis=kernel-resource-usage", "--cuda-device-only", "-c",
