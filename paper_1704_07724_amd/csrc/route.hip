@@ -60,6 +60,16 @@ __device__ __forceinline__ float exponential(float x) {
     return __builtin_ldexpf(__builtin_amdgcn_exp2f(f), static_cast<int>(n));
 }
 
+// s = 1 / (1 + e^-l) and s (1 - s), both from e^-|l| <= 1: neither comes from a
+// difference, and each has a value wherever fp32 has one.
+struct Sigmoid {
+    float s, slope;
+};
+__device__ __forceinline__ Sigmoid sigmoid_of(float l) {
+    const float e = exponential(-fabsf(l)), r = __builtin_amdgcn_rcpf(1.0f + e);
+    return {l < 0.0f ? e * r : r, e * r * r};
+}
+
 // A token's scores from its logits, expert i * LANES + lane in place i, written
 // over them; -1 for a logit that is not above -inf.  A logit of +inf stands for
 // all others' limit: it shares the softmax with its equals.  Returns the softmax's
@@ -67,12 +77,8 @@ __device__ __forceinline__ float exponential(float x) {
 template <int C, int LANES>
 __device__ __forceinline__ float scores(float (&s)[C], int sigmoid) {
     if (sigmoid) {
-        // from e^-|l| <= 1, which has a value wherever the score has one
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const float e = exponential(-fabsf(s[i])), r = __builtin_amdgcn_rcpf(1.0f + e);
-            s[i] = s[i] > -__builtin_inff() ? (s[i] < 0.0f ? e * r : r) : -1.0f;
-        }
+        for (int i = 0; i < C; ++i) s[i] = s[i] > -__builtin_inff() ? sigmoid_of(s[i]).s : -1.0f;
         return 0.0f;
     }
     uint32_t mx = 0;
@@ -398,9 +404,20 @@ __global__ void __launch_bounds__(256) route_bwd_kernel(RouteBwdArgs a) {
     int id = lane < a.k ? a.ids[t * a.k + lane] : -1;
     if (id >= a.E) id = -1;
     float dw = id >= 0 ? a.dweights[t * a.k + lane] * a.scale : 0.0f;
-    scores<C, 64>(s, a.sigmoid);
+    float slope[C];  // the sigmoid's
+    if (a.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) s[i] = fmaxf(s[i], 0.0f);
+        for (int i = 0; i < C; ++i) {
+            const Sigmoid g = sigmoid_of(s[i]);
+            const bool there = s[i] > -__builtin_inff();
+            s[i] = there ? g.s : 0.0f;
+            slope[i] = there ? g.slope : 0.0f;
+        }
+    } else {
+        scores<C, 64>(s, 0);
+#pragma unroll
+        for (int i = 0; i < C; ++i) s[i] = fmaxf(s[i], 0.0f);
+    }
     float chosen = 0.0f;  // slot `lane`'s score, from the lane that holds it
 #pragma unroll
     for (int i = 0; i < C; ++i) {
@@ -424,7 +441,7 @@ __global__ void __launch_bounds__(256) route_bwd_kernel(RouteBwdArgs a) {
         const int e = i * 64 + lane;
         if (e >= a.E) continue;
         const float d = row[e];
-        const float v = a.sigmoid ? d * s[i] * (1.0f - s[i]) : s[i] * (d - dot);
+        const float v = a.sigmoid ? d * slope[i] : s[i] * (d - dot);
         store_as(a.dlogits, t * a.ldd + e, v, a.type);
     }
 }

@@ -521,6 +521,25 @@ def test_route_bwd(torch, isc, T, E, k, score, renorm, dtype):
     assert np.array_equal(host(s), host(got))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k,renorm", [(1, 40, 40, False), (33, 60, 8, False), (33, 60, 8, True), (9, 300, 20, False)])
+def test_route_bwd_confident(torch, isc, T, E, k, renorm, dtype):
+    """Sigmoids near 1 and near 0: the gradient is to be right beside s (1 - s), not beside s."""
+    note("route bwd confident", T, E, k, renorm, dtype)
+    r = np.random.default_rng(T + E)
+    l = host(dev(torch, r.choice([-1.0, 1.0], (T, E)) * r.uniform(8, 30, (T, E)), dtype))
+    x, dw = dev(torch, l, dtype), dev(torch, r.standard_normal((T, k)))
+    ids = isc.isc_route(x, k, score="sigmoid").ids
+    got = host(isc.isc_route_bwd(dw, x, ids, score="sigmoid", renorm=renorm))
+    s, c, d, i = 1 / (1 + np.exp(-l)), 1 / (1 + np.exp(l)), host(dw), host(ids).astype(np.int64)
+    on = np.take_along_axis(s, i, 1)
+    total = on.sum(1, keepdims=True) + 1e-20
+    ds, size = np.zeros((T, E)), np.zeros((T, E))
+    np.put_along_axis(ds, i, (d - (d * on).sum(1, keepdims=True) / total) / total if renorm else d, 1)
+    np.put_along_axis(size, i, (np.abs(d) + (np.abs(d) * on).sum(1, keepdims=True) / total) / total if renorm else np.abs(d), 1)
+    close(got, ds * s * c, 128 * E24 * size * s * c, dtype, "dlogits")
+
+
 def test_route_bwd_more_tokens_than_a_launch_takes(torch, isc):
     """Tokens on either side of a launch's last one, and the last, as in a small call; none left out."""
     T, E, k = 2 ** 26 + 3, 4, 2
