@@ -42,13 +42,17 @@ __device__ __forceinline__ float block_sum(float v, float *sums) {
 
 // m^(-1/2) to half a unit in the last place and a little: the instruction's
 // value, and a Newton step on its error.  The 8-bit form's values move by whole
-// steps where the last bit does.
+// steps where the last bit does.  The instruction takes what is below 2^-126 for 0, so
+// that is raised by 2^48 first.
 __device__ __forceinline__ float reciprocal_root(float m) {
+    const bool small = m < 0x1p-126f;
+    m *= small ? 0x1p48f : 1.0f;
     const float r = __builtin_amdgcn_rsqf(m);
     const float h = m * r, low = fmaf(m, r, -h);
     const float e = fmaf(-low, r, fmaf(-h, r, 1.0f));
     const float better = fmaf(0.5f * r, e, r);
-    return fabsf(better) < __builtin_inff() ? better : r;  // 0 and infinity have no error to take off
+    // 0 and infinity have no error to take off
+    return (fabsf(better) < __builtin_inff() ? better : r) * (small ? 0x1p24f : 1.0f);
 }
 
 constexpr int kShortRows = 8;  // rows of one wavefront that a workgroup of the gradient takes at once

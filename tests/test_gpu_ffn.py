@@ -170,6 +170,23 @@ def test_norm_values(torch, isc):
     assert (s[4] == 255).all()
 
 
+@pytest.mark.parametrize("D", [40, 1001, 40000])
+def test_norm_small_means(torch, isc, D):
+    """Mean squares that fp32 holds below its smallest normal number, without an eps to hide them: down to
+    2^-140 they have 9 bits and more, so the root errs by 2^-11 of itself at most."""
+    note("norm small means", D)
+    r = np.random.default_rng(D)
+    powers = np.array([-60, -62, -63, -64, -66, -68, -70])
+    h = np.sign(r.standard_normal((len(powers), D))) * 2.0 ** powers[:, None]
+    w = 1 + 0.2 * r.standard_normal(D)
+    n = isc.isc_rmsnorm(dev(torch, h), dev(torch, w), eps=0.0, rstd=True)
+    # each square is exact; a sum's terms below 2^-126 are, too: they are multiples of 2^-140
+    want = 2.0 ** -powers.astype(np.float64)
+    assert (np.abs(host(n.rstd) - want) <= 2.0 ** -11 * want).all()
+    y = h * want[:, None] * host(dev(torch, w))
+    assert (np.abs(host(n.y) - y) <= 2.0 ** -11 * np.abs(y) + 2.0 ** -20).all()
+
+
 def test_norm_no_rows(torch, isc):
     note("norm no rows")
     x, w = torch.empty((0, 64), device="cuda"), torch.ones(64, device="cuda")
