@@ -571,7 +571,8 @@ int isc_w4_linear_workspace_size(const isc_w4_desc *d, int32_t T, int32_t x_type
  * stays), on the matrix cores; weights in the layout ISC_W4_TILES.
  *   x: T x K (T <= 2^20) of any isc_type; x_scales: an ISC_MX8 x's group scales
  *     (row stride ld_scales bytes), else NULL.  fp16 and fp32 inputs enter the
- *     products in full, as sums of bfloat16 values.
+ *     products in full, as sums of bfloat16 values; of fp32 inputs below 2^-110,
+ *     and 8-bit ones under a scale byte below 3, the bits under 2^-133 are lost.
  *   slots: 0 for one matrix (E = 1; ids, offsets, order unused), else the
  *     experts per token: pair p = t*slots + j gets row p of y from expert
  *     ids[p], by isc_route's ids, offsets and order; rows of pairs with an id

@@ -15,7 +15,6 @@ namespace isc {
 struct F32 {
     using type = float;
     static __device__ __forceinline__ float load(const float *p) { return *p; }
-    static __device__ __forceinline__ float round(float v) { return v; }
 };
 struct F16 {
     using type = uint16_t;

@@ -7,7 +7,9 @@
 // 32-bit x is cut into parts of its next 8 significant bits (1 for bfloat16, 2
 // for fp16, 3 for fp32).  Each part is a column of its own: the 16 columns of a
 // matrix instruction hold 16, 8 or 5 tokens, and the parts' sums are added at
-// the end, the small ones first.  Products are then exact and sums are fp32.
+// the end, the small ones first.  Products are then exact and sums are fp32.  (Bits
+// under 2^-133, bfloat16's smallest number, are lost: of fp32 inputs below 2^-110, and
+// of 8-bit inputs under a scale byte below 3.  Weights have none.)
 // (The scaled 8-bit matrix instruction would take both sides as they are
 // stored, but it adds neighbouring products in fewer bits than fp32: 2^-6 next
 // to 2^8 is lost.)

@@ -969,6 +969,48 @@ def test_fp32_inputs_count_in_full(torch, isc):
     assert np.array_equal(isc.isc_w4_linear(x, w).cpu().numpy(), np.repeat(v[:, None], 16, 1))
 
 
+@pytest.mark.parametrize("T", [1, 4, 30])
+def test_small_fp32_inputs(torch, isc, T):
+    """fp32 inputs from 2^-110 on enter with all their bits; below, the parts drop what is under 2^-133 (a
+    bfloat16's last place), of each input less than that."""
+    note("small fp32 inputs", T)
+    r = np.random.default_rng(T)
+    N, K = 40, 300
+    codes = r.integers(0, 256, (1, N, K // 2), dtype=np.uint8)
+    w = ffn.fp4_values(codes, np.full((1, N, (K + 31) // 32), 127, dtype=np.uint8), K)[0]
+    w4 = isc.isc_w4_pack_codes(torch.from_numpy(codes[0]).cuda(),
+                               torch.full((N, (K + 31) // 32), 127, dtype=torch.uint8, device="cuda"), "tiles")
+    for low, lost in ((-110, 0.0), (-126, 2.0 ** -133), (-140, 2.0 ** -133)):
+        x = (1 + r.random((T, K))) * 2.0 ** r.integers(low, low + 6, (T, K)) * r.choice([-1, 1], (T, K))
+        xd = dev(torch, x)
+        want, size = ffn.product(w, host(xd))
+        # and what fp32 sums drop below their own last place
+        bound = (K + 64) * E24 * size + lost * np.abs(w).sum(1)[None] + (K + 64) * 2.0 ** -149
+        got = host(isc.isc_w4_linear(xd, w4, dtype=torch.float32))
+        assert (np.abs(got - want) <= bound).all(), low
+
+
+@pytest.mark.parametrize("T", [1, 4, 30])
+def test_small_group_scales(torch, isc, T):
+    """8-bit inputs under scale bytes from 3 on, weights under any: with all their bits; under 0, 1 and 2 an input's bits
+    below 2^-133 are rounded."""
+    note("small group scales", T)
+    r = np.random.default_rng(T)
+    N, K = 40, 320
+    codes = r.integers(0, 256, (1, N, K // 2), dtype=np.uint8)
+    q = (r.integers(0, 127, (T, K)) | r.integers(0, 2, (T, K)) << 7).astype(np.uint8)
+    for ws, xs, lost in ((127, (3, 12), 0.0), (0, (120, 130), 0.0), (1, (140, 200), 0.0), (150, (3, 30), 0.0), (127, (0, 3), 2.0 ** -134)):
+        scales = r.integers(*xs, (T, K // 32), dtype=np.uint8)
+        w = ffn.fp4_values(codes, np.full((1, N, K // 32), ws, dtype=np.uint8), K)[0]
+        w4 = isc.isc_w4_pack_codes(torch.from_numpy(codes[0]).cuda(),
+                                   torch.full((N, K // 32), ws, dtype=torch.uint8, device="cuda"), "tiles")
+        x = isc.Mx8(torch.from_numpy(q).cuda().view(torch.float8_e4m3fn), torch.from_numpy(scales).cuda().view(torch.float8_e8m0fnu))
+        want, size = ffn.product(w, ffn.mx8_values(q, scales))
+        bound = (K + 64) * E24 * size + lost * np.abs(w).sum(1)[None] + (K + 64) * 2.0 ** -149
+        got = host(isc.isc_w4_linear(x, w4, dtype=torch.float32))
+        assert (np.abs(got - want) <= bound).all(), (ws, xs)
+
+
 # ------------------------------------------------- streams, graphs, offsets --
 
 def block(isc, x, res, nw, router, up, down):
