@@ -439,6 +439,48 @@ def test_route_workgroups(torch, isc, T, E, k, groups):
     assert np.array_equal(host(got.order)[:n], order[:n]) and (host(got.order)[n:] == -1).all()
 
 
+MANY = [
+    # T, E, k, score, bias, groups, keep, renorm: tokens enough for four a wavefront, up to 64, 128 and 256 experts
+    (17, 65, 3, "softmax", True, 1, 1, True),
+    (64, 128, 8, "sigmoid", False, 1, 1, False),
+    (50, 100, 16, "softmax", False, 10, 3, True),
+    (61, 40, 4, "softmax", True, 4, 2, True),
+    (4097, 128, 8, "softmax", False, 1, 1, True),
+    (4099, 256, 8, "sigmoid", True, 8, 4, True),
+    (4100, 129, 5, "softmax", True, 1, 1, False),
+    (4101, 200, 16, "softmax", True, 10, 4, True),
+    (4097, 250, 6, "sigmoid", False, 1, 1, True),
+    (4098, 64, 2, "sigmoid", True, 16, 5, True),
+    (8195, 90, 4, "softmax", False, 1, 1, True),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "-".join(map(str, c)))
+def test_route_many_tokens(torch, isc, case, dtype):
+    """Every token of a call that routes four a wavefront, masked ones among them, in every type."""
+    T, E, k, score, with_bias, groups, keep, renorm = case
+    note("route many tokens", case, dtype)
+    r = np.random.default_rng(T + 3 * E)
+    bias = (r.integers(-60, 61, E) * 0.001).astype(np.float32) if with_bias else None
+    # values that every type holds
+    logits = host(dev(torch, np.round(r.standard_normal((T, E)) * 1.5, 1), "bfloat16"))
+    logits[r.random((T, E)) < 0.1] = -np.inf
+    # tokens whose choice hangs on fp32's rounding of two keys, or of two groups' sums, lose all their experts
+    key = np.stack([ffn.scores(l, score)[0] for l in logits]) + (0.0 if bias is None else bias.astype(np.float64))
+    key[logits == -np.inf] = -9.0
+    best = np.sort(key.reshape(T, groups, -1), -1)[..., -2:].sum(-1)
+    for v in [key] + [best] * (groups > 1):
+        d = np.diff(np.sort(v, -1), axis=-1)
+        logits[((d > 0) & (d < 1e-6)).any(-1)] = -np.inf
+    assert (logits > -np.inf).any(1).mean() > 0.5
+    x = dev(torch, logits, dtype)
+    want = ffn.route(host(x), k, bias, score, groups, keep, renorm, 2.5)
+    got = isc.isc_route(x, k, bias=None if bias is None else dev(torch, bias), score=score, groups=groups, keep_groups=keep,
+                        renorm=renorm, scale=2.5)
+    check_route(got, want, E)
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 def test_route_types_and_ties(torch, isc, dtype):
     """Coarse logits: many exact ties, each to the lowest index."""
