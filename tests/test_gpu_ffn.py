@@ -962,6 +962,41 @@ def test_experts(torch, isc, T, E, k, N, K, empty, xtype):
     close(host(y), (vals * wt[..., None]).sum(1), (K * k + 64) * E24 * (sizes * wt[..., None]).sum(1), "float32", "sum")
 
 
+@pytest.mark.parametrize("xtype", TYPES + ["mx8"])
+@pytest.mark.parametrize("T,E,k,N,K,popular", [(100, 5, 2, 530, 2600, False), (150, 4, 2, 70, 1600, True), (24, 16, 2, 1040, 2600, False),
+                                               (40, 9, 2, 1840, 1100, True), (700, 6, 3, 130, 700, False)])
+def test_experts_many_long_rows(torch, isc, T, E, k, N, K, popular, xtype):
+    """Several tiles of an expert's pairs, each by several steps of every wavefront; half of all pairs with one expert."""
+    note("experts many long rows", T, E, k, N, K, popular, xtype)
+    r = np.random.default_rng(T + N)
+    ids = np.stack([r.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    if popular:
+        ids[:, 0] = 1
+        ids[:, 1] = np.where(r.random(T) < 0.1, -1, np.where(ids[:, 1] == 1, 0, ids[:, 1]))
+    offsets, order = ffn.lists(ids, E)
+    dv = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    route = isc.Route(dv(ids), torch.ones((T, k), device="cuda"), dv(offsets), dv(order))
+    w4, w = weights(torch, isc, r, E, N, K, "tiles", lead=E)
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.routed(w, xv, ids)
+    close(host(isc.isc_w4_linear(xd, w4, route=route, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
+@pytest.mark.parametrize("xtype", TYPES + ["mx8"])
+@pytest.mark.parametrize("T,N,K", [(257, 700, 1500), (1000, 260, 2100), (1003, 2100, 640), (3001, 100, 900)])
+def test_linear_many_tokens(torch, isc, T, N, K, xtype):
+    note("linear many tokens", T, N, K, xtype)
+    r = np.random.default_rng(T + N + K)
+    w4, w = weights(torch, isc, r, 1, N, K, "tiles")
+    x = r.standard_normal((T, K))
+    xd, xv = mx8(torch, isc, x) if xtype == "mx8" else (dev(torch, x, xtype), None)
+    xv = host(xd) if xv is None else xv
+    want, size = ffn.product(w[0], xv)
+    close(host(isc.isc_w4_linear(xd, w4, dtype=torch.float32)), want, (K + 64) * E24 * size, "float32", "y")
+
+
 def test_product_values(torch, isc):
     """NaN scales and inputs that are no numbers: where the 64-bit form has them, and
     a zero of a rectified x reads no weight."""
