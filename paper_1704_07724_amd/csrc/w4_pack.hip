@@ -15,27 +15,29 @@
 namespace isc {
 namespace {
 
-// One thread per group of 32 weights.
+// One thread per group of 32 weights, and the next ones where there are more than a grid's.
+constexpr int64_t kQuantizeBlocks = 1 << 22;
 __global__ void __launch_bounds__(256) w4_quantize_kernel(const void *src, int type, int64_t ld, int64_t rows, int K,
                                                           uint8_t *codes, uint8_t *scales) {
     const int groups = (K + 31) / 32;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (item >= rows * groups) return;
-    const int64_t row = item / groups;
-    const int g = static_cast<int>(item % groups);
-    const int n = K - g * 32 < 32 ? K - g * 32 : 32;
-    uint32_t m = 0;
-    for (int i = 0; i < n; ++i)
-        m = op_max(m, __float_as_uint(load_as(src, row * ld + g * 32 + i, type)) & 0x7fffffffu);
-    const uint32_t b = group_scale<2, 0x400000u>(m);  // 6 = 1.5 * 2^2
-    scales[row * groups + g] = static_cast<uint8_t>(b);
-    const float inv = __uint_as_float((254u - (b > 253u ? 253u : b)) << 23);
-    uint8_t *out = codes + row * ((K + 1) / 2) + g * 16;
-    for (int i = 0; i < n; i += 2) {
-        // a group with a weight that is not finite is NaN by its scale: codes 0
-        const float lo = b == 255u ? 0.0f : load_as(src, row * ld + g * 32 + i, type) * inv;
-        const float hi = b == 255u || i + 1 >= n ? 0.0f : load_as(src, row * ld + g * 32 + i + 1, type) * inv;
-        out[i / 2] = static_cast<uint8_t>(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, lo, hi, 1.0f, 0));
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; item < rows * groups;
+         item += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = item / groups;
+        const int g = static_cast<int>(item % groups);
+        const int n = K - g * 32 < 32 ? K - g * 32 : 32;
+        uint32_t m = 0;
+        for (int i = 0; i < n; ++i)
+            m = op_max(m, __float_as_uint(load_as(src, row * ld + g * 32 + i, type)) & 0x7fffffffu);
+        const uint32_t b = group_scale<2, 0x400000u>(m);  // 6 = 1.5 * 2^2
+        scales[row * groups + g] = static_cast<uint8_t>(b);
+        const float inv = __uint_as_float((254u - (b > 253u ? 253u : b)) << 23);
+        uint8_t *out = codes + row * ((K + 1) / 2) + g * 16;
+        for (int i = 0; i < n; i += 2) {
+            // a group with a weight that is not finite is NaN by its scale: codes 0
+            const float lo = b == 255u ? 0.0f : load_as(src, row * ld + g * 32 + i, type) * inv;
+            const float hi = b == 255u || i + 1 >= n ? 0.0f : load_as(src, row * ld + g * 32 + i + 1, type) * inv;
+            out[i / 2] = static_cast<uint8_t>(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, lo, hi, 1.0f, 0));
+        }
     }
 }
 
@@ -134,8 +136,9 @@ unsigned blocks_for(int64_t items) { return static_cast<unsigned>((items + 255) 
 hipError_t launch_w4_quantize(const W4Shape &w, const void *src, int type, int64_t ld, uint8_t *codes, uint8_t *scales,
                               hipStream_t s) {
     const int64_t rows = static_cast<int64_t>(w.E) * w.N;
-    w4_quantize_kernel<<<dim3(blocks_for(rows * w.groups())), dim3(256), 0, s>>>(src, type, ld, rows, w.K, codes,
-                                                                                scales);
+    const int64_t blocks = (rows * w.groups() + 255) / 256;
+    w4_quantize_kernel<<<dim3(static_cast<unsigned>(blocks < kQuantizeBlocks ? blocks : kQuantizeBlocks)), dim3(256), 0, s>>>(
+        src, type, ld, rows, w.K, codes, scales);
     return hipGetLastError();
 }
 

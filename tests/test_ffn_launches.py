@@ -199,3 +199,13 @@ def test_linear_of_many_tokens_by_experts(launches):
     shapes = [(T, N, K, xt) for T in (1, 2 ** 20) for N, K in ((16, 8), (4096, 4096), (2 ** 20, 32)) for xt in (0, 1, 2, 3)]
     for shape, (status, _, kernels) in zip(shapes, launches([linear(*s, slots=4, E_=1024) for s in shapes])):
         assert status == 0 and launchable(kernels), (shape, kernels)
+
+
+def test_weights_of_any_size(launches):
+    """Quantising and laying out up to the limits on a matrix and on their count."""
+    descs = [[e, n, k, layout] for e in (1, 1024) for n, k in ((1, 1), (2 ** 24, 1), (2 ** 24, 3000), (3000, 2 ** 24), (2 ** 18, 2 ** 17))
+             for layout in (0, 1)]
+    calls = [("isc_w4_quantize", [d, A, 2, d[2], D, F, None]) for d in descs]
+    calls += [("isc_w4_pack_codes", [d, A, D, F, None]) for d in descs]
+    for (name, args), (status, _, kernels) in zip(calls, launches(calls)):
+        assert status == 0 and launchable(kernels), (name, args, kernels)

@@ -677,6 +677,21 @@ def test_quantize(torch, isc, N, K, dtype):
     assert torch.equal(s, codes) and torch.equal(t.view(torch.uint8), scales.view(torch.uint8))
 
 
+def test_quantize_in_turns(torch, isc):
+    """More groups than a grid has threads."""
+    E, N, K = 70, 2 ** 24, 1
+    note("quantize in turns", E, N, K)
+    w = torch.randint(-127, 128, (E, N, K), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda",
+                      dtype=torch.int8).bfloat16()
+    codes, scales = isc.isc_w4_quantize(w)
+    assert w.numel() > 2 ** 30
+    # each of the 255 values by itself, then all of them bit for bit
+    want = [torch.from_numpy(v[:, 0]).cuda() for v in ffn.fp4_quantize(np.arange(-127.0, 128.0)[:, None])]
+    for e in range(E):
+        at = (w[e, :, 0].float() + 127).long()
+        assert torch.equal(codes[e, :, 0], want[0][at]) and torch.equal(scales[e].view(torch.uint8)[:, 0], want[1][at]), e
+
+
 PRODUCTS = [(1, 1, 1), (2, 15, 2), (1, 16, 31), (3, 17, 32), (5, 100, 33), (6, 64, 127), (8, 33, 128), (9, 130, 129),
             (16, 48, 511), (17, 20, 512), (1, 300, 513), (33, 40, 1000), (65, 70, 640), (130, 36, 300), (2, 24, 4500),
             (64, 200, 2050)]
