@@ -424,26 +424,49 @@ __global__ void __launch_bounds__(256) route_bwd_kernel(RouteBwdArgs a) {
         const float v = __shfl(s[i], id & 63);
         if (id >= 0 && id >> 6 == i) chosen = v;
     }
-    float ds = dw;
+    // A slot with more than half of a sum meets mostly its own gradient in it, and the
+    // difference of the two would be lost in their rounding.  But the gradients add up to
+    // a known sum: such a slot's is that less the others'.
+    float ds = dw, dot = 0.0f;
+    unsigned long long most = 0ull;  // the lane of that slot, for the softmax's own sum
     if (a.renorm) {
         const float total = wave_sum(chosen) + 1e-20f;
-        ds = (dw - wave_sum(dw * chosen) / total) / total;
+        const float mean = wave_sum(dw * chosen) / total;
+        ds = (dw - mean) / total;
+        dot = mean * (1e-20f / total);  // the sum of ds s
+        const bool own = chosen > 0.5f * total;
+        if (__ballot(own)) {
+            const float others = wave_sum(own ? 0.0f : ds * chosen);
+            if (own) ds = (dot - others) / chosen;
+        }
+    } else if (!a.sigmoid) {
+        dot = wave_sum(ds * chosen);
+        most = __ballot(chosen > 0.5f);
     }
     if (id < 0) ds = 0.0f;
-    const float dot = a.sigmoid ? 0.0f : wave_sum(ds * chosen);
     __builtin_amdgcn_wave_barrier();
     if (id >= 0) row[id] = ds;  // an expert of its own for every lane
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    float v[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        const int e = i * 64 + lane;
-        if (e >= a.E) continue;
-        const float d = row[e];
-        const float v = a.sigmoid ? d * slope[i] : s[i] * (d - dot);
-        store_as(a.dlogits, t * a.ldd + e, v, a.type);
+        const float d = i * 64 + lane < a.E ? row[i * 64 + lane] : 0.0f;
+        v[i] = a.sigmoid ? d * slope[i] : s[i] * (d - dot);
     }
+    if (most) {
+        const int own = __builtin_amdgcn_readlane(id, __builtin_ctzll(most));
+        float others = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) others += i * 64 + lane == own ? 0.0f : v[i];
+        others = wave_sum(others);
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = i * 64 + lane == own ? -others : v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+        if (i * 64 + lane < a.E) store_as(a.dlogits, t * a.ldd + i * 64 + lane, v[i], a.type);
 }
 
 // Grants a kernel the most dynamic LDS a call can ask for, once.

@@ -599,6 +599,41 @@ def test_route_bwd_confident(torch, isc, T, E, k, renorm, dtype):
     close(got, ds * s * c, 128 * E24 * size * s * c, dtype, "dlogits")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k,score,renorm,bias", [(33, 60, 8, "softmax", False, False), (33, 60, 8, "softmax", True, False),
+                                                     (9, 300, 20, "softmax", False, True), (40, 128, 8, "softmax", True, True),
+                                                     (5, 7, 2, "softmax", False, True), (33, 60, 8, "sigmoid", True, False),
+                                                     (9, 1024, 64, "sigmoid", True, True), (6, 3, 1, "softmax", True, False)])
+def test_route_bwd_dominant(torch, isc, T, E, k, score, renorm, bias, dtype):
+    """One expert with nearly all of a sum, chosen first, later or not at all: its gradient is to be right beside the
+    shares that the others have, since its own part of the sum goes out."""
+    note("route bwd dominant", T, E, k, score, renorm, bias, dtype)
+    r = np.random.default_rng(T + E)
+    l = r.standard_normal((T, E)) - 12 * (score == "sigmoid")
+    l[np.arange(T), r.integers(0, E, T)] += r.uniform(5, 25, T)
+    x, dw = dev(torch, l, dtype), dev(torch, r.standard_normal((T, k)))
+    ids = isc.isc_route(x, k, bias=dev(torch, r.standard_normal(E)) if bias else None, score=score).ids
+    got = host(isc.isc_route_bwd(dw, x, ids, score=score, renorm=renorm))
+    l, i, d = host(x), host(ids).astype(np.int64), host(dw)
+    ds, on = np.zeros((T, E)), np.zeros((T, E))
+    np.put_along_axis(ds, i, d, 1)
+    np.put_along_axis(on, i, 1.0, 1)
+    e = np.exp(l - l.max(1, keepdims=True))
+    full = e / e.sum(1, keepdims=True) if score == "softmax" else 1 / (1 + np.exp(-l))
+    share = full * on / ((full * on).sum(1, keepdims=True) + 1e-20) if renorm else full
+    outer = 1 / (1 + np.exp(l)) if score == "sigmoid" else 1.0  # the sigmoid's 1 - s beside it
+    # an expert's share times the sum over j of share_j (d_i - d_j)
+    pairs = share[:, :, None] * share[:, None, :]
+    want = outer * (pairs * (ds[:, :, None] - ds[:, None, :])).sum(2)
+    size = outer * (pairs * (1 - np.eye(E)) * (np.abs(ds)[:, :, None] + np.abs(ds)[:, None, :])).sum(2)
+    if renorm:  # and what the 1e-20 beside the sum leaves: of each share, and of the softmax's own sum
+        total = (full * on).sum(1, keepdims=True)
+        for v, sign, out in ((ds, 1, want), (np.abs(ds), -1, size)):
+            left = (full * v).sum(1, keepdims=True) * 1e-20 / (total + 1e-20) ** 2
+            out += outer * full * on * left / total - sign * (score == "softmax") * full * left
+    close(got, want, 128 * E24 * size, dtype, "dlogits")
+
+
 def test_route_bwd_more_tokens_than_a_launch_takes(torch, isc):
     """Tokens on either side of a launch's last one, and the last, as in a small call; none left out."""
     T, E, k = 2 ** 26 + 3, 4, 2
