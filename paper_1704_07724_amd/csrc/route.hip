@@ -13,8 +13,8 @@
 // as unsigned integers in the floats' order, the experts of a lane LANES apart;
 // a slot is a maximum and then a minimum of the indices that have it, by
 // data-parallel moves.  A token's slots wait for each other, and that bounds all
-// but the largest calls: 16 tokens of 256 experts in groups take 9.0 us, 4096
-// tokens 14.0, 8192 of 128 experts with their lists 11.4, where moving the 3 MB
+// but the largest calls: 16 tokens of 256 experts in groups take 9.1 us, 4096
+// tokens 14.0, 8192 of 128 experts with their lists 11.6, where moving the 3 MB
 // would take one; 16384 of 256 in groups, where the instructions count, 24.9.
 //
 // The experts' lists.  A token meets an expert at most once, so 64 tokens and
