@@ -607,6 +607,90 @@ int isc_w4_skip(const isc_w4_desc *d, const void *packed, int32_t T, const void 
                 int32_t slots, const int32_t *ids, const float *weights, void *y, int32_t y_type, int64_t ldy, void *ws,
                 size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Training of a routed feed-forward block, and serving it on weights that are
+ * not quantised: the experts' products in 16 or 32 bits, their gradients, and
+ * orthogonalised updates.  The conventions of the section above hold. */
+
+/* E matrices of weights, N outputs x K inputs each, and how a product uses
+ * them.  Row n of expert e begins (e * N + n) * ldw elements after w. */
+typedef struct isc_expert_desc {
+    int32_t E, N, K; /* E <= 1024, N and K <= 2^20 */
+    int32_t type;    /* of x, w and their gradients: ISC_F32, ISC_F16 or ISC_BF16 */
+    int32_t slots;   /* experts of a token, at most 64 */
+    int32_t shared;  /* nonzero: x has a row for each token, T x K; else one for each
+                        pair p = t*slots + j, T*slots x K */
+} isc_expert_desc;
+
+/* Bytes of workspace of isc_expert_linear.  Host-only.
+ * Errors: NULL, SHAPE, LIMIT, ARG. */
+int isc_expert_linear_workspace_size(const isc_expert_desc *d, int32_t T, int32_t combine, size_t *bytes);
+
+/* The products of tokens with their experts' matrices: with e = ids[p],
+ *   v[p][n] = sum over k of w[e][n][k] * x[.][k], with max(0, .) if relu (a NaN stays)
+ *   combine 0: y is T*slots x N, y[p] = v[p], 0 for a pair without an expert
+ *   combine 1: y is T x N, y[t] = sum over j of weights[p] * v[p] (relu has to be 0),
+ *     in the slots' order; a pair without an expert adds nothing.
+ *   ids, weights, offsets, order: isc_route's, T <= 2^20 tokens (weights may be
+ *     NULL unless combine); an id outside [0, E) is an empty slot.
+ *   y_type: ISC_F32, ISC_F16 or ISC_BF16.
+ *   ws: isc_expert_linear_workspace_size bytes, 256-byte aligned.
+ * fp32 operands are cut into three bfloat16 parts each, six of whose nine products
+ * are kept: fp32's precision for magnitudes from 2^-110 on (bits below 2^-133 are
+ * lost); an input that is not finite makes the sums that it enters not finite
+ * (NaN where fp32 may have an infinity).
+ * Deterministic.  Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_expert_linear(const isc_expert_desc *d, const void *w, int64_t ldw, int32_t T, const void *x, int64_t ldx,
+                      const int32_t *ids, const float *weights, const int32_t *offsets, const int32_t *order, void *y,
+                      int32_t y_type, int64_t ldy, int32_t relu, int32_t combine, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* Bytes of workspace of isc_expert_linear_bwd; relu: whether it gets y.  Host-only.
+ * Errors: NULL, SHAPE, LIMIT, ARG. */
+int isc_expert_linear_bwd_workspace_size(const isc_expert_desc *d, int32_t T, int32_t relu, int32_t combine,
+                                         size_t *bytes);
+
+/* The gradients of isc_expert_linear.
+ *   dy: y's gradient, T*slots x N, or T x N with combine, of d->type.
+ *   y: with relu, the rectified output in d->type (T*slots x N): where it is 0 or
+ *     below, nothing goes back.  NULL without relu.
+ *   dx: of x's shape, d->type, fully written: with d[p] the gradient of v[p],
+ *     w[e]^T d[p] times the pair's weight (combine), summed over a token's pairs if
+ *     x is shared; 0 for a pair, or a token, without an expert.
+ *   dw: E x N x K consecutive values of d->type, fully written: the sum over an
+ *     expert's pairs of d[p] x[p]^T times the pair's weight, 0 for an expert without
+ *     pairs.  With combine a weight times dy is rounded to d->type before it is summed.
+ *   dweights: T*slots floats with combine: v[p] . dy[t], 0 in empty slots.
+ *   dx, dw, dweights: NULL where not wanted, one at least given (dweights only with
+ *     combine).  ws: isc_expert_linear_bwd_workspace_size bytes, 256-byte aligned.
+ * Deterministic.  Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_expert_linear_bwd(const isc_expert_desc *d, const void *w, int64_t ldw, int32_t T, const void *x, int64_t ldx,
+                          const void *dy, int64_t lddy, const void *y, int64_t ldy, const int32_t *ids,
+                          const float *weights, const int32_t *offsets, const int32_t *order, int32_t combine, void *dx,
+                          int64_t lddx, void *dw, float *dweights, void *ws, size_t ws_bytes, void *stream);
+
+/* Bytes of workspace of isc_orthogonalize.  Host-only.  Errors: NULL, SHAPE, LIMIT. */
+int isc_orthogonalize_workspace_size(int32_t B, int32_t M, int32_t N, size_t *bytes);
+
+/* Orthogonalises B matrices of M x N: X = G / (|G| + eps), |G| the square root of
+ * the sum of G's squares, then for each of `steps` steps, with its a, b and c,
+ *   X <- a X + (b A + c A A) X,  A = X X^T     (M <= N)
+ *   X <- a X + X (b A + c A A),  A = X^T X     (M > N)
+ *   g: B*M rows of N values of `type`, ldg elements apart; M and N <= 65536.
+ *   coefficients: host array of 3 * steps floats, 1 to 64 steps.  They have to keep
+ *     singular values from [0, 1] within [0, 16] in magnitude after every step (else ARG).
+ *   o: B*M rows of N values of o_type (ISC_F16 or ISC_BF16), ldo elements apart.
+ *   ws: isc_orthogonalize_workspace_size bytes, 256-byte aligned.
+ * The state X and all sums are fp32; the products' operands X, A and b A + c A A are
+ * fp16, so o is within about 2e-3 of the exact result in the 2-norm, relative to it,
+ * before its own rounding.  A matrix with a value that is not finite becomes NaN, one
+ * of zeros stays (with eps > 0); others of the stack are not affected.
+ * Three launches a step and two before.  Deterministic.
+ * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
+int isc_orthogonalize(int32_t B, int32_t M, int32_t N, int32_t type, const void *g, int64_t ldg, int32_t steps,
+                      const float *coefficients, float eps, void *o, int32_t o_type, int64_t ldo, void *ws,
+                      size_t ws_bytes, void *stream);
+
 /* Short text for a status code (static storage). */
 const char *isc_status_str(int status);
 

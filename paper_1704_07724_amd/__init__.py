@@ -16,7 +16,8 @@ The functions carry the C names:
     isc_im2col, isc_gemm_f32, isc_status_str, isc_version
 and, for a rectified feed-forward block (ffn.py, imported here):
     isc_rmsnorm, isc_rmsnorm_bwd, isc_route, isc_route_bwd,
-    isc_w4_quantize, isc_w4_pack_codes, isc_w4_linear, isc_w4_skip
+    isc_w4_quantize, isc_w4_pack_codes, isc_w4_linear, isc_w4_skip,
+    isc_expert_linear, isc_expert_linear_bwd, isc_orthogonalize
 
 Defaults a user may set in the environment (read here, by the binding, at
 each call; the C library reads no environment): ISC_PATH = auto | sparse |
@@ -616,5 +617,6 @@ def _gemm(torch, a, b, out, stream):
 
 
 from . import ffn  # noqa: E402  (its functions use the helpers above)
-from .ffn import (Mx8, Norm, Route, W4, W4Desc, isc_rmsnorm, isc_rmsnorm_bwd, isc_route,  # noqa: E402,F401
-                  isc_route_bwd, isc_w4_linear, isc_w4_pack_codes, isc_w4_quantize, isc_w4_skip)
+from .ffn import (ExpertDesc, ExpertGrads, Mx8, Norm, Route, W4, W4Desc, isc_expert_linear,  # noqa: E402,F401
+                  isc_expert_linear_bwd, isc_orthogonalize, isc_rmsnorm, isc_rmsnorm_bwd, isc_route, isc_route_bwd,
+                  isc_w4_linear, isc_w4_pack_codes, isc_w4_quantize, isc_w4_skip)

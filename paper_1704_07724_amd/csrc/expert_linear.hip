@@ -1,0 +1,187 @@
+// Products of tokens with the matrices of the experts that a router gave them,
+// on weights in 16 or 32 bits (isc_expert_linear), and the launches that they
+// share with their gradients (expert_grad.hip).
+//
+// y[p] = w[e] x[p] for every pair p = (token, slot) of expert e: a matrix product
+// for each expert, whose rows are as many as the router gave it.  The first
+// launch cuts each expert's pairs into tiles of rows and lists them, the second
+// takes a workgroup for every tile of rows by a tile of outputs (tile_product.hpp).
+// A sum over a token's slots is a third launch over the pairs' fp32 results, in
+// the slots' order: added up by atomics its order would change from run to run.
+#include "expert.hpp"
+
+namespace isc {
+namespace {
+
+constexpr int kPlanThreads = 256;
+
+// Workgroup 0 lists the tiles; the others make the lists by place, and zero the
+// rows of pairs that have no expert.
+__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const ExpertArgs a, int rows, void *empty,
+                                                                   int64_t ld, int bytes) {
+    const int tid = threadIdx.x;
+    const int P = a.T * a.slots;
+    if (blockIdx.x == 0) {
+        __shared__ int32_t sums[kPlanThreads];
+        constexpr int kEach = 4;  // experts of a thread: at most 1024 in all
+        int32_t from[kEach], count[kEach], mine = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int e = kEach * tid + i;
+            from[i] = count[i] = 0;
+            if (e < a.E) {
+                const int lo = a.offsets[e], hi = a.offsets[e + 1];
+                from[i] = lo < 0 ? 0 : lo > P ? P : lo;
+                const int end = hi > P ? P : hi;
+                count[i] = end > from[i] ? end - from[i] : 0;
+            }
+            mine += (count[i] + rows - 1) / rows;
+        }
+        sums[tid] = mine;
+        __syncthreads();
+        for (int d = 1; d < kPlanThreads; d *= 2) {
+            const int32_t other = tid >= d ? sums[tid - d] : 0;
+            __syncthreads();
+            sums[tid] += other;
+            __syncthreads();
+        }
+        // lists that overlap could ask for more tiles than a route can have
+        const int most = P / rows + (P < a.E ? P : a.E);
+        int at = sums[tid] - mine;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            for (int r = 0; r < count[i] && at < most; r += rows, ++at)
+                reinterpret_cast<int4 *>(a.plan.tiles)[1 + at] =
+                    make_int4(kEach * tid + i, from[i] + r, count[i] - r < rows ? count[i] - r : rows, 0);
+        if (tid == kPlanThreads - 1) a.plan.tiles[0] = sums[tid] < most ? sums[tid] : most;
+        return;
+    }
+    const int i = (blockIdx.x - 1) * kPlanThreads + tid;
+    bool none = false;
+    if (i < P) {
+        const int p = a.order[i];
+        const bool there = p >= 0 && p < P;
+        a.plan.pairs[i] = there ? p : -1;
+        a.plan.tokens[i] = there ? p / a.slots : -1;
+        none = empty && static_cast<unsigned>(a.ids[i]) >= static_cast<unsigned>(a.E);
+    }
+    uint64_t mask = __ballot(none);
+    const int lane = tid & 63;
+    while (mask) {
+        const int64_t p = i - lane + __ffsll(static_cast<unsigned long long>(mask)) - 1;
+        mask &= mask - 1;
+        char *row = static_cast<char *>(empty) + p * ld;
+        for (int b = lane * 16; b < bytes; b += 1024) {
+            if (b + 16 <= bytes)
+                store_any(row + b, make_uint4(0, 0, 0, 0));
+            else
+                for (int c = b; c < bytes; c += 2) store_any(row + c, static_cast<uint16_t>(0));
+        }
+    }
+}
+
+// Four columns of a token a thread; loads of two slots in flight.
+template <class T>
+__global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, const float *part, int cols, int64_t ld,
+                                                         const float *weights, typename T::type *out, int64_t ldo) {
+    const int quads = (cols + 3) / 4;
+    const int64_t all = static_cast<int64_t>(a.T) * quads, hop = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += hop) {
+        const int64_t t = i / quads;
+        const int c = static_cast<int>(i - t * quads) * 4;
+        float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll 2
+        for (int j = 0; j < a.slots; ++j) {
+            const int64_t p = t * a.slots + j;
+            if (static_cast<unsigned>(a.ids[p]) >= static_cast<unsigned>(a.E)) continue;
+            const float w = weights ? weights[p] : 1.0f;
+            const float4 v = *reinterpret_cast<const float4 *>(part + p * ld + c);
+            sum.x = fmaf(w, v.x, sum.x);
+            sum.y = fmaf(w, v.y, sum.y);
+            sum.z = fmaf(w, v.z, sum.z);
+            sum.w = fmaf(w, v.w, sum.w);
+        }
+        typename T::type *to = out + t * ldo + c;
+        store<T>(to, sum.x);
+        if (c + 1 < cols) store<T>(to + 1, sum.y);
+        if (c + 2 < cols) store<T>(to + 2, sum.z);
+        if (c + 3 < cols) store<T>(to + 3, sum.w);
+    }
+}
+
+}  // namespace
+
+int expert_tile_rows(int64_t pairs, int E, int type) {
+    const int64_t of_one = pairs / (pairs < E ? pairs > 0 ? pairs : 1 : E);  // on average, of experts that can have any
+    if (type == ISC_F32) return of_one <= 64 ? 64 : 128;
+    return of_one <= 32 ? 32 : 128;
+}
+
+bool expert_launches_fit(int64_t pairs, int E, int N, int K, int type) {
+    const int64_t tiles = pairs / expert_tile_rows(pairs, E, type) + (pairs < E ? pairs : E);
+    const int64_t across = ((N > K ? N : K) + 127) / 128;
+    return tiles * across * 256 <= kLaunchThreads &&
+           ((N + 127) / 128) * static_cast<int64_t>((K + 127) / 128) * E * 256 <= kLaunchThreads;
+}
+
+size_t expert_plan_bytes(int64_t pairs, int E, int type) {
+    const int64_t tiles = pairs / expert_tile_rows(pairs, E, type) + (pairs < E ? pairs : E);
+    return static_cast<size_t>((16 * (1 + tiles) + 255) / 256 * 256 + (8 * pairs + 255) / 256 * 256);
+}
+
+ExpertPlan expert_plan_at(void *ws, int64_t pairs, int E, int type) {
+    const int64_t tiles = pairs / expert_tile_rows(pairs, E, type) + (pairs < E ? pairs : E);
+    ExpertPlan p;
+    p.tiles = static_cast<int32_t *>(ws);
+    p.pairs = past(p.tiles, (16 * (1 + tiles) + 255) / 256 * 256);
+    p.tokens = past(p.pairs, 4 * pairs);
+    return p;
+}
+
+hipError_t launch_expert_plan(const ExpertArgs &a, void *empty, int64_t ld, int cols, int size, hipStream_t s) {
+    const int64_t blocks = 1 + (a.pairs() + kPlanThreads - 1) / kPlanThreads;
+    hipLaunchKernelGGL(expert_plan_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kPlanThreads), 0, s, a,
+                       expert_tile_rows(a.pairs(), a.E, a.type), empty, ld * size, cols * size);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, const float *weights, void *out,
+                             int64_t ldo, int type, hipStream_t s) {
+    const int64_t all = static_cast<int64_t>(a.T) * ((cols + 3) / 4), blocks = (all + 255) / 256;
+    const dim3 grid(static_cast<unsigned>(blocks < 8192 ? blocks : 8192));
+    const int64_t ld = expert_ld(cols);
+    if (type == ISC_F32)
+        hipLaunchKernelGGL(expert_sum_kernel<F32>, grid, dim3(256), 0, s, a, part, cols, ld, weights,
+                           static_cast<float *>(out), ldo);
+    else if (type == ISC_BF16)
+        hipLaunchKernelGGL(expert_sum_kernel<BF16>, grid, dim3(256), 0, s, a, part, cols, ld, weights,
+                           static_cast<uint16_t *>(out), ldo);
+    else
+        hipLaunchKernelGGL(expert_sum_kernel<F16>, grid, dim3(256), 0, s, a, part, cols, ld, weights,
+                           static_cast<uint16_t *>(out), ldo);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_linear(const ExpertLinearArgs &l, hipStream_t s) {
+    const ExpertArgs &a = l.a;
+    const int size = a.type == ISC_F32 ? 4 : 2, ysize = l.ytype == ISC_F32 ? 4 : 2;
+    if (hipError_t e = launch_expert_plan(a, l.combine ? nullptr : l.y, l.ldy, a.N, ysize, s); e != hipSuccess) return e;
+    tp::RowsArgs r{};
+    r.plan = a.plan;
+    r.x = {static_cast<const char *>(a.x), a.ldx * size, a.shared ? a.plan.tokens : a.plan.pairs, 0, a.K};
+    r.w = {static_cast<const char *>(a.w), a.ldw * size, nullptr, a.N, a.K};
+    r.expert = a.N * a.ldw * size;
+    r.listed = 1;
+    r.inner = a.K;
+    r.cols = a.N;
+    r.out = l.combine ? l.part : l.y;
+    r.ldo = l.combine ? expert_ld(a.N) : l.ldy;
+    r.otype = l.combine ? ISC_F32 : l.ytype;
+    r.relu = l.relu;
+    const bool direct = tp::direct_rows(a.x, a.ldx, a.K, size) && tp::direct_rows(a.w, a.ldw, a.K, size);
+    if (hipError_t e = tp::launch_rows_by<tp::kAlong>(r, a.type, direct, a.pairs(), a.E, s); e != hipSuccess) return e;
+    if (!l.combine) return hipSuccess;
+    return launch_expert_sum(a, l.part, a.N, a.weights, l.y, l.ldy, l.ytype, s);
+}
+
+}  // namespace isc

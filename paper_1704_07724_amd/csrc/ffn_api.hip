@@ -1,7 +1,9 @@
 // C ABI of the feed-forward operators (include/isc.h): argument validation on
 // the host, then the launches.
-#include "ffn.hpp"
+#include "expert.hpp"
+#include "orthogonalize.hpp"
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <limits>
@@ -49,6 +51,40 @@ int check_w4(const isc_w4_desc *d, isc::W4Shape *w) {
         return ISC_ERR_LIMIT;
     *w = isc::W4Shape{d->E, d->N, d->K};
     return ISC_OK;
+}
+
+// The largest N and K of the experts' matrices, whose rows' bytes stay in 32 bits.
+constexpr int32_t kMaxWidth = 1 << 20;
+
+// A call on experts: what holds for it whatever it computes.
+int check_expert(const isc_expert_desc *d, int32_t T) {
+    if (!d) return ISC_ERR_NULL;
+    if (d->E < 1 || d->N < 1 || d->K < 1 || d->slots < 1 || T < 0) return ISC_ERR_SHAPE;
+    if (!element_type(d->type)) return ISC_ERR_ARG;
+    if (d->E > kMaxExperts || d->slots > kMaxSlots || d->N > kMaxWidth || d->K > kMaxWidth || T > kMaxTokens)
+        return ISC_ERR_LIMIT;
+    return isc::expert_launches_fit(static_cast<int64_t>(T) * d->slots, d->E, d->N, d->K, d->type) ? ISC_OK
+                                                                                                  : ISC_ERR_LIMIT;
+}
+
+// The largest magnitude of a s + b s^3 + c s^5 over [0, r]: at an end, or where the
+// slope a + 3 b s^2 + 5 c s^4 is 0.
+double most_of(double a, double b, double c, double r) {
+    const auto at = [=](double s) { return std::fabs(s * (a + s * s * (b + c * s * s))); };
+    double most = at(r);
+    const auto look = [&](double square) {
+        if (square > 0.0 && square < r * r) most = std::max(most, at(std::sqrt(square)));
+    };
+    if (c != 0.0) {
+        const double d = 9.0 * b * b - 20.0 * a * c;
+        if (d >= 0.0) {
+            look((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+            look((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+        }
+    } else if (b != 0.0) {
+        look(-a / (3.0 * b));
+    }
+    return most;
 }
 
 Span flat(const void *p, int64_t n, size_t size) { return Span{p, 1, n, n, size}; }
@@ -331,6 +367,157 @@ int isc_w4_skip(const isc_w4_desc *d, const void *packed, int32_t T, const void 
     a.y = y, a.ldy = ldy, a.ytype = y_type;
     a.part = static_cast<float *>(ws);
     return hip_status(isc::launch_w4_skip(a, static_cast<hipStream_t>(stream)));
+}
+
+int isc_expert_linear_workspace_size(const isc_expert_desc *d, int32_t T, int32_t combine, size_t *bytes) {
+    if (!bytes) return ISC_ERR_NULL;
+    if (const int st = check_expert(d, T)) return st;
+    const int64_t pairs = static_cast<int64_t>(T) * d->slots;
+    *bytes = isc::expert_plan_bytes(pairs, d->E, d->type) +
+             (combine ? sizeof(float) * static_cast<size_t>(pairs * isc::expert_ld(d->N)) : 0);
+    return ISC_OK;
+}
+
+int isc_expert_linear(const isc_expert_desc *d, const void *w, int64_t ldw, int32_t T, const void *x, int64_t ldx,
+                      const int32_t *ids, const float *weights, const int32_t *offsets, const int32_t *order, void *y,
+                      int32_t y_type, int64_t ldy, int32_t relu, int32_t combine, void *ws, size_t ws_bytes,
+                      void *stream) {
+    size_t need = 0;
+    if (const int st = isc_expert_linear_workspace_size(d, T, combine, &need)) return st;
+    if (!element_type(y_type) || (relu && combine)) return ISC_ERR_ARG;
+    if (T == 0) return ISC_OK;
+    if (!w || !x || !ids || !offsets || !order || !y || !ws || (combine && !weights)) return ISC_ERR_NULL;
+    const size_t b = type_bytes(d->type), yb = type_bytes(y_type);
+    const int64_t pairs = static_cast<int64_t>(T) * d->slots;
+    const Span in[6] = {{x, d->shared ? T : pairs, d->K, ldx, b}, {w, static_cast<int64_t>(d->E) * d->N, d->K, ldw, b},
+                        flat(ids, pairs, 4), flat(combine ? weights : nullptr, pairs, 4), flat(offsets, d->E + 1, 4),
+                        flat(order, pairs, 4)};
+    const Span out[2] = {{y, combine ? T : pairs, d->N, ldy, yb}, flat(ws, static_cast<int64_t>(need), 1)};
+    if (!in[0].shape_ok() || !in[1].shape_ok() || !out[0].shape_ok()) return ISC_ERR_SHAPE;
+    if (!aligned(w, b) || !aligned(x, b) || !aligned(y, yb) || !aligned(ids, 4) || !aligned(in[3].p, 4) ||
+        !aligned(offsets, 4) || !aligned(order, 4) || !aligned(ws, kAlign))
+        return ISC_ERR_ALIGN;
+    if (ws_bytes < need) return ISC_ERR_WORKSPACE;
+    for (const Span &o : out)
+        for (const Span &s : in)
+            if (overlap(o, s)) return ISC_ERR_ALIAS;
+    if (overlap(out[0], out[1])) return ISC_ERR_ALIAS;
+    if (const int st = isc::require_gfx950()) return st;
+    isc::ExpertLinearArgs a{};
+    a.a = {T, d->E, d->N, d->K, d->slots, d->type, d->shared != 0, x, w, ldx, ldw, ids, offsets, order, weights,
+           isc::expert_plan_at(ws, pairs, d->E, d->type)};
+    a.y = y;
+    a.ldy = ldy;
+    a.ytype = y_type;
+    a.relu = relu != 0;
+    a.combine = combine != 0;
+    a.part = static_cast<float *>(isc::past(ws, static_cast<int64_t>(isc::expert_plan_bytes(pairs, d->E, d->type))));
+    return hip_status(isc::launch_expert_linear(a, static_cast<hipStream_t>(stream)));
+}
+
+int isc_expert_linear_bwd_workspace_size(const isc_expert_desc *d, int32_t T, int32_t relu, int32_t combine,
+                                         size_t *bytes) {
+    if (!bytes) return ISC_ERR_NULL;
+    if (const int st = check_expert(d, T)) return st;
+    if (relu && combine) return ISC_ERR_ARG;
+    *bytes = isc::expert_bwd_bytes(T, d->E, d->N, d->K, d->slots, d->type, d->shared != 0, relu != 0, combine != 0).all;
+    return ISC_OK;
+}
+
+int isc_expert_linear_bwd(const isc_expert_desc *d, const void *w, int64_t ldw, int32_t T, const void *x, int64_t ldx,
+                          const void *dy, int64_t lddy, const void *y, int64_t ldy, const int32_t *ids,
+                          const float *weights, const int32_t *offsets, const int32_t *order, int32_t combine, void *dx,
+                          int64_t lddx, void *dw, float *dweights, void *ws, size_t ws_bytes, void *stream) {
+    size_t need = 0;
+    if (const int st = isc_expert_linear_bwd_workspace_size(d, T, y != nullptr, combine, &need)) return st;
+    if (dweights && !combine) return ISC_ERR_ARG;
+    if (!dx && !dw && !dweights) return ISC_ERR_NULL;
+    if (T == 0 && !dw) return ISC_OK;
+    if (T > 0 && (!w || !x || !dy || !ids || !offsets || !order || !ws || (combine && !weights))) return ISC_ERR_NULL;
+    const size_t b = type_bytes(d->type);
+    const int64_t pairs = static_cast<int64_t>(T) * d->slots, xrows = d->shared ? T : pairs;
+    const int64_t weightsn = static_cast<int64_t>(d->E) * d->N;
+    const Span in[8] = {{x, xrows, d->K, ldx, b}, {w, weightsn, d->K, ldw, b}, {dy, combine ? T : pairs, d->N, lddy, b},
+                        {y, pairs, d->N, ldy, b}, flat(ids, pairs, 4), flat(combine ? weights : nullptr, pairs, 4),
+                        flat(offsets, d->E + 1, 4), flat(order, pairs, 4)};
+    const Span out[4] = {{dx, xrows, d->K, lddx, b}, {dw, weightsn, d->K, d->K, b}, flat(dweights, pairs, 4),
+                         flat(ws, static_cast<int64_t>(need), 1)};
+    for (int i = 0; i < 4; ++i)
+        if (T > 0 && !in[i].shape_ok()) return ISC_ERR_SHAPE;
+    if (T > 0 && !out[0].shape_ok()) return ISC_ERR_SHAPE;
+    if (!aligned(w, b) || !aligned(x, b) || !aligned(dy, b) || !aligned(y, b) || !aligned(dx, b) || !aligned(dw, b) ||
+        !aligned(ids, 4) || !aligned(in[5].p, 4) || !aligned(offsets, 4) || !aligned(order, 4) ||
+        !aligned(dweights, 4) || !aligned(ws, kAlign))
+        return ISC_ERR_ALIGN;
+    if (T > 0 && ws_bytes < need) return ISC_ERR_WORKSPACE;
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; T > 0 && j < 8; ++j)
+            if (overlap(out[i], in[j])) return ISC_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (T > 0 && overlap(out[i], out[j])) return ISC_ERR_ALIAS;
+    }
+    if (const int st = isc::require_gfx950()) return st;
+    const isc::ExpertBwdBytes at =
+        isc::expert_bwd_bytes(T, d->E, d->N, d->K, d->slots, d->type, d->shared != 0, y != nullptr, combine != 0);
+    isc::ExpertBwdArgs a{};
+    a.a = {T, d->E, d->N, d->K, d->slots, d->type, d->shared != 0, x, w, ldx, ldw, ids, offsets, order, weights,
+           isc::expert_plan_at(ws, pairs, d->E, d->type)};
+    a.dy = dy;
+    a.y = y;
+    a.lddy = lddy;
+    a.ldy = ldy;
+    a.combine = combine != 0;
+    a.dx = dx;
+    a.dw = dw;
+    a.dweights = dweights;
+    a.lddx = lddx;
+    a.masked = isc::past(ws, static_cast<int64_t>(at.masked));
+    a.part = static_cast<float *>(isc::past(ws, static_cast<int64_t>(at.part)));
+    a.dots = static_cast<float *>(isc::past(ws, static_cast<int64_t>(at.dots)));
+    return hip_status(isc::launch_expert_bwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int isc_orthogonalize_workspace_size(int32_t B, int32_t M, int32_t N, size_t *bytes) {
+    if (!bytes) return ISC_ERR_NULL;
+    if (B < 0 || M < 1 || N < 1) return ISC_ERR_SHAPE;
+    const isc::OrthShape s{B, M, N};
+    if (B > 65535 || M > 65536 || N > 65536 || !isc::orth_launches_fit(s)) return ISC_ERR_LIMIT;
+    *bytes = static_cast<size_t>(s.bytes());
+    return ISC_OK;
+}
+
+int isc_orthogonalize(int32_t B, int32_t M, int32_t N, int32_t type, const void *g, int64_t ldg, int32_t steps,
+                      const float *coefficients, float eps, void *o, int32_t o_type, int64_t ldo, void *ws,
+                      size_t ws_bytes, void *stream) {
+    size_t need = 0;
+    if (const int st = isc_orthogonalize_workspace_size(B, M, N, &need)) return st;
+    if (!element_type(type) || (o_type != ISC_F16 && o_type != ISC_BF16) || steps < 1 || steps > 64 ||
+        !(eps >= 0.0f) || std::isinf(eps))
+        return ISC_ERR_ARG;
+    if (!coefficients) return ISC_ERR_NULL;
+    double most = 1.0;
+    for (int i = 0; i < steps; ++i) {
+        const double a = coefficients[3 * i], b = coefficients[3 * i + 1], c = coefficients[3 * i + 2];
+        // b A + c A A is an fp16 operand too: 2^6 times it stays below 2^16
+        if (!(std::fabs(b) * most * most + std::fabs(c) * std::pow(most, 4) <= 512.0)) return ISC_ERR_ARG;
+        most = most_of(a, b, c, most);
+        if (!(most <= 16.0)) return ISC_ERR_ARG;
+    }
+    if (B == 0) return ISC_OK;
+    if (!g || !o || !ws) return ISC_ERR_NULL;
+    const int64_t rows = static_cast<int64_t>(B) * M;
+    const Span in{g, rows, N, ldg, type_bytes(type)};
+    const Span out[2] = {{o, rows, N, ldo, 2}, flat(ws, static_cast<int64_t>(need), 1)};
+    if (!in.shape_ok() || !out[0].shape_ok()) return ISC_ERR_SHAPE;
+    if (!aligned(g, type_bytes(type)) || !aligned(o, 2) || !aligned(ws, kAlign)) return ISC_ERR_ALIGN;
+    if (ws_bytes < need) return ISC_ERR_WORKSPACE;
+    // g is read before o is written
+    if ((overlap(out[0], in) && !in_place(out[0], in)) || overlap(out[1], in) || overlap(out[0], out[1]))
+        return ISC_ERR_ALIAS;
+    if (const int st = isc::require_gfx950()) return st;
+    const isc::OrthArgs a{isc::OrthShape{B, M, N}, g, ldg, type, o_type, steps, coefficients, eps, o, ldo,
+                          static_cast<char *>(ws)};
+    return hip_status(isc::launch_orthogonalize(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -55,6 +55,18 @@ class Route(NamedTuple):
     order: object    # [T * k] int32
 
 
+class ExpertDesc(ctypes.Structure):
+    """isc_expert_desc: E matrices of N outputs x K inputs, and a product's rows."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("E", "N", "K", "type", "slots", "shared")]
+
+
+class ExpertGrads(NamedTuple):
+    """isc_expert_linear_bwd's outputs; None for those not asked for."""
+    dx: object        # as x
+    dw: object        # as w
+    dweights: object  # [T, k] float32, of a sum over the slots
+
+
 class W4:
     """Packed 4-bit weights (isc_w4_pack_codes): `desc` and the device buffer;
     `stacked` if they are several matrices, for the experts of a route."""
@@ -81,6 +93,14 @@ def declare(L):
     L.isc_w4_linear.argtypes = [dp, vp, i32, vp, i32, i64, vp, i64, i32, vp, vp, vp, vp, i32, i64, i32, vp, sz, vp]
     L.isc_w4_skip_workspace_size.argtypes = [dp, i32, i32, szp]
     L.isc_w4_skip.argtypes = [dp, vp, i32, vp, i32, i64, i32, vp, vp, vp, i32, i64, vp, sz, vp]
+    ep = ctypes.POINTER(ExpertDesc)
+    L.isc_expert_linear_workspace_size.argtypes = [ep, i32, i32, szp]
+    L.isc_expert_linear.argtypes = [ep, vp, i64, i32, vp, i64, vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, sz, vp]
+    L.isc_expert_linear_bwd_workspace_size.argtypes = [ep, i32, i32, i32, szp]
+    L.isc_expert_linear_bwd.argtypes = [ep, vp, i64, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i32, vp, i64, vp,
+                                        vp, vp, sz, vp]
+    L.isc_orthogonalize_workspace_size.argtypes = [i32, i32, i32, szp]
+    L.isc_orthogonalize.argtypes = [i32, i32, i32, i32, vp, i64, i32, ctypes.POINTER(f32), f32, vp, i32, i64, vp, sz, vp]
 
 
 _state = None
@@ -512,3 +532,160 @@ def isc_w4_skip(st, x, w4, route=None, dtype=None, ws=None, stream=None):
     if status:
         _isc._check(status, "isc_w4_skip")
     return y
+
+
+@functools.lru_cache(maxsize=4096)
+def _expert(query, E, N, K, code, slots, shared, *call):
+    """(the descriptor, its address, bytes of workspace) of a call on experts."""
+    d = ExpertDesc(E, N, K, code, slots, shared)
+    return d, ctypes.byref(d), _size.__wrapped__(query, d, *call)
+
+
+def _experts(st, x, w, route):
+    """The sizes, rows and lists of a call on experts, checked."""
+    ids, weights, offsets, order = route
+    if w.dim() != 3:
+        raise ValueError("w must be [E, N, K], not %r" % (tuple(w.shape),))
+    E, N, K = w.shape
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [T, K] or [T, k, K], not %r" % (tuple(x.shape),))
+    T = x.shape[0]
+    if ids.dim() != 2 or ids.shape[0] != T or (x.dim() == 3 and x.shape[1] != ids.shape[1]):
+        raise ValueError("the route has %r slots, x is %r" % (tuple(ids.shape), tuple(x.shape)))
+    if offsets is None or order is None:
+        raise ValueError("the route has no lists")
+    if w.dtype != x.dtype:
+        raise ValueError("x and w must have one type, not %s and %s" % (x.dtype, w.dtype))
+    slots = ids.shape[1]
+    xr, ldx = _rows(x, K, "x")
+    wr, ldw = _rows(w, K, "w")
+    lists = (_exact(ids, st.i32, (T, slots), "ids"), weights, _exact(offsets, st.i32, (E + 1,), "offsets"),
+             _exact(order, st.i32, (T * slots,), "order"))
+    return T, slots, E, N, K, xr, ldx, wr, ldw, lists
+
+
+@_on_stream
+def isc_expert_linear(st, x, w, route, relu=False, combine=False, dtype=None, ws=None, stream=None):
+    """The products of tokens with their experts' matrices, on weights in 16 or 32 bits.
+
+    x: [T, K], or [T, k, K] with a row for each slot; w: [E, N, K] in x's type
+    (float32, float16, bfloat16); route: isc_route's, with lists.  Returns
+    [T, k, N], slot j by the token's j-th expert (0 where it has none), with
+    max(0, .) if relu; with combine [T, N], the sum over a token's slots under
+    the route's weights.  dtype: the output's (default: x's)."""
+    code = _type(st, x.dtype, "x")
+    T, slots, E, N, K, xr, ldx, wr, ldw, (ids, weights, offsets, order) = _experts(st, x, w, route)
+    device = _device(st, x, w, ids, weights if combine else None, offsets, order, ws)
+    if combine:
+        weights = _exact(weights, st.f32, (T, slots), "weights")
+    _, desc, need = _expert("isc_expert_linear_workspace_size", E, N, K, code, slots, x.dim() == 2, T, bool(combine))
+    dtype = x.dtype if dtype is None else dtype
+    ycode = _type(st, dtype, "dtype")
+    y = _new(st, x, dtype, T, N) if combine else _new(st, x, dtype, T, slots, N)
+    if ws is None:
+        ws = _bytes(st, need, x)
+    status = st.lib.isc_expert_linear(
+        desc, wr.data_ptr(), ldw, T, xr.data_ptr(), ldx, ids.data_ptr(), weights.data_ptr() if combine else None,
+        offsets.data_ptr(), order.data_ptr(), y.data_ptr(), ycode, N, bool(relu), bool(combine), ws.data_ptr(),
+        _isc._nbytes(ws), _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_expert_linear")
+    return y
+
+
+@_on_stream
+def isc_expert_linear_bwd(st, dy, x, w, route, y=None, combine=False, dx=True, dw=True, dweights=None, ws=None,
+                          stream=None):
+    """The gradients of isc_expert_linear: ExpertGrads(dx, dw, dweights).
+
+    dy: the output's gradient, [T, k, N], or [T, N] with combine; x, w, route,
+    combine: as there; y: with relu, what it returned, else None; all in one
+    type.  dx and dw (of x's and w's shape and type) and dweights ([T, k] float32,
+    for isc_route_bwd) are computed if asked for; dweights, by default, with
+    combine."""
+    code = _type(st, x.dtype, "x")
+    T, slots, E, N, K, xr, ldx, wr, ldw, (ids, weights, offsets, order) = _experts(st, x, w, route)
+    dweights = bool(combine) if dweights is None else dweights
+    if not (dx or dw or dweights):
+        raise ValueError("nothing is asked for")
+    if dweights and not combine:
+        raise ValueError("dweights belong to a sum over the slots (combine)")
+    if y is not None and combine:
+        raise ValueError("a sum over the slots has no rectified output")
+    device = _device(st, x, w, dy, y, ids, weights if combine else None, offsets, order, ws)
+    if dy.dtype != x.dtype or dy.shape != ((T, N) if combine else (T, slots, N)):
+        raise ValueError("dy must be %s %r, not %s %r"
+                         % (x.dtype, (T, N) if combine else (T, slots, N), dy.dtype, tuple(dy.shape)))
+    if y is not None and (y.dtype != dy.dtype or y.shape != dy.shape):
+        raise ValueError("y must have dy's shape and type")
+    if combine:
+        weights = _exact(weights, st.f32, (T, slots), "weights")
+    dr, lddy = _rows(dy, N, "dy")
+    yr, ldy = (None, N) if y is None else _rows(y, N, "y")
+    _, desc, need = _expert("isc_expert_linear_bwd_workspace_size", E, N, K, code, slots, x.dim() == 2, T,
+                            y is not None, bool(combine))
+    gx = _new(st, x, x.dtype, *x.shape) if dx else None
+    gw = _new(st, x, x.dtype, E, N, K) if dw else None
+    gs = _new(st, x, st.f32, T, slots) if dweights else None
+    if ws is None:
+        ws = _bytes(st, need, x)
+    status = st.lib.isc_expert_linear_bwd(
+        desc, wr.data_ptr(), ldw, T, xr.data_ptr(), ldx, dr.data_ptr(), lddy, _ptr(yr), ldy, ids.data_ptr(),
+        weights.data_ptr() if combine else None, offsets.data_ptr(), order.data_ptr(), bool(combine), _ptr(gx), K,
+        _ptr(gw), _ptr(gs), ws.data_ptr(), _isc._nbytes(ws), _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_expert_linear_bwd")
+    return ExpertGrads(gx, gw, gs)
+
+
+@functools.lru_cache(maxsize=256)
+def _coefficients(steps, values):
+    """The C array of a, b and c for every step, from one triple or one for each."""
+    try:
+        rows = [tuple(float(v) for v in row) for row in (values if hasattr(values[0], "__len__") else (values,) * steps)]
+    except (TypeError, IndexError, ValueError):
+        rows = []
+    if len(rows) != steps or any(len(row) != 3 for row in rows):
+        raise ValueError("coefficients must be three numbers, or three for each of %d steps" % steps)
+    flat = [v for row in rows for v in row]
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def _tuples(values):
+    return tuple(_tuples(v) for v in values) if hasattr(values, "__len__") else values
+
+
+@_on_stream
+def isc_orthogonalize(st, g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, dtype=None, ws=None,
+                      stream=None):
+    """Each matrix of g with its singular values brought towards one (its own vectors kept).
+
+    g: [..., M, N] float32, float16 or bfloat16, divided by its root of the sum of
+    squares + eps; then `steps` steps X <- a X + (b A + c A A) X, A = X X^T (from
+    the right where M > N).  coefficients: (a, b, c), or one such triple for each
+    step.  Returns [..., M, N] of dtype (float16 or bfloat16; default g's,
+    bfloat16 for float32)."""
+    if g.dim() < 2:
+        raise ValueError("g must be [..., M, N], not %r" % (tuple(g.shape),))
+    M, N = g.shape[-2:]
+    code = _type(st, g.dtype, "g")
+    device = _device(st, g, ws)
+    gr, ldg = _rows(g, N, "g")
+    if dtype is None:
+        dtype = st.torch.bfloat16 if code == F32 else g.dtype
+    ocode = _type(st, dtype, "dtype")
+    if ocode == F32:
+        raise TypeError("dtype must be float16 or bfloat16: the products' operands are float16")
+    B = 1
+    for n in g.shape[:-2]:
+        B *= n
+    steps = int(steps)
+    coef = _coefficients(steps, _tuples(coefficients))
+    o = _new(st, g, dtype, *g.shape)
+    if ws is None:
+        ws = _bytes(st, _size("isc_orthogonalize_workspace_size", B, M, N), g)
+    status = st.lib.isc_orthogonalize(B, M, N, code, gr.data_ptr(), ldg, steps, coef, eps, o.data_ptr(), ocode, N,
+                                      ws.data_ptr(), _isc._nbytes(ws), _stream(st, stream, device))
+    if status:
+        _isc._check(status, "isc_orthogonalize")
+    return o
