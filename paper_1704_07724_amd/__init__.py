@@ -58,6 +58,9 @@ EXPORTS = ("isc_out_shape", "isc_workspace_size", "isc_conv2d", "isc_conv2d_tune
            "isc_w4_size", "isc_w4_quantize", "isc_w4_pack_codes",
            "isc_w4_linear_workspace_size", "isc_w4_linear",
            "isc_w4_skip_workspace_size", "isc_w4_skip",
+           "isc_expert_linear_workspace_size", "isc_expert_linear",
+           "isc_expert_linear_bwd_workspace_size", "isc_expert_linear_bwd",
+           "isc_orthogonalize_workspace_size", "isc_orthogonalize",
            "isc_status_str", "isc_version")
 
 
