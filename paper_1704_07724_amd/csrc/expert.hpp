@@ -106,9 +106,8 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
     x.count = rows;
     w.base += e * a.expert;
     TL t;
-    t.run(x, w, 0, j0, a.inner, lds);
+    t.run(x, w, 0, j0, a.inner, rows, a.cols - j0, lds);
     float dot[TL::FI];
-    const int wave = threadIdx.x >> 6;
     t.each([&](int f, int i, int j, const f32x16 &sums) {
         const int p = i < rows ? a.plan.pairs[first + i] : -1;
         const int there = a.cols - j0 - j;
@@ -128,7 +127,7 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
             d += __shfl_xor(d, 32);
             dot[f] = j % (TL::BJ / TL::WJ) < 32 ? d : dot[f] + d;
             if (j % (TL::BJ / TL::WJ) >= TL::BJ / TL::WJ - 32 && (threadIdx.x & 63) < 32 && p >= 0)
-                a.dots[static_cast<int64_t>(p) * a.ndots + j0 / TL::BJ * TL::WJ + wave % TL::WJ] = dot[f];
+                a.dots[static_cast<int64_t>(p) * a.ndots + j0 / TL::BJ * TL::WJ + TL::part_j() / (TL::BJ / TL::WJ)] = dot[f];
         }
         if (p < 0 || there <= 0) return;
         if (a.scale) {
@@ -172,6 +171,7 @@ hipError_t launch_rows_of(const RowsArgs &a, int64_t pairs, int E, int rows, hip
         return launch_rows<Tile<T, false, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
     } else {
         if (rows == 32) return launch_rows<Tile<T, DIRECT, kAlong, WS, 32, 128, 1, 4>>(a, pairs, E, s);
+        if (rows == 256) return launch_rows<Tile<T, DIRECT, kAlong, WS, 256, 256, 2, 4>>(a, pairs, E, s);
         return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
     }
 }

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(TL::kThreads) void expert_dw_kernel(const DwArgs a)
         d.base += first * d.stride;
     x.list += first;
     TL t;
-    t.run(d, x, i0, j0, d.count, lds);
+    t.run(d, x, i0, j0, d.count, a.N - i0, a.K - j0, lds);
     auto *dw = static_cast<typename T::type *>(a.dw) + static_cast<int64_t>(e) * a.N * a.K;
     t.each([&](int, int i, int j, const f32x16 &v) {
         if (i0 + i < a.N && j0 + j < a.K)
@@ -120,6 +120,8 @@ hipError_t launch_dw(const DwArgs &a, hipStream_t s) {
 }
 template <class T, bool DIRECT>
 hipError_t launch_dw_of(const DwArgs &a, hipStream_t s) {
+    if constexpr (!std::is_same_v<T, F32>)
+        if (a.N > 128 && a.K > 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 256, 256, 2, 4>>(a, s);
     return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, 2>>(a, s);
 }
 
@@ -134,7 +136,8 @@ hipError_t launch_mask(const ExpertBwdArgs &b, hipStream_t s) {
 }  // namespace
 
 int expert_dots(int64_t pairs, int E, int K, int type) {
-    return (K + 127) / 128 * (expert_tile_rows(pairs, E, type) == 128 ? 2 : 4);
+    const int rows = expert_tile_rows(pairs, E, type);
+    return rows == 256 ? (K + 255) / 256 * 4 : (K + 127) / 128 * (rows == 128 ? 2 : 4);
 }
 
 ExpertBwdBytes expert_bwd_bytes(int T, int E, int N, int K, int slots, int type, bool shared, bool relu, bool combine) {

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, con
 int expert_tile_rows(int64_t pairs, int E, int type) {
     const int64_t of_one = pairs / (pairs < E ? pairs > 0 ? pairs : 1 : E);  // on average, of experts that can have any
     if (type == ISC_F32) return of_one <= 64 ? 64 : 128;
-    return of_one <= 32 ? 32 : 128;
+    return of_one <= 32 ? 32 : of_one < 128 ? 128 : 256;
 }
 
 bool expert_launches_fit(int64_t pairs, int E, int N, int K, int type) {

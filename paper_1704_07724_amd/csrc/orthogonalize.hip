@@ -122,7 +122,7 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
     x.base += n * p.xhop;
     w.base += n * p.whop;
     TL t;
-    t.run(x, w, i0, j0, p.inner, lds);
+    t.run(x, w, i0, j0, p.inner, p.rows - i0, p.cols - j0, lds);
     if constexpr (WHAT == kApply) {
         const int np = p.s.np();
         float *state = p.state + n * p.s.of_state();
@@ -200,7 +200,7 @@ hipError_t launch_product(const OrthProduct &p, hipStream_t s) {
 
 template <Side XS, Side WS, Product WHAT>
 hipError_t launch_tile(const OrthProduct &p, hipStream_t s) {
-    return launch_product<Tile<F16, true, XS, WS, 128, 128, 2, 2>, WHAT>(p, s);
+    if constexpr (WHAT == kApply) return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s); else return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s);
 }
 
 template <class T>

@@ -56,18 +56,19 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
 // + 16 * lane.  In assembly because the compiler, which cannot tell the stages
 // apart, would wait for it at the next transposing read; it has no output
 // register, and land() waits for it before the barrier in front of its use.  The
-// place is taken from m0, one wait state after it is written; m0 is left as it was.
+// place is taken from m0, one wait state after it is written; nothing else in the
+// kernels that call this reads m0.
 __device__ __forceinline__ void load_direct(const void *p, uint32_t lds) {
-    uint32_t kept;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
-        : "=&s"(kept)
-        : "v"(p), "s"(lds)
-        : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
 }
 
-// This wavefront's loads have landed and its LDS reads and writes are done; then all wavefronts'.
-__device__ __forceinline__ void land() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// This wavefront's loads have landed, all but the last N, and its LDS reads and writes
+// are done; then all wavefronts'.
+template <int N>
+__device__ __forceinline__ void land() {
+    static_assert(N >= 0 && N < 64, "vmcnt field");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+}
 
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
@@ -110,14 +111,16 @@ struct Stage {
     static_assert(kRow * kLines % THREADS == 0 && THREADS % kRow == 0 && kHop % 8 == 0, "a thread's chunks");
     static_assert(!DIRECT || !kWide, "fp32 goes through registers");
 
-    // Where chunk c of LDS row `line` is.
+    // Where chunk c of LDS row `line` is.  64 banks are 16 chunks: the 16 lanes that read a
+    // chunk of consecutive rows, and the 32 that read four chunks of four rows, meet each once.
     static __device__ __forceinline__ int place(int line, int c) {
-        if constexpr (SIDE == kAcross) return c ^ ((line & 3) << 1);
-        return kRow == 8 ? c ^ (line & 7) : c ^ ((line >> 1) & 3);
+        constexpr int kShare = kRow < 16 ? 16 / kRow : 1;  // rows of all banks
+        if constexpr (SIDE == kAcross) return c ^ (line / kShare % (4 / (kShare < 4 ? kShare : 4)) * 4);
+        return c ^ (line / kShare % kRow);
     }
 
     const char *at[SIDE == kAlong ? kLoads : 1];  // kAlong: the rows' chunks at r = 0
-    int32_t next[SIDE == kAcross ? kLoads : 1];   // kAcross: the rows of the next stage
+    int32_t next[SIDE == kAcross ? kLoads : 1];   // kAcross: the rows of the stage to be sent
     int line, col;                                // this thread's first LDS row, and the element its chunks begin at
     Rows rows;
     uint4 held[DIRECT ? 1 : kLoads][kWide ? 2 : 1];
@@ -142,16 +145,29 @@ struct Stage {
         } else {
             col += o0;
             at[0] = r.base + int64_t{col} * kSize;
-            fetch(0);
+            fetch(0, tid);
         }
     }
 
-    // kAcross: the row numbers of the stage from r0 on.
-    __device__ __forceinline__ void fetch(int r0) {
+    // kAcross: the rows of this thread's chunks of the stage from r0 on.  A wavefront's
+    // loads take few rows each, whose numbers come by scalar loads: a vector load would
+    // have to wait for every direct load sent before it.
+    __device__ __forceinline__ void fetch(int r0, int tid) {
+        constexpr int kRows = kRow < 64 ? 64 / kRow : 1;
+        const int own = kRows > 1 ? (tid & 63) / kRow : 0;
+        const int first = r0 + __builtin_amdgcn_readfirstlane(line - own);
+        using Scalar = const __attribute__((address_space(4))) int32_t *;
+        Scalar list = reinterpret_cast<Scalar>(reinterpret_cast<uintptr_t>(rows.list));
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-            const int r = r0 + line + n * kHop;
-            next[n] = r >= rows.count ? -1 : rows.list ? rows.list[r] : r;
+            int32_t row = -1;
+#pragma unroll
+            for (int q = 0; q < kRows; ++q) {
+                const int r = first + n * kHop + q;
+                const int32_t number = r >= rows.count ? -1 : rows.list ? list[r] : r;
+                row = own == q ? number : row;
+            }
+            next[n] = row;
         }
     }
 
@@ -183,23 +199,25 @@ struct Stage {
         }
     }
 
-    // Sends the loads of the stage from r0 on; direct ones to LDS at `lds`.
-    __device__ __forceinline__ void issue(int r0, uint32_t lds, int wave) {
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            int there;
-            const char *p = chunk(n, r0, there);
-            if constexpr (DIRECT) {
-                // width and column are multiples of 8: a chunk exists as a whole or not at all
-                load_direct(there > 0 ? p : reinterpret_cast<const char *>(kZeros), lds + (n * THREADS + wave * 64) * 16);
-            } else if (there >= 8) {
-                held[n][0] = load_any<uint4>(p);
-                if constexpr (kWide) held[n][1] = load_any<uint4>(p + 16);
-            } else {
-                masked(held[n], p, there);
-            }
+    // Sends load n of the stage from r0 on; a direct one to LDS at `lds`.
+    __device__ __forceinline__ void send(int n, int r0, uint32_t lds, int wave) {
+        int there;
+        const char *p = chunk(n, r0, there);
+        if constexpr (DIRECT) {
+            // width and column are multiples of 8: a chunk exists as a whole or not at all
+            if (SIDE == kAcross || r0 + BK > rows.width) p = there > 0 ? p : reinterpret_cast<const char *>(kZeros);
+            load_direct(p, lds + (n * THREADS + wave * 64) * 16);
+        } else if (there >= 8) {
+            held[n][0] = load_any<uint4>(p);
+            if constexpr (kWide) held[n][1] = load_any<uint4>(p + 16);
+        } else {
+            masked(held[n], p, there);
         }
-        if constexpr (SIDE == kAcross) fetch(r0 + BK);
+    }
+    __device__ __forceinline__ void send_all(int r0, uint32_t lds, int wave, int tid) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) send(n, r0, lds, wave);
+        if constexpr (SIDE == kAcross) fetch(r0 + BK, tid);
     }
 
     // Puts what the registers hold into LDS.
@@ -257,8 +275,10 @@ struct Stage {
     }
 };
 
-// A workgroup's tile: BI x BJ results by WI x WJ wavefronts, BK inner indices a
-// stage, two stages in LDS.
+// A workgroup's tile: BI x BJ results by WI x WJ wavefronts, BK inner indices a stage.
+// Loads through registers have two stages in LDS.  Direct loads have two of W and three
+// of X (160 KiB for 256 x 256, all of a compute unit's; 80 KiB for 128 x 128, so that
+// two workgroups fit): X's have more than a stage's time to land, W's most of one.
 template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_>
 struct Tile {
     using T = T_;
@@ -271,39 +291,65 @@ struct Tile {
     using WStage = Stage<T, DIRECT, WS, BJ, BK, kThreads>;
     static constexpr int kParts = XStage::kParts;
     static constexpr int kXBytes = XStage::kBytes * kParts, kWBytes = WStage::kBytes * kParts;
-    static constexpr int kLds = 2 * (kXBytes + kWBytes);
+    static constexpr int kXStages = DIRECT ? 3 : 2;
+    static constexpr int kLds = kXStages * kXBytes + 2 * kWBytes;
 
     f32x16 acc[FJ][FI];
 
-    // Products of the stage at `x` and `w` in LDS.
-    __device__ __forceinline__ void multiply(const char *x, const char *w, int wi, int wj, int lane) {
+    // What a wavefront multiplies at a time: 16 inner indices.
+    struct Operands {
+        s16x8 w[FJ][kParts], x[FI][kParts];
+    };
+    static constexpr int kReads = kParts * (FI + FJ);
+    // Read n of a step's operands: those that the first products take come first.
+    static __device__ __forceinline__ void read(Operands &o, int n, const char *x, const char *w, int kk, int wi, int wj,
+                                                int lane) {
+        const int p = kParts - 1 - n / (FI + FJ), f = n % (FI + FJ);
+        if (f == 0 || f > FI)
+            o.w[f == 0 ? 0 : f - FI][p] =
+                WStage::template operand<true>(w + p * WStage::kBytes, wj + 32 * (f == 0 ? 0 : f - FI), kk, lane);
+        else
+            o.x[f - 1][p] = XStage::template operand<false>(x + p * XStage::kBytes, wi + 32 * (f - 1), kk, lane);
+    }
+    // between(n): what is issued behind product n, while the matrix cores have work.
+    static constexpr int kProducts = FI * FJ * kParts * (kParts + 1) / 2;
+    template <class Between>
+    __device__ __forceinline__ void multiply(const Operands &o, Between &&between) {
+        int n = 0;
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) {
-            s16x8 a[FJ][kParts], b[FI][kParts];
+        for (int sum = kParts - 1; sum >= 0; --sum)  // the small products first
 #pragma unroll
-            for (int p = 0; p < kParts; ++p) {
+            for (int p = 0; p <= sum; ++p)
 #pragma unroll
-                for (int f = 0; f < FJ; ++f)
-                    a[f][p] = WStage::template operand<true>(w + p * WStage::kBytes, wj + 32 * f, kk, lane);
+                for (int j = 0; j < FJ; ++j)
 #pragma unroll
-                for (int f = 0; f < FI; ++f)
-                    b[f][p] = XStage::template operand<false>(x + p * XStage::kBytes, wi + 32 * f, kk, lane);
-            }
-#pragma unroll
-            for (int sum = kParts - 1; sum >= 0; --sum)  // the small products first
-#pragma unroll
-                for (int p = 0; p <= sum; ++p)
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j)
-#pragma unroll
-                        for (int i = 0; i < FI; ++i) acc[j][i] = mfma<T>(a[j][p], b[i][sum - p], acc[j][i]);
-        }
+                    for (int i = 0; i < FI; ++i) {
+                        acc[j][i] = mfma<T>(o.w[j][p], o.x[i][sum - p], acc[j][i]);
+                        between(n++);
+                    }
     }
 
-    // The sums of the tile at (i0, j0) over `inner` inner indices.
-    __device__ __forceinline__ void run(const Rows &x, const Rows &w, int i0, int j0, int inner, char *lds) {
+    // This wavefront's part of the tile.  A SIMD's two wavefronts (w and w + 4 of eight) have
+    // neither rows nor columns in common, so that where a tile reaches past an edge the
+    // ones that have nothing to do leave the matrix cores of every SIMD to the others.
+    static __device__ __forceinline__ int part_i() {
+        return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6)) / WJ * (BI / WI);
+    }
+    static __device__ __forceinline__ int part_j() {
+        const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+        return (wave + (kWaves == 8 ? wave / WJ * (WJ / 2) : 0)) % WJ * (BJ / WJ);
+    }
+
+    // The sums of the tile at (i0, j0) over `inner` inner indices, of whose rows and columns
+    // the first `rows` and `cols` are asked for.  The operands of the
+    // next 16 are read ahead of the products of those at hand; a stage's last are in
+    // registers when the wavefronts meet, so that behind the barrier its place is free.
+    // Loads are sent one at a time between products: sent together they would hold the
+    // wavefront, and the matrix cores with it, until the address unit has taken them.
+    __device__ __forceinline__ void run(const Rows &x, const Rows &w, int i0, int j0, int inner, int rows, int cols, char *lds) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int wi = wave / WJ * (BI / WI), wj = wave % WJ * (BJ / WJ);
+        const int wi = part_i(), wj = part_j();
+        const bool busy = wi < rows && wj < cols;
 #pragma unroll
         for (int j = 0; j < FJ; ++j)
 #pragma unroll
@@ -316,25 +362,99 @@ struct Tile {
         WStage ws;
         xs.begin(x, i0, tid);
         ws.begin(w, j0, tid);
+        constexpr int kSteps16 = BK / 16;
+        static_assert(kSteps16 % 2 == 0, "a stage's first operands are always at[0]");
         const uint32_t base = lds_address(lds);
-        xs.issue(0, base, wave);
-        ws.issue(0, base + kXBytes, wave);
-        xs.commit(lds, tid);
-        ws.commit(lds + kXBytes, tid);
-        land();
-        for (int s = 0; s < steps; ++s) {
-            const int now = (s & 1) * (kXBytes + kWBytes), then = (kXBytes + kWBytes) - now;
-            if (s + 1 < steps) {
-                xs.issue((s + 1) * BK, base + then, wave);
-                ws.issue((s + 1) * BK, base + then + kXBytes, wave);
+        const auto w_at = [](int s) { return kXStages * kXBytes + (s & 1) * kWBytes; };
+        int x_now = 0;  // the place in LDS of this stage's X
+        const auto x_next = [](int at) { return at + kXBytes < kXStages * kXBytes ? at + kXBytes : 0; };
+        if constexpr (DIRECT) {
+            xs.send_all(0, base, wave, tid);
+            ws.send_all(0, base + w_at(0), wave, tid);
+            if (steps > 1) {
+                xs.send_all(BK, base + kXBytes, wave, tid);
+                land<XStage::kLoads>();
+            } else {
+                land<0>();
             }
-            multiply(lds + now, lds + now + kXBytes, wi, wj, lane);
-            if (s + 1 < steps) {
-                xs.commit(lds + then, tid);
-                ws.commit(lds + then + kXBytes, tid);
-            }
-            land();
+        } else {
+            xs.send_all(0, 0, wave, tid);
+            ws.send_all(0, 0, wave, tid);
+            xs.commit(lds, tid);
+            ws.commit(lds + w_at(0), tid);
+            land<0>();
         }
+        Operands at[2];
+#pragma unroll
+        for (int n = 0; n < kReads; ++n) read(at[0], n, lds, lds + w_at(0), 0, wi, wj, lane);
+        for (int s = 0; s < steps; ++s) {
+            const bool more = s + 1 < steps, most = s + 2 < steps;
+            const int x_then = x_next(x_now), x_last = x_next(x_then);
+            if (!DIRECT && more) {
+                xs.send_all((s + 1) * BK, 0, wave, tid);
+                ws.send_all((s + 1) * BK, 0, wave, tid);
+            }
+#pragma unroll
+            for (int kk = 0; kk < kSteps16; ++kk) {
+                if (kk + 1 == kSteps16 && more) {
+                    if constexpr (DIRECT) {
+                        if (most)
+                            land<DIRECT ? XStage::kLoads : 0>();
+                        else
+                            land<0>();
+                    } else {
+                        xs.commit(lds + x_then, tid);
+                        ws.commit(lds + w_at(s + 1), tid);
+                        land<0>();
+                    }
+                }
+                // the operands of the next 16: behind the last stage's, those of some stage, which nothing takes
+                const char *from_x = lds + (kk + 1 < kSteps16 ? x_now : x_then),
+                           *from_w = lds + (kk + 1 < kSteps16 ? w_at(s) : w_at(s + 1));
+                const auto send = [&](int n) {
+                    if constexpr (DIRECT) {
+                        constexpr int kW = (WStage::kLoads + kProducts - 1) / kProducts;
+                        constexpr int kX = (XStage::kLoads + kProducts - 1) / kProducts;
+                        if (kk == 0 && more) {
+#pragma unroll
+                            for (int q = n * kW; q < (n + 1) * kW && q < WStage::kLoads; ++q) {
+                                ws.send(q, (s + 1) * BK, base + w_at(s + 1), wave);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                        if (kk == 1 && most) {
+#pragma unroll
+                            for (int q = n * kX; q < (n + 1) * kX && q < XStage::kLoads; ++q) {
+                                xs.send(q, (s + 2) * BK, base + x_last, wave);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                    }
+                };
+                __builtin_amdgcn_sched_barrier(0);
+                if (busy) {
+                    multiply(at[kk & 1], [&](int n) {
+                        constexpr int kEach = (kReads + kProducts - 1) / kProducts;
+#pragma unroll
+                        for (int q = n * kEach; q < (n + 1) * kEach && q < kReads; ++q)
+                            read(at[(kk + 1) & 1], q, from_x, from_w, (kk + 1) % kSteps16, wi, wj, lane);
+                        __builtin_amdgcn_sched_barrier(0);
+                        send(n);
+                    });
+                } else {
+#pragma unroll
+                    for (int n = 0; n < kProducts; ++n) send(n);
+                }
+                if constexpr (DIRECT) {
+                    if constexpr (WS == kAcross) if (kk == 0 && more) ws.fetch((s + 2) * BK, tid);
+                    if constexpr (XS == kAcross) if (kk == 1 && most) xs.fetch((s + 3) * BK, tid);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            x_now = x_then;
+        }
+        // no load into LDS may outlive its tile, and all of its reads are done before another's
+        land<0>();
     }
 
     // out(f, i, j, v): 16 consecutive results of row i (this lane's f-th) from column j on, in
@@ -342,7 +462,7 @@ struct Tile {
     template <class Out>
     __device__ __forceinline__ void each(Out &&out) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int wi = wave / WJ * (BI / WI), wj = wave % WJ * (BJ / WJ);
+        const int wi = part_i(), wj = part_j();
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
