@@ -40,14 +40,15 @@ struct ExpertBwdArgs {
     void *dx, *dw;        // each nullptr where it is not asked for
     float *dweights;
     int64_t lddx;
-    void *masked;         // P rows of dy by expert: rectified or weighted, expert_ld() elements apart
+    void *masked;         // P rows of dy, rectified or weighted, expert_ld() elements apart
     float *part, *dots;   // part: P rows of dx; dots: what each row's tiles give to dweights
 };
 
 // Leading dimension of rows in the workspace: 16-byte boundaries in every type.
 inline int64_t expert_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
-// Rows of a tile of the experts' pairs, and the parts in which a row's dot products come.
-int expert_tile_rows(int64_t pairs, int E, int type);
+// Rows of a tile of the experts' pairs (direct: of operands that go into LDS by direct
+// loads), and the parts in which a row's dot products come.
+int expert_tile_rows(int64_t pairs, int E, int type, bool direct);
 int expert_dots(int64_t pairs, int E, int K, int type);
 size_t expert_plan_bytes(int64_t pairs, int E, int type);
 ExpertPlan expert_plan_at(void *ws, int64_t pairs, int E, int type);
@@ -60,7 +61,8 @@ struct ExpertBwdBytes {
 };
 ExpertBwdBytes expert_bwd_bytes(int T, int E, int N, int K, int slots, int type, bool shared, bool relu, bool combine);
 
-hipError_t launch_expert_plan(const ExpertArgs &a, void *empty, int64_t ld, int cols, int size, hipStream_t s);
+// Tiles of `rows` rows; `empty`: the pairs' output, of which rows without an expert become 0.
+hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_t ld, int cols, int size, hipStream_t s);
 // out[t] = the sum over a token's pairs of part's rows, weighted or not.
 hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, const float *weights, void *out,
                              int64_t ldo, int type, hipStream_t s);
@@ -72,9 +74,8 @@ namespace tp {
 // A product over rows by expert: out[pair] = sum over r of X(pair, r) W_e(j, r).
 struct RowsArgs {
     ExpertPlan plan;
-    Rows x, w;          // w: the first expert's
+    Rows x, w;          // x by the list of places; w: the first expert's
     int64_t expert;     // bytes from one expert's matrix to the next
-    int listed;         // whether x.list is read by place; else places are x's rows
     int inner, cols;    // inner indices, columns of the result
     void *out;
     int64_t ldo;
@@ -93,60 +94,62 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int across = (a.cols + TL::BJ - 1) / TL::BJ;
     const int total = a.plan.tiles[0] * across;
-    if (static_cast<int>(blockIdx.x) >= total) return;
-    const int id = of_xcd(blockIdx.x, total);
-    const int4 tile = reinterpret_cast<const int4 *>(a.plan.tiles)[1 + id / across];
-    const int e = __builtin_amdgcn_readfirstlane(tile.x), first = __builtin_amdgcn_readfirstlane(tile.y),
-              rows = __builtin_amdgcn_readfirstlane(tile.z), j0 = id % across * TL::BJ;
-    Rows x = a.x, w = a.w;
-    if (a.listed)
-        x.list += first;
-    else
-        x.base += first * x.stride;
-    x.count = rows;
-    w.base += e * a.expert;
+    struct Job {
+        int first, rows, j0;
+    } job, next;
     TL t;
-    t.run(x, w, 0, j0, a.inner, rows, a.cols - j0, lds);
-    float dot[TL::FI];
-    t.each([&](int f, int i, int j, const f32x16 &sums) {
-        const int p = i < rows ? a.plan.pairs[first + i] : -1;
-        const int there = a.cols - j0 - j;
-        f32x16 v = sums;
-        if (a.dotted) {
-            float d = 0.0f;
-            if (p >= 0 && there > 0) {
-                const auto *row = static_cast<const typename T::type *>(a.dotted) + p / a.dot_slots * a.lddot + j0 + j;
+    const auto start = [&](int n) {
+        const int id = of_xcd(n, total);
+        const int4 tile = reinterpret_cast<const int4 *>(a.plan.tiles)[1 + id / across];
+        const int e = __builtin_amdgcn_readfirstlane(tile.x);
+        const Job j{__builtin_amdgcn_readfirstlane(tile.y), __builtin_amdgcn_readfirstlane(tile.z), id % across * TL::BJ};
+        Rows x = a.x, w = a.w;
+        x.list += j.first;
+        x.count = j.rows;
+        w.base += e * a.expert;
+        t.start(x, w, 0, j.j0, a.inner, lds);
+        return j;
+    };
+    int n = blockIdx.x;
+    if (n >= total) return;
+    job = start(n);
+    for (bool landed = false;; landed = true) {
+        t.sums(a.inner, job.rows, a.cols - job.j0, landed, lds);
+        n += gridDim.x;
+        if (n < total) next = start(n);
+        t.template each<false>(
+            lds,
+            [&](int i, int j, const float (&sums)[8]) {
+                const int p = i < job.rows ? a.plan.pairs[job.first + i] : -1;
+                const int there = a.cols - job.j0 - j;
+                if (a.dotted) {
+                    float d = 0.0f;
+                    if (p >= 0 && there > 0) {
+                        float u[8];
+                        load8<T>(u, static_cast<const typename T::type *>(a.dotted) + p / a.dot_slots * a.lddot + job.j0 + j,
+                                 there);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float u[8];
-                    load8<T>(u, row + 8 * q, there - 8 * q);
+                        for (int k = 0; k < 8; ++k) d = fmaf(k < there ? sums[k] : 0.0f, u[k], d);
+                    }
 #pragma unroll
-                    for (int n = 0; n < 8; ++n) d = fmaf(n + 8 * q < there ? v[8 * q + n] : 0.0f, u[n], d);
+                    for (int by = 1; by < TL::kLanes; by *= 2) d += __shfl_xor(d, by);
+                    if (j % TL::kCols == 0 && p >= 0 && there > 0)
+                        a.dots[static_cast<int64_t>(p) * a.ndots + (job.j0 + j) / TL::kCols] = d;
                 }
-            }
-            d += __shfl_xor(d, 32);
-            dot[f] = j % (TL::BJ / TL::WJ) < 32 ? d : dot[f] + d;
-            if (j % (TL::BJ / TL::WJ) >= TL::BJ / TL::WJ - 32 && (threadIdx.x & 63) < 32 && p >= 0)
-                a.dots[static_cast<int64_t>(p) * a.ndots + j0 / TL::BJ * TL::WJ + TL::part_j() / (TL::BJ / TL::WJ)] = dot[f];
-        }
-        if (p < 0 || there <= 0) return;
-        if (a.scale) {
-            const float s = a.scale[p];
+                if (p < 0 || there <= 0) return;
+                const float s = a.scale ? a.scale[p] : 1.0f;
+                float v[8];
 #pragma unroll
-            for (int n = 0; n < 16; ++n) v[n] *= s;
-        }
-        if (a.relu) {
-#pragma unroll
-            for (int n = 0; n < 16; ++n) v[n] = v[n] < 0.0f ? 0.0f : v[n];  // a NaN stays
-        }
-        const int64_t at = p * a.ldo + j0 + j;
-        if (a.otype == ISC_F32)
-            store16<F32>(static_cast<float *>(a.out) + at, v, there);
-        else if (a.otype == ISC_BF16)
-            store16<BF16>(static_cast<uint16_t *>(a.out) + at, v, there);
-        else
-            store16<F16>(static_cast<uint16_t *>(a.out) + at, v, there);
-    });
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = sums[k] * s;
+                    if (a.relu) v[k] = v[k] < 0.0f ? 0.0f : v[k];  // a NaN stays
+                }
+                store8_as(a.out, p * a.ldo + job.j0 + j, v, there, a.otype);
+            },
+            [](int, int, const float (&)[8]) {});
+        if (n >= total) return;
+        job = next;
+    }
 }
 
 // Whether a side's rows can go into LDS by direct loads.
@@ -158,7 +161,7 @@ template <class TL>
 hipError_t launch_rows(const RowsArgs &a, int64_t pairs, int E, hipStream_t s) {
     if (hipError_t e = allow_lds(expert_rows_kernel<TL>, TL::kLds); e != hipSuccess) return e;
     const int64_t tiles = pairs / TL::BI + (pairs < E ? pairs : E);  // as many as there can be
-    const int64_t grid = tiles * ((a.cols + TL::BJ - 1) / TL::BJ);
+    const int64_t all = tiles * ((a.cols + TL::BJ - 1) / TL::BJ), grid = all < kResident<TL> ? all : kResident<TL>;
     hipLaunchKernelGGL(expert_rows_kernel<TL>, dim3(static_cast<unsigned>(grid)), dim3(TL::kThreads), TL::kLds, s, a);
     return hipGetLastError();
 }
@@ -171,13 +174,14 @@ hipError_t launch_rows_of(const RowsArgs &a, int64_t pairs, int E, int rows, hip
         return launch_rows<Tile<T, false, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
     } else {
         if (rows == 32) return launch_rows<Tile<T, DIRECT, kAlong, WS, 32, 128, 1, 4>>(a, pairs, E, s);
-        if (rows == 256) return launch_rows<Tile<T, DIRECT, kAlong, WS, 256, 256, 2, 4>>(a, pairs, E, s);
+        if constexpr (DIRECT)
+            if (rows == 256) return launch_rows<Tile<T, true, kAlong, WS, 256, 256, 2, 4>>(a, pairs, E, s);
         return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
     }
 }
 template <Side WS>
 hipError_t launch_rows_by(const RowsArgs &a, int type, bool direct, int64_t pairs, int E, hipStream_t s) {
-    const int rows = expert_tile_rows(pairs, E, type);
+    const int rows = expert_tile_rows(pairs, E, type, direct);
     if (type == ISC_F32) return launch_rows_of<F32, false, WS>(a, pairs, E, rows, s);
     if (type == ISC_BF16)
         return direct ? launch_rows_of<BF16, true, WS>(a, pairs, E, rows, s)

@@ -9,7 +9,7 @@
 //     the product w x is not made again; each tile of columns gives a part.
 //   dw[e] = sum over e's pairs of s d[p] x[p]^T: as many terms as e has pairs, and
 //     both operands have them across their rows.
-// Masked or weighted gradients are written once, by expert, in their own type (a
+// Masked or weighted gradients are written once, in their own type (a
 // weight times a gradient is rounded there: half a unit in the last place of each
 // term, which leaves of a sum what the sum's own rounding is), since the product
 // that reads them would do it for every tile.
@@ -20,7 +20,7 @@ namespace {
 
 using namespace tp;
 
-// masked[i] = the gradient of the pair at place i.
+// masked[p] = the gradient of pair p's product; nothing where it has no expert.
 template <class T>
 __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b, int64_t ld) {
     const ExpertArgs &a = b.a;
@@ -28,12 +28,11 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
     const int groups = static_cast<int>(ld / 8);
     const int64_t all = static_cast<int64_t>(a.T) * a.slots * groups, hop = static_cast<int64_t>(gridDim.x) * 256;
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; n < all; n += hop) {
-        const int64_t i = n / groups;
-        const int c = static_cast<int>(n - i * groups) * 8;
-        const int64_t p = a.plan.pairs[i];
-        float v[8] = {};
-        if (p >= 0) {
-            load8<T>(v, static_cast<const V *>(b.dy) + (b.combine ? a.plan.tokens[i] : p) * b.lddy + c, a.N - c);
+        const int64_t p = n / groups;
+        const int c = static_cast<int>(n - p * groups) * 8;
+        if (static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E)) {
+            float v[8];
+            load8<T>(v, static_cast<const V *>(b.dy) + (b.combine ? p / a.slots : p) * b.lddy + c, a.N - c);
             if (b.y) {
                 float y[8];
                 load8<T>(y, static_cast<const V *>(b.y) + p * b.ldy + c, a.N - c);
@@ -45,8 +44,8 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] = c + q < a.N ? v[q] * w : 0.0f;
             }
+            store8<T>(static_cast<V *>(b.masked) + p * ld + c, v, 8);
         }
-        store8<T>(static_cast<V *>(b.masked) + i * ld + c, v, 8);
     }
 }
 
@@ -62,35 +61,50 @@ __global__ __launch_bounds__(256) void expert_dots_kernel(const ExpertArgs a, co
 
 struct DwArgs {
     const int32_t *offsets;
-    Rows d, x;  // listed by place, or places themselves
-    int d_listed, P, N, K;
+    Rows d, x;  // listed by place
+    int P, N, K;
     void *dw;
     int nexp;
 };
 
 template <class TL>
-__global__ __launch_bounds__(TL::kThreads) void expert_dw_kernel(const DwArgs a) {
+__global__ __launch_bounds__(TL::kThreads) void expert_dw_kernel(const DwArgs a, int total) {
     using T = typename TL::T;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int down = (a.N + TL::BI - 1) / TL::BI, across = (a.K + TL::BJ - 1) / TL::BJ;
-    const int id = of_xcd(blockIdx.x, gridDim.x);
-    const int e = id / (down * across), i0 = id / across % down * TL::BI, j0 = id % across * TL::BJ;
-    const int lo = a.offsets[e], hi = a.offsets[e + 1];
-    const int first = lo < 0 ? 0 : lo > a.P ? a.P : lo, end = hi > a.P ? a.P : hi;
-    Rows d = a.d, x = a.x;
-    d.count = x.count = end > first ? end - first : 0;
-    if (a.d_listed)
-        d.list += first;
-    else
-        d.base += first * d.stride;
-    x.list += first;
+    struct Job {
+        int e, i0, j0, inner;
+    } job, next;
     TL t;
-    t.run(d, x, i0, j0, d.count, a.N - i0, a.K - j0, lds);
-    auto *dw = static_cast<typename T::type *>(a.dw) + static_cast<int64_t>(e) * a.N * a.K;
-    t.each([&](int, int i, int j, const f32x16 &v) {
-        if (i0 + i < a.N && j0 + j < a.K)
-            store16<T>(dw + static_cast<int64_t>(i0 + i) * a.K + j0 + j, v, a.K - j0 - j);
-    });
+    const auto start = [&](int n) {
+        const int id = of_xcd(n, total);
+        Job j{id / (down * across), id / across % down * TL::BI, id % across * TL::BJ, 0};
+        const int lo = a.offsets[j.e], hi = a.offsets[j.e + 1];
+        const int first = lo < 0 ? 0 : lo > a.P ? a.P : lo, end = hi > a.P ? a.P : hi;
+        Rows d = a.d, x = a.x;
+        d.count = x.count = j.inner = end > first ? end - first : 0;
+        d.list += first;
+        x.list += first;
+        t.start(d, x, j.i0, j.j0, j.inner, lds);
+        return j;
+    };
+    int n = blockIdx.x;
+    job = start(n);
+    for (bool landed = false;; landed = true) {
+        t.sums(job.inner, a.N - job.i0, a.K - job.j0, landed, lds);
+        n += gridDim.x;
+        if (n < total) next = start(n);
+        auto *dw = static_cast<typename T::type *>(a.dw) + static_cast<int64_t>(job.e) * a.N * a.K;
+        t.template each<false>(
+            lds,
+            [&](int i, int j, const float (&v)[8]) {
+                if (job.i0 + i < a.N && job.j0 + j < a.K)
+                    store8<T>(dw + static_cast<int64_t>(job.i0 + i) * a.K + job.j0 + j, v, a.K - job.j0 - j);
+            },
+            [](int, int, const float (&)[8]) {});
+        if (n >= total) return;
+        job = next;
+    }
 }
 
 // Without tokens every weight's gradient is 0, and there are no lists to read.
@@ -115,14 +129,15 @@ template <class TL>
 hipError_t launch_dw(const DwArgs &a, hipStream_t s) {
     if (hipError_t e = allow_lds(expert_dw_kernel<TL>, TL::kLds); e != hipSuccess) return e;
     const int64_t grid = static_cast<int64_t>((a.N + TL::BI - 1) / TL::BI) * ((a.K + TL::BJ - 1) / TL::BJ) * a.nexp;
-    hipLaunchKernelGGL(expert_dw_kernel<TL>, dim3(static_cast<unsigned>(grid)), dim3(TL::kThreads), TL::kLds, s, a);
+    hipLaunchKernelGGL(expert_dw_kernel<TL>, dim3(static_cast<unsigned>(grid < kResident<TL> ? grid : kResident<TL>)),
+                       dim3(TL::kThreads), TL::kLds, s, a, static_cast<int>(grid));
     return hipGetLastError();
 }
 template <class T, bool DIRECT>
 hipError_t launch_dw_of(const DwArgs &a, hipStream_t s) {
-    if constexpr (!std::is_same_v<T, F32>)
-        if (a.N > 128 && a.K > 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 256, 256, 2, 4>>(a, s);
-    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, 2>>(a, s);
+    if constexpr (DIRECT)
+        if (a.N > 128 && a.K > 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 256, 256, 2, 4, true>>(a, s);
+    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, 2, true>>(a, s);
 }
 
 template <class T>
@@ -136,8 +151,8 @@ hipError_t launch_mask(const ExpertBwdArgs &b, hipStream_t s) {
 }  // namespace
 
 int expert_dots(int64_t pairs, int E, int K, int type) {
-    const int rows = expert_tile_rows(pairs, E, type);
-    return rows == 256 ? (K + 255) / 256 * 4 : (K + 127) / 128 * (rows == 128 ? 2 : 4);
+    const int cols = expert_tile_rows(pairs, E, type, false) >= 128 ? 64 : 32;  // of a wavefront
+    return (K + cols - 1) / cols;
 }
 
 ExpertBwdBytes expert_bwd_bytes(int T, int E, int N, int K, int slots, int type, bool shared, bool relu, bool combine) {
@@ -157,7 +172,11 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
     const int size = a.type == ISC_F32 ? 4 : 2;
     const bool sum = a.shared && a.slots > 1;
     if (a.T == 0) return launch_zero_dw(b, s);
-    hipError_t e = launch_expert_plan(a, b.dx && !sum ? b.dx : nullptr, b.lddx, a.K, size, s);
+    const int64_t ldm = expert_ld(a.N);
+    const bool aligned_dy = direct_rows(b.dy, b.lddy, a.N, size), aligned_masked = direct_rows(b.masked, ldm, a.N, size);
+    const bool direct = (b.y ? aligned_masked : aligned_dy) && direct_rows(a.w, a.ldw, a.K, size);
+    hipError_t e = launch_expert_plan(a, expert_tile_rows(a.pairs(), a.E, a.type, direct), b.dx && !sum ? b.dx : nullptr,
+                                      b.lddx, a.K, size, s);
     if (e != hipSuccess) return e;
     // a sum's dx takes the gradient as it is (its own sums are weighted), a rectifier's takes it masked
     const bool masks = b.y || (b.combine && b.dw);
@@ -165,15 +184,12 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
         e = a.type == ISC_F32 ? launch_mask<F32>(b, s) : a.type == ISC_BF16 ? launch_mask<BF16>(b, s) : launch_mask<F16>(b, s);
         if (e != hipSuccess) return e;
     }
-    const int64_t ldm = expert_ld(a.N);
-    const Rows by_place{static_cast<const char *>(b.masked), ldm * size, nullptr, 0, a.N};
-    const Rows by_pair{static_cast<const char *>(b.dy), b.lddy * size, b.combine ? a.plan.tokens : a.plan.pairs, 0, a.N};
-    const bool aligned_dy = direct_rows(b.dy, b.lddy, a.N, size), aligned_masked = direct_rows(b.masked, ldm, a.N, size);
+    const Rows masked{static_cast<const char *>(b.masked), ldm * size, a.plan.pairs, 0, a.N};
+    const Rows given{static_cast<const char *>(b.dy), b.lddy * size, b.combine ? a.plan.tokens : a.plan.pairs, 0, a.N};
     if (b.dx || b.dweights) {
         RowsArgs r{};
         r.plan = a.plan;
-        r.x = b.y ? by_place : by_pair;
-        r.listed = !b.y;
+        r.x = b.y ? masked : given;
         r.w = {static_cast<const char *>(a.w), a.ldw * size, nullptr, a.N, a.K};
         r.expert = a.N * a.ldw * size;
         r.inner = a.N;
@@ -189,7 +205,6 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
             r.dots = b.dots;
             r.ndots = expert_dots(a.pairs(), a.E, a.K, a.type);
         }
-        const bool direct = (b.y ? aligned_masked : aligned_dy) && direct_rows(a.w, a.ldw, a.K, size);
         e = launch_rows_by<kAcross>(r, a.type, direct, a.pairs(), a.E, s);
         if (e != hipSuccess) return e;
         if (sum && b.dx) {
@@ -204,13 +219,13 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
     }
     if (!b.dw) return hipSuccess;
     const DwArgs d{a.offsets,
-                   masks ? by_place : by_pair,
+                   masks ? masked : given,
                    {static_cast<const char *>(a.x), a.ldx * size, a.shared ? a.plan.tokens : a.plan.pairs, 0, a.K},
-                   !masks, static_cast<int>(a.pairs()), a.N, a.K, b.dw, a.E};
-    const bool direct = (masks ? aligned_masked : aligned_dy) && direct_rows(a.x, a.ldx, a.K, size);
+                   static_cast<int>(a.pairs()), a.N, a.K, b.dw, a.E};
+    const bool direct_x = (masks ? aligned_masked : aligned_dy) && direct_rows(a.x, a.ldx, a.K, size);
     if (a.type == ISC_F32) return launch_dw_of<F32, false>(d, s);
-    if (a.type == ISC_BF16) return direct ? launch_dw_of<BF16, true>(d, s) : launch_dw_of<BF16, false>(d, s);
-    return direct ? launch_dw_of<F16, true>(d, s) : launch_dw_of<F16, false>(d, s);
+    if (a.type == ISC_BF16) return direct_x ? launch_dw_of<BF16, true>(d, s) : launch_dw_of<BF16, false>(d, s);
+    return direct_x ? launch_dw_of<F16, true>(d, s) : launch_dw_of<F16, false>(d, s);
 }
 
 }  // namespace isc

@@ -111,37 +111,45 @@ __global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, con
 
 }  // namespace
 
-int expert_tile_rows(int64_t pairs, int E, int type) {
-    const int64_t of_one = pairs / (pairs < E ? pairs > 0 ? pairs : 1 : E);  // on average, of experts that can have any
+// By the rows that an expert has on average, of experts that can have any.  Tiles of 256 x
+// 256 need all of a compute unit's LDS and direct loads; TABLE
+int expert_tile_rows(int64_t pairs, int E, int type, bool direct) {
+    const int64_t of_one = pairs / (pairs < E ? pairs > 0 ? pairs : 1 : E);
     if (type == ISC_F32) return of_one <= 64 ? 64 : 128;
-    return of_one <= 32 ? 32 : of_one < 128 ? 128 : 256;
+    return of_one <= 32 ? 32 : of_one < 128 || !direct ? 128 : 256;
 }
 
+namespace {
+
+// Tiles of rows that there can be, whichever kernel runs.
+int64_t most_tiles(int64_t pairs, int E, int type) {
+    return pairs / expert_tile_rows(pairs, E, type, false) + (pairs < E ? pairs : E);
+}
+
+}  // namespace
+
 bool expert_launches_fit(int64_t pairs, int E, int N, int K, int type) {
-    const int64_t tiles = pairs / expert_tile_rows(pairs, E, type) + (pairs < E ? pairs : E);
     const int64_t across = ((N > K ? N : K) + 127) / 128;
-    return tiles * across * 256 <= kLaunchThreads &&
-           ((N + 127) / 128) * static_cast<int64_t>((K + 127) / 128) * E * 256 <= kLaunchThreads;
+    return most_tiles(pairs, E, type) * across < int64_t{1} << 31 &&
+           ((N + 127) / 128) * static_cast<int64_t>((K + 127) / 128) * E < int64_t{1} << 31;
 }
 
 size_t expert_plan_bytes(int64_t pairs, int E, int type) {
-    const int64_t tiles = pairs / expert_tile_rows(pairs, E, type) + (pairs < E ? pairs : E);
-    return static_cast<size_t>((16 * (1 + tiles) + 255) / 256 * 256 + (8 * pairs + 255) / 256 * 256);
+    return static_cast<size_t>((16 * (1 + most_tiles(pairs, E, type)) + 255) / 256 * 256 + (8 * pairs + 255) / 256 * 256);
 }
 
 ExpertPlan expert_plan_at(void *ws, int64_t pairs, int E, int type) {
-    const int64_t tiles = pairs / expert_tile_rows(pairs, E, type) + (pairs < E ? pairs : E);
     ExpertPlan p;
     p.tiles = static_cast<int32_t *>(ws);
-    p.pairs = past(p.tiles, (16 * (1 + tiles) + 255) / 256 * 256);
+    p.pairs = past(p.tiles, (16 * (1 + most_tiles(pairs, E, type)) + 255) / 256 * 256);
     p.tokens = past(p.pairs, 4 * pairs);
     return p;
 }
 
-hipError_t launch_expert_plan(const ExpertArgs &a, void *empty, int64_t ld, int cols, int size, hipStream_t s) {
+hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_t ld, int cols, int size, hipStream_t s) {
     const int64_t blocks = 1 + (a.pairs() + kPlanThreads - 1) / kPlanThreads;
-    hipLaunchKernelGGL(expert_plan_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kPlanThreads), 0, s, a,
-                       expert_tile_rows(a.pairs(), a.E, a.type), empty, ld * size, cols * size);
+    hipLaunchKernelGGL(expert_plan_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kPlanThreads), 0, s, a, rows, empty,
+                       ld * size, cols * size);
     return hipGetLastError();
 }
 
@@ -165,20 +173,21 @@ hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, c
 hipError_t launch_expert_linear(const ExpertLinearArgs &l, hipStream_t s) {
     const ExpertArgs &a = l.a;
     const int size = a.type == ISC_F32 ? 4 : 2, ysize = l.ytype == ISC_F32 ? 4 : 2;
-    if (hipError_t e = launch_expert_plan(a, l.combine ? nullptr : l.y, l.ldy, a.N, ysize, s); e != hipSuccess) return e;
+    const bool direct = tp::direct_rows(a.x, a.ldx, a.K, size) && tp::direct_rows(a.w, a.ldw, a.K, size);
+    const int rows = expert_tile_rows(a.pairs(), a.E, a.type, direct);
+    if (hipError_t e = launch_expert_plan(a, rows, l.combine ? nullptr : l.y, l.ldy, a.N, ysize, s); e != hipSuccess)
+        return e;
     tp::RowsArgs r{};
     r.plan = a.plan;
     r.x = {static_cast<const char *>(a.x), a.ldx * size, a.shared ? a.plan.tokens : a.plan.pairs, 0, a.K};
     r.w = {static_cast<const char *>(a.w), a.ldw * size, nullptr, a.N, a.K};
     r.expert = a.N * a.ldw * size;
-    r.listed = 1;
     r.inner = a.K;
     r.cols = a.N;
     r.out = l.combine ? l.part : l.y;
     r.ldo = l.combine ? expert_ld(a.N) : l.ldy;
     r.otype = l.combine ? ISC_F32 : l.ytype;
     r.relu = l.relu;
-    const bool direct = tp::direct_rows(a.x, a.ldx, a.K, size) && tp::direct_rows(a.w, a.ldw, a.K, size);
     if (hipError_t e = tp::launch_rows_by<tp::kAlong>(r, a.type, direct, a.pairs(), a.E, s); e != hipSuccess) return e;
     if (!l.combine) return hipSuccess;
     return launch_expert_sum(a, l.part, a.N, a.weights, l.y, l.ldy, l.ytype, s);

@@ -4,16 +4,18 @@
 // an odd polynomial of X's singular values that leaves its singular vectors as
 // they are and brings the values towards one.
 //
-// What is held how.  The state X is fp32: what a step adds to a small singular
-// direction is small beside the large ones, and every later step magnifies an
-// error there as it does the direction (3.4^5 = 480 in all), so a state in 16 bits
-// loses 2^-6 of a gradient with few strong directions.  The operands of the
-// products, X, A and b A + c A^2, are fp16, whose errors stay where the operand is
-// one factor among fp32 sums: 1e-3 at most of the result's norm, as much as its
-// own rounding to bf16 (fp64 against it: 704 x 2048, noise over 16 directions,
-// 1.1e-4; noise alone 1.5e-3).  Operands are scaled by 2^6 on their way to fp16,
-// which keeps entries of 2^-14 normal and any that the coefficients' check lets
-// through finite.
+// What is held how.  What a step adds to a small singular direction is small beside the
+// large ones, and every later step magnifies an error there as it does the direction
+// (3.4^5 = 480 in all), so a state of one fp16 or bf16 value loses 2^-6 of a gradient
+// with few strong directions.  The state X is held in 32 bits, as the fp16 value that the
+// products take and what that leaves, in fp16 as well: 22 bits in all, read and written
+// with 8 bytes an element and step where fp32 beside the operand takes 10.  The operands
+// of the products, X's first part, A and b A + c A^2, are fp16, whose errors stay where
+// the operand is one factor among fp32 sums: 1e-3 at most of the result's norm, as much
+// as its own rounding to bf16 (against fp64: 704 x 2048, noise over 16 directions,
+// 1.1e-4; noise alone 1.5e-3).  Operands are scaled by 2^6 on their way to fp16, which
+// keeps entries of 2^-14 normal and any that the coefficients' check lets through finite;
+// what they leave by 2^11 more.
 //
 // A and b A + c A^2 are symmetric: tiles on and below the diagonal are computed,
 // the others are their mirror images.  All matrices of a stack share each launch:
@@ -27,21 +29,43 @@ namespace {
 
 using namespace tp;
 
-constexpr float kUp = 64.0f;  // of every fp16 operand
+constexpr float kUp = 64.0f;     // of every fp16 operand
+constexpr float kLow = 2048.0f;  // of what a state's operand leaves, beyond that
 
 struct OrthProduct {
     OrthShape s;
-    Rows x, w;                      // the first matrix's
-    int64_t xhop, whop;             // bytes to the next one's
+    Rows x, w;              // the first matrix's
+    int64_t xhop, whop;     // bytes to the next one's
     int inner, rows, cols;
-    const uint16_t *square;         // A, where b A is added
-    uint16_t *out16;                // fp16 results
-    float *state;
-    void *o;                        // the last step's results
+    const uint16_t *from;   // A, where b A is added; the state's operand
+    uint16_t *to;           // A, b A + c A^2, or the next state's operand
+    uint16_t *low;          // what the state's operand leaves
+    const void *g;          // the first step's state is G, scaled
+    int64_t ldg;
+    int type;
+    const double *squares;
+    float eps;
+    void *o;                // the last step's results
     int64_t ldo;
     int otype;
     float a, b, c;
 };
+
+__device__ __forceinline__ void load8_as(float (&v)[8], const void *p, int64_t at, int n, int type) {
+    if (type == ISC_F32)
+        load8<F32>(v, static_cast<const float *>(p) + at, n);
+    else if (type == ISC_BF16)
+        load8<BF16>(v, static_cast<const uint16_t *>(p) + at, n);
+    else
+        load8<F16>(v, static_cast<const uint16_t *>(p) + at, n);
+}
+
+// 1 / (|G| + eps) of matrix n, from its parts' sums of squares.
+__device__ __forceinline__ double inverse_norm(const double *squares, int n, int blocks, float eps) {
+    double sum = 0.0;
+    for (int i = 0; i < blocks; ++i) sum += squares[n * blocks + i];
+    return 1.0 / (sqrt(sum) + static_cast<double>(eps));
+}
 
 // Sums of squares, in fp64: no gradient's square leaves its range.
 template <class T>
@@ -69,14 +93,12 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(const OrthArgs a) {
     if (threadIdx.x == 0) reinterpret_cast<double *>(a.ws)[blockIdx.y * gridDim.x + blockIdx.x] = sums[0];
 }
 
+// The first state's operand; the first step takes the state itself from G.
 template <class T>
 __global__ __launch_bounds__(256) void orth_scale_kernel(const OrthArgs a) {
     const OrthShape &s = a.s;
     const int64_t row0 = static_cast<int64_t>(blockIdx.y) * s.M;
-    double sum = 0.0;
-    for (int i = 0; i < s.blocks(); ++i) sum += reinterpret_cast<const double *>(a.ws)[blockIdx.y * s.blocks() + i];
-    const double by = 1.0 / (sqrt(sum) + static_cast<double>(a.eps));
-    float *state = reinterpret_cast<float *>(a.ws + s.state()) + blockIdx.y * s.of_state();
+    const double by = inverse_norm(reinterpret_cast<const double *>(a.ws), blockIdx.y, s.blocks(), a.eps);
     uint16_t *operand = reinterpret_cast<uint16_t *>(a.ws + s.operand(0)) + blockIdx.y * s.of_state();
     const int groups = s.np() / 8;
     const int64_t all = static_cast<int64_t>(s.M) * groups, hop = static_cast<int64_t>(gridDim.x) * 256;
@@ -87,10 +109,7 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(const OrthArgs a) {
         load8<T>(v, static_cast<const typename T::type *>(a.g) + (row0 + r) * a.ldg + c, s.N - c);
 #pragma unroll
         for (int q = 0; q < 8; ++q)  // 0 * inf is no zero behind the last column
-            v[q] = c + q < s.N ? static_cast<float>(static_cast<double>(v[q]) * by) : 0.0f;
-        store8<F32>(state + r * s.np() + c, v, 8);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= kUp;
+            v[q] = c + q < s.N ? static_cast<float>(static_cast<double>(v[q]) * by) * kUp : 0.0f;
         store8<F16>(operand + r * s.np() + c, v, 8);
     }
 }
@@ -98,93 +117,110 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(const OrthArgs a) {
 enum Product { kGram, kPoly, kApply };
 
 template <class TL, Product WHAT>
-__global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthProduct p) {
+__global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthProduct p, int total) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int id = of_xcd(blockIdx.x, gridDim.x);
-    const int down = (p.rows + TL::BI - 1) / TL::BI;
-    int n, ti, tj;
-    if constexpr (WHAT == kApply) {
-        const int across = (p.cols + TL::BJ - 1) / TL::BJ;
-        n = id / (down * across);
-        ti = id / across % down;
-        tj = id % across;
-    } else {
-        const int half = down * (down + 1) / 2;
-        n = id / half;
-        const int at = id % half;  // ti (ti + 1) / 2 + tj
-        ti = static_cast<int>((__builtin_sqrtf(8.0f * at + 1.0f) - 1.0f) * 0.5f);
-        if (ti * (ti + 1) / 2 > at) --ti;
-        if ((ti + 1) * (ti + 2) / 2 <= at) ++ti;
-        tj = at - ti * (ti + 1) / 2;
-    }
-    const int i0 = ti * TL::BI, j0 = tj * TL::BJ;
-    Rows x = p.x, w = p.w;
-    x.base += n * p.xhop;
-    w.base += n * p.whop;
+    const int down = (p.rows + TL::BI - 1) / TL::BI, across = (p.cols + TL::BJ - 1) / TL::BJ;
+    struct Job {
+        int n, i0, j0;
+    } job, next;
     TL t;
-    t.run(x, w, i0, j0, p.inner, p.rows - i0, p.cols - j0, lds);
-    if constexpr (WHAT == kApply) {
-        const int np = p.s.np();
-        float *state = p.state + n * p.s.of_state();
-        t.each([&](int, int i, int j, const f32x16 &sums) {
-            const int row = i0 + i, col = j0 + j;
-            if (row >= p.rows || col >= p.cols) return;
-            float *x = state + static_cast<int64_t>(row) * np + col;
-            f32x16 v;
+    const auto start = [&](int at) {
+        int id = of_xcd(at, total), ti, tj;
+        Job j;
+        if constexpr (WHAT == kApply) {
+            j.n = id / (down * across);
+            ti = id / across % down;
+            tj = id % across;
+        } else {
+            const int half = down * (down + 1) / 2;
+            j.n = id / half;
+            id %= half;  // ti (ti + 1) / 2 + tj
+            ti = static_cast<int>((__builtin_sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
+            if (ti * (ti + 1) / 2 > id) --ti;
+            if ((ti + 1) * (ti + 2) / 2 <= id) ++ti;
+            tj = id - ti * (ti + 1) / 2;
+        }
+        j.i0 = ti * TL::BI;
+        j.j0 = tj * TL::BJ;
+        Rows x = p.x, w = p.w;
+        x.base += j.n * p.xhop;
+        w.base += j.n * p.whop;
+        t.start(x, w, j.i0, j.j0, p.inner, lds);
+        return j;
+    };
+    int at = blockIdx.x;
+    job = start(at);
+    for (bool landed = false;; landed = true) {
+        t.sums(p.inner, p.rows - job.i0, p.cols - job.j0, landed, lds);
+        at += gridDim.x;
+        if (at < total) next = start(at);
+        if constexpr (WHAT == kApply) {
+            const int np = p.s.np();
+            const int64_t first = job.n * p.s.of_state();
+            const float by = p.g ? static_cast<float>(inverse_norm(p.squares, job.n, p.s.blocks(), p.eps) * kUp) : 0.0f;
+            t.template each<false>(
+                lds,
+                [&](int i, int j, const float (&sums)[8]) {
+                    const int row = job.i0 + i, col = job.j0 + j;
+                    if (row >= p.rows || col >= p.cols) return;
+                    const int64_t place = first + static_cast<int64_t>(row) * np + col;
+                    float x[8], v[8];
+                    if (p.g) {
+                        load8_as(x, p.g, (static_cast<int64_t>(job.n) * p.rows + row) * p.ldg + col, p.cols - col, p.type);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float u[8];
-                load8<F32>(u, x + 8 * q, np - col - 8 * q);
+                        for (int k = 0; k < 8; ++k) x[k] *= by;
+                    } else {
+                        float low[8];
+                        load8<F16>(x, p.from + place, 8);
+                        load8<F16>(low, p.low + place, 8);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    v[8 * q + k] = fmaf(p.a, u[k], sums[8 * q + k] * (1.0f / (kUp * kUp)));
-            }
-            if (p.o) {
-                const int64_t at = (static_cast<int64_t>(n) * p.rows + row) * p.ldo + col;
-                if (p.otype == ISC_BF16)
-                    store16<BF16>(static_cast<uint16_t *>(p.o) + at, v, p.cols - col);
-                else
-                    store16<F16>(static_cast<uint16_t *>(p.o) + at, v, p.cols - col);
-                return;
-            }
-            // behind the last column the operands' zeros made zeros, or another column's sums
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = col + k < p.cols ? v[k] : 0.0f;
-            store16<F32>(x, v, np - col);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] *= kUp;
-            store16<F16>(p.out16 + n * p.s.of_state() + static_cast<int64_t>(row) * np + col, v, np - col);
-        });
-    } else {
-        const int m = p.rows, mp = p.s.mp();
-        uint16_t *out = p.out16 + n * p.s.of_square();
-        const uint16_t *square = p.square + n * p.s.of_square();
-        t.each([&](int, int i, int j, const f32x16 &sums) {
-            const int row = i0 + i, col = j0 + j;
-            if (row >= mp || col >= mp) return;
-            f32x16 v;
-            if constexpr (WHAT == kGram) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) v[k] = sums[k] * (1.0f / kUp);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float u[8] = {};
-                    if (row < m) load8<F16>(u, square + static_cast<int64_t>(row) * mp + col + 8 * q, mp - col - 8 * q);
+                        for (int k = 0; k < 8; ++k) x[k] = fmaf(low[k], 1.0f / kLow, x[k]);
+                    }
+                    // x and what becomes of it are 2^6 times the state, the sums 2^12 times theirs;
+                    // behind the last column the operands' zeros made zeros, or another column's sums
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        v[8 * q + k] = fmaf(p.b, u[k], p.c * (sums[8 * q + k] * (1.0f / kUp)));
+                        v[k] = col + k < p.cols ? fmaf(p.a, x[k], sums[k] * (1.0f / kUp)) : 0.0f;
+                    if (p.o) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] *= 1.0f / kUp;
+                        store8_as(p.o, (static_cast<int64_t>(job.n) * p.rows + row) * p.ldo + col, v, p.cols - col,
+                                  p.otype);
+                        return;
+                    }
+                    float low[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) low[k] = (v[k] - F16::widen(F16::narrow(v[k]))) * kLow;
+                    store8<F16>(p.to + place, v, 8);
+                    store8<F16>(p.low + place, low, 8);
+                },
+                [](int, int, const float (&)[8]) {});
+        } else {
+            const int m = p.rows, mp = p.s.mp();
+            const int64_t first = job.n * p.s.of_square();
+            // A, or b A + c A^2: the 8 results of row r from column c on, zeros behind the last
+            const auto store = [&](int r, int c, const float (&sums)[8]) {
+                if (r >= m || c >= mp) return;
+                const int64_t place = first + static_cast<int64_t>(r) * mp + c;
+                float v[8], u[8];
+                if (WHAT == kPoly) load8<F16>(u, p.from + place, 8);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = sums[k] * (1.0f / kUp);
+                    if (WHAT == kPoly) v[k] = fmaf(p.b, u[k], p.c * v[k]);
+                    v[k] = c + k < m ? v[k] : 0.0f;
                 }
-            }
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = row < m && col + k < m ? v[k] : 0.0f;
-            if (row < m) store16<F16>(out + static_cast<int64_t>(row) * mp + col, v, mp - col);
-            if (ti != tj) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (col + k < m) store<F16>(out + static_cast<int64_t>(col + k) * mp + row, v[k]);
-            }
-        });
+                store8<F16>(p.to + place, v, 8);
+            };
+            const bool mirror = job.i0 != job.j0;
+            t.template each<true>(
+                lds, [&](int i, int j, const float (&v)[8]) { store(job.i0 + i, job.j0 + j, v); },
+                [&](int j, int i, const float (&v)[8]) {
+                    if (mirror) store(job.j0 + j, job.i0 + i, v);
+                });
+        }
+        if (at >= total) return;
+        job = next;
     }
 }
 
@@ -192,15 +228,20 @@ template <class TL, Product WHAT>
 hipError_t launch_product(const OrthProduct &p, hipStream_t s) {
     if (hipError_t e = allow_lds(orth_product_kernel<TL, WHAT>, TL::kLds); e != hipSuccess) return e;
     const int64_t down = (p.rows + TL::BI - 1) / TL::BI, across = (p.cols + TL::BJ - 1) / TL::BJ;
-    const int64_t grid = p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2);
-    hipLaunchKernelGGL((orth_product_kernel<TL, WHAT>), dim3(static_cast<unsigned>(grid)), dim3(TL::kThreads), TL::kLds,
-                       s, p);
+    const int64_t total = p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2);
+    hipLaunchKernelGGL((orth_product_kernel<TL, WHAT>),
+                       dim3(static_cast<unsigned>(total < kResident<TL> ? total : kResident<TL>)), dim3(TL::kThreads),
+                       TL::kLds, s, p, static_cast<int>(total));
     return hipGetLastError();
 }
 
+// Tiles of 256 x 256 where there are more than half as many as compute units.
 template <Side XS, Side WS, Product WHAT>
 hipError_t launch_tile(const OrthProduct &p, hipStream_t s) {
-    if constexpr (WHAT == kApply) return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s); else return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s);
+    const int64_t down = (p.rows + 255) / 256, across = (p.cols + 255) / 256;
+    if (p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2) > 128)
+        return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s);
+    return launch_product<Tile<F16, true, XS, WS, 128, 128, 2, 2>, WHAT>(p, s);
 }
 
 template <class T>
@@ -239,8 +280,8 @@ hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s) {
         p.rows = p.cols = m;
         p.xhop = p.whop = 2 * h.of_state();
         p.x = p.w = {x, int64_t{2} * np, nullptr, h.M, np};
-        p.out16 = square;
-        p.square = square;
+        p.to = square;
+        p.from = square;
         p.inner = h.wide() ? np : h.M;
         e = h.wide() ? launch_tile<kAlong, kAlong, kGram>(p, s) : launch_tile<kAcross, kAcross, kGram>(p, s);
         if (e != hipSuccess) return e;
@@ -248,14 +289,22 @@ hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s) {
         p.x = p.w = sq;
         p.xhop = p.whop = 2 * h.of_square();
         p.inner = mp;
-        p.out16 = poly;
+        p.to = poly;
         if ((e = launch_tile<kAlong, kAlong, kPoly>(p, s)) != hipSuccess) return e;
         const Rows pl{reinterpret_cast<const char *>(poly), int64_t{2} * mp, nullptr, m, mp};
         const Rows st{x, int64_t{2} * np, nullptr, h.M, np};
         p.rows = h.M;
         p.cols = h.N;
-        p.state = reinterpret_cast<float *>(a.ws + h.state());
-        p.out16 = reinterpret_cast<uint16_t *>(a.ws + h.operand((i + 1) & 1));
+        p.from = reinterpret_cast<const uint16_t *>(x);
+        p.to = reinterpret_cast<uint16_t *>(a.ws + h.operand((i + 1) & 1));
+        p.low = reinterpret_cast<uint16_t *>(a.ws + h.low());
+        if (i == 0) {
+            p.g = a.g;
+            p.ldg = a.ldg;
+            p.type = a.type;
+            p.squares = reinterpret_cast<const double *>(a.ws);
+            p.eps = a.eps;
+        }
         p.o = i + 1 == a.steps ? a.o : nullptr;
         p.ldo = a.ldo;
         p.otype = a.otype;

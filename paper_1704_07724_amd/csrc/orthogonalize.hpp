@@ -20,8 +20,8 @@ struct OrthShape {
         const int64_t n = (of_state() + 16383) / 16384;
         return static_cast<int>(n < 256 ? n : 256);
     }
-    __host__ __device__ int64_t state() const { return round(8 * static_cast<int64_t>(B) * blocks()); }
-    __host__ __device__ int64_t operand(int i) const { return state() + round(4 * B * of_state()) + i * round(2 * B * of_state()); }
+    __host__ __device__ int64_t low() const { return round(8 * static_cast<int64_t>(B) * blocks()); }
+    __host__ __device__ int64_t operand(int i) const { return low() + (1 + i) * round(2 * B * of_state()); }
     __host__ __device__ int64_t square(int i) const { return operand(2) + i * round(2 * B * of_square()); }
     int64_t bytes() const { return square(2); }
 };

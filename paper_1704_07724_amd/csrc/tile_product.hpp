@@ -70,6 +70,9 @@ __device__ __forceinline__ void land() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
+// This wavefront's LDS reads and writes are done; then all wavefronts'.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
 }
@@ -98,8 +101,10 @@ __device__ __forceinline__ void cut(float v, uint32_t &a, uint32_t &b, uint32_t 
 }
 
 // Stages of one operand: OUT outer indices (i or j) by BK inner ones.
-template <class T, bool DIRECT, Side SIDE, int OUT, int BK, int THREADS>
+// LISTED: rows across come by a list (rows along may have one or not).
+template <class T, bool DIRECT, Side SIDE, bool LISTED, int OUT, int BK, int THREADS>
 struct Stage {
+    static constexpr bool kFetch = SIDE == kAcross && LISTED;
     static constexpr bool kWide = std::is_same_v<T, F32>;
     static constexpr int kParts = kWide ? 3 : 1;
     static constexpr int kSize = kWide ? 4 : 2;
@@ -120,7 +125,7 @@ struct Stage {
     }
 
     const char *at[SIDE == kAlong ? kLoads : 1];  // kAlong: the rows' chunks at r = 0
-    int32_t next[SIDE == kAcross ? kLoads : 1];   // kAcross: the rows of the stage to be sent
+    int32_t next[kFetch ? kLoads : 1];            // the listed rows of the stage to be sent
     int line, col;                                // this thread's first LDS row, and the element its chunks begin at
     Rows rows;
     uint4 held[DIRECT ? 1 : kLoads][kWide ? 2 : 1];
@@ -145,11 +150,11 @@ struct Stage {
         } else {
             col += o0;
             at[0] = r.base + int64_t{col} * kSize;
-            fetch(0, tid);
+            if constexpr (kFetch) fetch(0, tid);
         }
     }
 
-    // kAcross: the rows of this thread's chunks of the stage from r0 on.  A wavefront's
+    // The listed rows of this thread's chunks of the stage from r0 on.  A wavefront's
     // loads take few rows each, whose numbers come by scalar loads: a vector load would
     // have to wait for every direct load sent before it.
     __device__ __forceinline__ void fetch(int r0, int tid) {
@@ -164,7 +169,7 @@ struct Stage {
 #pragma unroll
             for (int q = 0; q < kRows; ++q) {
                 const int r = first + n * kHop + q;
-                const int32_t number = r >= rows.count ? -1 : rows.list ? list[r] : r;
+                const int32_t number = r >= rows.count ? -1 : list[r];
                 row = own == q ? number : row;
             }
             next[n] = row;
@@ -177,8 +182,13 @@ struct Stage {
             there = rows.width - r0 - col;
             return at[n] + int64_t{r0} * kSize;
         } else {
-            there = next[n] < 0 ? 0 : rows.width - col;
-            return at[0] + int64_t{next[n]} * rows.stride;
+            int32_t row = r0 + line + n * kHop;
+            if constexpr (kFetch)
+                row = next[n];
+            else
+                row = row < rows.count ? row : -1;
+            there = row < 0 ? 0 : rows.width - col;
+            return at[0] + int64_t{row} * rows.stride;
         }
     }
 
@@ -217,7 +227,7 @@ struct Stage {
     __device__ __forceinline__ void send_all(int r0, uint32_t lds, int wave, int tid) {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) send(n, r0, lds, wave);
-        if constexpr (SIDE == kAcross) fetch(r0 + BK, tid);
+        if constexpr (kFetch) fetch(r0 + BK, tid);
     }
 
     // Puts what the registers hold into LDS.
@@ -279,7 +289,7 @@ struct Stage {
 // Loads through registers have two stages in LDS.  Direct loads have two of W and three
 // of X (160 KiB for 256 x 256, all of a compute unit's; 80 KiB for 128 x 128, so that
 // two workgroups fit): X's have more than a stage's time to land, W's most of one.
-template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_>
+template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, bool LISTED = false>
 struct Tile {
     using T = T_;
     static constexpr bool DIRECT = DIRECT_;
@@ -287,8 +297,8 @@ struct Tile {
     static constexpr int kWaves = WI * WJ, kThreads = 64 * kWaves;
     static constexpr int BK = std::is_same_v<T, F32> ? 32 : 64;
     static constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;
-    using XStage = Stage<T, DIRECT, XS, BI, BK, kThreads>;
-    using WStage = Stage<T, DIRECT, WS, BJ, BK, kThreads>;
+    using XStage = Stage<T, DIRECT, XS, LISTED, BI, BK, kThreads>;
+    using WStage = Stage<T, DIRECT, WS, LISTED, BJ, BK, kThreads>;
     static constexpr int kParts = XStage::kParts;
     static constexpr int kXBytes = XStage::kBytes * kParts, kWBytes = WStage::kBytes * kParts;
     static constexpr int kXStages = DIRECT ? 3 : 2;
@@ -340,13 +350,37 @@ struct Tile {
         return (wave + (kWaves == 8 ? wave / WJ * (WJ / 2) : 0)) % WJ * (BJ / WJ);
     }
 
-    // The sums of the tile at (i0, j0) over `inner` inner indices, of whose rows and columns
-    // the first `rows` and `cols` are asked for.  The operands of the
+    // Where stages are in LDS.
+    static __device__ __forceinline__ int w_at(int s) { return kXStages * kXBytes + (s & 1) * kWBytes; }
+    static __device__ __forceinline__ int x_next(int at) { return at + kXBytes < kXStages * kXBytes ? at + kXBytes : 0; }
+
+    XStage xs;
+    WStage ws;
+
+    // Sends the first loads of the tile at (i0, j0): direct ones of a stage of W and two of
+    // X.  Nothing reads LDS any more when this is called, but for what each() puts into the
+    // places that stay free.
+    __device__ __forceinline__ void start(const Rows &x, const Rows &w, int i0, int j0, int inner, char *lds) {
+        const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        if (inner <= 0) return;
+        xs.begin(x, i0, tid);
+        ws.begin(w, j0, tid);
+        if constexpr (DIRECT) {
+            const uint32_t base = lds_address(lds);
+            xs.send_all(0, base, wave, tid);
+            ws.send_all(0, base + w_at(0), wave, tid);
+            if (inner > BK) xs.send_all(BK, base + kXBytes, wave, tid);
+        }
+    }
+
+    // The sums of the tile that start() began, over `inner` inner indices, of whose rows and
+    // columns the first `rows` and `cols` are asked for.  The operands of the
     // next 16 are read ahead of the products of those at hand; a stage's last are in
     // registers when the wavefronts meet, so that behind the barrier its place is free.
     // Loads are sent one at a time between products: sent together they would hold the
     // wavefront, and the matrix cores with it, until the address unit has taken them.
-    __device__ __forceinline__ void run(const Rows &x, const Rows &w, int i0, int j0, int inner, int rows, int cols, char *lds) {
+    // landed: each() has waited for start()'s loads.
+    __device__ __forceinline__ void sums(int inner, int rows, int cols, bool landed, char *lds) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wi = part_i(), wj = part_j();
         const bool busy = wi < rows && wj < cols;
@@ -358,28 +392,19 @@ struct Tile {
                 for (int n = 0; n < 16; ++n) acc[j][i][n] = 0.0f;
         const int steps = (inner + BK - 1) / BK;
         if (steps <= 0) return;
-        XStage xs;
-        WStage ws;
-        xs.begin(x, i0, tid);
-        ws.begin(w, j0, tid);
         constexpr int kSteps16 = BK / 16;
         static_assert(kSteps16 % 2 == 0, "a stage's first operands are always at[0]");
         const uint32_t base = lds_address(lds);
-        const auto w_at = [](int s) { return kXStages * kXBytes + (s & 1) * kWBytes; };
         int x_now = 0;  // the place in LDS of this stage's X
-        const auto x_next = [](int at) { return at + kXBytes < kXStages * kXBytes ? at + kXBytes : 0; };
         if constexpr (DIRECT) {
-            xs.send_all(0, base, wave, tid);
-            ws.send_all(0, base + w_at(0), wave, tid);
-            if (steps > 1) {
-                xs.send_all(BK, base + kXBytes, wave, tid);
-                land<XStage::kLoads>();
-            } else {
+            if (landed)
+                meet();
+            else
                 land<0>();
-            }
         } else {
-            xs.send_all(0, 0, wave, tid);
-            ws.send_all(0, 0, wave, tid);
+            xs.send_all(0, base, wave, tid);
+            ws.send_all(0, base, wave, tid);
+            meet();
             xs.commit(lds, tid);
             ws.commit(lds + w_at(0), tid);
             land<0>();
@@ -446,49 +471,95 @@ struct Tile {
                     for (int n = 0; n < kProducts; ++n) send(n);
                 }
                 if constexpr (DIRECT) {
-                    if constexpr (WS == kAcross) if (kk == 0 && more) ws.fetch((s + 2) * BK, tid);
-                    if constexpr (XS == kAcross) if (kk == 1 && most) xs.fetch((s + 3) * BK, tid);
+                    if constexpr (WStage::kFetch) if (kk == 0 && more) ws.fetch((s + 2) * BK, tid);
+                    if constexpr (XStage::kFetch) if (kk == 1 && most) xs.fetch((s + 3) * BK, tid);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
             x_now = x_then;
         }
-        // no load into LDS may outlive its tile, and all of its reads are done before another's
+        // no load into LDS may outlive its tile, and all of its reads are done before the next one's
         land<0>();
     }
 
-    // out(f, i, j, v): 16 consecutive results of row i (this lane's f-th) from column j on, in
-    // the tile's own numbering; all of a row's, before the next row.
-    template <class Out>
-    __device__ __forceinline__ void each(Out &&out) {
+    // A wavefront's results pass through LDS, 32 rows at a time and in places that start()
+    // leaves free, so that a row's columns are 8 consecutive ones of consecutive lanes:
+    // stores are whole lines.  out(i, j, v): the 8 results of row i from column j on, of the
+    // tile's own numbering; turned(j, i, v): the 8 of column j from row i on, if MIRROR.
+    static constexpr int kCols = BJ / WJ, kChunks = kCols / 4, kLanes = kCols / 8;
+    static constexpr int kScratch = 32 * kCols * 4;
+    static_assert(!DIRECT || kWaves * kScratch <= kXBytes + kWBytes, "the places left free");
+    static_assert(kWaves * kScratch <= kLds && kXBytes % kScratch == 0, "whole wavefronts' places");
+    template <bool MIRROR, class Out, class Turned>
+    __device__ __forceinline__ void each(char *lds, Out &&out, Turned &&turned) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wi = part_i(), wj = part_j();
+        char *own;
+        if constexpr (DIRECT) {
+            const int at = wave * kScratch;
+            own = lds + (at < kXBytes ? 2 * kXBytes + at : 3 * kXBytes + kWBytes + at - kXBytes);
+        } else {
+            own = lds + wave * kScratch;
+        }
+        const auto place = [&](int row, int c) { return own + (row * kChunks + (c ^ (row & (kChunks - 1)))) * 16; };
 #pragma unroll
-        for (int i = 0; i < FI; ++i)
+        for (int i = 0; i < FI; ++i) {
+            // the last rows' stores are the only ones that follow start()'s loads unwaited for
+            if (i == FI - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
             for (int j = 0; j < FJ; ++j)
-                out(i, wi + 32 * i + (lane & 31), wj + 32 * j + 16 * (lane >> 5), acc[j][i]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4 *>(place(lane & 31, 8 * j + 4 * (lane >> 5) + q)) =
+                        make_float4(acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]);
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int r = 0; r < 32; r += 64 / kLanes) {
+                const int row = r + lane / kLanes, c = lane % kLanes * 2;
+                const float4 a = *reinterpret_cast<const float4 *>(place(row, c));
+                const float4 b = *reinterpret_cast<const float4 *>(place(row, c + 1));
+                const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                out(wi + 32 * i + row, wj + 4 * c, v);
+            }
+            if constexpr (MIRROR) {
+#pragma unroll 1
+                for (int c = 0; c < kCols; c += 64)
+#pragma unroll 1
+                    for (int r = 0; r < 32; r += 8) {
+                        const int col = c + lane % kCols;
+                        float v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            v[k] = reinterpret_cast<const float *>(place(r + k, col >> 2))[col & 3];
+                        turned(wj + col, wi + 32 * i + r, v);
+                    }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
     }
 };
 
-// The tile that workgroup `id` of `total` takes: workgroups are dealt to the 8
-// XCDs in turn, and each XCD gets consecutive tiles, which share operands in its L2.
+// Tile `id` in the order of the launch: workgroups are dealt to the 8 XCDs in turn, and
+// each XCD gets consecutive tiles, which share operands in its L2.
 __device__ __forceinline__ int of_xcd(int id, int total) {
     const int each = total >> 3, more = total & 7, x = id & 7;
     return x * each + (x < more ? x : more) + (id >> 3);
 }
 
-// 16 values to 16 or fewer places of a row.
-template <class T>
-__device__ __forceinline__ void store16(typename T::type *p, const f32x16 &v, int there) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        float u[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
-        if (there > 8 * q) store8<T>(p + 8 * q, u, there - 8 * q);
-    }
+// 8 values, or as many as there are places for, of a type known at run time.
+__device__ __forceinline__ void store8_as(void *p, int64_t at, const float (&v)[8], int there, int type) {
+    if (type == ISC_F32)
+        store8<F32>(static_cast<float *>(p) + at, v, there);
+    else if (type == ISC_BF16)
+        store8<BF16>(static_cast<uint16_t *>(p) + at, v, there);
+    else
+        store8<F16>(static_cast<uint16_t *>(p) + at, v, there);
 }
+
+// Workgroups that fill the chip's 256 compute units: tiles beyond them are taken in turn,
+// the next one's first loads on their way while a tile's results are stored.
+template <class TL>
+constexpr int kResident = 256 * (163840 / TL::kLds < 2 ? 1 : 163840 / TL::kLds < 4 ? 163840 / TL::kLds : 4);
 
 // LDS of a kernel beyond 64 KiB has to be asked for, once for each device: the
 // attribute belongs to the device's copy of the kernel.
