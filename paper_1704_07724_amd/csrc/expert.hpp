@@ -46,10 +46,10 @@ struct ExpertBwdArgs {
 
 // Leading dimension of rows in the workspace: 16-byte boundaries in every type.
 inline int64_t expert_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
-// Rows of a tile of the experts' pairs (direct: of operands that go into LDS by direct
-// loads), and the parts in which a row's dot products come.
-int expert_tile_rows(int64_t pairs, int E, int type, bool direct);
-int expert_dots(int64_t pairs, int E, int K, int type);
+// Rows of a tile of the experts' pairs for a product with `cols` columns (direct: of operands
+// that go into LDS by direct loads), and the parts in which a row's dot products come.
+int expert_tile_rows(int64_t pairs, int E, int cols, int type, bool direct);
+int expert_dots(int64_t pairs, int E, int K, int type, bool direct);
 size_t expert_plan_bytes(int64_t pairs, int E, int type);
 ExpertPlan expert_plan_at(void *ws, int64_t pairs, int E, int type);
 
@@ -67,6 +67,9 @@ hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_
 hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, const float *weights, void *out,
                              int64_t ldo, int type, hipStream_t s);
 hipError_t launch_expert_linear(const ExpertLinearArgs &a, hipStream_t s);
+// The same for few pairs (expert_few.hip): one launch, and a sum's; no plan.
+bool expert_few(int64_t pairs, int E, int type);
+hipError_t launch_expert_few(const ExpertLinearArgs &a, hipStream_t s);
 hipError_t launch_expert_bwd(const ExpertBwdArgs &a, hipStream_t s);
 
 namespace tp {
@@ -97,6 +100,11 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
     struct Job {
         int first, rows, j0;
     } job, next;
+    struct Beside {
+        int p;
+        float s;
+        Raw8<T> row;
+    };
     TL t;
     const auto start = [&](int n) {
         const int id = of_xcd(n, total);
@@ -119,29 +127,33 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
         if (n < total) next = start(n);
         t.template each<false>(
             lds,
-            [&](int i, int j, const float (&sums)[8]) {
-                const int p = i < job.rows ? a.plan.pairs[job.first + i] : -1;
-                const int there = a.cols - job.j0 - j;
+            [&](int i, int j) {
+                Beside b;
+                b.p = i < job.rows ? a.plan.pairs[job.first + i] : -1;
+                b.s = a.scale && b.p >= 0 ? a.scale[b.p] : 1.0f;
+                if (a.dotted)
+                    b.row.load(static_cast<const typename T::type *>(a.dotted) + (b.p < 0 ? 0 : b.p) / a.dot_slots * a.lddot +
+                                   job.j0 + j,
+                               b.p < 0 ? 0 : a.cols - job.j0 - j);
+                return b;
+            },
+            [&](int i, int j, const float (&sums)[8], const Beside &b) {
+                const int p = b.p, there = a.cols - job.j0 - j;
                 if (a.dotted) {
-                    float d = 0.0f;
-                    if (p >= 0 && there > 0) {
-                        float u[8];
-                        load8<T>(u, static_cast<const typename T::type *>(a.dotted) + p / a.dot_slots * a.lddot + job.j0 + j,
-                                 there);
+                    float u[8], d = 0.0f;
+                    b.row.widen(u);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) d = fmaf(k < there ? sums[k] : 0.0f, u[k], d);
-                    }
+                    for (int k = 0; k < 8; ++k) d = fmaf(k < there ? sums[k] : 0.0f, u[k], d);
 #pragma unroll
                     for (int by = 1; by < TL::kLanes; by *= 2) d += __shfl_xor(d, by);
                     if (j % TL::kCols == 0 && p >= 0 && there > 0)
                         a.dots[static_cast<int64_t>(p) * a.ndots + (job.j0 + j) / TL::kCols] = d;
                 }
                 if (p < 0 || there <= 0) return;
-                const float s = a.scale ? a.scale[p] : 1.0f;
                 float v[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    v[k] = sums[k] * s;
+                    v[k] = sums[k] * b.s;
                     if (a.relu) v[k] = v[k] < 0.0f ? 0.0f : v[k];  // a NaN stays
                 }
                 store8_as(a.out, p * a.ldo + job.j0 + j, v, there, a.otype);
@@ -166,22 +178,18 @@ hipError_t launch_rows(const RowsArgs &a, int64_t pairs, int E, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The tiles of 16- and 32-bit rows: few rows, or many.
 template <class T, bool DIRECT, Side WS>
 hipError_t launch_rows_of(const RowsArgs &a, int64_t pairs, int E, int rows, hipStream_t s) {
-    if constexpr (std::is_same_v<T, F32>) {
-        if (rows == 64) return launch_rows<Tile<T, false, kAlong, WS, 64, 128, 1, 4>>(a, pairs, E, s);
-        return launch_rows<Tile<T, false, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
-    } else {
+    if constexpr (DIRECT)
+        if (rows == 256) return launch_rows<Tile<T, true, kAlong, WS, 256, 256, 2, 4>>(a, pairs, E, s);
+    if constexpr (!std::is_same_v<T, F32>)
         if (rows == 32) return launch_rows<Tile<T, DIRECT, kAlong, WS, 32, 128, 1, 4>>(a, pairs, E, s);
-        if constexpr (DIRECT)
-            if (rows == 256) return launch_rows<Tile<T, true, kAlong, WS, 256, 256, 2, 4>>(a, pairs, E, s);
-        return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
-    }
+    if (rows == 64) return launch_rows<Tile<T, DIRECT, kAlong, WS, 64, 64, 2, 2>>(a, pairs, E, s);
+    return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
 }
 template <Side WS>
 hipError_t launch_rows_by(const RowsArgs &a, int type, bool direct, int64_t pairs, int E, hipStream_t s) {
-    const int rows = expert_tile_rows(pairs, E, type, direct);
+    const int rows = expert_tile_rows(pairs, E, a.cols, type, direct);
     if (type == ISC_F32) return launch_rows_of<F32, false, WS>(a, pairs, E, rows, s);
     if (type == ISC_BF16)
         return direct ? launch_rows_of<BF16, true, WS>(a, pairs, E, rows, s)

@@ -1,0 +1,140 @@
+// isc_expert_linear for few pairs an expert: a decoding step's.
+//
+// Each weight is read once and meets a handful of rows, so the time is that of
+// reading the met experts' matrices.  A workgroup takes 16 outputs of an expert and
+// up to 16 of its pairs at a time; its wavefronts share the inputs, and every lane
+// has its weights of 512 inputs on the way at once: neither LDS nor a first launch
+// that lists tiles stands in front of the reads.  The lists are read as they are.
+//
+// v_mfma_f32_16x16x32 (16 bits): lane l holds 8 r of row l % 16 of either operand.  Which
+// 8 is free as long as both agree, so a lane takes 16 consecutive inputs of a step of 64
+// in two loads, and the four lanes of a row a whole line.  fp32 takes v_mfma_f32_16x16x4
+// on the values as they are: the matrix cores have time.
+#include "expert.hpp"
+
+namespace isc {
+namespace {
+
+using namespace tp;
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+
+constexpr int kWaves = 4;
+
+template <class T>
+struct Few {
+    static constexpr bool kWide = std::is_same_v<T, F32>;
+    static constexpr int kStep = kWide ? 32 : 64;   // inputs of a step
+    static constexpr int kAhead = 8;                // steps on their way
+    static __device__ __forceinline__ f32x4 product(const Raw8<T> &w, const Raw8<T> &x, f32x4 c) {
+        if constexpr (kWide) {
+            const uint32_t a[8] = {w.a.x, w.a.y, w.a.z, w.a.w, w.b.x, w.b.y, w.b.z, w.b.w};
+            const uint32_t b[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+            return c;
+        } else if constexpr (std::is_same_v<T, BF16>) {
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.a), __builtin_bit_cast(bf16x8, x.a),
+                                                           c, 0, 0, 0);
+        } else {
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w.a), __builtin_bit_cast(f16x8, x.a), c,
+                                                          0, 0, 0);
+        }
+    }
+};
+
+template <class T>
+__global__ __launch_bounds__(64 * kWaves) void expert_few_kernel(const ExpertArgs a, void *out, int64_t ldo, int otype,
+                                                                 int relu, int zeros) {
+    using F = Few<T>;
+    using V = typename T::type;
+    constexpr int kEach = F::kWide ? 1 : 2;  // loads of a lane and step
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int e = blockIdx.y, n0 = blockIdx.x * 16, P = a.T * a.slots;
+    if (e == a.E) {  // the rows of pairs without an expert
+        if (!zeros) return;
+        for (int i = tid; i < P * 16; i += 64 * kWaves) {
+            const int p = i >> 4, n = n0 + (i & 15);
+            if (static_cast<unsigned>(a.ids[p]) >= static_cast<unsigned>(a.E) && n < a.N)
+                store_as(out, p * ldo + n, 0.0f, otype);
+        }
+        return;
+    }
+    const int lo = a.offsets[e], hi = a.offsets[e + 1];
+    const int first = lo < 0 ? 0 : lo > P ? P : lo, end = hi > P ? P : hi;
+    const int row = n0 + (lane & 15) < a.N ? n0 + (lane & 15) : a.N - 1;
+    const V *w = static_cast<const V *>(a.w) + (static_cast<int64_t>(e) * a.N + row) * a.ldw;
+    const int mine = lane >> 4;  // of the four parts of a step
+    // the inputs in kWaves parts of whole steps
+    const int steps = (a.K + F::kStep - 1) / F::kStep;
+    const int s0 = steps * wave / kWaves, s1 = steps * (wave + 1) / kWaves;
+    __shared__ f32x4 sums[kWaves - 1][64];
+    for (int at = first; at < end; at += 16) {
+        const int place = at + (lane & 15);
+        int p = place < end ? a.order[place] : -1;
+        if (p >= P) p = -1;
+        const V *x = static_cast<const V *>(a.x) + (p < 0 ? 0 : a.shared ? p / a.slots : p) * a.ldx;
+        f32x4 sum = {0, 0, 0, 0};
+        for (int s = s0; s < s1; s += F::kAhead) {
+            Raw8<T> wv[F::kAhead][kEach], xv[F::kAhead][kEach];
+#pragma unroll
+            for (int q = 0; q < F::kAhead; ++q)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int k = (s + q) * F::kStep + (mine * kEach + i) * 8;
+                    wv[q][i].load(w + k, s + q < s1 ? a.K - k : 0);
+                }
+#pragma unroll
+            for (int q = 0; q < F::kAhead; ++q)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int k = (s + q) * F::kStep + (mine * kEach + i) * 8;
+                    xv[q][i].load(x + k, s + q < s1 && p >= 0 ? a.K - k : 0);
+                }
+#pragma unroll
+            for (int q = 0; q < F::kAhead; ++q)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) sum = F::product(wv[q][i], xv[q][i], sum);
+        }
+        if (at > first) __syncthreads();  // the sums before are read
+        if (wave) sums[wave - 1][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && p >= 0) {
+#pragma unroll
+            for (int i = 0; i < kWaves - 1; ++i) sum += sums[i][lane];
+            const int n = n0 + 4 * mine;  // results 4 * (l / 16) .. + 4 of column l % 16
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = relu && sum[i] < 0.0f ? 0.0f : sum[i];  // a NaN stays
+                if (n + i < a.N) store_as(out, p * ldo + n + i, v, otype);
+            }
+        }
+    }
+}
+
+template <class T>
+hipError_t launch(const ExpertLinearArgs &l, hipStream_t s) {
+    const ExpertArgs &a = l.a;
+    const bool zeros = !l.combine;
+    hipLaunchKernelGGL(expert_few_kernel<T>,
+                       dim3(static_cast<unsigned>((a.N + 15) / 16), static_cast<unsigned>(a.E + (zeros ? 1 : 0))),
+                       dim3(64 * kWaves), 0, s, a, l.combine ? static_cast<void *>(l.part) : l.y,
+                       l.combine ? expert_ld(a.N) : l.ldy, l.combine ? static_cast<int>(ISC_F32) : l.ytype, l.relu, zeros);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Up to 4 pairs an expert on average, 8 in fp32 (64 experts of 1408 of 2048, 8 a token, us by
+// this kernel and by tiles: 16 tokens 63 and 77, 32 tokens 71 and 83, 64 tokens 85 and 85;
+// fp32 at 64 tokens 183 and 249).
+bool expert_few(int64_t pairs, int E, int type) { return pairs <= (type == ISC_F32 ? 8 : 4) * static_cast<int64_t>(E); }
+
+hipError_t launch_expert_few(const ExpertLinearArgs &l, hipStream_t s) {
+    const ExpertArgs &a = l.a;
+    const hipError_t e = a.type == ISC_F32 ? launch<F32>(l, s) : a.type == ISC_BF16 ? launch<BF16>(l, s) : launch<F16>(l, s);
+    if (e != hipSuccess || !l.combine) return e;
+    return launch_expert_sum(a, l.part, a.N, a.weights, l.y, l.ldy, l.ytype, s);
+}
+
+}  // namespace isc

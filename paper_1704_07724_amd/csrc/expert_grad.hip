@@ -97,7 +97,8 @@ __global__ __launch_bounds__(TL::kThreads) void expert_dw_kernel(const DwArgs a,
         auto *dw = static_cast<typename T::type *>(a.dw) + static_cast<int64_t>(job.e) * a.N * a.K;
         t.template each<false>(
             lds,
-            [&](int i, int j, const float (&v)[8]) {
+            [](int, int) { return 0; },
+            [&](int i, int j, const float (&v)[8], int) {
                 if (job.i0 + i < a.N && job.j0 + j < a.K)
                     store8<T>(dw + static_cast<int64_t>(job.i0 + i) * a.K + job.j0 + j, v, a.K - job.j0 - j);
             },
@@ -135,9 +136,14 @@ hipError_t launch_dw(const DwArgs &a, hipStream_t s) {
 }
 template <class T, bool DIRECT>
 hipError_t launch_dw_of(const DwArgs &a, hipStream_t s) {
+    const auto tiles = [&](int side) {
+        return static_cast<int64_t>(a.nexp) * ((a.N + side - 1) / side) * ((a.K + side - 1) / side);
+    };
+    const int side = tile_side(DIRECT ? tiles(256) : 0, tiles(128));
     if constexpr (DIRECT)
-        if (a.N > 128 && a.K > 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 256, 256, 2, 4, true>>(a, s);
-    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, 2, true>>(a, s);
+        if (side == 256) return launch_dw<Tile<T, true, kAcross, kAcross, 256, 256, 2, 4, true>>(a, s);
+    if (side == 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, 2, true>>(a, s);
+    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 64, 64, 2, 2, true>>(a, s);
 }
 
 template <class T>
@@ -150,8 +156,8 @@ hipError_t launch_mask(const ExpertBwdArgs &b, hipStream_t s) {
 
 }  // namespace
 
-int expert_dots(int64_t pairs, int E, int K, int type) {
-    const int cols = expert_tile_rows(pairs, E, type, false) >= 128 ? 64 : 32;  // of a wavefront
+int expert_dots(int64_t pairs, int E, int K, int type, bool direct) {
+    const int cols = expert_tile_rows(pairs, E, K, type, direct) >= 128 ? 64 : 32;  // of a wavefront
     return (K + cols - 1) / cols;
 }
 
@@ -163,7 +169,7 @@ ExpertBwdBytes expert_bwd_bytes(int T, int E, int N, int K, int slots, int type,
     b.part = b.masked + (relu || combine ? round(pairs * expert_ld(N) * (type == ISC_F32 ? 4 : 2)) : 0);
     // a call without dx has its rows there too
     b.dots = b.part + (combine || (shared && slots > 1) ? round(pairs * expert_ld(K) * 4) : 0);
-    b.all = b.dots + (combine ? round(pairs * expert_dots(pairs, E, K, type) * 4) : 0);
+    b.all = b.dots + (combine ? round(pairs * ((K + 31) / 32) * 4) : 0);
     return b;
 }
 
@@ -175,7 +181,7 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
     const int64_t ldm = expert_ld(a.N);
     const bool aligned_dy = direct_rows(b.dy, b.lddy, a.N, size), aligned_masked = direct_rows(b.masked, ldm, a.N, size);
     const bool direct = (b.y ? aligned_masked : aligned_dy) && direct_rows(a.w, a.ldw, a.K, size);
-    hipError_t e = launch_expert_plan(a, expert_tile_rows(a.pairs(), a.E, a.type, direct), b.dx && !sum ? b.dx : nullptr,
+    hipError_t e = launch_expert_plan(a, expert_tile_rows(a.pairs(), a.E, a.K, a.type, direct), b.dx && !sum ? b.dx : nullptr,
                                       b.lddx, a.K, size, s);
     if (e != hipSuccess) return e;
     // a sum's dx takes the gradient as it is (its own sums are weighted), a rectifier's takes it masked
@@ -203,7 +209,7 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
             r.lddot = a.ldx;
             r.dot_slots = a.shared ? a.slots : 1;
             r.dots = b.dots;
-            r.ndots = expert_dots(a.pairs(), a.E, a.K, a.type);
+            r.ndots = expert_dots(a.pairs(), a.E, a.K, a.type, direct);
         }
         e = launch_rows_by<kAcross>(r, a.type, direct, a.pairs(), a.E, s);
         if (e != hipSuccess) return e;

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const ExpertA
     }
 }
 
-// Four columns of a token a thread; loads of two slots in flight.
+// Four columns of a token a thread; eight slots' loads in flight.
 template <class T>
 __global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, const float *part, int cols, int64_t ld,
                                                          const float *weights, typename T::type *out, int64_t ldo) {
@@ -90,16 +90,25 @@ __global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, con
         const int64_t t = i / quads;
         const int c = static_cast<int>(i - t * quads) * 4;
         float4 sum = make_float4(0, 0, 0, 0);
-#pragma unroll 2
-        for (int j = 0; j < a.slots; ++j) {
-            const int64_t p = t * a.slots + j;
-            if (static_cast<unsigned>(a.ids[p]) >= static_cast<unsigned>(a.E)) continue;
-            const float w = weights ? weights[p] : 1.0f;
-            const float4 v = *reinterpret_cast<const float4 *>(part + p * ld + c);
-            sum.x = fmaf(w, v.x, sum.x);
-            sum.y = fmaf(w, v.y, sum.y);
-            sum.z = fmaf(w, v.z, sum.z);
-            sum.w = fmaf(w, v.w, sum.w);
+        for (int j0 = 0; j0 < a.slots; j0 += 8) {
+            float4 v[8];
+            float w[8];
+            bool there[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t p = t * a.slots + (j0 + j < a.slots ? j0 + j : j0);
+                v[j] = *reinterpret_cast<const float4 *>(part + p * ld + c);
+                there[j] = j0 + j < a.slots && static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E);
+                w[j] = weights ? weights[p] : 1.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!there[j]) continue;  // a row that nothing wrote
+                sum.x = fmaf(w[j], v[j].x, sum.x);
+                sum.y = fmaf(w[j], v[j].y, sum.y);
+                sum.z = fmaf(w[j], v[j].z, sum.z);
+                sum.w = fmaf(w[j], v[j].w, sum.w);
+            }
         }
         typename T::type *to = out + t * ldo + c;
         store<T>(to, sum.x);
@@ -111,37 +120,36 @@ __global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, con
 
 }  // namespace
 
-// By the rows that an expert has on average, of experts that can have any.  Tiles of 256 x
-// 256 need all of a compute unit's LDS and direct loads; TABLE
-int expert_tile_rows(int64_t pairs, int E, int type, bool direct) {
-    const int64_t of_one = pairs / (pairs < E ? pairs > 0 ? pairs : 1 : E);
-    if (type == ISC_F32) return of_one <= 64 ? 64 : 128;
-    return of_one <= 32 ? 32 : of_one < 128 || !direct ? 128 : 256;
+// By the rows that an expert has on average, of experts that can have any, and the tiles that
+// this makes.  Tiles of 256 x 256 need all of a compute unit's LDS, and direct loads.
+int expert_tile_rows(int64_t pairs, int E, int cols, int type, bool direct) {
+    const int64_t met = pairs < E ? pairs > 0 ? pairs : 1 : E, of_one = pairs / met;
+    if (of_one <= 32 && type != ISC_F32) return 32;
+    const auto tiles = [&](int side) { return met * ((of_one + side - 1) / side) * ((cols + side - 1) / side); };
+    return tp::tile_side(direct && of_one >= 128 ? tiles(256) : 0, tiles(128));
 }
 
 namespace {
 
 // Tiles of rows that there can be, whichever kernel runs.
-int64_t most_tiles(int64_t pairs, int E, int type) {
-    return pairs / expert_tile_rows(pairs, E, type, false) + (pairs < E ? pairs : E);
-}
+int64_t most_tiles(int64_t pairs, int E) { return pairs / 32 + (pairs < E ? pairs : E); }
 
 }  // namespace
 
 bool expert_launches_fit(int64_t pairs, int E, int N, int K, int type) {
-    const int64_t across = ((N > K ? N : K) + 127) / 128;
-    return most_tiles(pairs, E, type) * across < int64_t{1} << 31 &&
-           ((N + 127) / 128) * static_cast<int64_t>((K + 127) / 128) * E < int64_t{1} << 31;
+    const int64_t across = ((N > K ? N : K) + 63) / 64;
+    return most_tiles(pairs, E) * across < int64_t{1} << 31 &&
+           ((N + 63) / 64) * static_cast<int64_t>((K + 63) / 64) * E < int64_t{1} << 31;
 }
 
 size_t expert_plan_bytes(int64_t pairs, int E, int type) {
-    return static_cast<size_t>((16 * (1 + most_tiles(pairs, E, type)) + 255) / 256 * 256 + (8 * pairs + 255) / 256 * 256);
+    return static_cast<size_t>((16 * (1 + most_tiles(pairs, E)) + 255) / 256 * 256 + (8 * pairs + 255) / 256 * 256);
 }
 
 ExpertPlan expert_plan_at(void *ws, int64_t pairs, int E, int type) {
     ExpertPlan p;
     p.tiles = static_cast<int32_t *>(ws);
-    p.pairs = past(p.tiles, (16 * (1 + most_tiles(pairs, E, type)) + 255) / 256 * 256);
+    p.pairs = past(p.tiles, (16 * (1 + most_tiles(pairs, E)) + 255) / 256 * 256);
     p.tokens = past(p.pairs, 4 * pairs);
     return p;
 }
@@ -172,9 +180,10 @@ hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, c
 
 hipError_t launch_expert_linear(const ExpertLinearArgs &l, hipStream_t s) {
     const ExpertArgs &a = l.a;
+    if (expert_few(a.pairs(), a.E, a.type)) return launch_expert_few(l, s);
     const int size = a.type == ISC_F32 ? 4 : 2, ysize = l.ytype == ISC_F32 ? 4 : 2;
     const bool direct = tp::direct_rows(a.x, a.ldx, a.K, size) && tp::direct_rows(a.w, a.ldw, a.K, size);
-    const int rows = expert_tile_rows(a.pairs(), a.E, a.type, direct);
+    const int rows = expert_tile_rows(a.pairs(), a.E, a.N, a.type, direct);
     if (hipError_t e = launch_expert_plan(a, rows, l.combine ? nullptr : l.y, l.ldy, a.N, ysize, s); e != hipSuccess)
         return e;
     tp::RowsArgs r{};

@@ -49,16 +49,9 @@ struct OrthProduct {
     int64_t ldo;
     int otype;
     float a, b, c;
+    int parts;              // of A's sums, whose fp32 results go to `partial`
+    float *partial;
 };
-
-__device__ __forceinline__ void load8_as(float (&v)[8], const void *p, int64_t at, int n, int type) {
-    if (type == ISC_F32)
-        load8<F32>(v, static_cast<const float *>(p) + at, n);
-    else if (type == ISC_BF16)
-        load8<BF16>(v, static_cast<const uint16_t *>(p) + at, n);
-    else
-        load8<F16>(v, static_cast<const uint16_t *>(p) + at, n);
-}
 
 // 1 / (|G| + eps) of matrix n, from its parts' sums of squares.
 __device__ __forceinline__ double inverse_norm(const double *squares, int n, int blocks, float eps) {
@@ -121,18 +114,26 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int down = (p.rows + TL::BI - 1) / TL::BI, across = (p.cols + TL::BJ - 1) / TL::BJ;
     struct Job {
-        int n, i0, j0;
+        int n, i0, j0, part, inner;
     } job, next;
+    struct Beside {  // the state's two parts, or G's values
+        Raw8<F16> one, other;
+    };
     TL t;
     const auto start = [&](int at) {
-        int id = of_xcd(at, total), ti, tj;
+        int id = of_xcd(at, total), ti, tj, inner = p.inner;
         Job j;
+        j.part = 0;
         if constexpr (WHAT == kApply) {
             j.n = id / (down * across);
             ti = id / across % down;
             tj = id % across;
         } else {
             const int half = down * (down + 1) / 2;
+            if (WHAT == kGram) {
+                j.part = id % p.parts;
+                id /= p.parts;
+            }
             j.n = id / half;
             id %= half;  // ti (ti + 1) / 2 + tj
             ti = static_cast<int>((__builtin_sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
@@ -145,13 +146,28 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
         Rows x = p.x, w = p.w;
         x.base += j.n * p.xhop;
         w.base += j.n * p.whop;
-        t.start(x, w, j.i0, j.j0, p.inner, lds);
+        if (WHAT == kGram && p.parts > 1) {  // a range of whole stages of the inner indices
+            const int stages = (p.inner + TL::BK - 1) / TL::BK, from = stages * j.part / p.parts * TL::BK;
+            const int to = stages * (j.part + 1) / p.parts * TL::BK;
+            inner = (to < p.inner ? to : p.inner) - from;
+            if (TL::kXAcross) {
+                x.base += from * x.stride;
+                w.base += from * w.stride;
+                x.count = w.count = inner;
+            } else {
+                x.base += int64_t{2} * from;
+                w.base += int64_t{2} * from;
+                x.width = w.width = inner;
+            }
+        }
+        j.inner = inner;
+        t.start(x, w, j.i0, j.j0, inner, lds);
         return j;
     };
     int at = blockIdx.x;
     job = start(at);
     for (bool landed = false;; landed = true) {
-        t.sums(p.inner, p.rows - job.i0, p.cols - job.j0, landed, lds);
+        t.sums(job.inner, p.rows - job.i0, p.cols - job.j0, landed, lds);
         at += gridDim.x;
         if (at < total) next = start(at);
         if constexpr (WHAT == kApply) {
@@ -160,19 +176,45 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
             const float by = p.g ? static_cast<float>(inverse_norm(p.squares, job.n, p.s.blocks(), p.eps) * kUp) : 0.0f;
             t.template each<false>(
                 lds,
-                [&](int i, int j, const float (&sums)[8]) {
+                [&](int i, int j) {
+                    Beside b = {};
+                    const int row = job.i0 + i, col = job.j0 + j;
+                    if (row >= p.rows || col >= p.cols) return b;
+                    if (p.g) {
+                        const int64_t place = (static_cast<int64_t>(job.n) * p.rows + row) * p.ldg + col;
+                        if (p.type == ISC_F32) {
+                            Raw8<F32> g;
+                            g.load(static_cast<const float *>(p.g) + place, p.cols - col);
+                            b.one.a = g.a;
+                            b.other.a = g.b;
+                        } else {
+                            b.one.load(static_cast<const uint16_t *>(p.g) + place, p.cols - col);
+                        }
+                    } else {
+                        const int64_t place = first + static_cast<int64_t>(row) * np + col;
+                        b.one.load(p.from + place, 8);
+                        b.other.load(p.low + place, 8);
+                    }
+                    return b;
+                },
+                [&](int i, int j, const float (&sums)[8], const Beside &beside) {
                     const int row = job.i0 + i, col = job.j0 + j;
                     if (row >= p.rows || col >= p.cols) return;
                     const int64_t place = first + static_cast<int64_t>(row) * np + col;
                     float x[8], v[8];
                     if (p.g) {
-                        load8_as(x, p.g, (static_cast<int64_t>(job.n) * p.rows + row) * p.ldg + col, p.cols - col, p.type);
+                        if (p.type == ISC_F32)
+                            Raw8<F32>{beside.one.a, beside.other.a}.widen(x);
+                        else if (p.type == ISC_BF16)
+                            Raw8<BF16>{beside.one.a, {}}.widen(x);
+                        else
+                            beside.one.widen(x);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) x[k] *= by;
                     } else {
                         float low[8];
-                        load8<F16>(x, p.from + place, 8);
-                        load8<F16>(low, p.low + place, 8);
+                        beside.one.widen(x);
+                        beside.other.widen(low);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) x[k] = fmaf(low[k], 1.0f / kLow, x[k]);
                     }
@@ -198,25 +240,38 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
         } else {
             const int m = p.rows, mp = p.s.mp();
             const int64_t first = job.n * p.s.of_square();
-            // A, or b A + c A^2: the 8 results of row r from column c on, zeros behind the last
-            const auto store = [&](int r, int c, const float (&sums)[8]) {
-                if (r >= m || c >= mp) return;
-                const int64_t place = first + static_cast<int64_t>(r) * mp + c;
-                float v[8], u[8];
-                if (WHAT == kPoly) load8<F16>(u, p.from + place, 8);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = sums[k] * (1.0f / kUp);
-                    if (WHAT == kPoly) v[k] = fmaf(p.b, u[k], p.c * v[k]);
-                    v[k] = c + k < m ? v[k] : 0.0f;
-                }
-                store8<F16>(p.to + place, v, 8);
-            };
             const bool mirror = job.i0 != job.j0;
+            const auto store = [&](int row, int col, const float (&v)[8]) {
+                const int64_t place = first + static_cast<int64_t>(row) * mp + col;
+                if (WHAT == kGram && p.parts > 1)
+                    store8<F32>(p.partial + job.part * p.s.B * p.s.of_square() + place, v, 8);
+                else
+                    store8<F16>(p.to + place, v, 8);
+            };
             t.template each<true>(
-                lds, [&](int i, int j, const float (&v)[8]) { store(job.i0 + i, job.j0 + j, v); },
+                lds,
+                [&](int i, int j) {
+                    Raw8<F16> u = {};
+                    const int row = job.i0 + i, col = job.j0 + j;
+                    if (WHAT == kPoly && row < m && col < mp) u.load(p.from + first + static_cast<int64_t>(row) * mp + col, 8);
+                    return u;
+                },
+                // A, or b A + c A^2, zeros behind the last column
+                [&](int i, int j, float (&v)[8], const Raw8<F16> &beside) {
+                    const int row = job.i0 + i, col = job.j0 + j;
+                    float u[8];
+                    beside.widen(u);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        v[k] *= 1.0f / kUp;
+                        if (WHAT == kPoly) v[k] = fmaf(p.b, u[k], p.c * v[k]);
+                        v[k] = row < m && col + k < m ? v[k] : 0.0f;
+                    }
+                    if (row < m && col < mp) store(row, col, v);
+                },
                 [&](int j, int i, const float (&v)[8]) {
-                    if (mirror) store(job.j0 + j, job.i0 + i, v);
+                    const int row = job.j0 + j, col = job.i0 + i;
+                    if (mirror && row < m && col < mp) store(row, col, v);
                 });
         }
         if (at >= total) return;
@@ -224,24 +279,47 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
     }
 }
 
+// A from the parts of its sums, in their order.
+__global__ __launch_bounds__(256) void orth_join_kernel(const float *partial, int parts, int64_t n, uint16_t *to) {
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    if (i >= n) return;  // n is a multiple of 8
+    float sum[8] = {};
+#pragma unroll 4
+    for (int q = 0; q < parts; ++q) {
+        float v[8];
+        load8<F32>(v, partial + q * n + i, 8);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] += v[k];
+    }
+    store8<F16>(to + i, sum, 8);
+}
+
 template <class TL, Product WHAT>
 hipError_t launch_product(const OrthProduct &p, hipStream_t s) {
     if (hipError_t e = allow_lds(orth_product_kernel<TL, WHAT>, TL::kLds); e != hipSuccess) return e;
     const int64_t down = (p.rows + TL::BI - 1) / TL::BI, across = (p.cols + TL::BJ - 1) / TL::BJ;
-    const int64_t total = p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2);
+    const int64_t total = p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2 * (WHAT == kGram ? p.parts : 1));
     hipLaunchKernelGGL((orth_product_kernel<TL, WHAT>),
                        dim3(static_cast<unsigned>(total < kResident<TL> ? total : kResident<TL>)), dim3(TL::kThreads),
                        TL::kLds, s, p, static_cast<int>(total));
     return hipGetLastError();
 }
 
-// Tiles of 256 x 256 where there are more than half as many as compute units.
 template <Side XS, Side WS, Product WHAT>
 hipError_t launch_tile(const OrthProduct &p, hipStream_t s) {
-    const int64_t down = (p.rows + 255) / 256, across = (p.cols + 255) / 256;
-    if (p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2) > 128)
-        return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s);
-    return launch_product<Tile<F16, true, XS, WS, 128, 128, 2, 2>, WHAT>(p, s);
+    const auto tiles = [&](int side) {
+        const int64_t down = (p.rows + side - 1) / side, across = (p.cols + side - 1) / side;
+        return p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2);
+    };
+    const int side = WHAT == kGram && p.parts > 1 ? 64 : tile_side(tiles(256), tiles(128));
+    if (side == 256) return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s);
+    if (side == 128) return launch_product<Tile<F16, true, XS, WS, 128, 128, 2, 2>, WHAT>(p, s);
+    if (hipError_t e = launch_product<Tile<F16, true, XS, WS, 64, 64, 2, 2>, WHAT>(p, s); e != hipSuccess) return e;
+    if (WHAT != kGram || p.parts == 1) return hipSuccess;
+    const int64_t n = p.s.B * p.s.of_square();
+    hipLaunchKernelGGL(orth_join_kernel, dim3(static_cast<unsigned>((n / 8 + 255) / 256)), dim3(256), 0, s, p.partial,
+                       p.parts, n, p.to);
+    return hipGetLastError();
 }
 
 template <class T>
@@ -256,9 +334,9 @@ hipError_t launch_state(const OrthArgs &a, hipStream_t s) {
 }  // namespace
 
 bool orth_launches_fit(const OrthShape &s) {
-    const int64_t down = (s.M + 127) / 128, across = (s.N + 127) / 128, m = (s.m() + 127) / 128;
+    const int64_t down = (s.M + 63) / 64, across = (s.N + 63) / 64, m = (s.m() + 63) / 64;
     const int64_t most = down * across > m * (m + 1) / 2 ? down * across : m * (m + 1) / 2;
-    return s.B * most * 256 <= kLaunchThreads;
+    return s.B * most < int64_t{1} << 31;
 }
 
 hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s) {
@@ -283,6 +361,8 @@ hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s) {
         p.to = square;
         p.from = square;
         p.inner = h.wide() ? np : h.M;
+        p.parts = h.parts();
+        p.partial = reinterpret_cast<float *>(a.ws + h.partial());
         e = h.wide() ? launch_tile<kAlong, kAlong, kGram>(p, s) : launch_tile<kAcross, kAcross, kGram>(p, s);
         if (e != hipSuccess) return e;
         const Rows sq{reinterpret_cast<const char *>(square), int64_t{2} * mp, nullptr, m, mp};

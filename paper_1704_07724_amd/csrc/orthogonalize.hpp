@@ -23,7 +23,16 @@ struct OrthShape {
     __host__ __device__ int64_t low() const { return round(8 * static_cast<int64_t>(B) * blocks()); }
     __host__ __device__ int64_t operand(int i) const { return low() + (1 + i) * round(2 * B * of_state()); }
     __host__ __device__ int64_t square(int i) const { return operand(2) + i * round(2 * B * of_square()); }
-    int64_t bytes() const { return square(2); }
+    // Parts in which A's sums over the state's rows or columns are made, and added up after: where
+    // A has so few tiles that its inner indices in turn are the time.
+    int parts() const {
+        const int64_t side = (m() + 63) / 64, tiles = B * side * (side + 1) / 2, steps = ((wide() ? N : M) + 63) / 64;
+        if (tiles > 64 || steps < 8) return 1;
+        const int64_t most = 256 / tiles < steps / 2 ? 256 / tiles : steps / 2;
+        return static_cast<int>(most < 16 ? most : 16);
+    }
+    int64_t partial() const { return square(2); }
+    int64_t bytes() const { return partial() + (parts() > 1 ? round(4 * B * parts() * of_square()) : 0); }
 };
 
 struct OrthArgs {

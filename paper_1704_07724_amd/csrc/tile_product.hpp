@@ -77,6 +77,50 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
 }
 
+// Eight values as they are in memory, the first n of them and zeros: a load whose widening
+// can wait.
+template <class T>
+struct Raw8 {
+    static constexpr bool kWide = sizeof(typename T::type) == 4;
+    uint4 a, b;  // b: the upper four of 32-bit values
+    __device__ __forceinline__ void load(const void *from, int n) {
+        const char *p = static_cast<const char *>(from);
+        if (n >= 8) {
+            a = load_any<uint4>(p);
+            if constexpr (kWide) b = load_any<uint4>(p + 16);
+        } else if (n <= 0) {
+            a = make_uint4(0, 0, 0, 0);
+            if constexpr (kWide) b = a;
+        } else if constexpr (kWide) {
+            const auto one = [&](int i) { return i < n ? load_any<uint32_t>(p + 4 * i) : 0u; };
+            a = make_uint4(one(0), one(1), one(2), one(3));
+            b = make_uint4(one(4), one(5), one(6), one(7));
+        } else {
+            const auto two = [&](int i) {
+                const uint32_t low = i < n ? load_any<uint16_t>(p + 2 * i) : 0u;
+                return i + 1 < n ? low | static_cast<uint32_t>(load_any<uint16_t>(p + 2 * i + 2)) << 16 : low;
+            };
+            a = make_uint4(two(0), two(2), two(4), two(6));
+        }
+    }
+    static __device__ __forceinline__ void widen2(float &low, float &high, uint32_t w) {
+        low = T::widen(w & 0xffffu);
+        high = T::widen(w >> 16);
+    }
+    __device__ __forceinline__ void widen(float (&f)[8]) const {
+        if constexpr (kWide) {
+            f[0] = __uint_as_float(a.x), f[1] = __uint_as_float(a.y), f[2] = __uint_as_float(a.z);
+            f[3] = __uint_as_float(a.w), f[4] = __uint_as_float(b.x), f[5] = __uint_as_float(b.y);
+            f[6] = __uint_as_float(b.z), f[7] = __uint_as_float(b.w);
+        } else {
+            widen2(f[0], f[1], a.x);
+            widen2(f[2], f[3], a.y);
+            widen2(f[4], f[5], a.z);
+            widen2(f[6], f[7], a.w);
+        }
+    }
+};
+
 // One operand of a tile.  Rows of `width` elements, `stride` bytes apart.
 struct Rows {
     const char *base;
@@ -128,7 +172,7 @@ struct Stage {
     int32_t next[kFetch ? kLoads : 1];            // the listed rows of the stage to be sent
     int line, col;                                // this thread's first LDS row, and the element its chunks begin at
     Rows rows;
-    uint4 held[DIRECT ? 1 : kLoads][kWide ? 2 : 1];
+    Raw8<T> held[DIRECT ? 1 : kLoads];
 
     // o0: the tile's first outer index; inner: how many inner indices there are.
     __device__ __forceinline__ void begin(const Rows &r, int o0, int tid) {
@@ -192,23 +236,6 @@ struct Stage {
         }
     }
 
-    static __device__ __forceinline__ void masked(uint4 (&v)[kWide ? 2 : 1], const char *p, int there) {
-        uint32_t w[8];
-        if constexpr (kWide) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = i < there ? load_any<uint32_t>(p + 4 * i) : 0u;
-            v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            v[1] = make_uint4(w[4], w[5], w[6], w[7]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = 2 * i < there ? load_any<uint16_t>(p + 4 * i) : 0u;
-                if (2 * i + 1 < there) w[i] |= static_cast<uint32_t>(load_any<uint16_t>(p + 4 * i + 2)) << 16;
-            }
-            v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    }
-
     // Sends load n of the stage from r0 on; a direct one to LDS at `lds`.
     __device__ __forceinline__ void send(int n, int r0, uint32_t lds, int wave) {
         int there;
@@ -217,11 +244,8 @@ struct Stage {
             // width and column are multiples of 8: a chunk exists as a whole or not at all
             if (SIDE == kAcross || r0 + BK > rows.width) p = there > 0 ? p : reinterpret_cast<const char *>(kZeros);
             load_direct(p, lds + (n * THREADS + wave * 64) * 16);
-        } else if (there >= 8) {
-            held[n][0] = load_any<uint4>(p);
-            if constexpr (kWide) held[n][1] = load_any<uint4>(p + 16);
         } else {
-            masked(held[n], p, there);
+            held[n].load(p, there);
         }
     }
     __device__ __forceinline__ void send_all(int r0, uint32_t lds, int wave, int tid) {
@@ -237,10 +261,10 @@ struct Stage {
             for (int n = 0; n < kLoads; ++n) {
                 char *to = lds + (n * THREADS + tid) * 16;
                 if constexpr (!kWide) {
-                    *reinterpret_cast<uint4 *>(to) = held[n][0];
+                    *reinterpret_cast<uint4 *>(to) = held[n].a;
                 } else {
-                    const uint32_t v[8] = {held[n][0].x, held[n][0].y, held[n][0].z, held[n][0].w,
-                                           held[n][1].x, held[n][1].y, held[n][1].z, held[n][1].w};
+                    const uint32_t v[8] = {held[n].a.x, held[n].a.y, held[n].a.z, held[n].a.w,
+                                           held[n].b.x, held[n].b.y, held[n].b.z, held[n].b.w};
                     uint32_t part[3][4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -292,10 +316,10 @@ struct Stage {
 template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, bool LISTED = false>
 struct Tile {
     using T = T_;
-    static constexpr bool DIRECT = DIRECT_;
+    static constexpr bool DIRECT = DIRECT_, kXAcross = XS == kAcross;
     static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
     static constexpr int kWaves = WI * WJ, kThreads = 64 * kWaves;
-    static constexpr int BK = std::is_same_v<T, F32> ? 32 : 64;
+    static constexpr int BK = std::is_same_v<T, F32> && BI > 64 ? 32 : 64;
     static constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;
     using XStage = Stage<T, DIRECT, XS, LISTED, BI, BK, kThreads>;
     using WStage = Stage<T, DIRECT, WS, LISTED, BJ, BK, kThreads>;
@@ -484,14 +508,16 @@ struct Tile {
 
     // A wavefront's results pass through LDS, 32 rows at a time and in places that start()
     // leaves free, so that a row's columns are 8 consecutive ones of consecutive lanes:
-    // stores are whole lines.  out(i, j, v): the 8 results of row i from column j on, of the
-    // tile's own numbering; turned(j, i, v): the 8 of column j from row i on, if MIRROR.
+    // stores are whole lines.  ahead(i, j): what out() reads beside the 8 results of row i
+    // from column j on (of the tile's own numbering), sent for all of the 32 rows first;
+    // out(i, j, v, ahead), which leaves in v what, if MIRROR, turned(j, i, v) gets of
+    // column j, its 8 values from row i on.
     static constexpr int kCols = BJ / WJ, kChunks = kCols / 4, kLanes = kCols / 8;
     static constexpr int kScratch = 32 * kCols * 4;
     static_assert(!DIRECT || kWaves * kScratch <= kXBytes + kWBytes, "the places left free");
     static_assert(kWaves * kScratch <= kLds && kXBytes % kScratch == 0, "whole wavefronts' places");
-    template <bool MIRROR, class Out, class Turned>
-    __device__ __forceinline__ void each(char *lds, Out &&out, Turned &&turned) {
+    template <bool MIRROR, class Ahead, class Out, class Turned>
+    __device__ __forceinline__ void each(char *lds, Ahead &&ahead, Out &&out, Turned &&turned) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int wi = part_i(), wj = part_j();
         char *own;
@@ -504,6 +530,11 @@ struct Tile {
         const auto place = [&](int row, int c) { return own + (row * kChunks + (c ^ (row & (kChunks - 1)))) * 16; };
 #pragma unroll
         for (int i = 0; i < FI; ++i) {
+            constexpr int kRows = 64 / kLanes;  // of all lanes at a time
+            const int row = lane / kLanes, c = lane % kLanes * 2;
+            decltype(ahead(0, 0)) beside[32 / kRows];
+#pragma unroll
+            for (int r = 0; r < 32 / kRows; ++r) beside[r] = ahead(wi + 32 * i + r * kRows + row, wj + 4 * c);
             // the last rows' stores are the only ones that follow start()'s loads unwaited for
             if (i == FI - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
@@ -513,26 +544,28 @@ struct Tile {
                     *reinterpret_cast<float4 *>(place(lane & 31, 8 * j + 4 * (lane >> 5) + q)) =
                         make_float4(acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]);
             __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-            for (int r = 0; r < 32; r += 64 / kLanes) {
-                const int row = r + lane / kLanes, c = lane % kLanes * 2;
-                const float4 a = *reinterpret_cast<const float4 *>(place(row, c));
-                const float4 b = *reinterpret_cast<const float4 *>(place(row, c + 1));
-                const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                out(wi + 32 * i + row, wj + 4 * c, v);
+#pragma unroll
+            for (int r = 0; r < 32 / kRows; ++r) {
+                const float4 a = *reinterpret_cast<const float4 *>(place(r * kRows + row, c));
+                const float4 b = *reinterpret_cast<const float4 *>(place(r * kRows + row, c + 1));
+                float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                out(wi + 32 * i + r * kRows + row, wj + 4 * c, v, beside[r]);
+                if constexpr (MIRROR) {
+                    *reinterpret_cast<float4 *>(place(r * kRows + row, c)) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4 *>(place(r * kRows + row, c + 1)) = make_float4(v[4], v[5], v[6], v[7]);
+                }
             }
             if constexpr (MIRROR) {
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-                for (int c = 0; c < kCols; c += 64)
-#pragma unroll 1
-                    for (int r = 0; r < 32; r += 8) {
-                        const int col = c + lane % kCols;
-                        float v[8];
+                for (int r = 0; r < 32; r += 8) {  // a lane a column
+                    const int col = lane % kCols;
+                    float v[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            v[k] = reinterpret_cast<const float *>(place(r + k, col >> 2))[col & 3];
-                        turned(wj + col, wi + 32 * i + r, v);
-                    }
+                    for (int k = 0; k < 8; ++k)
+                        v[k] = reinterpret_cast<const float *>(place(r + k, col >> 2))[col & 3];
+                    turned(wj + col, wi + 32 * i + r, v);
+                }
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -555,6 +588,12 @@ __device__ __forceinline__ void store8_as(void *p, int64_t at, const float (&v)[
     else
         store8<F16>(static_cast<uint16_t *>(p) + at, v, there);
 }
+
+// The side of a launch's tiles, by how many of each there are (of 256, or 0 where they cannot
+// be taken; of 128): half of the compute units busy on tiles of 256 beat all on smaller ones,
+// which ask for twice the operands a product; below that a tile's steps in turn are the time,
+// and 64 x 64 has the shortest (777 x 1155, 3 matrices, GRAM a launch: SIDES).
+inline int tile_side(int64_t of256, int64_t of128) { return of256 > 128 ? 256 : of128 > 256 ? 128 : 64; }
 
 // Workgroups that fill the chip's 256 compute units: tiles beyond them are taken in turn,
 // the next one's first loads on their way while a tile's results are stored.
