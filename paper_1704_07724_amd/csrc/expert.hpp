@@ -185,7 +185,7 @@ hipError_t launch_rows_of(const RowsArgs &a, int64_t pairs, int E, int rows, hip
     if constexpr (!std::is_same_v<T, F32>)
         if (rows == 32) return launch_rows<Tile<T, DIRECT, kAlong, WS, 32, 128, 1, 4>>(a, pairs, E, s);
     if (rows == 64) return launch_rows<Tile<T, DIRECT, kAlong, WS, 64, 64, 2, 2>>(a, pairs, E, s);
-    return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, 2>>(a, pairs, E, s);
+    return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, kWavesOf128<T>>>(a, pairs, E, s);
 }
 template <Side WS>
 hipError_t launch_rows_by(const RowsArgs &a, int type, bool direct, int64_t pairs, int E, hipStream_t s) {

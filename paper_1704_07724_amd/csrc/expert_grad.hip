@@ -139,10 +139,10 @@ hipError_t launch_dw_of(const DwArgs &a, hipStream_t s) {
     const auto tiles = [&](int side) {
         return static_cast<int64_t>(a.nexp) * ((a.N + side - 1) / side) * ((a.K + side - 1) / side);
     };
-    const int side = tile_side(DIRECT ? tiles(256) : 0, tiles(128));
+    const int side = tile_side(DIRECT ? tiles(256) : 0, tiles(128), std::is_same_v<T, F32>);
     if constexpr (DIRECT)
         if (side == 256) return launch_dw<Tile<T, true, kAcross, kAcross, 256, 256, 2, 4, true>>(a, s);
-    if (side == 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, 2, true>>(a, s);
+    if (side == 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, kWavesOf128<T>, true>>(a, s);
     return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 64, 64, 2, 2, true>>(a, s);
 }
 
@@ -157,7 +157,7 @@ hipError_t launch_mask(const ExpertBwdArgs &b, hipStream_t s) {
 }  // namespace
 
 int expert_dots(int64_t pairs, int E, int K, int type, bool direct) {
-    const int cols = expert_tile_rows(pairs, E, K, type, direct) >= 128 ? 64 : 32;  // of a wavefront
+    const int cols = expert_tile_rows(pairs, E, K, type, direct) >= 128 && type != ISC_F32 ? 64 : 32;  // of a wavefront
     return (K + cols - 1) / cols;
 }
 

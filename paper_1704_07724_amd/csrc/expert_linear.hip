@@ -126,7 +126,7 @@ int expert_tile_rows(int64_t pairs, int E, int cols, int type, bool direct) {
     const int64_t met = pairs < E ? pairs > 0 ? pairs : 1 : E, of_one = pairs / met;
     if (of_one <= 32 && type != ISC_F32) return 32;
     const auto tiles = [&](int side) { return met * ((of_one + side - 1) / side) * ((cols + side - 1) / side); };
-    return tp::tile_side(direct && of_one >= 128 ? tiles(256) : 0, tiles(128));
+    return tp::tile_side(direct && of_one >= 128 ? tiles(256) : 0, tiles(128), type == ISC_F32);
 }
 
 namespace {

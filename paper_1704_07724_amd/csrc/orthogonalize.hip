@@ -311,7 +311,7 @@ hipError_t launch_tile(const OrthProduct &p, hipStream_t s) {
         const int64_t down = (p.rows + side - 1) / side, across = (p.cols + side - 1) / side;
         return p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2);
     };
-    const int side = WHAT == kGram && p.parts > 1 ? 64 : tile_side(tiles(256), tiles(128));
+    const int side = WHAT == kGram && p.parts > 1 ? 64 : tile_side(tiles(256), tiles(128), false);
     if (side == 256) return launch_product<Tile<F16, true, XS, WS, 256, 256, 2, 4>, WHAT>(p, s);
     if (side == 128) return launch_product<Tile<F16, true, XS, WS, 128, 128, 2, 2>, WHAT>(p, s);
     if (hipError_t e = launch_product<Tile<F16, true, XS, WS, 64, 64, 2, 2>, WHAT>(p, s); e != hipSuccess) return e;

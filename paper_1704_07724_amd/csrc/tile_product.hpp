@@ -130,18 +130,17 @@ struct Rows {
     int width;            // elements of a row
 };
 
-// fp32 values as three bf16 parts: the upper 16 bits, those of what is left, and
-// of what that leaves.  Cut, not rounded, so that the largest values stay finite;
-// a value that is not finite is its first part alone.
-__device__ __forceinline__ void cut(float v, uint32_t &a, uint32_t &b, uint32_t &c) {
-    const uint32_t u = __float_as_uint(v);
-    a = u >> 16;
-    const bool finite = (u & 0x7f800000u) != 0x7f800000u;
-    if (!finite && (u & 0xffffu)) a |= 1u;  // a NaN whose upper bits are an infinity's
-    const float r = finite ? v - __uint_as_float(u & 0xffff0000u) : 0.0f;
-    const uint32_t ur = __float_as_uint(r);
-    b = ur >> 16;
-    c = BF16::narrow(r - __uint_as_float(ur & 0xffff0000u));
+// Two fp32 values as three pairs of bf16 parts: the upper 16 bits, those of what is left,
+// and of what that leaves.  Cut, not rounded, so that the largest values stay finite and
+// 24 bits are all there.  Of a value that is not finite the second part is NaN.
+__device__ __forceinline__ void cut(uint32_t v0, uint32_t v1, uint32_t &a, uint32_t &b, uint32_t &c) {
+    const auto rest = [](uint32_t v) {
+        return __float_as_uint(__uint_as_float(v) - __uint_as_float(v & 0xffff0000u));
+    };
+    const uint32_t r0 = rest(v0), r1 = rest(v1);
+    a = __builtin_amdgcn_perm(v1, v0, 0x07060302u);  // the upper halves
+    b = __builtin_amdgcn_perm(r1, r0, 0x07060302u);
+    c = __builtin_amdgcn_perm(rest(r1), rest(r0), 0x07060302u);
 }
 
 // Stages of one operand: OUT outer indices (i or j) by BK inner ones.
@@ -267,14 +266,8 @@ struct Stage {
                                            held[n].b.x, held[n].b.y, held[n].b.z, held[n].b.w};
                     uint32_t part[3][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t a[2], b[2], c[2];
-                        cut(__uint_as_float(v[2 * i]), a[0], b[0], c[0]);
-                        cut(__uint_as_float(v[2 * i + 1]), a[1], b[1], c[1]);
-                        part[0][i] = a[0] | a[1] << 16;
-                        part[1][i] = b[0] | b[1] << 16;
-                        part[2][i] = c[0] | c[1] << 16;
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        cut(v[2 * i], v[2 * i + 1], part[0][i], part[1][i], part[2][i]);
 #pragma unroll
                     for (int q = 0; q < 3; ++q)
                         *reinterpret_cast<uint4 *>(to + q * kBytes) =
@@ -589,11 +582,22 @@ __device__ __forceinline__ void store8_as(void *p, int64_t at, const float (&v)[
         store8<F16>(static_cast<uint16_t *>(p) + at, v, there);
 }
 
+// Wavefronts that share a 128 x 128 tile's columns.  fp32 has eight in all: one of a SIMD's
+// two cuts values while the other's products run (2048 tokens through 2 of 8 experts of
+// 1408 of 2048, 232 us with four wavefronts, 187 with eight).
+template <class T>
+constexpr int kWavesOf128 = std::is_same_v<T, F32> ? 4 : 2;
+
 // The side of a launch's tiles, by how many of each there are (of 256, or 0 where they cannot
-// be taken; of 128): half of the compute units busy on tiles of 256 beat all on smaller ones,
-// which ask for twice the operands a product; below that a tile's steps in turn are the time,
-// and 64 x 64 has the shortest (777 x 1155, 3 matrices, GRAM a launch: SIDES).
-inline int tile_side(int64_t of256, int64_t of128) { return of256 > 128 ? 256 : of128 > 256 ? 128 : 64; }
+// be taken; of 128).  Half of the compute units busy on tiles of 256 beat all on smaller ones,
+// which ask for twice the operands a product.  Where there are few tiles one's steps in turn
+// are the time, and those of 64 x 64 are the shortest (us by 128 and by 64: 3 matrices of 777 x
+// 1155, the whole call, 320 and 244; 777 tokens of 1155 through 2 of 7 experts of 515, fp32, 98
+// and 47); fp32's tiles of 128 pay from fewer on, since one of them fills a compute unit (1024
+// tokens of 2048 through 2 of 8 experts of 1408, 192 tiles: 109 and 145).
+inline int tile_side(int64_t of256, int64_t of128, bool wide) {
+    return of256 > 128 ? 256 : of128 > (wide ? 96 : 256) ? 128 : 64;
+}
 
 // Workgroups that fill the chip's 256 compute units: tiles beyond them are taken in turn,
 // the next one's first loads on their way while a tile's results are stored.
