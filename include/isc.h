@@ -635,10 +635,10 @@ int isc_expert_linear_workspace_size(const isc_expert_desc *d, int32_t T, int32_
  *     NULL unless combine); an id outside [0, E) is an empty slot.
  *   y_type: ISC_F32, ISC_F16 or ISC_BF16.
  *   ws: isc_expert_linear_workspace_size bytes, 256-byte aligned.
- * fp32 operands are cut into three bfloat16 parts each, six of whose nine products
- * are kept: fp32's precision for magnitudes from 2^-110 on (bits below 2^-133 are
- * lost); an input that is not finite makes the sums that it enters not finite
- * (NaN where fp32 may have an infinity).
+ * Sums are fp32.  Of fp32 operands, cut into three bfloat16 parts each, six of the
+ * nine products are kept (the others come to 2^-21 of a term at most, 2^-24 on
+ * average), and bits below 2^-133 are lost; an input that is not finite makes the
+ * sums that it enters not finite (NaN where fp32 may have an infinity).
  * Deterministic.  Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_expert_linear(const isc_expert_desc *d, const void *w, int64_t ldw, int32_t T, const void *x, int64_t ldx,
                       const int32_t *ids, const float *weights, const int32_t *offsets, const int32_t *order, void *y,
@@ -681,11 +681,12 @@ int isc_orthogonalize_workspace_size(int32_t B, int32_t M, int32_t N, size_t *by
  *     singular values from [0, 1] within [0, 16] in magnitude after every step (else ARG).
  *   o: B*M rows of N values of o_type (ISC_F16 or ISC_BF16), ldo elements apart.
  *   ws: isc_orthogonalize_workspace_size bytes, 256-byte aligned.
- * The state X and all sums are fp32; the products' operands X, A and b A + c A A are
+ * The state X is held in 32 bits (two fp16 values, 22 significant bits, entries below
+ * 2^-41 are 0) and all sums are fp32; the products' operands X, A and b A + c A A are
  * fp16, so o is within about 2e-3 of the exact result in the 2-norm, relative to it,
  * before its own rounding.  A matrix with a value that is not finite becomes NaN, one
  * of zeros stays (with eps > 0); others of the stack are not affected.
- * Three launches a step and two before.  Deterministic.
+ * Three launches a step, four where A is small and X long, and two before.  Deterministic.
  * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_orthogonalize(int32_t B, int32_t M, int32_t N, int32_t type, const void *g, int64_t ldg, int32_t steps,
                       const float *coefficients, float eps, void *o, int32_t o_type, int64_t ldo, void *ws,

@@ -171,7 +171,7 @@ inline bool direct_rows(const void *p, int64_t ld, int width, int size) {
 
 template <class TL>
 hipError_t launch_rows(const RowsArgs &a, int64_t pairs, int E, hipStream_t s) {
-    if (hipError_t e = allow_lds(expert_rows_kernel<TL>, TL::kLds); e != hipSuccess) return e;
+    if (hipError_t e = allow_lds<expert_rows_kernel<TL>>(TL::kLds); e != hipSuccess) return e;
     const int64_t tiles = pairs / TL::BI + (pairs < E ? pairs : E);  // as many as there can be
     const int64_t all = tiles * ((a.cols + TL::BJ - 1) / TL::BJ), grid = all < kResident<TL> ? all : kResident<TL>;
     hipLaunchKernelGGL(expert_rows_kernel<TL>, dim3(static_cast<unsigned>(grid)), dim3(TL::kThreads), TL::kLds, s, a);

@@ -128,7 +128,7 @@ hipError_t launch_zero_dw(const ExpertBwdArgs &b, hipStream_t s) {
 
 template <class TL>
 hipError_t launch_dw(const DwArgs &a, hipStream_t s) {
-    if (hipError_t e = allow_lds(expert_dw_kernel<TL>, TL::kLds); e != hipSuccess) return e;
+    if (hipError_t e = allow_lds<expert_dw_kernel<TL>>(TL::kLds); e != hipSuccess) return e;
     const int64_t grid = static_cast<int64_t>((a.N + TL::BI - 1) / TL::BI) * ((a.K + TL::BJ - 1) / TL::BJ) * a.nexp;
     hipLaunchKernelGGL(expert_dw_kernel<TL>, dim3(static_cast<unsigned>(grid < kResident<TL> ? grid : kResident<TL>)),
                        dim3(TL::kThreads), TL::kLds, s, a, static_cast<int>(grid));

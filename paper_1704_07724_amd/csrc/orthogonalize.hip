@@ -296,7 +296,7 @@ __global__ __launch_bounds__(256) void orth_join_kernel(const float *partial, in
 
 template <class TL, Product WHAT>
 hipError_t launch_product(const OrthProduct &p, hipStream_t s) {
-    if (hipError_t e = allow_lds(orth_product_kernel<TL, WHAT>, TL::kLds); e != hipSuccess) return e;
+    if (hipError_t e = (allow_lds<orth_product_kernel<TL, WHAT>>(TL::kLds)); e != hipSuccess) return e;
     const int64_t down = (p.rows + TL::BI - 1) / TL::BI, across = (p.cols + TL::BJ - 1) / TL::BJ;
     const int64_t total = p.s.B * (WHAT == kApply ? down * across : down * (down + 1) / 2 * (WHAT == kGram ? p.parts : 1));
     hipLaunchKernelGGL((orth_product_kernel<TL, WHAT>),

@@ -12,9 +12,9 @@
 //     through registers; chunks past an edge come from a block of zeros, or are
 //     masked, so that nothing outside of an operand is read.
 //   - fp32 operands are cut into three bf16 parts on their way into LDS, and six
-//     of the nine products of parts are kept (the others are below 2^-24 of the
-//     largest): fp32's precision at a sixth of the bf16 rate, which is 2.6 times
-//     that of the fp32 matrix instruction.
+//     of the nine products of parts are kept.  The others come to 2^-24 of a term
+//     on average and to 2^-21 at most: fp32's precision at a sixth of the bf16
+//     rate, which is 2.6 times that of the fp32 matrix instruction.
 //
 // v_mfma_f32_32x32x16: lane l holds 8 consecutive r (from 8 * (l / 32)) of row
 // l % 32 of each operand; of the result, column l % 32 and the rows
@@ -606,15 +606,15 @@ constexpr int kResident = 256 * (163840 / TL::kLds < 2 ? 1 : 163840 / TL::kLds <
 
 // LDS of a kernel beyond 64 KiB has to be asked for, once for each device: the
 // attribute belongs to the device's copy of the kernel.
-template <class F>
-hipError_t allow_lds(F *kernel, int bytes) {
+template <auto *KERNEL>
+hipError_t allow_lds(int bytes) {
     static uint64_t done = 0;  // a bit for each of the first 64 devices
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
     const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
     if (__atomic_load_n(&done, __ATOMIC_RELAXED) & bit) return hipSuccess;
     const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == hipSuccess) __atomic_fetch_or(&done, bit, __ATOMIC_RELAXED);
     return e;
 }

@@ -1,0 +1,597 @@
+"""The operators that train a routed block on the GPU against their 64-bit forms.
+
+Tolerances, from the arithmetic (u: half a unit in the last place of the
+output's type relative to the value, 2^-24, 2^-11, 2^-8; e = 2^-24; size: the sum
+of the magnitudes of an output's terms):
+  products    n terms: (n + 64) e size for any order of fp32 additions and the
+              matrix cores' aligned ones, in fp32 8 e size more for the products
+              of parts that are left out, plus u |y|.  A sum over k slots: k e size.
+  dw          of a sum under weights: u size more, each weighted gradient being
+              rounded to its type
+  dweights    a dot product of K terms, each a sum over N: (N + K + 64) e size
+  orth        the 64-bit form with operands rounded to fp16 errs by some d in the
+              2-norm; other roundings (fp32 sums, the state's 22 bits) make others of
+              the same size: 3 d, plus u |o| for the output
+"""
+import ctypes
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import train
+
+pytestmark = pytest.mark.gpu
+
+E24 = 2.0 ** -24
+U = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+TYPES = ["float32", "float16", "bfloat16"]
+TINY = 2.0 ** -25  # half a step of the smallest fp16 numbers
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available()
+    return t
+
+
+@pytest.fixture(scope="module")
+def isc(torch):
+    import paper_1704_07724_amd as m
+    m.lib()
+    return m
+
+
+@pytest.fixture(autouse=True)
+def said(request):
+    print("[case]", request.node.name, flush=True)
+    sys.stdout.flush()
+
+
+def host(t):
+    return t.cpu().double().numpy() if t.dtype.is_floating_point else t.cpu().numpy()
+
+
+def dev(torch, a, dtype="float32"):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(getattr(torch, dtype)).cuda()
+
+
+def close(got, want, size, dtype, what):
+    """|got - want| <= size + u |want|."""
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    ok = np.abs(got - want) <= size + U[dtype] * np.abs(want) + TINY * (dtype == "float16")
+    if not ok.all():
+        i = tuple(np.argwhere(~ok)[0])
+        raise AssertionError("%s: %d of %d off; first at %s: %r, not %r within %g" % (what, (~ok).sum(), ok.size, i, got[i], want[i],
+                                                                                     np.broadcast_to(size, ok.shape)[i]))
+
+
+def route(torch, isc, seed, T, k, E, empty=0.0, only=None):
+    """(Route, ids): each slot another expert, some slots empty; only: the experts that are asked for."""
+    r = np.random.default_rng(seed)
+    among = np.arange(E) if only is None else np.asarray(only)
+    ids = np.stack([r.permutation(among)[:k] for _ in range(T)]).astype(np.int32) if T else np.zeros((0, k), np.int32)
+    ids[r.random(ids.shape) < empty] = -1
+    weights = (r.random(ids.shape) * (ids >= 0)).astype(np.float32)
+    offsets, order = train.lists(ids, E)
+    return isc.Route(*(torch.from_numpy(v).cuda() for v in (ids, weights, offsets, order))), ids
+
+
+def operands(torch, seed, T, k, E, K, N, dtype, shared, rectified=False):
+    r = np.random.default_rng(seed + 1000)
+    x = r.standard_normal((T, K) if shared else (T, k, K))
+    x = np.maximum(x, 0) if rectified else x
+    return dev(torch, x, dtype), dev(torch, r.standard_normal((E, N, K)) * K ** -0.5, dtype)
+
+
+def check_linear(torch, isc, T, k, E, K, N, dtype, relu=False, combine=False, shared=True, empty=0.1, out=None, only=None, seed=0):
+    rt, ids = route(torch, isc, seed, T, k, E, empty, only)
+    x, w = operands(torch, seed, T, k, E, K, N, dtype, shared, combine)
+    got = isc.isc_expert_linear(x, w, rt, relu=relu, combine=combine, dtype=None if out is None else getattr(torch, out))
+    want, size = train.expert_linear(host(x), host(w), ids, relu, host(rt.weights) if combine else None)
+    out = out or dtype
+    assert str(got.dtype) == "torch." + out
+    close(host(got), want, (K + 64 + k * combine + 8 * (dtype == "float32")) * E24 * size, out, "y")
+    if not combine:
+        assert (host(got)[ids < 0] == 0).all()
+    again = isc.isc_expert_linear(x, w, rt, relu=relu, combine=combine, dtype=getattr(torch, out))
+    assert torch.equal(got, again)
+
+
+# T, k, E, K, N: one pair, few, tiles of 32, 64, 128 and 256 rows; widths within, on and past a tile's and a step's
+SHAPES = [(1, 1, 1, 1, 1), (1, 2, 5, 33, 17), (3, 2, 4, 64, 64), (5, 3, 3, 70, 130), (40, 2, 3, 96, 40), (70, 2, 2, 64, 128),
+          (90, 1, 2, 65, 33), (150, 2, 3, 136, 72), (33, 4, 64, 128, 96)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("form", ["relu", "combine"])
+def test_linear(torch, isc, shape, dtype, form):
+    check_linear(torch, isc, *shape, dtype, relu=form == "relu", combine=form == "combine", shared=form == "relu")
+
+
+@pytest.mark.parametrize("dtype,out", [("bfloat16", "float32"), ("float16", "bfloat16"), ("float32", "float16")])
+@pytest.mark.parametrize("shape", [(3, 2, 4, 40, 20), (200, 2, 2, 72, 48)], ids=str)
+def test_linear_of_another_type_and_layout(torch, isc, shape, dtype, out):
+    check_linear(torch, isc, *shape, dtype, shared=False, out=out)
+    check_linear(torch, isc, *shape, dtype, combine=True, shared=True, out=out)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("K", [64, 128, 192, 264, 328])
+def test_linear_by_the_largest_tiles(torch, isc, K, dtype):
+    """One stage of inputs, two, three, and ends within one; experts with less than a tile's rows, more, and none."""
+    T, E, N = 1500, 4, 264
+    rt, ids = route(torch, isc, K, T, 2, E, 0.05, only=[0, 1, 3])
+    ids = ids.copy()
+    ids[40:] = np.where(ids[40:] == 3, 1 - ids[40:, ::-1].clip(0, 1), ids[40:])  # expert 3: a few rows
+    offsets, order = train.lists(ids, E)
+    rt = isc.Route(dev(torch, ids, "int32"), rt.weights, dev(torch, offsets, "int32"), dev(torch, order, "int32"))
+    x, w = operands(torch, K, T, 2, E, K, N, dtype, True)
+    # enough columns of tiles that the rule takes 256 x 256: the matrix repeated
+    w = w.repeat(1, 40, 1)[:, : 40 * N]
+    got = host(isc.isc_expert_linear(x, w, rt, relu=True))
+    want, size = train.expert_linear(host(x), host(w[:, :N]), ids, True)
+    for i in (0, 17, 39):
+        close(got[..., i * N:(i + 1) * N], want, (K + 64) * E24 * size, dtype, "y, columns %d" % i)
+    first = got[..., :N]
+    assert all((got[..., i * N:(i + 1) * N] == first).all() for i in range(40))
+
+
+def test_linear_with_experts_left_out(torch, isc):
+    for dtype in TYPES:
+        check_linear(torch, isc, 60, 2, 9, 72, 40, dtype, only=[2, 8])
+        check_linear(torch, isc, 2, 2, 9, 72, 40, dtype, only=[2, 8], empty=0.0)
+    check_linear(torch, isc, 50, 2, 3, 64, 64, "bfloat16", empty=1.0)
+    check_linear(torch, isc, 50, 2, 3, 64, 64, "bfloat16", empty=1.0, combine=True)
+
+
+def check_bwd(torch, isc, T, k, E, K, N, dtype, form, shared, empty=0.1, only=None, seed=0):
+    rt, ids = route(torch, isc, seed, T, k, E, empty, only)
+    combine = form == "combine"
+    x, w = operands(torch, seed, T, k, E, K, N, dtype, shared, combine)
+    y = isc.isc_expert_linear(x, w, rt, relu=True) if form == "relu" else None
+    dy = dev(torch, np.random.default_rng(seed + 7).standard_normal((T, N) if combine else (T, k, N)), dtype)
+    got = isc.isc_expert_linear_bwd(dy, x, w, rt, y=y, combine=combine)
+    want = train.expert_linear_bwd(host(dy), host(x), host(w), ids, None if y is None else host(y),
+                                   host(rt.weights) if combine else None)
+    parts = 8 * (dtype == "float32")
+    value, size = want["dx"]
+    close(host(got.dx), value, (N + 64 + k + parts) * E24 * size, dtype, "dx")
+    value, size = want["dw"]
+    most = max(1, np.bincount(ids[ids >= 0], minlength=E).max()) if ids.size else 1
+    close(host(got.dw), value, ((most + 64 + parts) * E24 + (U[dtype] if combine else 0)) * size
+          + (TINY * most * np.abs(host(x)).max() if combine and dtype == "float16" and ids.size else 0), dtype, "dw")
+    if combine:
+        value, size = want["dweights"]
+        close(host(got.dweights), value, (N + K + 64 + parts) * E24 * size, "float32", "dweights")
+        assert (host(got.dweights)[ids < 0] == 0).all()
+    else:
+        assert got.dweights is None
+    again = isc.isc_expert_linear_bwd(dy, x, w, rt, y=y, combine=combine)
+    for a, b in zip(got, again):
+        assert a is None or torch.equal(a, b)
+    return got, (dy, x, w, rt, y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("form,shared", [("relu", True), ("combine", False), ("combine", True), ("plain", False)])
+def test_bwd(torch, isc, shape, dtype, form, shared):
+    check_bwd(torch, isc, *shape, dtype, form, shared)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("form", ["relu", "combine"])
+@pytest.mark.parametrize("many,groups", [(60, 8), (80, 10), (130, 16)])  # sides of dx's tiles, of dw's: 128, 64; 256, 128; 256, 256
+def test_bwd_by_larger_tiles(torch, isc, dtype, form, many, groups):
+    """Wide matrices: gradients that are the same for every group of columns, since the matrices are."""
+    T, k, E, K, N = 700, 2, 2, 72, 40
+    rt, ids = route(torch, isc, 4, T, k, E, 0.05)
+    combine = form == "combine"
+    x, w = operands(torch, 4, T, k, E, K, N, dtype, not combine, combine)
+    xx, ww = x.repeat(*([1] * (x.dim() - 1)), many), w.repeat(1, groups, many)
+    dy = dev(torch, np.random.default_rng(9).standard_normal((T, N) if combine else (T, k, N)), dtype)
+    dd = torch.cat([dy] + [torch.zeros_like(dy)] * (groups - 2) + [dy], -1)  # the first and the last group of outputs
+    y = None
+    if not combine:
+        y = torch.relu(dev(torch, np.random.default_rng(2).standard_normal((T, k, N)), dtype)).repeat(1, 1, groups)
+    got = isc.isc_expert_linear_bwd(dd, xx, ww, rt, y=y, combine=combine)
+    want = train.expert_linear_bwd(host(dy), host(x), host(w), ids, None if y is None else host(y[..., :N]),
+                                   host(rt.weights) if combine else None)
+    dx, dw = host(got.dx), host(got.dw)
+    value, size = want["dx"]
+    for i in (0, 31, many - 1):
+        close(dx[..., i * K:(i + 1) * K], 2 * value, (2 * N + 64 + k) * E24 * 2 * size, dtype, "dx, columns %d" % i)
+    value, size = want["dw"]
+    for j in (0, groups - 1):
+        for i in (0, many - 1):
+            close(dw[:, j * N:(j + 1) * N, i * K:(i + 1) * K], value,
+                  ((T * k + 64) * E24 + (U[dtype] if combine else 0)) * size
+                  + (TINY * T * k * np.abs(host(x)).max() if combine and dtype == "float16" else 0), dtype, "dw, group %d, %d" % (j, i))
+    assert (dw[:, N:(groups - 1) * N] == 0).all()
+    if combine:
+        value, size = want["dweights"]
+        close(host(got.dweights), 2 * many * value, (groups * N + many * K + 64) * E24 * 2 * many * size, "float32", "dweights")
+
+
+def test_bwd_gradient_against_differences(torch, isc):
+    """fp32 differences of the forward pass itself, a step of 2^-6 of it: sums are linear in each operand."""
+    T, k, E, K, N = 20, 2, 3, 24, 12
+    got, (dy, x, w, rt, _) = check_bwd(torch, isc, T, k, E, K, N, "float32", "combine", False)
+    r = np.random.default_rng(1)
+    for name, at in (("x", x), ("w", w)):
+        step = dev(torch, r.standard_normal(at.shape))
+        f = lambda v: (isc.isc_expert_linear(v if name == "x" else x, v if name == "w" else w, rt, combine=True).double()  # noqa: E731
+                       * dy.double()).sum()
+        slope = float(f(at + 2.0 ** -6 * step) - f(at - 2.0 ** -6 * step)) / 2.0 ** -5
+        grad = got.dx if name == "x" else got.dw
+        # 480 outputs of some K e each, over the step
+        assert abs(slope - float((grad.double() * step.double()).sum())) < 2.0 ** 5 * T * N * (K + 80) * E24 * 30, name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_bwd_asked_for_in_parts(torch, isc, dtype):
+    for form in ("relu", "combine"):
+        got, (dy, x, w, rt, y) = check_bwd(torch, isc, 50, 2, 3, 72, 40, dtype, form, True)
+        combine = form == "combine"
+        for name in ("dx", "dw") + (("dweights",) if combine else ()):
+            ask = dict(dx=name == "dx", dw=name == "dw", dweights=name == "dweights")
+            part = isc.isc_expert_linear_bwd(dy, x, w, rt, y=y, combine=combine, **ask)
+            assert torch.equal(getattr(part, name), getattr(got, name)), name
+            assert sum(v is not None for v in part) == 1
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_and_addresses(torch, isc, dtype):
+    """Rows apart, rows off 16 bytes, views of larger tensors, broadcast gradients."""
+    T, k, E, K, N = 60, 2, 3, 72, 40
+    rt, ids = route(torch, isc, 3, T, k, E, 0.1)
+    x, w = operands(torch, 3, T, k, E, K, N, dtype, True)
+    want = isc.isc_expert_linear(x, w, rt, relu=True)
+    wide = torch.full((T, K + 9), float("nan"), dtype=x.dtype, device="cuda")
+    for at in (0, 1, 8, 9):
+        view = wide[:, at:at + K]
+        view.copy_(x)
+        ww = torch.full((E, N, K + 24), float("nan"), dtype=x.dtype, device="cuda")[..., at:at + K]
+        ww.copy_(w)
+        assert torch.equal(isc.isc_expert_linear(view, ww, rt, relu=True), want), at
+        wide.fill_(float("nan"))
+    turned = w.transpose(1, 2).contiguous().transpose(1, 2)  # values of a row apart: copied first
+    assert torch.equal(isc.isc_expert_linear(x, turned, rt, relu=True), want)
+    one = torch.ones((), dtype=x.dtype, device="cuda")
+    a = isc.isc_expert_linear_bwd(one.expand(T, k, N), x, w, rt, y=want)
+    b = isc.isc_expert_linear_bwd(torch.ones_like(want), x, w, rt, y=want)
+    assert torch.equal(a.dx, b.dx) and torch.equal(a.dw, b.dw)
+    dy = torch.randn_like(want)
+    far = torch.full((T, k, N + 7), float("nan"), dtype=x.dtype, device="cuda")[..., 3:3 + N]
+    far.copy_(dy)
+    a, b = (isc.isc_expert_linear_bwd(v, x, w, rt, y=want) for v in (far, dy))
+    assert torch.equal(a.dx, b.dx) and torch.equal(a.dw, b.dw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [3, 90])
+def test_values_that_are_not_finite_stay_in_their_rows(torch, isc, T, dtype):
+    k, E, K, N = 2, 3, 72, 40
+    rt, ids = route(torch, isc, 5, T, k, E, 0.2)
+    x, w = operands(torch, 5, T, k, E, K, N, dtype, True)
+    want = isc.isc_expert_linear(x, w, rt)
+    bad = x.clone()
+    bad[1, 5], bad[2, 7] = float("inf"), float("nan")
+    got = isc.isc_expert_linear(bad, w, rt)
+    rest = [t for t in range(T) if t not in (1, 2)]
+    assert torch.equal(got[rest], want[rest])
+    for t in (1, 2):
+        for j in range(k):
+            assert not torch.isfinite(got[t, j]).any() if ids[t, j] >= 0 else (got[t, j] == 0).all()
+    gone = w.clone()
+    gone[0, 3] = float("nan")  # one output of one expert
+    got = isc.isc_expert_linear(x, gone, rt)
+    hit = torch.zeros(got.shape, dtype=torch.bool, device="cuda")
+    hit[..., 3] = rt.ids == 0
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], want[~hit])
+    # a NaN that the rectifier kept lets its gradient through, a 0 does not
+    y = torch.relu(want)
+    y[0, 0, 0], y[0, 0, 1] = float("nan"), 0.0
+    dy = torch.ones_like(y)
+    a = isc.isc_expert_linear_bwd(dy, x, w, rt, y=y)
+    y[0, 0, 0] = 1.0
+    b = isc.isc_expert_linear_bwd(dy, x, w, rt, y=y)
+    assert torch.equal(a.dx, b.dx) and torch.equal(a.dw, b.dw)
+
+
+def test_fp32_over_its_range(torch, isc):
+    """Magnitudes from 2^-60 to 2^60, and the largest there are."""
+    T, k, E, K, N = 70, 1, 2, 64, 32
+    rt, ids = route(torch, isc, 6, T, k, E, 0.0)
+    r = np.random.default_rng(6)
+    for lo, hi in ((-60, 0), (-20, 20), (0, 60)):
+        x = dev(torch, r.standard_normal((T, K)) * 2.0 ** r.integers(lo, hi, (T, K)))
+        w = dev(torch, r.standard_normal((E, N, K)))
+        want, size = train.expert_linear(host(x), host(w), ids)
+        close(host(isc.isc_expert_linear(x, w, rt)), want, (K + 72) * E24 * size, "float32", "2^%d to 2^%d" % (lo, hi))
+    x = torch.zeros((T, K), device="cuda")
+    x[:, 3] = torch.finfo(torch.float32).max
+    w = torch.full((E, N, K), 1.0, device="cuda")
+    assert (isc.isc_expert_linear(x, w, rt) == torch.finfo(torch.float32).max).all()
+
+
+def test_no_tokens(torch, isc):
+    for dtype in TYPES:
+        rt, _ = route(torch, isc, 0, 0, 2, 3)
+        x, w = operands(torch, 0, 0, 2, 3, 40, 24, dtype, True)
+        assert isc.isc_expert_linear(x, w, rt).shape == (0, 2, 24)
+        assert isc.isc_expert_linear(x, w, rt, combine=True).shape == (0, 24)
+        g = isc.isc_expert_linear_bwd(x.new_empty(0, 24), x, w, rt, combine=True)
+        assert g.dx.shape == (0, 40) and g.dweights.shape == (0, 2) and (g.dw == 0).all() and g.dw.shape == w.shape
+
+
+def test_lists_out_of_range_touch_nothing_else(torch, isc):
+    """Offsets and pairs that no route has are passed over: what the good ones say is computed."""
+    T, k, E, K, N = 40, 2, 3, 64, 64
+    for tokens in (T, 3):
+        rt, ids = route(torch, isc, 8, tokens, k, E, 0.0)
+        x, w = operands(torch, 8, tokens, k, E, K, N, "bfloat16", True)
+        want = isc.isc_expert_linear(x, w, rt)
+        order = rt.order.clone()
+        lost = int(order[1])
+        order[1] = 10 ** 9
+        offsets = rt.offsets.clone()
+        offsets[0], offsets[E] = -5, 10 ** 9
+        got = isc.isc_expert_linear(x, w, isc.Route(rt.ids, rt.weights, offsets, order))
+        keep = torch.ones(tokens * k, dtype=torch.bool, device="cuda")
+        keep[lost] = False
+        assert torch.equal(got.view(-1, N)[keep], want.view(-1, N)[keep])
+
+
+# ------------------------------------------------------------ orthogonalize --
+
+def gradient(seed, B, M, N, rank):
+    r = np.random.default_rng(seed)
+    g = r.standard_normal((B, M, N)) * (0.1 if rank else 1.0)
+    return (g + (r.standard_normal((B, M, rank)) @ r.standard_normal((B, rank, N)) if rank else 0.0)) * 1e-3
+
+
+def check_orth(torch, isc, g, out, coefficients=None, steps=5, eps=1e-7, **kw):
+    coefficients = [COEFFICIENTS] * steps if coefficients is None else coefficients
+    got = isc.isc_orthogonalize(g, steps=steps, coefficients=tuple(coefficients), eps=eps, dtype=getattr(torch, out), **kw)
+    assert got.shape == g.shape and str(got.dtype) == "torch." + out
+    flat, each = host(got).reshape(-1, *g.shape[-2:]), host(g).reshape(-1, *g.shape[-2:])
+    for i, (o, m) in enumerate(zip(flat, each)):
+        exact, rounded = (train.orthogonalize(m, coefficients, eps, v) for v in (False, True))
+        allowed = 3 * np.linalg.norm(rounded - exact) + U[out] * np.linalg.norm(exact) + TINY * o.size ** 0.5
+        assert np.linalg.norm(o - exact) <= allowed, (i, np.linalg.norm(o - exact), allowed)
+    assert torch.equal(got, isc.isc_orthogonalize(g, steps=steps, coefficients=tuple(coefficients), eps=eps,
+                                                  dtype=getattr(torch, out)))
+    return got
+
+
+# one row, one column, less than an operand, off and on tiles' edges, long and narrow (A in parts), several
+MATRICES = [(1, 1, 1), (1, 1, 9), (2, 9, 1), (1, 7, 40), (2, 64, 64), (1, 65, 130), (3, 130, 65), (1, 33, 1030), (2, 1030, 33),
+            (1, 8, 4096), (1, 200, 328), (2, 260, 100)]
+
+
+@pytest.mark.parametrize("dtype,out", [("bfloat16", "bfloat16"), ("float32", "float16"), ("float16", "bfloat16")])
+@pytest.mark.parametrize("shape", MATRICES, ids=str)
+def test_orthogonalize(torch, isc, shape, dtype, out):
+    check_orth(torch, isc, dev(torch, gradient(1, *shape, 0), dtype), out)
+    if min(shape[1:]) > 8:
+        check_orth(torch, isc, dev(torch, gradient(2, *shape, 3), dtype), out)
+
+
+@pytest.mark.parametrize("shape,many", [((1, 300, 200), 110), ((1, 200, 300), 100), ((1, 300, 520), 90), ((1, 520, 300), 90)], ids=str)
+def test_orthogonalize_by_larger_tiles(torch, isc, shape, many):
+    """Tiles of 128 and 256 sides, which take many matrices: the same one many times, one other at the end."""
+    g = dev(torch, np.concatenate([gradient(3, *shape, 5), gradient(4, *shape, 0)]), "bfloat16")
+    stack = torch.cat([g[:1].expand(many, -1, -1), g[1:]])
+    got = isc.isc_orthogonalize(stack)
+    check_orth(torch, isc, stack[-2:], "bfloat16")
+    for i in (0, -1):
+        exact, rounded = (train.orthogonalize(host(stack[i]), [COEFFICIENTS] * 5, 1e-7, v) for v in (False, True))
+        allowed = 3 * np.linalg.norm(rounded - exact) + U["bfloat16"] * np.linalg.norm(exact)
+        assert np.linalg.norm(host(got[i]) - exact) <= allowed
+    assert all(torch.equal(got[i], got[0]) for i in range(many))
+
+
+def test_orthogonalize_steps_and_coefficients(torch, isc):
+    g = dev(torch, gradient(5, 1, 90, 150, 4)[0], "bfloat16")
+    own = [(4.0, -6.5, 3.0), (3.5, -5.0, 2.1), (1.875, -1.25, 0.375)]
+    check_orth(torch, isc, g, "bfloat16", own, steps=3)
+    for steps in (1, 2, 8):
+        check_orth(torch, isc, g, "float16", steps=steps)
+    check_orth(torch, isc, g, "bfloat16", [(1.5, -0.5, 0.0)] * 4, steps=4)  # the cubic iteration
+    check_orth(torch, isc, g, "bfloat16", [(1.0, 0.0, 0.0)], steps=1)       # none
+    one = isc.isc_orthogonalize(g, steps=3, coefficients=COEFFICIENTS)
+    assert torch.equal(one, isc.isc_orthogonalize(g, steps=3, coefficients=[list(COEFFICIENTS)] * 3))
+
+
+def test_orthogonalize_strides_scale_and_shapes(torch, isc):
+    m = gradient(6, 4, 40, 56, 3)
+    for dtype in TYPES:
+        g = dev(torch, m, dtype)
+        want = isc.isc_orthogonalize(g)
+        assert torch.equal(isc.isc_orthogonalize(g.view(2, 2, 40, 56)).view(4, 40, 56), want)
+        assert torch.equal(isc.isc_orthogonalize(g[2]), want[2])
+        wide = torch.full((4, 40, 61), float("nan"), dtype=g.dtype, device="cuda")[..., 3:59]
+        wide.copy_(g)
+        assert torch.equal(isc.isc_orthogonalize(wide), want)
+        assert torch.equal(isc.isc_orthogonalize(g.transpose(1, 2).contiguous().transpose(1, 2)), want)
+    # fp32 gradients of any scale: squares leave fp32's range
+    for scale in (1e-25, 1e25):
+        check_orth(torch, isc, dev(torch, m[0] * scale), "bfloat16", eps=0.0)
+    check_orth(torch, isc, dev(torch, m[0] * 1e-9), "bfloat16")  # a norm beside eps
+
+
+def test_orthogonalize_zeros_and_values_that_are_not_finite(torch, isc):
+    g = dev(torch, gradient(7, 5, 40, 24, 0), "bfloat16")
+    want = isc.isc_orthogonalize(g)
+    g[1] = 0
+    g[2, 3, 4] = float("inf")
+    g[3, 39, 23] = float("nan")
+    got = isc.isc_orthogonalize(g)
+    assert (got[1] == 0).all() and torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[4], want[4])
+    assert isc.isc_orthogonalize(g[:0]).shape == (0, 40, 24)
+
+
+# ------------------------------------------------------- together, streams --
+
+def step(torch, isc, x, router, up, down, dout):
+    """A routed block's training step: forward, gradients, orthogonalised updates."""
+    r = isc.isc_route(x.float() @ router, 2, score="sigmoid")
+    u = isc.isc_expert_linear(x, up, r, relu=True)
+    out = isc.isc_expert_linear(u, down, r, combine=True)
+    g2 = isc.isc_expert_linear_bwd(dout, u, down, r, combine=True)
+    g1 = isc.isc_expert_linear_bwd(g2.dx, x, up, r, y=u)
+    dl = isc.isc_route_bwd(g2.dweights, x.float() @ router, r.ids, score="sigmoid")
+    return out, g1.dx, g1.dw, g2.dw, dl, isc.isc_orthogonalize(g1.dw), isc.isc_orthogonalize(g2.dw)
+
+
+def block(torch, seed, T=40, D=64, F=96, E=4):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    return (draw(T, D).bfloat16(), draw(D, E) * D ** -0.5, (draw(E, F, D) * D ** -0.5).bfloat16(),
+            (draw(E, D, F) * F ** -0.5).bfloat16(), draw(T, D).bfloat16())
+
+
+def test_a_training_step(torch, isc):
+    """Against autograd on the same values in 64 bits: bfloat16 roundings of u, of its gradient and of the results."""
+    x, router, up, down, dout = block(torch, 1)
+    out, dx, dup, ddown, dl, ou, od = step(torch, isc, x, router, up, down, dout)
+    r = isc.isc_route(x.float() @ router, 2, score="sigmoid")
+    xd, upd, dnd = (v.double().requires_grad_(True) for v in (x, up, down))
+    logits = (x.float() @ router).double().requires_grad_(True)
+    ids = r.ids.long()
+    s = torch.sigmoid(torch.gather(logits, 1, ids))
+    wts = s / s.sum(-1, keepdim=True)
+    u = torch.relu((upd[ids] * xd[:, None, None, :]).sum(-1))
+    y = ((dnd[ids] * u[:, :, None, :]).sum(-1) * wts[..., None]).sum(1)
+    (y * dout.double()).sum().backward()
+    y = y.detach()
+    for name, got, want in (("out", out, y), ("dx", dx, xd.grad), ("dup", dup, upd.grad), ("ddown", ddown, dnd.grad),
+                            ("dlogits", dl, logits.grad)):
+        off = float((got.double() - want).norm() / want.norm())
+        # three roundings in turn of 2^-9 at most, in the 2-norm; the rectifier's border moves by one of them
+        assert off < 4 * 2.0 ** -8, (name, off)
+    assert torch.equal(ou, isc.isc_orthogonalize(dup)) and torch.equal(od, isc.isc_orthogonalize(ddown))
+
+
+def test_streams(torch, isc):
+    x, router, up, down, dout = block(torch, 2)
+    want = step(torch, isc, x, router, up, down, dout)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            outs.append(step(torch, isc, x, router, up, down, dout))
+    r = isc.isc_route(x.float() @ router, 2, score="sigmoid")
+    torch.cuda.synchronize()
+    named = isc.isc_expert_linear(x, up, r, relu=True, stream=streams[0])
+    other = isc.isc_orthogonalize(want[2], stream=streams[1])
+    torch.cuda.synchronize()
+    for got in outs:
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    assert torch.equal(other, want[5]) and named.shape == (40, 2, 96)
+
+
+def test_graphs(torch, isc):
+    """Captured once, replayed on other inputs, with eager work in between; two graphs, and kernels first met in one."""
+    a = block(torch, 3)
+    inputs = [v.clone() for v in a]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(torch, isc, *inputs)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(torch, isc, *inputs)
+        graphs.append((graph, out))
+    tall = torch.randn((70, 20), device="cuda").half()
+    alone = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(alone):
+        first = isc.isc_orthogonalize(tall, steps=2)
+    for seed in (3, 4, 5, 6):
+        for to, frm in zip(inputs, block(torch, seed)):
+            to.copy_(frm)
+        want = step(torch, isc, *[v.clone() for v in inputs])
+        for graph, out in graphs:
+            graph.replay()
+            torch.cuda.synchronize()
+            for got, w in zip(out, want):
+                assert torch.equal(got, w), seed
+        alone.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, isc.isc_orthogonalize(tall, steps=2))
+
+
+def test_workspace_given(torch, isc):
+    """A caller's workspace, with anything in it, and behind its end nothing is written."""
+    x, router, up, down, dout = block(torch, 4)
+    r = isc.isc_route(x.float() @ router, 2, score="sigmoid")
+    E, F, D = up.shape
+    n = ctypes.c_size_t()
+    d = isc.ExpertDesc(E, F, D, 2, 2, 1)
+
+    def room(size):
+        ws = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+        return ws, ws[:size]
+
+    assert isc.lib().isc_expert_linear_workspace_size(d, 40, 0, n) == 0
+    whole, ws = room(n.value)
+    want = isc.isc_expert_linear(x, up, r, relu=True)
+    assert torch.equal(isc.isc_expert_linear(x, up, r, relu=True, ws=ws), want) and (whole[n.value:] == 255).all()
+    assert isc.lib().isc_expert_linear_bwd_workspace_size(d, 40, 1, 0, n) == 0
+    whole, ws = room(n.value)
+    dy = torch.randn_like(want)
+    got, ref = (isc.isc_expert_linear_bwd(dy, x, up, r, y=want, ws=w) for w in (ws, None))
+    assert torch.equal(got.dx, ref.dx) and torch.equal(got.dw, ref.dw) and (whole[n.value:] == 255).all()
+    d = isc.ExpertDesc(E, D, F, 2, 2, 0)
+    for name, query, args in (("linear", "isc_expert_linear_workspace_size", (40, 1)),
+                              ("bwd", "isc_expert_linear_bwd_workspace_size", (40, 0, 1))):
+        assert getattr(isc.lib(), query)(d, *args, n) == 0
+        whole, ws = room(n.value)
+        if name == "linear":
+            assert torch.equal(isc.isc_expert_linear(want, down, r, combine=True, ws=ws), isc.isc_expert_linear(want, down, r, combine=True))
+        else:
+            got, ref = (isc.isc_expert_linear_bwd(dout, want, down, r, combine=True, ws=w) for w in (ws, None))
+            assert all(torch.equal(p, q) for p, q in zip(got, ref))
+        assert (whole[n.value:] == 255).all()
+    for shape in ((3, 40, 24), (1, 8, 4096)):
+        assert isc.lib().isc_orthogonalize_workspace_size(*shape, n) == 0
+        whole, ws = room(n.value)
+        g = torch.randn(shape, device="cuda")
+        assert torch.equal(isc.isc_orthogonalize(g, ws=ws), isc.isc_orthogonalize(g)) and (whole[n.value:] == 255).all()
+
+
+def test_binding_refusals(torch, isc):
+    x, router, up, down, dout = block(torch, 5)
+    r = isc.isc_route(x.float() @ router, 2)
+    bare = isc.isc_route(x.float() @ router, 2, lists=False)
+    u = isc.isc_expert_linear(x, up, r, relu=True)
+    for call in (lambda: isc.isc_expert_linear(x, up, bare), lambda: isc.isc_expert_linear(x, up[0], r),
+                 lambda: isc.isc_expert_linear(x[:5], up, r), lambda: isc.isc_expert_linear(x.float(), up, r),
+                 lambda: isc.isc_expert_linear(x, up[:3], r), lambda: isc.isc_expert_linear(x[:, :5], up, r),
+                 lambda: isc.isc_expert_linear(x.cpu(), up, r), lambda: isc.isc_expert_linear_bwd(dout, x, up, r),
+                 lambda: isc.isc_expert_linear_bwd(u, x, up, r, y=u[:1]), lambda: isc.isc_expert_linear_bwd(u, x, up, r, dweights=True),
+                 lambda: isc.isc_expert_linear_bwd(u, x, up, r, dx=False, dw=False),
+                 lambda: isc.isc_expert_linear_bwd(dout, u, down, r, y=u, combine=True), lambda: isc.isc_orthogonalize(x[0]),
+                 lambda: isc.isc_orthogonalize(x, coefficients=(1, 2)), lambda: isc.isc_orthogonalize(x, steps=2, coefficients=[(1, 0, 0)])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: isc.isc_expert_linear(x.int(), up, r), lambda: isc.isc_expert_linear(x, up, r, dtype=torch.float64),
+                 lambda: isc.isc_orthogonalize(x, dtype=torch.float32), lambda: isc.isc_orthogonalize(x.double())):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: isc.isc_expert_linear(x, up, r, relu=True, combine=True), lambda: isc.isc_orthogonalize(x, steps=0),
+                 lambda: isc.isc_orthogonalize(x, coefficients=(30.0, 0.0, 0.0)), lambda: isc.isc_orthogonalize(x, eps=-1.0),
+                 lambda: isc.isc_expert_linear(x, up, r, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(isc.IscError):
+            call()

@@ -1,0 +1,96 @@
+"""Pins of the 64-bit forms of the operators that train a routed block: gradients
+against differences, the polynomial against the singular values, and planted
+mistakes that the pins have to see."""
+import numpy as np
+import pytest
+
+from oracle import train
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def rng(seed):
+    return np.random.default_rng(seed)
+
+
+def numeric(f, x, h=1e-6):
+    g = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        u, v = x.copy(), x.copy()
+        u[i] += h
+        v[i] -= h
+        g[i] = (f(u) - f(v)) / (2 * h)
+    return g
+
+
+# a difference of step h errs by h^2 times a third derivative (0 here, but across a
+# rectifier's border) and by 2^-53 / h of the values, some 1e-9
+DIFF = 1e-7
+
+
+def case(seed, T, k, E, N, K, shared):
+    r = rng(seed)
+    ids = np.stack([r.permutation(E)[:k] for _ in range(T)])
+    ids[r.random(ids.shape) < 0.15] = -1
+    return (r.standard_normal((T, K) if shared else (T, k, K)), r.standard_normal((E, N, K)), ids, r.random(ids.shape))
+
+
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("form", ["plain", "relu", "combine"])
+def test_gradients_against_differences(shared, form):
+    x, w, ids, s = case(3, 4, 2, 3, 5, 6, shared)
+    relu, weights = form == "relu", s if form == "combine" else None
+    y, _ = train.expert_linear(x, w, ids, relu, weights)
+    dy = rng(5).standard_normal(y.shape)
+    got = train.expert_linear_bwd(dy, x, w, ids, y if relu else None, weights)
+    f = lambda x_, w_, s_: (train.expert_linear(x_, w_, ids, relu, s_)[0] * dy).sum()  # noqa: E731
+    assert np.abs(got["dx"][0] - numeric(lambda v: f(v, w, weights), x)).max() < DIFF
+    assert np.abs(got["dw"][0] - numeric(lambda v: f(x, v, weights), w)).max() < DIFF
+    if weights is not None:
+        empty = ids < 0
+        assert np.abs(got["dweights"][0] - numeric(lambda v: f(x, w, v), s))[~empty].max() < DIFF
+        assert (got["dweights"][0][empty] == 0).all()
+    for value, size in got.values():
+        assert (np.abs(value) <= size * (1 + 1e-12)).all()
+
+
+def test_differences_see_mistakes():
+    x, w, ids, s = case(3, 4, 2, 3, 5, 6, False)
+    y, _ = train.expert_linear(x, w, ids, False, s)
+    dy = rng(5).standard_normal(y.shape)
+    want = numeric(lambda v: (train.expert_linear(v, w, ids, False, s)[0] * dy).sum(), x)
+    unweighted = train.expert_linear_bwd(np.repeat(dy[:, None], 2, 1), x, w, ids)["dx"][0]
+    assert np.abs(unweighted - want).max() > 0.01
+    swapped = train.expert_linear_bwd(dy, x, w, np.where(ids == 0, 1, np.where(ids == 1, 0, ids)), None, s)["dx"][0]
+    assert np.abs(swapped - want).max() > 0.01
+
+
+def test_lists():
+    ids = np.array([[2, 0], [-1, 2], [0, 1], [7, -1]])
+    offsets, order = train.lists(ids, 3)
+    assert offsets.tolist() == [0, 2, 3, 5] and order.tolist() == [1, 4, 5, 0, 3, -1, -1, -1]
+
+
+@pytest.mark.parametrize("M,N", [(1, 1), (1, 7), (5, 5), (6, 20), (20, 6)])
+def test_orthogonalize_is_a_polynomial_of_the_singular_values(M, N):
+    g = rng(M * 100 + N).standard_normal((M, N))
+    u, s, vt = np.linalg.svd(g, full_matrices=False)
+    s = s / (np.sqrt((s * s).sum()) + 1e-7)
+    for a, b, c in [COEFFICIENTS] * 5:
+        s = s * (a + b * s ** 2 + c * s ** 4)
+    got = train.orthogonalize(g, [COEFFICIENTS] * 5, 1e-7)
+    assert np.abs(got - (u * s) @ vt).max() < 1e-9
+    other = train.orthogonalize(g, [COEFFICIENTS] * 4 + [(3.4445, -4.7750, 2.0)], 1e-7)
+    assert np.abs(other - got).max() > 1e-6  # a coefficient's third digit shows
+
+
+def test_rounded_operands_err_as_stated():
+    """2e-3 of the result's norm at most: what the header says."""
+    r = rng(8)
+    for M, N, rank in ((64, 64, 0), (200, 500, 0), (300, 100, 8), (128, 128, 4)):
+        g = r.standard_normal((M, N)) * (0.1 if rank else 1.0)
+        if rank:
+            g += r.standard_normal((M, rank)) @ r.standard_normal((rank, N))
+        exact, rounded = (train.orthogonalize(g, [COEFFICIENTS] * 5, 1e-7, v) for v in (False, True))
+        err = np.linalg.norm(rounded - exact) / np.linalg.norm(exact)
+        assert 1e-5 < err < 2e-3, (M, N, rank, err)
