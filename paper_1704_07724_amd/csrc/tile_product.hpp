@@ -321,7 +321,10 @@ struct Tile {
     static constexpr int kXStages = DIRECT ? 3 : 2;
     static constexpr int kLds = kXStages * kXBytes + 2 * kWBytes;
 
-    f32x16 acc[FJ][FI];
+    // fp32: the products with a part of less than the first add up beside the others, which
+    // then are rounded once for every 16 inner indices, not six times.
+    static constexpr int kSums = kParts > 1 ? 2 : 1;
+    f32x16 acc[FJ][FI], low[kSums > 1 ? FJ : 1][kSums > 1 ? FI : 1];
 
     // What a wavefront multiplies at a time: 16 inner indices.
     struct Operands {
@@ -351,7 +354,10 @@ struct Tile {
                 for (int j = 0; j < FJ; ++j)
 #pragma unroll
                     for (int i = 0; i < FI; ++i) {
-                        acc[j][i] = mfma<T>(o.w[j][p], o.x[i][sum - p], acc[j][i]);
+                        if (sum > 0)
+                            low[j][i] = mfma<T>(o.w[j][p], o.x[i][sum - p], low[j][i]);
+                        else
+                            acc[j][i] = mfma<T>(o.w[j][p], o.x[i][sum - p], acc[j][i]);
                         between(n++);
                     }
     }
@@ -406,7 +412,10 @@ struct Tile {
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
-                for (int n = 0; n < 16; ++n) acc[j][i][n] = 0.0f;
+                for (int n = 0; n < 16; ++n) {
+                    acc[j][i][n] = 0.0f;
+                    if constexpr (kSums > 1) low[j][i][n] = 0.0f;
+                }
         const int steps = (inner + BK - 1) / BK;
         if (steps <= 0) return;
         constexpr int kSteps16 = BK / 16;
@@ -528,6 +537,9 @@ struct Tile {
             decltype(ahead(0, 0)) beside[32 / kRows];
 #pragma unroll
             for (int r = 0; r < 32 / kRows; ++r) beside[r] = ahead(wi + 32 * i + r * kRows + row, wj + 4 * c);
+            if constexpr (kSums > 1)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) acc[j][i] += low[j][i];
             // the last rows' stores are the only ones that follow start()'s loads unwaited for
             if (i == FI - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
