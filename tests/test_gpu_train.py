@@ -595,3 +595,12 @@ def test_binding_refusals(torch, isc):
                  lambda: isc.isc_expert_linear(x, up, r, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(isc.IscError):
             call()
+
+
+def test_the_example_runs_and_its_gradients_hold(torch, isc):
+    import os
+    import runpy
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    main = runpy.run_path(os.path.join(root, "examples", "trained_experts.py"))["main"]
+    # roundings to bfloat16 of the hidden layer, its gradient and the results: four of 2^-8 at most, in the 2-norm
+    assert main(["--tokens", "64", "--width", "64", "--hidden", "96", "--experts", "8", "--steps", "3"]) < 4 * 2.0 ** -8
