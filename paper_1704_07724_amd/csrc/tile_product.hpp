@@ -427,6 +427,7 @@ struct Tile {
                 meet();
             else
                 land<0>();
+            if (steps > 1) ws.send_all(BK, base + w_at(1), wave, tid);
         } else {
             xs.send_all(0, base, wave, tid);
             ws.send_all(0, base, wave, tid);
@@ -462,21 +463,23 @@ struct Tile {
                 // the operands of the next 16: behind the last stage's, those of some stage, which nothing takes
                 const char *from_x = lds + (kk + 1 < kSteps16 ? x_now : x_then),
                            *from_w = lds + (kk + 1 < kSteps16 ? w_at(s) : w_at(s + 1));
+                // X's next-but-two goes where the last stage's X was, W's next-but-one, from the
+                // meeting on, where this stage's is
                 const auto send = [&](int n) {
                     if constexpr (DIRECT) {
                         constexpr int kW = (WStage::kLoads + kProducts - 1) / kProducts;
                         constexpr int kX = (XStage::kLoads + kProducts - 1) / kProducts;
-                        if (kk == 0 && more) {
-#pragma unroll
-                            for (int q = n * kW; q < (n + 1) * kW && q < WStage::kLoads; ++q) {
-                                ws.send(q, (s + 1) * BK, base + w_at(s + 1), wave);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                        }
-                        if (kk == 1 && most) {
+                        if (kk == 0 && most) {
 #pragma unroll
                             for (int q = n * kX; q < (n + 1) * kX && q < XStage::kLoads; ++q) {
                                 xs.send(q, (s + 2) * BK, base + x_last, wave);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                        if (kk + 1 == kSteps16 && most) {
+#pragma unroll
+                            for (int q = n * kW; q < (n + 1) * kW && q < WStage::kLoads; ++q) {
+                                ws.send(q, (s + 2) * BK, base + w_at(s), wave);
                                 __builtin_amdgcn_sched_barrier(0);
                             }
                         }
@@ -497,8 +500,8 @@ struct Tile {
                     for (int n = 0; n < kProducts; ++n) send(n);
                 }
                 if constexpr (DIRECT) {
-                    if constexpr (WStage::kFetch) if (kk == 0 && more) ws.fetch((s + 2) * BK, tid);
-                    if constexpr (XStage::kFetch) if (kk == 1 && most) xs.fetch((s + 3) * BK, tid);
+                    if constexpr (WStage::kFetch) if (kk + 1 == kSteps16 && most) ws.fetch((s + 3) * BK, tid);
+                    if constexpr (XStage::kFetch) if (kk == 0 && most) xs.fetch((s + 3) * BK, tid);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
