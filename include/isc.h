@@ -686,7 +686,8 @@ int isc_orthogonalize_workspace_size(int32_t B, int32_t M, int32_t N, size_t *by
  * fp16, so o is within about 2e-3 of the exact result in the 2-norm, relative to it,
  * before its own rounding.  A matrix with a value that is not finite becomes NaN, one
  * of zeros stays (with eps > 0); others of the stack are not affected.
- * Three launches a step, four where A is small and X long, and two before.  Deterministic.
+ * Three launches a step, four where A is small and X long, one where a side is at most
+ * 64, and two before.  Deterministic.
  * Errors: NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, ALIGN, ARG, DEVICE, HIP. */
 int isc_orthogonalize(int32_t B, int32_t M, int32_t N, int32_t type, const void *g, int64_t ldg, int32_t steps,
                       const float *coefficients, float eps, void *o, int32_t o_type, int64_t ldo, void *ws,

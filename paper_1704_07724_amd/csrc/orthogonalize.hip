@@ -29,8 +29,7 @@ namespace {
 
 using namespace tp;
 
-constexpr float kUp = 64.0f;     // of every fp16 operand
-constexpr float kLow = 2048.0f;  // of what a state's operand leaves, beyond that
+constexpr float kUp = kOrthUp, kLow = kOrthLow;
 
 struct OrthProduct {
     OrthShape s;
@@ -52,13 +51,6 @@ struct OrthProduct {
     int parts;              // of A's sums, whose fp32 results go to `partial`
     float *partial;
 };
-
-// 1 / (|G| + eps) of matrix n, from its parts' sums of squares.
-__device__ __forceinline__ double inverse_norm(const double *squares, int n, int blocks, float eps) {
-    double sum = 0.0;
-    for (int i = 0; i < blocks; ++i) sum += squares[n * blocks + i];
-    return 1.0 / (sqrt(sum) + static_cast<double>(eps));
-}
 
 // Sums of squares, in fp64: no gradient's square leaves its range.
 template <class T>
@@ -91,7 +83,7 @@ template <class T>
 __global__ __launch_bounds__(256) void orth_scale_kernel(const OrthArgs a) {
     const OrthShape &s = a.s;
     const int64_t row0 = static_cast<int64_t>(blockIdx.y) * s.M;
-    const double by = inverse_norm(reinterpret_cast<const double *>(a.ws), blockIdx.y, s.blocks(), a.eps);
+    const double by = orth_inverse_norm(reinterpret_cast<const double *>(a.ws), blockIdx.y, s.blocks(), a.eps);
     uint16_t *operand = reinterpret_cast<uint16_t *>(a.ws + s.operand(0)) + blockIdx.y * s.of_state();
     const int groups = s.np() / 8;
     const int64_t all = static_cast<int64_t>(s.M) * groups, hop = static_cast<int64_t>(gridDim.x) * 256;
@@ -173,7 +165,7 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
         if constexpr (WHAT == kApply) {
             const int np = p.s.np();
             const int64_t first = job.n * p.s.of_state();
-            const float by = p.g ? static_cast<float>(inverse_norm(p.squares, job.n, p.s.blocks(), p.eps) * kUp) : 0.0f;
+            const float by = p.g ? static_cast<float>(orth_inverse_norm(p.squares, job.n, p.s.blocks(), p.eps) * kUp) : 0.0f;
             t.template each<false>(
                 lds,
                 [&](int i, int j) {
@@ -322,16 +314,25 @@ hipError_t launch_tile(const OrthProduct &p, hipStream_t s) {
     return hipGetLastError();
 }
 
+dim3 norm_grid(const OrthShape &s) { return dim3(static_cast<unsigned>(s.blocks()), static_cast<unsigned>(s.B)); }
+
 template <class T>
-hipError_t launch_state(const OrthArgs &a, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(a.s.blocks()), static_cast<unsigned>(a.s.B));
-    hipLaunchKernelGGL(orth_norm_kernel<T>, grid, dim3(256), 0, s, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(orth_scale_kernel<T>, grid, dim3(256), 0, s, a);
+hipError_t launch_scale(const OrthArgs &a, hipStream_t s) {
+    hipLaunchKernelGGL(orth_scale_kernel<T>, norm_grid(a.s), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
 }  // namespace
+
+hipError_t launch_orth_norm(const OrthArgs &a, hipStream_t s) {
+    if (a.type == ISC_F32)
+        hipLaunchKernelGGL(orth_norm_kernel<F32>, norm_grid(a.s), dim3(256), 0, s, a);
+    else if (a.type == ISC_BF16)
+        hipLaunchKernelGGL(orth_norm_kernel<BF16>, norm_grid(a.s), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL(orth_norm_kernel<F16>, norm_grid(a.s), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
 
 bool orth_launches_fit(const OrthShape &s) {
     const int64_t down = (s.M + 63) / 64, across = (s.N + 63) / 64, m = (s.m() + 63) / 64;
@@ -341,9 +342,12 @@ bool orth_launches_fit(const OrthShape &s) {
 
 hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s) {
     const OrthShape &h = a.s;
-    hipError_t e = a.type == ISC_F32    ? launch_state<F32>(a, s)
-                   : a.type == ISC_BF16 ? launch_state<BF16>(a, s)
-                                        : launch_state<F16>(a, s);
+    hipError_t e = launch_orth_norm(a, s);
+    if (e != hipSuccess) return e;
+    if (h.small()) return launch_orth_small(a, s);
+    e = a.type == ISC_F32    ? launch_scale<F32>(a, s)
+        : a.type == ISC_BF16 ? launch_scale<BF16>(a, s)
+                             : launch_scale<F16>(a, s);
     if (e != hipSuccess) return e;
     uint16_t *square = reinterpret_cast<uint16_t *>(a.ws + h.square(0)),
              *poly = reinterpret_cast<uint16_t *>(a.ws + h.square(1));

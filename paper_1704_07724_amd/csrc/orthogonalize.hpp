@@ -23,16 +23,26 @@ struct OrthShape {
     __host__ __device__ int64_t low() const { return round(8 * static_cast<int64_t>(B) * blocks()); }
     __host__ __device__ int64_t operand(int i) const { return low() + (1 + i) * round(2 * B * of_state()); }
     __host__ __device__ int64_t square(int i) const { return operand(2) + i * round(2 * B * of_square()); }
-    // Parts in which A's sums over the state's rows or columns are made, and added up after: where
-    // A has so few tiles that its inner indices in turn are the time.
-    int parts() const {
-        const int64_t side = (m() + 63) / 64, tiles = B * side * (side + 1) / 2, steps = ((wide() ? N : M) + 63) / 64;
+    // Matrices of which one side is at most 64 have all of A in a workgroup (orth_small.hip).
+    __host__ __device__ bool small() const { return m() <= 64; }
+    __host__ __device__ int64_t span() const { return wide() ? N : M; }  // the longer side
+    // Parts in which A's sums over the longer side are made, and added up after: where A has so
+    // few tiles that its inner indices in turn are the time.
+    __host__ __device__ int parts() const {
+        if (small()) {
+            const int64_t fours = (span() + 255) / 256;
+            return static_cast<int>(fours < 16 ? fours : 16);
+        }
+        const int64_t side = (m() + 63) / 64, tiles = B * side * (side + 1) / 2, steps = (span() + 63) / 64;
         if (tiles > 64 || steps < 8) return 1;
         const int64_t most = 256 / tiles < steps / 2 ? 256 / tiles : steps / 2;
         return static_cast<int>(most < 16 ? most : 16);
     }
     int64_t partial() const { return square(2); }
-    int64_t bytes() const { return partial() + (parts() > 1 ? round(4 * B * parts() * of_square()) : 0); }
+    int64_t bytes() const {
+        if (small()) return partial() + round(int64_t{2} * 4 * B * parts() * 4096);
+        return partial() + (parts() > 1 ? round(4 * B * parts() * of_square()) : 0);
+    }
 };
 
 struct OrthArgs {
@@ -48,5 +58,19 @@ struct OrthArgs {
 };
 bool orth_launches_fit(const OrthShape &s);
 hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s);
+hipError_t launch_orth_norm(const OrthArgs &a, hipStream_t s);   // the parts of every |G|^2
+hipError_t launch_orth_small(const OrthArgs &a, hipStream_t s);  // all of it, behind them
+
+constexpr float kOrthUp = 64.0f;     // of every fp16 operand
+constexpr float kOrthLow = 2048.0f;  // of what a state's operand leaves, beyond that
+
+#if defined(__HIPCC__)
+// 1 / (|G| + eps) of matrix n, from its parts' sums of squares.
+__device__ __forceinline__ double orth_inverse_norm(const double *squares, int n, int blocks, float eps) {
+    double sum = 0.0;
+    for (int i = 0; i < blocks; ++i) sum += squares[n * blocks + i];
+    return 1.0 / (sqrt(sum) + static_cast<double>(eps));
+}
+#endif
 
 }  // namespace isc

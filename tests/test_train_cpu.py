@@ -205,11 +205,13 @@ def test_no_tokens_launch_one_kernel_for_the_weights(launches):
 
 def test_orthogonalize_launches(launches):
     shapes = [(B, M, N) for B in (1, 3, 64) for M, N in ((1, 1), (64, 2048), (2048, 64), (777, 1155), (1408, 2048), (4096, 9216), (9216, 4096))]
-    shapes += [(1, 65536, 65536), (65535, 8, 8), (1, 16, 65536), (1, 65536, 16)]
+    shapes += [(1, 65536, 65536), (65535, 8, 8), (1, 16, 65536), (1, 65536, 16), (1, 100, 4096)]
     a = FAR
     calls = [("isc_orthogonalize", [B, M, N, 0, a[0], N, 3, [1.5, -0.5, 0.0] * 3, 1e-7, a[1], 2, N, a[2], 1 << 55, None]) for B, M, N in shapes]
     for shape, (status, _, kernels) in zip(shapes, launches(calls)):
-        assert status == 0 and launchable(kernels) and len(kernels) in (11, 14), (shape, len(kernels))
+        assert status == 0 and launchable(kernels), shape
+        # two launches and three a step, a fourth where A comes in parts; one a step where a side is at most 64
+        assert len(kernels) in ((5,) if min(shape[1:]) <= 64 else (11, 14)), (shape, len(kernels))
 
 
 def test_orthogonalize_stops_at_what_is_counted(launches):
