@@ -143,7 +143,7 @@ hipError_t launch_dw_of(const DwArgs &a, hipStream_t s) {
     if constexpr (DIRECT)
         if (side == 256) return launch_dw<Tile<T, true, kAcross, kAcross, 256, 256, 2, 4, true>>(a, s);
     if (side == 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, kWavesOf128<T>, true>>(a, s);
-    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 64, 64, 2, 2, true>>(a, s);
+    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 64, 64, 2, 2, true, kInner64<DIRECT>>>(a, s);
 }
 
 template <class T>

@@ -19,8 +19,7 @@
 // v_mfma_f32_32x32x16: lane l holds 8 consecutive r (from 8 * (l / 32)) of row
 // l % 32 of each operand; of the result, column l % 32 and the rows
 // 8 * (n / 4) + 4 * (l / 32) + n % 4.  W's rows are dealt to the instruction's so
-// that these are the 16 consecutive j from 16 * (l / 32): a lane stores 32 or 64
-// consecutive bytes.
+// that these are the 16 consecutive j from 16 * (l / 32).
 //
 // LDS rows are whole multiples of the banks' width, so chunks of 16 bytes change
 // places within a row by the row's number: the 64 lanes of a read meet all banks.
@@ -305,14 +304,22 @@ struct Stage {
 // A workgroup's tile: BI x BJ results by WI x WJ wavefronts, BK inner indices a stage.
 // Loads through registers have two stages in LDS.  Direct loads have two of W and three
 // of X (160 KiB for 256 x 256, all of a compute unit's; 80 KiB for 128 x 128, so that
-// two workgroups fit): X's have more than a stage's time to land, W's most of one.
-template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, bool LISTED = false>
+// two workgroups fit): X's have more than a stage's time to land, W's all of one.
+//   256 x 256, eight wavefronts   a wavefront's 128 x 64 results take 6 operands for 8
+//     products.  4096 tokens of 2048 through 8 of 64 experts of 1408, us a launch: 246 (768
+//     TFLOP/s), by 128 x 128 283; dw of the same 350 and 609; 4 wavefronts of 128 x 128
+//     results, one a SIMD, are 15 % slower, four stages of 32 inner indices 5 %, since half
+//     a line a row is asked for at a time.
+//   A stage of 256 x 256 takes 2.0 us with every compute unit busy: its products alone take
+//     1.1, its loads and reads alone 1.0, and they overlap in part.
+template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, bool LISTED = false,
+          int BK_ = 64>
 struct Tile {
     using T = T_;
     static constexpr bool DIRECT = DIRECT_, kXAcross = XS == kAcross;
     static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
     static constexpr int kWaves = WI * WJ, kThreads = 64 * kWaves;
-    static constexpr int BK = std::is_same_v<T, F32> && BI > 64 ? 32 : 64;
+    static constexpr int BK = std::is_same_v<T, F32> && BI > 64 ? 32 : BK_;
     static constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;
     using XStage = Stage<T, DIRECT, XS, LISTED, BI, BK, kThreads>;
     using WStage = Stage<T, DIRECT, WS, LISTED, BJ, BK, kThreads>;
@@ -602,6 +609,12 @@ __device__ __forceinline__ void store8_as(void *p, int64_t at, const float (&v)[
 // 1408 of 2048, 232 us with four wavefronts, 187 with eight).
 template <class T>
 constexpr int kWavesOf128 = std::is_same_v<T, F32> ? 4 : 2;
+
+// Inner indices of a stage of the experts' 64 x 64 tiles, of which there are few a compute
+// unit: half as many meetings (300 tokens of 2048 through 2 of 4 experts of 1408 24.0 and 21.2 us
+// by 64 and 128; where more workgroups share a compute unit, as in the orthogonalisation, 64).
+template <bool DIRECT>
+constexpr int kInner64 = DIRECT ? 128 : 64;
 
 // The side of a launch's tiles, by how many of each there are (of 256, or 0 where they cannot
 // be taken; of 128).  Half of the compute units busy on tiles of 256 beat all on smaller ones,
