@@ -93,8 +93,10 @@ __global__ __launch_bounds__(1024) void orth_small_kernel(const SmallStep p) {
     const int row = wi + (lane & 31), col = wj + 16 * (lane >> 5);
     const int blocks = static_cast<int>((s.span() + 63) / 64);
     const bool first = p.step <= 0, last = p.step + 1 == p.a.steps;
-    const float by = first ? static_cast<float>(
-        orth_inverse_norm(reinterpret_cast<const double *>(p.a.ws), n, s.blocks(), p.a.eps) * kOrthUp) : 0.0f;
+    float by = 0.0f;
+    if (first)
+        by = static_cast<float>(orth_inverse_norm(reinterpret_cast<const double *>(p.a.ws), n, s.blocks(), p.a.eps,
+                                                  reinterpret_cast<double *>(lds[1])) * kOrthUp);
     uint16_t *high = reinterpret_cast<uint16_t *>(p.a.ws + s.operand(0)) + n * s.of_state(),
              *low = reinterpret_cast<uint16_t *>(p.a.ws + s.low()) + n * s.of_state();
     char *square = lds[0], *poly = lds[1], *x = lds[2 + group];

@@ -42,8 +42,7 @@ struct OrthProduct {
     const void *g;          // the first step's state is G, scaled
     int64_t ldg;
     int type;
-    const double *squares;
-    float eps;
+    const double *inverse;  // of the norms
     void *o;                // the last step's results
     int64_t ldo;
     int otype;
@@ -83,7 +82,9 @@ template <class T>
 __global__ __launch_bounds__(256) void orth_scale_kernel(const OrthArgs a) {
     const OrthShape &s = a.s;
     const int64_t row0 = static_cast<int64_t>(blockIdx.y) * s.M;
-    const double by = orth_inverse_norm(reinterpret_cast<const double *>(a.ws), blockIdx.y, s.blocks(), a.eps);
+    __shared__ double sums[256];
+    const double by = orth_inverse_norm(reinterpret_cast<const double *>(a.ws), blockIdx.y, s.blocks(), a.eps, sums);
+    if (blockIdx.x == 0 && threadIdx.x == 0) reinterpret_cast<double *>(a.ws + s.inverse())[blockIdx.y] = by;
     uint16_t *operand = reinterpret_cast<uint16_t *>(a.ws + s.operand(0)) + blockIdx.y * s.of_state();
     const int groups = s.np() / 8;
     const int64_t all = static_cast<int64_t>(s.M) * groups, hop = static_cast<int64_t>(gridDim.x) * 256;
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
         if constexpr (WHAT == kApply) {
             const int np = p.s.np();
             const int64_t first = job.n * p.s.of_state();
-            const float by = p.g ? static_cast<float>(orth_inverse_norm(p.squares, job.n, p.s.blocks(), p.eps) * kUp) : 0.0f;
+            const float by = p.g ? static_cast<float>(p.inverse[job.n] * kUp) : 0.0f;
             t.template each<false>(
                 lds,
                 [&](int i, int j) {
@@ -386,8 +387,7 @@ hipError_t launch_orthogonalize(const OrthArgs &a, hipStream_t s) {
             p.g = a.g;
             p.ldg = a.ldg;
             p.type = a.type;
-            p.squares = reinterpret_cast<const double *>(a.ws);
-            p.eps = a.eps;
+            p.inverse = reinterpret_cast<const double *>(a.ws + h.inverse());
         }
         p.o = i + 1 == a.steps ? a.o : nullptr;
         p.ldo = a.ldo;

@@ -17,10 +17,11 @@ struct OrthShape {
     __host__ __device__ int64_t of_square() const { return static_cast<int64_t>(m()) * mp(); }
     __host__ __device__ static int64_t round(int64_t n) { return (n + 255) / 256 * 256; }
     __host__ __device__ int blocks() const {  // workgroups that sum a matrix's squares
-        const int64_t n = (of_state() + 16383) / 16384;
-        return static_cast<int>(n < 256 ? n : 256);
+        const int64_t n = (of_state() + 8191) / 8192;
+        return static_cast<int>(n < 1024 ? n : 1024);
     }
-    __host__ __device__ int64_t low() const { return round(8 * static_cast<int64_t>(B) * blocks()); }
+    __host__ __device__ int64_t inverse() const { return round(8 * static_cast<int64_t>(B) * blocks()); }
+    __host__ __device__ int64_t low() const { return inverse() + round(8 * static_cast<int64_t>(B)); }
     __host__ __device__ int64_t operand(int i) const { return low() + (1 + i) * round(2 * B * of_state()); }
     __host__ __device__ int64_t square(int i) const { return operand(2) + i * round(2 * B * of_square()); }
     // Matrices of which one side is at most 64 have all of A in a workgroup (orth_small.hip).
@@ -65,11 +66,21 @@ constexpr float kOrthUp = 64.0f;     // of every fp16 operand
 constexpr float kOrthLow = 2048.0f;  // of what a state's operand leaves, beyond that
 
 #if defined(__HIPCC__)
-// 1 / (|G| + eps) of matrix n, from its parts' sums of squares.
-__device__ __forceinline__ double orth_inverse_norm(const double *squares, int n, int blocks, float eps) {
+// 1 / (|G| + eps) of matrix n, from its parts' sums of squares, by all of a workgroup of 256 or
+// 1024 threads; `sums` is its LDS.
+__device__ __forceinline__ double orth_inverse_norm(const double *squares, int n, int blocks, float eps, double *sums) {
     double sum = 0.0;
-    for (int i = 0; i < blocks; ++i) sum += squares[n * blocks + i];
-    return 1.0 / (sqrt(sum) + static_cast<double>(eps));
+    for (int i = threadIdx.x; i < blocks; i += 256)
+        if (threadIdx.x < 256) sum += squares[static_cast<int64_t>(n) * blocks + i];
+    if (threadIdx.x < 256) sums[threadIdx.x] = sum;
+    __syncthreads();
+    for (int d = 128; d > 0; d /= 2) {
+        if (threadIdx.x < static_cast<unsigned>(d)) sums[threadIdx.x] += sums[threadIdx.x + d];
+        __syncthreads();
+    }
+    const double all = sums[0];
+    __syncthreads();
+    return 1.0 / (sqrt(all) + static_cast<double>(eps));
 }
 #endif
 
