@@ -6,16 +6,15 @@
 //
 // What is held how.  What a step adds to a small singular direction is small beside the
 // large ones, and every later step magnifies an error there as it does the direction
-// (3.4^5 = 480 in all), so a state of one fp16 or bf16 value loses 2^-6 of a gradient
-// with few strong directions.  The state X is held in 32 bits, as the fp16 value that the
-// products take and what that leaves, in fp16 as well: 22 bits in all, read and written
-// with 8 bytes an element and step where fp32 beside the operand takes 10.  The operands
-// of the products, X's first part, A and b A + c A^2, are fp16, whose errors stay where
-// the operand is one factor among fp32 sums: 1e-3 at most of the result's norm, as much
-// as its own rounding to bf16 (against fp64: 704 x 2048, noise over 16 directions,
-// 1.1e-4; noise alone 1.5e-3).  Operands are scaled by 2^6 on their way to fp16, which
-// keeps entries of 2^-14 normal and any that the coefficients' check lets through finite;
-// what they leave by 2^11 more.
+// (3.4^5 = 480 in all): a state of one fp16 value gives a result 4 % off where noise of
+// 0.01 lies over 16 directions (704 x 2048; bf16 34 %).  The state X is held in 32 bits,
+// as the fp16 value that the products take and what that leaves, in fp16 as well: 22 bits
+// in all, read and written with 8 bytes an element and step where fp32 beside the operand
+// takes 10.  The operands of the products, X's first part, A and b A + c A^2, are fp16,
+// whose errors stay where the operand is one factor among fp32 sums: 3.3e-4 of the same
+// result, 1.5e-3 on noise alone, its rounding to bf16 1.7e-3.  Operands are scaled by 2^6
+// on their way to fp16, which keeps entries of 2^-14 normal and any that the coefficients'
+// check lets through finite; what they leave by 2^11 more.
 //
 // A and b A + c A^2 are symmetric: tiles on and below the diagonal are computed,
 // the others are their mirror images.  All matrices of a stack share each launch:

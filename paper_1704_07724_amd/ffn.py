@@ -5,6 +5,13 @@
     u = isc_w4_linear(n.mx8, up, route=r, relu=True)   # [T, 8, F], most of it zeros
     y = isc_w4_skip(u, down, route=r)                  # [T, D], the zeros of u skipped
 
+and of those that train it, on weights in 16 or 32 bits:
+
+    u = isc_expert_linear(x, w_up, r, relu=True)
+    y = isc_expert_linear(u, w_down, r, combine=True)
+    g = isc_expert_linear_bwd(dy, u, w_down, r, combine=True)   # g.dx, g.dw, g.dweights
+    o = isc_orthogonalize(g.dw)
+
 Argument marshalling only, as in the package itself; the C functions' names
 and rules (include/isc.h) are these functions'.  Leading dimensions of a tensor
 count as rows; a tensor whose rows are not evenly spaced, or whose values
