@@ -93,10 +93,10 @@ __global__ __launch_bounds__(1024) void orth_small_kernel(const SmallStep p) {
     const int row = wi + (lane & 31), col = wj + 16 * (lane >> 5);
     const int blocks = static_cast<int>((s.span() + 63) / 64);
     const bool first = p.step <= 0, last = p.step + 1 == p.a.steps;
-    float by = 0.0f;
+    double by = 0.0;  // as a double: the inverse of a small norm may be beyond fp32
     if (first)
-        by = static_cast<float>(orth_inverse_norm(reinterpret_cast<const double *>(p.a.ws), n, s.blocks(), p.a.eps,
-                                                  reinterpret_cast<double *>(lds[1])) * kOrthUp);
+        by = orth_inverse_norm(reinterpret_cast<const double *>(p.a.ws), n, s.blocks(), p.a.eps,
+                               reinterpret_cast<double *>(lds[1]));
     uint16_t *high = reinterpret_cast<uint16_t *>(p.a.ws + s.operand(0)) + n * s.of_state(),
              *low = reinterpret_cast<uint16_t *>(p.a.ws + s.low()) + n * s.of_state();
     char *square = lds[0], *poly = lds[1], *x = lds[2 + group];
@@ -141,7 +141,8 @@ __global__ __launch_bounds__(1024) void orth_small_kernel(const SmallStep p) {
                        there);
                 g.widen(u);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[8 * q + k] = k < there ? u[k] * by : 0.0f;  // inf * 0 is no zero
+                for (int k = 0; k < 8; ++k)  // inf * 0 is no zero
+                    v[8 * q + k] = k < there ? static_cast<float>(static_cast<double>(u[k]) * by) * kOrthUp : 0.0f;
             } else {
                 Raw8<F16> hi, lo;
                 hi.load(high + static_cast<int64_t>(r) * np + c + 8 * q, there > 0 ? 8 : 0);

@@ -76,7 +76,8 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(const OrthArgs a) {
     if (threadIdx.x == 0) reinterpret_cast<double *>(a.ws)[blockIdx.y * gridDim.x + blockIdx.x] = sums[0];
 }
 
-// The first state's operand; the first step takes the state itself from G.
+// The first state's operand; the first step takes the state itself from G.  Both scale in
+// fp64: the inverse of a small norm may be beyond fp32.
 template <class T>
 __global__ __launch_bounds__(256) void orth_scale_kernel(const OrthArgs a) {
     const OrthShape &s = a.s;
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
         if constexpr (WHAT == kApply) {
             const int np = p.s.np();
             const int64_t first = job.n * p.s.of_state();
-            const float by = p.g ? static_cast<float>(p.inverse[job.n] * kUp) : 0.0f;
+            const double by = p.g ? p.inverse[job.n] : 0.0;
             t.template each<false>(
                 lds,
                 [&](int i, int j) {
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(TL::kThreads) void orth_product_kernel(const OrthPr
                         else
                             beside.one.widen(x);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) x[k] *= by;
+                        for (int k = 0; k < 8; ++k) x[k] = static_cast<float>(static_cast<double>(x[k]) * by) * kUp;
                     } else {
                         float low[8];
                         beside.one.widen(x);

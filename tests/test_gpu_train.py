@@ -303,6 +303,62 @@ def test_values_that_are_not_finite_stay_in_their_rows(torch, isc, T, dtype):
     assert torch.equal(a.dx, b.dx) and torch.equal(a.dw, b.dw)
 
 
+@pytest.mark.parametrize("T", [9, 300])
+def test_an_expert_twice_and_many_pairs_of_one(torch, isc, T):
+    """Slots that name one expert are pairs like others; few pairs of many experts that all meet one."""
+    E, K, N, k = 64, 72, 40, 3
+    r = np.random.default_rng(T)
+    ids = np.full((T, k), 5, np.int32)
+    ids[:, 2] = r.integers(-1, E, T)
+    offsets, order = train.lists(ids, E)
+    weights = (r.random(ids.shape) * (ids >= 0)).astype(np.float32)
+    rt = isc.Route(*(torch.from_numpy(v).cuda() for v in (ids, weights, offsets, order)))
+    x, w = operands(torch, T, T, k, E, K, N, "bfloat16", True)
+    for combine in (False, True):
+        want, size = train.expert_linear(host(x), host(w), ids, False, weights.astype(np.float64) if combine else None)
+        close(host(isc.isc_expert_linear(x, w, rt, combine=combine)), want, (K + 64 + k) * E24 * size, "bfloat16", "y")
+    dy = dev(torch, r.standard_normal((T, k, N)), "bfloat16")
+    g = isc.isc_expert_linear_bwd(dy, x, w, rt)
+    there = (ids >= 0)[..., None]
+    d, xs = host(dy) * there, host(x)
+    back = np.einsum("tjn,tjnk->tjk", d, host(w)[ids.clip(0)])
+    size = np.einsum("tjn,tjnk->tjk", np.abs(d), np.abs(host(w))[ids.clip(0)])
+    close(host(g.dx), back.sum(1), (N + 64 + k) * E24 * size.sum(1), "bfloat16", "dx")
+    dw, dws = np.zeros((E, N, K)), np.zeros((E, N, K))
+    for j in range(k):
+        np.add.at(dw, ids[:, j].clip(0), d[:, j, :, None] * xs[:, None, :])
+        np.add.at(dws, ids[:, j].clip(0), np.abs(d[:, j, :, None] * xs[:, None, :]))
+    close(host(g.dw), dw, (T * k + 64) * E24 * dws, "bfloat16", "dw")
+
+
+@pytest.mark.parametrize("T", [5, 400])
+def test_weights_beyond_32_bits(torch, isc, T):
+    """2^32 weights and more: the last expert's products and gradients as those of a call on it alone."""
+    E, N, K = 9, 21848, 21848
+    ids = np.full((T, 1), E - 1, np.int32)
+    rt = isc.Route(*(dev(torch, v, "int32") if v.dtype != np.float32 else dev(torch, v)
+                     for v in (ids, np.ones((T, 1), np.float32), *train.lists(ids, E))))
+    only = isc.Route(*(dev(torch, v, "int32") if v.dtype != np.float32 else dev(torch, v)
+                       for v in (ids * 0, np.ones((T, 1), np.float32), *train.lists(ids * 0, 1))))
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn((T, K), generator=g, device="cuda").bfloat16()
+    w = torch.zeros((E, N, K), dtype=torch.bfloat16, device="cuda")
+    assert w.numel() > 2 ** 32
+    w[-1] = torch.randn((N, K), generator=g, device="cuda") * K ** -0.5
+    y = isc.isc_expert_linear(x, w, rt)
+    alone = w[-1:].clone()
+    rows = torch.arange(0, N, 311, device="cuda")
+    want = (x.double() @ alone[0, rows].double().t())[:, None]
+    size = (x.double().abs() @ alone[0, rows].double().abs().t())[:, None]
+    close(host(y[..., rows]), host(want), (K + 64) * E24 * host(size), "bfloat16", "y")
+    got, ref = isc.isc_expert_linear_bwd(y, x, w, rt), isc.isc_expert_linear_bwd(y, x, alone, only)
+    cols = torch.arange(0, K, 311, device="cuda")
+    back = y[:, 0].double() @ alone[0, :, cols].double()
+    size = y[:, 0].double().abs() @ alone[0, :, cols].double().abs()
+    close(host(got.dx[:, cols]), host(back), (N + 64) * E24 * host(size), "bfloat16", "dx")
+    assert torch.equal(got.dw[-1], ref.dw[0]) and all((part == 0).all() for part in got.dw[:-1])
+
+
 def test_fp32_over_its_range(torch, isc):
     """Magnitudes from 2^-60 to 2^60, and the largest there are."""
     T, k, E, K, N = 70, 1, 2, 64, 32
@@ -423,6 +479,34 @@ def test_orthogonalize_strides_scale_and_shapes(torch, isc):
     for scale in (1e-25, 1e25):
         check_orth(torch, isc, dev(torch, m[0] * scale), "bfloat16", eps=0.0)
     check_orth(torch, isc, dev(torch, m[0] * 1e-9), "bfloat16")  # a norm beside eps
+
+
+@pytest.mark.parametrize("shape", [(64, 70), (70, 64), (65, 72), (72, 65), (300, 200)], ids=str)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_orthogonalize_at_the_ends_of_the_range(torch, isc, shape, dtype):
+    """A power of two scales a norm and its inverse exactly, also where the inverse is beyond fp32."""
+    g = dev(torch, np.random.default_rng(8).integers(-7, 8, shape), dtype)
+    want = isc.isc_orthogonalize(g, eps=0.0)
+    assert torch.isfinite(want).all()
+    for power in (-133, -110, 100, 124):
+        scaled = torch.ldexp(g.double(), torch.tensor(power, device="cuda")).to(g.dtype)
+        assert (scaled != 0).sum() == (g != 0).sum()
+        assert torch.equal(isc.isc_orthogonalize(scaled, eps=0.0), want), power
+
+
+@pytest.mark.parametrize("shape", [(64, 520), (72, 464)], ids=str)
+def test_orthogonalize_beyond_32_bits(torch, isc, shape):
+    """2^31 values and more in a stack: the last matrix as the first."""
+    M, N = shape
+    many = 2 ** 31 // (M * N) + 8
+    g = dev(torch, gradient(9, 1, M, N, 4)[0], "bfloat16")
+    got = isc.isc_orthogonalize(g.expand(many, M, N).contiguous(), steps=2)
+    assert got.numel() > 2 ** 31
+    assert all((part == got[0]).all() for part in got.split(4096))
+    check_orth(torch, isc, g, "bfloat16", steps=2)
+    exact, rounded = (train.orthogonalize(host(g), [COEFFICIENTS] * 2, 1e-7, v) for v in (False, True))
+    allowed = 3 * np.linalg.norm(rounded - exact) + U["bfloat16"] * np.linalg.norm(exact)
+    assert np.linalg.norm(host(got[-1]) - exact) <= allowed
 
 
 def test_orthogonalize_zeros_and_values_that_are_not_finite(torch, isc):
