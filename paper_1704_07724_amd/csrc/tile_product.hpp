@@ -16,8 +16,11 @@
 //     on average and to 2^-21 at most: fp32's precision at a sixth of the bf16
 //     rate, which is 2.6 times that of the fp32 matrix instruction.
 //
-// v_mfma_f32_32x32x16: lane l holds 8 consecutive r (from 8 * (l / 32)) of row
-// l % 32 of each operand; of the result, column l % 32 and the rows
+// 16 bits, v_mfma_f32_16x16x32: lane l holds 8 consecutive r (from 8 * (l / 16)) of
+// row l % 16 of each operand; of the result, column l % 16 and the four rows from
+// 4 * (l / 16) on.
+// fp32's parts, v_mfma_f32_32x32x16: lane l holds 8 consecutive r (from 8 * (l / 32))
+// of row l % 32 of each operand; of the result, column l % 32 and the rows
 // 8 * (n / 4) + 4 * (l / 32) + n % 4.  W's rows are dealt to the instruction's so
 // that these are the 16 consecutive j from 16 * (l / 32).
 //
@@ -31,6 +34,7 @@ namespace isc {
 namespace tp {
 
 using f32x16 = __attribute__((ext_vector_type(16))) float;
+using f32x4 = __attribute__((ext_vector_type(4))) float;
 using s16x8 = __attribute__((ext_vector_type(8))) short;
 using s16x4 = __attribute__((ext_vector_type(4))) short;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
@@ -49,6 +53,15 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
     else
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
                                                        0, 0, 0);
+}
+
+// 16 x 16 results of 32 inner indices.
+template <class T>
+__device__ __forceinline__ f32x4 mfma_16(s16x8 a, s16x8 b, f32x4 c) {
+    if constexpr (std::is_same_v<T, F16>)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 // A direct load into LDS: 16 bytes from each lane's address to `lds` (uniform)
@@ -155,18 +168,23 @@ struct Stage {
     static constexpr int kBytes = OUT * BK * 2;                     // of a part
     static constexpr int kLoads = kRow * kLines / THREADS;          // chunks of a thread
     static constexpr int kHop = THREADS / kRow;                     // LDS rows between a thread's chunks
-    static_assert(kRow * kLines % THREADS == 0 && THREADS % kRow == 0 && kHop % 8 == 0, "a thread's chunks");
+    static_assert(kRow * kLines % THREADS == 0 && THREADS % kRow == 0 && kHop % (SIDE == kAcross ? 16 : 8) == 0,
+                  "a thread's chunks");
     static_assert(!DIRECT || !kWide, "fp32 goes through registers");
 
     // Where chunk c of LDS row `line` is.  64 banks are 16 chunks: the 16 lanes that read a
     // chunk of consecutive rows, and the 32 that read four chunks of four rows, meet each once.
     static __device__ __forceinline__ int place(int line, int c) {
         constexpr int kShare = kRow < 16 ? 16 / kRow : 1;  // rows of all banks
-        if constexpr (SIDE == kAcross) return c ^ (line / kShare % (4 / (kShare < 4 ? kShare : 4)) * 4);
+        if constexpr (SIDE == kAcross)
+            return c ^ (line / kShare % (4 / (kShare < 4 ? kShare : 4)) * 4) ^ (line >> 3 & 1) * 2;
         return c ^ (line / kShare % kRow);
     }
 
-    const char *at[SIDE == kAlong ? kLoads : 1];  // kAlong: the rows' chunks at r = 0
+    const char *at[SIDE == kAlong ? kLoads : 1];  // kAlong: the rows' chunks at r = 0; else the first row's
+    int width, count;                             // of `rows`, known to be uniform
+    int64_t stride;
+    bool edge;                                    // kAcross: some of the tile's columns are past the last one
     int32_t next[kFetch ? kLoads : 1];            // the listed rows of the stage to be sent
     int line, col;                                // this thread's first LDS row, and the element its chunks begin at
     Rows rows;
@@ -175,6 +193,12 @@ struct Stage {
     // o0: the tile's first outer index; inner: how many inner indices there are.
     __device__ __forceinline__ void begin(const Rows &r, int o0, int tid) {
         rows = r;
+        width = __builtin_amdgcn_readfirstlane(r.width);
+        count = __builtin_amdgcn_readfirstlane(r.count);
+        stride = static_cast<int64_t>(static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(r.stride >> 32)))
+                                          << 32 |
+                                      static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(r.stride))));
+        edge = o0 + OUT > width;
         line = tid / kRow;
         col = place(line, tid % kRow) * 8;
         if constexpr (SIDE == kAlong) {
@@ -191,7 +215,7 @@ struct Stage {
             }
         } else {
             col += o0;
-            at[0] = r.base + int64_t{col} * kSize;
+            at[0] = r.base + int64_t{col} * kSize + (kFetch ? 0 : line * stride);
             if constexpr (kFetch) fetch(0, tid);
         }
     }
@@ -218,32 +242,41 @@ struct Stage {
         }
     }
 
-    // The address of chunk n of the stage at r0, and how many of its elements exist.
-    __device__ __forceinline__ const char *chunk(int n, int r0, int &there) const {
-        if constexpr (SIDE == kAlong) {
-            there = rows.width - r0 - col;
+    // The address of chunk n of the stage at r0 ...
+    __device__ __forceinline__ const char *chunk(int n, int r0) const {
+        if constexpr (SIDE == kAlong)
             return at[n] + int64_t{r0} * kSize;
-        } else {
-            int32_t row = r0 + line + n * kHop;
-            if constexpr (kFetch)
-                row = next[n];
-            else
-                row = row < rows.count ? row : -1;
-            there = row < 0 ? 0 : rows.width - col;
-            return at[0] + int64_t{row} * rows.stride;
+        else if constexpr (kFetch)
+            return at[0] + int64_t{next[n]} * stride;
+        else {
+            int64_t past = (r0 + n * kHop) * stride;
+            asm("" : "+s"(past));  // by the scalar unit: a vector one would multiply for every lane
+            return at[0] + past;
         }
+    }
+    // ... and how many of its elements exist.
+    __device__ __forceinline__ int there(int n, int r0) const {
+        if constexpr (SIDE == kAlong)
+            return width - r0 - col;
+        else if constexpr (kFetch)
+            return next[n] < 0 ? 0 : width - col;
+        else
+            return r0 + line + n * kHop < count ? width - col : 0;
     }
 
     // Sends load n of the stage from r0 on; a direct one to LDS at `lds`.
     __device__ __forceinline__ void send(int n, int r0, uint32_t lds, int wave) {
-        int there;
-        const char *p = chunk(n, r0, there);
+        const char *p = chunk(n, r0);
         if constexpr (DIRECT) {
-            // width and column are multiples of 8: a chunk exists as a whole or not at all
-            if (SIDE == kAcross || r0 + BK > rows.width) p = there > 0 ? p : reinterpret_cast<const char *>(kZeros);
+            // width and column are multiples of 8: a chunk exists as a whole or not at all.  Where
+            // all do, nothing is to be asked: the empty asm keeps this a branch.
+            if (kFetch || (SIDE == kAlong ? r0 + BK > width : edge || r0 + BK > count)) {
+                if constexpr (!kFetch) asm volatile("");
+                p = there(n, r0) > 0 ? p : reinterpret_cast<const char *>(kZeros);
+            }
             load_direct(p, lds + (n * THREADS + wave * 64) * 16);
         } else {
-            held[n].load(p, there);
+            held[n].load(p, there(n, r0));
         }
     }
     __device__ __forceinline__ void send_all(int r0, uint32_t lds, int wave, int tid) {
@@ -299,6 +332,28 @@ struct Stage {
             return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
+
+    // The same for mfma_16, of 32 inner indices from 32 * kk on and 16 outer ones, number t of
+    // those of a wavefront, that begin at o: lane_at(o) + what t and kk change, which are bits
+    // that the lane's place leaves alone or are flipped in it.
+    static __device__ __forceinline__ int lane_at(int o, int lane) {
+        const int i = lane & 15, g = lane >> 4;
+        if constexpr (SIDE == kAlong) return ((o + i) * kRow + place(o + i, g)) * 16;
+        const int r = 8 * g + (i >> 2), c = o + 4 * (i & 3);
+        return (r * kRow + place(r, c >> 3)) * 16 + (c & 7) * 2;
+    }
+    static __device__ __forceinline__ s16x8 operand_16(const char *lds, int at, int t, int kk) {
+        if constexpr (SIDE == kAlong) {
+            return *reinterpret_cast<const s16x8 *>(lds + (at ^ 64 * kk) + t * 256 * kRow);
+        } else {
+            s16x4 v[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                v[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(
+                    lds + (at ^ 32 * t) + (32 * kk + 4 * q) * kRow * 16));
+            return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
 };
 
 // A workgroup's tile: BI x BJ results by WI x WJ wavefronts, BK inner indices a stage.
@@ -310,8 +365,8 @@ struct Stage {
 //     TFLOP/s), by 128 x 128 283; dw of the same 350 and 609; 4 wavefronts of 128 x 128
 //     results, one a SIMD, are 15 % slower, four stages of 32 inner indices 5 %, since half
 //     a line a row is asked for at a time.
-//   A stage of 256 x 256 takes 2.0 us with every compute unit busy: its products alone take
-//     1.1, its loads and reads alone 1.0, and they overlap in part.
+//   A stage of 256 x 256 takes 1.8 us with every compute unit busy; what is sent, read and
+//     multiplied in it, without the tile around it, 1.4.
 template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, bool LISTED = false,
           int BK_ = 64>
 struct Tile {
@@ -320,7 +375,14 @@ struct Tile {
     static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
     static constexpr int kWaves = WI * WJ, kThreads = 64 * kWaves;
     static constexpr int BK = std::is_same_v<T, F32> && BI > 64 ? 32 : BK_;
-    static constexpr int FI = BI / WI / 32, FJ = BJ / WJ / 32;
+    // 16 bits go by the smaller instruction, which takes less power for a product.  Power is what
+    // bounds a loop of nothing but a stage's products, reads and loads: with all compute
+    // units busy 1.05 us where all operands are alike, on random ones 1.41, by
+    // 32 x 32 x 16 1.62.
+    static constexpr bool kSmall = !std::is_same_v<T, F32>;
+    static constexpr int kEdge = kSmall ? 16 : 32;  // of an instruction's results
+    static constexpr int FI = BI / WI / kEdge, FJ = BJ / WJ / kEdge;
+    using Sums = std::conditional_t<kSmall, f32x4, f32x16>;
     using XStage = Stage<T, DIRECT, XS, LISTED, BI, BK, kThreads>;
     using WStage = Stage<T, DIRECT, WS, LISTED, BJ, BK, kThreads>;
     static constexpr int kParts = XStage::kParts;
@@ -331,7 +393,7 @@ struct Tile {
     // fp32: the products with a part of less than the first add up beside the others, which
     // then are rounded once for every 16 inner indices, not six times.
     static constexpr int kSums = kParts > 1 ? 2 : 1;
-    f32x16 acc[FJ][FI], low[kSums > 1 ? FJ : 1][kSums > 1 ? FI : 1];
+    Sums acc[FJ][FI], low[kSums > 1 ? FJ : 1][kSums > 1 ? FI : 1];
 
     // What a wavefront multiplies at a time: 16 inner indices.
     struct Operands {
@@ -404,8 +466,8 @@ struct Tile {
     }
 
     // The sums of the tile that start() began, over `inner` inner indices, of whose rows and
-    // columns the first `rows` and `cols` are asked for.  The operands of the
-    // next 16 are read ahead of the products of those at hand; a stage's last are in
+    // columns the first `rows` and `cols` are asked for.  Operands are
+    // read ahead of their products; a stage's last are in
     // registers when the wavefronts meet, so that behind the barrier its place is free.
     // Loads are sent one at a time between products: sent together they would hold the
     // wavefront, and the matrix cores with it, until the address unit has taken them.
@@ -419,16 +481,13 @@ struct Tile {
 #pragma unroll
             for (int i = 0; i < FI; ++i)
 #pragma unroll
-                for (int n = 0; n < 16; ++n) {
+                for (int n = 0; n < kEdge * kEdge / 64; ++n) {
                     acc[j][i][n] = 0.0f;
                     if constexpr (kSums > 1) low[j][i][n] = 0.0f;
                 }
         const int steps = (inner + BK - 1) / BK;
         if (steps <= 0) return;
-        constexpr int kSteps16 = BK / 16;
-        static_assert(kSteps16 % 2 == 0, "a stage's first operands are always at[0]");
         const uint32_t base = lds_address(lds);
-        int x_now = 0;  // the place in LDS of this stage's X
         if constexpr (DIRECT) {
             if (landed)
                 meet();
@@ -443,9 +502,75 @@ struct Tile {
             ws.commit(lds + w_at(0), tid);
             land<0>();
         }
+        if constexpr (kSmall)
+            small_steps(steps, busy, wi, wj, lds);
+        else
+            wide_steps(steps, busy, wi, wj, lds);
+        // no load into LDS may outlive its tile, and all of its reads are done before the next one's
+        land<0>();
+    }
+
+    // fp32's stages
+    __device__ __forceinline__ void wide_steps(int steps, bool busy, int wi, int wj, char *lds) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        constexpr int kSteps16 = BK / 16;
+        static_assert(kSmall || kSteps16 % 2 == 0, "a stage's first operands are always at[0]");
+        int x_now = 0;  // the place in LDS of this stage's X
         Operands at[2];
 #pragma unroll
         for (int n = 0; n < kReads; ++n) read(at[0], n, lds, lds + w_at(0), 0, wi, wj, lane);
+        for (int s = 0; s < steps; ++s) {
+            const bool more = s + 1 < steps;
+            const int x_then = x_next(x_now);
+            if (more) {
+                xs.send_all((s + 1) * BK, 0, wave, tid);
+                ws.send_all((s + 1) * BK, 0, wave, tid);
+            }
+#pragma unroll
+            for (int kk = 0; kk < kSteps16; ++kk) {
+                if (kk + 1 == kSteps16 && more) {
+                    xs.commit(lds + x_then, tid);
+                    ws.commit(lds + w_at(s + 1), tid);
+                    land<0>();
+                }
+                // the operands of the next 16: behind the last stage's, those of some stage, which nothing takes
+                const char *from_x = lds + (kk + 1 < kSteps16 ? x_now : x_then),
+                           *from_w = lds + (kk + 1 < kSteps16 ? w_at(s) : w_at(s + 1));
+                __builtin_amdgcn_sched_barrier(0);
+                if (busy)
+                    multiply(at[kk & 1], [&](int n) {
+                        constexpr int kEach = (kReads + kProducts - 1) / kProducts;
+#pragma unroll
+                        for (int q = n * kEach; q < (n + 1) * kEach && q < kReads; ++q)
+                            read(at[(kk + 1) & 1], q, from_x, from_w, (kk + 1) % kSteps16, wi, wj, lane);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            x_now = x_then;
+        }
+    }
+
+    // 16 bits': a step of 32 inner indices is a product of each of X's operands, in turn, with
+    // all of W's.  Of the 256 x 256 tile's X four are in registers, read three ahead of their
+    // products, of smaller tiles' a step's beside the next one's; W's are a step's and the next.
+    static constexpr int kAhead = FI > 4 ? 3 : FI, kPlaces = FI > 4 ? 4 : 2 * FI;
+    static constexpr int kMeet = FI - kAhead;  // behind this many of X's operands only the next step's are read
+    static_assert(!kSmall || FI <= 4 || (FI % 4 == 0 && DIRECT), "X's places");
+    static constexpr int kWGroups = kAhead > 1 ? kAhead - 1 : 1, kWEach = (FJ + kWGroups - 1) / kWGroups;
+    __device__ __forceinline__ void small_steps(int steps, bool busy, int wi, int wj, char *lds) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const uint32_t base = lds_address(lds);
+        constexpr int kSteps = BK / 32;
+        static_assert(!kSmall || kSteps % 2 == 0, "a stage's first operands have the first places");
+        int x_now = 0;  // the place in LDS of this stage's X
+        const int lane_x = XStage::lane_at(wi, lane), lane_w = WStage::lane_at(wj, lane);
+        s16x8 w[2][FJ], x[kPlaces];
+        const auto at = [](int kk, int i) { return FI > 4 ? i % 4 : (kk & 1) * FI + i; };
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) w[0][j] = WStage::operand_16(lds + w_at(0), lane_w, j, 0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) x[at(0, i)] = XStage::operand_16(lds, lane_x, i, 0);
         for (int s = 0; s < steps; ++s) {
             const bool more = s + 1 < steps, most = s + 2 < steps;
             const int x_then = x_next(x_now), x_last = x_next(x_then);
@@ -454,8 +579,61 @@ struct Tile {
                 ws.send_all((s + 1) * BK, 0, wave, tid);
             }
 #pragma unroll
-            for (int kk = 0; kk < kSteps16; ++kk) {
-                if (kk + 1 == kSteps16 && more) {
+            for (int kk = 0; kk < kSteps; ++kk) {
+                const bool end = kk + 1 == kSteps;
+                // behind the last stage's operands those of some stage are read, which nothing takes
+                const char *from_x = lds + (end ? x_then : x_now), *from_w = lds + (end ? w_at(s + 1) : w_at(s));
+                // X's next-but-two goes where the last stage's X was, W's next-but-one, from the
+                // meeting on, where this stage's is
+                const auto send = [&](int n) {
+                    if constexpr (DIRECT) {
+                        constexpr int kX = (XStage::kLoads + FI * FJ - 1) / (FI * FJ);
+                        constexpr int kW = (WStage::kLoads + kAhead * FJ - 1) / (kAhead * FJ);
+                        if (kk == 0 && most) {
+#pragma unroll
+                            for (int q = n * kX; q < (n + 1) * kX && q < XStage::kLoads; ++q) {
+                                xs.send(q, (s + 2) * BK, base + x_last, wave);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                        const int m = n - kMeet * FJ;
+                        if (end && most && m >= 0) {
+#pragma unroll
+                            for (int q = m * kW; q < (m + 1) * kW && q < WStage::kLoads; ++q) {
+                                ws.send(q, (s + 2) * BK, base + w_at(s), wave);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                    }
+                };
+                const auto group = [&](int i) {
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) {
+                        acc[j][i] = mfma_16<T>(w[kk & 1][j], x[at(kk, i)], acc[j][i]);
+                        const int n = i - kMeet;  // W's of the next step, kWEach with each of X's
+                        if (j == 0) {
+                            const int t = i + kAhead;
+                            if (t < FI)
+                                x[at(kk, t)] = XStage::operand_16(lds + x_now, lane_x, t, kk);
+                            else
+                                x[at(kk + 1, t - FI)] = XStage::operand_16(from_x, lane_x, t - FI, (kk + 1) % kSteps);
+                        }
+                        if (n >= 0 && j < kWEach && n * kWEach + j < FJ)
+                            w[(kk + 1) & 1][n * kWEach + j] =
+                                WStage::operand_16(from_w, lane_w, n * kWEach + j, (kk + 1) % kSteps);
+                        __builtin_amdgcn_sched_barrier(0);
+                        send(i * FJ + j);
+                    }
+                };
+                __builtin_amdgcn_sched_barrier(0);
+                if (busy) {
+#pragma unroll
+                    for (int i = 0; i < kMeet; ++i) group(i);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < kMeet * FJ; ++n) send(n);
+                }
+                if (end && more) {
                     if constexpr (DIRECT) {
                         if (most)
                             land<DIRECT ? XStage::kLoads : 0>();
@@ -467,55 +645,22 @@ struct Tile {
                         land<0>();
                     }
                 }
-                // the operands of the next 16: behind the last stage's, those of some stage, which nothing takes
-                const char *from_x = lds + (kk + 1 < kSteps16 ? x_now : x_then),
-                           *from_w = lds + (kk + 1 < kSteps16 ? w_at(s) : w_at(s + 1));
-                // X's next-but-two goes where the last stage's X was, W's next-but-one, from the
-                // meeting on, where this stage's is
-                const auto send = [&](int n) {
-                    if constexpr (DIRECT) {
-                        constexpr int kW = (WStage::kLoads + kProducts - 1) / kProducts;
-                        constexpr int kX = (XStage::kLoads + kProducts - 1) / kProducts;
-                        if (kk == 0 && most) {
-#pragma unroll
-                            for (int q = n * kX; q < (n + 1) * kX && q < XStage::kLoads; ++q) {
-                                xs.send(q, (s + 2) * BK, base + x_last, wave);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                        }
-                        if (kk + 1 == kSteps16 && most) {
-#pragma unroll
-                            for (int q = n * kW; q < (n + 1) * kW && q < WStage::kLoads; ++q) {
-                                ws.send(q, (s + 2) * BK, base + w_at(s), wave);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                        }
-                    }
-                };
                 __builtin_amdgcn_sched_barrier(0);
                 if (busy) {
-                    multiply(at[kk & 1], [&](int n) {
-                        constexpr int kEach = (kReads + kProducts - 1) / kProducts;
 #pragma unroll
-                        for (int q = n * kEach; q < (n + 1) * kEach && q < kReads; ++q)
-                            read(at[(kk + 1) & 1], q, from_x, from_w, (kk + 1) % kSteps16, wi, wj, lane);
-                        __builtin_amdgcn_sched_barrier(0);
-                        send(n);
-                    });
+                    for (int i = kMeet; i < FI; ++i) group(i);
                 } else {
 #pragma unroll
-                    for (int n = 0; n < kProducts; ++n) send(n);
+                    for (int n = kMeet * FJ; n < FI * FJ; ++n) send(n);
                 }
                 if constexpr (DIRECT) {
-                    if constexpr (WStage::kFetch) if (kk + 1 == kSteps16 && most) ws.fetch((s + 3) * BK, tid);
+                    if constexpr (WStage::kFetch) if (end && most) ws.fetch((s + 3) * BK, tid);
                     if constexpr (XStage::kFetch) if (kk == 0 && most) xs.fetch((s + 3) * BK, tid);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
             x_now = x_then;
         }
-        // no load into LDS may outlive its tile, and all of its reads are done before the next one's
-        land<0>();
     }
 
     // A wavefront's results pass through LDS, 32 rows at a time and in places that start()
@@ -541,7 +686,7 @@ struct Tile {
         }
         const auto place = [&](int row, int c) { return own + (row * kChunks + (c ^ (row & (kChunks - 1)))) * 16; };
 #pragma unroll
-        for (int i = 0; i < FI; ++i) {
+        for (int i = 0; i < BI / WI / 32; ++i) {
             constexpr int kRows = 64 / kLanes;  // of all lanes at a time
             const int row = lane / kLanes, c = lane % kLanes * 2;
             decltype(ahead(0, 0)) beside[32 / kRows];
@@ -551,13 +696,20 @@ struct Tile {
 #pragma unroll
                 for (int j = 0; j < FJ; ++j) acc[j][i] += low[j][i];
             // the last rows' stores are the only ones that follow start()'s loads unwaited for
-            if (i == FI - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+            if (i == BI / WI / 32 - 1) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 #pragma unroll
             for (int j = 0; j < FJ; ++j)
+                if constexpr (kSmall) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<float4 *>(place(lane & 31, 8 * j + 4 * (lane >> 5) + q)) =
-                        make_float4(acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]);
+                    for (int q = 0; q < 2; ++q)
+                        *reinterpret_cast<float4 *>(place(16 * q + (lane & 15), 4 * j + (lane >> 4))) =
+                            make_float4(acc[j][2 * i + q][0], acc[j][2 * i + q][1], acc[j][2 * i + q][2], acc[j][2 * i + q][3]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<float4 *>(place(lane & 31, 8 * j + 4 * (lane >> 5) + q)) = make_float4(
+                            acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]);
+                }
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int r = 0; r < 32 / kRows; ++r) {
