@@ -725,13 +725,13 @@ struct Tile {
             if constexpr (MIRROR) {
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-                for (int r = 0; r < 32; r += 8) {  // a lane a column
-                    const int col = lane % kCols;
+                for (int r = 0; r < kCols; r += 16) {  // four lanes a column
+                    const int col = r + lane / 4, from = lane % 4 * 8;
                     float v[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        v[k] = reinterpret_cast<const float *>(place(r + k, col >> 2))[col & 3];
-                    turned(wj + col, wi + 32 * i + r, v);
+                        v[k] = reinterpret_cast<const float *>(place(from + k, col >> 2))[col & 3];
+                    turned(wj + col, wi + 32 * i + from, v);
                 }
             }
             __builtin_amdgcn_wave_barrier();
