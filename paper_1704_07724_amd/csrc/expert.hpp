@@ -40,7 +40,7 @@ struct ExpertBwdArgs {
     void *dx, *dw;        // each nullptr where it is not asked for
     float *dweights;
     int64_t lddx;
-    void *masked;         // P rows of dy, rectified or weighted, expert_ld() elements apart
+    void *masked;         // P rows of dy, rectified or weighted, in the places' order, expert_ld() elements apart
     float *part, *dots;   // part: P rows of dx; dots: what each row's tiles give to dweights
 };
 
@@ -77,7 +77,7 @@ namespace tp {
 // A product over rows by expert: out[pair] = sum over r of X(pair, r) W_e(j, r).
 struct RowsArgs {
     ExpertPlan plan;
-    Rows x, w;          // x by the list of places; w: the first expert's
+    Rows x, w;          // x by the list of places, or its rows in their order; w: the first expert's
     int64_t expert;     // bytes from one expert's matrix to the next
     int inner, cols;    // inner indices, columns of the result
     void *out;
@@ -112,7 +112,10 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
         const int e = __builtin_amdgcn_readfirstlane(tile.x);
         const Job j{__builtin_amdgcn_readfirstlane(tile.y), __builtin_amdgcn_readfirstlane(tile.z), id % across * TL::BJ};
         Rows x = a.x, w = a.w;
-        x.list += j.first;
+        if (x.list)
+            x.list += j.first;
+        else
+            x.base += j.first * x.stride;
         x.count = j.rows;
         w.base += e * a.expert;
         t.start(x, w, 0, j.j0, a.inner, lds);
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
 
 // Whether a side's rows can go into LDS by direct loads.
 inline bool direct_rows(const void *p, int64_t ld, int width, int size) {
-    return size == 2 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && width % 8 == 0;
+    return size == 2 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && width % 8 == 0 && ld < int64_t{1} << 31;
 }
 
 template <class TL>

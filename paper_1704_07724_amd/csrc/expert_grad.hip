@@ -20,7 +20,8 @@ namespace {
 
 using namespace tp;
 
-// masked[p] = the gradient of pair p's product; nothing where it has no expert.
+// masked[i] = the gradient of the product of the pair at place i; nothing where it has no
+// expert.  In the places' order, so that the products read consecutive rows.
 template <class T>
 __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b, int64_t ld) {
     const ExpertArgs &a = b.a;
@@ -28,9 +29,9 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
     const int groups = static_cast<int>(ld / 8);
     const int64_t all = static_cast<int64_t>(a.T) * a.slots * groups, hop = static_cast<int64_t>(gridDim.x) * 256;
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; n < all; n += hop) {
-        const int64_t p = n / groups;
-        const int c = static_cast<int>(n - p * groups) * 8;
-        if (static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E)) {
+        const int64_t i = n / groups, p = a.plan.pairs[i];
+        const int c = static_cast<int>(n - i * groups) * 8;
+        if (p >= 0 && static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E)) {
             float v[8];
             load8<T>(v, static_cast<const V *>(b.dy) + (b.combine ? p / a.slots : p) * b.lddy + c, a.N - c);
             if (b.y) {
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] = c + q < a.N ? v[q] * w : 0.0f;
             }
-            store8<T>(static_cast<V *>(b.masked) + p * ld + c, v, 8);
+            store8<T>(static_cast<V *>(b.masked) + i * ld + c, v, 8);
         }
     }
 }
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(256) void expert_dots_kernel(const ExpertArgs a, co
 
 struct DwArgs {
     const int32_t *offsets;
-    Rows d, x;  // listed by place
+    Rows d, x;  // listed by place, or d's in the places' order
     int P, N, K;
     void *dw;
     int nexp;
@@ -83,7 +84,10 @@ __global__ __launch_bounds__(TL::kThreads) void expert_dw_kernel(const DwArgs a,
         const int first = lo < 0 ? 0 : lo > a.P ? a.P : lo, end = hi > a.P ? a.P : hi;
         Rows d = a.d, x = a.x;
         d.count = x.count = j.inner = end > first ? end - first : 0;
-        d.list += first;
+        if (d.list)
+            d.list += first;
+        else
+            d.base += first * d.stride;
         x.list += first;
         t.start(d, x, j.i0, j.j0, j.inner, lds);
         return j;
@@ -190,7 +194,7 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
         e = a.type == ISC_F32 ? launch_mask<F32>(b, s) : a.type == ISC_BF16 ? launch_mask<BF16>(b, s) : launch_mask<F16>(b, s);
         if (e != hipSuccess) return e;
     }
-    const Rows masked{static_cast<const char *>(b.masked), ldm * size, a.plan.pairs, 0, a.N};
+    const Rows masked{static_cast<const char *>(b.masked), ldm * size, nullptr, 0, a.N};
     const Rows given{static_cast<const char *>(b.dy), b.lddy * size, b.combine ? a.plan.tokens : a.plan.pairs, 0, a.N};
     if (b.dx || b.dweights) {
         RowsArgs r{};

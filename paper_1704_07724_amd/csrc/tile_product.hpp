@@ -226,6 +226,11 @@ struct Stage {
     __device__ __forceinline__ void fetch(int r0, int tid) {
         constexpr int kRows = kRow < 64 ? 64 / kRow : 1;
         const int own = kRows > 1 ? (tid & 63) / kRow : 0;
+        if (!rows.list) {
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) next[n] = r0 + line + n * kHop < count ? r0 + line + n * kHop : -1;
+            return;
+        }
         const int first = r0 + __builtin_amdgcn_readfirstlane(line - own);
         using Scalar = const __attribute__((address_space(4))) int32_t *;
         Scalar list = reinterpret_cast<Scalar>(reinterpret_cast<uintptr_t>(rows.list));
@@ -235,7 +240,7 @@ struct Stage {
 #pragma unroll
             for (int q = 0; q < kRows; ++q) {
                 const int r = first + n * kHop + q;
-                const int32_t number = r >= rows.count ? -1 : list[r];
+                const int32_t number = r >= count ? -1 : list[r];
                 row = own == q ? number : row;
             }
             next[n] = row;
@@ -247,7 +252,9 @@ struct Stage {
         if constexpr (SIDE == kAlong)
             return at[n] + int64_t{r0} * kSize;
         else if constexpr (kFetch)
-            return at[0] + int64_t{next[n]} * stride;
+            // direct loads are taken where a stride has 32 bits (direct_rows): one instruction
+            return at[0] + (DIRECT ? static_cast<int64_t>(uint64_t{static_cast<uint32_t>(next[n])} * static_cast<uint32_t>(stride))
+                                   : next[n] * stride);
         else {
             int64_t past = (r0 + n * kHop) * stride;
             asm("" : "+s"(past));  // by the scalar unit: a vector one would multiply for every lane
