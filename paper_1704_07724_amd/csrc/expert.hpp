@@ -187,7 +187,7 @@ hipError_t launch_rows_of(const RowsArgs &a, int64_t pairs, int E, int rows, hip
         if (rows == 256) return launch_rows<Tile<T, true, kAlong, WS, 256, 256, 2, 4>>(a, pairs, E, s);
     if constexpr (!std::is_same_v<T, F32>)
         if (rows == 32) return launch_rows<Tile<T, DIRECT, kAlong, WS, 32, 128, 1, 4>>(a, pairs, E, s);
-    if (rows == 64) return launch_rows<Tile<T, DIRECT, kAlong, WS, 64, 64, 2, 2, false, kInner64<DIRECT>>>(a, pairs, E, s);
+    if (rows == 64) return launch_rows<Tile<T, DIRECT, kAlong, WS, 64, 64, 2, 2, 0, kInner64<DIRECT>>>(a, pairs, E, s);
     return launch_rows<Tile<T, DIRECT, kAlong, WS, 128, 128, 2, kWavesOf128<T>>>(a, pairs, E, s);
 }
 template <Side WS>

@@ -145,9 +145,11 @@ hipError_t launch_dw_of(const DwArgs &a, hipStream_t s) {
     };
     const int side = tile_side(DIRECT ? tiles(256) : 0, tiles(128), std::is_same_v<T, F32>);
     if constexpr (DIRECT)
-        if (side == 256) return launch_dw<Tile<T, true, kAcross, kAcross, 256, 256, 2, 4, true>>(a, s);
-    if (side == 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, kWavesOf128<T>, true>>(a, s);
-    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 64, 64, 2, 2, true, kInner64<DIRECT>>>(a, s);
+        if (side == 256)
+            return a.d.list ? launch_dw<Tile<T, true, kAcross, kAcross, 256, 256, 2, 4, 3>>(a, s)
+                            : launch_dw<Tile<T, true, kAcross, kAcross, 256, 256, 2, 4, 2>>(a, s);
+    if (side == 128) return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 128, 128, 2, kWavesOf128<T>, 3>>(a, s);
+    return launch_dw<Tile<T, DIRECT, kAcross, kAcross, 64, 64, 2, 2, 3, kInner64<DIRECT>>>(a, s);
 }
 
 template <class T>

@@ -372,9 +372,10 @@ struct Stage {
 //     TFLOP/s), by 128 x 128 283; dw of the same 350 and 609; 4 wavefronts of 128 x 128
 //     results, one a SIMD, are 15 % slower, four stages of 32 inner indices 5 %, since half
 //     a line a row is asked for at a time.
+//   LISTED: whose rows across come by a list, X's 1, W's 2.
 //   A stage of 256 x 256 takes 1.8 us with every compute unit busy; what is sent, read and
 //     multiplied in it, without the tile around it, 1.4.
-template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, bool LISTED = false,
+template <class T_, bool DIRECT_, Side XS, Side WS, int BI_, int BJ_, int WI_, int WJ_, int LISTED = 0,
           int BK_ = 64>
 struct Tile {
     using T = T_;
@@ -390,8 +391,8 @@ struct Tile {
     static constexpr int kEdge = kSmall ? 16 : 32;  // of an instruction's results
     static constexpr int FI = BI / WI / kEdge, FJ = BJ / WJ / kEdge;
     using Sums = std::conditional_t<kSmall, f32x4, f32x16>;
-    using XStage = Stage<T, DIRECT, XS, LISTED, BI, BK, kThreads>;
-    using WStage = Stage<T, DIRECT, WS, LISTED, BJ, BK, kThreads>;
+    using XStage = Stage<T, DIRECT, XS, (LISTED & 1) != 0, BI, BK, kThreads>;
+    using WStage = Stage<T, DIRECT, WS, (LISTED & 2) != 0, BJ, BK, kThreads>;
     static constexpr int kParts = XStage::kParts;
     static constexpr int kXBytes = XStage::kBytes * kParts, kWBytes = WStage::kBytes * kParts;
     static constexpr int kXStages = DIRECT ? 3 : 2;

@@ -184,7 +184,7 @@ def test_bwd(torch, isc, shape, dtype, form, shared):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("form", ["relu", "combine"])
+@pytest.mark.parametrize("form", ["relu", "combine", "plain"])
 @pytest.mark.parametrize("many,groups", [(60, 8), (80, 10), (130, 16)])  # sides of dx's tiles, of dw's: 128, 64; 256, 128; 256, 256
 def test_bwd_by_larger_tiles(torch, isc, dtype, form, many, groups):
     """Wide matrices: gradients that are the same for every group of columns, since the matrices are."""
@@ -196,7 +196,7 @@ def test_bwd_by_larger_tiles(torch, isc, dtype, form, many, groups):
     dy = dev(torch, np.random.default_rng(9).standard_normal((T, N) if combine else (T, k, N)), dtype)
     dd = torch.cat([dy] + [torch.zeros_like(dy)] * (groups - 2) + [dy], -1)  # the first and the last group of outputs
     y = None
-    if not combine:
+    if form == "relu":
         y = torch.relu(dev(torch, np.random.default_rng(2).standard_normal((T, k, N)), dtype)).repeat(1, 1, groups)
     got = isc.isc_expert_linear_bwd(dd, xx, ww, rt, y=y, combine=combine)
     want = train.expert_linear_bwd(host(dy), host(x), host(w), ids, None if y is None else host(y[..., :N]),
