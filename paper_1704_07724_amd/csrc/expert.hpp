@@ -12,6 +12,7 @@ struct ExpertPlan {
     int32_t *tiles;   // the number of row tiles, then from [4] on four words each: expert, first place, rows, 0
     int32_t *pairs;   // P: the pair at each place of the experts' order, -1 where there is none
     int32_t *tokens;  // P: its token, -1 where there is none
+    int32_t *by_size; // E: the experts in the order of weight gradients' tiles (expert_by_size)
 };
 
 struct ExpertArgs {
@@ -62,7 +63,9 @@ struct ExpertBwdBytes {
 ExpertBwdBytes expert_bwd_bytes(int T, int E, int N, int K, int slots, int type, bool shared, bool relu, bool combine);
 
 // Tiles of `rows` rows; `empty`: the pairs' output, of which rows without an expert become 0.
-hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_t ld, int cols, int size, hipStream_t s);
+// by_size: whether the experts' order is made too.
+hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_t ld, int cols, int size, bool by_size,
+                              hipStream_t s);
 // out[t] = the sum over a token's pairs of part's rows, weighted or not.
 hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, const float *weights, void *out,
                              int64_t ldo, int type, hipStream_t s);

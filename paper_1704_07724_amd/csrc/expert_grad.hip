@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void expert_dots_kernel(const ExpertArgs a, co
 }
 
 struct DwArgs {
-    const int32_t *offsets;
+    const int32_t *offsets, *by_size;
     Rows d, x;  // listed by place, or d's in the places' order
     int P, N, K;
     void *dw;
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(TL::kThreads) void expert_dw_kernel(const DwArgs a,
     TL t;
     const auto start = [&](int n) {
         const int id = of_xcd(n, total);
-        Job j{id / (down * across), id / across % down * TL::BI, id % across * TL::BJ, 0};
+        Job j{a.by_size ? a.by_size[id / (down * across)] : id / (down * across), id / across % down * TL::BI, id % across * TL::BJ, 0};
         const int lo = a.offsets[j.e], hi = a.offsets[j.e + 1];
         const int first = lo < 0 ? 0 : lo > a.P ? a.P : lo, end = hi > a.P ? a.P : hi;
         Rows d = a.d, x = a.x;
@@ -187,8 +187,10 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
     const int64_t ldm = expert_ld(a.N);
     const bool aligned_dy = direct_rows(b.dy, b.lddy, a.N, size), aligned_masked = direct_rows(b.masked, ldm, a.N, size);
     const bool direct = (b.y ? aligned_masked : aligned_dy) && direct_rows(a.w, a.ldw, a.K, size);
+    // where every workgroup has tiles of several experts
+    const bool by_size = b.dw && static_cast<int64_t>(a.E) * ((a.N + 255) / 256) * ((a.K + 255) / 256) > 512;
     hipError_t e = launch_expert_plan(a, expert_tile_rows(a.pairs(), a.E, a.K, a.type, direct), b.dx && !sum ? b.dx : nullptr,
-                                      b.lddx, a.K, size, s);
+                                      b.lddx, a.K, size, by_size, s);
     if (e != hipSuccess) return e;
     // a sum's dx takes the gradient as it is (its own sums are weighted), a rectifier's takes it masked
     const bool masks = b.y || (b.combine && b.dw);
@@ -230,7 +232,7 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
         }
     }
     if (!b.dw) return hipSuccess;
-    const DwArgs d{a.offsets,
+    const DwArgs d{a.offsets, by_size ? a.plan.by_size : nullptr,
                    masks ? masked : given,
                    {static_cast<const char *>(a.x), a.ldx * size, a.shared ? a.plan.tokens : a.plan.pairs, 0, a.K},
                    static_cast<int>(a.pairs()), a.N, a.K, b.dw, a.E};

@@ -217,6 +217,27 @@ def test_bwd_by_larger_tiles(torch, isc, dtype, form, many, groups):
         close(host(got.dweights), 2 * many * value, (groups * N + many * K + 64) * E24 * 2 * many * size, "float32", "dweights")
 
 
+@pytest.mark.parametrize("E,K", [(24, 2904), (21, 3104)])
+def test_bwd_of_many_uneven_experts(torch, isc, E, K):
+    """Tiles of experts in the order of their sizes: some without pairs, some of one size, E a multiple of 8 and not."""
+    T, k, N = 300, 3, 304
+    r = np.random.default_rng(E)
+    share = np.where(np.arange(E) % 5 == 1, 0.0, 1.0 + np.arange(E) % 4 * 3)
+    ids = np.stack([r.choice(E, k, replace=False, p=share / share.sum()) for _ in range(T)]).astype(np.int32)
+    offsets, order = train.lists(ids, E)
+    rt = isc.Route(*(torch.from_numpy(v).cuda() for v in (ids, np.ones(ids.shape, np.float32), offsets, order)))
+    x, w = operands(torch, E, T, k, E, K, N, "bfloat16", True)
+    dy = dev(torch, r.standard_normal((T, k, N)), "bfloat16")
+    y = isc.isc_expert_linear(x, w, rt, relu=True)
+    for out in (None, y):
+        got = host(isc.isc_expert_linear_bwd(dy, x, w, rt, y=out, dx=False).dw)
+        d = host(dy) * (1 if out is None else host(out) > 0)
+        for e in range(E):
+            at = ids == e
+            own, rows = d[at], host(x)[np.nonzero(at)[0]]
+            close(got[e], own.T @ rows, (at.sum() + 64) * E24 * (np.abs(own).T @ np.abs(rows)), "bfloat16", "dw of %d" % e)
+
+
 def test_bwd_gradient_against_differences(torch, isc):
     """fp32 differences of the forward pass itself, a step of 2^-6 of it: sums are linear in each operand."""
     T, k, E, K, N = 20, 2, 3, 24, 12
