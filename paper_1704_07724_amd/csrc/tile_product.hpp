@@ -367,11 +367,12 @@ struct Stage {
 // Loads through registers have two stages in LDS.  Direct loads have two of W and three
 // of X (160 KiB for 256 x 256, all of a compute unit's; 80 KiB for 128 x 128, so that
 // two workgroups fit): X's have more than a stage's time to land, W's all of one.
-//   256 x 256, eight wavefronts   a wavefront's 128 x 64 results take 6 operands for 8
-//     products.  4096 tokens of 2048 through 8 of 64 experts of 1408, us a launch: 246 (768
-//     TFLOP/s), by 128 x 128 283; dw of the same 350 and 609; 4 wavefronts of 128 x 128
-//     results, one a SIMD, are 15 % slower, four stages of 32 inner indices 5 %, since half
-//     a line a row is asked for at a time.
+//   256 x 256, eight wavefronts   a wavefront's 128 x 64 results take 12 operands for 32
+//     products.  4096 tokens of 2048 through 8 of 64 experts of 1408, us a launch: 255 (740
+//     TFLOP/s), by 128 x 128, whose rows fit the experts better, 259; dx of the same 260 and
+//     337, dw 315 and 460.  Four wavefronts of 128 x 128 results, one a SIMD, are 15 %
+//     slower, four stages of 32 inner indices 5 %, since half a line a row is asked for at
+//     a time.
 //   LISTED: whose rows across come by a list, X's 1, W's 2.
 //   A stage of 256 x 256 takes 1.8 us with every compute unit busy; what is sent, read and
 //     multiplied in it, without the tile around it, 1.4.
@@ -385,8 +386,8 @@ struct Tile {
     static constexpr int BK = std::is_same_v<T, F32> && BI > 64 ? 32 : BK_;
     // 16 bits go by the smaller instruction, which takes less power for a product.  Power is what
     // bounds a loop of nothing but a stage's products, reads and loads: with all compute
-    // units busy 1.05 us where all operands are alike, on random ones 1.41, by
-    // 32 x 32 x 16 1.62.
+    // units busy 1.41 us on random operands, by 32 x 32 x 16 1.62, and 1.05 by that where all
+    // operands are alike.
     static constexpr bool kSmall = !std::is_same_v<T, F32>;
     static constexpr int kEdge = kSmall ? 16 : 32;  // of an instruction's results
     static constexpr int FI = BI / WI / kEdge, FJ = BJ / WJ / kEdge;
