@@ -20,8 +20,8 @@ namespace {
 
 using namespace tp;
 
-// masked[i] = the gradient of the product of the pair at place i; nothing where it has no
-// expert.  In the places' order, so that the products read consecutive rows.
+// masked[i] = the gradient of the product of the pair at place i, 0 where an expert's place has
+// no pair.  In the places' order, so that the products read consecutive rows.
 template <class T>
 __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b, int64_t ld) {
     const ExpertArgs &a = b.a;
@@ -31,8 +31,10 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; n < all; n += hop) {
         const int64_t i = n / groups, p = a.plan.pairs[i];
         const int c = static_cast<int>(n - i * groups) * 8;
-        if (p >= 0 && static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E)) {
-            float v[8];
+        const bool there = p >= 0 && static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E);
+        if (!there && i >= a.offsets[a.E]) continue;
+        float v[8] = {};
+        if (there) {
             load8<T>(v, static_cast<const V *>(b.dy) + (b.combine ? p / a.slots : p) * b.lddy + c, a.N - c);
             if (b.y) {
                 float y[8];
@@ -45,8 +47,8 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] = c + q < a.N ? v[q] * w : 0.0f;
             }
-            store8<T>(static_cast<V *>(b.masked) + i * ld + c, v, 8);
         }
+        store8<T>(static_cast<V *>(b.masked) + i * ld + c, v, 8);
     }
 }
 

@@ -424,6 +424,32 @@ def test_lists_out_of_range_touch_nothing_else(torch, isc):
         assert torch.equal(got.view(-1, N)[keep], want.view(-1, N)[keep])
 
 
+@pytest.mark.parametrize("form", ["relu", "combine", "plain"])
+def test_a_place_without_a_pair_adds_nothing(torch, isc, form):
+    """Weight gradients of lists with a hole, in a workspace of NaN."""
+    T, k, E, K, N = 60, 2, 3, 64, 72
+    combine = form == "combine"
+    rt, ids = route(torch, isc, 11, T, k, E, 0.1)
+    x, w = operands(torch, 11, T, k, E, K, N, "bfloat16", not combine)
+    dy = dev(torch, np.random.default_rng(12).standard_normal((T, N) if combine else (T, k, N)), "bfloat16")
+    y = isc.isc_expert_linear(x, w, rt, relu=True) if form == "relu" else None
+    order = rt.order.clone()
+    lost = int(order[1])
+    order[1] = 10 ** 9
+    n = ctypes.c_size_t()
+    d = isc.ExpertDesc(E, N, K, 2, k, not combine)
+    assert isc.lib().isc_expert_linear_bwd_workspace_size(d, T, form == "relu", combine, n) == 0
+    ws = torch.full((n.value,), 255, dtype=torch.uint8, device="cuda")
+    got = isc.isc_expert_linear_bwd(dy, x, w, isc.Route(rt.ids, rt.weights, rt.offsets, order), y=y, combine=combine,
+                                    dx=False, dweights=False, ws=ws)
+    ids = ids.copy()
+    ids.reshape(-1)[lost] = -1
+    want = train.expert_linear_bwd(host(dy), host(x), host(w), ids, None if y is None else host(y),
+                                   host(rt.weights) if combine else None)
+    value, size = want["dw"]
+    close(host(got.dw), value, ((T * k + 64) * E24 + (U["bfloat16"] if combine else 0)) * size, "bfloat16", "dw")
+
+
 # ------------------------------------------------------------ orthogonalize --
 
 def gradient(seed, B, M, N, rank):
