@@ -30,6 +30,7 @@ struct OrthShape {
     // Parts in which A's sums over the longer side are made, and added up after: where A has so
     // few tiles that its inner indices in turn are the time.
     __host__ __device__ int parts() const {
+        if (B < 1) return 1;  // an empty stack has no tiles to divide by
         if (small()) {
             const int64_t fours = (span() + 255) / 256;
             return static_cast<int>(fours < 16 ? fours : 16);

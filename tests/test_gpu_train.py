@@ -735,3 +735,11 @@ def test_the_example_runs_and_its_gradients_hold(torch, isc):
     main = runpy.run_path(os.path.join(root, "examples", "trained_experts.py"))["main"]
     # roundings to bfloat16 of the hidden layer, its gradient and the results: four of 2^-8 at most, in the 2-norm
     assert main(["--tokens", "64", "--width", "64", "--hidden", "96", "--experts", "8", "--steps", "3"]) < 4 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("M,N", [(128, 1024), (1024, 128), (777, 1155)])
+def test_an_empty_stack_of_long_matrices(torch, isc, M, N):
+    """Shapes whose sums come in parts."""
+    for dtype in TYPES:
+        got = isc.isc_orthogonalize(torch.empty((0, M, N), dtype=getattr(torch, dtype), device="cuda"))
+        assert got.shape == (0, M, N)

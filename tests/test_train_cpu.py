@@ -220,3 +220,13 @@ def test_orthogonalize_stops_at_what_is_counted(launches):
         ("isc_orthogonalize", [65535, 65536, 65536, 0, a[0], 65536, 1, [1.5, -0.5, 0.0], 1e-7, a[1], 2, 65536, a[2], 1 << 60, None]),
         ("isc_orthogonalize_workspace_size", [65535, 65536, 65536])])
     assert status == size == LIMIT and kernels == []
+
+
+def test_an_empty_stack_of_any_shape(launches):
+    """Nothing is launched and nothing divided by its number, also where A's sums would come in parts."""
+    a = FAR
+    shapes = [(1, 1), (24, 40), (128, 1024), (1024, 128), (65, 449), (777, 1155), (4096, 9216), (65536, 65536)]
+    calls = [("isc_orthogonalize", [0, M, N, 0, a[0], N, 3, [1.5, -0.5, 0.0] * 3, 1e-7, a[1], 2, N, a[2], 1 << 55, None]) for M, N in shapes]
+    sizes = [("isc_orthogonalize_workspace_size", [0, M, N]) for M, N in shapes]
+    for shape, (status, _, kernels) in zip(shapes * 2, launches(calls + sizes)):
+        assert status == 0 and kernels == [], shape
