@@ -632,7 +632,10 @@ int isc_expert_linear_workspace_size(const isc_expert_desc *d, int32_t T, int32_
  *   combine 1: y is T x N, y[t] = sum over j of weights[p] * v[p] (relu has to be 0),
  *     in the slots' order; a pair without an expert adds nothing.
  *   ids, weights, offsets, order: isc_route's, T <= 2^20 tokens (weights may be
- *     NULL unless combine); an id outside [0, E) is an empty slot.
+ *     NULL unless combine); an id outside [0, E) is an empty slot, and so is a pair
+ *     that no place of its expert's, order[offsets[e]] to order[offsets[e + 1] - 1],
+ *     holds.  A place with anything but a pair of its expert's counts for nothing.
+ *     Offsets ascend, and a pair is held once.
  *   y_type: ISC_F32, ISC_F16 or ISC_BF16.
  *   ws: isc_expert_linear_workspace_size bytes, 256-byte aligned.
  * Sums are fp32.  Of fp32 operands, cut into three bfloat16 parts each, six of the

@@ -10,8 +10,9 @@ namespace isc {
 // expert_plan_kernel from a route's lists, with what lies outside of them taken out.
 struct ExpertPlan {
     int32_t *tiles;   // the number of row tiles, then from [4] on four words each: expert, first place, rows, 0
-    int32_t *pairs;   // P: the pair at each place of the experts' order, -1 where there is none
+    int32_t *pairs;   // P: the pair at each place of the experts' order, -1 where it holds none of its expert's
     int32_t *tokens;  // P: its token, -1 where there is none
+    int32_t *places;  // P: a place that holds the pair; anything where none does (expert_listed)
     int32_t *by_size; // E: the experts in the order of weight gradients' tiles (expert_by_size)
 };
 
@@ -62,10 +63,8 @@ struct ExpertBwdBytes {
 };
 ExpertBwdBytes expert_bwd_bytes(int T, int E, int N, int K, int slots, int type, bool shared, bool relu, bool combine);
 
-// Tiles of `rows` rows; `empty`: the pairs' output, of which rows without an expert become 0.
-// by_size: whether the experts' order is made too.
-hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_t ld, int cols, int size, bool by_size,
-                              hipStream_t s);
+// Tiles of `rows` rows.  by_size: whether the experts' order is made too.
+hipError_t launch_expert_plan(const ExpertArgs &a, int rows, bool by_size, hipStream_t s);
 // out[t] = the sum over a token's pairs of part's rows, weighted or not.
 hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, const float *weights, void *out,
                              int64_t ldo, int type, hipStream_t s);
@@ -75,11 +74,27 @@ bool expert_few(int64_t pairs, int E, int type);
 hipError_t launch_expert_few(const ExpertLinearArgs &a, hipStream_t s);
 hipError_t launch_expert_bwd(const ExpertBwdArgs &a, hipStream_t s);
 
+#if defined(__HIPCC__)
+// Whether a place of its expert's holds pair p of P.  Nothing clears `places`, where a pair that
+// no place holds has what was in the workspace: the place that it names does not hold it.
+__device__ __forceinline__ bool expert_listed(const ExpertPlan &plan, int P, int p) {
+    const int i = plan.places[p];
+    return static_cast<unsigned>(i) < static_cast<unsigned>(P) && plan.pairs[i] == p;
+}
+#endif
+
 namespace tp {
+
+// Which rows of the result become 0 of those that no place lists: none, those of pairs that
+// have an expert (the others are not read), or all.
+enum Unlisted { kLeave, kWithExpert, kAll };
 
 // A product over rows by expert: out[pair] = sum over r of X(pair, r) W_e(j, r).
 struct RowsArgs {
     ExpertPlan plan;
+    Unlisted unlisted;
+    const int32_t *ids;
+    int P, E;
     Rows x, w;          // x by the list of places, or its rows in their order; w: the first expert's
     int64_t expert;     // bytes from one expert's matrix to the next
     int inner, cols;    // inner indices, columns of the result
@@ -93,6 +108,31 @@ struct RowsArgs {
     float *dots;
     int ndots;
 };
+
+// The rows of pairs that no place lists, 64 pairs a wavefront in turn.
+template <int WAVES>
+__device__ __forceinline__ void clear_unlisted(const RowsArgs &a) {
+    if (a.unlisted == kLeave) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int size = a.otype == ISC_F32 ? 4 : 2, bytes = a.cols * size, hop = gridDim.x * WAVES;
+    for (int first = (wave * gridDim.x + blockIdx.x) * 64; first < a.P; first += hop * 64) {
+        const int p = first + lane;
+        const bool none = p < a.P && !expert_listed(a.plan, a.P, p) &&
+                          (a.unlisted == kAll || static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E));
+        uint64_t mask = __ballot(none);
+        while (mask) {
+            char *row = static_cast<char *>(a.out) +
+                        (first + __ffsll(static_cast<unsigned long long>(mask)) - 1) * a.ldo * size;
+            mask &= mask - 1;
+            for (int b = lane * 16; b < bytes; b += 1024) {
+                if (b + 16 <= bytes)
+                    store_any(row + b, make_uint4(0, 0, 0, 0));
+                else
+                    for (int c = b; c < bytes; c += 2) store_any(row + c, static_cast<uint16_t>(0));
+            }
+        }
+    }
+}
 
 template <class TL>
 __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArgs a) {
@@ -125,8 +165,9 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
         return j;
     };
     int n = blockIdx.x;
+    if (n < total) job = start(n);
+    clear_unlisted<TL::kWaves>(a);  // while the first tile's loads are on their way
     if (n >= total) return;
-    job = start(n);
     for (bool landed = false;; landed = true) {
         t.sums(a.inner, job.rows, a.cols - job.j0, landed, lds);
         n += gridDim.x;
@@ -168,6 +209,17 @@ __global__ __launch_bounds__(TL::kThreads) void expert_rows_kernel(const RowsArg
         if (n >= total) return;
         job = next;
     }
+}
+
+// The part of a product's arguments that the call's lists make.
+inline RowsArgs rows_of(const ExpertArgs &a, Unlisted unlisted) {
+    RowsArgs r{};
+    r.plan = a.plan;
+    r.unlisted = unlisted;
+    r.ids = a.ids;
+    r.P = static_cast<int>(a.pairs());
+    r.E = a.E;
+    return r;
 }
 
 // Whether a side's rows can go into LDS by direct loads.

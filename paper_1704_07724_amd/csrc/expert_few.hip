@@ -19,6 +19,8 @@ using namespace tp;
 using f32x4 = __attribute__((ext_vector_type(4))) float;
 
 constexpr int kWaves = 4;
+constexpr int kFewEach = 4, kFewEachWide = 8;  // pairs an expert on average, of 16 and of 32 bits
+constexpr int kFewPairs = kFewEachWide * 1024;  // the most that there can be
 
 template <class T>
 struct Few {
@@ -50,14 +52,32 @@ __global__ __launch_bounds__(64 * kWaves) void expert_few_kernel(const ExpertArg
     using V = typename T::type;
     constexpr int kEach = F::kWide ? 1 : 2;  // loads of a lane and step
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int e = blockIdx.y, n0 = blockIdx.x * 16, P = a.T * a.slots;
-    if (e == a.E) {  // the rows of pairs without an expert
-        if (!zeros) return;
-        for (int i = tid; i < P * 16; i += 64 * kWaves) {
-            const int p = i >> 4, n = n0 + (i & 15);
-            if (static_cast<unsigned>(a.ids[p]) >= static_cast<unsigned>(a.E) && n < a.N)
-                store_as(out, p * ldo + n, 0.0f, otype);
+    const int e = static_cast<int>(blockIdx.y) - 1, n0 = blockIdx.x * 16, P = a.T * a.slots;
+    if (e < 0) {  // the rows of pairs that no place of their expert lists become 0
+        // to be summed, only those that have an expert, of which there are none as a rule: one workgroup's
+        if (!zeros && blockIdx.x) return;
+        __shared__ uint32_t kept[kFewPairs / 32];
+        const auto has = [&](int p) { return static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E); };
+        for (int i = tid; i < (P + 31) / 32; i += 64 * kWaves) kept[i] = 32 * i + 32 > P ? ~0u << (P & 31) : 0;
+        __syncthreads();
+        for (int i = tid; i < P; i += 64 * kWaves) {
+            if (!zeros && !has(i)) atomicOr(&kept[i >> 5], 1u << (i & 31));
+            const int p = a.order[i];
+            if (static_cast<unsigned>(p) < static_cast<unsigned>(P) && has(p) && i >= a.offsets[a.ids[p]] &&
+                i < a.offsets[a.ids[p] + 1])
+                atomicOr(&kept[p >> 5], 1u << (p & 31));
         }
+        __syncthreads();
+        if (zeros) {
+            for (int i = tid; i < P * 16; i += 64 * kWaves) {
+                const int p = i >> 4, n = n0 + (i & 15);
+                if (!(kept[p >> 5] >> (p & 31) & 1) && n < a.N) store_as(out, p * ldo + n, 0.0f, otype);
+            }
+            return;
+        }
+        for (int q = 0; q < (P + 31) / 32; ++q)
+            for (uint32_t gone = ~kept[q]; gone; gone &= gone - 1)
+                for (int n = tid; n < a.N; n += 64 * kWaves) store_as(out, (32 * q + __ffs(gone) - 1) * ldo + n, 0.0f, otype);
         return;
     }
     const int lo = a.offsets[e], hi = a.offsets[e + 1];
@@ -71,7 +91,7 @@ __global__ __launch_bounds__(64 * kWaves) void expert_few_kernel(const ExpertArg
     __shared__ f32x4 sums[kWaves - 1][64];
     for (int at = first; at < end; at += 16) {
         const int place = at + (lane & 15);
-        int p = place < end ? a.order[place] : -1;
+        int p = place < end ? a.order[place] : -1, own = -1;
         if (p >= P) p = -1;
         const V *x = static_cast<const V *>(a.x) + (p < 0 ? 0 : a.shared ? p / a.slots : p) * a.ldx;
         f32x4 sum = {0, 0, 0, 0};
@@ -84,6 +104,8 @@ __global__ __launch_bounds__(64 * kWaves) void expert_few_kernel(const ExpertArg
                     const int k = (s + q) * F::kStep + (mine * kEach + i) * 8;
                     wv[q][i].load(w + k, s + q < s1 ? a.K - k : 0);
                 }
+            // asked for in front of x, which is waited for anyway (the 16 tokens' sum 61.2 us, behind x 63.6)
+            if (wave == 0 && s == s0 && p >= 0) own = a.ids[p];
 #pragma unroll
             for (int q = 0; q < F::kAhead; ++q)
 #pragma unroll
@@ -96,10 +118,11 @@ __global__ __launch_bounds__(64 * kWaves) void expert_few_kernel(const ExpertArg
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) sum = F::product(wv[q][i], xv[q][i], sum);
         }
+        if (wave == 0 && s0 >= s1 && p >= 0) own = a.ids[p];
         if (at > first) __syncthreads();  // the sums before are read
         if (wave) sums[wave - 1][lane] = sum;
         __syncthreads();
-        if (wave == 0 && p >= 0) {
+        if (wave == 0 && own == e) {  // a place that holds another's pair counts for nothing
 #pragma unroll
             for (int i = 0; i < kWaves - 1; ++i) sum += sums[i][lane];
             const int n = n0 + 4 * mine;  // results 4 * (l / 16) .. + 4 of column l % 16
@@ -115,11 +138,10 @@ __global__ __launch_bounds__(64 * kWaves) void expert_few_kernel(const ExpertArg
 template <class T>
 hipError_t launch(const ExpertLinearArgs &l, hipStream_t s) {
     const ExpertArgs &a = l.a;
-    const bool zeros = !l.combine;
     hipLaunchKernelGGL(expert_few_kernel<T>,
-                       dim3(static_cast<unsigned>((a.N + 15) / 16), static_cast<unsigned>(a.E + (zeros ? 1 : 0))),
+                       dim3(static_cast<unsigned>((a.N + 15) / 16), static_cast<unsigned>(a.E + 1)),
                        dim3(64 * kWaves), 0, s, a, l.combine ? static_cast<void *>(l.part) : l.y,
-                       l.combine ? expert_ld(a.N) : l.ldy, l.combine ? static_cast<int>(ISC_F32) : l.ytype, l.relu, zeros);
+                       l.combine ? expert_ld(a.N) : l.ldy, l.combine ? static_cast<int>(ISC_F32) : l.ytype, l.relu, !l.combine);
     return hipGetLastError();
 }
 
@@ -128,7 +150,7 @@ hipError_t launch(const ExpertLinearArgs &l, hipStream_t s) {
 // Up to 4 pairs an expert on average, 8 in fp32 (64 experts of 1408 of 2048, 8 a token, us by
 // this kernel and by tiles: 16 tokens 63 and 77, 32 tokens 71 and 83, 64 tokens 85 and 85;
 // fp32 at 64 tokens 183 and 249).
-bool expert_few(int64_t pairs, int E, int type) { return pairs <= (type == ISC_F32 ? 8 : 4) * static_cast<int64_t>(E); }
+bool expert_few(int64_t pairs, int E, int type) { return pairs <= (type == ISC_F32 ? kFewEachWide : kFewEach) * static_cast<int64_t>(E); }
 
 hipError_t launch_expert_few(const ExpertLinearArgs &l, hipStream_t s) {
     const ExpertArgs &a = l.a;

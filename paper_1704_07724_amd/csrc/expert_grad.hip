@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
     for (int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; n < all; n += hop) {
         const int64_t i = n / groups, p = a.plan.pairs[i];
         const int c = static_cast<int>(n - i * groups) * 8;
-        const bool there = p >= 0 && static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E);
+        const bool there = p >= 0;
         if (!there && i >= a.offsets[a.E]) continue;
         float v[8] = {};
         if (there) {
@@ -55,9 +55,10 @@ __global__ __launch_bounds__(256) void expert_mask_kernel(const ExpertBwdArgs b,
 // dweights[p] from its tiles' parts, in their order.
 __global__ __launch_bounds__(256) void expert_dots_kernel(const ExpertArgs a, const float *dots, int n, float *out) {
     const int64_t p = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (p >= static_cast<int64_t>(a.T) * a.slots) return;
+    const int P = a.T * a.slots;
+    if (p >= P) return;
     float sum = 0.0f;
-    if (static_cast<unsigned>(a.ids[p]) < static_cast<unsigned>(a.E))
+    if (expert_listed(a.plan, P, static_cast<int>(p)))
         for (int i = 0; i < n; ++i) sum += dots[p * n + i];
     out[p] = sum;
 }
@@ -191,8 +192,7 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
     const bool direct = (b.y ? aligned_masked : aligned_dy) && direct_rows(a.w, a.ldw, a.K, size);
     // where every workgroup has tiles of several experts
     const bool by_size = b.dw && static_cast<int64_t>(a.E) * ((a.N + 255) / 256) * ((a.K + 255) / 256) > 512;
-    hipError_t e = launch_expert_plan(a, expert_tile_rows(a.pairs(), a.E, a.K, a.type, direct), b.dx && !sum ? b.dx : nullptr,
-                                      b.lddx, a.K, size, by_size, s);
+    hipError_t e = launch_expert_plan(a, expert_tile_rows(a.pairs(), a.E, a.K, a.type, direct), by_size, s);
     if (e != hipSuccess) return e;
     // a sum's dx takes the gradient as it is (its own sums are weighted), a rectifier's takes it masked
     const bool masks = b.y || (b.combine && b.dw);
@@ -203,8 +203,7 @@ hipError_t launch_expert_bwd(const ExpertBwdArgs &b, hipStream_t s) {
     const Rows masked{static_cast<const char *>(b.masked), ldm * size, nullptr, 0, a.N};
     const Rows given{static_cast<const char *>(b.dy), b.lddy * size, b.combine ? a.plan.tokens : a.plan.pairs, 0, a.N};
     if (b.dx || b.dweights) {
-        RowsArgs r{};
-        r.plan = a.plan;
+        RowsArgs r = rows_of(a, !b.dx ? kLeave : sum ? kWithExpert : kAll);
         r.x = b.y ? masked : given;
         r.w = {static_cast<const char *>(a.w), a.ldw * size, nullptr, a.N, a.K};
         r.expert = a.N * a.ldw * size;

@@ -28,9 +28,9 @@ __device__ __forceinline__ int expert_by_size(int rank, int E) {
 }
 
 // Workgroup 0 lists the tiles, with by_size the last one the experts' order; the others make
-// the lists by place, and zero the rows of pairs that have no expert.
-__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const ExpertArgs a, int rows, void *empty,
-                                                                   int64_t ld, int bytes, bool by_size) {
+// the lists by place.  A place holds a pair if it is one of those of the expert that ids
+// gives the pair: whatever `order` says, a row is its own expert's or 0.
+__global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const ExpertArgs a, int rows, bool by_size) {
     const int tid = threadIdx.x;
     const int P = a.T * a.slots;
     if (by_size && blockIdx.x == gridDim.x - 1) {
@@ -93,27 +93,16 @@ __global__ __launch_bounds__(kPlanThreads) void expert_plan_kernel(const ExpertA
         return;
     }
     const int i = (blockIdx.x - 1) * kPlanThreads + tid;
-    bool none = false;
-    if (i < P) {
-        const int p = a.order[i];
-        const bool there = p >= 0 && p < P;
-        a.plan.pairs[i] = there ? p : -1;
-        a.plan.tokens[i] = there ? p / a.slots : -1;
-        none = empty && static_cast<unsigned>(a.ids[i]) >= static_cast<unsigned>(a.E);
+    if (i >= P) return;
+    const int p = a.order[i];
+    bool there = static_cast<unsigned>(p) < static_cast<unsigned>(P);
+    if (there) {
+        const int e = a.ids[p];
+        there = static_cast<unsigned>(e) < static_cast<unsigned>(a.E) && i >= a.offsets[e] && i < a.offsets[e + 1];
     }
-    uint64_t mask = __ballot(none);
-    const int lane = tid & 63;
-    while (mask) {
-        const int64_t p = i - lane + __ffsll(static_cast<unsigned long long>(mask)) - 1;
-        mask &= mask - 1;
-        char *row = static_cast<char *>(empty) + p * ld;
-        for (int b = lane * 16; b < bytes; b += 1024) {
-            if (b + 16 <= bytes)
-                store_any(row + b, make_uint4(0, 0, 0, 0));
-            else
-                for (int c = b; c < bytes; c += 2) store_any(row + c, static_cast<uint16_t>(0));
-        }
-    }
+    a.plan.pairs[i] = there ? p : -1;
+    a.plan.tokens[i] = there ? p / a.slots : -1;
+    if (there) a.plan.places[p] = i;
 }
 
 // Four columns of a token a thread; eight slots' loads in flight.
@@ -139,7 +128,7 @@ __global__ __launch_bounds__(256) void expert_sum_kernel(const ExpertArgs a, con
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (!there[j]) continue;  // a row that nothing wrote
+                if (!there[j]) continue;  // a row that nothing wrote, a weight that may be anything
                 sum.x = fmaf(w[j], v[j].x, sum.x);
                 sum.y = fmaf(w[j], v[j].y, sum.y);
                 sum.z = fmaf(w[j], v[j].z, sum.z);
@@ -179,7 +168,7 @@ bool expert_launches_fit(int64_t pairs, int E, int N, int K, int type) {
 }
 
 size_t expert_plan_bytes(int64_t pairs, int E, int type) {
-    return static_cast<size_t>((16 * (1 + most_tiles(pairs, E)) + 255) / 256 * 256 + (8 * pairs + 255) / 256 * 256 +
+    return static_cast<size_t>((16 * (1 + most_tiles(pairs, E)) + 255) / 256 * 256 + (12 * pairs + 255) / 256 * 256 +
                                (4 * E + 255) / 256 * 256);
 }
 
@@ -188,15 +177,15 @@ ExpertPlan expert_plan_at(void *ws, int64_t pairs, int E, int type) {
     p.tiles = static_cast<int32_t *>(ws);
     p.pairs = past(p.tiles, (16 * (1 + most_tiles(pairs, E)) + 255) / 256 * 256);
     p.tokens = past(p.pairs, 4 * pairs);
-    p.by_size = past(p.pairs, (8 * pairs + 255) / 256 * 256);
+    p.places = past(p.tokens, 4 * pairs);
+    p.by_size = past(p.pairs, (12 * pairs + 255) / 256 * 256);
     return p;
 }
 
-hipError_t launch_expert_plan(const ExpertArgs &a, int rows, void *empty, int64_t ld, int cols, int size, bool by_size,
-                              hipStream_t s) {
+hipError_t launch_expert_plan(const ExpertArgs &a, int rows, bool by_size, hipStream_t s) {
     const int64_t blocks = 1 + (a.pairs() + kPlanThreads - 1) / kPlanThreads + by_size;
-    hipLaunchKernelGGL(expert_plan_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kPlanThreads), 0, s, a, rows, empty,
-                       ld * size, cols * size, by_size);
+    hipLaunchKernelGGL(expert_plan_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kPlanThreads), 0, s, a, rows,
+                       by_size);
     return hipGetLastError();
 }
 
@@ -220,13 +209,11 @@ hipError_t launch_expert_sum(const ExpertArgs &a, const float *part, int cols, c
 hipError_t launch_expert_linear(const ExpertLinearArgs &l, hipStream_t s) {
     const ExpertArgs &a = l.a;
     if (expert_few(a.pairs(), a.E, a.type)) return launch_expert_few(l, s);
-    const int size = a.type == ISC_F32 ? 4 : 2, ysize = l.ytype == ISC_F32 ? 4 : 2;
+    const int size = a.type == ISC_F32 ? 4 : 2;
     const bool direct = tp::direct_rows(a.x, a.ldx, a.K, size) && tp::direct_rows(a.w, a.ldw, a.K, size);
     const int rows = expert_tile_rows(a.pairs(), a.E, a.N, a.type, direct);
-    if (hipError_t e = launch_expert_plan(a, rows, l.combine ? nullptr : l.y, l.ldy, a.N, ysize, false, s); e != hipSuccess)
-        return e;
-    tp::RowsArgs r{};
-    r.plan = a.plan;
+    if (hipError_t e = launch_expert_plan(a, rows, false, s); e != hipSuccess) return e;
+    tp::RowsArgs r = tp::rows_of(a, l.combine ? tp::kWithExpert : tp::kAll);
     r.x = {static_cast<const char *>(a.x), a.ldx * size, a.shared ? a.plan.tokens : a.plan.pairs, 0, a.K};
     r.w = {static_cast<const char *>(a.w), a.ldw * size, nullptr, a.N, a.K};
     r.expert = a.N * a.ldw * size;

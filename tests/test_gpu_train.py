@@ -743,3 +743,84 @@ def test_an_empty_stack_of_long_matrices(torch, isc, M, N):
     for dtype in TYPES:
         got = isc.isc_orthogonalize(torch.empty((0, M, N), dtype=getattr(torch, dtype), device="cuda"))
         assert got.shape == (0, M, N)
+
+
+def listed(ids, offsets, order, E):
+    """ids with -1 for every pair that no place of its own expert's holds."""
+    flat, at = ids.reshape(-1), np.full(ids.size, -1, dtype=ids.dtype)
+    for i, p in enumerate(order):
+        if 0 <= p < flat.size and 0 <= flat[p] < E and offsets[flat[p]] <= i < offsets[flat[p] + 1]:
+            at[p] = flat[p]
+    return at.reshape(ids.shape)
+
+
+def disturbed(torch, isc, what, seed, T, k, E):
+    """A route whose lists and ids do not agree, and the experts that are left."""
+    rt, ids = route(torch, isc, seed, T, k, E, 0.1)
+    ids, order, offsets = ids.copy(), host(rt.order).copy(), host(rt.offsets)
+    weights = host(rt.weights).astype(np.float32)
+    if what == "hole":            # pairs that no place holds
+        order[[0, int(offsets[-1]) - 1]] = (10 ** 9, -1)
+    elif what == "taken away":    # pairs whose expert was taken away after the lists were made
+        for p in order[[0, int(offsets[-1]) - 1]]:
+            ids.reshape(-1)[p] = (-1, E)[p % 2]
+            weights.reshape(-1)[p] = np.nan
+    else:                         # pairs among another expert's
+        order[[0, int(offsets[-1]) - 1]] = order[[int(offsets[-1]) - 1, 0]]
+    left = listed(ids, offsets, order, E)
+    assert 0 < (left >= 0).sum() < (host(rt.ids) >= 0).sum()
+    return isc.Route(*(torch.from_numpy(np.ascontiguousarray(v)).cuda() for v in (ids, weights, offsets, order))), left
+
+
+def nothing_in_it(torch, isc, query, *args):
+    """A workspace of NaN."""
+    n = ctypes.c_size_t()
+    assert getattr(isc.lib(), query)(*args, n) == 0
+    return torch.full((n.value,), 255, dtype=torch.uint8, device="cuda")
+
+
+def leave_nan(torch, *like):
+    """Memory that the next tensors of these sizes take has NaN in it."""
+    for t in [torch.full_like(t, float("nan")) for t in like]:
+        del t
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("what", ["hole", "taken away", "another's"])
+@pytest.mark.parametrize("T,E", [(6, 5), (40, 3), (400, 3)])  # few pairs; tiles of 32 and of 64 rows
+def test_lists_that_ids_do_not_agree_with(torch, isc, T, E, what, dtype):
+    """A pair is computed where its own expert's list has it; the others are empty slots, and nothing that a
+    workspace or an output held before is in a result."""
+    k, K, N = 2, 72, 104
+    code = 0 if dtype == "float32" else 2
+    parts = 8 * (dtype == "float32")
+    rt, left = disturbed(torch, isc, what, 21, T, k, E)
+    weights = np.where(left >= 0, host(rt.weights), 0.0)
+    for shared in (True, False):
+        x, w = operands(torch, 21, T, k, E, K, N, dtype, shared)
+        desc = isc.ExpertDesc(E, N, K, code, k, shared)
+        for form in ("plain", "relu", "combine"):
+            combine, relu = form == "combine", form == "relu"
+            want, size = train.expert_linear(host(x), host(w), left, relu, weights if combine else None)
+            ws = nothing_in_it(torch, isc, "isc_expert_linear_workspace_size", desc, T, combine)
+            leave_nan(torch, x.new_empty(want.shape))
+            got = isc.isc_expert_linear(x, w, rt, relu=relu, combine=combine, ws=ws)
+            close(host(got), want, (K + 64 + k * combine + parts) * E24 * size, dtype, "y")
+            if not combine:
+                assert (host(got)[left < 0] == 0).all()
+            dy = dev(torch, np.random.default_rng(5).standard_normal(want.shape), dtype)
+            ws = nothing_in_it(torch, isc, "isc_expert_linear_bwd_workspace_size", desc, T, relu, combine)
+            leave_nan(torch, x, w, rt.weights)
+            grads = isc.isc_expert_linear_bwd(dy, x, w, rt, y=got if relu else None, combine=combine, ws=ws)
+            want = train.expert_linear_bwd(host(dy), host(x), host(w), left, host(got) if relu else None, weights if combine else None)
+            value, size = want["dx"]
+            close(host(grads.dx), value, (N + 64 + k + parts) * E24 * size, dtype, "dx")
+            value, size = want["dw"]
+            close(host(grads.dw), value, ((T * k + 64 + parts) * E24 + (U[dtype] if combine else 0)) * size, dtype, "dw")
+            if combine:
+                value, size = want["dweights"]
+                close(host(grads.dweights), value, (N + K + 64 + parts) * E24 * size, "float32", "dweights")
+                assert (host(grads.dweights)[left < 0] == 0).all()
+                alone = isc.isc_expert_linear_bwd(dy, x, w, rt, combine=True, dx=False, dw=False,
+                                                  ws=nothing_in_it(torch, isc, "isc_expert_linear_bwd_workspace_size", desc, T, 0, 1))
+                assert torch.equal(alone.dweights, grads.dweights)
