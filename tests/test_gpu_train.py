@@ -19,6 +19,7 @@ import sys
 import numpy as np
 import pytest
 
+import test_oracle_train
 from oracle import train
 
 pytestmark = pytest.mark.gpu
@@ -824,3 +825,17 @@ def test_lists_that_ids_do_not_agree_with(torch, isc, T, E, what, dtype):
                 alone = isc.isc_expert_linear_bwd(dy, x, w, rt, combine=True, dx=False, dw=False,
                                                   ws=nothing_in_it(torch, isc, "isc_expert_linear_bwd_workspace_size", desc, T, 0, 1))
                 assert torch.equal(alone.dweights, grads.dweights)
+
+
+@pytest.mark.parametrize("steps,frobenius,spectral", test_oracle_train.ERRORS)
+@pytest.mark.parametrize("shape", [(64, 64), (64, 300), (100, 100), (130, 64), (200, 300), (520, 600)], ids=str)
+def test_orthogonalize_errs_as_stated(torch, isc, shape, steps, frobenius, spectral):
+    """Against the exact result, by the header's figures beside the rounding to fp16."""
+    g = np.stack(list(test_oracle_train.draws(*shape, 14 if max(shape) < 200 else 3)))
+    got = host(isc.isc_orthogonalize(dev(torch, g), steps=steps, dtype=torch.float16))
+    for o, m in zip(got, g.astype(np.float32)):
+        exact = train.orthogonalize(m, [COEFFICIENTS] * steps, 1e-7)
+        own = U["float16"] * np.linalg.norm(exact) + TINY * o.size ** 0.5
+        off = np.linalg.norm(o - exact)
+        assert off <= frobenius * np.linalg.norm(exact) + own, off / np.linalg.norm(exact)
+        assert np.linalg.norm(o - exact, 2) <= spectral * np.linalg.norm(exact, 2) + own

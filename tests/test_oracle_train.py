@@ -94,3 +94,37 @@ def test_rounded_operands_err_as_stated():
         exact, rounded = (train.orthogonalize(g, [COEFFICIENTS] * 5, 1e-7, v) for v in (False, True))
         err = np.linalg.norm(rounded - exact) / np.linalg.norm(exact)
         assert 1e-5 < err < 2e-3, (M, N, rank, err)
+
+
+# What the rounded operands cost where both sides are 64 or more, of the result's norm, as the header has it: steps,
+# Frobenius norm, 2-norm.  The form below was tried on 70 to 105 matrices of each of eight shapes: 2.7e-3 and 6.0e-3
+# were the most after 5 steps, 4.0e-3 and 2.0e-2 after 8, 3.3e-2 and 0.22 after 16, 6.2e-2 and 0.40 after 64; a half
+# more for others and for other roundings of the same size.
+ERRORS = [(5, 4e-3, 1e-2), (8, 8e-3, 4e-2), (16, 6e-2, 0.4), (64, 0.12, 0.7)]
+
+
+def draws(M, N, seeds):
+    """Noise, and a few strong directions over it, some with rows of unlike lengths."""
+    for seed in range(seeds):
+        r = rng(seed * 7919 + M * 31 + N)
+        rank, noise = [(0, 1), (1, .1), (4, .1), (16, .1), (16, .01), (3, .01), (1, .003)][seed % 7]
+        g = r.standard_normal((M, N)) * noise
+        if rank:
+            g = g + r.standard_normal((M, rank)) @ r.standard_normal((rank, N))
+        yield g * np.exp(r.standard_normal((M, 1)) * 2) if seed % 5 == 4 else g
+
+
+@pytest.mark.parametrize("steps,frobenius,spectral", ERRORS)
+@pytest.mark.parametrize("shape", [(64, 64), (64, 300), (100, 100), (130, 64), (200, 300)], ids=str)
+def test_rounded_operands_err_by_steps(shape, steps, frobenius, spectral):
+    for g in draws(*shape, 21):
+        exact, rounded = (train.orthogonalize(g, [COEFFICIENTS] * steps, 1e-7, v) for v in (False, True))
+        assert np.linalg.norm(rounded - exact) < frobenius * np.linalg.norm(exact)
+        assert np.linalg.norm(rounded - exact, 2) < spectral * np.linalg.norm(exact, 2)
+
+
+def test_small_matrices_err_more():
+    """The figure of large ones is not theirs: 2 x 3 is off by more than 1e-2 after five steps."""
+    most = max(np.linalg.norm(train.orthogonalize(g, [COEFFICIENTS] * 5, 1e-7, True) - exact) / np.linalg.norm(exact)
+               for g in draws(2, 3, 60) for exact in [train.orthogonalize(g, [COEFFICIENTS] * 5, 1e-7)])
+    assert most > 1e-2
