@@ -68,10 +68,9 @@ __device__ __forceinline__ f32x4 mfma_16(s16x8 a, s16x8 b, f32x4 c) {
 // + 16 * lane.  In assembly because the compiler, which cannot tell the stages
 // apart, would wait for it at the next transposing read; it has no output
 // register, and land() waits for it before the barrier in front of its use.  The
-// place is taken from m0, one wait state after it is written; nothing else in the
-// kernels that call this reads m0.
+// place is taken from m0, one wait state after it is written.
 __device__ __forceinline__ void load_direct(const void *p, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "m0", "memory");
 }
 
 // This wavefront's loads have landed, all but the last N, and its LDS reads and writes
