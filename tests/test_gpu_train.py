@@ -839,3 +839,70 @@ def test_orthogonalize_errs_as_stated(torch, isc, shape, steps, frobenius, spect
         off = np.linalg.norm(o - exact)
         assert off <= frobenius * np.linalg.norm(exact) + own, off / np.linalg.norm(exact)
         assert np.linalg.norm(o - exact, 2) <= spectral * np.linalg.norm(exact, 2) + own
+
+
+# Calls by tiles of 128 and 256 that need matrices so wide: 1400 pairs of two experts, K and N given as
+# (inputs, how often they are repeated); the tile's kernel is the one whose name has `kernel`.
+WIDE = {"float32": [("F32ELb0E.*Li128ELi128E", (72, 1), (40, 30))],
+        "bfloat16": [("BF16ELb0E.*Li128ELi128E", (71, 1), (33, 90)), ("BF16ELb1E.*Li128ELi128E", (72, 1), (40, 71)),
+                     ("BF16ELb1E.*Li256ELi256E", (72, 1), (40, 140))],
+        "float16": [("F16ELb0E.*Li128ELi128E", (71, 1), (33, 90)), ("F16ELb1E.*Li128ELi128E", (72, 1), (40, 71)),
+                    ("F16ELb1E.*Li256ELi256E", (72, 1), (40, 140))]}
+WIDE_BWD = {"float32": [("F32ELb0E.*Li128ELi128E", (71, 31), (33, 9))], "bfloat16": [("BF16ELb0E.*Li128ELi128E", (71, 61), (33, 17))],
+            "float16": [("F16ELb0E.*Li128ELi128E", (71, 61), (33, 17))]}
+WIDE_CALL = (700, 2, 2)  # T, k, E
+
+
+@pytest.mark.parametrize("dtype,shape", [(t, s) for t in TYPES for s in WIDE[t]], ids=str)
+@pytest.mark.parametrize("form", ["relu", "combine"])
+def test_linear_of_wide_matrices(torch, isc, dtype, shape, form):
+    """The tiles that no smaller call takes: fp32's of 128, those through registers, sums by all."""
+    (T, k, E), (_, (K, _), (N, groups)), combine = WIDE_CALL, shape, form == "combine"
+    rt, ids = route(torch, isc, 31, T, k, E, 0.05)
+    x, w = operands(torch, 31, T, k, E, K, N, dtype, not combine, combine)
+    got = isc.isc_expert_linear(x, w.repeat(1, groups, 1), rt, relu=not combine, combine=combine)
+    want, size = train.expert_linear(host(x), host(w), ids, not combine, host(rt.weights) if combine else None)
+    close(host(got[..., :N]), want, (K + 64 + k * combine + 8 * (dtype == "float32")) * E24 * size, dtype, "y")
+    assert (got.unflatten(-1, (groups, N)) == got[..., None, :N]).all()
+    if not combine:
+        assert (got[rt.ids < 0] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,shape", [(t, s) for t in TYPES for s in WIDE_BWD[t]], ids=str)
+@pytest.mark.parametrize("form", ["relu", "combine", "plain"])
+def test_bwd_of_wide_matrices(torch, isc, dtype, shape, form):
+    """As above: dx and dw by fp32's tiles of 128, and by those of rows that are off 16 bytes."""
+    (T, k, E), (_, (K, many), (N, groups)), combine = WIDE_CALL, shape, form == "combine"
+    rt, ids = route(torch, isc, 32, T, k, E, 0.05)
+    x, w = operands(torch, 32, T, k, E, K, N, dtype, not combine, combine)
+    dy = dev(torch, np.random.default_rng(33).standard_normal((T, N) if combine else (T, k, N)), dtype)
+    dd = torch.cat([dy] + [torch.zeros_like(dy)] * (groups - 2) + [dy], -1)  # the first and the last group of outputs
+    y = torch.relu(dev(torch, np.random.default_rng(34).standard_normal((T, k, N)), dtype)) if form == "relu" else None
+    got = isc.isc_expert_linear_bwd(dd, x.repeat(*([1] * (x.dim() - 1)), many), w.repeat(1, groups, many), rt,
+                                    y=None if y is None else y.repeat(1, 1, groups), combine=combine)
+    want = train.expert_linear_bwd(host(dy), host(x), host(w), ids, None if y is None else host(y), host(rt.weights) if combine else None)
+    parts = 8 * (dtype == "float32")
+    value, size = want["dx"]
+    dx = got.dx.unflatten(-1, (many, K))
+    close(host(dx[..., 0, :]), 2 * value, (2 * N + 64 + k + parts) * E24 * 2 * size, dtype, "dx")
+    assert (dx == dx[..., :1, :]).all()
+    value, size = want["dw"]
+    dw = got.dw.unflatten(-1, (many, K)).unflatten(1, (groups, N))
+    close(host(dw[:, 0, :, 0]), value, ((T * k + 64 + parts) * E24 + (U[dtype] if combine else 0)) * size
+          + (TINY * T * k * np.abs(host(x)).max() if combine and dtype == "float16" else 0), dtype, "dw")
+    assert (dw[:, 0] == dw[:, 0, :, :1]).all() and (dw[:, -1] == dw[:, 0]).all() and (dw[:, 1:-1] == 0).all()
+    if combine:
+        value, size = want["dweights"]
+        close(host(got.dweights), 2 * many * value, (2 * N + many * K + 64 + parts) * E24 * 2 * many * size, "float32", "dweights")
+
+
+@pytest.mark.parametrize("shape", [(3, 130, 65), (1, 72, 465), (1, 465, 72), (2, 521, 301), (2, 301, 521), (1, 200, 328), (1, 130, 1100)], ids=str)
+def test_orthogonalize_in_a_workspace_of_its_size(torch, isc, shape):
+    """NaN in it and a guard behind its end: matrices by tiles, with sums in parts and without, wide and tall."""
+    ws = nothing_in_it(torch, isc, "isc_orthogonalize_workspace_size", *shape)
+    whole = torch.full((ws.numel() + 4096,), 255, dtype=torch.uint8, device="cuda")
+    for dtype in TYPES:
+        g = dev(torch, gradient(41, *shape, 3), dtype)
+        whole.fill_(255)
+        assert torch.equal(isc.isc_orthogonalize(g, ws=whole[:ws.numel()]), isc.isc_orthogonalize(g))
+        assert (whole[ws.numel():] == 255).all()

@@ -5,12 +5,14 @@ launch takes, up to the limits."""
 import ctypes
 import json
 import os
+import re
 import subprocess
 import sys
 
 import pytest
 
 import paper_1704_07724_amd as isc
+import test_gpu_train as wide
 from test_ffn_launches import RECORDER, ROCM, ROOT
 
 NULL, SHAPE, LIMIT, WORKSPACE, ALIAS, DEVICE, ALIGN, ARG = 1, 2, 3, 4, 5, 7, 9, 10
@@ -230,3 +232,24 @@ def test_an_empty_stack_of_any_shape(launches):
     sizes = [("isc_orthogonalize_workspace_size", [0, M, N]) for M, N in shapes]
     for shape, (status, _, kernels) in zip(shapes * 2, launches(calls + sizes)):
         assert status == 0 and kernels == [], shape
+
+
+def test_the_wide_calls_take_the_tiles_that_they_are_for(launches):
+    """By the names of the kernels that the GPU's tests of wide matrices launch."""
+    (T, k, E), a, code = wide.WIDE_CALL, FAR, {"float32": 0, "float16": 1, "bfloat16": 2}
+    forward, backward = ([(t, *s) for t in wide.TYPES for s in table[t]] for table in (wide.WIDE, wide.WIDE_BWD))
+    calls = []
+    for t, _, (K, _), (N, groups) in forward:
+        for combine in (0, 1):
+            calls.append(("isc_expert_linear", [[E, N * groups, K, code[t], k, 1 - combine], a[0], K, T, a[1], K, a[2], a[3], a[4], a[5],
+                                                a[6], code[t], N * groups, 1 - combine, combine, a[7], 1 << 55, None]))
+    for t, _, (K, many), (N, groups) in backward:
+        for form in ("relu", "combine", "plain"):
+            calls.append(("isc_expert_linear_bwd", [[E, N * groups, K * many, code[t], k, int(form != "combine")], a[0], K * many, T, a[1],
+                                                    K * many, a[2], N * groups, a[3] if form == "relu" else None, N * groups, a[4], a[5],
+                                                    a[6], a[7], int(form == "combine"), a[8], K * many, a[9],
+                                                    a[10] if form == "combine" else None, a[11], 1 << 55, None]))
+    expected = [pattern for _, pattern, _, _ in forward for _ in range(2)] + [pattern for _, pattern, _, _ in backward for _ in range(3)]
+    for pattern, (status, _, kernels) in zip(expected, launches(calls)):
+        names = [name for name, _ in kernels if "expert_rows" in name or "expert_dw" in name]
+        assert status == 0 and names and all(re.search(pattern, name) for name in names), (pattern, names)
