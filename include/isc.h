@@ -638,7 +638,8 @@ int isc_expert_linear_workspace_size(const isc_expert_desc *d, int32_t T, int32_
  *     Offsets ascend, and a pair is held once.
  *   y_type: ISC_F32, ISC_F16 or ISC_BF16.
  *   ws: isc_expert_linear_workspace_size bytes, 256-byte aligned.
- * Sums are fp32.  Of fp32 operands, cut into three bfloat16 parts each, six of the
+ * Sums are fp32.  Up to 8 pairs an expert on average, fp32 operands are multiplied as
+ * they are; of others, cut into three bfloat16 parts each, six of the
  * nine products are kept (the others come to 2^-21 of a term at most, 2^-24 on
  * average), and bits below 2^-133 are lost; an input that is not finite makes the
  * sums that it enters not finite (NaN where fp32 may have an infinity).
@@ -662,7 +663,8 @@ int isc_expert_linear_bwd_workspace_size(const isc_expert_desc *d, int32_t T, in
  *     x is shared; 0 for a pair, or a token, without an expert.
  *   dw: E x N x K consecutive values of d->type, fully written: the sum over an
  *     expert's pairs of d[p] x[p]^T times the pair's weight, 0 for an expert without
- *     pairs.  With combine a weight times dy is rounded to d->type before it is summed.
+ *     pairs.  With combine a weight times dy is rounded to d->type before it is summed
+ *     (in fp16 to a multiple of 2^-24 where it is below 2^-14).
  *   dweights: T*slots floats with combine: v[p] . dy[t], 0 in empty slots.
  *   dx, dw, dweights: NULL where not wanted, one at least given (dweights only with
  *     combine).  ws: isc_expert_linear_bwd_workspace_size bytes, 256-byte aligned.

@@ -1,9 +1,9 @@
 // isc_expert_linear for few pairs an expert: a decoding step's.
 //
-// Each weight is read once and meets a handful of rows, so the time is that of
-// reading the met experts' matrices.  A workgroup takes 16 outputs of an expert and
-// up to 16 of its pairs at a time; its wavefronts share the inputs, and every lane
-// has its weights of 512 inputs on the way at once: neither LDS nor a first launch
+// A weight is read once for every 16 pairs of its expert, which has a handful, so the
+// time is that of reading the met experts' matrices.  A workgroup takes 16 outputs of an
+// expert and up to 16 of its pairs at a time; its wavefronts share the inputs, and every
+// lane has its weights of 512 inputs on the way at once: neither LDS nor a first launch
 // that lists tiles stands in front of the reads.  The lists are read as they are.
 //
 // v_mfma_f32_16x16x32 (16 bits): lane l holds 8 r of row l % 16 of either operand.  Which
@@ -148,8 +148,11 @@ hipError_t launch(const ExpertLinearArgs &l, hipStream_t s) {
 }  // namespace
 
 // Up to 4 pairs an expert on average, 8 in fp32 (64 experts of 1408 of 2048, 8 a token, us by
-// this kernel and by tiles: 16 tokens 63 and 77, 32 tokens 71 and 83, 64 tokens 85 and 85;
-// fp32 at 64 tokens 183 and 249).
+// this kernel and by tiles: 16 tokens 61 and 77, 32 tokens 66 and 83, 64 tokens 85 and 85;
+// fp32 at 64 tokens 171 and 249).  The host knows no more of the lists: where a few experts
+// have all pairs their weights are read over and over, in less time than an even load takes
+// but more than by tiles (512 tokens, 8 of 1024 experts of 512 of 512: even 180 and 107, the
+// same 8 experts for all 97 and 17).
 bool expert_few(int64_t pairs, int E, int type) { return pairs <= (type == ISC_F32 ? kFewEachWide : kFewEach) * static_cast<int64_t>(E); }
 
 hipError_t launch_expert_few(const ExpertLinearArgs &l, hipStream_t s) {
