@@ -788,7 +788,7 @@ def leave_nan(torch, *like):
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("what", ["hole", "taken away", "another's"])
-@pytest.mark.parametrize("T,E", [(6, 5), (40, 3), (400, 3)])  # few pairs; tiles of 32 and of 64 rows
+@pytest.mark.parametrize("T,E", [(6, 5), (25, 20), (160, 81), (40, 3), (400, 3)])  # few pairs; tiles of 32 and of 64 rows
 def test_lists_that_ids_do_not_agree_with(torch, isc, T, E, what, dtype):
     """A pair is computed where its own expert's list has it; the others are empty slots, and nothing that a
     workspace or an output held before is in a result."""
@@ -906,3 +906,30 @@ def test_orthogonalize_in_a_workspace_of_its_size(torch, isc, shape):
         whole.fill_(255)
         assert torch.equal(isc.isc_orthogonalize(g, ws=whole[:ws.numel()]), isc.isc_orthogonalize(g))
         assert (whole[ws.numel():] == 255).all()
+
+
+@pytest.mark.parametrize("what", ["hole", "taken away", "another's"])
+def test_lists_that_ids_do_not_agree_with_by_the_largest_tiles(torch, isc, what):
+    """Rows, sums and dweights by tiles of 256 x 256 are those of lists made for the pairs that are left."""
+    T, k, E, K, N, many = 700, 2, 2, 72, 40, 140
+    rt, left = disturbed(torch, isc, what, 51, T, k, E)
+    offsets, order = train.lists(left, E)
+    clean = isc.Route(*(torch.from_numpy(np.ascontiguousarray(v)).cuda() for v in (left, host(rt.weights).astype(np.float32), offsets, order)))
+    x, w = operands(torch, 51, T, k, E, K, N, "bfloat16", True)
+    wide = w.repeat(1, many, 1)
+    desc = isc.ExpertDesc(E, N * many, K, 2, k, 1)
+    for combine in (False, True):
+        ws = nothing_in_it(torch, isc, "isc_expert_linear_workspace_size", desc, T, combine)
+        leave_nan(torch, x.new_empty((T, N * many) if combine else (T, k, N * many)))
+        assert torch.equal(isc.isc_expert_linear(x, wide, rt, combine=combine, ws=ws),
+                           isc.isc_expert_linear(x, wide, clean, combine=combine))
+    wide = w.repeat(1, 1, many)
+    for shared in (True, False):
+        xx = (x if shared else x[:, None].expand(-1, k, -1)).repeat(*([1] * (1 if shared else 2)), many)
+        desc = isc.ExpertDesc(E, N, K * many, 2, k, shared)
+        dy = dev(torch, np.random.default_rng(52).standard_normal((T, N)), "bfloat16")
+        ws = nothing_in_it(torch, isc, "isc_expert_linear_bwd_workspace_size", desc, T, 0, 1)
+        leave_nan(torch, xx, rt.weights)
+        got = isc.isc_expert_linear_bwd(dy, xx, wide, rt, combine=True, ws=ws)
+        want = isc.isc_expert_linear_bwd(dy, xx, wide, clean, combine=True)
+        assert torch.equal(got.dx, want.dx) and torch.equal(got.dweights, want.dweights)
