@@ -75,14 +75,12 @@ double most_of(double a, double b, double c, double r) {
     const auto look = [&](double square) {
         if (square > 0.0 && square < r * r) most = std::max(most, at(std::sqrt(square)));
     };
-    if (c != 0.0) {
-        const double d = 9.0 * b * b - 20.0 * a * c;
-        if (d >= 0.0) {
-            look((-3.0 * b + std::sqrt(d)) / (10.0 * c));
-            look((-3.0 * b - std::sqrt(d)) / (10.0 * c));
-        }
-    } else if (b != 0.0) {
-        look(-a / (3.0 * b));
+    // the slope's roots by the sum that does not cancel, so that a small c loses neither
+    const double d = 9.0 * b * b - 20.0 * a * c;
+    if (d >= 0.0) {
+        const double t = -(3.0 * b + std::copysign(std::sqrt(d), b));
+        look(t / (10.0 * c));
+        look(2.0 * a / t);
     }
     return most;
 }

@@ -253,3 +253,12 @@ def test_the_wide_calls_take_the_tiles_that_they_are_for(launches):
     for pattern, (status, _, kernels) in zip(expected, launches(calls)):
         names = [name for name, _ in kernels if "expert_rows" in name or "expert_dw" in name]
         assert status == 0 and names and all(re.search(pattern, name) for name in names), (pattern, names)
+
+
+def test_coefficients_whose_largest_value_lies_between():
+    """30 s - 30 s^3 has 11.5 at s^2 = 1/3 whatever little c s^5 is added: twice that is out of range."""
+    for c in (0.0, 1e-20, -1e-20, 1e-12, -1e-12, 1e-6, -1e-6, 1e-3):
+        assert orth(coef=(30.0, -30.0, c) + (1.3, 0, 0)) in OK and orth(coef=(30.0, -30.0, c) + (2.0, 0, 0)) == ARG, c
+        assert orth(coef=(-30.0, 30.0, c) + (1.3, 0, 0)) in OK and orth(coef=(-30.0, 30.0, c) + (2.0, 0, 0)) == ARG, c
+    # s - s^5 has 0.535 at s^4 = 1/5; 30 times that is in range, 31 is not
+    assert orth(coef=(1.0, 0.0, -1.0) + (29.9, 0, 0)) in OK and orth(coef=(1.0, 0.0, -1.0) + (30.0, 0, 0)) == ARG
