@@ -687,14 +687,14 @@ int isc_orthogonalize_workspace_size(int32_t B, int32_t M, int32_t N, size_t *by
  *   o: B*M rows of N values of o_type (ISC_F16 or ISC_BF16), ldo elements apart.
  *   ws: isc_orthogonalize_workspace_size bytes, 256-byte aligned.
  * The state X is held in 32 bits (two fp16 values, 22 significant bits, entries below
- * 2^-41 are 0) and all sums are fp32; the products' operands X, A and b A + c A A are
- * fp16.  Each step multiplies what their roundings leave by the polynomial's slope at the
- * singular values, so o's error, beside its own rounding, depends on the coefficients
- * and grows with the steps.  With (3.4445, -4.775, 2.0315) and both sides 64 or more it is,
- * relative to the exact result in the Frobenius norm, about 2e-3 after 5 steps and below
- * 4e-3 in all that was tried, below 8e-3 after 8, 6e-2 after 16 and 0.12 after 64 (in the
- * 2-norm below 1e-2, 4e-2, 0.4 and 0.7); matrices with fewer rows or columns, whose
- * singular values are few, err several times as much (2 x 3: up to 1.4e-2 after 5 steps).
+ * 2^-41 are 0) and all sums are fp32.  The products' operands X, A and b A + c A A are
+ * fp16, and two such values each where a side is at most 64.  Each step multiplies what
+ * their roundings leave by the polynomial's slope at the singular values, so o's error,
+ * beside its own rounding, depends on the coefficients and grows with the steps.  With
+ * (3.4445, -4.775, 2.0315) it is, relative to the exact result in the Frobenius norm,
+ *   sides from 65 on: about 2e-3 after 5 steps and below 4e-3 in all that was tried, below
+ *     8e-3 after 8, 6e-2 after 16, 0.12 after 64 (2-norm: 1e-2, 4e-2, 0.4 and 0.7),
+ *   a side of at most 64: below 1e-4 after 5 steps and 4e-4 after 8.
  * A matrix with a value that is not finite becomes NaN, one
  * of zeros stays (with eps > 0); others of the stack are not affected.
  * Three launches a step, four where A is small and X long, one where a side is at most

@@ -8,7 +8,7 @@ the terms that it adds up, which the errors of sums are proportional to.
   expert_linear           v[p] = w[e] x[p], rectified, or summed under weights
   expert_linear_bwd       the gradient of sum(dy * y) to x, w and the weights
   orthogonalize           X <- a X + (b A + c A^2) X, exactly, or with the
-                          products' operands rounded to fp16
+                          products' operands rounded to fp16, or to two such parts
 """
 from __future__ import annotations
 
@@ -78,14 +78,22 @@ def _f16(v):
     return v.astype(np.float16).astype(np.float64)
 
 
+def _two(v):
+    """v as an fp16 value and what that leaves, times 2^11, in fp16."""
+    high = _f16(v)
+    return high + _f16((v - high) * 2048) / 2048
+
+
 def orthogonalize(g, coefficients, eps, rounded=False):
-    """One matrix, in its own orientation; rounded: the products' operands in fp16 (times 2^6)."""
+    """One matrix, in its own orientation; rounded: the products' operands in fp16 (times 2^6), or, "parts", in two
+    such values each, and so the state."""
     x = np.asarray(g, dtype=np.float64)
     with np.errstate(all="ignore"):
         x = x / (np.sqrt((x * x).sum()) + eps)
-        r = (lambda v: _f16(64 * v) / 64) if rounded else (lambda v: v)  # noqa: E731
+        r = (lambda v: _two(64 * v) / 64) if rounded == "parts" else (lambda v: _f16(64 * v) / 64) if rounded else (lambda v: v)  # noqa: E731
         for a, b, c in coefficients:
             o = r(x)
+            x = o if rounded == "parts" else x
             s = r(o @ o.T if x.shape[0] <= x.shape[1] else o.T @ o)
             p = r(b * s + c * (s @ s))
             x = a * x + (p @ o if x.shape[0] <= x.shape[1] else o @ p)

@@ -12,7 +12,8 @@
 // in all, read and written with 8 bytes an element and step where fp32 beside the operand
 // takes 10.  The operands of the products, X's first part, A and b A + c A^2, are fp16,
 // whose errors stay where the operand is one factor among fp32 sums: 3.3e-4 of the same
-// result, 1.5e-3 on noise alone, its rounding to bf16 1.7e-3.  Operands are scaled by 2^6
+// result, 1.5e-3 on noise alone, its rounding to bf16 1.7e-3.  (Where a side is at most 64 the
+// operands are in two parts as well: orth_small.hip.)  Operands are scaled by 2^6
 // on their way to fp16, which keeps entries of 2^-14 normal and any that the coefficients'
 // check lets through finite; what they leave by 2^11 more.
 //

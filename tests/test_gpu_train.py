@@ -827,11 +827,9 @@ def test_lists_that_ids_do_not_agree_with(torch, isc, T, E, what, dtype):
                 assert torch.equal(alone.dweights, grads.dweights)
 
 
-@pytest.mark.parametrize("steps,frobenius,spectral", test_oracle_train.ERRORS)
-@pytest.mark.parametrize("shape", [(64, 64), (64, 300), (100, 100), (130, 64), (200, 300), (520, 600)], ids=str)
-def test_orthogonalize_errs_as_stated(torch, isc, shape, steps, frobenius, spectral):
+def errs_as_stated(torch, isc, shape, steps, frobenius, spectral, many):
     """Against the exact result, by the header's figures beside the rounding to fp16."""
-    g = np.stack(list(test_oracle_train.draws(*shape, 14 if max(shape) < 200 else 3)))
+    g = np.stack(list(test_oracle_train.draws(*shape, many)))
     got = host(isc.isc_orthogonalize(dev(torch, g), steps=steps, dtype=torch.float16))
     for o, m in zip(got, g.astype(np.float32)):
         exact = train.orthogonalize(m, [COEFFICIENTS] * steps, 1e-7)
@@ -839,6 +837,19 @@ def test_orthogonalize_errs_as_stated(torch, isc, shape, steps, frobenius, spect
         off = np.linalg.norm(o - exact)
         assert off <= frobenius * np.linalg.norm(exact) + own, off / np.linalg.norm(exact)
         assert np.linalg.norm(o - exact, 2) <= spectral * np.linalg.norm(exact, 2) + own
+
+
+@pytest.mark.parametrize("steps,frobenius,spectral", test_oracle_train.ERRORS)
+@pytest.mark.parametrize("shape", [(65, 65), (65, 300), (100, 100), (130, 66), (200, 300), (520, 600)], ids=str)
+def test_orthogonalize_errs_as_stated(torch, isc, shape, steps, frobenius, spectral):
+    errs_as_stated(torch, isc, shape, steps, frobenius, spectral, 14 if max(shape) < 200 else 3)
+
+
+@pytest.mark.parametrize("steps,frobenius,spectral", test_oracle_train.SMALL_ERRORS)
+@pytest.mark.parametrize("shape", [(1, 1), (2, 2), (2, 3), (3, 5), (5, 3), (1, 40), (8, 8), (16, 300), (500, 32), (64, 64), (64, 300), (130, 64),
+                                   (2100, 64)], ids=str)
+def test_orthogonalize_small_sides_err_as_stated(torch, isc, shape, steps, frobenius, spectral):
+    errs_as_stated(torch, isc, shape, steps, frobenius, spectral, 28 if max(shape) < 200 else 5)
 
 
 # Calls by tiles of 128 and 256 that need matrices so wide: 1400 pairs of two experts, K and N given as
