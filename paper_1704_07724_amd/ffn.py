@@ -577,10 +577,9 @@ def isc_expert_linear(st, x, w, route, relu=False, combine=False, dtype=None, ws
 
     x: [T, K], or [T, k, K] with a row for each slot; w: [E, N, K] in x's type
     (float32, float16, bfloat16); route: isc_route's, with lists.  Returns
-    [T, k, N], slot j by the token's j-th expert (0 where it has none, or where the
-    lists do not hold it), with
-    max(0, .) if relu; with combine [T, N], the sum over a token's slots under
-    the route's weights.  dtype: the output's (default: x's)."""
+    [T, k, N], slot j by the token's j-th expert (0 where it has none, or the lists
+    do not hold it), with max(0, .) if relu; with combine [T, N], the sum over a
+    token's slots under the route's weights.  dtype: the output's (default: x's)."""
     code = _type(st, x.dtype, "x")
     T, slots, E, N, K, xr, ldx, wr, ldw, (ids, weights, offsets, order) = _experts(st, x, w, route)
     device = _device(st, x, w, ids, weights if combine else None, offsets, order, ws)
